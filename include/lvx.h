@@ -255,6 +255,61 @@ lvx_status lvx_xattn_project_bwd(const lvx_projection* p, lvx_dtype dtype, const
                                  int n_out, const void* const* d_out, void* dx, float* dw,
                                  void* hip_stream);
 
+/* ---- around the layer: norms of the token features and their 8-bit checkpoint ----
+ *
+ * The 8-bit form of token features that the activation recomputation keeps instead of them (33 / 64 of their size in
+ * bf16).  The 32 features 32 i .. 32 i + 31 of a token (the last group may be shorter) share an exponent byte e and are
+ * whole numbers of steps,
+ *     x[f] = q[f] * 2^(e[f / 32] - 133),   |q| <= 127,
+ * rounded half to even; e is the biased float32 exponent of the group's largest magnitude, one more where that would round to
+ * 128 steps, and at least 8.  A packed value is off by half a step at most, a 127th of the group's largest magnitude
+ * (of groups below 2^-118: by 2^-126), and is exact in bf16 and in float32.  e = 255: the group holds a NaN, an infinity or a
+ * magnitude of 2^128 (1 - 2^-8) or more, and all of it reads as NaN.
+ * q [n, E] and e [n, (E + 31) / 32], both device, contiguous, any alignment; the struct itself is host memory. */
+typedef struct {
+  int8_t* q;
+  uint8_t* e;
+} lvx_packed;
+/* x: device, n rows of E features of `dtype`, x_ss elements apart (x_ss >= E; any alignment that the type has). */
+lvx_status lvx_pack(int64_t n, int32_t E, int64_t x_ss, lvx_dtype dtype, const void* x, const lvx_packed* to, void* hip_stream);
+lvx_status lvx_unpack(int64_t n, int32_t E, int64_t x_ss, lvx_dtype dtype, const lvx_packed* from, void* x, void* hip_stream);
+
+/* Layer norm of n tokens of E features, or (rms != 0) their root-mean-square norm:
+ *     y[i, f] = (x[i, f] - mu_i) r_i gamma[f] + beta[f],   r_i = 1 / sqrt(mean_f (x[i, f] - mu_i)^2 + eps)
+ * with mu_i the mean over f (rms: 0).
+ * x      device, `dtype`, rows x_ss elements apart, with y, rows y_ss apart, overwritten; y may be x (equal strides).
+ * gamma, beta   device, [E] of `dtype`, contiguous; beta may be NULL (0).
+ * stats  device, [n, 2] float32: mu_i and r_i, overwritten (what lvx_norm_bwd reads).
+ * packed NULL: y is the norm of x.
+ *        With x: x is packed there on the way, and y is the norm of the values that the packed form stands for.  What a
+ *        backward pass makes again from the packed form is then what the forward pass used, bit for bit: K and V agree with
+ *        the saved L, and the probabilities made from them add up to 1.
+ *        With x == NULL: y is the norm of what was packed there before.
+ * Any alignment that the types have, any strides of at least E.  No workspace. */
+typedef struct {
+  int64_t n;                /* tokens */
+  int32_t E, rms;           /* features; 0: layer norm, 1: root-mean-square norm */
+  int64_t x_ss, y_ss;       /* elements from one row to the next of x and dx, of y and dy */
+  float eps;                /* > 0 */
+} lvx_norm;
+lvx_status lvx_norm_fwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const lvx_packed* packed, const void* gamma,
+                        const void* beta, void* y, float* stats, void* hip_stream);
+
+/* Its gradients, with xh = (x - mu) r, a = dy gamma:
+ *     dx = r (a - mean_f(a) - xh mean_f(a xh))  (rms: without mean_f(a)),   dgamma[f] += sum_i dy xh,   dbeta[f] += sum_i dy.
+ * x or packed: exactly one of them, what the forward pass normalised (from packed features dx is the gradient with respect
+ *        to the values that these stand for, that is of x with the rounding passed over).
+ * stats  what lvx_norm_fwd left.
+ * dx     `dtype`, x's strides (x_ss also where x is NULL), OVERWRITTEN; may be dy or x (equal strides); NULL = not wanted.
+ * dgamma, dbeta   float32 [E], contiguous, ACCUMULATED INTO like lvx_xattn_project_bwd's dw (the order of the additions is
+ *        that of the calls, and inside a call fixed: results repeat bit for bit); either may be NULL.
+ * workspace   of lvx_norm_workspace_bytes(n, E) (0: invalid sizes), which also serves fewer tokens and fewer features; NULL
+ *        where neither dgamma nor dbeta is wanted. */
+size_t lvx_norm_workspace_bytes(int64_t n, int32_t E);
+lvx_status lvx_norm_bwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const lvx_packed* packed, const void* gamma,
+                        const float* stats, const void* dy, void* dx, float* dgamma, float* dbeta, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
 /* Human-readable name of a status code (static storage). */
 const char* lvx_strerror(lvx_status s);
 

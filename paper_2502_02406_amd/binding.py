@@ -26,7 +26,8 @@ LVX_BWD_FUSED, LVX_BWD_SPLIT = 8, 16
 LVX_STATIC_SCRATCH_BYTES = 64 << 20
 
 EXPORTS = ("lvx_xattn_workspace_bytes", "lvx_xattn_fwd", "lvx_xattn_fwd_static", "lvx_xattn_fwd_merge", "lvx_xattn_fwd_merge_last", "lvx_xattn_merge", "lvx_xattn_bwd",
-           "lvx_xattn_bwd_stages", "lvx_xattn_bwd_visit", "lvx_xattn_bwd_error_word", "lvx_xattn_dq_finalize", "lvx_xattn_project", "lvx_xattn_project_bwd", "lvx_strerror")
+           "lvx_xattn_bwd_stages", "lvx_xattn_bwd_visit", "lvx_xattn_bwd_error_word", "lvx_xattn_dq_finalize", "lvx_xattn_project", "lvx_xattn_project_bwd",
+           "lvx_pack", "lvx_unpack", "lvx_norm_fwd", "lvx_norm_workspace_bytes", "lvx_norm_bwd", "lvx_strerror")
 
 
 class LvxError(RuntimeError):
@@ -52,6 +53,15 @@ class lvx_mask(C.Structure):
 class lvx_projection(C.Structure):
     _fields_ = [("B", C.c_int32), ("S", C.c_int32), ("E", C.c_int32), ("H", C.c_int32),
                 ("D", C.c_int32), ("x_sb", C.c_int64), ("x_ss", C.c_int64)]
+
+
+class lvx_norm(C.Structure):
+    _fields_ = [("n", C.c_int64), ("E", C.c_int32), ("rms", C.c_int32), ("x_ss", C.c_int64), ("y_ss", C.c_int64),
+                ("eps", C.c_float)]
+
+
+class lvx_packed(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("e", C.c_void_p)]
 
 
 _lib = None
@@ -105,6 +115,15 @@ def load() -> C.CDLL:
         lib.lvx_xattn_project_bwd.argtypes = [C.POINTER(lvx_projection), C.c_int, C.c_void_p, C.c_void_p,
                                               C.c_int, C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p,
                                               C.c_void_p]
+        lib.lvx_pack.restype = lib.lvx_unpack.restype = lib.lvx_norm_fwd.restype = lib.lvx_norm_bwd.restype = C.c_int
+        lib.lvx_pack.argtypes = [C.c_int64, C.c_int32, C.c_int64, C.c_int, C.c_void_p, C.POINTER(lvx_packed), C.c_void_p]
+        lib.lvx_unpack.argtypes = [C.c_int64, C.c_int32, C.c_int64, C.c_int, C.POINTER(lvx_packed), C.c_void_p, C.c_void_p]
+        lib.lvx_norm_fwd.argtypes = [C.POINTER(lvx_norm), C.c_int, C.c_void_p, C.POINTER(lvx_packed), C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.lvx_norm_workspace_bytes.restype = C.c_size_t
+        lib.lvx_norm_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
+        lib.lvx_norm_bwd.argtypes = [C.POINTER(lvx_norm), C.c_int, C.c_void_p, C.POINTER(lvx_packed)] + [C.c_void_p] * 7 + \
+                                    [C.c_size_t, C.c_void_p]
         lib.lvx_strerror.restype = C.c_char_p
         lib.lvx_strerror.argtypes = [C.c_int]
         _lib = lib
@@ -363,3 +382,121 @@ def lvx_xattn_project_bwd(x, w, d_outs, dx=None, dw=None) -> None:
                                         len(d_outs), arr, dx.data_ptr() if dx is not None else None,
                                         dw.data_ptr() if dw is not None else None, _stream())
     _check(code, "lvx_xattn_project_bwd")
+
+
+# ---- around the layer: norms of the token features, their 8-bit checkpoint ----
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _on_device(where: str, *ts) -> None:
+    """Every tensor lies on the device whose stream the call goes to."""
+    at = torch.cuda.current_device() if torch.cuda.is_available() else None
+    if not all(t.is_cuda and t.device.index == at for t in ts if t is not None):
+        raise RuntimeError(f"{where} needs tensors of the current device")
+
+
+def _token_rows(t, name: str):
+    """(tokens, features, elements from one token to the next) of t [n, E] or [B, S, E] (features contiguous, batches that
+    follow each other)."""
+    _need(t.dim() in (2, 3) and (t.stride(-1) == 1 or t.shape[-1] == 1), f"{name} has to be [n, E] or [B, S, E] with contiguous features")
+    E, S = t.shape[-1], t.shape[-2]
+    n = t.numel() // E if E else 0
+    if t.dim() == 3 and t.shape[0] > 1 and S > 1:
+        _need(t.stride(0) == S * t.stride(1), f"{name}: the batches have to follow each other")
+    if t.dim() == 3 and S == 1:
+        return n, E, t.stride(0) if t.shape[0] > 1 else E
+    return n, E, t.stride(-2) if n > 1 else E
+
+
+class Packed:
+    """The 8-bit form of n tokens x E features (lvx_packed): whole numbers of steps, and an exponent byte for every 32 features."""
+
+    def __init__(self, n: int, E: int, device="cuda"):
+        self.q = torch.empty((n, E), dtype=torch.int8, device=device)
+        self.e = torch.empty((n, (E + 31) // 32), dtype=torch.uint8, device=device)
+
+    def rows(self, first: int, last: int) -> "Packed":
+        """Tokens first .. last - 1, as a view."""
+        p = Packed.__new__(Packed)
+        p.q, p.e = self.q[first:last], self.e[first:last]
+        return p
+
+    @property
+    def shape(self):
+        return self.q.shape
+
+    def _struct(self, where: str, n: int, E: int) -> lvx_packed:
+        _need(tuple(self.q.shape) == (n, E) and tuple(self.e.shape) == (n, (E + 31) // 32), f"{where}: packed has to hold [{n}, {E}]")
+        _need(self.q.is_contiguous() and self.e.is_contiguous() and self.q.dtype == torch.int8 and self.e.dtype == torch.uint8,
+              f"{where}: packed has to be contiguous int8 and uint8")
+        _on_device(where, self.q, self.e)
+        return lvx_packed(self.q.data_ptr(), self.e.data_ptr())
+
+
+def lvx_pack(x, packed: Packed) -> None:
+    """packed is overwritten with the 8-bit form of x [n, E] or [B, S, E]."""
+    _on_device("lvx_pack", x)
+    n, E, ss = _token_rows(x, "x")
+    _check(load().lvx_pack(n, E, ss, dtype_code(x.dtype), x.data_ptr(), C.byref(packed._struct("lvx_pack", n, E)), _stream()), "lvx_pack")
+
+
+def lvx_unpack(packed: Packed, x) -> None:
+    """x [n, E] or [B, S, E] is overwritten with the values that packed stands for."""
+    _on_device("lvx_unpack", x)
+    n, E, ss = _token_rows(x, "x")
+    _check(load().lvx_unpack(n, E, ss, dtype_code(x.dtype), C.byref(packed._struct("lvx_unpack", n, E)), x.data_ptr(), _stream()), "lvx_unpack")
+
+
+def _norm_struct(where, like_x, like_y, gamma, stats, rms, eps):
+    """Sizes and strides of a norm call; like_x: x or dx or None (features that exist packed only)."""
+    n, E, y_ss = _token_rows(like_y, "y")
+    x_ss = E
+    if like_x is not None:
+        nx, Ex, x_ss = _token_rows(like_x, "x")
+        _need((nx, Ex) == (n, E), f"{where}: x and y differ in shape")
+        _need(like_x.dtype == like_y.dtype, f"{where}: x and y differ in type")
+    _need(tuple(gamma.shape) == (E,) and gamma.is_contiguous() and gamma.dtype == like_y.dtype, f"{where}: gamma has to be [{E}] of y's type")
+    _need(stats.numel() == 2 * n and stats.is_contiguous() and stats.dtype == torch.float32, f"{where}: stats has to be float32 [{n}, 2]")
+    return lvx_norm(n, E, int(bool(rms)), x_ss, y_ss, float(eps))
+
+
+def lvx_norm_fwd(x, gamma, beta, y, stats, rms: bool = False, eps: float = 1e-5, packed: Optional[Packed] = None) -> None:
+    """y ([n, E] or [B, S, E]; may be x) and stats (float32 [n, 2]) are overwritten with the norm of x and its (mean, 1 / spread).
+    With packed: x is packed there and y is the norm of the packed values; with x None, of what was packed there before."""
+    w = "lvx_norm_fwd"
+    _need(x is not None or packed is not None, f"{w}: neither x nor packed")
+    _on_device(w, x, gamma, beta, y, stats)
+    p = _norm_struct(w, x, y, gamma, stats, rms, eps)
+    _need(beta is None or tuple(beta.shape) == (p.E,) and beta.is_contiguous() and beta.dtype == y.dtype, f"{w}: beta has to be [{p.E}] of y's type")
+    pk = packed._struct(w, p.n, p.E) if packed is not None else None
+    _check(load().lvx_norm_fwd(C.byref(p), dtype_code(y.dtype), x.data_ptr() if x is not None else None, C.byref(pk) if pk is not None else None,
+                               gamma.data_ptr(), beta.data_ptr() if beta is not None else None, y.data_ptr(), stats.data_ptr(), _stream()), w)
+
+
+def lvx_norm_workspace_bytes(n: int, E: int) -> int:
+    return int(load().lvx_norm_workspace_bytes(n, E))
+
+
+def lvx_norm_bwd(x, gamma, stats, d_y, dx=None, dgamma=None, dbeta=None, workspace=None, rms: bool = False, eps: float = 1e-5,
+                 packed: Optional[Packed] = None) -> None:
+    """The gradients of lvx_norm_fwd, from x or (x None) from what was packed.  dx (x's shape, strides and type; may be x or d_y) is
+    overwritten, dgamma and dbeta (float32 [E]) are added to; any of the three may be None."""
+    w = "lvx_norm_bwd"
+    _need((x is None) != (packed is None), f"{w}: x or packed, one of them")
+    _need(dx is not None or dgamma is not None or dbeta is not None, f"{w}: nothing asked for")
+    _on_device(w, x, gamma, stats, d_y, dx, dgamma, dbeta, workspace)
+    p = _norm_struct(w, x if x is not None else dx, d_y, gamma, stats, rms, eps)
+    if dx is not None:
+        _need(dx.shape == d_y.shape and dx.dtype == d_y.dtype, f"{w}: dx and d_y differ in shape or type")
+        _need(x is None or _token_rows(dx, "dx")[2] == p.x_ss, f"{w}: dx has to have x's strides")
+    for t, name in ((dgamma, "dgamma"), (dbeta, "dbeta")):
+        _need(t is None or tuple(t.shape) == (p.E,) and t.is_contiguous() and t.dtype == torch.float32, f"{w}: {name} has to be float32 [{p.E}]")
+    _need(workspace is None or workspace.is_contiguous(), f"{w}: the workspace has to be contiguous")
+    pk = packed._struct(w, p.n, p.E) if packed is not None else None
+    at = lambda t: t.data_ptr() if t is not None else None
+    _check(load().lvx_norm_bwd(C.byref(p), dtype_code(d_y.dtype), at(x), C.byref(pk) if pk is not None else None, gamma.data_ptr(),
+                               stats.data_ptr(), d_y.data_ptr(), at(dx), at(dgamma), at(dbeta), at(workspace),
+                               workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), w)

@@ -8,12 +8,7 @@
 
 using namespace lvx;
 
-namespace {
-
-constexpr size_t ALIGN = 256;
-constexpr bool FUSED_BY_DEFAULT = false;   // lvx_xattn_bwd: one fused kernel where it applies, else dK/dV + dQ kernels
-inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
-
+namespace lvx {
 int device_cu_count() {
   static int n = 0;
   if (n == 0) {
@@ -26,6 +21,13 @@ int device_cu_count() {
   }
   return n;
 }
+}  // namespace lvx
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+constexpr bool FUSED_BY_DEFAULT = false;   // lvx_xattn_bwd: one fused kernel where it applies, else dK/dV + dQ kernels
+inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 
 lvx_status check_problem(const lvx_problem* p, lvx_dtype dtype) {
   if (!p) return LVX_ERR_NULL;

@@ -176,6 +176,31 @@ struct ProjBwdArgs {
 bool project_bwd_bf16_supported(const ProjBwdArgs& a);   // shapes the matrix-core kernels take
 hipError_t launch_project_bwd(const ProjBwdArgs& a, int is_f32, hipStream_t s);
 
+// Norms of token features, their gradients, and the packed form of what they read (lvx_packed.h).
+struct NormArgs {
+  const void* x;        // [n, E], row stride x_ss elements; null: the packed form is read
+  int8_t* q;            // the packed form: [n, E] and [n, groups] contiguous, or null.  With x: written (forward)
+  uint8_t* b;
+  const void *gamma, *beta;     // [E]; beta may be null
+  void* y;              // [n, E], row stride y_ss
+  float* stats;         // [n, 2]: mean, 1 / spread
+  const float* stats_in;
+  const void* dy;       // like y
+  void* dx;             // like x, or null
+  float *dgamma, *dbeta;        // [E], added to, or null
+  float* part;          // workspace, [parts, 2, E]
+  long n, x_ss, y_ss;
+  int E, rms, n_cu, parts;
+  float eps;
+};
+int norm_parts(long n, int E);          // partial sums of dgamma and dbeta: no more with fewer rows or features
+hipError_t launch_norm_fwd(const NormArgs& a, int is_f32, hipStream_t s);
+hipError_t launch_norm_bwd(const NormArgs& a, int is_f32, hipStream_t s);
+hipError_t launch_pack(const NormArgs& a, int is_f32, hipStream_t s);
+hipError_t launch_unpack(const NormArgs& a, int is_f32, hipStream_t s);     // to y
+
+int device_cu_count();   // of the first device asked for (256 where there is none)
+
 // Bytes of workspace that lvx_xattn_fwd needs for exactly this call (with this mask or without
 // one; lvx_xattn_workspace_bytes returns the larger of the two cases) when it is given `room`; 0 for
 // invalid arguments.

@@ -1,0 +1,305 @@
+"""Norms of token features, their gradients and the 8-bit checkpoint through the C ABI, against float64.
+
+Tolerances, from the arithmetic.  A float32 sum of m terms in chains of at most c, joined by a tree, is off by at most
+(c + log2 m) 2^-24 times the sum of the terms' magnitudes; the chains here have at most E / 64 terms along a row and n / 256 + 48
+along the rows (a part of the rows each, then the parts), so with every product's and difference's own 2^-24
+    k = (E / 64 + 24) 2^-24,  kn = (n / 256 + 64) 2^-24
+cover them.  d(mu) <= k mean|x|;  d(r) <= 2 k r;  xh = (x - mu) r is off by exh = k r mean|x| + 4 k |xh|;  the rest follows from
+the formulas.  A bf16 result is off by another half step, 2^-8 of its value."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_02406_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+EPS = 1e-5
+
+
+def inputs(n, E, dtype, seed, pad=0):
+    g = torch.Generator().manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, generator=g)
+    x = rnd(n, E) * torch.exp(0.5 * rnd(E)) + 0.5 * rnd(E)
+    x[0] += 30.0                                        # a mean that is large against the spread
+    if n > 2:
+        x[2] = 3.25                                     # no spread at all
+    if n > 4:
+        x[4] = 0.0
+    dev = lambda t: t.to(DT[dtype]).cuda()
+    buf = torch.full((n + 1, E + pad), 77.0, dtype=DT[dtype], device="cuda")
+    buf[:n, :E] = dev(x)
+    return buf, dev(1.0 + 0.2 * rnd(E)), dev(0.3 * rnd(E)), dev(rnd(n, E))
+
+
+def unpacked64(p):
+    q, e = p.q.cpu().numpy().astype(np.float64), p.e.cpu().numpy().astype(np.float64)
+    return q * np.repeat(2.0 ** (e - 133.0), 32, axis=1)[:, :q.shape[1]]
+
+
+def reference(x, gamma, beta, d_y, rms):
+    n, E = x.shape
+    mu = np.zeros(n) if rms else x.mean(1)
+    r = 1.0 / np.sqrt(((x - mu[:, None]) ** 2).mean(1) + EPS)
+    xh = (x - mu[:, None]) * r[:, None]
+    a = d_y * gamma
+    dx = r[:, None] * (a - (0.0 if rms else a.mean(1, keepdims=True)) - xh * (a * xh).mean(1, keepdims=True))
+    return dict(y=xh * gamma + beta, stats=np.stack([mu, r], 1), dx=dx, dgamma=(d_y * xh).sum(0), dbeta=d_y.sum(0), xh=xh, a=a, r=r)
+
+
+def bounds(x, gamma, beta, d_y, ref, dtype):
+    n, E = x.shape
+    k, kn = (E / 64 + 24) * 2.0 ** -24, (n / 256 + 64) * 2.0 ** -24
+    half = 2.0 ** -8 if dtype == "bf16" else 0.0
+    r, xh, a = ref["r"][:, None], np.abs(ref["xh"]), np.abs(ref["a"])
+    mx = np.abs(x).mean(1, keepdims=True)
+    exh = k * r * mx + 4 * k * xh
+    m = (a * xh).mean(1, keepdims=True)
+    e_m = (a * exh).mean(1, keepdims=True) + k * m
+    return dict(y=half * np.abs(ref["y"]) + exh * np.abs(gamma) + k * np.abs(beta) + 2 * k * xh * np.abs(gamma),
+                stats=np.stack([k * mx[:, 0], 2 * k * ref["r"]], 1) + 1e-30,
+                dx=half * np.abs(ref["dx"]) + r * (k * (a + a.mean(1, keepdims=True) + 4 * xh * m) + exh * m + xh * e_m) + 1e-30,
+                dgamma=(np.abs(d_y) * exh).sum(0) + kn * (np.abs(d_y) * xh).sum(0) + 1e-30, dbeta=kn * np.abs(d_y).sum(0) + 1e-30)
+
+
+def check(got, ref, bound, tag):
+    for name, t in got.items():
+        g = t.double().cpu().numpy()
+        assert np.isfinite(g).all(), f"{tag} {name}: not finite"
+        # (bf16: the half step belongs to the value before rounding, which may lie on the far side of the reference)
+        worst = (np.abs(g - ref[name]) / (bound[name] * 1.01 + 1e-35)).max()
+        assert worst <= 1.0, f"{tag} {name}: off by {worst:.3g} of the bound"
+
+
+SIZES = [(1, 1), (1, 31), (3, 33), (5, 64), (70, 200), (33, 1001), (130, 768), (19, 1024), (300, 512), (2, 1032), (17, 4096), (6, 6144),
+         (9, 8192), (3, 8193), (5, 16384), (3, 20001), (700, 96), (2100, 40)]
+
+
+@pytest.mark.parametrize("source", ["x", "keep"])
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,E", SIZES)
+def test_norm_and_gradients(n, E, dtype, rms, source):
+    pad = (0, 8, 1)[(n + E) % 3]
+    buf, gamma, beta, d_y = inputs(n, E, dtype, 10 * n + E, pad)
+    x = buf[:n, :E]
+    pk = B.Packed(n, E) if source == "keep" else None
+    y = torch.full((n + 1, E + pad), 55.0, dtype=x.dtype, device="cuda")
+    dx = torch.full((n + 1, E + pad), 55.0, dtype=x.dtype, device="cuda")
+    stats = torch.full((n, 2), float("nan"), device="cuda")
+    dgamma, dbeta = torch.full((E,), 2.0, device="cuda"), torch.full((E,), -1.0, device="cuda")
+    ws = torch.full((B.lvx_norm_workspace_bytes(n, E),), 255, dtype=torch.uint8, device="cuda")
+    B.lvx_norm_fwd(x, gamma, beta, y[:n, :E], stats, rms=rms, eps=EPS, packed=pk)
+    first = y[:n, :E].clone()
+    if pk is not None:                                  # the norm made again: the same bits
+        again, stats2 = torch.empty_like(first), torch.empty_like(stats)
+        B.lvx_norm_fwd(None, gamma, beta, again, stats2, rms=rms, eps=EPS, packed=pk)
+        assert torch.equal(again, first) and torch.equal(stats, stats2)
+    B.lvx_norm_bwd(x if pk is None else None, gamma, stats, d_y, dx[:n, :E], dgamma, dbeta, ws, rms=rms, packed=pk)
+    torch.cuda.synchronize()
+    for t in (y, dx, buf):                              # what lies between and behind the rows
+        assert (t[n:] == t[n, 0]).all() and (t[:, E:] == t[n, 0]).all()
+    x64 = x.double().cpu().numpy() if pk is None else unpacked64(pk)
+    g64, b64, d64 = (t.double().cpu().numpy() for t in (gamma, beta, d_y))
+    ref = reference(x64, g64, b64, d64, rms)
+    bound = bounds(x64, g64, b64, d64, ref, dtype)
+    bound["dgamma"] += 2.0 ** -23 * (2 + np.abs(ref["dgamma"]))
+    bound["dbeta"] += 2.0 ** -23 * (1 + np.abs(ref["dbeta"]))
+    check(dict(y=y[:n, :E], stats=stats, dx=dx[:n, :E], dgamma=dgamma.double() - 2.0, dbeta=dbeta.double() + 1.0), ref, bound, f"{n}x{E} {dtype}")
+
+
+def test_norm_gradient_by_differences():
+    """float64 central differences of loss = sum(y w) through the definition, for x, gamma and beta."""
+    for rms in (False, True):
+        buf, gamma, beta, d_y = inputs(3, 24, "f32", 5)
+        x = buf[:3, :24]
+        y, stats, dx = torch.empty_like(d_y), torch.empty((3, 2), device="cuda"), torch.empty_like(d_y)
+        dgamma, dbeta = torch.zeros(24, device="cuda"), torch.zeros(24, device="cuda")
+        ws = torch.empty(B.lvx_norm_workspace_bytes(3, 24), dtype=torch.uint8, device="cuda")
+        B.lvx_norm_fwd(x, gamma, beta, y, stats, rms=rms, eps=0.1)
+        B.lvx_norm_bwd(x, gamma, stats, d_y, dx, dgamma, dbeta, ws, rms=rms, eps=0.1)
+        x64, g64, b64, d64 = (t.double().cpu().numpy() for t in (x, gamma, beta, d_y))
+
+        def loss(xv, gv, bv):
+            mu = 0.0 if rms else xv.mean(1, keepdims=True)
+            return float((((xv - mu) / np.sqrt(((xv - mu) ** 2).mean(1, keepdims=True) + 0.1) * gv + bv) * d64).sum())
+
+        h = 1e-5
+        for i in range(3):
+            for e in range(24):
+                up, dn = x64.copy(), x64.copy()
+                up[i, e] += h
+                dn[i, e] -= h
+                # (differences: h^2 third derivatives ~ 1e-9, cancellation 1e-16 * 100 / 1e-5 = 1e-9; float32 results ~ 1e-5)
+                assert abs((loss(up, g64, b64) - loss(dn, g64, b64)) / (2 * h) - float(dx[i, e])) <= 1e-4
+        for e in range(24):
+            up, dn = g64.copy(), g64.copy()
+            up[e] += h
+            dn[e] -= h
+            assert abs((loss(x64, up, b64) - loss(x64, dn, b64)) / (2 * h) - float(dgamma[e])) <= 1e-4
+            assert abs(d64[:, e].sum() - float(dbeta[e])) <= 1e-5
+
+
+def test_norm_in_place_and_parts_left_out():
+    for n, E, dtype in ((40, 512, "bf16"), (7, 77, "f32"), (5, 20000, "bf16")):
+        buf, gamma, beta, d_y = inputs(n, E, dtype, 3)
+        x = buf[:n]
+        y, stats, dx = torch.empty_like(d_y), torch.empty((n, 2), device="cuda"), torch.empty_like(d_y)
+        dgamma, dbeta = torch.zeros(E, device="cuda"), torch.zeros(E, device="cuda")
+        ws = torch.empty(B.lvx_norm_workspace_bytes(n, E), dtype=torch.uint8, device="cuda")
+        B.lvx_norm_fwd(x, gamma, None, y, stats)
+        B.lvx_norm_bwd(x, gamma, stats, d_y, dx, dgamma, dbeta, ws)
+        own = x.clone()
+        B.lvx_norm_fwd(own, gamma, None, own, torch.empty_like(stats))
+        assert torch.equal(own, y)
+        zero = torch.empty_like(y)
+        B.lvx_norm_fwd(x, gamma, torch.zeros_like(beta), zero, torch.empty_like(stats))
+        assert torch.equal(zero, y)
+        for place in ("dy", "x"):
+            g2, b2, o = torch.zeros_like(dgamma), torch.zeros_like(dbeta), (d_y if place == "dy" else x).clone()
+            B.lvx_norm_bwd(x if place == "dy" else o, gamma, stats, o if place == "dy" else d_y, o, g2, b2, ws)
+            assert torch.equal(o, dx) and torch.equal(g2, dgamma) and torch.equal(b2, dbeta), place
+        only = torch.empty_like(dx)
+        B.lvx_norm_bwd(x, gamma, stats, d_y, only)
+        assert torch.equal(only, dx)
+        for a, b in ((True, False), (False, True)):
+            g2, b2 = torch.zeros_like(dgamma), torch.zeros_like(dbeta)
+            B.lvx_norm_bwd(x, gamma, stats, d_y, None, g2 if a else None, b2 if b else None, ws)
+            assert torch.equal(g2, dgamma if a else torch.zeros_like(g2)) and torch.equal(b2, dbeta if b else torch.zeros_like(b2))
+
+
+def test_norm_nan_stays_in_its_row():
+    for E, dtype in ((512, "bf16"), (4096, "bf16"), (300, "f32"), (77, "bf16")):
+        buf, gamma, beta, d_y = inputs(9, E, dtype, 8)
+        x, y, stats, dx = buf[:9], torch.empty_like(d_y), torch.empty((9, 2), device="cuda"), torch.empty_like(d_y)
+        B.lvx_norm_fwd(x, gamma, beta, y, stats)
+        B.lvx_norm_bwd(x, gamma, stats, d_y, dx)
+        bad = x.clone()
+        bad[1, E // 2], bad[6, 0] = float("nan"), float("inf")
+        y2, dx2, s2, pk = torch.empty_like(y), torch.empty_like(dx), torch.empty_like(stats), B.Packed(9, E)
+        for packed in (None, pk):
+            B.lvx_norm_fwd(bad, gamma, beta, y2, s2, packed=packed)
+            B.lvx_norm_bwd(bad if packed is None else None, gamma, s2, d_y, dx2, packed=packed)
+            rest = [0, 2, 3, 4, 5, 7, 8]
+            assert y2[[1, 6]].isnan().all() and dx2[[1, 6]].isnan().all()
+            assert y2[rest].isfinite().all() and dx2[rest].isfinite().all()
+            if packed is None:
+                assert torch.equal(y2[rest], y[rest]) and torch.equal(dx2[rest], dx[rest])
+
+
+def packed_reference(x):
+    """q and e from the definition in include/lvx.h, in float64 (exact there)."""
+    n, E = x.shape
+    ng = (E + 31) // 32
+    v = np.zeros((n, ng * 32), dtype=np.float32)
+    v[:, :E] = x
+    v = v.reshape(n, ng, 32)
+    u = (v.view(np.uint32) & 0x7fffffff).max(2).astype(np.int64)
+    e = np.clip((u + 0x10000) >> 23, 8, 255)
+    with np.errstate(invalid="ignore"):
+        q = np.where((e == 255)[:, :, None], 0.0, np.rint(v.astype(np.float64) * 2.0 ** (133.0 - e[:, :, None])))
+    assert np.abs(q).max() <= 127
+    return q.reshape(n, -1)[:, :E].astype(np.int8), e.astype(np.uint8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,E,pad", [(1, 1, 0), (3, 31, 2), (2, 33, 0), (7, 64, 0), (5, 200, 8), (300, 96, 3), (4, 4096, 0), (1000, 40, 0), (9, 1001, 0)])
+def test_pack_and_unpack(n, E, pad, dtype):
+    g = torch.Generator().manual_seed(n + E)
+    x = torch.randn((n, E), generator=g) * torch.exp(3.0 * torch.randn((n, E), generator=g))
+    x[0, ::7] = 0.0
+    flat = x.view(-1)
+    # the borders of the rounding, the smallest and the largest numbers, what is no number (where there is room for all)
+    special = [127.5, 127.0, -127.5, 1.9921875, 1.9765625, 2.0 ** -126, 1e-40, -2.0 ** -119, 2.0 ** -118, 3.3e38, 2.0 ** 127, -3.38e38,
+               float("inf"), float("nan"), -float("inf"), 0.5, 1.5, 2.5]
+    for i, s in enumerate(special):
+        if (i + 1) * 41 < flat.numel():
+            flat[(i + 1) * 41] = s
+    x = x.to(DT[dtype])
+    buf = torch.full((n + 1, E + pad), 9.0, dtype=DT[dtype], device="cuda")
+    buf[:n, :E] = x.cuda()
+    room = torch.full((n + 1, E), 33, dtype=torch.int8, device="cuda")
+    pk = B.Packed(n, E)
+    pk.q = room[:n]
+    B.lvx_pack(buf[:n, :E], pk)
+    q, e = packed_reference(x.float().numpy())
+    assert np.array_equal(pk.e.cpu().numpy(), e)
+    on = np.repeat(e != 255, 32, axis=1)[:, :E]
+    assert np.array_equal(pk.q.cpu().numpy()[on], q[on])
+    assert (room[n] == 33).all()
+    for out in ("bf16", "f32"):
+        y = torch.full((n + 1, E + pad), 9.0, dtype=DT[out], device="cuda")
+        B.lvx_unpack(pk, y[:n, :E])
+        v = y[:n, :E].double().cpu().numpy()
+        assert np.array_equal(np.isnan(v), ~on)
+        assert np.array_equal(v[on], unpacked64(pk)[on])
+        assert (y[n:] == 9.0).all() and (y[:, E:] == 9.0).all()
+    # half a step at most, of what is a 127th of the group's largest magnitude at most
+    xf = x.double().numpy()
+    step = np.repeat(2.0 ** (e.astype(np.float64) - 133.0), 32, axis=1)[:, :E]
+    with np.errstate(invalid="ignore"):
+        assert (np.abs(unpacked64(pk) - xf)[on] <= 0.5 * step[on]).all()
+
+
+def test_norms_repeat_on_another_stream_and_in_a_graph():
+    n, E = 333, 1536
+    buf, gamma, beta, d_y = inputs(n, E, "bf16", 21)
+    x = buf[:n]
+    ws = torch.empty(B.lvx_norm_workspace_bytes(n, E), dtype=torch.uint8, device="cuda")
+    out = [torch.empty_like(x), torch.empty((n, 2), device="cuda"), torch.empty_like(x), torch.empty_like(x), torch.empty((2, E), device="cuda")]
+    pk = B.Packed(n, E)
+
+    def step():
+        y, stats, y2, dx, dp = out
+        B.lvx_norm_fwd(x, gamma, beta, y, stats, packed=pk)
+        B.lvx_norm_fwd(None, gamma, beta, y2, stats, packed=pk)
+        dp.zero_()
+        B.lvx_norm_bwd(None, gamma, stats, d_y, dx, dp[0], dp[1], ws, packed=pk)
+
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in out] + [pk.q.clone(), pk.e.clone()]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for t in out:
+            t.fill_(7.0)
+        step()
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out + [pk.q, pk.e], want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    keep = x.clone()
+    for i in range(3):
+        x.copy_(keep * (i + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in out] + [pk.q.clone(), pk.e.clone()]
+        for t in out:
+            t.fill_(3.0)
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out + [pk.q, pk.e], replayed)), i
+
+
+def test_norm_past_32_bit_offsets():
+    """Rows whose elements lie more than 2^31 apart: the first and the last ones of a strided view."""
+    n, E, ss = 3, 640, (1 << 30) + 8
+    room = torch.empty(2 * ss + E, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(room, (n, E), (ss, 1))
+    src = torch.randn((n, E), device="cuda").bfloat16()
+    x.copy_(src)
+    gamma = torch.ones(E, dtype=torch.bfloat16, device="cuda")
+    y, y2, stats, pk = torch.empty_like(src), torch.empty_like(src), torch.empty((n, 2), device="cuda"), B.Packed(n, E)
+    B.lvx_norm_fwd(src, gamma, None, y, stats)
+    B.lvx_norm_fwd(x, gamma, None, y2, stats)
+    assert torch.equal(y, y2)
+    B.lvx_norm_bwd(src, gamma, stats, src, y)
+    B.lvx_norm_bwd(src, gamma, stats, src, y2)
+    B.lvx_norm_bwd(x, gamma, stats, src, x)
+    assert torch.equal(y, x) and torch.equal(y, y2)
+    B.lvx_pack(src, pk)
+    B.lvx_unpack(pk, x)
+    B.lvx_unpack(pk, y)
+    assert torch.equal(x, y)
