@@ -12,6 +12,12 @@
 #include "lvx_mfma.h"
 #include "lvx_packed.h"
 
+#include <type_traits>
+
+// What is fused is written out (fmaf): the norm made again from the packed form has to be the first one bit for bit, and the
+// compiler's own choice differs from kernel to kernel.
+#pragma clang fp contract(off)
+
 namespace lvx {
 
 namespace {
@@ -21,18 +27,31 @@ constexpr int WG = 256;
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __bf16* p) { return (float)*p; }
 
-template <int W> __device__ __forceinline__ float lanes_sum(float x) {
-#pragma unroll
-  for (int o = 1; o < W; o *= 2) x += __shfl_xor(x, o);
-  return x;
+// Sums and maxima over 4, 32 or all 64 lanes, in every lane the same: neighbours inside a quad, mirrored halves and rows of 16, then
+// rows against each other.  (Both sides of every step add the same two numbers, so the lanes agree to the last bit.)
+template <int CTRL> __device__ __forceinline__ unsigned dpp(unsigned x) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
 }
-template <int W> __device__ __forceinline__ unsigned lanes_max(unsigned x) {
-#pragma unroll
-  for (int o = 1; o < W; o *= 2) {
-    const unsigned y = (unsigned)__shfl_xor((int)x, o);
-    x = x > y ? x : y;
+template <int W, class F> __device__ __forceinline__ unsigned lanes_join(unsigned x, F&& f) {
+  x = f(x, dpp<0xB1>(x));                            // lanes 1 apart
+  x = f(x, dpp<0x4E>(x));                            // 2
+  if constexpr (W > 4) {
+    x = f(x, dpp<0x141>(x));                         // the other quad of 8
+    x = f(x, dpp<0x140>(x));                         // the other half of 16
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = f(r[0], r[1]);
+  }
+  if constexpr (W > 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = f(r[0], r[1]);
   }
   return x;
+}
+template <int W> __device__ __forceinline__ float lanes_sum(float x) {
+  return __uint_as_float(lanes_join<W>(__float_as_uint(x), [](unsigned a, unsigned b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+template <int W> __device__ __forceinline__ unsigned lanes_max(unsigned x) {
+  return lanes_join<W>(x, [](unsigned a, unsigned b) { return a > b ? a : b; });
 }
 // over the workgroup, the same in every thread (`at`: 4 floats of LDS that no wave still reads)
 __device__ __forceinline__ float wg_sum(float x, float* at) {
@@ -79,14 +98,13 @@ __global__ void __launch_bounds__(WG) norm_fwd_any_kernel(NormArgs a) {
     s = 0.f;
     for (int e = tid; e < E32; e += WG) {
       const float d = norm_in<T, SRC>(x, q, b, e, E, false) - mu;
-      s += e < E ? d * d : 0.f;
+      s = e < E ? fmaf(d, d, s) : s;
     }
     const float r = 1.f / sqrtf(wg_sum(s, sums[1]) * inv + a.eps);
     for (int e = tid; e < E32; e += WG) {
       const float v = norm_in<T, SRC>(x, q, b, e, E, true);
       if (e < E) {
-        const float yv = (v - mu) * r * load1((const T*)a.gamma + e);
-        y[e] = (T)(a.beta ? yv + load1((const T*)a.beta + e) : yv);
+        y[e] = (T)fmaf((v - mu) * r, load1((const T*)a.gamma + e), a.beta ? load1((const T*)a.beta + e) : 0.f);
       }
     }
     if (tid == 0) {
@@ -112,7 +130,7 @@ __global__ void __launch_bounds__(WG) norm_bwd_any_kernel(NormArgs a) {
     for (int e = tid; e < E; e += WG) {
       const float g = load1(dy + e) * load1((const T*)a.gamma + e);
       s += g;
-      sx += g * ((norm_in<T, SRC>(x, q, b, e, E, false) - mu) * r);
+      sx = fmaf(g, (norm_in<T, SRC>(x, q, b, e, E, false) - mu) * r, sx);
     }
     __syncthreads();
     s = a.rms ? 0.f : wg_sum(s, sums[0]) * inv;
@@ -120,7 +138,7 @@ __global__ void __launch_bounds__(WG) norm_bwd_any_kernel(NormArgs a) {
     for (int e = tid; e < E; e += WG) {
       const float g = load1(dy + e) * load1((const T*)a.gamma + e);
       const float xh = (norm_in<T, SRC>(x, q, b, e, E, false) - mu) * r;
-      dx[e] = (T)(r * (g - s - xh * sx));
+      dx[e] = (T)(r * fmaf(-xh, sx, g - s));
     }
   }
 }
@@ -136,7 +154,7 @@ __global__ void __launch_bounds__(WG) norm_param_any_kernel(NormArgs a) {
     const float dy = load1((const T*)a.dy + row * a.y_ss + e);
     const float xh = (norm_in<T, SRC>((const T*)a.x + row * a.x_ss, a.q + row * E, a.b + row * packed::groups(E), e, E, false) -
                       a.stats_in[2 * row]) * a.stats_in[2 * row + 1];
-    sg += dy * xh;
+    sg = fmaf(dy, xh, sg);
     sb += dy;
   }
   a.part[(2L * blockIdx.y) * E + e] = sg;
@@ -161,75 +179,468 @@ __global__ void __launch_bounds__(WG) norm_param_sum_kernel(NormArgs a) {
   if (to) to[at < a.E ? at : at - a.E] += s;
 }
 
-// ---- packing by itself ----
+// ---- rows in registers: a team of TPR threads has a row, a thread NV chunks of 8 features of it ----
+//
+// A chunk is moved at once wherever it lies: the memory instructions take any address that the element type has.  FULL: E is a
+// multiple of 8; otherwise a row's last chunk goes element by element.  Which thread has which features goes by E alone, so
+// the norm made again from the packed form is the first one bit for bit, whatever x's addresses were.
 
-// 32 lanes per group of a row, any width and alignment
-template <typename T>
-__global__ void __launch_bounds__(WG) pack_any_kernel(NormArgs a) {
-  const int E = a.E, ng = packed::groups(E), l = threadIdx.x % 32;
-  const long total = a.n * ng;
-  for (long g = (long)blockIdx.x * (WG / 32) + threadIdx.x / 32; g < total; g += (long)gridDim.x * (WG / 32)) {
-    const long row = g / ng;
-    const int e = (int)(g % ng) * 32 + l;
-    norm_in<T, 1>((const T*)a.x + row * a.x_ss, a.q + row * E, a.b + row * ng, e, E, true);
+constexpr int V = 8;
+__host__ __device__ constexpr int chunks(int E) { return (E + V - 1) / V; }
+typedef u32x4 __attribute__((aligned(2))) u32x4_any2;
+typedef u32x4 __attribute__((aligned(4))) u32x4_any4;
+typedef u32x2 __attribute__((aligned(1))) u32x2_any;
+
+// chunk c of a row of E features as it lies in memory; a chunk behind the last one is the last one again, what is behind a row's
+// end in the last one is 0
+template <typename T> struct Chunk;
+template <> struct Chunk<__bf16> {
+  u32x4 w;
+  template <bool FULL> __device__ __forceinline__ void load(const __bf16* row, int c, int E) {
+    c = min(c, chunks(E) - 1);
+    if (FULL || V * c + V <= E) {
+      w = *(const u32x4_any2*)(row + V * c);
+    } else {
+      w = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (V * c + k < E) w[k / 2] |= (unsigned)((const uint16_t*)row)[V * c + k] << (16 * (k % 2));
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
+  template <bool FULL> static __device__ __forceinline__ void store(__bf16* row, int c, int E, const float (&v)[V]) {
+    if (c >= chunks(E)) return;
+    if (FULL || V * c + V <= E) {
+      *(u32x4_any2*)(row + V * c) = u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (V * c + k < E) row[V * c + k] = (__bf16)v[k];
+    }
+  }
+};
+template <> struct Chunk<float> {
+  u32x4 w[2];
+  template <bool FULL> __device__ __forceinline__ void load(const float* row, int c, int E) {
+    c = min(c, chunks(E) - 1);
+    if (FULL || V * c + V <= E) {
+      w[0] = *(const u32x4_any4*)(row + V * c);
+      w[1] = *(const u32x4_any4*)(row + V * c + 4);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) w[k / 4][k % 4] = V * c + k < E ? __float_as_uint(row[V * c + k]) : 0u;
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i / 4][i % 4]); }
+  template <bool FULL> static __device__ __forceinline__ void store(float* row, int c, int E, const float (&v)[V]) {
+    if (c >= chunks(E)) return;
+    if (FULL || V * c + V <= E) {
+      *(u32x4_any4*)(row + V * c) = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+      *(u32x4_any4*)(row + V * c + 4) = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (V * c + k < E) row[V * c + k] = v[k];
+    }
+  }
+};
+// whether feature k of chunk c is one
+template <bool FULL> __device__ __forceinline__ bool is_on(int c, int k, int E) { return FULL ? c < chunks(E) : V * c + k < E; }
+
+// 8 packed features and their exponent byte
+struct PackedChunk {
+  u32x2 w;
+  unsigned b;
+  template <bool FULL> __device__ __forceinline__ void load(const int8_t* q, const uint8_t* e, int c, int E) {
+    c = min(c, chunks(E) - 1);
+    if (FULL || V * c + V <= E) {
+      w = *(const u32x2_any*)(q + V * c);
+    } else {
+      w = u32x2{0u, 0u};
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (V * c + k < E) w[k / 4] |= (unsigned)(uint8_t)q[V * c + k] << (8 * (k % 4));
+    }
+    b = e[c / (packed::GROUP / V)];
+  }
+  __device__ __forceinline__ void values(float (&v)[V]) const {
+    const float step = packed::step_of(b);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * step;
+  }
+};
+// Packs a chunk (all lanes of its group of 32 features take part, with zeros behind the row's end) and puts in its place what the
+// packed form stands for.
+template <bool FULL> __device__ __forceinline__ void pack_chunk(float (&v)[V], int8_t* q, uint8_t* e, int c, int E) {
+  unsigned m = packed::magnitude(v[0]);
+#pragma unroll
+  for (int i = 1; i < V; ++i) {
+    const unsigned x = packed::magnitude(v[i]);
+    m = m > x ? m : x;
+  }
+  const unsigned b = packed::exponent_of(lanes_max<packed::GROUP / V>(m));
+  const float inverse = packed::inverse_step_of(b), step = packed::step_of(b);
+  unsigned s[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float x = packed::steps(b == 255u ? 0.f : v[i], inverse);
+    s[i] = __float_as_uint(x);
+    v[i] = packed::value(x, step);
+  }
+  if (c >= chunks(E)) return;
+  if (FULL || V * c + V <= E) {
+    const auto four = [](unsigned s0, unsigned s1, unsigned s2, unsigned s3) {          // their low bytes
+      return __builtin_amdgcn_perm(__builtin_amdgcn_perm(s3, s2, 0x0c0c0400), __builtin_amdgcn_perm(s1, s0, 0x0c0c0400), 0x05040100);
+    };
+    *(u32x2_any*)(q + V * c) = u32x2{four(s[0], s[1], s[2], s[3]), four(s[4], s[5], s[6], s[7])};
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (V * c + k < E) q[V * c + k] = (int8_t)(s[k] & 0xffu);
+  }
+  if (c % (packed::GROUP / V) == 0) e[c / (packed::GROUP / V)] = (uint8_t)b;
+}
+
+// Sums over a team.  One wave: by lanes.  More: through LDS, in two places that take turns, with one barrier each: who writes a
+// place again has crossed the barrier of the sum between, which every wave reaches after reading the place.
+template <int TPR> struct TeamSum {
+  float (*at)[2][16];                                // [turn][which][wave]
+  int turn = 0;
+  template <int N> __device__ __forceinline__ void operator()(float (&x)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = lanes_sum<64>(x[k]);
+    if constexpr (TPR > 64) {
+      constexpr int W = TPR / 64;
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) at[turn][k][threadIdx.x >> 6] = x[k];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += at[turn][k][w];
+        x[k] = s;
+      }
+    }
+  }
+};
+constexpr int wg_of(int tpr) { return tpr > WG ? tpr : WG; }
+
+template <typename T, int SRC, bool FULL, int TPR, int NV>
+__global__ void __launch_bounds__(wg_of(TPR)) norm_fwd_kernel(NormArgs a) {
+  constexpr int TEAMS = wg_of(TPR) / TPR;
+  __shared__ float sums[2][2][16];
+  TeamSum<TPR> team_sum{sums};
+  const int t = threadIdx.x % TPR, E = a.E;
+  const float inv = 1.f / (float)a.E;
+  Chunk<T> gamma[NV], beta[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    gamma[i].template load<FULL>((const T*)a.gamma, t + TPR * i, E);
+    if (a.beta) beta[i].template load<FULL>((const T*)a.beta, t + TPR * i, E);
+    else beta[i] = Chunk<T>{};
+  }
+  for (long row = (long)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.n; row += (long)gridDim.x * TEAMS) {
+    int8_t* const q = a.q + row * a.E;
+    uint8_t* const e = a.b + row * packed::groups(a.E);
+    float v[NV][V];
+    if constexpr (SRC == 2) {
+      PackedChunk raw[NV];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) raw[i].template load<FULL>(q, e, t + TPR * i, E);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) raw[i].values(v[i]);
+    } else {
+      Chunk<T> raw[NV];
+      const T* const x = (const T*)a.x + row * a.x_ss;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) raw[i].template load<FULL>(x, t + TPR * i, E);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[i][k] = raw[i][k];
+    }
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + TPR * i;
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[i][k] = is_on<FULL>(c, k, E) ? v[i][k] : 0.f;
+      if constexpr (SRC == 1) pack_chunk<FULL>(v[i], q, e, c, E);
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[0] += v[i][k];
+    }
+    float mu = 0.f;
+    if (!a.rms) {
+      team_sum(s);
+      mu = s[0] * inv;
+    }
+    s[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        v[i][k] = is_on<FULL>(t + TPR * i, k, E) ? v[i][k] - mu : 0.f;
+        s[0] = fmaf(v[i][k], v[i][k], s[0]);
+      }
+    }
+    team_sum(s);
+    const float r = 1.f / sqrtf(s[0] * inv + a.eps);
+    T* const y = (T*)a.y + row * a.y_ss;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + TPR * i;
+      float o[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) o[k] = fmaf(v[i][k] * r, gamma[i][k], beta[i][k]);
+      Chunk<T>::template store<FULL>(y, c, E, o);
+    }
+    if (t == 0) {
+      a.stats[2 * row] = mu;
+      a.stats[2 * row + 1] = r;
+    }
   }
 }
-template <typename T>
-__global__ void __launch_bounds__(WG) unpack_any_kernel(NormArgs a) {
-  const int E = a.E, ng = packed::groups(E), l = threadIdx.x % 32;
-  const long total = a.n * ng;
-  for (long g = (long)blockIdx.x * (WG / 32) + threadIdx.x / 32; g < total; g += (long)gridDim.x * (WG / 32)) {
-    const long row = g / ng;
-    const int e = (int)(g % ng) * 32 + l;
-    const float v = norm_in<T, 2>((const T*)nullptr, a.q + row * E, a.b + row * ng, e, E, false);
-    if (e < E) ((T*)a.y + row * a.y_ss)[e] = (T)v;
+
+// dx of the rows, and (PARAM) the part of dgamma and dbeta that these rows make: a thread adds up its own columns over all of
+// its rows, the teams of a workgroup are joined in LDS, a workgroup writes one part.  The next row is on its way while one is
+// worked on.
+template <typename T, int SRC, bool FULL, int TPR, int NV, bool PARAM>
+__global__ void __launch_bounds__(wg_of(TPR)) norm_bwd_kernel(NormArgs a) {
+  constexpr int TEAMS = wg_of(TPR) / TPR;
+  __shared__ float sums[2][2][16];
+  __shared__ float join[PARAM && TEAMS > 1 ? 2 * TPR * NV * V : 1];
+  TeamSum<TPR> team_sum{sums};
+  const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, E = a.E;
+  const float inv = 1.f / (float)a.E;
+  struct Row {
+    Chunk<T> x[SRC == 2 ? 1 : NV], dy[NV];
+    PackedChunk p[SRC == 2 ? NV : 1];
+    float mu, r;
+  };
+  auto load = [&](Row& w, long row) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + TPR * i;
+      w.dy[i].template load<FULL>((const T*)a.dy + row * a.y_ss, c, E);
+      if constexpr (SRC == 2) w.p[i].template load<FULL>(a.q + row * E, a.b + row * packed::groups(E), c, E);
+      else w.x[i].template load<FULL>((const T*)a.x + row * a.x_ss, c, E);
+    }
+    w.mu = a.stats_in[2 * row];
+    w.r = a.stats_in[2 * row + 1];
+  };
+  Chunk<T> gamma[NV];
+  float pg[PARAM ? NV : 1][V], pb[PARAM ? NV : 1][V];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    gamma[i].template load<FULL>((const T*)a.gamma, t + TPR * i, E);
+    if constexpr (PARAM) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) pg[i][k] = pb[i][k] = 0.f;
+    }
+  }
+  const long step = (long)gridDim.x * TEAMS;
+  long row = (long)blockIdx.x * TEAMS + team;
+  Row next;
+  if (row < a.n) load(next, row);
+  for (; row < a.n; row += step) {
+    const Row w = next;
+    if (row + step < a.n) load(next, row + step);
+    float s[2] = {0.f, 0.f};
+    float xh[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float v[V];
+      if constexpr (SRC == 2) w.p[i].values(v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if constexpr (SRC != 2) v[k] = w.x[i][k];
+        xh[i][k] = (v[k] - w.mu) * w.r;
+        const float dy = w.dy[i][k], g = dy * gamma[i][k];
+        const bool on = is_on<FULL>(t + TPR * i, k, E);
+        s[0] += on ? g : 0.f;
+        s[1] = fmaf(on ? g : 0.f, xh[i][k], s[1]);
+        if constexpr (PARAM) {
+          pg[i][k] = fmaf(dy, xh[i][k], pg[i][k]);
+          pb[i][k] += dy;
+        }
+      }
+    }
+    if (a.dx) {                                      // (uniform)
+      team_sum(s);
+      const float m = a.rms ? 0.f : s[0] * inv, mx = s[1] * inv;
+      T* const dx = (T*)a.dx + row * a.x_ss;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = t + TPR * i;
+        float o[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) o[k] = w.r * fmaf(-xh[i][k], mx, w.dy[i][k] * gamma[i][k] - m);
+        Chunk<T>::template store<FULL>(dx, c, E, o);
+      }
+    }
+  }
+  if constexpr (PARAM) {
+    if constexpr (TEAMS > 1) {
+      for (int k = 0; k < TEAMS; ++k) {
+        if (team == k) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int u = 0; u < V; ++u) {
+              float* const at = join + 2 * (t + TPR * (V * i + u));
+              at[0] = pg[i][u] += k > 0 ? at[0] : 0.f;
+              at[1] = pb[i][u] += k > 0 ? at[1] : 0.f;
+            }
+        }
+        __syncthreads();
+      }
+      if (team != TEAMS - 1) return;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + TPR * i;
+      float* const to = a.part + 2L * blockIdx.x * E;
+      Chunk<float>::store<FULL>(to, c, E, pg[i]);
+      Chunk<float>::store<FULL>(to + E, c, E, pb[i]);
+    }
+  }
+}
+
+// ---- packing by itself: a thread has 8 features, four chunks of a wave are in flight, a wave takes 2048 features of one row after
+// the other ----
+
+template <typename T, bool FULL>
+__global__ void __launch_bounds__(WG) pack_kernel(NormArgs a) {
+  const int E = a.E, ng = packed::groups(E), c0 = blockIdx.x * 256 + (threadIdx.x & 63);
+  for (long row = (long)blockIdx.y * 4 + (threadIdx.x >> 6); row < a.n; row += (long)gridDim.y * 4) {
+    Chunk<T> raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i].template load<FULL>((const T*)a.x + row * a.x_ss, c0 + 64 * i, E);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = is_on<FULL>(c0 + 64 * i, k, E) ? raw[i][k] : 0.f;
+      pack_chunk<FULL>(v, a.q + row * E, a.b + row * ng, c0 + 64 * i, E);
+    }
+  }
+}
+template <typename T, bool FULL>
+__global__ void __launch_bounds__(WG) unpack_kernel(NormArgs a) {
+  const int E = a.E, ng = packed::groups(E), c0 = blockIdx.x * 256 + (threadIdx.x & 63);
+  for (long row = (long)blockIdx.y * 4 + (threadIdx.x >> 6); row < a.n; row += (long)gridDim.y * 4) {
+    PackedChunk raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i].template load<FULL>(a.q + row * E, a.b + row * ng, c0 + 64 * i, E);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v[V];
+      raw[i].values(v);
+      Chunk<T>::template store<FULL>((T*)a.y + row * a.y_ss, c0 + 64 * i, E, v);
+    }
   }
 }
 
 unsigned grid_of(long n, long most) { return (unsigned)(n < most ? n : most); }
 
-template <typename T> hipError_t fwd(const NormArgs& a, hipStream_t s) {
-  const unsigned grid = grid_of(a.n, 16L * a.n_cu);
-  if (a.x && a.q) norm_fwd_any_kernel<T, 1><<<grid, WG, 0, s>>>(a);
-  else if (a.q) norm_fwd_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
-  else norm_fwd_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
+template <typename T, bool FULL, int TPR, int NV> void fwd_rows(const NormArgs& a, hipStream_t s) {
+  constexpr int W = wg_of(TPR);
+  const unsigned grid = grid_of((a.n + W / TPR - 1) / (W / TPR), 8L * a.n_cu);
+  if (a.x && a.q) norm_fwd_kernel<T, 1, FULL, TPR, NV><<<grid, W, 0, s>>>(a);
+  else if (a.q) norm_fwd_kernel<T, 2, FULL, TPR, NV><<<grid, W, 0, s>>>(a);
+  else norm_fwd_kernel<T, 0, FULL, TPR, NV><<<grid, W, 0, s>>>(a);
+}
+template <typename T, bool FULL, int TPR, int NV> void bwd_rows(const NormArgs& a, hipStream_t s) {
+  constexpr int W = wg_of(TPR);
+  if (a.dgamma || a.dbeta) {
+    if (a.q) norm_bwd_kernel<T, 2, FULL, TPR, NV, true><<<(unsigned)a.parts, W, 0, s>>>(a);
+    else norm_bwd_kernel<T, 0, FULL, TPR, NV, true><<<(unsigned)a.parts, W, 0, s>>>(a);
+    norm_param_sum_kernel<<<(unsigned)((2L * a.E + 15) / 16), WG, 0, s>>>(a);
+    return;
+  }
+  const unsigned grid = grid_of((a.n + W / TPR - 1) / (W / TPR), 8L * a.n_cu);
+  if (a.q) norm_bwd_kernel<T, 2, FULL, TPR, NV, false><<<grid, W, 0, s>>>(a);
+  else norm_bwd_kernel<T, 0, FULL, TPR, NV, false><<<grid, W, 0, s>>>(a);
+}
+
+// by the width alone (see above)
+template <typename T, bool FULL> hipError_t fwd(const NormArgs& a, hipStream_t s) {
+  const int E = a.E;
+  if (E <= 512) fwd_rows<T, FULL, 64, 1>(a, s);
+  else if (E <= 1024) fwd_rows<T, FULL, 64, 2>(a, s);
+  else if (E <= 2048) fwd_rows<T, FULL, 64, 4>(a, s);
+  else if (E <= 4096) fwd_rows<T, FULL, 64, 8>(a, s);
+  else if (E <= 8192) fwd_rows<T, FULL, 256, 4>(a, s);
+  else if (E <= 16384) fwd_rows<T, FULL, 256, 8>(a, s);
+  else {
+    const unsigned grid = grid_of(a.n, 16L * a.n_cu);
+    if (a.x && a.q) norm_fwd_any_kernel<T, 1><<<grid, WG, 0, s>>>(a);
+    else if (a.q) norm_fwd_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
+    else norm_fwd_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
-template <typename T> hipError_t bwd(const NormArgs& a, hipStream_t s) {
-  // (the sums over the rows first: dx may lie where dy does)
-  if (a.dgamma || a.dbeta) {
-    const dim3 grid((unsigned)((a.E + WG - 1) / WG), (unsigned)a.parts);
-    if (a.q) norm_param_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
-    else norm_param_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
-    norm_param_sum_kernel<<<(unsigned)((2L * a.E + 15) / 16), WG, 0, s>>>(a);
-  }
-  if (a.dx) {
-    const unsigned grid = grid_of(a.n, 16L * a.n_cu);
-    if (a.q) norm_bwd_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
-    else norm_bwd_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
+template <typename T, bool FULL> hipError_t bwd(const NormArgs& a, hipStream_t s) {
+  const int E = a.E;
+  if (E <= 512) bwd_rows<T, FULL, 64, 1>(a, s);
+  else if (E <= 1024) bwd_rows<T, FULL, 64, 2>(a, s);
+  else if (E <= 2048) bwd_rows<T, FULL, 256, 1>(a, s);
+  else if (E <= 4096) bwd_rows<T, FULL, 256, 2>(a, s);
+  else if (E <= 8192) bwd_rows<T, FULL, 256, 4>(a, s);
+  else if (E <= 16384) bwd_rows<T, FULL, 1024, 2>(a, s);
+  else {
+    // (the sums over the rows first: dx may lie where dy does)
+    if (a.dgamma || a.dbeta) {
+      const dim3 grid((unsigned)((a.E + WG - 1) / WG), (unsigned)a.parts);
+      if (a.q) norm_param_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
+      else norm_param_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
+      norm_param_sum_kernel<<<(unsigned)((2L * a.E + 15) / 16), WG, 0, s>>>(a);
+    }
+    if (a.dx) {
+      const unsigned grid = grid_of(a.n, 16L * a.n_cu);
+      if (a.q) norm_bwd_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
+      else norm_bwd_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
+    }
   }
   return hipGetLastError();
+}
+// f(an element, whether E is a multiple of 8)
+template <class F> hipError_t by_type(const NormArgs& a, int is_f32, F&& f) {
+  using yes = std::true_type;
+  using no = std::false_type;
+  if (a.E % V == 0) return is_f32 ? f(0.f, yes{}) : f(__bf16{}, yes{});
+  return is_f32 ? f(0.f, no{}) : f(__bf16{}, no{});
 }
 }  // namespace
 
 int norm_parts(long n, int E) {
   (void)E;
-  const long parts = (n + 15) / 16;
-  return (int)(parts < 256 ? parts : 256);
+  const long parts = (n + 7) / 8, most = 2L * device_cu_count();
+  return (int)(parts < most ? parts : most);
 }
-hipError_t launch_norm_fwd(const NormArgs& a, int is_f32, hipStream_t s) { return is_f32 ? fwd<float>(a, s) : fwd<__bf16>(a, s); }
-hipError_t launch_norm_bwd(const NormArgs& a, int is_f32, hipStream_t s) { return is_f32 ? bwd<float>(a, s) : bwd<__bf16>(a, s); }
+hipError_t launch_norm_fwd(const NormArgs& a, int is_f32, hipStream_t s) {
+  return by_type(a, is_f32, [&](auto t, auto full) { return fwd<decltype(t), decltype(full)::value>(a, s); });
+}
+hipError_t launch_norm_bwd(const NormArgs& a, int is_f32, hipStream_t s) {
+  return by_type(a, is_f32, [&](auto t, auto full) { return bwd<decltype(t), decltype(full)::value>(a, s); });
+}
 hipError_t launch_pack(const NormArgs& a, int is_f32, hipStream_t s) {
-  const unsigned grid = grid_of((a.n * packed::groups(a.E) + 7) / 8, 32L * a.n_cu);
-  if (is_f32) pack_any_kernel<float><<<grid, WG, 0, s>>>(a);
-  else pack_any_kernel<__bf16><<<grid, WG, 0, s>>>(a);
-  return hipGetLastError();
+  const dim3 grid((unsigned)((a.E + 2047) / 2048), grid_of((a.n + 3) / 4, 16384));
+  return by_type(a, is_f32, [&](auto t, auto full) {
+    pack_kernel<decltype(t), decltype(full)::value><<<grid, WG, 0, s>>>(a);
+    return hipGetLastError();
+  });
 }
 hipError_t launch_unpack(const NormArgs& a, int is_f32, hipStream_t s) {
-  const unsigned grid = grid_of((a.n * packed::groups(a.E) + 7) / 8, 32L * a.n_cu);
-  if (is_f32) unpack_any_kernel<float><<<grid, WG, 0, s>>>(a);
-  else unpack_any_kernel<__bf16><<<grid, WG, 0, s>>>(a);
-  return hipGetLastError();
+  const dim3 grid((unsigned)((a.E + 2047) / 2048), grid_of((a.n + 3) / 4, 16384));
+  return by_type(a, is_f32, [&](auto t, auto full) {
+    unpack_kernel<decltype(t), decltype(full)::value><<<grid, WG, 0, s>>>(a);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace lvx
