@@ -142,7 +142,13 @@ def dtype_code(dt: torch.dtype) -> int:
     raise TypeError(f"unsupported dtype {dt}")
 
 
+# (the current stream without an object for it: 2.8 us a call otherwise)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
+    if _raw_stream is not None:
+        return int(_raw_stream(torch.cuda.current_device()))
     return int(torch.cuda.current_stream().cuda_stream)
 
 
@@ -386,29 +392,29 @@ def lvx_xattn_project_bwd(x, w, d_outs, dx=None, dw=None) -> None:
 
 # ---- around the layer: norms of the token features, their 8-bit checkpoint ----
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
-
-
 def _on_device(where: str, *ts) -> None:
     """Every tensor lies on the device whose stream the call goes to."""
-    at = torch.cuda.current_device() if torch.cuda.is_available() else None
-    if not all(t.is_cuda and t.device.index == at for t in ts if t is not None):
-        raise RuntimeError(f"{where} needs tensors of the current device")
+    at = None
+    for t in ts:
+        if t is not None:
+            if t.is_cuda and at is None:
+                at = torch.cuda.current_device()
+            if not t.is_cuda or t.get_device() != at:
+                raise RuntimeError(f"{where} needs tensors of the current device")
 
 
 def _token_rows(t, name: str):
     """(tokens, features, elements from one token to the next) of t [n, E] or [B, S, E] (features contiguous, batches that
     follow each other)."""
-    _need(t.dim() in (2, 3) and (t.stride(-1) == 1 or t.shape[-1] == 1), f"{name} has to be [n, E] or [B, S, E] with contiguous features")
-    E, S = t.shape[-1], t.shape[-2]
-    n = t.numel() // E if E else 0
-    if t.dim() == 3 and t.shape[0] > 1 and S > 1:
-        _need(t.stride(0) == S * t.stride(1), f"{name}: the batches have to follow each other")
-    if t.dim() == 3 and S == 1:
-        return n, E, t.stride(0) if t.shape[0] > 1 else E
-    return n, E, t.stride(-2) if n > 1 else E
+    size, stride = t.shape, t.stride()
+    if len(size) not in (2, 3) or (stride[-1] != 1 and size[-1] != 1):
+        raise ValueError(f"{name} has to be [n, E] or [B, S, E] with contiguous features")
+    if len(size) == 2:
+        return size[0], size[1], stride[0] if size[0] > 1 else size[1]
+    Bn, S, E = size
+    if Bn > 1 and S > 1 and stride[0] != S * stride[1]:
+        raise ValueError(f"{name}: the batches have to follow each other")
+    return Bn * S, E, E if Bn * S <= 1 else stride[1] if S > 1 else stride[0]
 
 
 class Packed:
@@ -429,9 +435,8 @@ class Packed:
         return self.q.shape
 
     def _struct(self, where: str, n: int, E: int) -> lvx_packed:
-        _need(tuple(self.q.shape) == (n, E) and tuple(self.e.shape) == (n, (E + 31) // 32), f"{where}: packed has to hold [{n}, {E}]")
-        _need(self.q.is_contiguous() and self.e.is_contiguous() and self.q.dtype == torch.int8 and self.e.dtype == torch.uint8,
-              f"{where}: packed has to be contiguous int8 and uint8")
+        if not _of(self.q, torch.int8, n, E) or not _of(self.e, torch.uint8, n, (E + 31) // 32):
+            raise ValueError(f"{where}: packed has to hold [{n}, {E}], contiguous")
         _on_device(where, self.q, self.e)
         return lvx_packed(self.q.data_ptr(), self.e.data_ptr())
 
@@ -450,27 +455,35 @@ def lvx_unpack(packed: Packed, x) -> None:
     _check(load().lvx_unpack(n, E, ss, dtype_code(x.dtype), C.byref(packed._struct("lvx_unpack", n, E)), x.data_ptr(), _stream()), "lvx_unpack")
 
 
+def _of(t, dtype, *shape) -> bool:
+    return t.shape == shape and t.dtype == dtype and t.is_contiguous()
+
+
 def _norm_struct(where, like_x, like_y, gamma, stats, rms, eps):
     """Sizes and strides of a norm call; like_x: x or dx or None (features that exist packed only)."""
     n, E, y_ss = _token_rows(like_y, "y")
     x_ss = E
     if like_x is not None:
         nx, Ex, x_ss = _token_rows(like_x, "x")
-        _need((nx, Ex) == (n, E), f"{where}: x and y differ in shape")
-        _need(like_x.dtype == like_y.dtype, f"{where}: x and y differ in type")
-    _need(tuple(gamma.shape) == (E,) and gamma.is_contiguous() and gamma.dtype == like_y.dtype, f"{where}: gamma has to be [{E}] of y's type")
-    _need(stats.numel() == 2 * n and stats.is_contiguous() and stats.dtype == torch.float32, f"{where}: stats has to be float32 [{n}, 2]")
-    return lvx_norm(n, E, int(bool(rms)), x_ss, y_ss, float(eps))
+        if nx != n or Ex != E or like_x.dtype != like_y.dtype:
+            raise ValueError(f"{where}: x and y differ in shape or type")
+    if not _of(gamma, like_y.dtype, E):
+        raise ValueError(f"{where}: gamma has to be [{E}] of y's type")
+    if stats.numel() != 2 * n or stats.dtype != torch.float32 or not stats.is_contiguous():
+        raise ValueError(f"{where}: stats has to be float32 [{n}, 2]")
+    return lvx_norm(n, E, 1 if rms else 0, x_ss, y_ss, eps)
 
 
 def lvx_norm_fwd(x, gamma, beta, y, stats, rms: bool = False, eps: float = 1e-5, packed: Optional[Packed] = None) -> None:
     """y ([n, E] or [B, S, E]; may be x) and stats (float32 [n, 2]) are overwritten with the norm of x and its (mean, 1 / spread).
     With packed: x is packed there and y is the norm of the packed values; with x None, of what was packed there before."""
     w = "lvx_norm_fwd"
-    _need(x is not None or packed is not None, f"{w}: neither x nor packed")
+    if x is None and packed is None:
+        raise ValueError(f"{w}: neither x nor packed")
     _on_device(w, x, gamma, beta, y, stats)
     p = _norm_struct(w, x, y, gamma, stats, rms, eps)
-    _need(beta is None or tuple(beta.shape) == (p.E,) and beta.is_contiguous() and beta.dtype == y.dtype, f"{w}: beta has to be [{p.E}] of y's type")
+    if beta is not None and not _of(beta, y.dtype, p.E):
+        raise ValueError(f"{w}: beta has to be [{p.E}] of y's type")
     pk = packed._struct(w, p.n, p.E) if packed is not None else None
     _check(load().lvx_norm_fwd(C.byref(p), dtype_code(y.dtype), x.data_ptr() if x is not None else None, C.byref(pk) if pk is not None else None,
                                gamma.data_ptr(), beta.data_ptr() if beta is not None else None, y.data_ptr(), stats.data_ptr(), _stream()), w)
@@ -485,16 +498,22 @@ def lvx_norm_bwd(x, gamma, stats, d_y, dx=None, dgamma=None, dbeta=None, workspa
     """The gradients of lvx_norm_fwd, from x or (x None) from what was packed.  dx (x's shape, strides and type; may be x or d_y) is
     overwritten, dgamma and dbeta (float32 [E]) are added to; any of the three may be None."""
     w = "lvx_norm_bwd"
-    _need((x is None) != (packed is None), f"{w}: x or packed, one of them")
-    _need(dx is not None or dgamma is not None or dbeta is not None, f"{w}: nothing asked for")
+    if (x is None) == (packed is None):
+        raise ValueError(f"{w}: x or packed, one of them")
+    if dx is None and dgamma is None and dbeta is None:
+        raise ValueError(f"{w}: nothing asked for")
     _on_device(w, x, gamma, stats, d_y, dx, dgamma, dbeta, workspace)
     p = _norm_struct(w, x if x is not None else dx, d_y, gamma, stats, rms, eps)
     if dx is not None:
-        _need(dx.shape == d_y.shape and dx.dtype == d_y.dtype, f"{w}: dx and d_y differ in shape or type")
-        _need(x is None or _token_rows(dx, "dx")[2] == p.x_ss, f"{w}: dx has to have x's strides")
-    for t, name in ((dgamma, "dgamma"), (dbeta, "dbeta")):
-        _need(t is None or tuple(t.shape) == (p.E,) and t.is_contiguous() and t.dtype == torch.float32, f"{w}: {name} has to be float32 [{p.E}]")
-    _need(workspace is None or workspace.is_contiguous(), f"{w}: the workspace has to be contiguous")
+        if dx.shape != d_y.shape or dx.dtype != d_y.dtype:
+            raise ValueError(f"{w}: dx and d_y differ in shape or type")
+        if x is not None and _token_rows(dx, "dx")[2] != p.x_ss:
+            raise ValueError(f"{w}: dx has to have x's strides")
+    for t in (dgamma, dbeta):
+        if t is not None and not _of(t, torch.float32, p.E):
+            raise ValueError(f"{w}: dgamma and dbeta have to be float32 [{p.E}]")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError(f"{w}: the workspace has to be contiguous")
     pk = packed._struct(w, p.n, p.E) if packed is not None else None
     at = lambda t: t.data_ptr() if t is not None else None
     _check(load().lvx_norm_bwd(C.byref(p), dtype_code(d_y.dtype), at(x), C.byref(pk) if pk is not None else None, gamma.data_ptr(),

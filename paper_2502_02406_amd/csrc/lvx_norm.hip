@@ -71,7 +71,7 @@ __device__ __forceinline__ float norm_in(const T* x, int8_t* q, uint8_t* b, int 
   if constexpr (SRC == 2) return e < E ? (float)q[e] * packed::step_of(b[e / packed::GROUP]) : 0.f;
   const float v = e < E ? load1(x + e) : 0.f;
   const unsigned byte = packed::exponent_of(lanes_max<32>(packed::magnitude(v)));
-  const float s = packed::steps(byte == 255u ? 0.f : v, packed::inverse_step_of(byte));
+  const float s = packed::steps(v, packed::inverse_step_of(byte));
   if (keep && e < E) {
     q[e] = packed::whole(s);
     if (e % packed::GROUP == 0) b[e / packed::GROUP] = (uint8_t)byte;
@@ -161,22 +161,40 @@ __global__ void __launch_bounds__(WG) norm_param_any_kernel(NormArgs a) {
   a.part[(2L * blockIdx.y + 1) * E + e] = sb;
 }
 
-// dgamma += the parts' sums, dbeta likewise, in a fixed order: 16 threads share a column
+// dgamma += the parts' sums, dbeta likewise, in a fixed order: 32 threads share a column, 8 parts of each are on their way at once
 __global__ void __launch_bounds__(WG) norm_param_sum_kernel(NormArgs a) {
-  __shared__ float sums[16][17];
-  const long at = (long)blockIdx.x * 16 + threadIdx.x % 16;      // dgamma's columns, then dbeta's
-  const int lane = threadIdx.x / 16;
-  float s = 0.f;
-  if (at < 2L * a.E)
-    for (int p = lane; p < a.parts; p += 16) s += a.part[2L * p * a.E + at];
-  sums[lane][threadIdx.x % 16] = s;
-  __syncthreads();
-  if (threadIdx.x >= 16 || at >= 2L * a.E) return;
-  s = 0.f;
+  __shared__ float sums[32][33];
+  const int col = threadIdx.x % 8, lane = threadIdx.x / 8;
+  const long at = (long)blockIdx.x * 32 + 4 * col, n = 2L * a.E;  // dgamma's columns, then dbeta's
+  typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  const int whole = (int)min(n - at, 4L);            // (a place's last columns: fewer, or none)
+  for (int p0 = lane; p0 < a.parts; p0 += 256) {
+    f32x4 v[8];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += sums[i][threadIdx.x];
-  float* const to = at < a.E ? a.dgamma : a.dbeta;
-  if (to) to[at < a.E ? at : at - a.E] += s;
+    for (int i = 0; i < 8; ++i) {
+      const float* const from = a.part + n * min(p0 + 32 * i, a.parts - 1) + at;
+      v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (whole == 4) v[i] = *(const f32x4_any*)from;
+      else
+        for (int k = 0; k < 3; ++k)
+          if (k < whole) v[i][k] = from[k];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k] += p0 + 32 * i < a.parts ? v[i][k] : 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sums[lane][4 * col + k] = s[k];
+  __syncthreads();
+  const long c = (long)blockIdx.x * 32 + threadIdx.x;
+  if (threadIdx.x >= 32 || c >= n) return;
+  float x = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x += sums[i][threadIdx.x];
+  float* const to = c < a.E ? a.dgamma : a.dbeta;
+  if (to) to[c < a.E ? c : c - a.E] += x;
 }
 
 // ---- rows in registers: a team of TPR threads has a row, a thread NV chunks of 8 features of it ----
@@ -191,28 +209,34 @@ typedef u32x4 __attribute__((aligned(2))) u32x4_any2;
 typedef u32x4 __attribute__((aligned(4))) u32x4_any4;
 typedef u32x2 __attribute__((aligned(1))) u32x2_any;
 
-// chunk c of a row of E features as it lies in memory; a chunk behind the last one is the last one again, what is behind a row's
-// end in the last one is 0
+// chunk c of a row of E features as it lies in memory; what is behind the row's end is 0
 template <typename T> struct Chunk;
 template <> struct Chunk<__bf16> {
   u32x4 w;
   template <bool FULL> __device__ __forceinline__ void load(const __bf16* row, int c, int E) {
-    c = min(c, chunks(E) - 1);
-    if (FULL || V * c + V <= E) {
+    w = u32x4{0u, 0u, 0u, 0u};
+    if (FULL ? c < chunks(E) : V * c + V <= E) {
       w = *(const u32x4_any2*)(row + V * c);
-    } else {
-      w = u32x4{0u, 0u, 0u, 0u};
+    } else if (!FULL) {
 #pragma unroll
       for (int k = 0; k < V; ++k)
         if (V * c + k < E) w[k / 2] |= (unsigned)((const uint16_t*)row)[V * c + k] << (16 * (k % 2));
     }
   }
   __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
+  // the largest magnitude, as the bits of a float32
+  __device__ __forceinline__ unsigned largest() const {
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    u16x2 m = __builtin_bit_cast(u16x2, w[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    const unsigned x = (unsigned)m[0] << 16, y = (unsigned)m[1] << 16;
+    return x > y ? x : y;
+  }
   template <bool FULL> static __device__ __forceinline__ void store(__bf16* row, int c, int E, const float (&v)[V]) {
-    if (c >= chunks(E)) return;
-    if (FULL || V * c + V <= E) {
+    if (FULL ? c < chunks(E) : V * c + V <= E) {
       *(u32x4_any2*)(row + V * c) = u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
-    } else {
+    } else if (!FULL) {
 #pragma unroll
       for (int k = 0; k < V; ++k)
         if (V * c + k < E) row[V * c + k] = (__bf16)v[k];
@@ -222,83 +246,80 @@ template <> struct Chunk<__bf16> {
 template <> struct Chunk<float> {
   u32x4 w[2];
   template <bool FULL> __device__ __forceinline__ void load(const float* row, int c, int E) {
-    c = min(c, chunks(E) - 1);
-    if (FULL || V * c + V <= E) {
+    w[0] = w[1] = u32x4{0u, 0u, 0u, 0u};
+    if (FULL ? c < chunks(E) : V * c + V <= E) {
       w[0] = *(const u32x4_any4*)(row + V * c);
       w[1] = *(const u32x4_any4*)(row + V * c + 4);
-    } else {
+    } else if (!FULL) {
 #pragma unroll
-      for (int k = 0; k < V; ++k) w[k / 4][k % 4] = V * c + k < E ? __float_as_uint(row[V * c + k]) : 0u;
+      for (int k = 0; k < V; ++k)
+        if (V * c + k < E) w[k / 4][k % 4] = __float_as_uint(row[V * c + k]);
     }
   }
   __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i / 4][i % 4]); }
+  __device__ __forceinline__ unsigned largest() const {
+    unsigned m = 0u;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const unsigned x = w[i / 4][i % 4] & 0x7fffffffu;
+      m = m > x ? m : x;
+    }
+    return m;
+  }
   template <bool FULL> static __device__ __forceinline__ void store(float* row, int c, int E, const float (&v)[V]) {
-    if (c >= chunks(E)) return;
-    if (FULL || V * c + V <= E) {
+    if (FULL ? c < chunks(E) : V * c + V <= E) {
       *(u32x4_any4*)(row + V * c) = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
       *(u32x4_any4*)(row + V * c + 4) = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
-    } else {
+    } else if (!FULL) {
 #pragma unroll
       for (int k = 0; k < V; ++k)
         if (V * c + k < E) row[V * c + k] = v[k];
     }
   }
 };
-// whether feature k of chunk c is one
-template <bool FULL> __device__ __forceinline__ bool is_on(int c, int k, int E) { return FULL ? c < chunks(E) : V * c + k < E; }
 
-// 8 packed features and their exponent byte
+// 8 packed features and their exponent byte (behind the row's end: 0 steps)
 struct PackedChunk {
   u32x2 w;
   unsigned b;
   template <bool FULL> __device__ __forceinline__ void load(const int8_t* q, const uint8_t* e, int c, int E) {
-    c = min(c, chunks(E) - 1);
-    if (FULL || V * c + V <= E) {
+    w = u32x2{0u, 0u};
+    b = 8u;
+    if (FULL ? c < chunks(E) : V * c + V <= E) {
       w = *(const u32x2_any*)(q + V * c);
-    } else {
-      w = u32x2{0u, 0u};
+    } else if (!FULL) {
 #pragma unroll
       for (int k = 0; k < V; ++k)
         if (V * c + k < E) w[k / 4] |= (unsigned)(uint8_t)q[V * c + k] << (8 * (k % 4));
     }
-    b = e[c / (packed::GROUP / V)];
+    if (c < chunks(E)) b = e[c / (packed::GROUP / V)];
   }
-  __device__ __forceinline__ void values(float (&v)[V]) const {
-    const float step = packed::step_of(b);
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * step;
-  }
+  __device__ __forceinline__ float step() const { return packed::step_of(b); }
+  __device__ __forceinline__ float operator[](int i) const { return (float)(int8_t)(w[i / 4] >> (8 * (i % 4))); }     // in steps
 };
-// Packs a chunk (all lanes of its group of 32 features take part, with zeros behind the row's end) and puts in its place what the
-// packed form stands for.
-template <bool FULL> __device__ __forceinline__ void pack_chunk(float (&v)[V], int8_t* q, uint8_t* e, int c, int E) {
-  unsigned m = packed::magnitude(v[0]);
-#pragma unroll
-  for (int i = 1; i < V; ++i) {
-    const unsigned x = packed::magnitude(v[i]);
-    m = m > x ? m : x;
-  }
-  const unsigned b = packed::exponent_of(lanes_max<packed::GROUP / V>(m));
-  const float inverse = packed::inverse_step_of(b), step = packed::step_of(b);
+// Packs a chunk (all lanes of its group of 32 features take part): its values in steps, and the step.
+template <bool FULL, typename T> __device__ __forceinline__ float pack_chunk(const Chunk<T>& x, float (&v)[V], int8_t* q, uint8_t* e, int c, int E) {
+  const unsigned b = packed::exponent_of(lanes_max<packed::GROUP / V>(x.largest()));
+  const float inverse = packed::inverse_step_of(b);
   unsigned s[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const float x = packed::steps(b == 255u ? 0.f : v[i], inverse);
-    s[i] = __float_as_uint(x);
-    v[i] = packed::value(x, step);
+    const float y = packed::steps(x[i], inverse);
+    s[i] = __float_as_uint(y);
+    v[i] = y - packed::ROUNDER;
   }
-  if (c >= chunks(E)) return;
-  if (FULL || V * c + V <= E) {
+  if (FULL ? c < chunks(E) : V * c + V <= E) {
     const auto four = [](unsigned s0, unsigned s1, unsigned s2, unsigned s3) {          // their low bytes
       return __builtin_amdgcn_perm(__builtin_amdgcn_perm(s3, s2, 0x0c0c0400), __builtin_amdgcn_perm(s1, s0, 0x0c0c0400), 0x05040100);
     };
     *(u32x2_any*)(q + V * c) = u32x2{four(s[0], s[1], s[2], s[3]), four(s[4], s[5], s[6], s[7])};
-  } else {
+  } else if (!FULL) {
 #pragma unroll
     for (int k = 0; k < V; ++k)
       if (V * c + k < E) q[V * c + k] = (int8_t)(s[k] & 0xffu);
   }
-  if (c % (packed::GROUP / V) == 0) e[c / (packed::GROUP / V)] = (uint8_t)b;
+  if (c < chunks(E) && c % (packed::GROUP / V) == 0) e[c / (packed::GROUP / V)] = (uint8_t)b;
+  return packed::step_of(b);
 }
 
 // Sums over a team.  One wave: by lanes.  More: through LDS, in two places that take turns, with one barrier each: who writes a
@@ -329,13 +350,35 @@ template <int TPR> struct TeamSum {
 };
 constexpr int wg_of(int tpr) { return tpr > WG ? tpr : WG; }
 
+// A team, and the same number in a scalar register (a wave belongs to one team)
+template <int TPR> __device__ __forceinline__ int team_of() { return TPR >= WG ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR); }
+
+// waves per SIMD that the registers are kept for
+constexpr int waves_for(int nv) { return nv <= 2 ? 4 : nv <= 4 ? 2 : 1; }
+
+// The next row is on its way while one is worked on.  Values are v[i][k] * step[i] (packed features: whole steps; others: step 1).
 template <typename T, int SRC, bool FULL, int TPR, int NV>
-__global__ void __launch_bounds__(wg_of(TPR)) norm_fwd_kernel(NormArgs a) {
+__global__ void __launch_bounds__(wg_of(TPR), waves_for(NV)) norm_fwd_kernel(NormArgs a) {
   constexpr int TEAMS = wg_of(TPR) / TPR;
   __shared__ float sums[2][2][16];
   TeamSum<TPR> team_sum{sums};
   const int t = threadIdx.x % TPR, E = a.E;
-  const float inv = 1.f / (float)a.E;
+  const float inv = 1.f / (float)E;
+  struct Row {
+    Chunk<T> x[SRC == 2 ? 1 : NV];
+    PackedChunk p[SRC == 2 ? NV : 1];
+  };
+  auto load = [&](Row& w, long row) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if constexpr (SRC == 2) w.p[i].template load<FULL>(a.q + row * E, a.b + row * packed::groups(E), t + TPR * i, E);
+      else w.x[i].template load<FULL>((const T*)a.x + row * a.x_ss, t + TPR * i, E);
+    }
+  };
+  const long by = (long)gridDim.x * TEAMS;
+  long row = (long)blockIdx.x * TEAMS + team_of<TPR>();
+  Row next;
+  if (row < a.n) load(next, row);
   Chunk<T> gamma[NV], beta[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -343,35 +386,28 @@ __global__ void __launch_bounds__(wg_of(TPR)) norm_fwd_kernel(NormArgs a) {
     if (a.beta) beta[i].template load<FULL>((const T*)a.beta, t + TPR * i, E);
     else beta[i] = Chunk<T>{};
   }
-  for (long row = (long)blockIdx.x * TEAMS + threadIdx.x / TPR; row < a.n; row += (long)gridDim.x * TEAMS) {
-    int8_t* const q = a.q + row * a.E;
-    uint8_t* const e = a.b + row * packed::groups(a.E);
-    float v[NV][V];
-    if constexpr (SRC == 2) {
-      PackedChunk raw[NV];
-#pragma unroll
-      for (int i = 0; i < NV; ++i) raw[i].template load<FULL>(q, e, t + TPR * i, E);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) raw[i].values(v[i]);
-    } else {
-      Chunk<T> raw[NV];
-      const T* const x = (const T*)a.x + row * a.x_ss;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) raw[i].template load<FULL>(x, t + TPR * i, E);
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[i][k] = raw[i][k];
-    }
+  for (; row < a.n; row += by) {
+    const Row w = next;
+    if (row + by < a.n) load(next, row + by);
+    float v[NV][V], step[NV];
     float s[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = t + TPR * i;
+      if constexpr (SRC == 1) {
+        step[i] = pack_chunk<FULL>(w.x[i], v[i], a.q + row * E, a.b + row * packed::groups(E), t + TPR * i, E);
+      } else {
+        if constexpr (SRC == 2) step[i] = w.p[i].step();
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[i][k] = is_on<FULL>(c, k, E) ? v[i][k] : 0.f;
-      if constexpr (SRC == 1) pack_chunk<FULL>(v[i], q, e, c, E);
+        for (int k = 0; k < V; ++k) {
+          if constexpr (SRC == 2) v[i][k] = w.p[i][k];
+          else v[i][k] = w.x[i][k];
+        }
+      }
+      if (SRC == 0) step[i] = 1.f;
+      float c = 0.f;
 #pragma unroll
-      for (int k = 0; k < V; ++k) s[0] += v[i][k];
+      for (int k = 0; k < V; ++k) c += v[i][k];
+      s[0] = SRC == 0 ? s[0] + c : fmaf(c, step[i], s[0]);
     }
     float mu = 0.f;
     if (!a.rms) {
@@ -381,22 +417,25 @@ __global__ void __launch_bounds__(wg_of(TPR)) norm_fwd_kernel(NormArgs a) {
     s[0] = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      const int c = t + TPR * i;
+      float z = 0.f;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        v[i][k] = is_on<FULL>(t + TPR * i, k, E) ? v[i][k] - mu : 0.f;
-        s[0] = fmaf(v[i][k], v[i][k], s[0]);
+        v[i][k] = SRC == 0 ? v[i][k] - mu : fmaf(v[i][k], step[i], -mu);
+        const float d = FULL || V * c + k < E ? v[i][k] : 0.f;
+        z = fmaf(d, d, z);
       }
+      s[0] += c < chunks(E) ? z : 0.f;
     }
     team_sum(s);
     const float r = 1.f / sqrtf(s[0] * inv + a.eps);
     T* const y = (T*)a.y + row * a.y_ss;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = t + TPR * i;
       float o[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) o[k] = fmaf(v[i][k] * r, gamma[i][k], beta[i][k]);
-      Chunk<T>::template store<FULL>(y, c, E, o);
+      Chunk<T>::template store<FULL>(y, t + TPR * i, E, o);
     }
     if (t == 0) {
       a.stats[2 * row] = mu;
@@ -409,12 +448,12 @@ __global__ void __launch_bounds__(wg_of(TPR)) norm_fwd_kernel(NormArgs a) {
 // its rows, the teams of a workgroup are joined in LDS, a workgroup writes one part.  The next row is on its way while one is
 // worked on.
 template <typename T, int SRC, bool FULL, int TPR, int NV, bool PARAM>
-__global__ void __launch_bounds__(wg_of(TPR)) norm_bwd_kernel(NormArgs a) {
+__global__ void __launch_bounds__(wg_of(TPR), TPR > WG ? 2 : waves_for(NV + 1)) norm_bwd_kernel(NormArgs a) {
   constexpr int TEAMS = wg_of(TPR) / TPR;
   __shared__ float sums[2][2][16];
   __shared__ float join[PARAM && TEAMS > 1 ? 2 * TPR * NV * V : 1];
   TeamSum<TPR> team_sum{sums};
-  const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, E = a.E;
+  const int t = threadIdx.x % TPR, team = team_of<TPR>(), E = a.E;
   const float inv = 1.f / (float)a.E;
   struct Row {
     Chunk<T> x[SRC == 2 ? 1 : NV], dy[NV];
@@ -449,20 +488,21 @@ __global__ void __launch_bounds__(wg_of(TPR)) norm_bwd_kernel(NormArgs a) {
   for (; row < a.n; row += step) {
     const Row w = next;
     if (row + step < a.n) load(next, row + step);
+    // (dy is 0 behind the row's end, and with it all that is summed)
     float s[2] = {0.f, 0.f};
     float xh[NV][V];
+    const float shift = -w.mu * w.r;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float v[V];
-      if constexpr (SRC == 2) w.p[i].values(v);
+      float scale = w.r;
+      if constexpr (SRC == 2) scale *= w.p[i].step();
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        if constexpr (SRC != 2) v[k] = w.x[i][k];
-        xh[i][k] = (v[k] - w.mu) * w.r;
+        if constexpr (SRC == 2) xh[i][k] = fmaf(w.p[i][k], scale, shift);
+        else xh[i][k] = fmaf(w.x[i][k], scale, shift);
         const float dy = w.dy[i][k], g = dy * gamma[i][k];
-        const bool on = is_on<FULL>(t + TPR * i, k, E);
-        s[0] += on ? g : 0.f;
-        s[1] = fmaf(on ? g : 0.f, xh[i][k], s[1]);
+        s[0] += g;
+        s[1] = fmaf(g, xh[i][k], s[1]);
         if constexpr (PARAM) {
           pg[i][k] = fmaf(dy, xh[i][k], pg[i][k]);
           pb[i][k] += dy;
@@ -471,15 +511,14 @@ __global__ void __launch_bounds__(wg_of(TPR)) norm_bwd_kernel(NormArgs a) {
     }
     if (a.dx) {                                      // (uniform)
       team_sum(s);
-      const float m = a.rms ? 0.f : s[0] * inv, mx = s[1] * inv;
+      const float m = a.rms ? 0.f : -s[0] * inv * w.r, mx = -s[1] * inv * w.r;
       T* const dx = (T*)a.dx + row * a.x_ss;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int c = t + TPR * i;
         float o[V];
 #pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = w.r * fmaf(-xh[i][k], mx, w.dy[i][k] * gamma[i][k] - m);
-        Chunk<T>::template store<FULL>(dx, c, E, o);
+        for (int k = 0; k < V; ++k) o[k] = fmaf(xh[i][k], mx, fmaf(w.dy[i][k] * gamma[i][k], w.r, m));
+        Chunk<T>::template store<FULL>(dx, t + TPR * i, E, o);
       }
     }
   }
@@ -523,9 +562,7 @@ __global__ void __launch_bounds__(WG) pack_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float v[V];
-#pragma unroll
-      for (int k = 0; k < V; ++k) v[k] = is_on<FULL>(c0 + 64 * i, k, E) ? raw[i][k] : 0.f;
-      pack_chunk<FULL>(v, a.q + row * E, a.b + row * ng, c0 + 64 * i, E);
+      pack_chunk<FULL>(raw[i], v, a.q + row * E, a.b + row * ng, c0 + 64 * i, E);
     }
   }
 }
@@ -539,7 +576,8 @@ __global__ void __launch_bounds__(WG) unpack_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float v[V];
-      raw[i].values(v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = raw[i][k] * raw[i].step();
       Chunk<T>::template store<FULL>((T*)a.y + row * a.y_ss, c0 + 64 * i, E, v);
     }
   }
@@ -559,7 +597,7 @@ template <typename T, bool FULL, int TPR, int NV> void bwd_rows(const NormArgs& 
   if (a.dgamma || a.dbeta) {
     if (a.q) norm_bwd_kernel<T, 2, FULL, TPR, NV, true><<<(unsigned)a.parts, W, 0, s>>>(a);
     else norm_bwd_kernel<T, 0, FULL, TPR, NV, true><<<(unsigned)a.parts, W, 0, s>>>(a);
-    norm_param_sum_kernel<<<(unsigned)((2L * a.E + 15) / 16), WG, 0, s>>>(a);
+    norm_param_sum_kernel<<<(unsigned)((2L * a.E + 31) / 32), WG, 0, s>>>(a);
     return;
   }
   const unsigned grid = grid_of((a.n + W / TPR - 1) / (W / TPR), 8L * a.n_cu);
@@ -572,8 +610,8 @@ template <typename T, bool FULL> hipError_t fwd(const NormArgs& a, hipStream_t s
   const int E = a.E;
   if (E <= 512) fwd_rows<T, FULL, 64, 1>(a, s);
   else if (E <= 1024) fwd_rows<T, FULL, 64, 2>(a, s);
-  else if (E <= 2048) fwd_rows<T, FULL, 64, 4>(a, s);
-  else if (E <= 4096) fwd_rows<T, FULL, 64, 8>(a, s);
+  else if (E <= 2048) fwd_rows<T, FULL, 256, 1>(a, s);
+  else if (E <= 4096) fwd_rows<T, FULL, 256, 2>(a, s);
   else if (E <= 8192) fwd_rows<T, FULL, 256, 4>(a, s);
   else if (E <= 16384) fwd_rows<T, FULL, 256, 8>(a, s);
   else {
@@ -591,14 +629,14 @@ template <typename T, bool FULL> hipError_t bwd(const NormArgs& a, hipStream_t s
   else if (E <= 2048) bwd_rows<T, FULL, 256, 1>(a, s);
   else if (E <= 4096) bwd_rows<T, FULL, 256, 2>(a, s);
   else if (E <= 8192) bwd_rows<T, FULL, 256, 4>(a, s);
-  else if (E <= 16384) bwd_rows<T, FULL, 1024, 2>(a, s);
+  else if (E <= 16384) bwd_rows<T, FULL, 512, 4>(a, s);
   else {
     // (the sums over the rows first: dx may lie where dy does)
     if (a.dgamma || a.dbeta) {
       const dim3 grid((unsigned)((a.E + WG - 1) / WG), (unsigned)a.parts);
       if (a.q) norm_param_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
       else norm_param_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
-      norm_param_sum_kernel<<<(unsigned)((2L * a.E + 15) / 16), WG, 0, s>>>(a);
+      norm_param_sum_kernel<<<(unsigned)((2L * a.E + 31) / 32), WG, 0, s>>>(a);
     }
     if (a.dx) {
       const unsigned grid = grid_of(a.n, 16L * a.n_cu);

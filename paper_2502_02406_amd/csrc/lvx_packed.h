@@ -25,8 +25,8 @@ __device__ __forceinline__ unsigned exponent_of(unsigned largest) {
 __device__ __forceinline__ float step_of(unsigned b) { return b == 255u ? __builtin_nanf("") : __uint_as_float((b - 6u) << 23); }
 __device__ __forceinline__ float inverse_step_of(unsigned b) { return b == 255u ? 0.f : __uint_as_float((260u - b) << 23); }
 
-// x in whole steps (half to even): the sum with 1.5 * 2^23 has no bits below one, and the product is exact.  (A group that reads
-// as NaN: inverse 0; what is not finite becomes 0 by the callers' use of the low byte only.)
+// x in whole steps (half to even): the sum with 1.5 * 2^23 has no bits below one, and the product is exact.  (What the numbers of a
+// group that reads as NaN are says nothing.)
 constexpr float ROUNDER = 12582912.f;
 __device__ __forceinline__ float steps(float x, float inverse) { return fmaf(x, inverse, ROUNDER); }
 __device__ __forceinline__ int8_t whole(float s) { return (int8_t)(__float_as_uint(s) & 0xffu); }
