@@ -53,7 +53,7 @@ typedef enum {
   LVX_ERR_STRIDE = -4,      /* stride too small for the shape, or misaligned for vector access */
   LVX_ERR_MASK = -5,        /* mask geometry does not cover Sq x Skv */
   LVX_ERR_WORKSPACE = -6,   /* workspace NULL, misaligned or smaller than required */
-  LVX_ERR_UNSUPPORTED = -7, /* head dim other than 64 / 96 / 128; projection shape the bf16 kernel does not take */
+  LVX_ERR_UNSUPPORTED = -7, /* head dim other than 64 / 96 / 128; projection or loss shape the bf16 kernel does not take */
   LVX_ERR_HIP = -8          /* a kernel launch failed (hipGetLastError) */
 } lvx_status;
 
@@ -309,6 +309,40 @@ size_t lvx_norm_workspace_bytes(int64_t n, int32_t E);
 lvx_status lvx_norm_bwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const lvx_packed* packed, const void* gamma,
                         const float* stats, const void* dy, void* dx, float* dgamma, float* dbeta, void* workspace,
                         size_t workspace_bytes, void* hip_stream);
+
+/* Softmax cross entropy of n tokens against a vocabulary of V entries, whose logits z = x w^T are never kept:
+ *     lse[i] = ln sum_v exp z[i, v],   loss[i] = lse[i] - z[i, labels[i]].
+ * x       device, n rows of E features of `dtype`, x_ss elements apart.
+ * w       device, [V, E] of `dtype`, contiguous: one row of weights per entry, the layout of lvx_xattn_project's w.
+ * labels  device, [n] int64.  A negative label: the token takes no part (loss 0, lse 0, no gradient; its features may hold
+ *         anything, NaN included).  V or more: loss and lse are NaN, and the gradients that the token is in.
+ * loss, lse   device, [n] float32, overwritten.
+ * A token with a NaN logit or one of +infinity has a NaN loss; logits of -infinity count as 0.
+ * LVX_BF16 runs on the matrix cores (exact products, float32 sums) and needs E % 64 == 0 (LVX_ERR_UNSUPPORTED otherwise), 16-byte
+ * aligned pointers and x_ss % 8 == 0; n and V are arbitrary.  LVX_F32 takes any E and alignment.  n * x_ss may not pass 2^31
+ * (LVX_ERR_STRIDE): larger batches go in several calls.
+ * workspace   of lvx_xent_workspace_bytes(n, E, V, dtype) (0: invalid sizes), for either pass; it also serves fewer tokens, fewer
+ *         features and smaller vocabularies.  lvx_xent_bwd takes less, down to pieces of 256 entries of the vocabulary, and is slower. */
+typedef struct {
+  int64_t n, V;             /* tokens, entries of the vocabulary */
+  int32_t E;                /* features */
+  int64_t x_ss;             /* elements from one row of x (and dx) to the next */
+} lvx_xent;
+size_t lvx_xent_workspace_bytes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype);
+lvx_status lvx_xent_fwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, float* loss, float* lse,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients, with the logits made again piece by piece of the vocabulary:
+ *     g[i, v] = (exp(z[i, v] - lse[i]) - [v == labels[i]]) d_loss[i],   dx[i] = sum_v g[i, v] w[v],   dw[v] = sum_i g[i, v] x[i].
+ * lse     what lvx_xent_fwd left for the same x, w and labels.
+ * d_loss  device, [n] float32: the gradient of every token's loss (1 / number of labels for their mean); not read where the label
+ *         is negative.
+ * dx      `dtype`, x's strides, OVERWRITTEN (0 for tokens without a label); may not be x; NULL = not wanted.
+ * dw      `dtype`, [V, E], contiguous, OVERWRITTEN: unlike lvx_xattn_project_bwd's, every row of w is in one call only, and g is
+ *         rounded to `dtype` before it is multiplied, which float32 sums would not undo; NULL = not wanted.  At least one must be given.
+ * Sums are float32, in a fixed order: results repeat bit for bit. */
+lvx_status lvx_xent_bwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, const float* lse,
+                        const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Human-readable name of a status code (static storage). */
 const char* lvx_strerror(lvx_status s);

@@ -27,7 +27,8 @@ LVX_STATIC_SCRATCH_BYTES = 64 << 20
 
 EXPORTS = ("lvx_xattn_workspace_bytes", "lvx_xattn_fwd", "lvx_xattn_fwd_static", "lvx_xattn_fwd_merge", "lvx_xattn_fwd_merge_last", "lvx_xattn_merge", "lvx_xattn_bwd",
            "lvx_xattn_bwd_stages", "lvx_xattn_bwd_visit", "lvx_xattn_bwd_error_word", "lvx_xattn_dq_finalize", "lvx_xattn_project", "lvx_xattn_project_bwd",
-           "lvx_pack", "lvx_unpack", "lvx_norm_fwd", "lvx_norm_workspace_bytes", "lvx_norm_bwd", "lvx_strerror")
+           "lvx_pack", "lvx_unpack", "lvx_norm_fwd", "lvx_norm_workspace_bytes", "lvx_norm_bwd",
+           "lvx_xent_workspace_bytes", "lvx_xent_fwd", "lvx_xent_bwd", "lvx_strerror")
 
 
 class LvxError(RuntimeError):
@@ -58,6 +59,10 @@ class lvx_projection(C.Structure):
 class lvx_norm(C.Structure):
     _fields_ = [("n", C.c_int64), ("E", C.c_int32), ("rms", C.c_int32), ("x_ss", C.c_int64), ("y_ss", C.c_int64),
                 ("eps", C.c_float)]
+
+
+class lvx_xent(C.Structure):
+    _fields_ = [("n", C.c_int64), ("V", C.c_int64), ("E", C.c_int32), ("x_ss", C.c_int64)]
 
 
 class lvx_packed(C.Structure):
@@ -124,6 +129,11 @@ def load() -> C.CDLL:
         lib.lvx_norm_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
         lib.lvx_norm_bwd.argtypes = [C.POINTER(lvx_norm), C.c_int, C.c_void_p, C.POINTER(lvx_packed)] + [C.c_void_p] * 7 + \
                                     [C.c_size_t, C.c_void_p]
+        lib.lvx_xent_workspace_bytes.restype = C.c_size_t
+        lib.lvx_xent_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int64, C.c_int]
+        lib.lvx_xent_fwd.restype = lib.lvx_xent_bwd.restype = C.c_int
+        lib.lvx_xent_fwd.argtypes = [C.POINTER(lvx_xent), C.c_int] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+        lib.lvx_xent_bwd.argtypes = [C.POINTER(lvx_xent), C.c_int] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
         lib.lvx_strerror.restype = C.c_char_p
         lib.lvx_strerror.argtypes = [C.c_int]
         _lib = lib
@@ -519,3 +529,50 @@ def lvx_norm_bwd(x, gamma, stats, d_y, dx=None, dgamma=None, dbeta=None, workspa
     _check(load().lvx_norm_bwd(C.byref(p), dtype_code(d_y.dtype), at(x), C.byref(pk) if pk is not None else None, gamma.data_ptr(),
                                stats.data_ptr(), d_y.data_ptr(), at(dx), at(dgamma), at(dbeta), at(workspace),
                                workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), w)
+
+
+# ---- the loss over a vocabulary ----
+
+def lvx_xent_workspace_bytes(n: int, E: int, V: int, dtype: int) -> int:
+    return int(load().lvx_xent_workspace_bytes(n, E, V, dtype))
+
+
+def _xent_struct(where, x, w, labels, per_token, workspace):
+    """Sizes of a loss call; per_token: the float32 [n] tensors of it."""
+    n, E, x_ss = _token_rows(x, "x")
+    if w.dim() != 2 or w.shape[1] != E or w.dtype != x.dtype or not w.is_contiguous():
+        raise ValueError(f"{where}: w has to be [V, {E}] of x's type, contiguous")
+    if labels.numel() != n or labels.dtype != torch.int64 or not labels.is_contiguous():
+        raise ValueError(f"{where}: labels have to be int64 [{n}], contiguous")
+    for t in per_token:
+        if t.numel() != n or t.dtype != torch.float32 or not t.is_contiguous():
+            raise ValueError(f"{where}: loss, lse and d_loss have to be float32 [{n}], contiguous")
+    if not workspace.is_contiguous():
+        raise ValueError(f"{where}: the workspace has to be contiguous")
+    return lvx_xent(n, w.shape[0], E, x_ss)
+
+
+def lvx_xent_fwd(x, w, labels, loss, lse, workspace) -> None:
+    """loss and lse (float32, one value for every token) are overwritten with the cross entropy of x [n, E] or [B, S, E] against the
+    vocabulary's weights w [V, E]; tokens with a negative label (int64) take no part."""
+    _on_device("lvx_xent_fwd", x, w, labels, loss, lse, workspace)
+    p = _xent_struct("lvx_xent_fwd", x, w, labels, (loss, lse), workspace)
+    _check(load().lvx_xent_fwd(C.byref(p), dtype_code(x.dtype), x.data_ptr(), w.data_ptr(), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(),
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), "lvx_xent_fwd")
+
+
+def lvx_xent_bwd(x, w, labels, lse, d_loss, dx=None, dw=None, workspace=None) -> None:
+    """dx (x's shape, strides and type) and dw (w's) are overwritten with the gradients; either may be None.  lse: what lvx_xent_fwd left;
+    d_loss: the gradient of every token's loss."""
+    where = "lvx_xent_bwd"
+    if workspace is None or (dx is None and dw is None):
+        raise ValueError(f"{where}: no workspace, or nothing asked for")
+    _on_device(where, x, w, labels, lse, d_loss, dx, dw, workspace)
+    p = _xent_struct(where, x, w, labels, (lse, d_loss), workspace)
+    if dx is not None and (dx.shape != x.shape or dx.dtype != x.dtype or _token_rows(dx, "dx")[2] != p.x_ss):
+        raise ValueError(f"{where}: dx has to have x's shape, strides and type")
+    if dw is not None and (dw.shape != w.shape or dw.dtype != w.dtype or not dw.is_contiguous()):
+        raise ValueError(f"{where}: dw has to be [{p.V}, {p.E}] of w's type, contiguous")
+    _check(load().lvx_xent_bwd(C.byref(p), dtype_code(x.dtype), x.data_ptr(), w.data_ptr(), labels.data_ptr(), lse.data_ptr(), d_loss.data_ptr(),
+                               dx.data_ptr() if dx is not None else None, dw.data_ptr() if dw is not None else None,
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), where)

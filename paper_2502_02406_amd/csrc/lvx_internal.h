@@ -199,6 +199,37 @@ hipError_t launch_norm_bwd(const NormArgs& a, int is_f32, hipStream_t s);
 hipError_t launch_pack(const NormArgs& a, int is_f32, hipStream_t s);
 hipError_t launch_unpack(const NormArgs& a, int is_f32, hipStream_t s);     // to y
 
+// Cross entropy against a vocabulary (lvx_xent.hip).
+struct XentArgs {
+  const void* x;        // [n, E], row stride ldx elements
+  const void* w;        // [V, E] contiguous
+  const int64_t* labels;        // [n]
+  float *loss, *lse_out;        // [n] (forward)
+  const float *lse, *d_loss;    // [n] (backward)
+  void *dx, *dw;        // like x, like w; or null
+  long n, ldx, V;
+  int E, n_cu;
+  // workspace
+  int* count;           // how many tokens have a label,
+  int *tok, *lab;       // [n]: which, in order, and their labels (-1: not in the vocabulary)
+  long Mp;              // n rounded up to 256
+  float2* part;         // forward, [xent_stat_parts][Mp]: largest logit (times log2 e) and sum of exponentials
+  float* zlab;          // forward, [n]: the label's logit
+  void* g;              // backward, [Mp][g_pitch] of x's type: the logits' gradient of a piece of the vocabulary
+  long g_pitch, piece;  // columns of a piece; a row of g has as many, rounded up to 256
+  float* dx_part;       // backward, [parts] sums of dx
+  int parts;            // workgroups that share a tile of dx
+  // set by the launches
+  long v0, v1;          // the piece at hand
+  int first;            // whether it is the first one
+  long grid_part;       // workgroups of one part
+};
+bool xent_bf16_supported(int E);
+int xent_stat_parts(long V, int is_f32);
+int xent_dx_parts(long n, int E, int n_cu, int is_f32);   // of a roomy workspace
+hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s);
+hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s);
+
 int device_cu_count();   // of the first device asked for (256 where there is none)
 
 // Bytes of workspace that lvx_xattn_fwd needs for exactly this call (with this mask or without

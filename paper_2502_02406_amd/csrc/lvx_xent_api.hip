@@ -1,0 +1,120 @@
+// C ABI of the cross entropy against a vocabulary (see include/lvx.h): argument validation on the host, workspace carving, and
+// launches on the caller's stream.
+#include "../../include/lvx.h"
+#include "lvx_internal.h"
+
+using namespace lvx;
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+bool aligned(const void* p, size_t by) { return (uintptr_t)p % by == 0; }
+
+lvx_status check_sizes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
+  if (dtype != LVX_F32 && dtype != LVX_BF16) return LVX_ERR_DTYPE;
+  if (n < 1 || E < 1 || V < 1 || n > (1 << 30) || V > (1 << 30) || E > (1 << 20)) return LVX_ERR_SHAPE;
+  if (dtype == LVX_BF16 && !xent_bf16_supported(E)) return LVX_ERR_UNSUPPORTED;
+  return LVX_OK;
+}
+
+// The workspace: the list of tokens; then (forward) what the tiles leave, or (backward) dx's sums and the gradient of a piece of the logits.
+// `parts` of dx's sums, 0: as many as the launch would like.
+struct Plan { size_t tok, lab, zlab, part, fwd, dx, g, row; int64_t Mp; int parts; };
+Plan plan_of(int64_t n, int32_t E, int64_t V, lvx_dtype dtype, int parts = 0) {
+  const int f32 = dtype == LVX_F32;
+  Plan p;
+  p.parts = parts > 0 ? parts : xent_dx_parts(n, E, device_cu_count(), f32);
+  p.Mp = (n + 255) / 256 * 256;
+  p.tok = ALIGN;
+  p.lab = p.tok + align_up(n * 4);
+  p.zlab = p.lab + align_up(n * 4);
+  p.part = p.dx = p.zlab + align_up(n * 4);
+  p.fwd = p.part + (size_t)xent_stat_parts(V, f32) * p.Mp * sizeof(float2);
+  p.g = p.dx + align_up((size_t)p.parts * p.Mp * ((E + 255) / 256 * 256) * sizeof(float));
+  p.row = (size_t)p.Mp * (f32 ? 4 : 2);                // bytes of a column of the logits' gradient
+  return p;
+}
+// Columns of a piece of the vocabulary: as many as the last-level cache holds half full of, but 8192 at least, since the sums of
+// dx go through memory once a piece.
+int64_t piece_of(const Plan& p, int64_t V) {
+  int64_t piece = (int64_t)((128u << 20) / p.row) / 256 * 256;
+  if (piece < 8192) piece = 8192;
+  if (piece > (1 << 18)) piece = 1 << 18;
+  const int64_t whole = (V + 255) / 256 * 256;
+  return piece < whole ? piece : whole;
+}
+
+lvx_status xent_args(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, void* workspace,
+                     XentArgs* a, Plan* plan) {
+  if (!p || !x || !w || !labels) return LVX_ERR_NULL;
+  const lvx_status st = check_sizes(p->n, p->E, p->V, dtype);
+  if (st != LVX_OK) return st;
+  const size_t el = dtype == LVX_F32 ? 4 : 2;
+  if (p->x_ss < p->E || p->n * (double)p->x_ss > 2147483648.0) return LVX_ERR_STRIDE;
+  if (dtype == LVX_BF16 ? !aligned(x, 16) || !aligned(w, 16) || p->x_ss % 8 != 0 : !aligned(x, el) || !aligned(w, el)) return LVX_ERR_STRIDE;
+  if (!aligned(labels, 8)) return LVX_ERR_STRIDE;
+  if (!workspace || !aligned(workspace, ALIGN)) return LVX_ERR_WORKSPACE;
+  *plan = plan_of(p->n, p->E, p->V, dtype);
+  *a = XentArgs{};
+  a->x = x; a->w = w; a->labels = labels;
+  a->n = p->n; a->ldx = p->x_ss; a->V = p->V; a->E = p->E; a->n_cu = device_cu_count();
+  const auto at = [&](size_t o) -> char* { return (char*)workspace + o; };
+  a->count = (int*)workspace;
+  a->tok = (int*)at(plan->tok); a->lab = (int*)at(plan->lab); a->zlab = (float*)at(plan->zlab);
+  a->part = (float2*)at(plan->part); a->dx_part = (float*)at(plan->dx); a->g = at(plan->g);
+  a->Mp = plan->Mp;
+  return LVX_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lvx_xent_workspace_bytes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
+  if (check_sizes(n, E, V, dtype) != LVX_OK) return 0;
+  const Plan p = plan_of(n, E, V, dtype);
+  const size_t bwd = p.g + (size_t)piece_of(p, V) * p.row;
+  return align_up(p.fwd > bwd ? p.fwd : bwd);
+}
+
+lvx_status lvx_xent_fwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, float* loss, float* lse,
+                        void* workspace, size_t workspace_bytes, void* hip_stream) {
+  XentArgs a;
+  Plan plan;
+  if (!loss || !lse) return LVX_ERR_NULL;
+  const lvx_status st = xent_args(p, dtype, x, w, labels, workspace, &a, &plan);
+  if (st != LVX_OK) return st;
+  if (!aligned(loss, 4) || !aligned(lse, 4)) return LVX_ERR_STRIDE;
+  if (workspace_bytes < plan.fwd) return LVX_ERR_WORKSPACE;
+  a.loss = loss; a.lse_out = lse;
+  return launch_xent_fwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
+}
+
+lvx_status lvx_xent_bwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, const float* lse,
+                        const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  XentArgs a;
+  Plan plan;
+  if (!lse || !d_loss || (!dx && !dw)) return LVX_ERR_NULL;
+  const lvx_status st = xent_args(p, dtype, x, w, labels, workspace, &a, &plan);
+  if (st != LVX_OK) return st;
+  const size_t out = dtype == LVX_F32 ? 4 : 16;
+  if (!aligned(lse, 4) || !aligned(d_loss, 4) || !aligned(dx, out) || !aligned(dw, out) || dx == x) return LVX_ERR_STRIDE;
+  // the piece that there is room for: fewer sums of dx first, then fewer columns (what was made for more tokens or features may
+  // hold fewer of these sums: 2304 tokens want one, 2048 two)
+  int64_t piece = piece_of(plan, p->V), room = 0;
+  for (;;) {
+    room = workspace_bytes > plan.g ? (int64_t)((workspace_bytes - plan.g) / plan.row) / 256 * 256 : 0;
+    if (room >= piece || plan.parts == 1) break;
+    plan = plan_of(p->n, p->E, p->V, dtype, plan.parts - 1);
+  }
+  if (piece > room) piece = room;
+  if (piece < 256) return LVX_ERR_WORKSPACE;
+  a.g = (char*)workspace + plan.g;
+  a.parts = plan.parts;
+  a.piece = a.g_pitch = piece;
+  a.lse = lse; a.d_loss = d_loss; a.dx = dx; a.dw = dw;
+  return launch_xent_bwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
+}
+
+}  // extern "C"
