@@ -200,6 +200,11 @@ hipError_t launch_pack(const NormArgs& a, int is_f32, hipStream_t s);
 hipError_t launch_unpack(const NormArgs& a, int is_f32, hipStream_t s);     // to y
 
 // Cross entropy against a vocabulary (lvx_xent.hip).
+struct XentHead {       // what the first launch of a call finds out
+  int count;            // tokens that have a label
+  int parts;            // workgroups that share a tile of dx
+  float scale;          // the largest |d_loss|: the logits' gradient is kept divided by it
+};
 struct XentArgs {
   const void* x;        // [n, E], row stride ldx elements
   const void* w;        // [V, E] contiguous
@@ -210,23 +215,24 @@ struct XentArgs {
   long n, ldx, V;
   int E, n_cu;
   // workspace
-  int* count;           // how many tokens have a label,
-  int *tok, *lab;       // [n]: which, in order, and their labels (-1: not in the vocabulary)
+  XentHead* head;
+  int *tok, *lab;       // [n]: the tokens that have a label, in order, and their labels (-1: not in the vocabulary)
   long Mp;              // n rounded up to 256
   float2* part;         // forward, [xent_stat_parts][Mp]: largest logit (times log2 e) and sum of exponentials
   float* zlab;          // forward, [n]: the label's logit
   void* g;              // backward, [Mp][g_pitch] of x's type: the logits' gradient of a piece of the vocabulary
   long g_pitch, piece;  // columns of a piece; a row of g has as many, rounded up to 256
-  float* dx_part;       // backward, [parts] sums of dx
-  int parts;            // workgroups that share a tile of dx
+  float* dx_part;       // backward, [slots] tiles of sums of dx
+  int slots;
   // set by the launches
   long v0, v1;          // the piece at hand
   int first;            // whether it is the first one
-  long grid_part;       // workgroups of one part
+  int tile;             // edge of a tile of dx
 };
 bool xent_bf16_supported(int E);
 int xent_stat_parts(long V, int is_f32);
-int xent_dx_parts(long n, int E, int n_cu, int is_f32);   // of a roomy workspace
+long xent_dx_slots(long n, int E, int n_cu, int is_f32);
+size_t xent_dx_slot_bytes(int is_f32);
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s);
 

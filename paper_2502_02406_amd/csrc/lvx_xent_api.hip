@@ -19,19 +19,18 @@ lvx_status check_sizes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
 }
 
 // The workspace: the list of tokens; then (forward) what the tiles leave, or (backward) dx's sums and the gradient of a piece of the logits.
-// `parts` of dx's sums, 0: as many as the launch would like.
-struct Plan { size_t tok, lab, zlab, part, fwd, dx, g, row; int64_t Mp; int parts; };
-Plan plan_of(int64_t n, int32_t E, int64_t V, lvx_dtype dtype, int parts = 0) {
+struct Plan { size_t tok, lab, zlab, part, fwd, dx, g, row; int64_t Mp, slots; };
+Plan plan_of(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
   const int f32 = dtype == LVX_F32;
   Plan p;
-  p.parts = parts > 0 ? parts : xent_dx_parts(n, E, device_cu_count(), f32);
+  p.slots = xent_dx_slots(n, E, device_cu_count(), f32);
   p.Mp = (n + 255) / 256 * 256;
   p.tok = ALIGN;
   p.lab = p.tok + align_up(n * 4);
   p.zlab = p.lab + align_up(n * 4);
   p.part = p.dx = p.zlab + align_up(n * 4);
   p.fwd = p.part + (size_t)xent_stat_parts(V, f32) * p.Mp * sizeof(float2);
-  p.g = p.dx + align_up((size_t)p.parts * p.Mp * ((E + 255) / 256 * 256) * sizeof(float));
+  p.g = p.dx + align_up((size_t)p.slots * xent_dx_slot_bytes(f32));
   p.row = (size_t)p.Mp * (f32 ? 4 : 2);                // bytes of a column of the logits' gradient
   return p;
 }
@@ -41,8 +40,8 @@ int64_t piece_of(const Plan& p, int64_t V) {
   int64_t piece = (int64_t)((128u << 20) / p.row) / 256 * 256;
   if (piece < 8192) piece = 8192;
   if (piece > (1 << 18)) piece = 1 << 18;
-  const int64_t whole = (V + 255) / 256 * 256;
-  return piece < whole ? piece : whole;
+  const int64_t pieces = (V + piece - 1) / piece;      // (even ones)
+  return ((V + pieces - 1) / pieces + 255) / 256 * 256;
 }
 
 lvx_status xent_args(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, void* workspace,
@@ -60,10 +59,11 @@ lvx_status xent_args(const lvx_xent* p, lvx_dtype dtype, const void* x, const vo
   a->x = x; a->w = w; a->labels = labels;
   a->n = p->n; a->ldx = p->x_ss; a->V = p->V; a->E = p->E; a->n_cu = device_cu_count();
   const auto at = [&](size_t o) -> char* { return (char*)workspace + o; };
-  a->count = (int*)workspace;
+  a->head = (XentHead*)workspace;
   a->tok = (int*)at(plan->tok); a->lab = (int*)at(plan->lab); a->zlab = (float*)at(plan->zlab);
   a->part = (float2*)at(plan->part); a->dx_part = (float*)at(plan->dx); a->g = at(plan->g);
   a->Mp = plan->Mp;
+  a->slots = (int)plan->slots;
   return LVX_OK;
 }
 
@@ -100,18 +100,11 @@ lvx_status lvx_xent_bwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const
   if (st != LVX_OK) return st;
   const size_t out = dtype == LVX_F32 ? 4 : 16;
   if (!aligned(lse, 4) || !aligned(d_loss, 4) || !aligned(dx, out) || !aligned(dw, out) || dx == x) return LVX_ERR_STRIDE;
-  // the piece that there is room for: fewer sums of dx first, then fewer columns (what was made for more tokens or features may
-  // hold fewer of these sums: 2304 tokens want one, 2048 two)
-  int64_t piece = piece_of(plan, p->V), room = 0;
-  for (;;) {
-    room = workspace_bytes > plan.g ? (int64_t)((workspace_bytes - plan.g) / plan.row) / 256 * 256 : 0;
-    if (room >= piece || plan.parts == 1) break;
-    plan = plan_of(p->n, p->E, p->V, dtype, plan.parts - 1);
-  }
+  // the piece that there is room for
+  int64_t piece = piece_of(plan, p->V);
+  const int64_t room = workspace_bytes > plan.g ? (int64_t)((workspace_bytes - plan.g) / plan.row) / 256 * 256 : 0;
   if (piece > room) piece = room;
   if (piece < 256) return LVX_ERR_WORKSPACE;
-  a.g = (char*)workspace + plan.g;
-  a.parts = plan.parts;
   a.piece = a.g_pitch = piece;
   a.lse = lse; a.d_loss = d_loss; a.dx = dx; a.dw = dw;
   return launch_xent_bwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;

@@ -109,7 +109,9 @@ def test_small_workspace_and_parts_left_out(dtype):
     ref, tol = reference(*args, dtype)
     el, Mp = (2 if dtype == "bf16" else 4), 512
     up = lambda v: (v + 255) // 256 * 256
-    least = 256 + 3 * up(4 * n) + Mp * up(E) * 4 + 256 * Mp * el
+    edge = 128 if dtype == "f32" else 256
+    tiles = -(-n // edge) * -(-E // edge)
+    least = 256 + 3 * up(4 * n) + max(tiles, min(16 * tiles, 2 * torch.cuda.get_device_properties(0).multi_processor_count)) * edge * edge * 4 + 256 * Mp * el
     check(run(*args, ws_bytes=least), ref, tol, "pieces of 256")
     with pytest.raises(B.LvxError):
         run(*args, ws_bytes=least - 256)
