@@ -227,12 +227,12 @@ struct XentArgs {
   // set by the launches
   long v0, v1;          // the piece at hand
   int first;            // whether it is the first one
-  int tile;             // edge of a tile of dx
+  int tile, tile_rows;  // columns and rows of a tile of dx
 };
 bool xent_bf16_supported(int E);
 int xent_stat_parts(long V, int is_f32);
 long xent_dx_slots(long n, int E, int n_cu, int is_f32);
-size_t xent_dx_slot_bytes(int is_f32);
+size_t xent_dx_bytes(long n, int E, int n_cu, int is_f32);
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s);
 

@@ -70,18 +70,17 @@ template <int MODE> __device__ __forceinline__ bool take_tile(int n_rt, int n_ct
   return true;
 }
 // Parts that the contraction of dx is cut into, by how many tiles the listed tokens make: as many as make the rounds of workgroups
-// shortest, within the room for their sums.
-__device__ inline int dx_parts(long tiles, int n_cu, int slots) {
-  int best = 1;
-  float best_t = 1e30f;
-  for (int p = 1; p <= 16 && p * tiles <= slots; ++p) {
-    const float t = (float)((tiles * p + n_cu - 1) / n_cu) / (float)p;
-    if (t < 0.95f * best_t) {
-      best = p;
-      best_t = t;
-    }
+// shortest, within the room for their sums.  (The first 16 lanes try one number each; `at`: 16 floats of LDS.)
+__device__ inline int dx_parts(int tiles, int n_cu, int slots, float* at) {
+  if (threadIdx.x < 16) {
+    const int p = threadIdx.x + 1;
+    at[threadIdx.x] = p * tiles <= slots ? (float)((tiles * p + n_cu - 1) / n_cu) / (float)p : 1e30f;
   }
-  return best;
+  __syncthreads();
+  int best = 0;
+  for (int p = 1; p < 16; ++p)
+    if (at[p] < 0.95f * at[best]) best = p;
+  return best + 1;
 }
 
 // ---- the tokens that have a label, in order: tok[i] and its label (-1: not in the vocabulary), and how many they are ----
@@ -93,11 +92,13 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
   float top = 0.f;                                   // the largest finite |d_loss|
   for (long base = 0; base < a.n; base += 8192) {
     long lab[8];
+    float d[8];
     int mine = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const long i = base + 8 * tid + k;
       lab[k] = i < a.n ? a.labels[i] : -1;
+      d[k] = a.d_loss && i < a.n ? fabsf(a.d_loss[i]) : 0.f;
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) mine += lab[k] >= 0 ? 1 : 0;
@@ -123,10 +124,7 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
         a.tok[at] = (int)i;
         a.lab[at] = lab[k] < a.V ? (int)lab[k] : -1;
         ++at;
-        if (a.d_loss) {
-          const float d = fabsf(a.d_loss[i]);
-          if (d > top && d < __builtin_inff()) top = d;
-        }
+        if (d[k] > top && d[k] < __builtin_inff()) top = d[k];
       } else if (a.loss && i < a.n) {
         a.loss[i] = 0.f;
         a.lse_out[i] = 0.f;
@@ -137,11 +135,13 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
   for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
   if (lane == 0) tops[wave] = top;
   __syncthreads();
+  __shared__ float tries[16];
+  const int parts = dx_parts((total + a.tile_rows - 1) / a.tile_rows * ((a.E + a.tile - 1) / a.tile), a.n_cu, a.slots, tries);
   if (tid != 0) return;
   for (int w = 0; w < 16; ++w) top = fmaxf(top, tops[w]);
   a.head->count = total;
   a.head->scale = top > 0.f ? top : 1.f;
-  a.head->parts = dx_parts((long)((total + a.tile - 1) / a.tile) * ((a.E + a.tile - 1) / a.tile), a.n_cu, a.slots);
+  a.head->parts = parts;
 }
 
 // ---- a wave's columns of a logits tile.  z(v, j): the logit in column 32 j + 8 (v / 4) + 4 g + v % 4 of the wave's, JB blocks of 32 ----
@@ -188,6 +188,11 @@ template <int JB, class Z> __device__ __forceinline__ float tile_pick(int g, int
   return y;
 }
 
+__device__ __forceinline__ void join_stats(float* m, float* s, float m1, float s1) {
+  const float top = fmaxf(*m, m1), at = top == -__builtin_inff() ? 0.f : top;
+  *s = *s * exp2_fast(*m - at) + s1 * exp2_fast(m1 - at);
+  *m = top;
+}
 // lse and loss of the listed tokens from what the tiles' waves left: 8 tokens a workgroup, 32 threads each
 __global__ void __launch_bounds__(256) xent_join_kernel(XentArgs a, int n_parts) {
   __shared__ float sm[8][33], ss[8][33];
@@ -195,11 +200,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(XentArgs a, int n_parts)
   for (int r0 = blockIdx.x * 8; r0 < count; r0 += gridDim.x * 8) {
     const int r = min(r0 + row_l, count - 1);
     float m = -__builtin_inff(), s = 0.f;
-    const auto join = [&](float m1, float s1) {
-      const float top = fmaxf(m, m1), at = top == -__builtin_inff() ? 0.f : top;
-      s = s * exp2_fast(m - at) + s1 * exp2_fast(m1 - at);
-      m = top;
-    };
+    const auto join = [&](float m1, float s1) { join_stats(&m, &s, m1, s1); };
     for (int p0 = lane; p0 < n_parts; p0 += 32 * 8) {
       float2 v[8];
 #pragma unroll
@@ -238,7 +239,7 @@ template <int MODE, int RB>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 xent_bf16_kernel(XentArgs a) {
   constexpr bool LOGITS = MODE == STATS || MODE == GRAD;
-  static_assert(RB == 4 || LOGITS, "the low tiles are for logits of few tokens");
+  static_assert(RB == 4 || (RB == 2 && MODE != DW), "the low tiles are for few tokens");
   constexpr int TR = 64 * RB;                        // rows of a workgroup's tile
   constexpr int NB = MODE == DW ? 8 : 2 * RB;        // copies per wave and tile pair: B side (rows),
   constexpr int NPART = 8 + NB;                      // and with the 8 of the A side (columns)
@@ -455,7 +456,7 @@ xent_bf16_kernel(XentArgs a) {
     }
   } else if constexpr (MODE == DX) {
     // in the order of the registers, 16 bytes a lane (xent_dx_kernel reads them so), on top of what the pieces before left
-    float* const out = a.dx_part + (((long)part * n_rt + rt) * n_ct + ct) * (T * T) + wave * (T * T / 4) + lane * 4;
+    float* const out = a.dx_part + (((long)part * n_rt + rt) * n_ct + ct) * (TR * T) + wave * (TR * T / 4) + lane * 4;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       f32x4 old[RB][4];
@@ -534,16 +535,142 @@ xent_bf16_kernel(XentArgs a) {
   }
 }
 
+// Logits of at most 64 tokens: bound by reading w.  A workgroup takes 128 entries of the vocabulary, a wave 32 of them against 32 RB tokens, and
+// NS slots of 64 features are on their way (of w alone, 16 KB each; two-slot tiles of 256 entries kept half of the compute units
+// waiting, 16 tokens x 4096 against 32768: 85 -> 66 us).  Six slots where the workgroups have a compute unit each, three where two share
+// one.  Behind the last features the copies go on with these again, so that every step waits for the same number.
+template <int MODE, int RB, int NS>
+__global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
+  constexpr int CT = 128, A_B = CT * RK_ROWB, B_B = 32 * RB * RK_ROWB, S_B = A_B + B_B, NP = 4 + RB;
+  constexpr int W_PITCH = 32 * 2 + 16, W_B = 32 * RB * W_PITCH;      // GRAD: a wave's rows on their way out
+  static_assert(4 * W_B <= NS * S_B, "they fit the slots");
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int M = a.head->count, E = a.E, cols = (int)(a.v1 - a.v0), nk = E / BK;
+  if (M == 0) return;
+  const int c0 = blockIdx.x * CT;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned xrow_b = (unsigned)(a.ldx * 2), wrow_b = (unsigned)(E * 2);
+  const unsigned smem_u = lds_base(smem);
+  unsigned ao[4], bo[RB];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = 32 * wave + 8 * j + (lane >> 3);
+    ao[j] = (unsigned)min((long)r, a.V - 1 - a.v0 - c0) * wrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + (lane >> 3)));
+  }
+#pragma unroll
+  for (int j = 0; j < RB; ++j) {
+    const int r = 8 * RB * wave + 8 * j + (lane >> 3);
+    bo[j] = (unsigned)a.tok[min(r, M - 1)] * xrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(r));
+  }
+  const char* const wg = (const char*)a.w + (a.v0 + c0) * wrow_b;
+  const auto issue = [&](int kt, int slot) __attribute__((always_inline)) {
+    const long k_b = (long)min(kt, nk - 1) * RK_ROWB;
+    const unsigned st = smem_u + (unsigned)(slot * S_B);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dma16u(wg + k_b, ao[j], st + (unsigned)((32 * wave + 8 * j) * RK_ROWB));
+#pragma unroll
+    for (int j = 0; j < RB; ++j) dma16u((const char*)a.x + k_b, bo[j], st + (unsigned)(A_B + (8 * RB * wave + 8 * j) * RK_ROWB));
+  };
+  f32x16 acc[RB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i) acc[i] = zero16();
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) issue(s, s);
+  int slot = 0, free = NS - 1;
+  for (int kt = 0; kt < nk; ++kt) {
+    // This step's copies have landed and the reads of the step before have returned; behind the barrier everybody's have, and that step's
+    // slot is the next to be filled.
+    wait_vmcnt<NP * (NS - 2)>();
+    __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    wg_barrier();
+    asm volatile("" ::: "memory");
+    issue(kt + NS - 1, free);
+    const char* const st = smem + slot * S_B;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int rd = l31 * RK_ROWB + 16 * ((2 * q + g) ^ perm_of(l31));
+      const bf16x8 av = *(const bf16x8*)(st + 32 * wave * RK_ROWB + rd);
+#pragma unroll
+      for (int i = 0; i < RB; ++i) acc[i] = mfma32(av, *(const bf16x8*)(st + A_B + 32 * i * RK_ROWB + rd), acc[i]);
+    }
+    asm volatile("" ::: "memory");
+    free = slot;
+    slot = slot + 1 == NS ? 0 : slot + 1;
+  }
+  wait_vmcnt<0>();
+  asm volatile("" ::: "memory");
+  wg_barrier();                                      // (the slots are free, and nothing more lands in them)
+  asm volatile("" ::: "memory");
+  const int cw = 32 * wave, left = cols - c0 - cw;
+  if constexpr (MODE == STATS) {
+    float2* const sums = (float2*)smem;              // [4][32 RB]
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      const int r = 32 * i + l31;
+      const auto z = [&](int v, int) __attribute__((always_inline)) -> float { return acc[i][v]; };
+      float m2, s;
+      tile_stats<1>(g, left, z, &m2, &s);
+      if (g == 0) sums[wave * 32 * RB + r] = make_float2(m2, s);
+      const int c = r < M ? a.lab[r] - c0 - cw : -1;
+      const float y = tile_pick<1>(g, c, z);
+      if (c >= 0 && c < 32 && ((c >> 2) & 1) == g) a.zlab[r] = y;
+    }
+    __syncthreads();
+    if (tid < 32 * RB && tid < M) {
+      float m = -__builtin_inff(), s = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) join_stats(&m, &s, sums[w * 32 * RB + tid].x, sums[w * 32 * RB + tid].y);
+      a.part[(long)blockIdx.x * a.Mp + tid] = make_float2(m, s);
+    }
+  } else {
+    const float scale = a.head->scale;
+    char* const tb = smem + wave * W_B;
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      const int r = 32 * i + l31;
+      float lse2 = 0.f, d = 0.f;
+      int c = -1;
+      if (r < M) {
+        const int t = a.tok[r];
+        lse2 = a.lse[t] * LOG2E;
+        d = a.lab[r] < 0 ? __builtin_nanf("") : a.d_loss[t] / scale;
+        c = a.lab[r] - (int)a.v0 - c0 - cw;
+      }
+      const int end = d != 0.f ? left - 4 * g : 0, hot = c - 4 * g;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int at = 8 * q + k;
+          y[k] = exp2_fast(fmaf(acc[i][4 * q + k], LOG2E, -lse2)) - (at == hot ? 1.f : 0.f);
+          y[k] = at < end ? y[k] * d : 0.f;
+        }
+        *(u32x2*)(tb + r * W_PITCH + (8 * q + 4 * g) * 2) = u32x2{pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3])};
+      }
+    }
+    // (the buffer is this wave's own)
+#pragma unroll
+    for (int it = 0; it < 2 * RB; ++it) {
+      const int r = 16 * it + (lane >> 2), ch = lane & 3;
+      const u32x4 y = *(const u32x4*)(tb + r * W_PITCH + 16 * ch);
+      *(u32x4*)((char*)a.g + (long)r * a.g_pitch * 2 + 2L * (c0 + cw + 8 * ch)) = y;
+    }
+  }
+}
+
 // dx of the listed tokens: the parts' sums, 32 tokens x 32 features a workgroup; 0 for the others
 __global__ void __launch_bounds__(256) xent_dx_bf16_kernel(XentArgs a, unsigned tiles) {
   const int M = a.head->count, E = a.E, tid = threadIdx.x, n_ec = (E + 31) / 32;
   if (blockIdx.x < tiles) {
     const int r = (int)(blockIdx.x / n_ec) * 32 + tid % 32, c = (int)(blockIdx.x % n_ec) * 32 + 4 * (tid / 32);
     if (r >= M || c >= E) return;
-    const int n_ct = (E + T - 1) / T, rl = r % T, cl = c % T;
-    const long tile = (long)(r / T) * n_ct + c / T, step = (long)((M + T - 1) / T) * n_ct * T * T;
-    const int wave = (rl / 128) * 2 + cl / 128, i = rl % 128 / 32, j = cl % 128 / 32, q = cl % 32 / 8;
-    const float* from = a.dx_part + tile * (T * T) + wave * (T * T / 4) + ((j * 4 + i) * 4 + q) * 256 + (rl % 32 + 32 * (cl / 4 % 2)) * 4;
+    const int tr = a.tile_rows, n_ct = (E + T - 1) / T, rl = r % tr, cl = c % T;
+    const long tile = (long)(r / tr) * n_ct + c / T, step = (long)((M + tr - 1) / tr) * n_ct * tr * T;
+    const int wave = rl / (tr / 2) * 2 + cl / 128, i = rl % (tr / 2) / 32, j = cl % 128 / 32, q = cl % 32 / 8;
+    const float* from = a.dx_part + tile * (tr * T) + wave * (tr * T / 4) + ((j * (tr / 64) + i) * 4 + q) * 256 + (rl % 32 + 32 * (cl / 4 % 2)) * 4;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     for (int p = 0; p < a.head->parts; ++p) s += *(const f32x4*)(from + p * step);
     s *= a.head->scale;
@@ -555,13 +682,30 @@ __global__ void __launch_bounds__(256) xent_dx_bf16_kernel(XentArgs a, unsigned 
       for (int e = 8 * (tid & 63); e < E; e += 512) *(u32x4*)((uint16_t*)a.dx + i * a.ldx + e) = u32x4{0u, 0u, 0u, 0u};
 }
 
-// ---- float32: 128 x 128 tiles, 16 contraction steps at a time through LDS, any width ----
-
-constexpr int FT = 128, FK = 16, FP = FT + 4;
-template <int MODE>
+// ---- float32: FT x FT tiles (128, or 64 where these are too few), 32 contraction steps at a time through LDS, any width ----
+//
+// v_mfma_f32_32x32x2_f32 takes two steps at a time, one from each half of the wave.  The lower half takes steps 0 .. 15 of a tile, the
+// upper one 16 .. 31, so that of an operand which has the contraction contiguous (LDS [row][32 + 4]) a lane reads four steps at once.
+// Operands that have it along their rows lie as [step][FT].  A wave makes FT / 2 x FT / 2.
+constexpr int FK = 32, FPK = FK + 4;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+__device__ __forceinline__ f32x4 load4(const float* p, int there) {      // four floats, of which `there` exist (0 for the others)
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (there >= 4) {
+    v = *(const f32x4_any*)p;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (k < there) v[k] = p[k];
+  }
+  return v;
+}
+template <int MODE, int FT>
 __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   constexpr bool LOGITS = MODE == STATS || MODE == GRAD;
-  __shared__ float sa[FK][FP], sb[FK][FP];
+  constexpr bool AK = LOGITS, BK_ = MODE != DW;      // whether the operand has the contraction contiguous
+  constexpr int NB = FT / 64, NL = FT * FK / 1024;   // 32-blocks of a wave per side; 16-byte loads of a thread per side
+  __shared__ __attribute__((aligned(16))) float sa[FT * FPK], sb[FT * FPK];
   const int M = a.head->count, E = a.E, cols = (int)(a.v1 - a.v0);
   const int n_rt = MODE == DW ? (cols + FT - 1) / FT : (M + FT - 1) / FT;
   const int n_ct = LOGITS ? (cols + FT - 1) / FT : (E + FT - 1) / FT;
@@ -576,102 +720,124 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   const int k_to = MODE == DX ? (int)((long)(part + 1) * nk_all / parts) : nk_all;
   const float *const x = (const float*)a.x, *const w = (const float*)a.w;
   float* const gg = (float*)a.g;
-  // thread's elements of a tile: contraction contiguous: step tid % 16 of rows tid / 16 + 16 i; else row tid % 128 at steps tid / 128 + 2 i
-  const int kc = tid % 16, kr = tid / 16, rc = tid % 128, rk = tid / 128;
-  const float* brow[8];
-  if (LOGITS) {
+  // load i of a thread: contraction contiguous: steps 4 (u % 8) .. of row u / 8; else four columns 4 (u % (FT / 4)) .. of step u / (FT / 4),
+  // u = tid + 256 i
+  f32x4 va[NL], vb[NL];
+  long xrow[NL];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) brow[i] = x + a.tok[min(r0 + kr + 16 * i, M - 1)] * a.ldx;
-  }
-  float va[8], vb[8];
+  for (int i = 0; i < NL; ++i) xrow[i] = LOGITS ? a.tok[min(r0 + (tid + 256 * i) / 8, M - 1)] * a.ldx : 0;
   const auto fetch = [&](int kt) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < NL; ++i) {
+      const int u = tid + 256 * i;
+      const int row = u / 8, kc = kt * FK + 4 * (u % 8), kr = kt * FK + u / (FT / 4), col = 4 * (u % (FT / 4));
       if constexpr (LOGITS) {
-        const int k = kt * FK + kc;
-        va[i] = k < E && c0 + kr + 16 * i < cols ? w[(a.v0 + c0 + kr + 16 * i) * E + k] : 0.f;
-        vb[i] = k < E ? brow[i][k] : 0.f;
+        va[i] = load4(w + (a.v0 + c0 + row) * E + kc, c0 + row < cols ? E - kc : 0);
+        vb[i] = load4(x + xrow[i] + kc, E - kc);
       } else if constexpr (MODE == DX) {
-        const int k = kt * FK + rk + 2 * i, kb = kt * FK + kc;
-        va[i] = k < cols && c0 + rc < E ? w[(a.v0 + k) * E + c0 + rc] : 0.f;
-        vb[i] = kb < cols ? gg[(r0 + kr + 16 * i) * a.g_pitch + kb] : 0.f;
+        va[i] = load4(w + (a.v0 + kr) * E + c0 + col, kr < cols ? E - c0 - col : 0);
+        vb[i] = load4(gg + (r0 + row) * a.g_pitch + kc, cols - kc);
       } else {
-        const int k = kt * FK + rk + 2 * i;
-        va[i] = k < M && c0 + rc < E ? x[a.tok[k] * a.ldx + c0 + rc] : 0.f;
-        vb[i] = k < M && r0 + rc < cols ? gg[k * a.g_pitch + r0 + rc] : 0.f;
+        va[i] = load4(x + (kr < M ? a.tok[kr] * a.ldx : 0) + c0 + col, kr < M ? E - c0 - col : 0);
+        vb[i] = load4(gg + kr * a.g_pitch + r0 + col, kr < M ? cols - r0 - col : 0);
       }
     }
   };
-  f32x16 acc[2][2];
+  f32x16 acc[NB][NB];
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (int j = 0; j < NB; ++j)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) acc[j][i] = zero16();
+    for (int i = 0; i < NB; ++i) acc[j][i] = zero16();
   if (k_from < k_to) fetch(k_from);
   for (int kt = k_from; kt < k_to; ++kt) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (LOGITS) sa[kc][kr + 16 * i] = va[i];
-      else sa[rk + 2 * i][rc] = va[i];
-      if (MODE != DW) sb[kc][kr + 16 * i] = vb[i];
-      else sb[rk + 2 * i][rc] = vb[i];
+    for (int i = 0; i < NL; ++i) {
+      const int u = tid + 256 * i, at_k = (u / 8) * FPK + 4 * (u % 8), at_r = (u / (FT / 4)) * FT + 4 * (u % (FT / 4));
+      *(f32x4*)(sa + (AK ? at_k : at_r)) = va[i];
+      *(f32x4*)(sb + (BK_ ? at_k : at_r)) = vb[i];
     }
     __syncthreads();
     if (kt + 1 < k_to) fetch(kt + 1);
 #pragma unroll
-    for (int k = 0; k < FK; k += 2) {
-      float av[2], bv[2];
+    for (int s = 0; s < FK / 2; s += 4) {
+      f32x4 av[NB], bv[NB];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        av[j] = sa[k + g][64 * wn + 32 * j + l31];
-        bv[j] = sb[k + g][64 * wm + 32 * j + l31];
+      for (int j = 0; j < NB; ++j) {
+        const int ra = FT / 2 * wn + 32 * j + l31, rb = FT / 2 * wm + 32 * j + l31;
+        if constexpr (AK) {
+          av[j] = *(const f32x4*)(sa + ra * FPK + FK / 2 * g + s);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) av[j][k] = sa[(FK / 2 * g + s + k) * FT + ra];
+        }
+        if constexpr (BK_) {
+          bv[j] = *(const f32x4*)(sb + rb * FPK + FK / 2 * g + s);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) bv[j][k] = sb[(FK / 2 * g + s + k) * FT + rb];
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(av[j], bv[i], acc[j][i], 0, 0, 0);
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int i = 0; i < NB; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(av[j][k], bv[i][k], acc[j][i], 0, 0, 0);
     }
     __syncthreads();
   }
+  const float scale = MODE == STATS ? 1.f : a.head->scale;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float scale = MODE == STATS ? 1.f : a.head->scale;
-    const int r = r0 + 64 * wm + 32 * i + l31, left = cols - c0 - 64 * wn;
+  for (int i = 0; i < NB; ++i) {
+    const int r = r0 + FT / 2 * wm + 32 * i + l31, cw = c0 + FT / 2 * wn, left = cols - cw;
     if constexpr (MODE == STATS) {
       const auto z = [&](int v, int j) -> float { return acc[j][i][v]; };
       float m2, s;
-      tile_stats<2>(g, left, z, &m2, &s);
+      tile_stats<NB>(g, left, z, &m2, &s);
       if (g == 0 && r < M) a.part[(2L * ct + wn) * a.Mp + r] = make_float2(m2, s);
-      const int c = r < M ? a.lab[r] - c0 - wn * 64 : -1;
-      if (c >= 0 && c < 64 && ((c >> 2) & 1) == g) a.zlab[r] = tile_pick<2>(g, c, z);
-      continue;
-    }
-    float lse2 = 0.f, d = 0.f;
-    int c = -1;
-    if constexpr (MODE == GRAD) {
-      if (r < M) {
-        const int t = a.tok[r];
-        lse2 = a.lse[t] * LOG2E;
-        d = a.lab[r] < 0 ? __builtin_nanf("") : a.d_loss[t] / scale;
-        c = a.lab[r] - (int)a.v0;
+      const int c = r < M ? a.lab[r] - cw : -1;
+      if (__any(c >= 0 && c < FT / 2)) {
+        const float y = tile_pick<NB>(g, c, z);
+        if (c >= 0 && c < FT / 2 && ((c >> 2) & 1) == g) a.zlab[r] = y;
       }
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int at = c0 + 64 * wn + 32 * j + 8 * (v / 4) + 4 * g + v % 4;
-        float y = acc[j][i][v];
-        if constexpr (MODE == GRAD) {
-          y = exp2_fast(fmaf(y, LOG2E, -lse2)) - (at == c ? 1.f : 0.f);
-          if (at < a.g_pitch) gg[r * a.g_pitch + at] = at < cols && d != 0.f ? y * d : 0.f;
-        } else if constexpr (MODE == DX) {
-          float* const to = a.dx_part + (((long)part * n_rt + rt) * n_ct + ct) * (FT * FT) + (r - r0) * FT + (at - c0);
-          *to = a.first ? y : *to + y;
-        } else {
-          if (r < cols && at < E) ((float*)a.dw)[(a.v0 + r) * E + at] = y * scale;
+    } else {
+      float lse2 = 0.f, d = 0.f;
+      int c = -1;
+      if constexpr (MODE == GRAD) {
+        if (r < M) {
+          const int t = a.tok[r];
+          lse2 = a.lse[t] * LOG2E;
+          d = a.lab[r] < 0 ? __builtin_nanf("") : a.d_loss[t] / scale;
+          c = a.lab[r] - (int)a.v0;
         }
       }
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int at = cw + 32 * j + 8 * q + 4 * g;          // four columns from here
+          f32x4 y = {acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
+          if constexpr (MODE == GRAD) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float p = exp2_fast(fmaf(y[k], LOG2E, -lse2)) - (at + k == c ? 1.f : 0.f);
+              y[k] = at + k < cols && d != 0.f ? p * d : 0.f;
+            }
+            *(f32x4*)(gg + r * a.g_pitch + at) = y;            // (a row of g has room for whole tiles)
+          } else if constexpr (MODE == DX) {
+            float* const to = a.dx_part + (((long)part * n_rt + rt) * n_ct + ct) * (FT * FT) + (r - r0) * FT + (at - c0);
+            if (!a.first) y += *(const f32x4*)to;
+            *(f32x4*)to = y;
+          } else if (r < cols) {
+            float* const to = (float*)a.dw + (a.v0 + r) * E + at;
+            y *= scale;
+            if (at + 4 <= E) *(f32x4_any*)to = y;
+            else
+              for (int k = 0; k < 3; ++k)
+                if (at + k < E) to[k] = y[k];
+          }
+        }
+    }
   }
 }
 __global__ void __launch_bounds__(256) xent_dx_f32_kernel(XentArgs a, unsigned rows) {
@@ -679,10 +845,10 @@ __global__ void __launch_bounds__(256) xent_dx_f32_kernel(XentArgs a, unsigned r
   if (blockIdx.x < rows) {
     const int r = blockIdx.x;
     if (r >= M) return;
-    const int n_ct = (E + FT - 1) / FT, parts = a.head->parts;
-    const long step = (long)((M + FT - 1) / FT) * n_ct * (FT * FT);
+    const int t = a.tile, n_ct = (E + t - 1) / t, parts = a.head->parts;
+    const long step = (long)((M + t - 1) / t) * n_ct * (t * t);
     for (int e = threadIdx.x; e < E; e += 256) {
-      const float* const from = a.dx_part + ((long)(r / FT) * n_ct + e / FT) * (FT * FT) + (r % FT) * FT + e % FT;
+      const float* const from = a.dx_part + ((long)(r / t) * n_ct + e / t) * (t * t) + (r % t) * t + e % t;
       float s = 0.f;
       for (int p = 0; p < parts; ++p) s += from[p * step];
       ((float*)a.dx)[a.tok[r] * a.ldx + e] = s * a.head->scale;
@@ -701,57 +867,81 @@ template <int MODE, int RB> hipError_t launch_tiles(const XentArgs& a, long grid
   xent_bf16_kernel<MODE, RB><<<(unsigned)grid, 256, SMEM_B, s>>>(a);
   return hipGetLastError();
 }
+// (GRAD: 64 tokens whatever their number: the contraction of dw runs over g's rows 64 at a time)
+constexpr int FEW = 64;
+template <int MODE, int RB, int NS> hipError_t launch_few(const XentArgs& a, long wgs, hipStream_t s) {
+  constexpr int bytes = NS * (128 + 32 * RB) * RK_ROWB;
+  static SmemOnce once;
+  const hipError_t e = ensure_dynamic_lds((const void*)xent_few_bf16_kernel<MODE, RB, NS>, bytes, &once);
+  if (e != hipSuccess) return e;
+  xent_few_bf16_kernel<MODE, RB, NS><<<(unsigned)wgs, 256, bytes, s>>>(a);
+  return hipGetLastError();
+}
 long up(long n, long by) { return (n + by - 1) / by; }
+// float32: the edge of the tiles of a product.  64 where 128 makes less than two for every compute unit: 300 tokens x 512 features against 5003,
+// the four products 246 -> 112 us
+int f32_edge(long rows, long cols, int n_cu) { return up(rows, 128) * up(cols, 128) < 2L * n_cu ? 64 : 128; }
+template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long cols, int edge, hipStream_t s) {
+  const unsigned grid = (unsigned)strip_grid(MODE == DX ? a.slots : up(rows, edge) * up(cols, edge));
+  if (edge == 64) xent_f32_kernel<MODE, 64><<<grid, 256, 0, s>>>(a);
+  else xent_f32_kernel<MODE, 128><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
 template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t s) {
   const long cols = a.v1 - a.v0;
-  if (is_f32) {
-    xent_f32_kernel<MODE><<<(unsigned)strip_grid(up(a.n, FT) * up(cols, FT)), 256, 0, s>>>(a);
-    return hipGetLastError();
+  if (is_f32) return f32_product<MODE>(a, a.n, cols, f32_edge(a.n, cols, a.n_cu), s);
+  if (a.n <= FEW) {
+    const long wgs = up(cols, 128);
+    if constexpr (MODE == STATS)
+      if (a.n <= 32) return wgs <= a.n_cu ? launch_few<MODE, 1, 6>(a, wgs, s) : launch_few<MODE, 1, 3>(a, wgs, s);
+    return wgs <= a.n_cu ? launch_few<MODE, 2, 6>(a, wgs, s) : launch_few<MODE, 2, 3>(a, wgs, s);
   }
   return a.n <= 128 ? launch_tiles<MODE, 2>(a, strip_grid(up(cols, T)), s) : launch_tiles<MODE, 4>(a, strip_grid(up(a.n, T) * up(cols, T)), s);
 }
+// dx: columns and rows of a tile
+int dx_edge(long n, int E, int n_cu, int is_f32) { return is_f32 ? f32_edge(n, E, n_cu) : T; }
+int dx_rows(long n, int E, int n_cu, int is_f32) { return is_f32 ? f32_edge(n, E, n_cu) : n <= 128 ? 128 : T; }
 }  // namespace
 
 bool xent_bf16_supported(int E) { return E % BK == 0; }
-int xent_stat_parts(long V, int is_f32) { return (int)(2 * up(V, is_f32 ? FT : T)); }
-// one for every tile at least, two for every compute unit where 16 parts of a tile make so many: no more with fewer tokens or features
+int xent_stat_parts(long V, int is_f32) { return (int)(2 * up(V, is_f32 ? 64 : T)); }
+// Bytes of the tiles of dx's sums, and how many these are: one for every tile at least, two for every compute unit where 16 parts of a tile
+// make so many; no more with fewer tokens or features.
 long xent_dx_slots(long n, int E, int n_cu, int is_f32) {
-  const int t = is_f32 ? FT : T;
-  const long tiles = up(n, t) * up(E, t), some = 16 * tiles < 2L * n_cu ? 16 * tiles : 2L * n_cu;
+  const long tiles = up(n, dx_rows(n, E, n_cu, is_f32)) * up(E, dx_edge(n, E, n_cu, is_f32)), some = 16 * tiles < 2L * n_cu ? 16 * tiles : 2L * n_cu;
   return tiles > some ? tiles : some;
 }
-size_t xent_dx_slot_bytes(int is_f32) { return sizeof(float) * (is_f32 ? FT * FT : T * T); }
+size_t xent_dx_bytes(long n, int E, int n_cu, int is_f32) {
+  return sizeof(float) * dx_rows(n, E, n_cu, is_f32) * dx_edge(n, E, n_cu, is_f32) * xent_dx_slots(n, E, n_cu, is_f32);
+}
 
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
-  a.tile = is_f32 ? FT : T;
+  a.tile = a.tile_rows = T;
   xent_list_kernel<<<1, 1024, 0, s>>>(a);
   a.v0 = 0;
   a.v1 = a.V;
   const hipError_t e = logits<STATS>(a, is_f32, s);
   if (e != hipSuccess) return e;
   const long wgs = up(a.n, 8);
-  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, xent_stat_parts(a.V, is_f32));
+  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : a.n <= FEW ? (int)up(a.V, 128) : (int)(2 * up(a.V, T)));
   return hipGetLastError();
 }
 
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
-  const int t = is_f32 ? FT : T;
-  a.tile = t;
+  a.tile = dx_edge(a.n, a.E, a.n_cu, is_f32);
+  a.tile_rows = dx_rows(a.n, a.E, a.n_cu, is_f32);
   xent_list_kernel<<<1, 1024, 0, s>>>(a);
   a.first = 1;
   hipError_t e = hipGetLastError();
   for (a.v0 = 0; a.v0 < a.V && e == hipSuccess; a.v0 = a.v1) {
     a.v1 = a.v0 + a.piece < a.V ? a.v0 + a.piece : a.V;
+    const long cols = a.v1 - a.v0;
     e = logits<GRAD>(a, is_f32, s);
-    if (e == hipSuccess && a.dw) {
-      const long grid = strip_grid(up(a.v1 - a.v0, t) * up(a.E, t));
-      if (is_f32) xent_f32_kernel<DW><<<(unsigned)grid, 256, 0, s>>>(a);
-      e = is_f32 ? hipGetLastError() : launch_tiles<DW, 4>(a, grid, s);
-    }
+    if (e == hipSuccess && a.dw)
+      e = is_f32 ? f32_product<DW>(a, cols, a.E, f32_edge(cols, a.E, a.n_cu), s) : launch_tiles<DW, 4>(a, strip_grid(up(cols, T) * up(a.E, T)), s);
     if (e == hipSuccess && a.dx) {
-      const long grid = strip_grid(a.slots);
-      if (is_f32) xent_f32_kernel<DX><<<(unsigned)grid, 256, 0, s>>>(a);
-      e = is_f32 ? hipGetLastError() : launch_tiles<DX, 4>(a, grid, s);
+      e = is_f32 ? f32_product<DX>(a, a.n, a.E, a.tile, s)
+                 : a.tile_rows == 128 ? launch_tiles<DX, 2>(a, strip_grid(a.slots), s) : launch_tiles<DX, 4>(a, strip_grid(a.slots), s);
       a.first = 0;
     }
   }
