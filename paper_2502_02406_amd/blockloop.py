@@ -171,6 +171,73 @@ class BlockLoop:
         return self.dq
 
 
+@dataclass
+class Norm:
+    """The weights of a norm of token features: gamma and (or None) beta, [E], of the features' type."""
+    gamma: torch.Tensor
+    beta: Optional[torch.Tensor] = None
+
+
+class _Features:
+    """n tokens of E features on their way into a product, `at_once` at a time: normalised (norm = "layer" or "rms"), kept in 8 bits
+    (packed), or both; made again for the backward pass, from their 8-bit form where they have one.  With neither they pass through."""
+
+    def __init__(self, n, E, at_once, dtype, norm, packed, eps, device):
+        if norm not in (None, "layer", "rms"):
+            raise ValueError('norm is None, "layer" or "rms"')
+        self.norm, self.eps, self.rms = norm, eps, norm == "rms"
+        self.packed = B.Packed(n, E, device) if packed else None
+        self.plain = norm is None and not packed
+        if not self.plain:
+            self.out = torch.empty((at_once, E), dtype=dtype, device=device)
+        if norm is not None:
+            self.stats = torch.empty((n, 2), dtype=torch.float32, device=device)
+            self.dparam = torch.empty((2, E), dtype=torch.float32, device=device)
+            self.ws = torch.empty(B.lvx_norm_workspace_bytes(at_once, E), dtype=torch.uint8, device=device)
+
+    def _check(self, weights):
+        if (weights is None) != (self.norm is None):
+            raise ValueError("a norm's weights are given where there is a norm, and only there")
+
+    def forward(self, t, first, shape, weights):
+        """The features of the tokens t (`shape`, the first of them is token `first` of n); t None: of what was packed before."""
+        self._check(weights)
+        if t is None and self.packed is None:
+            raise ValueError("only packed features can be made again from nothing")
+        if self.plain:
+            return t
+        n = shape.numel() // shape[-1]
+        out = self.out[:n].view(shape)
+        pk = self.packed.rows(first, first + n) if self.packed is not None else None
+        if self.norm is not None:
+            B.lvx_norm_fwd(t, weights.gamma, weights.beta, out, self.stats[first:first + n], self.rms, self.eps, pk)
+            return out
+        if t is not None:
+            B.lvx_pack(t, pk)
+        B.lvx_unpack(pk, out)
+        return out
+
+    def again(self, t, first, shape, weights):
+        """The same features once more, bit for bit (t is not read where they are packed)."""
+        return self.forward(t if self.packed is None else None, first, shape, weights)
+
+    def start_backward(self):
+        if self.norm is not None:
+            self.dparam.zero_()
+
+    def backward(self, t, first, weights, grad):
+        """grad, the gradient of the features, becomes that of the tokens in place; the norm's weights' gradients are added up."""
+        if self.norm is None:
+            return
+        n = grad.numel() // grad.shape[-1]
+        pk = self.packed.rows(first, first + n) if self.packed is not None else None
+        B.lvx_norm_bwd(t if pk is None else None, weights.gamma, self.stats[first:first + n], grad, grad, self.dparam[0],
+                       self.dparam[1] if weights.beta is not None else None, self.ws, self.rms, self.eps, pk)
+
+    def gradients(self, weights):
+        return () if self.norm is None else (self.dparam[0], self.dparam[1] if weights.beta is not None else None)
+
+
 class RecomputeLayer:
     """One cross-attention layer under the activation recomputation of Section 3.2, on one GPU: the
     forward pass keeps the token features x, y and (O, L) and nothing else; the backward pass makes
@@ -180,10 +247,17 @@ class RecomputeLayer:
 
     x [B, Sq, E] text tokens, y [B, Skv, E] visual tokens (B > 1: n_blocks must be 1, the
     projection entry points want the batches of a call to follow each other), wq [Hq D, E],
-    wkv [2 Hkv D, E] (W_K^T on top of W_V^T).  Only sequences C-ABI calls."""
+    wkv [2 Hkv D, E] (W_K^T on top of W_V^T).  Only sequences C-ABI calls.
+
+    norm = "layer" or "rms": the projections read the norm of x and of y; forward and backward take the two norms'
+    weights, and backward returns their gradients behind the others.
+    packed: the layer keeps x and y in 8 bits (33 / 64 of their bf16 size) and the caller need not: the forward pass works from
+    the values that these stand for, so what the backward pass makes again from them, x and y None, is the forward
+    pass's bit for bit.  The gradients are those with respect to these values."""
 
     def __init__(self, Bsz, Sq, Skv, E, Hq, Hkv, D, dtype: torch.dtype, n_blocks: int = 1,
-                 softmax_scale: float = 0.0, device: str = "cuda"):
+                 softmax_scale: float = 0.0, device: str = "cuda", norm: Optional[str] = None, packed: bool = False,
+                 eps: float = 1e-5):
         assert Skv % n_blocks == 0 and (Bsz == 1 or n_blocks == 1)
         self.n_blocks, self.blk = n_blocks, Skv // n_blocks
         self.loop = BlockLoop((Bsz, Hq, Sq, D), (Bsz, Hkv, self.blk, D), dtype, 1, None, softmax_scale, device)
@@ -197,19 +271,24 @@ class RecomputeLayer:
         self.dy = torch.empty((Bsz, Skv, E), **kw)
         self.dwq = torch.empty((Hq * D, E), dtype=torch.float32, device=device)
         self.dwkv = torch.empty((2 * Hkv * D, E), dtype=torch.float32, device=device)
+        self.fx = _Features(Bsz * Sq, E, Bsz * Sq, dtype, norm, packed, eps, device)
+        self.fy = _Features(Bsz * Skv, E, Bsz * self.blk, dtype, norm, packed, eps, device)
 
-    def _kv_of_block(self, y, wkv, n):
-        yb = y[:, n * self.blk:(n + 1) * self.blk]
-        B.lvx_xattn_project(yb, wkv, [self.k, self.v])
-        return yb
+    def _kv_of_block(self, y, wkv, n, norm_y, again=False):
+        """The block's tokens and their features, of which K and V are made."""
+        yb = y[:, n * self.blk:(n + 1) * self.blk] if y is not None else None
+        shape = torch.Size((self.dy.shape[0], self.blk, self.dy.shape[2]))
+        feat = (self.fy.again if again else self.fy.forward)(yb, n * self.blk, shape, norm_y)
+        B.lvx_xattn_project(feat, wkv, [self.k, self.v])
+        return yb, feat
 
-    def forward(self, x, y, wq, wkv) -> Tuple[torch.Tensor, torch.Tensor]:
+    def forward(self, x, y, wq, wkv, norm_x: Optional[Norm] = None, norm_y: Optional[Norm] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """(O in the input dtype, L float32); Q, K, V are not kept."""
         lp = self.loop
-        B.lvx_xattn_project(x, wq, [self.q])
+        B.lvx_xattn_project(self.fx.forward(x, 0, self.dx.shape, norm_x), wq, [self.q])
         p = B.make_problem(self.q, self.k, lp.scale)
         for n in range(self.n_blocks):
-            self._kv_of_block(y, wkv, n)
+            self._kv_of_block(y, wkv, n, norm_y)
             if self.n_blocks == 1:
                 B.lvx_xattn_fwd(p, self.q, self.k, self.v, None, lp.o, lp.lse, lp.ws)
                 return lp.o, lp.lse
@@ -223,19 +302,71 @@ class RecomputeLayer:
         B.lvx_xattn_merge([self.o_acc], [lp.lse], lp.o, lp.lse)
         return lp.o, lp.lse
 
-    def backward(self, x, y, wq, wkv, o, lse, d_o):
-        """(dx, dy in the input dtype, dW_Q, dW_KV float32) from x, y, (O, L) and dO alone."""
+    def backward(self, x, y, wq, wkv, o, lse, d_o, norm_x: Optional[Norm] = None, norm_y: Optional[Norm] = None):
+        """(dx, dy in the input dtype, dW_Q, dW_KV float32) from x, y (None where the layer keeps them packed), (O, L) and dO alone;
+        with norms followed by the gradients (float32, or None) of norm_x's gamma and beta and of norm_y's."""
         lp = self.loop
-        B.lvx_xattn_project(x, wq, [self.q])                       # Q again
+        feat_x = self.fx.again(x, 0, self.dx.shape, norm_x)
+        B.lvx_xattn_project(feat_x, wq, [self.q])                  # Q again
         self.dwq.zero_()
         self.dwkv.zero_()
+        self.fx.start_backward()
+        self.fy.start_backward()
         p = B.make_problem(self.q, self.k, lp.scale)
         last = lp.dq if lp.dq is not lp.dq_accum else None
         for n in range(self.n_blocks):
-            yb = self._kv_of_block(y, wkv, n)                       # K, V of the block again
+            yb, feat = self._kv_of_block(y, wkv, n, norm_y, again=True)       # K, V of the block again
             B.lvx_xattn_bwd_visit(p, self.q, self.k, self.v, o, lse, d_o, None, lp.dq_accum, self.dk, self.dv, lp.ws, n == 0,
                                   last if n == self.n_blocks - 1 else None)
-            B.lvx_xattn_project_bwd(yb, wkv, [self.dk, self.dv],
-                                    dx=self.dy[:, n * self.blk:(n + 1) * self.blk], dw=self.dwkv)
-        B.lvx_xattn_project_bwd(x, wq, [lp.dq], dx=self.dx, dw=self.dwq)
-        return self.dx, self.dy, self.dwq, self.dwkv
+            dyb = self.dy[:, n * self.blk:(n + 1) * self.blk]
+            # (a single batch's stride means nothing, but has to be the same in a block's features and in its gradient)
+            B.lvx_xattn_project_bwd(feat, wkv, [self.dk, self.dv], dx=dyb.as_strided(feat.shape, feat.stride()), dw=self.dwkv)
+            self.fy.backward(yb, n * self.blk, norm_y, dyb)
+        B.lvx_xattn_project_bwd(feat_x, wq, [lp.dq], dx=self.dx, dw=self.dwq)
+        self.fx.backward(x, 0, norm_x, self.dx)
+        return (self.dx, self.dy, self.dwq, self.dwkv) + self.fx.gradients(norm_x) + self.fy.gradients(norm_y)
+
+
+class LossHead:
+    """The end of a training step on one GPU: the norm of the last hidden features (norm = "layer" or "rms", or None), their product
+    with a vocabulary's weights, and the cross entropy of every token, without the logits.  Between the passes it keeps the norm's
+    statistics and lse, and (packed) the features in 8 bits, so that the caller need not keep them; the rest is made again.
+
+    h [n, E] or [B, S, E], contiguous, w [V, E], labels int64 (negative: the token takes no part).  Only sequences C-ABI calls."""
+
+    def __init__(self, n, E, V, dtype: torch.dtype, norm: Optional[str] = None, packed: bool = False, eps: float = 1e-5,
+                 device: str = "cuda"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("LossHead needs a GPU: there is no CPU fallback")
+        nbytes = B.lvx_xent_workspace_bytes(n, E, V, B.dtype_code(dtype))
+        if nbytes == 0:
+            raise B.LvxError(-2, "lvx_xent_workspace_bytes")
+        self.f = _Features(n, E, n, dtype, norm, packed, eps, device)
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.loss = torch.empty(n, dtype=torch.float32, device=device)
+        self.lse = torch.empty(n, dtype=torch.float32, device=device)
+        self.dh = torch.empty((n, E), dtype=dtype, device=device)
+        self.dw = torch.empty((V, E), dtype=dtype, device=device)
+
+    def _tokens(self, h):
+        if h is None:
+            return None
+        if h.numel() != self.dh.numel() or h.shape[-1] != self.dh.shape[1] or not h.is_contiguous():
+            raise ValueError("h has to be contiguous, of as many tokens and features as this object was made for")
+        return h.view(self.dh.shape)
+
+    def forward(self, h, w, labels, norm: Optional[Norm] = None) -> torch.Tensor:
+        """The tokens' losses (float32 [n], a buffer of this object; 0 without a label)."""
+        feat = self.f.forward(self._tokens(h), 0, self.dh.shape, norm)
+        B.lvx_xent_fwd(feat, w, labels, self.loss, self.lse, self.ws)
+        return self.loss
+
+    def backward(self, h, w, labels, d_loss, norm: Optional[Norm] = None):
+        """(dh [n, E], dw in the input dtype) of sum(loss * d_loss), d_loss float32 [n]; h None where it is kept packed.  With a norm
+        followed by the gradients (float32, or None) of its gamma and beta."""
+        h = self._tokens(h)
+        feat = self.f.again(h, 0, self.dh.shape, norm)
+        self.f.start_backward()
+        B.lvx_xent_bwd(feat, w, labels, self.lse, d_loss, self.dh, self.dw, self.ws)
+        self.f.backward(h, 0, norm, self.dh)
+        return (self.dh, self.dw) + self.f.gradients(norm)
