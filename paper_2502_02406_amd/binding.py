@@ -402,15 +402,19 @@ def lvx_xattn_project_bwd(x, w, d_outs, dx=None, dw=None) -> None:
 
 # ---- around the layer: norms of the token features, their 8-bit checkpoint ----
 
-def _on_device(where: str, *ts) -> None:
-    """Every tensor lies on the device whose stream the call goes to."""
-    at = None
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _on_device(where: str, first, *ts) -> int:
+    """The current stream, after a look that every tensor lies on its device."""
+    at = first.get_device()
+    ok = at >= 0 and at == _get_device()
     for t in ts:
-        if t is not None:
-            if t.is_cuda and at is None:
-                at = torch.cuda.current_device()
-            if not t.is_cuda or t.get_device() != at:
-                raise RuntimeError(f"{where} needs tensors of the current device")
+        if t is not None and t.get_device() != at:
+            ok = False
+    if not ok:
+        raise RuntimeError(f"{where} needs tensors of the current device")
+    return int(_raw_stream(at)) if _raw_stream is not None else _stream()
 
 
 def _token_rows(t, name: str):
@@ -447,26 +451,28 @@ class Packed:
     def _struct(self, where: str, n: int, E: int) -> lvx_packed:
         if not _of(self.q, torch.int8, n, E) or not _of(self.e, torch.uint8, n, (E + 31) // 32):
             raise ValueError(f"{where}: packed has to hold [{n}, {E}], contiguous")
-        _on_device(where, self.q, self.e)
         return lvx_packed(self.q.data_ptr(), self.e.data_ptr())
 
 
 def lvx_pack(x, packed: Packed) -> None:
     """packed is overwritten with the 8-bit form of x [n, E] or [B, S, E]."""
-    _on_device("lvx_pack", x)
+    s = _on_device("lvx_pack", x, packed.q, packed.e)
     n, E, ss = _token_rows(x, "x")
-    _check(load().lvx_pack(n, E, ss, dtype_code(x.dtype), x.data_ptr(), C.byref(packed._struct("lvx_pack", n, E)), _stream()), "lvx_pack")
+    _check(load().lvx_pack(n, E, ss, dtype_code(x.dtype), x.data_ptr(), C.byref(packed._struct("lvx_pack", n, E)), s), "lvx_pack")
 
 
 def lvx_unpack(packed: Packed, x) -> None:
     """x [n, E] or [B, S, E] is overwritten with the values that packed stands for."""
-    _on_device("lvx_unpack", x)
+    s = _on_device("lvx_unpack", x, packed.q, packed.e)
     n, E, ss = _token_rows(x, "x")
-    _check(load().lvx_unpack(n, E, ss, dtype_code(x.dtype), C.byref(packed._struct("lvx_unpack", n, E)), x.data_ptr(), _stream()), "lvx_unpack")
+    _check(load().lvx_unpack(n, E, ss, dtype_code(x.dtype), C.byref(packed._struct("lvx_unpack", n, E)), x.data_ptr(), s), "lvx_unpack")
 
 
 def _of(t, dtype, *shape) -> bool:
     return t.shape == shape and t.dtype == dtype and t.is_contiguous()
+
+
+_norms = {}
 
 
 def _norm_struct(where, like_x, like_y, gamma, stats, rms, eps):
@@ -481,7 +487,13 @@ def _norm_struct(where, like_x, like_y, gamma, stats, rms, eps):
         raise ValueError(f"{where}: gamma has to be [{E}] of y's type")
     if stats.numel() != 2 * n or stats.dtype != torch.float32 or not stats.is_contiguous():
         raise ValueError(f"{where}: stats has to be float32 [{n}, 2]")
-    return lvx_norm(n, E, 1 if rms else 0, x_ss, y_ss, eps)
+    key = (n, E, 1 if rms else 0, x_ss, y_ss, eps)
+    p = _norms.get(key)                              # (made once for a set of sizes: 1 us a call)
+    if p is None:
+        if len(_norms) >= 256:
+            _norms.clear()
+        p = _norms[key] = lvx_norm(*key)
+    return p
 
 
 def lvx_norm_fwd(x, gamma, beta, y, stats, rms: bool = False, eps: float = 1e-5, packed: Optional[Packed] = None) -> None:
@@ -490,13 +502,16 @@ def lvx_norm_fwd(x, gamma, beta, y, stats, rms: bool = False, eps: float = 1e-5,
     w = "lvx_norm_fwd"
     if x is None and packed is None:
         raise ValueError(f"{w}: neither x nor packed")
-    _on_device(w, x, gamma, beta, y, stats)
+    s = _on_device(w, y, x, gamma, beta, stats)
     p = _norm_struct(w, x, y, gamma, stats, rms, eps)
     if beta is not None and not _of(beta, y.dtype, p.E):
         raise ValueError(f"{w}: beta has to be [{p.E}] of y's type")
-    pk = packed._struct(w, p.n, p.E) if packed is not None else None
+    pk = None
+    if packed is not None:
+        _on_device(w, y, packed.q, packed.e)
+        pk = packed._struct(w, p.n, p.E)
     _check(load().lvx_norm_fwd(C.byref(p), dtype_code(y.dtype), x.data_ptr() if x is not None else None, C.byref(pk) if pk is not None else None,
-                               gamma.data_ptr(), beta.data_ptr() if beta is not None else None, y.data_ptr(), stats.data_ptr(), _stream()), w)
+                               gamma.data_ptr(), beta.data_ptr() if beta is not None else None, y.data_ptr(), stats.data_ptr(), s), w)
 
 
 def lvx_norm_workspace_bytes(n: int, E: int) -> int:
@@ -512,7 +527,7 @@ def lvx_norm_bwd(x, gamma, stats, d_y, dx=None, dgamma=None, dbeta=None, workspa
         raise ValueError(f"{w}: x or packed, one of them")
     if dx is None and dgamma is None and dbeta is None:
         raise ValueError(f"{w}: nothing asked for")
-    _on_device(w, x, gamma, stats, d_y, dx, dgamma, dbeta, workspace)
+    s = _on_device(w, d_y, x, gamma, stats, dx, dgamma, dbeta, workspace)
     p = _norm_struct(w, x if x is not None else dx, d_y, gamma, stats, rms, eps)
     if dx is not None:
         if dx.shape != d_y.shape or dx.dtype != d_y.dtype:
@@ -524,11 +539,14 @@ def lvx_norm_bwd(x, gamma, stats, d_y, dx=None, dgamma=None, dbeta=None, workspa
             raise ValueError(f"{w}: dgamma and dbeta have to be float32 [{p.E}]")
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError(f"{w}: the workspace has to be contiguous")
-    pk = packed._struct(w, p.n, p.E) if packed is not None else None
+    pk = None
+    if packed is not None:
+        _on_device(w, d_y, packed.q, packed.e)
+        pk = packed._struct(w, p.n, p.E)
     at = lambda t: t.data_ptr() if t is not None else None
     _check(load().lvx_norm_bwd(C.byref(p), dtype_code(d_y.dtype), at(x), C.byref(pk) if pk is not None else None, gamma.data_ptr(),
                                stats.data_ptr(), d_y.data_ptr(), at(dx), at(dgamma), at(dbeta), at(workspace),
-                               workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), w)
+                               workspace.numel() * workspace.element_size() if workspace is not None else 0, s), w)
 
 
 # ---- the loss over a vocabulary ----
@@ -555,10 +573,10 @@ def _xent_struct(where, x, w, labels, per_token, workspace):
 def lvx_xent_fwd(x, w, labels, loss, lse, workspace) -> None:
     """loss and lse (float32, one value for every token) are overwritten with the cross entropy of x [n, E] or [B, S, E] against the
     vocabulary's weights w [V, E]; tokens with a negative label (int64) take no part."""
-    _on_device("lvx_xent_fwd", x, w, labels, loss, lse, workspace)
+    s = _on_device("lvx_xent_fwd", x, w, labels, loss, lse, workspace)
     p = _xent_struct("lvx_xent_fwd", x, w, labels, (loss, lse), workspace)
     _check(load().lvx_xent_fwd(C.byref(p), dtype_code(x.dtype), x.data_ptr(), w.data_ptr(), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(),
-                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), "lvx_xent_fwd")
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), s), "lvx_xent_fwd")
 
 
 def lvx_xent_bwd(x, w, labels, lse, d_loss, dx=None, dw=None, workspace=None) -> None:
@@ -567,7 +585,7 @@ def lvx_xent_bwd(x, w, labels, lse, d_loss, dx=None, dw=None, workspace=None) ->
     where = "lvx_xent_bwd"
     if workspace is None or (dx is None and dw is None):
         raise ValueError(f"{where}: no workspace, or nothing asked for")
-    _on_device(where, x, w, labels, lse, d_loss, dx, dw, workspace)
+    s = _on_device(where, x, w, labels, lse, d_loss, dx, dw, workspace)
     p = _xent_struct(where, x, w, labels, (lse, d_loss), workspace)
     if dx is not None and (dx.shape != x.shape or dx.dtype != x.dtype or _token_rows(dx, "dx")[2] != p.x_ss):
         raise ValueError(f"{where}: dx has to have x's shape, strides and type")
@@ -575,4 +593,4 @@ def lvx_xent_bwd(x, w, labels, lse, d_loss, dx=None, dw=None, workspace=None) ->
         raise ValueError(f"{where}: dw has to be [{p.V}, {p.E}] of w's type, contiguous")
     _check(load().lvx_xent_bwd(C.byref(p), dtype_code(x.dtype), x.data_ptr(), w.data_ptr(), labels.data_ptr(), lse.data_ptr(), d_loss.data_ptr(),
                                dx.data_ptr() if dx is not None else None, dw.data_ptr() if dw is not None else None,
-                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), where)
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), s), where)

@@ -61,7 +61,7 @@ __device__ __forceinline__ float wg_sum(float x, float* at) {
   return (at[0] + at[1]) + (at[2] + at[3]);
 }
 
-// ---- any width: a workgroup per row, an element per thread, the row read again for every sum ----
+// ---- rows of fewer than 8 features or more than 16384: a workgroup each, an element per thread, the row read again for every sum ----
 
 // Element e of a row as the norm sees it (any e of a group of 32 lanes that asks for a group, E and more: 0).
 // SRC 0: x.  1: the packed form of x (which is written where `keep` says so).  2: what was packed before.
@@ -200,8 +200,10 @@ __global__ void __launch_bounds__(WG) norm_param_sum_kernel(NormArgs a) {
 // ---- rows in registers: a team of TPR threads has a row, a thread NV chunks of 8 features of it ----
 //
 // A chunk is moved at once wherever it lies: the memory instructions take any address that the element type has.  FULL: E is a
-// multiple of 8; otherwise a row's last chunk goes element by element.  Which thread has which features goes by E alone, so
-// the norm made again from the packed form is the first one bit for bit, whatever x's addresses were.
+// multiple of 8.  Otherwise a row's last chunk is loaded as the row's last 8 features, of which the first skip_of belong to the chunk before and
+// are cleared where they are used (not where they are loaded, which would wait for the row while it is on its way), and stored element by
+// element.  Which thread has which features goes by E alone, so the norm made again from the packed form is the first one bit for
+// bit, whatever x's addresses were.
 
 constexpr int V = 8;
 __host__ __device__ constexpr int chunks(int E) { return (E + V - 1) / V; }
@@ -209,19 +211,21 @@ typedef u32x4 __attribute__((aligned(2))) u32x4_any2;
 typedef u32x4 __attribute__((aligned(4))) u32x4_any4;
 typedef u32x2 __attribute__((aligned(1))) u32x2_any;
 
-// chunk c of a row of E features as it lies in memory; what is behind the row's end is 0
+// where chunk c starts as it is loaded (E >= 8), and how many of its 8 features are not its own
+template <bool FULL> __device__ __forceinline__ int start_of(int c, int E) { return FULL ? V * c : min(V * c, E - V); }
+template <bool FULL> __device__ __forceinline__ int skip_of(int c, int E) { return FULL || c < chunks(E) - 1 ? 0 : c < chunks(E) ? V * c - (E - V) : V; }
+
+// chunk c of a row of E features as it lies in memory; 0 behind the row's end
 template <typename T> struct Chunk;
 template <> struct Chunk<__bf16> {
   u32x4 w;
   template <bool FULL> __device__ __forceinline__ void load(const __bf16* row, int c, int E) {
     w = u32x4{0u, 0u, 0u, 0u};
-    if (FULL ? c < chunks(E) : V * c + V <= E) {
-      w = *(const u32x4_any2*)(row + V * c);
-    } else if (!FULL) {
+    if (c < chunks(E)) w = *(const u32x4_any2*)(row + start_of<FULL>(c, E));
+  }
+  __device__ __forceinline__ void keep_from(int skip) {
 #pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (V * c + k < E) w[k / 2] |= (unsigned)((const uint16_t*)row)[V * c + k] << (16 * (k % 2));
-    }
+    for (int j = 0; j < 4; ++j) w[j] &= (2 * j >= skip ? 0x0000ffffu : 0u) | (2 * j + 1 >= skip ? 0xffff0000u : 0u);
   }
   __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
   // the largest magnitude, as the bits of a float32
@@ -233,28 +237,23 @@ template <> struct Chunk<__bf16> {
     const unsigned x = (unsigned)m[0] << 16, y = (unsigned)m[1] << 16;
     return x > y ? x : y;
   }
-  template <bool FULL> static __device__ __forceinline__ void store(__bf16* row, int c, int E, const float (&v)[V]) {
-    if (FULL ? c < chunks(E) : V * c + V <= E) {
-      *(u32x4_any2*)(row + V * c) = u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
-    } else if (!FULL) {
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (V * c + k < E) row[V * c + k] = (__bf16)v[k];
-    }
+  static __device__ __forceinline__ void store8(__bf16* p, const float (&v)[V]) {
+    *(u32x4_any2*)p = u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
   }
 };
 template <> struct Chunk<float> {
   u32x4 w[2];
   template <bool FULL> __device__ __forceinline__ void load(const float* row, int c, int E) {
     w[0] = w[1] = u32x4{0u, 0u, 0u, 0u};
-    if (FULL ? c < chunks(E) : V * c + V <= E) {
-      w[0] = *(const u32x4_any4*)(row + V * c);
-      w[1] = *(const u32x4_any4*)(row + V * c + 4);
-    } else if (!FULL) {
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (V * c + k < E) w[k / 4][k % 4] = __float_as_uint(row[V * c + k]);
+    if (c < chunks(E)) {
+      const u32x4_any4* const p = (const u32x4_any4*)(row + start_of<FULL>(c, E));
+      w[0] = p[0];
+      w[1] = p[1];
     }
+  }
+  __device__ __forceinline__ void keep_from(int skip) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i / 4][i % 4] = i >= skip ? w[i / 4][i % 4] : 0u;
   }
   __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i / 4][i % 4]); }
   __device__ __forceinline__ unsigned largest() const {
@@ -266,17 +265,21 @@ template <> struct Chunk<float> {
     }
     return m;
   }
-  template <bool FULL> static __device__ __forceinline__ void store(float* row, int c, int E, const float (&v)[V]) {
-    if (FULL ? c < chunks(E) : V * c + V <= E) {
-      *(u32x4_any4*)(row + V * c) = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
-      *(u32x4_any4*)(row + V * c + 4) = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
-    } else if (!FULL) {
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (V * c + k < E) row[V * c + k] = v[k];
-    }
+  static __device__ __forceinline__ void store8(float* p, const float (&v)[V]) {
+    *(u32x4_any4*)p = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+    *(u32x4_any4*)(p + 4) = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
   }
 };
+template <bool FULL, typename T> __device__ __forceinline__ void store_chunk(T* row, int c, int E, const float (&v)[V]) {
+  if (FULL ? c < chunks(E) : V * c + V <= E) {
+    Chunk<T>::store8(row + V * c, v);
+  } else if (!FULL && c < chunks(E)) {
+    const int skip = skip_of<FULL>(c, E);
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k >= skip) row[E - V + k] = (T)v[k];
+  }
+}
 
 // 8 packed features and their exponent byte (behind the row's end: 0 steps)
 struct PackedChunk {
@@ -285,14 +288,15 @@ struct PackedChunk {
   template <bool FULL> __device__ __forceinline__ void load(const int8_t* q, const uint8_t* e, int c, int E) {
     w = u32x2{0u, 0u};
     b = 8u;
-    if (FULL ? c < chunks(E) : V * c + V <= E) {
-      w = *(const u32x2_any*)(q + V * c);
-    } else if (!FULL) {
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (V * c + k < E) w[k / 4] |= (unsigned)(uint8_t)q[V * c + k] << (8 * (k % 4));
+    if (c < chunks(E)) {
+      w = *(const u32x2_any*)(q + start_of<FULL>(c, E));
+      b = e[c / (packed::GROUP / V)];
     }
-    if (c < chunks(E)) b = e[c / (packed::GROUP / V)];
+  }
+  __device__ __forceinline__ void keep_from(int skip) {
+    const unsigned long long m = skip >= V ? 0ull : ~0ull << (8 * skip);
+    w[0] &= (unsigned)m;
+    w[1] &= (unsigned)(m >> 32);
   }
   __device__ __forceinline__ float step() const { return packed::step_of(b); }
   __device__ __forceinline__ float operator[](int i) const { return (float)(int8_t)(w[i / 4] >> (8 * (i % 4))); }     // in steps
@@ -313,10 +317,11 @@ template <bool FULL, typename T> __device__ __forceinline__ float pack_chunk(con
       return __builtin_amdgcn_perm(__builtin_amdgcn_perm(s3, s2, 0x0c0c0400), __builtin_amdgcn_perm(s1, s0, 0x0c0c0400), 0x05040100);
     };
     *(u32x2_any*)(q + V * c) = u32x2{four(s[0], s[1], s[2], s[3]), four(s[4], s[5], s[6], s[7])};
-  } else if (!FULL) {
+  } else if (!FULL && c < chunks(E)) {
+    const int skip = skip_of<FULL>(c, E);
 #pragma unroll
     for (int k = 0; k < V; ++k)
-      if (V * c + k < E) q[V * c + k] = (int8_t)(s[k] & 0xffu);
+      if (k >= skip) q[E - V + k] = (int8_t)(s[k] & 0xffu);
   }
   if (c < chunks(E) && c % (packed::GROUP / V) == 0) e[c / (packed::GROUP / V)] = (uint8_t)b;
   return packed::step_of(b);
@@ -353,12 +358,10 @@ constexpr int wg_of(int tpr) { return tpr > WG ? tpr : WG; }
 // A team, and the same number in a scalar register (a wave belongs to one team)
 template <int TPR> __device__ __forceinline__ int team_of() { return TPR >= WG ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR); }
 
-// waves per SIMD that the registers are kept for
-constexpr int waves_for(int nv) { return nv <= 2 ? 4 : nv <= 4 ? 2 : 1; }
 
 // The next row is on its way while one is worked on.  Values are v[i][k] * step[i] (packed features: whole steps; others: step 1).
 template <typename T, int SRC, bool FULL, int TPR, int NV>
-__global__ void __launch_bounds__(wg_of(TPR), waves_for(NV)) norm_fwd_kernel(NormArgs a) {
+__global__ void __launch_bounds__(wg_of(TPR), 4) norm_fwd_kernel(NormArgs a) {
   constexpr int TEAMS = wg_of(TPR) / TPR;
   __shared__ float sums[2][2][16];
   TeamSum<TPR> team_sum{sums};
@@ -387,8 +390,15 @@ __global__ void __launch_bounds__(wg_of(TPR), waves_for(NV)) norm_fwd_kernel(Nor
     else beta[i] = Chunk<T>{};
   }
   for (; row < a.n; row += by) {
-    const Row w = next;
+    Row w = next;
     if (row + by < a.n) load(next, row + by);
+    if constexpr (!FULL) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if constexpr (SRC == 2) w.p[i].keep_from(skip_of<FULL>(t + TPR * i, E));
+        else w.x[i].keep_from(skip_of<FULL>(t + TPR * i, E));
+      }
+    }
     float v[NV][V], step[NV];
     float s[1] = {0.f};
 #pragma unroll
@@ -422,7 +432,7 @@ __global__ void __launch_bounds__(wg_of(TPR), waves_for(NV)) norm_fwd_kernel(Nor
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         v[i][k] = SRC == 0 ? v[i][k] - mu : fmaf(v[i][k], step[i], -mu);
-        const float d = FULL || V * c + k < E ? v[i][k] : 0.f;
+        const float d = FULL || k >= skip_of<FULL>(c, E) ? v[i][k] : 0.f;
         z = fmaf(d, d, z);
       }
       s[0] += c < chunks(E) ? z : 0.f;
@@ -435,7 +445,7 @@ __global__ void __launch_bounds__(wg_of(TPR), waves_for(NV)) norm_fwd_kernel(Nor
       float o[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) o[k] = fmaf(v[i][k] * r, gamma[i][k], beta[i][k]);
-      Chunk<T>::template store<FULL>(y, t + TPR * i, E, o);
+      store_chunk<FULL>(y, t + TPR * i, E, o);
     }
     if (t == 0) {
       a.stats[2 * row] = mu;
@@ -444,11 +454,13 @@ __global__ void __launch_bounds__(wg_of(TPR), waves_for(NV)) norm_fwd_kernel(Nor
   }
 }
 
+// waves per SIMD that leave registers for a row, the next one and the columns' sums without spills
+constexpr int bwd_waves(int tpr, int nv, bool param) { return nv == 1 || (!param && nv == 2) ? 4 : tpr > WG || nv > 2 ? 2 : 3; }
 // dx of the rows, and (PARAM) the part of dgamma and dbeta that these rows make: a thread adds up its own columns over all of
 // its rows, the teams of a workgroup are joined in LDS, a workgroup writes one part.  The next row is on its way while one is
 // worked on.
 template <typename T, int SRC, bool FULL, int TPR, int NV, bool PARAM>
-__global__ void __launch_bounds__(wg_of(TPR), TPR > WG ? 2 : waves_for(NV + 1)) norm_bwd_kernel(NormArgs a) {
+__global__ void __launch_bounds__(wg_of(TPR), bwd_waves(TPR, NV, PARAM)) norm_bwd_kernel(NormArgs a) {
   constexpr int TEAMS = wg_of(TPR) / TPR;
   __shared__ float sums[2][2][16];
   __shared__ float join[PARAM && TEAMS > 1 ? 2 * TPR * NV * V : 1];
@@ -486,25 +498,28 @@ __global__ void __launch_bounds__(wg_of(TPR), TPR > WG ? 2 : waves_for(NV + 1)) 
   Row next;
   if (row < a.n) load(next, row);
   for (; row < a.n; row += step) {
-    const Row w = next;
+    Row w = next;
     if (row + step < a.n) load(next, row + step);
+    if constexpr (!FULL) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) w.dy[i].keep_from(skip_of<FULL>(t + TPR * i, E));
+    }
     // (dy is 0 behind the row's end, and with it all that is summed)
     float s[2] = {0.f, 0.f};
-    float xh[NV][V];
     const float shift = -w.mu * w.r;
+    const auto xh = [&](int i, int k) __attribute__((always_inline)) -> float {      // (made twice: kept, they cost more registers than time)
+      if constexpr (SRC == 2) return fmaf(w.p[i][k], w.r * w.p[i].step(), shift);
+      else return fmaf(w.x[i][k], w.r, shift);
+    };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float scale = w.r;
-      if constexpr (SRC == 2) scale *= w.p[i].step();
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        if constexpr (SRC == 2) xh[i][k] = fmaf(w.p[i][k], scale, shift);
-        else xh[i][k] = fmaf(w.x[i][k], scale, shift);
-        const float dy = w.dy[i][k], g = dy * gamma[i][k];
+        const float x = xh(i, k), dy = w.dy[i][k], g = dy * gamma[i][k];
         s[0] += g;
-        s[1] = fmaf(g, xh[i][k], s[1]);
+        s[1] = fmaf(g, x, s[1]);
         if constexpr (PARAM) {
-          pg[i][k] = fmaf(dy, xh[i][k], pg[i][k]);
+          pg[i][k] = fmaf(dy, x, pg[i][k]);
           pb[i][k] += dy;
         }
       }
@@ -517,8 +532,8 @@ __global__ void __launch_bounds__(wg_of(TPR), TPR > WG ? 2 : waves_for(NV + 1)) 
       for (int i = 0; i < NV; ++i) {
         float o[V];
 #pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = fmaf(xh[i][k], mx, fmaf(w.dy[i][k] * gamma[i][k], w.r, m));
-        Chunk<T>::template store<FULL>(dx, t + TPR * i, E, o);
+        for (int k = 0; k < V; ++k) o[k] = fmaf(xh(i, k), mx, fmaf(w.dy[i][k] * gamma[i][k], w.r, m));
+        store_chunk<FULL>(dx, t + TPR * i, E, o);
       }
     }
   }
@@ -543,8 +558,8 @@ __global__ void __launch_bounds__(wg_of(TPR), TPR > WG ? 2 : waves_for(NV + 1)) 
     for (int i = 0; i < NV; ++i) {
       const int c = t + TPR * i;
       float* const to = a.part + 2L * blockIdx.x * E;
-      Chunk<float>::store<FULL>(to, c, E, pg[i]);
-      Chunk<float>::store<FULL>(to + E, c, E, pb[i]);
+      store_chunk<FULL>(to, c, E, pg[i]);
+      store_chunk<FULL>(to + E, c, E, pb[i]);
     }
   }
 }
@@ -562,6 +577,7 @@ __global__ void __launch_bounds__(WG) pack_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float v[V];
+      if constexpr (!FULL) raw[i].keep_from(skip_of<FULL>(c0 + 64 * i, E));
       pack_chunk<FULL>(raw[i], v, a.q + row * E, a.b + row * ng, c0 + 64 * i, E);
     }
   }
@@ -578,7 +594,20 @@ __global__ void __launch_bounds__(WG) unpack_kernel(NormArgs a) {
       float v[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = raw[i][k] * raw[i].step();
-      Chunk<T>::template store<FULL>((T*)a.y + row * a.y_ss, c0 + 64 * i, E, v);
+      store_chunk<FULL>((T*)a.y + row * a.y_ss, c0 + 64 * i, E, v);
+    }
+  }
+}
+
+// ... rows of fewer than 8 features: one group each, 32 lanes
+template <typename T>
+__global__ void __launch_bounds__(WG) pack_narrow_kernel(NormArgs a, bool back) {
+  const int E = a.E, e = threadIdx.x % 32;
+  for (long row = (long)blockIdx.x * (WG / 32) + threadIdx.x / 32; row < a.n; row += (long)gridDim.x * (WG / 32)) {
+    if (!back) {
+      norm_in<T, 1>((const T*)a.x + row * a.x_ss, a.q + row * E, a.b + row, e, E, true);
+    } else if (e < E) {
+      ((T*)a.y + row * a.y_ss)[e] = (T)norm_in<T, 2>((const T*)nullptr, a.q + row * E, a.b + row, e, E, false);
     }
   }
 }
@@ -608,29 +637,22 @@ template <typename T, bool FULL, int TPR, int NV> void bwd_rows(const NormArgs& 
 // by the width alone (see above)
 template <typename T, bool FULL> hipError_t fwd(const NormArgs& a, hipStream_t s) {
   const int E = a.E;
-  if (E <= 512) fwd_rows<T, FULL, 64, 1>(a, s);
-  else if (E <= 1024) fwd_rows<T, FULL, 64, 2>(a, s);
-  else if (E <= 2048) fwd_rows<T, FULL, 256, 1>(a, s);
-  else if (E <= 4096) fwd_rows<T, FULL, 256, 2>(a, s);
-  else if (E <= 8192) fwd_rows<T, FULL, 256, 4>(a, s);
-  else if (E <= 16384) fwd_rows<T, FULL, 256, 8>(a, s);
-  else {
+  if (E < V || E > 16384) {
     const unsigned grid = grid_of(a.n, 16L * a.n_cu);
     if (a.x && a.q) norm_fwd_any_kernel<T, 1><<<grid, WG, 0, s>>>(a);
     else if (a.q) norm_fwd_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
     else norm_fwd_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
-  }
+  } else if (E <= 512) fwd_rows<T, FULL, 64, 1>(a, s);
+  else if (E <= 1024) fwd_rows<T, FULL, 64, 2>(a, s);
+  else if (E <= 2048) fwd_rows<T, FULL, 256, 1>(a, s);
+  else if (E <= 4096) fwd_rows<T, FULL, 256, 2>(a, s);
+  else if (E <= 8192) fwd_rows<T, FULL, 512, 2>(a, s);
+  else fwd_rows<T, FULL, 1024, 2>(a, s);
   return hipGetLastError();
 }
 template <typename T, bool FULL> hipError_t bwd(const NormArgs& a, hipStream_t s) {
   const int E = a.E;
-  if (E <= 512) bwd_rows<T, FULL, 64, 1>(a, s);
-  else if (E <= 1024) bwd_rows<T, FULL, 64, 2>(a, s);
-  else if (E <= 2048) bwd_rows<T, FULL, 256, 1>(a, s);
-  else if (E <= 4096) bwd_rows<T, FULL, 256, 2>(a, s);
-  else if (E <= 8192) bwd_rows<T, FULL, 256, 4>(a, s);
-  else if (E <= 16384) bwd_rows<T, FULL, 512, 4>(a, s);
-  else {
+  if (E < V || E > 16384) {
     // (the sums over the rows first: dx may lie where dy does)
     if (a.dgamma || a.dbeta) {
       const dim3 grid((unsigned)((a.E + WG - 1) / WG), (unsigned)a.parts);
@@ -643,7 +665,12 @@ template <typename T, bool FULL> hipError_t bwd(const NormArgs& a, hipStream_t s
       if (a.q) norm_bwd_any_kernel<T, 2><<<grid, WG, 0, s>>>(a);
       else norm_bwd_any_kernel<T, 0><<<grid, WG, 0, s>>>(a);
     }
-  }
+  } else if (E <= 512) bwd_rows<T, FULL, 64, 1>(a, s);
+  else if (E <= 1024) bwd_rows<T, FULL, 64, 2>(a, s);
+  else if (E <= 2048) bwd_rows<T, FULL, 256, 1>(a, s);
+  else if (E <= 4096) bwd_rows<T, FULL, 256, 2>(a, s);
+  else if (E <= 8192) bwd_rows<T, FULL, 512, 2>(a, s);
+  else bwd_rows<T, FULL, 512, 4>(a, s);
   return hipGetLastError();
 }
 // f(an element, whether E is a multiple of 8)
@@ -669,14 +696,18 @@ hipError_t launch_norm_bwd(const NormArgs& a, int is_f32, hipStream_t s) {
 hipError_t launch_pack(const NormArgs& a, int is_f32, hipStream_t s) {
   const dim3 grid((unsigned)((a.E + 2047) / 2048), grid_of((a.n + 3) / 4, 16384));
   return by_type(a, is_f32, [&](auto t, auto full) {
-    pack_kernel<decltype(t), decltype(full)::value><<<grid, WG, 0, s>>>(a);
+    using E = decltype(t);
+    if (a.E < V) pack_narrow_kernel<E><<<grid_of((a.n + 7) / 8, 16384), WG, 0, s>>>(a, false);
+    else pack_kernel<E, decltype(full)::value><<<grid, WG, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 hipError_t launch_unpack(const NormArgs& a, int is_f32, hipStream_t s) {
   const dim3 grid((unsigned)((a.E + 2047) / 2048), grid_of((a.n + 3) / 4, 16384));
   return by_type(a, is_f32, [&](auto t, auto full) {
-    unpack_kernel<decltype(t), decltype(full)::value><<<grid, WG, 0, s>>>(a);
+    using E = decltype(t);
+    if (a.E < V) pack_narrow_kernel<E><<<grid_of((a.n + 7) / 8, 16384), WG, 0, s>>>(a, true);
+    else unpack_kernel<E, decltype(full)::value><<<grid, WG, 0, s>>>(a);
     return hipGetLastError();
   });
 }

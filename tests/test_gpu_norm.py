@@ -71,7 +71,7 @@ def check(got, ref, bound, tag):
         assert worst <= 1.0, f"{tag} {name}: off by {worst:.3g} of the bound"
 
 
-SIZES = [(1, 1), (1, 31), (3, 33), (5, 64), (70, 200), (33, 1001), (130, 768), (19, 1024), (300, 512), (2, 1032), (17, 4096), (6, 6144),
+SIZES = [(1, 1), (40, 7), (9, 8), (77, 9), (11, 15), (1, 31), (3, 33), (5, 64), (70, 200), (33, 1001), (130, 768), (19, 1024), (300, 512), (2, 1032), (17, 4096), (6, 6144),
          (9, 8192), (3, 8193), (5, 16384), (3, 20001), (700, 96), (2100, 40)]
 
 
@@ -203,7 +203,7 @@ def packed_reference(x):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n,E,pad", [(1, 1, 0), (3, 31, 2), (2, 33, 0), (7, 64, 0), (5, 200, 8), (300, 96, 3), (4, 4096, 0), (1000, 40, 0), (9, 1001, 0)])
+@pytest.mark.parametrize("n,E,pad", [(1, 1, 0), (60, 5, 1), (33, 8, 0), (21, 13, 0), (3, 31, 2), (2, 33, 0), (7, 64, 0), (5, 200, 8), (300, 96, 3), (4, 4096, 0), (1000, 40, 0), (9, 1001, 0)])
 def test_pack_and_unpack(n, E, pad, dtype):
     g = torch.Generator().manual_seed(n + E)
     x = torch.randn((n, E), generator=g) * torch.exp(3.0 * torch.randn((n, E), generator=g))
