@@ -14,9 +14,11 @@
 // entry p - 1 is then near -1 and next to exact, where -1 / count would carry the same rounding, up to 2^-8, into every gradient.
 // No atomics: results repeat bit for bit.
 //
-// bf16 tiles as in the projections (lvx_project.hip, lvx_project_bwd.hip): a workgroup of 4 waves makes 256 x 256 of a product, a
-// wave 128 x 128 of it as 4 x 4 blocks in the accumulation registers, tile pairs of 64 contraction steps go through two
-// slots of 64 KB.
+// bf16 tiles of 256 x 256 and tile pairs of 64 contraction steps in two slots of 64 KB, as in the projections (lvx_project.hip,
+// lvx_project_bwd.hip), but of 8 waves, two on a SIMD, each 128 x 64 as 4 x 2 blocks in the accumulation registers: the tile loop is
+// no faster than that of 4 waves with 128 x 128 each (it reads a third more from LDS, and both run at what the chip's power allows), but
+// what stands before and behind it is: a tile with one pair 13.7 -> 10.6 us (statistics), 19.5 -> 16.9 (gradient), 300 tokens x 1024 x 50000,
+// 16 pairs, dw 64 -> 57.
 #include "lvx_internal.h"
 #include "lvx_mfma.h"
 #include "lvx_kv_ring.h"
@@ -32,8 +34,11 @@ constexpr int T = 256, BK = 64, NSLOT = 2;
 constexpr int RK_ROWB = BK * 2;        // [256][64] tile: bytes of a row
 constexpr int KR_ROWB = T * 2;         // [64][256] tile
 constexpr int TILE_B = BK * KR_ROWB, SLOT_B = 2 * TILE_B, RING_B = NSLOT * SLOT_B;
-constexpr int TB_PITCH = 128 * 2 + 16, TB_WAVE = 128 * TB_PITCH;       // epilogue: a wave's rows on their way out
-constexpr int SMEM_B = RING_B > 4 * TB_WAVE ? RING_B : 4 * TB_WAVE;
+constexpr int NW = 8;                  // waves of a workgroup
+constexpr int CB = 16 / NW, WC = 32 * CB;              // a wave's column blocks, and its columns
+constexpr int TB_PITCH = WC * 2 + 16;  // epilogue: a wave's rows on their way out
+constexpr int SMEM_B = RING_B > NW * 128 * TB_PITCH ? RING_B : NW * 128 * TB_PITCH;
+static_assert(SMEM_B <= 160 * 1024, "the layout fits a compute unit");
 enum { STATS = 0, GRAD = 1, DX = 2, DW = 3 };
 
 __device__ __forceinline__ int perm_of(int r) { return (r & 7) ^ ((r >> 3) & 1); }
@@ -149,12 +154,12 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
 // the largest logit (times log2 e) and the sum of exponentials against it
 template <int JB, bool WHOLE, class Z> __device__ __forceinline__ void tile_stats_of(int g, int cols, Z&& z, float* m2, float* s) {
   float y[JB][16];
-  const int end = opaque(cols - 4 * g);
+  const int end = WHOLE ? 0 : opaque(cols - 4 * g);
 #pragma unroll
   for (int j = 0; j < JB; ++j)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      y[j][v] = z(v, j) * LOG2E;
+      y[j][v] = z(v, j);
       if (!WHOLE) y[j][v] = 32 * j + 8 * (v / 4) + v % 4 < end ? y[j][v] : -__builtin_inff();
     }
   // (a NaN is dropped here and comes back in the sum)
@@ -163,15 +168,15 @@ template <int JB, bool WHOLE, class Z> __device__ __forceinline__ void tile_stat
   for (int j = 0; j < JB; ++j)
 #pragma unroll
     for (int v = 0; v < 16; v += 2) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(mx) : "v"(y[j][v]), "v"(y[j][v + 1]));
-  mx = xhalf_max(mx);
+  mx = xhalf_max(mx) * LOG2E;
   const float at = mx == -__builtin_inff() ? 0.f : mx;
-  float sum = 0.f;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < JB; ++j)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) sum += exp2_fast(y[j][v] - at);
+    for (int v = 0; v < 16; ++v) sum[v % 4] += exp2_fast(fmaf(y[j][v], LOG2E, -at));
   *m2 = mx;
-  *s = xhalf_sum(sum);
+  *s = xhalf_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
 }
 template <int JB, class Z> __device__ __forceinline__ void tile_stats(int g, int cols, Z&& z, float* m2, float* s) {
   if (cols >= 32 * JB) tile_stats_of<JB, true>(g, cols, z, m2, s);      // (uniform)
@@ -236,17 +241,17 @@ __global__ void __launch_bounds__(256) xent_join_kernel(XentArgs a, int n_parts)
 // Rows of x go by the list; rows behind the last token read the last one again (their g is 0), rows of w behind the vocabulary its last
 // (their columns of g are 0).
 template <int MODE, int RB>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
+__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4, NW / 4)))
 xent_bf16_kernel(XentArgs a) {
   constexpr bool LOGITS = MODE == STATS || MODE == GRAD;
-  static_assert(RB == 4 || (RB == 2 && MODE != DW), "the low tiles are for few tokens");
+  static_assert(RB == 4 || RB == 2, "tile heights");
   constexpr int TR = 64 * RB;                        // rows of a workgroup's tile
-  constexpr int NB = MODE == DW ? 8 : 2 * RB;        // copies per wave and tile pair: B side (rows),
-  constexpr int NPART = 8 + NB;                      // and with the 8 of the A side (columns)
+  constexpr int NA = 32 / NW, NB = 8 * RB / NW;      // copies per wave and tile pair: A side (columns), B side (rows)
+  constexpr int NPART = NA + NB;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int M = a.head->count, E = a.E;
   const int cols = (int)(a.v1 - a.v0);               // of the piece
-  const int n_rt = MODE == DW ? (cols + T - 1) / T : (M + TR - 1) / TR;
+  const int n_rt = ((MODE == DW ? cols : M) + TR - 1) / TR;
   const int n_ct = LOGITS ? (cols + T - 1) / T : (E + T - 1) / T;
   const int parts = MODE == DX ? a.head->parts : 1;
   int rt, ct, part;
@@ -254,7 +259,7 @@ xent_bf16_kernel(XentArgs a) {
   const int r0 = rt * TR, c0 = ct * T;               // (of the list / of the piece / of the features)
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave >> 1, wn = wave & 1;
+  const int wm = wave / (NW / 2), wn = wave % (NW / 2);
   const int nk_all = LOGITS ? E / BK : MODE == DX ? (cols + BK - 1) / BK : (M + BK - 1) / BK;
   const int k0 = MODE == DX ? (int)((long)part * nk_all / parts) : 0;
   const int nk = MODE == DX ? (int)((long)(part + 1) * nk_all / parts) - k0 : nk_all;
@@ -263,43 +268,50 @@ xent_bf16_kernel(XentArgs a) {
   const long g_row_b = a.g_pitch * 2L;
 
   // ---- copies into [rows][64] tiles: one instruction moves 8 rows x 128 bytes, lane l the chunk (l % 8) ^ perm_of(row) of row l / 8
-  unsigned bo[LOGITS || MODE == DX ? 2 * RB : 1], ao[LOGITS ? 8 : 1];
+  unsigned bo[MODE == DW ? 1 : NB], ao[LOGITS ? NA : 1];
   if constexpr (LOGITS || MODE == DX) {
 #pragma unroll
-    for (int j = 0; j < 2 * RB; ++j) {
-      const int r = r0 + 16 * RB * wave + 8 * j + (lane >> 3);
+    for (int j = 0; j < NB; ++j) {
+      const int r = r0 + 8 * NB * wave + 8 * j + (lane >> 3);
       const unsigned swz = 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + (lane >> 3)));
       if (LOGITS) bo[j] = (unsigned)a.tok[min(r, M - 1)] * xrow_b + swz;
-      else bo[j] = (unsigned)((16 * RB * wave + 8 * j + (lane >> 3)) * g_row_b) + swz;
+      else bo[j] = (unsigned)((8 * NB * wave + 8 * j + (lane >> 3)) * g_row_b) + swz;
     }
   }
   if constexpr (LOGITS) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int r = 64 * wave + 8 * j + (lane >> 3);
+    for (int j = 0; j < NA; ++j) {
+      const int r = 8 * NA * wave + 8 * j + (lane >> 3);
       ao[j] = (unsigned)min((long)r, a.V - 1 - a.v0 - c0) * wrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + (lane >> 3)));
     }
   }
   // ---- copies into [64][256] tiles: one instruction moves 2 rows x 512 bytes, lane l position l % 32 of row l / 32, which holds the
-  // chunk (l % 32) ^ 4 (row % 4); a wave copies rows 16 wave + 2 j + l / 32.  Features past the last one: the tile's first chunk again.
+  // chunk (l % 32) ^ 4 (row % 4); a wave copies rows 2 NA wave + 2 j + l / 32.  Features past the last one: the tile's first chunk again.
   const int lh = lane >> 5, pos = lane & 31;
   unsigned kr_a[2], kr_b[2];
 #pragma unroll
   for (int par = 0; par < 2; ++par) {
     const int c = pos ^ (4 * ((2 * par + lh) & 3));
     kr_a[par] = LOGITS || c0 + 8 * c >= E ? 0u : 16u * (unsigned)c;
-    kr_b[par] = 16u * (unsigned)c + (MODE == DW ? (unsigned)((16 * wave + lh) * g_row_b) : 0u);
+  }
+  // (DW's tile of g: [64][TR], an instruction moves BR rows, lane l position l % (64 / BR) of row l / (64 / BR))
+  constexpr int BR = 512 / TR, B_ROWB = TR * 2;
+  if constexpr (MODE == DW) {
+    const int row = lane / (64 / BR);
+#pragma unroll
+    for (int par = 0; par < 2; ++par)
+      kr_b[par] = 16u * (unsigned)((lane % (64 / BR)) ^ (4 * ((BR * par + row) & 3))) + (unsigned)((BR * NB * wave + row) * g_row_b);
   }
   // Where the next pair to go out starts on either side (its copies go out in order, pair by pair).  DX: the rows of w left behind the
-  // pair's first, and a lane's row.  DW: the byte offsets of the rows of x that a wave copies, lane l that of row 16 wave + 2 (l % 8) + l / 32.
+  // pair's first, and a lane's row.  DW: the byte offsets of the rows of x that a wave copies, lane l that of row 2 NA wave + 2 (l % 8) + l / 32.
   const char* ap = LOGITS ? (const char*)a.w + (a.v0 + c0) * wrow_b
                           : MODE == DX ? (const char*)a.w + ((a.v0 + k0 * BK) * E + c0) * 2 : (const char*)a.x + 2L * c0;
   const char* bp = LOGITS ? (const char*)a.x
                           : MODE == DX ? (const char*)a.g + r0 * g_row_b + (long)k0 * RK_ROWB : (const char*)a.g + 2L * r0;
-  const unsigned a_lane = (unsigned)(16 * wave + lh) * wrow_b;
+  const unsigned a_lane = (unsigned)(2 * NA * wave + lh) * wrow_b;
   long w_left = a.V - 1 - a.v0 - (long)k0 * BK;
   unsigned w_last = 0u;
-  const auto x_rows = [&](int kt) __attribute__((always_inline)) -> int { return a.tok[min(kt * BK + 16 * wave + 2 * (lane & 7) + lh, M - 1)]; };
+  const auto x_rows = [&](int kt) __attribute__((always_inline)) -> int { return a.tok[min(kt * BK + 2 * NA * wave + 2 * (lane & 7) + lh, M - 1)]; };
   unsigned xr = 0u;
   // lane j of every 16 lanes
   const auto lane_of_16 = [&](unsigned x, int j) __attribute__((always_inline)) -> unsigned {
@@ -316,24 +328,24 @@ xent_bf16_kernel(XentArgs a) {
   };
   auto issue_part = [&](int kt, int p) __attribute__((always_inline)) {
     const unsigned st = smem_u + (unsigned)((kt % NSLOT) * SLOT_B);
-    if (p < 8) {                                     // A side
+    if (p < NA) {                                    // A side
       const int j = p;
       if constexpr (LOGITS) {
-        dma16u(ap, ao[j], st + (unsigned)((64 * wave + 8 * j) * RK_ROWB));
+        dma16u(ap, ao[j], st + (unsigned)((8 * NA * wave + 8 * j) * RK_ROWB));
       } else if constexpr (MODE == DX) {
         if (j == 0) w_last = (unsigned)min(w_left, 63L) * wrow_b;
-        dma16u(ap, min(a_lane + (unsigned)(2 * j) * wrow_b, w_last) + kr_a[j & 1], st + (unsigned)((16 * wave + 2 * j) * KR_ROWB));
+        dma16u(ap, min(a_lane + (unsigned)(2 * j) * wrow_b, w_last) + kr_a[j & 1], st + (unsigned)((2 * NA * wave + 2 * j) * KR_ROWB));
       } else {
-        dma16u(ap, lane_of_16(xr, j) + kr_a[j & 1], st + (unsigned)((16 * wave + 2 * j) * KR_ROWB));
+        dma16u(ap, lane_of_16(xr, j) + kr_a[j & 1], st + (unsigned)((2 * NA * wave + 2 * j) * KR_ROWB));
       }
-      if (j == 7) {
+      if (j == NA - 1) {
         if (LOGITS) ap += RK_ROWB;
         if (MODE == DX) { ap += 64L * wrow_b; w_left -= 64; }
       }
     } else {                                         // B side
-      const int j = p - 8;
-      if constexpr (MODE != DW) dma16u(bp, bo[j], st + (unsigned)(TILE_B + (16 * RB * wave + 8 * j) * RK_ROWB));
-      else dma16u(bp, kr_b[j & 1] + (unsigned)(2 * j) * (unsigned)g_row_b, st + (unsigned)(TILE_B + (16 * wave + 2 * j) * KR_ROWB));
+      const int j = p - NA;
+      if constexpr (MODE != DW) dma16u(bp, bo[j], st + (unsigned)(TILE_B + (8 * NB * wave + 8 * j) * RK_ROWB));
+      else dma16u(bp, kr_b[j & 1] + (unsigned)(BR * j) * (unsigned)g_row_b, st + (unsigned)(TILE_B + BR * (NB * wave + j) * B_ROWB));
       if (j == NB - 1) bp += MODE == DW ? 64 * g_row_b : RK_ROWB;
     }
   };
@@ -342,38 +354,39 @@ xent_bf16_kernel(XentArgs a) {
   // where the other operand has its eight steps in one chunk (DX), 4 g .. and 8 + 4 g .. where both are such tiles (DW)
   const int j16 = lane & 15, jr = j16 >> 2, tr_col = 32 * ((lane >> 4) & 1) + 8 * (j16 & 3);
   constexpr int KG = MODE == DX ? 8 : 4, KH = MODE == DX ? 4 : 8;
-  int rd[4], ka[4], kb[4];
+  int rd[4], ka[CB], kb[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) rd[q] = l31 * RK_ROWB + 16 * ((2 * q + g) ^ perm_of(l31));
 #pragma unroll
+  for (int jj = 0; jj < CB; ++jj) ka[jj] = (KG * g + jr) * KR_ROWB + tr_col + 64 * ((CB * wn + jj) ^ jr);
+#pragma unroll
   for (int jj = 0; jj < 4; ++jj) {
-    ka[jj] = (KG * g + jr) * KR_ROWB + tr_col + 64 * ((4 * wn + jj) ^ jr);
-    kb[jj] = TILE_B + (KG * g + jr) * KR_ROWB + tr_col + 64 * ((4 * wm + jj) ^ jr);
+    kb[jj] = TILE_B + (KG * g + jr) * B_ROWB + tr_col + 64 * ((RB * wm + jj) ^ jr);
   }
-  auto tr_op = [&](const char* p) __attribute__((always_inline)) -> bf16x8 {
-    const s16x4 lo = lds_read_tr(p), hi = lds_read_tr(p + KH * KR_ROWB);
+  auto tr_op = [&](const char* p, auto pitch) __attribute__((always_inline)) -> bf16x8 {
+    const s16x4 lo = lds_read_tr(p), hi = lds_read_tr(p + KH * decltype(pitch)::value);
     typedef __attribute__((ext_vector_type(8))) short s16x8;
     const s16x8 r = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     return __builtin_bit_cast(bf16x8, r);
   };
   auto a_op = [&](const char* st, int q, int j) __attribute__((always_inline)) -> bf16x8 {
-    if constexpr (LOGITS) return *(const bf16x8*)(st + (wn * 128 + 32 * j) * RK_ROWB + rd[q]);
-    else return tr_op(st + ka[j] + 16 * q * KR_ROWB);
+    if constexpr (LOGITS) return *(const bf16x8*)(st + (wn * WC + 32 * j) * RK_ROWB + rd[q]);
+    else return tr_op(st + ka[j] + 16 * q * KR_ROWB, std::integral_constant<int, KR_ROWB>{});
   };
   auto b_op = [&](const char* st, int q, int i) __attribute__((always_inline)) -> bf16x8 {
     if constexpr (MODE != DW) return *(const bf16x8*)(st + TILE_B + (wm * 32 * RB + 32 * i) * RK_ROWB + rd[q]);
-    else return tr_op(st + kb[i] + 16 * q * KR_ROWB);
+    else return tr_op(st + kb[i] + 16 * q * B_ROWB, std::integral_constant<int, B_ROWB>{});
   };
 
-  f32x16 acc[4][RB];                                 // [column block j][row block i]: lane = row, registers = columns
+  f32x16 acc[CB][RB];                                // [column block j][row block i]: lane = row, registers = columns
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < CB; ++j)
 #pragma unroll
     for (int i = 0; i < RB; ++i) { acc[j][i] = zero16(); asm volatile("" : "+a"(acc[j][i])); }
-  constexpr int NU = 4 * RB;
-  auto mma16 = [&](const bf16x8 (&bv)[RB], const bf16x8 (&av)[4], auto&& hook) __attribute__((always_inline)) {
+  constexpr int NU = CB * RB;
+  auto mma16 = [&](const bf16x8 (&bv)[RB], const bf16x8 (&av)[CB], auto&& hook) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < CB; ++j)
 #pragma unroll
       for (int i = 0; i < RB; ++i) {
         kvring::mfma_acc(acc[j][i], av[j], bv[i]);
@@ -393,23 +406,23 @@ xent_bf16_kernel(XentArgs a) {
     if (nk > 1) wait_vmcnt<NPART>();
     else wait_vmcnt<0>();
     wg_barrier();
-    bf16x8 ba[RB], aa[4], bb[RB], ab[4];             // operands of even / odd k-steps
+    bf16x8 ba[RB], aa[CB], bb[RB], ab[CB];             // operands of even / odd k-steps
 #pragma unroll
     for (int i = 0; i < RB; ++i) ba[i] = b_op(smem, 0, i);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) aa[i] = a_op(smem, 0, i);
-    auto fetch = [&](const char* st, int q, int u, bf16x8 (&bv)[RB], bf16x8 (&av)[4]) __attribute__((always_inline)) {
+    for (int i = 0; i < CB; ++i) aa[i] = a_op(smem, 0, i);
+    auto fetch = [&](const char* st, int q, int u, bf16x8 (&bv)[RB], bf16x8 (&av)[CB]) __attribute__((always_inline)) {
       if (u < RB) bv[u] = b_op(st, q, u);
-      else if (u < RB + 4) av[u - RB] = a_op(st, q, u - RB);
+      else if (u < RB + CB) av[u - RB] = a_op(st, q, u - RB);
     };
-    constexpr int EB = NU / NB, EA = NU / 8;         // a copy of one side every so many matrix instructions of a k-step
+    constexpr int EB = NU / NB, EA = NU / NA;        // a copy of one side every so many matrix instructions of a k-step
     auto pair = [&](int P, auto steady, bool send2, bool send1, bool more) __attribute__((always_inline)) {
       constexpr bool STEADY = decltype(steady)::value;
       const char* const st = smem + (P % NSLOT) * SLOT_B;
       const char* const sn = smem + ((P + 1) % NSLOT) * SLOT_B;
       mma16(ba, aa, [&](int u) __attribute__((always_inline)) {
         fetch(st, 1, u, bb, ab);
-        if ((STEADY || send2) && u % EB == EB - 1) issue_part(P + 1, 8 + u / EB);
+        if ((STEADY || send2) && u % EB == EB - 1) issue_part(P + 1, NA + u / EB);
       });
       int next_rows = 0;
       if constexpr (MODE == DW) next_rows = x_rows(P + 2);        // (has come when the wait below is over)
@@ -435,30 +448,37 @@ xent_bf16_kernel(XentArgs a) {
   // ---- epilogue: every wave has left the ring, and the last matrix instructions have retired
   wg_barrier();
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < CB; ++j)
 #pragma unroll
     for (int i = 0; i < RB; i += 2) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[j][i]), "+a"(acc[j][i + 1]));
   if constexpr (MODE == STATS) {
-    const int left = (int)min((long)T, a.V - c0) - wn * 128;      // columns of this wave
-    const int p = 2 * ct + wn;
+    const int cw = c0 + wn * WC, left = (int)min((long)WC, a.V - cw);      // columns of this wave
+    float2* const sums = (float2*)smem;              // [NW / 2][TR]
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
-      const int r = r0 + wm * 32 * RB + 32 * i + l31;
+      const int rl = wm * 32 * RB + 32 * i + l31, r = r0 + rl;
       const auto z = [&](int v, int j) __attribute__((always_inline)) -> float { return acc[j][i][v]; };
       float m2, s;
-      tile_stats<4>(g, left, z, &m2, &s);
-      if (g == 0 && r < M) a.part[(long)p * a.Mp + r] = make_float2(m2, s);
-      const int c = r < M ? a.lab[r] - c0 - wn * 128 : -1;
-      if (__any(c >= 0 && c < 128)) {
-        const float y = tile_pick<4>(g, c, z);
-        if (c >= 0 && c < 128 && ((c >> 2) & 1) == g) a.zlab[r] = y;
+      tile_stats<CB>(g, left, z, &m2, &s);
+      if (g == 0) sums[wn * TR + rl] = make_float2(m2, s);
+      const int c = r < M ? a.lab[r] - cw : -1;
+      if (__any(c >= 0 && c < WC)) {
+        const float y = tile_pick<CB>(g, c, z);
+        if (c >= 0 && c < WC && ((c >> 2) & 1) == g) a.zlab[r] = y;
       }
+    }
+    __syncthreads();
+    if (tid < TR && r0 + tid < M) {                  // one number for all columns of the tile
+      float m = -__builtin_inff(), s = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW / 2; ++w) join_stats(&m, &s, sums[w * TR + tid].x, sums[w * TR + tid].y);
+      a.part[(long)ct * a.Mp + r0 + tid] = make_float2(m, s);
     }
   } else if constexpr (MODE == DX) {
     // in the order of the registers, 16 bytes a lane (xent_dx_kernel reads them so), on top of what the pieces before left
-    float* const out = a.dx_part + (((long)part * n_rt + rt) * n_ct + ct) * (TR * T) + wave * (TR * T / 4) + lane * 4;
+    float* const out = a.dx_part + (((long)part * n_rt + rt) * n_ct + ct) * (TR * T) + wave * (TR * T / NW) + lane * 4;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < CB; ++j) {
       f32x4 old[RB][4];
       if (!a.first) {
 #pragma unroll
@@ -476,10 +496,10 @@ xent_bf16_kernel(XentArgs a) {
         }
     }
   } else {
-    // turned around in LDS, rounded to bf16, written in whole 256-byte row segments
-    char* const tb = smem + wave * TB_WAVE;
+    // turned around in LDS, rounded to bf16, written in whole segments of a row, 64 CB bytes each
+    char* const tb = smem + wave * (32 * RB * TB_PITCH);
     const float scale = a.head->scale;
-    const int left = cols - c0 - wn * 128;           // columns of this wave (GRAD)
+    const int left = cols - c0 - wn * WC;            // columns of this wave (GRAD)
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
       float lse2 = 0.f, d = 0.f;
@@ -490,7 +510,7 @@ xent_bf16_kernel(XentArgs a) {
           const int t = a.tok[r];
           lse2 = a.lse[t] * LOG2E;
           d = a.lab[r] < 0 ? __builtin_nanf("") : a.d_loss[t] / scale;
-          c = a.lab[r] - (int)a.v0 - c0 - wn * 128;
+          c = a.lab[r] - (int)a.v0 - c0 - wn * WC;
         }
       }
       const auto put = [&](auto plain) __attribute__((always_inline)) {
@@ -498,7 +518,7 @@ xent_bf16_kernel(XentArgs a) {
         constexpr bool PLAIN = decltype(plain)::value;
         const int end = PLAIN ? 0 : opaque(d != 0.f ? left - 4 * g : 0), hot = PLAIN ? 0 : opaque(c - 4 * g);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < CB; ++j)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {              // registers 4 q .. 4 q + 3: columns 32 j + 8 q + 4 g + (0..3)
             float y[4];
@@ -517,19 +537,20 @@ xent_bf16_kernel(XentArgs a) {
             *(u32x2*)(tb + (32 * i + l31) * TB_PITCH + (32 * j + 8 * q + 4 * g) * 2) = u32x2{pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3])};
           }
       };
-      if (MODE == DW || (left >= 128 && !__any((c >= 0 && c < 128) || d == 0.f))) put(std::true_type{});
+      if (MODE == DW || (left >= WC && !__any((c >= 0 && c < WC) || d == 0.f))) put(std::true_type{});
       else put(std::false_type{});
     }
-    const int row0 = lane >> 4, ch = lane & 15;
+    constexpr int LR = WC / 8, RI = 64 / LR;         // lanes that write a row, rows at a time
+    const int row0 = lane / LR, ch = lane % LR;
 #pragma unroll 4
-    for (int it = 0; it < 8 * RB; ++it) {
-      const u32x4 y = *(const u32x4*)(tb + (4 * it + row0) * TB_PITCH + ch * 16);
-      const int r = r0 + wm * 32 * RB + 4 * it + row0;
+    for (int it = 0; it < 32 * RB / RI; ++it) {
+      const int rl = RI * it + row0, r = r0 + wm * 32 * RB + rl;
+      const u32x4 y = *(const u32x4*)(tb + rl * TB_PITCH + ch * 16);
+      const int c = c0 + wn * WC + 8 * ch;
       if constexpr (MODE == GRAD) {
-        *(u32x4*)((char*)a.g + r * g_row_b + 2L * (c0 + wn * 128 + 8 * ch)) = y;
+        *(u32x4*)((char*)a.g + r * g_row_b + 2L * c) = y;
       } else {
-        const int e = c0 + wn * 128 + 8 * ch;
-        if (r < cols && e < E) *(u32x4*)((uint16_t*)a.dw + (a.v0 + r) * E + e) = y;
+        if (r < cols && c < E) *(u32x4*)((uint16_t*)a.dw + (a.v0 + r) * E + c) = y;
       }
     }
   }
@@ -669,8 +690,8 @@ __global__ void __launch_bounds__(256) xent_dx_bf16_kernel(XentArgs a, unsigned 
     if (r >= M || c >= E) return;
     const int tr = a.tile_rows, n_ct = (E + T - 1) / T, rl = r % tr, cl = c % T;
     const long tile = (long)(r / tr) * n_ct + c / T, step = (long)((M + tr - 1) / tr) * n_ct * tr * T;
-    const int wave = rl / (tr / 2) * 2 + cl / 128, i = rl % (tr / 2) / 32, j = cl % 128 / 32, q = cl % 32 / 8;
-    const float* from = a.dx_part + tile * (tr * T) + wave * (tr * T / 4) + ((j * (tr / 64) + i) * 4 + q) * 256 + (rl % 32 + 32 * (cl / 4 % 2)) * 4;
+    const int wave = rl / (tr / 2) * (NW / 2) + cl / WC, i = rl % (tr / 2) / 32, j = cl % WC / 32, q = cl % 32 / 8;
+    const float* from = a.dx_part + tile * (tr * T) + wave * (tr * T / NW) + ((j * (tr / 64) + i) * 4 + q) * 256 + (rl % 32 + 32 * (cl / 4 % 2)) * 4;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     for (int p = 0; p < a.head->parts; ++p) s += *(const f32x4*)(from + p * step);
     s *= a.head->scale;
@@ -864,7 +885,7 @@ template <int MODE, int RB> hipError_t launch_tiles(const XentArgs& a, long grid
   static SmemOnce once;
   const hipError_t e = ensure_dynamic_lds((const void*)xent_bf16_kernel<MODE, RB>, SMEM_B, &once);
   if (e != hipSuccess) return e;
-  xent_bf16_kernel<MODE, RB><<<(unsigned)grid, 256, SMEM_B, s>>>(a);
+  xent_bf16_kernel<MODE, RB><<<(unsigned)grid, 64 * NW, SMEM_B, s>>>(a);
   return hipGetLastError();
 }
 // (GRAD: 64 tokens whatever their number: the contraction of dw runs over g's rows 64 at a time)
@@ -878,6 +899,11 @@ template <int MODE, int RB, int NS> hipError_t launch_few(const XentArgs& a, lon
   return hipGetLastError();
 }
 long up(long n, long by) { return (n + by - 1) / by; }
+// dw: tiles of 128 rows where those of 256 leave a quarter of the compute units without one (2000 tokens x 512 against 8000: 43 -> 31 us)
+hipError_t launch_dw(const XentArgs& a, long cols, hipStream_t s) {
+  if (up(cols, T) * up(a.E, T) * 4 <= 3L * a.n_cu) return launch_tiles<DW, 2>(a, strip_grid(up(cols, 128) * up(a.E, T)), s);
+  return launch_tiles<DW, 4>(a, strip_grid(up(cols, T) * up(a.E, T)), s);
+}
 // float32: the edge of the tiles of a product.  64 where 128 makes less than two for every compute unit: 300 tokens x 512 features against 5003,
 // the four products 246 -> 112 us
 int f32_edge(long rows, long cols, int n_cu) { return up(rows, 128) * up(cols, 128) < 2L * n_cu ? 64 : 128; }
@@ -923,7 +949,7 @@ hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
   const hipError_t e = logits<STATS>(a, is_f32, s);
   if (e != hipSuccess) return e;
   const long wgs = up(a.n, 8);
-  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : a.n <= FEW ? (int)up(a.V, 128) : (int)(2 * up(a.V, T)));
+  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : a.n <= FEW ? (int)up(a.V, 128) : (int)up(a.V, T));
   return hipGetLastError();
 }
 
@@ -938,7 +964,7 @@ hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
     const long cols = a.v1 - a.v0;
     e = logits<GRAD>(a, is_f32, s);
     if (e == hipSuccess && a.dw)
-      e = is_f32 ? f32_product<DW>(a, cols, a.E, f32_edge(cols, a.E, a.n_cu), s) : launch_tiles<DW, 4>(a, strip_grid(up(cols, T) * up(a.E, T)), s);
+      e = is_f32 ? f32_product<DW>(a, cols, a.E, f32_edge(cols, a.E, a.n_cu), s) : launch_dw(a, cols, s);
     if (e == hipSuccess && a.dx) {
       e = is_f32 ? f32_product<DX>(a, a.n, a.E, a.tile, s)
                  : a.tile_rows == 128 ? launch_tiles<DX, 2>(a, strip_grid(a.slots), s) : launch_tiles<DX, 4>(a, strip_grid(a.slots), s);
