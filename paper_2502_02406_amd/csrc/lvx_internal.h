@@ -220,6 +220,7 @@ struct XentArgs {
   long Mp;              // n rounded up to 256
   float2* part;         // forward, [xent_stat_parts][Mp]: largest logit (times log2 e) and sum of exponentials
   float* zlab;          // forward, [n]: the label's logit
+  float2* row;          // backward, [n]: lse log2 e, and d_loss (NaN where the label is not in the vocabulary)
   void* g;              // backward, [Mp][g_pitch] of x's type: the logits' gradient of a piece of the vocabulary
   long g_pitch, piece;  // columns of a piece; a row of g has as many, rounded up to 256
   float* dx_part;       // backward, [slots] tiles of sums of dx

@@ -36,9 +36,9 @@ constexpr int KR_ROWB = T * 2;         // [64][256] tile
 constexpr int TILE_B = BK * KR_ROWB, SLOT_B = 2 * TILE_B, RING_B = NSLOT * SLOT_B;
 constexpr int NW = 8;                  // waves of a workgroup
 constexpr int CB = 16 / NW, WC = 32 * CB;              // a wave's column blocks, and its columns
-constexpr int TB_PITCH = WC * 2 + 16;  // epilogue: a wave's rows on their way out
-constexpr int SMEM_B = RING_B > NW * 128 * TB_PITCH ? RING_B : NW * 128 * TB_PITCH;
-static_assert(SMEM_B <= 160 * 1024, "the layout fits a compute unit");
+constexpr int OUT_B = 32 * WC * 2;     // epilogue: 32 rows of a wave on their way out
+constexpr int SMEM_B = RING_B + NW * OUT_B;
+static_assert(SMEM_B <= 160 * 1024 && NW / 2 * T * 8 <= NW * OUT_B, "the layout fits a compute unit, and a tile's statistics the way out");
 enum { STATS = 0, GRAD = 1, DX = 2, DW = 3 };
 
 __device__ __forceinline__ int perm_of(int r) { return (r & 7) ^ ((r >> 3) & 1); }
@@ -62,17 +62,20 @@ __device__ __forceinline__ void strip_tile(long entry, int n_a, int n_b, int* ta
   *tb = rest / w;
 }
 inline long strip_grid(long tiles) { return (tiles + 7) / 8 * 8; }
-// The tile (and, DX, the part of the contraction) of workgroup blockIdx.x; false: none.  The grid is made for all tokens, the tiles
-// are those of the listed ones.
-template <int MODE> __device__ __forceinline__ bool take_tile(int n_rt, int n_ct, int parts, int* rt, int* ct, int* part) {
+// Entries `entry`, `entry` + `step`, .. < `end` of a list of `total` are this workgroup's: every XCD has a run of the list, and its
+// workgroups take the next ones of it in turn.  The grid (a multiple of 8) may be made for more entries, or for fewer.
+struct Turns { long entry, end, step; };
+__device__ __forceinline__ Turns turns_of(long total) {
+  const long x = blockIdx.x % 8;
+  return {total * x / 8 + blockIdx.x / 8, total * (x + 1) / 8, (long)(gridDim.x / 8)};
+}
+// The tile of an entry, and (DX) the part of its contraction.
+template <int MODE> __device__ __forceinline__ void tile_of(long entry, int n_rt, int n_ct, int* rt, int* ct, int* part) {
   const long tiles = (long)n_rt * n_ct;
-  long entry;
-  if (!xcd_run(blockIdx.x, tiles * parts, &entry)) return false;
   *part = MODE == DX ? (int)(entry / tiles) : 0;
   if (MODE == DX) entry -= *part * tiles;
   if (MODE == STATS || MODE == GRAD) strip_tile(entry, n_ct, n_rt, ct, rt);
   else strip_tile(entry, n_rt, n_ct, rt, ct);
-  return true;
 }
 // Parts that the contraction of dx is cut into, by how many tiles the listed tokens make: as many as make the rounds of workgroups
 // shortest, within the room for their sums.  (The first 16 lanes try one number each; `at`: 16 floats of LDS.)
@@ -88,7 +91,8 @@ __device__ inline int dx_parts(int tiles, int n_cu, int slots, float* at) {
   return best + 1;
 }
 
-// ---- the tokens that have a label, in order: tok[i] and its label (-1: not in the vocabulary), and how many they are ----
+// ---- the tokens that have a label, in order: tok[i], its label (-1: not in the vocabulary) and (backward) its lse log2 e and d_loss (NaN for
+// such a label), and how many they are ----
 __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
   __shared__ int sums[2][16];
   __shared__ float tops[16];
@@ -97,13 +101,14 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
   float top = 0.f;                                   // the largest finite |d_loss|
   for (long base = 0; base < a.n; base += 8192) {
     long lab[8];
-    float d[8];
+    float d[8], lse[8];
     int mine = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const long i = base + 8 * tid + k;
       lab[k] = i < a.n ? a.labels[i] : -1;
-      d[k] = a.d_loss && i < a.n ? fabsf(a.d_loss[i]) : 0.f;
+      d[k] = a.d_loss && i < a.n ? a.d_loss[i] : 0.f;
+      lse[k] = a.d_loss && i < a.n ? a.lse[i] : 0.f;
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) mine += lab[k] >= 0 ? 1 : 0;
@@ -128,8 +133,9 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
       if (lab[k] >= 0) {
         a.tok[at] = (int)i;
         a.lab[at] = lab[k] < a.V ? (int)lab[k] : -1;
+        if (a.d_loss) a.row[at] = make_float2(lse[k] * LOG2E, lab[k] < a.V ? d[k] : __builtin_nanf(""));
         ++at;
-        if (d[k] > top && d[k] < __builtin_inff()) top = d[k];
+        if (fabsf(d[k]) > top && fabsf(d[k]) < __builtin_inff()) top = fabsf(d[k]);
       } else if (a.loss && i < a.n) {
         a.loss[i] = 0.f;
         a.lse_out[i] = 0.f;
@@ -240,6 +246,11 @@ __global__ void __launch_bounds__(256) xent_join_kernel(XentArgs a, int n_parts)
 // MODE DW: rows = vocabulary of the piece, columns = features, contraction over the listed tokens: both as [64 tokens][256].
 // Rows of x go by the list; rows behind the last token read the last one again (their g is 0), rows of w behind the vocabulary its last
 // (their columns of g are 0).
+//
+// A workgroup stays and takes one tile after the other (turns_of).  The first two pairs of the next one go out before the epilogue of a tile,
+// which keeps out of the slots, and is over when they have come.  What the epilogue reads of the rows, and the next tile's list, is
+// loaded ahead and has come before these copies start: a wait of the compiler's for it would wait for them too, which it does not
+// see.  (DX, which reads its sums, starts the next tile behind them; it rarely has one.)
 template <int MODE, int RB>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4, NW / 4)))
 xent_bf16_kernel(XentArgs a) {
@@ -254,78 +265,95 @@ xent_bf16_kernel(XentArgs a) {
   const int n_rt = ((MODE == DW ? cols : M) + TR - 1) / TR;
   const int n_ct = LOGITS ? (cols + T - 1) / T : (E + T - 1) / T;
   const int parts = MODE == DX ? a.head->parts : 1;
-  int rt, ct, part;
-  if (!take_tile<MODE>(n_rt, n_ct, parts, &rt, &ct, &part)) return;
-  const int r0 = rt * TR, c0 = ct * T;               // (of the list / of the piece / of the features)
+  const int nk_all = LOGITS ? E / BK : MODE == DX ? (cols + BK - 1) / BK : (M + BK - 1) / BK;
+  struct Tile { int rt, ct, part, r0, c0, k0, nk; }; // (r0: of the list / of the piece, c0: of the piece / of the features)
+  const auto tile_at = [&](long entry) __attribute__((always_inline)) -> Tile {
+    Tile t;
+    tile_of<MODE>(entry, n_rt, n_ct, &t.rt, &t.ct, &t.part);
+    t.r0 = t.rt * TR;
+    t.c0 = t.ct * T;
+    t.k0 = MODE == DX ? (int)((long)t.part * nk_all / parts) : 0;
+    t.nk = MODE == DX ? (int)((long)(t.part + 1) * nk_all / parts) - t.k0 : nk_all;
+    return t;
+  };
+  Turns turn = turns_of((long)n_rt * n_ct * parts);
+  if (turn.entry >= turn.end) return;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / (NW / 2), wn = wave % (NW / 2);
-  const int nk_all = LOGITS ? E / BK : MODE == DX ? (cols + BK - 1) / BK : (M + BK - 1) / BK;
-  const int k0 = MODE == DX ? (int)((long)part * nk_all / parts) : 0;
-  const int nk = MODE == DX ? (int)((long)(part + 1) * nk_all / parts) - k0 : nk_all;
   const unsigned smem_u = lds_base(smem);
   const unsigned xrow_b = (unsigned)(a.ldx * 2), wrow_b = (unsigned)(E * 2);
   const long g_row_b = a.g_pitch * 2L;
 
-  // ---- copies into [rows][64] tiles: one instruction moves 8 rows x 128 bytes, lane l the chunk (l % 8) ^ perm_of(row) of row l / 8
-  unsigned bo[MODE == DW ? 1 : NB], ao[LOGITS ? NA : 1];
-  if constexpr (LOGITS || MODE == DX) {
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const int r = r0 + 8 * NB * wave + 8 * j + (lane >> 3);
-      const unsigned swz = 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + (lane >> 3)));
-      if (LOGITS) bo[j] = (unsigned)a.tok[min(r, M - 1)] * xrow_b + swz;
-      else bo[j] = (unsigned)((8 * NB * wave + 8 * j + (lane >> 3)) * g_row_b) + swz;
-    }
-  }
-  if constexpr (LOGITS) {
-#pragma unroll
-    for (int j = 0; j < NA; ++j) {
-      const int r = 8 * NA * wave + 8 * j + (lane >> 3);
-      ao[j] = (unsigned)min((long)r, a.V - 1 - a.v0 - c0) * wrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + (lane >> 3)));
-    }
-  }
+  // ---- copies into [rows][64] tiles: one instruction moves 8 rows x 128 bytes, lane l the chunk (l % 8) ^ perm_of(row) of row l / 8;
+  // a wave copies rows 8 NA (NB) wave + 8 j + l / 8
   // ---- copies into [64][256] tiles: one instruction moves 2 rows x 512 bytes, lane l position l % 32 of row l / 32, which holds the
   // chunk (l % 32) ^ 4 (row % 4); a wave copies rows 2 NA wave + 2 j + l / 32.  Features past the last one: the tile's first chunk again.
-  const int lh = lane >> 5, pos = lane & 31;
-  unsigned kr_a[2], kr_b[2];
-#pragma unroll
-  for (int par = 0; par < 2; ++par) {
-    const int c = pos ^ (4 * ((2 * par + lh) & 3));
-    kr_a[par] = LOGITS || c0 + 8 * c >= E ? 0u : 16u * (unsigned)c;
-  }
   // (DW's tile of g: [64][TR], an instruction moves BR rows, lane l position l % (64 / BR) of row l / (64 / BR))
   constexpr int BR = 512 / TR, B_ROWB = TR * 2;
+  const int lh = lane >> 5, pos = lane & 31, l8 = lane >> 3;
+  unsigned bo[MODE == DW ? 1 : NB], ao[LOGITS ? NA : 1], kr_a[2], kr_b[2];
+  if constexpr (MODE == DX) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      bo[j] = (unsigned)((8 * NB * wave + 8 * j + l8) * g_row_b) + 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + l8));
+  }
   if constexpr (MODE == DW) {
     const int row = lane / (64 / BR);
 #pragma unroll
     for (int par = 0; par < 2; ++par)
       kr_b[par] = 16u * (unsigned)((lane % (64 / BR)) ^ (4 * ((BR * par + row) & 3))) + (unsigned)((BR * NB * wave + row) * g_row_b);
   }
-  // Where the next pair to go out starts on either side (its copies go out in order, pair by pair).  DX: the rows of w left behind the
-  // pair's first, and a lane's row.  DW: the byte offsets of the rows of x that a wave copies, lane l that of row 2 NA wave + 2 (l % 8) + l / 32.
-  const char* ap = LOGITS ? (const char*)a.w + (a.v0 + c0) * wrow_b
-                          : MODE == DX ? (const char*)a.w + ((a.v0 + k0 * BK) * E + c0) * 2 : (const char*)a.x + 2L * c0;
-  const char* bp = LOGITS ? (const char*)a.x
-                          : MODE == DX ? (const char*)a.g + r0 * g_row_b + (long)k0 * RK_ROWB : (const char*)a.g + 2L * r0;
   const unsigned a_lane = (unsigned)(2 * NA * wave + lh) * wrow_b;
-  long w_left = a.V - 1 - a.v0 - (long)k0 * BK;
-  unsigned w_last = 0u;
+  // DW: the rows of x that a wave copies of a pair, lane l row 2 NA wave + 2 (l % 8) + l / 32; those of the first two pairs are every tile's
   const auto x_rows = [&](int kt) __attribute__((always_inline)) -> int { return a.tok[min(kt * BK + 2 * NA * wave + 2 * (lane & 7) + lh, M - 1)]; };
-  unsigned xr = 0u;
+  unsigned xr = 0u, xr01[2] = {0u, 0u};              // their byte offsets
+  if (MODE == DW && M > 0) {
+    xr01[0] = (unsigned)x_rows(0) * xrow_b;
+    xr01[1] = (unsigned)x_rows(1) * xrow_b;
+  }
+  // LOGITS: the tokens of a tile that a wave copies
+  int tok[NB];
+  const auto load_tokens = [&](const Tile& t) __attribute__((always_inline)) {
+    if constexpr (LOGITS) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) tok[j] = a.tok[min(t.r0 + 8 * NB * wave + 8 * j + l8, M - 1)];
+    }
+  };
+  // Where the next pair to go out starts on either side (its copies go out in order, pair by pair), and what of w is left behind its first row
+  const char *ap, *bp;
+  long w_left = 0;
+  unsigned w_last = 0u;
+  const auto point_at = [&](const Tile& t) __attribute__((always_inline)) {
+    if constexpr (LOGITS) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) bo[j] = (unsigned)tok[j] * xrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + l8));
+#pragma unroll
+      for (int j = 0; j < NA; ++j)
+        ao[j] = (unsigned)min((long)(8 * NA * wave + 8 * j + l8), a.V - 1 - a.v0 - t.c0) * wrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + l8));
+      ap = (const char*)a.w + (a.v0 + t.c0) * wrow_b;
+      bp = (const char*)a.x;
+    } else {
+#pragma unroll
+      for (int par = 0; par < 2; ++par) {
+        const int c = pos ^ (4 * ((2 * par + lh) & 3));
+        kr_a[par] = t.c0 + 8 * c >= E ? 0u : 16u * (unsigned)c;
+      }
+      ap = MODE == DX ? (const char*)a.w + ((a.v0 + t.k0 * BK) * E + t.c0) * 2 : (const char*)a.x + 2L * t.c0;
+      bp = MODE == DX ? (const char*)a.g + t.r0 * g_row_b + (long)t.k0 * RK_ROWB : (const char*)a.g + 2L * t.r0;
+      w_left = a.V - 1 - a.v0 - (long)t.k0 * BK;
+    }
+  };
   // lane j of every 16 lanes
   const auto lane_of_16 = [&](unsigned x, int j) __attribute__((always_inline)) -> unsigned {
     switch (j) {
       case 0: return row_lane<0>(x);
       case 1: return row_lane<1>(x);
       case 2: return row_lane<2>(x);
-      case 3: return row_lane<3>(x);
-      case 4: return row_lane<4>(x);
-      case 5: return row_lane<5>(x);
-      case 6: return row_lane<6>(x);
-      default: return row_lane<7>(x);
+      default: return row_lane<3>(x);
     }
   };
+  static_assert(NA <= 4, "lane_of_16");
   auto issue_part = [&](int kt, int p) __attribute__((always_inline)) {
     const unsigned st = smem_u + (unsigned)((kt % NSLOT) * SLOT_B);
     if (p < NA) {                                    // A side
@@ -349,20 +377,28 @@ xent_bf16_kernel(XentArgs a) {
       if (j == NB - 1) bp += MODE == DW ? 64 * g_row_b : RK_ROWB;
     }
   };
+  const auto start = [&](const Tile& t) __attribute__((always_inline)) {      // a tile's first two pairs
+    point_at(t);
+#pragma unroll
+    for (int q = 0; q < NSLOT; ++q)
+      if (q < t.nk) {
+        if (MODE == DW) xr = xr01[q];
+#pragma unroll
+        for (int p = 0; p < NPART; ++p) issue_part(q, p);
+      }
+  };
 
   // ---- operands (see lvx_project_bwd.hip): from [rows][64] one 16-byte read; from [64][256] two transposing reads, of rows 8 g ..
   // where the other operand has its eight steps in one chunk (DX), 4 g .. and 8 + 4 g .. where both are such tiles (DW)
   const int j16 = lane & 15, jr = j16 >> 2, tr_col = 32 * ((lane >> 4) & 1) + 8 * (j16 & 3);
   constexpr int KG = MODE == DX ? 8 : 4, KH = MODE == DX ? 4 : 8;
-  int rd[4], ka[CB], kb[4];
+  int rd[4], ka[CB], kb[RB];
 #pragma unroll
   for (int q = 0; q < 4; ++q) rd[q] = l31 * RK_ROWB + 16 * ((2 * q + g) ^ perm_of(l31));
 #pragma unroll
   for (int jj = 0; jj < CB; ++jj) ka[jj] = (KG * g + jr) * KR_ROWB + tr_col + 64 * ((CB * wn + jj) ^ jr);
 #pragma unroll
-  for (int jj = 0; jj < 4; ++jj) {
-    kb[jj] = TILE_B + (KG * g + jr) * B_ROWB + tr_col + 64 * ((RB * wm + jj) ^ jr);
-  }
+  for (int jj = 0; jj < RB; ++jj) kb[jj] = TILE_B + (KG * g + jr) * B_ROWB + tr_col + 64 * ((RB * wm + jj) ^ jr);
   auto tr_op = [&](const char* p, auto pitch) __attribute__((always_inline)) -> bf16x8 {
     const s16x4 lo = lds_read_tr(p), hi = lds_read_tr(p + KH * decltype(pitch)::value);
     typedef __attribute__((ext_vector_type(8))) short s16x8;
@@ -379,10 +415,6 @@ xent_bf16_kernel(XentArgs a) {
   };
 
   f32x16 acc[CB][RB];                                // [column block j][row block i]: lane = row, registers = columns
-#pragma unroll
-  for (int j = 0; j < CB; ++j)
-#pragma unroll
-    for (int i = 0; i < RB; ++i) { acc[j][i] = zero16(); asm volatile("" : "+a"(acc[j][i])); }
   constexpr int NU = CB * RB;
   auto mma16 = [&](const bf16x8 (&bv)[RB], const bf16x8 (&av)[CB], auto&& hook) __attribute__((always_inline)) {
 #pragma unroll
@@ -394,165 +426,195 @@ xent_bf16_kernel(XentArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       }
   };
+  constexpr int EB = NU / NB, EA = NU / NA;          // a copy of one side every so many matrix instructions of a k-step
 
-  if (nk > 0) {
+  Tile cur = tile_at(turn.entry);
+  load_tokens(cur);
+  start(cur);
+  char* const out = smem + RING_B + wave * OUT_B;
+  const float scale = MODE == GRAD || MODE == DW ? a.head->scale : 1.f;
+  for (;;) {
+    turn.entry += turn.step;
+    const bool again = turn.entry < turn.end;
+    const Tile nxt = again ? tile_at(turn.entry) : cur;
 #pragma unroll
-    for (int q = 0; q < NSLOT; ++q)
-      if (q < nk) {
-        if constexpr (MODE == DW) xr = (unsigned)x_rows(q) * xrow_b;
+    for (int j = 0; j < CB; ++j)
 #pragma unroll
-        for (int p = 0; p < NPART; ++p) issue_part(q, p);
-      }
-    if (nk > 1) wait_vmcnt<NPART>();
-    else wait_vmcnt<0>();
-    wg_barrier();
-    bf16x8 ba[RB], aa[CB], bb[RB], ab[CB];             // operands of even / odd k-steps
+      for (int i = 0; i < RB; ++i) { acc[j][i] = zero16(); asm volatile("" : "+a"(acc[j][i])); }
+    // what the epilogue needs of the rows, and the next tile's
+    int lab[LOGITS ? RB : 1];
+    float2 row[MODE == GRAD ? RB : 1];
+    const auto load_rows = [&]() __attribute__((always_inline)) {
+      if constexpr (LOGITS) {
 #pragma unroll
-    for (int i = 0; i < RB; ++i) ba[i] = b_op(smem, 0, i);
-#pragma unroll
-    for (int i = 0; i < CB; ++i) aa[i] = a_op(smem, 0, i);
-    auto fetch = [&](const char* st, int q, int u, bf16x8 (&bv)[RB], bf16x8 (&av)[CB]) __attribute__((always_inline)) {
-      if (u < RB) bv[u] = b_op(st, q, u);
-      else if (u < RB + CB) av[u - RB] = a_op(st, q, u - RB);
-    };
-    constexpr int EB = NU / NB, EA = NU / NA;        // a copy of one side every so many matrix instructions of a k-step
-    auto pair = [&](int P, auto steady, bool send2, bool send1, bool more) __attribute__((always_inline)) {
-      constexpr bool STEADY = decltype(steady)::value;
-      const char* const st = smem + (P % NSLOT) * SLOT_B;
-      const char* const sn = smem + ((P + 1) % NSLOT) * SLOT_B;
-      mma16(ba, aa, [&](int u) __attribute__((always_inline)) {
-        fetch(st, 1, u, bb, ab);
-        if ((STEADY || send2) && u % EB == EB - 1) issue_part(P + 1, NA + u / EB);
-      });
-      int next_rows = 0;
-      if constexpr (MODE == DW) next_rows = x_rows(P + 2);        // (has come when the wait below is over)
-      mma16(bb, ab, [&](int u) __attribute__((always_inline)) { fetch(st, 2, u, ba, aa); });
-      mma16(ba, aa, [&](int u) __attribute__((always_inline)) { fetch(st, 3, u, bb, ab); });
-      if (STEADY || more) {
-        __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) and lgkmcnt(0)
-        wg_barrier();
-      }
-      if constexpr (MODE == DW) xr = (unsigned)next_rows * xrow_b;
-      mma16(bb, ab, [&](int u) __attribute__((always_inline)) {
-        if (STEADY || more) fetch(sn, 0, u, ba, aa);
-        if ((STEADY || send1) && u % EA == EA - 1) issue_part(P + 2, u / EA);
-      });
-    };
-    int P = 0;
-    pair(0, std::false_type{}, false, 2 < nk, 1 < nk);
-    P = 1;
-    for (; P + 2 < nk; ++P) pair(P, std::true_type{}, true, true, true);
-    for (; P < nk; ++P) pair(P, std::false_type{}, P + 1 < nk, false, P + 1 < nk);
-  }
-
-  // ---- epilogue: every wave has left the ring, and the last matrix instructions have retired
-  wg_barrier();
-#pragma unroll
-  for (int j = 0; j < CB; ++j)
-#pragma unroll
-    for (int i = 0; i < RB; i += 2) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[j][i]), "+a"(acc[j][i + 1]));
-  if constexpr (MODE == STATS) {
-    const int cw = c0 + wn * WC, left = (int)min((long)WC, a.V - cw);      // columns of this wave
-    float2* const sums = (float2*)smem;              // [NW / 2][TR]
-#pragma unroll
-    for (int i = 0; i < RB; ++i) {
-      const int rl = wm * 32 * RB + 32 * i + l31, r = r0 + rl;
-      const auto z = [&](int v, int j) __attribute__((always_inline)) -> float { return acc[j][i][v]; };
-      float m2, s;
-      tile_stats<CB>(g, left, z, &m2, &s);
-      if (g == 0) sums[wn * TR + rl] = make_float2(m2, s);
-      const int c = r < M ? a.lab[r] - cw : -1;
-      if (__any(c >= 0 && c < WC)) {
-        const float y = tile_pick<CB>(g, c, z);
-        if (c >= 0 && c < WC && ((c >> 2) & 1) == g) a.zlab[r] = y;
-      }
-    }
-    __syncthreads();
-    if (tid < TR && r0 + tid < M) {                  // one number for all columns of the tile
-      float m = -__builtin_inff(), s = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW / 2; ++w) join_stats(&m, &s, sums[w * TR + tid].x, sums[w * TR + tid].y);
-      a.part[(long)ct * a.Mp + r0 + tid] = make_float2(m, s);
-    }
-  } else if constexpr (MODE == DX) {
-    // in the order of the registers, 16 bytes a lane (xent_dx_kernel reads them so), on top of what the pieces before left
-    float* const out = a.dx_part + (((long)part * n_rt + rt) * n_ct + ct) * (TR * T) + wave * (TR * T / NW) + lane * 4;
-#pragma unroll
-    for (int j = 0; j < CB; ++j) {
-      f32x4 old[RB][4];
-      if (!a.first) {
-#pragma unroll
-        for (int i = 0; i < RB; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) old[i][q] = *(const f32x4*)(out + ((j * RB + i) * 4 + q) * 256);
-      }
-#pragma unroll
-      for (int i = 0; i < RB; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          f32x4 v = {acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
-          if (!a.first) v += old[i][q];
-          *(f32x4*)(out + ((j * RB + i) * 4 + q) * 256) = v;
-        }
-    }
-  } else {
-    // turned around in LDS, rounded to bf16, written in whole segments of a row, 64 CB bytes each
-    char* const tb = smem + wave * (32 * RB * TB_PITCH);
-    const float scale = a.head->scale;
-    const int left = cols - c0 - wn * WC;            // columns of this wave (GRAD)
-#pragma unroll
-    for (int i = 0; i < RB; ++i) {
-      float lse2 = 0.f, d = 0.f;
-      int c = -1;
-      if constexpr (MODE == GRAD) {
-        const int r = r0 + wm * 32 * RB + 32 * i + l31;
-        if (r < M) {
-          const int t = a.tok[r];
-          lse2 = a.lse[t] * LOG2E;
-          d = a.lab[r] < 0 ? __builtin_nanf("") : a.d_loss[t] / scale;
-          c = a.lab[r] - (int)a.v0 - c0 - wn * WC;
+        for (int i = 0; i < RB; ++i) {
+          const int r = min(cur.r0 + wm * 32 * RB + 32 * i + l31, M - 1);
+          lab[i] = a.lab[r];
+          if constexpr (MODE == GRAD) row[i] = a.row[r];
         }
       }
-      const auto put = [&](auto plain) __attribute__((always_inline)) {
-        // plain: no label among the wave's columns and rows, all columns are in the piece, all rows have a factor
-        constexpr bool PLAIN = decltype(plain)::value;
-        const int end = PLAIN ? 0 : opaque(d != 0.f ? left - 4 * g : 0), hot = PLAIN ? 0 : opaque(c - 4 * g);
+      load_tokens(nxt);
+    };
+    if (cur.nk > 0) {
+      const int nk = cur.nk;
+      if (nk > 1) wait_vmcnt<NPART>();               // (what an epilogue has written since stands behind the copies: it is waited for as well)
+      else wait_vmcnt<0>();
+      wg_barrier();
+      bf16x8 ba[RB], aa[CB], bb[RB], ab[CB];         // operands of even / odd k-steps
 #pragma unroll
-        for (int j = 0; j < CB; ++j)
+      for (int i = 0; i < RB; ++i) ba[i] = b_op(smem, 0, i);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {              // registers 4 q .. 4 q + 3: columns 32 j + 8 q + 4 g + (0..3)
-            float y[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              y[k] = acc[j][i][4 * q + k];
-              if constexpr (MODE == GRAD) {
-                const int at = 32 * j + 8 * q + k;
-                y[k] = exp2_fast(fmaf(y[k], LOG2E, -lse2));
-                if (!PLAIN) y[k] -= at == hot ? 1.f : 0.f;
-                y[k] = PLAIN || at < end ? y[k] * d : 0.f;
-              } else {
-                y[k] *= scale;
-              }
-            }
-            *(u32x2*)(tb + (32 * i + l31) * TB_PITCH + (32 * j + 8 * q + 4 * g) * 2) = u32x2{pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3])};
-          }
+      for (int i = 0; i < CB; ++i) aa[i] = a_op(smem, 0, i);
+      auto fetch = [&](const char* st, int q, int u, bf16x8 (&bv)[RB], bf16x8 (&av)[CB]) __attribute__((always_inline)) {
+        if (u < RB) bv[u] = b_op(st, q, u);
+        else if (u < RB + CB) av[u - RB] = a_op(st, q, u - RB);
       };
-      if (MODE == DW || (left >= WC && !__any((c >= 0 && c < WC) || d == 0.f))) put(std::true_type{});
-      else put(std::false_type{});
+      auto pair = [&](int P, auto steady, bool send2, bool send1, bool more) __attribute__((always_inline)) {
+        constexpr bool STEADY = decltype(steady)::value;
+        const char* const st = smem + (P % NSLOT) * SLOT_B;
+        const char* const sn = smem + ((P + 1) % NSLOT) * SLOT_B;
+        mma16(ba, aa, [&](int u) __attribute__((always_inline)) {
+          fetch(st, 1, u, bb, ab);
+          if ((STEADY || send2) && u % EB == EB - 1) issue_part(P + 1, NA + u / EB);
+        });
+        int next_rows = 0;
+        if constexpr (MODE == DW) next_rows = x_rows(P + 2);        // (has come when the wait below is over)
+        mma16(bb, ab, [&](int u) __attribute__((always_inline)) { fetch(st, 2, u, ba, aa); });
+        mma16(ba, aa, [&](int u) __attribute__((always_inline)) { fetch(st, 3, u, bb, ab); });
+        if (STEADY || more) {
+          __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) and lgkmcnt(0)
+          wg_barrier();
+        }
+        if constexpr (MODE == DW) xr = (unsigned)next_rows * xrow_b;
+        mma16(bb, ab, [&](int u) __attribute__((always_inline)) {
+          if (STEADY || more) fetch(sn, 0, u, ba, aa);
+          if ((STEADY || send1) && u % EA == EA - 1) issue_part(P + 2, u / EA);
+        });
+      };
+      load_rows();
+      int P = 0;
+      pair(0, std::false_type{}, false, 2 < nk, 1 < nk);
+      P = 1;
+      for (; P + 2 < nk; ++P) pair(P, std::true_type{}, true, true, true);
+      for (; P < nk; ++P) pair(P, std::false_type{}, P + 1 < nk, false, P + 1 < nk);
     }
-    constexpr int LR = WC / 8, RI = 64 / LR;         // lanes that write a row, rows at a time
-    const int row0 = lane / LR, ch = lane % LR;
-#pragma unroll 4
-    for (int it = 0; it < 32 * RB / RI; ++it) {
-      const int rl = RI * it + row0, r = r0 + wm * 32 * RB + rl;
-      const u32x4 y = *(const u32x4*)(tb + rl * TB_PITCH + ch * 16);
-      const int c = c0 + wn * WC + 8 * ch;
-      if constexpr (MODE == GRAD) {
-        *(u32x4*)((char*)a.g + r * g_row_b + 2L * c) = y;
-      } else {
-        if (r < cols && c < E) *(u32x4*)((uint16_t*)a.dw + (a.v0 + r) * E + c) = y;
+
+    // ---- epilogue: every wave has left the slots, what was loaded ahead has come, and the last matrix instructions have retired
+    __builtin_amdgcn_s_waitcnt(0x0070);                  // vmcnt(0) and lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    wg_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+#pragma unroll
+      for (int i = 0; i < RB; i += 2) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[j][i]), "+a"(acc[j][i + 1]));
+    if (MODE != DX && again) start(nxt);
+    if constexpr (MODE == STATS) {
+      const int cw = cur.c0 + wn * WC, left = (int)min((long)WC, a.V - cw);      // columns of this wave
+      float2* const sums = (float2*)(smem + RING_B);  // [NW / 2][TR]
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        const int rl = wm * 32 * RB + 32 * i + l31, r = cur.r0 + rl;
+        const auto z = [&](int v, int j) __attribute__((always_inline)) -> float { return acc[j][i][v]; };
+        float m2, s;
+        tile_stats<CB>(g, left, z, &m2, &s);
+        if (g == 0) sums[wn * TR + rl] = make_float2(m2, s);
+        const int c = r < M ? lab[i] - cw : -1;
+        if (__any(c >= 0 && c < WC)) {
+          const float y = tile_pick<CB>(g, c, z);
+          if (c >= 0 && c < WC && ((c >> 2) & 1) == g) a.zlab[r] = y;
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0)
+      asm volatile("" ::: "memory");
+      wg_barrier();
+      asm volatile("" ::: "memory");
+      if (tid < TR && cur.r0 + tid < M) {              // one number for all columns of the tile
+        float m = -__builtin_inff(), s = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW / 2; ++w) join_stats(&m, &s, sums[w * TR + tid].x, sums[w * TR + tid].y);
+        a.part[(long)cur.ct * a.Mp + cur.r0 + tid] = make_float2(m, s);
+      }
+    } else if constexpr (MODE == DX) {
+      // in the order of the registers, 16 bytes a lane (xent_dx_kernel reads them so), on top of what the pieces before left
+      float* const to = a.dx_part + (((long)cur.part * n_rt + cur.rt) * n_ct + cur.ct) * (TR * T) + wave * (TR * T / NW) + lane * 4;
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+#pragma unroll
+        for (int i0 = 0; i0 < RB; i0 += 2) {             // (eight old values on their way: more would not fit the registers)
+          f32x4 old[2][4];
+          if (!a.first) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) old[i][q] = *(const f32x4*)(to + ((j * RB + i0 + i) * 4 + q) * 256);
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const f32x16& s = acc[j][i0 + i];
+              f32x4 v = {s[4 * q], s[4 * q + 1], s[4 * q + 2], s[4 * q + 3]};
+              if (!a.first) v += old[i][q];
+              *(f32x4*)(to + ((j * RB + i0 + i) * 4 + q) * 256) = v;
+            }
+        }
+    } else {
+      // 32 rows at a time: turned around in LDS, rounded to bf16, written in whole lines.  (Chunk c of a row lies at c ^ row % 8.)
+      const int left = cols - cur.c0 - wn * WC;        // columns of this wave (GRAD)
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        float lse2 = 0.f, d = 0.f;
+        int c = -1;
+        if constexpr (MODE == GRAD) {
+          if (cur.r0 + wm * 32 * RB + 32 * i + l31 < M) {
+            lse2 = row[i].x;
+            d = row[i].y / scale;
+            c = lab[i] - (int)a.v0 - cur.c0 - wn * WC;
+          }
+        }
+        const auto put = [&](auto plain) __attribute__((always_inline)) {
+          // plain: no label among the wave's columns and rows, all columns are in the piece, all rows have a factor
+          constexpr bool PLAIN = decltype(plain)::value;
+          const int end = PLAIN ? 0 : opaque(d != 0.f ? left - 4 * g : 0), hot = PLAIN ? 0 : opaque(c - 4 * g);
+#pragma unroll
+          for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {              // registers 4 q .. 4 q + 3: columns 32 j + 8 q + 4 g + (0..3)
+              float y[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                y[k] = acc[j][i][4 * q + k];
+                if constexpr (MODE == GRAD) {
+                  const int at = 32 * j + 8 * q + k;
+                  y[k] = exp2_fast(fmaf(y[k], LOG2E, -lse2));
+                  if (!PLAIN) y[k] -= at == hot ? 1.f : 0.f;
+                  y[k] = PLAIN || at < end ? y[k] * d : 0.f;
+                } else {
+                  y[k] *= scale;
+                }
+              }
+              *(u32x2*)(out + l31 * (2 * WC) + ((4 * j + q) ^ (l31 & 7)) * 16 + 8 * g) = u32x2{pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3])};
+            }
+        };
+        if (MODE == DW || (left >= WC && !__any((c >= 0 && c < WC) || d == 0.f))) put(std::true_type{});
+        else put(std::false_type{});
+        // (the buffer is this wave's own: its reads are ordered after its writes, and the next writes after them)
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const int rl = 8 * it + l8, ch = lane & 7, r = cur.r0 + wm * 32 * RB + 32 * i + rl, e = cur.c0 + wn * WC + 8 * ch;
+          const u32x4 y = *(const u32x4*)(out + rl * (2 * WC) + (ch ^ (rl & 7)) * 16);
+          if constexpr (MODE == GRAD) {
+            *(u32x4*)((char*)a.g + r * g_row_b + 2L * e) = y;
+          } else {
+            if (r < cols && e < E) *(u32x4*)((uint16_t*)a.dw + (a.v0 + r) * E + e) = y;
+          }
+        }
       }
     }
+    if (!again) break;
+    if (MODE == DX) start(nxt);
+    cur = nxt;
   }
 }
 
@@ -654,9 +716,8 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       float lse2 = 0.f, d = 0.f;
       int c = -1;
       if (r < M) {
-        const int t = a.tok[r];
-        lse2 = a.lse[t] * LOG2E;
-        d = a.lab[r] < 0 ? __builtin_nanf("") : a.d_loss[t] / scale;
+        lse2 = a.row[r].x;
+        d = a.row[r].y / scale;
         c = a.lab[r] - (int)a.v0 - c0 - cw;
       }
       const int end = d != 0.f ? left - 4 * g : 0, hot = c - 4 * g;
@@ -732,7 +793,9 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   const int n_ct = LOGITS ? (cols + FT - 1) / FT : (E + FT - 1) / FT;
   const int parts = MODE == DX ? a.head->parts : 1;
   int rt, ct, part;
-  if (!take_tile<MODE>(n_rt, n_ct, parts, &rt, &ct, &part)) return;
+  const Turns turn = turns_of((long)n_rt * n_ct * parts);
+  if (turn.entry >= turn.end) return;
+  tile_of<MODE>(turn.entry, n_rt, n_ct, &rt, &ct, &part);
   const int r0 = rt * FT, c0 = ct * FT;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
   const int K = LOGITS ? E : MODE == DX ? cols : M;
@@ -826,9 +889,8 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
       int c = -1;
       if constexpr (MODE == GRAD) {
         if (r < M) {
-          const int t = a.tok[r];
-          lse2 = a.lse[t] * LOG2E;
-          d = a.lab[r] < 0 ? __builtin_nanf("") : a.d_loss[t] / scale;
+          lse2 = a.row[r].x;
+          d = a.row[r].y / scale;
           c = a.lab[r] - (int)a.v0;
         }
       }
@@ -885,7 +947,8 @@ template <int MODE, int RB> hipError_t launch_tiles(const XentArgs& a, long grid
   static SmemOnce once;
   const hipError_t e = ensure_dynamic_lds((const void*)xent_bf16_kernel<MODE, RB>, SMEM_B, &once);
   if (e != hipSuccess) return e;
-  xent_bf16_kernel<MODE, RB><<<(unsigned)grid, 64 * NW, SMEM_B, s>>>(a);
+  const long stay = a.n_cu >= 8 ? a.n_cu / 8 * 8 : 8;
+  xent_bf16_kernel<MODE, RB><<<(unsigned)(grid < stay ? grid : stay), 64 * NW, SMEM_B, s>>>(a);
   return hipGetLastError();
 }
 // (GRAD: 64 tokens whatever their number: the contraction of dw runs over g's rows 64 at a time)

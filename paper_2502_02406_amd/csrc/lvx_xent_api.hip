@@ -28,7 +28,7 @@ Plan plan_of(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
   p.tok = ALIGN;
   p.lab = p.tok + align_up(n * 4);
   p.zlab = p.lab + align_up(n * 4);
-  p.part = p.dx = p.zlab + align_up(n * 4);
+  p.part = p.dx = p.zlab + align_up(n * 8);              // (zlab: the forward pass's label logits or the backward pass's rows)
   p.fwd = p.part + (size_t)xent_stat_parts(V, f32) * p.Mp * sizeof(float2);
   p.g = p.dx + align_up(xent_dx_bytes(n, E, device_cu_count(), f32));
   p.row = (size_t)p.Mp * (f32 ? 4 : 2);                // bytes of a column of the logits' gradient
@@ -62,7 +62,7 @@ lvx_status xent_args(const lvx_xent* p, lvx_dtype dtype, const void* x, const vo
   a->n = p->n; a->ldx = p->x_ss; a->V = p->V; a->E = p->E; a->n_cu = device_cu_count();
   const auto at = [&](size_t o) -> char* { return (char*)workspace + o; };
   a->head = (XentHead*)workspace;
-  a->tok = (int*)at(plan->tok); a->lab = (int*)at(plan->lab); a->zlab = (float*)at(plan->zlab);
+  a->tok = (int*)at(plan->tok); a->lab = (int*)at(plan->lab); a->zlab = (float*)at(plan->zlab); a->row = (float2*)at(plan->zlab);
   a->part = (float2*)at(plan->part); a->dx_part = (float*)at(plan->dx); a->g = at(plan->g);
   a->Mp = plan->Mp;
   a->slots = (int)plan->slots;
