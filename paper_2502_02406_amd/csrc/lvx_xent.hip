@@ -78,17 +78,16 @@ template <int MODE> __device__ __forceinline__ void tile_of(long entry, int n_rt
   else strip_tile(entry, n_rt, n_ct, rt, ct);
 }
 // Parts that the contraction of dx is cut into, by how many tiles the listed tokens make: as many as make the rounds of workgroups
-// shortest, within the room for their sums.  (The first 16 lanes try one number each; `at`: 16 floats of LDS.)
-__device__ inline int dx_parts(int tiles, int n_cu, int slots, float* at) {
-  if (threadIdx.x < 16) {
-    const int p = threadIdx.x + 1;
-    at[threadIdx.x] = p * tiles <= slots ? (float)((tiles * p + n_cu - 1) / n_cu) / (float)p : 1e30f;
-  }
-  __syncthreads();
-  int best = 0;
-  for (int p = 1; p < 16; ++p)
-    if (at[p] < 0.95f * at[best]) best = p;
-  return best + 1;
+// shortest, within the room for their sums, and four tile pairs each (300 tokens x 256 features against 50000, two tiles: 16 parts 61 us, 64
+// 30).  A number a lane.
+constexpr int MOST_PARTS = 64;
+__device__ inline int dx_parts(int tiles, int pairs, int n_cu, int slots) {
+  const int p = (threadIdx.x & 63) + 1;
+  const float t = p * tiles <= slots && (4 * p <= pairs || p == 1) ? (float)((tiles * p + n_cu - 1) / n_cu) / (float)p : 1e30f;
+  float least = t;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) least = fminf(least, __shfl_xor(least, o));
+  return __ffsll(__ballot(t <= 1.05f * least));      // (the fewest that come within a twentieth)
 }
 
 // ---- the tokens that have a label, in order: tok[i], its label (-1: not in the vocabulary) and (backward) its lse log2 e and d_loss (NaN for
@@ -146,8 +145,7 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
   for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
   if (lane == 0) tops[wave] = top;
   __syncthreads();
-  __shared__ float tries[16];
-  const int parts = dx_parts((total + a.tile_rows - 1) / a.tile_rows * ((a.E + a.tile - 1) / a.tile), a.n_cu, a.slots, tries);
+  const int parts = dx_parts((total + a.tile_rows - 1) / a.tile_rows * ((a.E + a.tile - 1) / a.tile), (int)(a.piece / BK), a.n_cu, a.slots);
   if (tid != 0) return;
   for (int w = 0; w < 16; ++w) top = fmaxf(top, tops[w]);
   a.head->count = total;
@@ -754,7 +752,15 @@ __global__ void __launch_bounds__(256) xent_dx_bf16_kernel(XentArgs a, unsigned 
     const int wave = rl / (tr / 2) * (NW / 2) + cl / WC, i = rl % (tr / 2) / 32, j = cl % WC / 32, q = cl % 32 / 8;
     const float* from = a.dx_part + tile * (tr * T) + wave * (tr * T / NW) + ((j * (tr / 64) + i) * 4 + q) * 256 + (rl % 32 + 32 * (cl / 4 % 2)) * 4;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < a.head->parts; ++p) s += *(const f32x4*)(from + p * step);
+    const int parts = a.head->parts;
+    for (int p0 = 0; p0 < parts; p0 += 8) {              // (eight on their way at once)
+      f32x4 v[8];
+#pragma unroll
+      for (int p = 0; p < 8; ++p) v[p] = *(const f32x4*)(from + min(p0 + p, parts - 1) * step);
+#pragma unroll
+      for (int p = 0; p < 8; ++p)
+        if (p0 + p < parts) s += v[p];
+    }
     s *= a.head->scale;
     *(u32x2*)((uint16_t*)a.dx + a.tok[r] * a.ldx + c) = u32x2{pack2_bf16(s[0], s[1]), pack2_bf16(s[2], s[3])};
     return;
@@ -933,7 +939,13 @@ __global__ void __launch_bounds__(256) xent_dx_f32_kernel(XentArgs a, unsigned r
     for (int e = threadIdx.x; e < E; e += 256) {
       const float* const from = a.dx_part + ((long)(r / t) * n_ct + e / t) * (t * t) + (r % t) * t + e % t;
       float s = 0.f;
-      for (int p = 0; p < parts; ++p) s += from[p * step];
+      for (int p0 = 0; p0 < parts; p0 += 8) {
+        float v[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) v[p] = from[min(p0 + p, parts - 1) * step];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) s += p0 + p < parts ? v[p] : 0.f;
+      }
       ((float*)a.dx)[a.tok[r] * a.ldx + e] = s * a.head->scale;
     }
     return;
@@ -962,10 +974,17 @@ template <int MODE, int RB, int NS> hipError_t launch_few(const XentArgs& a, lon
   return hipGetLastError();
 }
 long up(long n, long by) { return (n + by - 1) / by; }
-// dw: tiles of 128 rows where those of 256 leave a quarter of the compute units without one (2000 tokens x 512 against 8000: 43 -> 31 us)
-hipError_t launch_dw(const XentArgs& a, long cols, hipStream_t s) {
-  if (up(cols, T) * up(a.E, T) * 4 <= 3L * a.n_cu) return launch_tiles<DW, 2>(a, strip_grid(up(cols, 128) * up(a.E, T)), s);
-  return launch_tiles<DW, 4>(a, strip_grid(up(cols, T) * up(a.E, T)), s);
+// Whether tiles of 128 rows are the better ones for a product of `rows` x `cols` with `pairs` tile pairs: by the rounds of workgroups, a
+// tile's pairs at 1.55 us (128 rows: 0.85) and what a tile costs beside them, 6 us (3.5).  Statistics and gradient of 300 tokens x 256 against
+// 50000 26.8 -> 20.8 and 31.5 -> 24.7, x 1024 66 -> 61 and 62 -> 54; dw of 2000 x 512 against 8000 43 -> 31; where the rule keeps 256
+// rows, 2048 x 1024 against 8192 34.5 -> 39.4 and 37 -> 40, 1000 x 512 against 30000 40 -> 44, 44 -> 46 and (dw) 34 -> 38.
+bool low_tiles(long rows, long cols, long pairs, int n_cu) {
+  const long ct = up(cols, T);
+  return rows <= 128 || up(up(rows, 128) * ct, n_cu) * (0.85 * pairs + 3.5) < up(up(rows, T) * ct, n_cu) * (1.55 * pairs + 6.0);
+}
+template <int MODE> hipError_t product(const XentArgs& a, long rows, long cols, long pairs, hipStream_t s) {
+  if (low_tiles(rows, cols, pairs, a.n_cu)) return launch_tiles<MODE, 2>(a, strip_grid(up(rows, 128) * up(cols, T)), s);
+  return launch_tiles<MODE, 4>(a, strip_grid(up(rows, T) * up(cols, T)), s);
 }
 // float32: the edge of the tiles of a product.  64 where 128 makes less than two for every compute unit: 300 tokens x 512 features against 5003,
 // the four products 246 -> 112 us
@@ -985,7 +1004,7 @@ template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t
       if (a.n <= 32) return wgs <= a.n_cu ? launch_few<MODE, 1, 6>(a, wgs, s) : launch_few<MODE, 1, 3>(a, wgs, s);
     return wgs <= a.n_cu ? launch_few<MODE, 2, 6>(a, wgs, s) : launch_few<MODE, 2, 3>(a, wgs, s);
   }
-  return a.n <= 128 ? launch_tiles<MODE, 2>(a, strip_grid(up(cols, T)), s) : launch_tiles<MODE, 4>(a, strip_grid(up(a.n, T) * up(cols, T)), s);
+  return product<MODE>(a, a.n, cols, a.E / BK, s);
 }
 // dx: columns and rows of a tile
 int dx_edge(long n, int E, int n_cu, int is_f32) { return is_f32 ? f32_edge(n, E, n_cu) : T; }
@@ -994,10 +1013,10 @@ int dx_rows(long n, int E, int n_cu, int is_f32) { return is_f32 ? f32_edge(n, E
 
 bool xent_bf16_supported(int E) { return E % BK == 0; }
 int xent_stat_parts(long V, int is_f32) { return (int)(2 * up(V, is_f32 ? 64 : T)); }
-// Bytes of the tiles of dx's sums, and how many these are: one for every tile at least, two for every compute unit where 16 parts of a tile
+// Bytes of the tiles of dx's sums, and how many these are: one for every tile at least, two for every compute unit where 64 parts of a tile
 // make so many; no more with fewer tokens or features.
 long xent_dx_slots(long n, int E, int n_cu, int is_f32) {
-  const long tiles = up(n, dx_rows(n, E, n_cu, is_f32)) * up(E, dx_edge(n, E, n_cu, is_f32)), some = 16 * tiles < 2L * n_cu ? 16 * tiles : 2L * n_cu;
+  const long tiles = up(n, dx_rows(n, E, n_cu, is_f32)) * up(E, dx_edge(n, E, n_cu, is_f32)), some = MOST_PARTS * tiles < 2L * n_cu ? MOST_PARTS * tiles : 2L * n_cu;
   return tiles > some ? tiles : some;
 }
 size_t xent_dx_bytes(long n, int E, int n_cu, int is_f32) {
@@ -1006,6 +1025,7 @@ size_t xent_dx_bytes(long n, int E, int n_cu, int is_f32) {
 
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
   a.tile = a.tile_rows = T;
+  a.piece = a.V;
   xent_list_kernel<<<1, 1024, 0, s>>>(a);
   a.v0 = 0;
   a.v1 = a.V;
@@ -1027,7 +1047,7 @@ hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
     const long cols = a.v1 - a.v0;
     e = logits<GRAD>(a, is_f32, s);
     if (e == hipSuccess && a.dw)
-      e = is_f32 ? f32_product<DW>(a, cols, a.E, f32_edge(cols, a.E, a.n_cu), s) : launch_dw(a, cols, s);
+      e = is_f32 ? f32_product<DW>(a, cols, a.E, f32_edge(cols, a.E, a.n_cu), s) : product<DW>(a, cols, a.E, up(a.n, BK), s);
     if (e == hipSuccess && a.dx) {
       e = is_f32 ? f32_product<DX>(a, a.n, a.E, a.tile, s)
                  : a.tile_rows == 128 ? launch_tiles<DX, 2>(a, strip_grid(a.slots), s) : launch_tiles<DX, 4>(a, strip_grid(a.slots), s);
