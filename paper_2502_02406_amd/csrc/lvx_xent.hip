@@ -616,9 +616,9 @@ xent_bf16_kernel(XentArgs a) {
   }
 }
 
-// Logits of at most 64 tokens: bound by reading w.  A workgroup takes 128 entries of the vocabulary, a wave 32 of them against 32 RB tokens, and
+// Logits of few tokens (few_takes): bound by reading w.  A workgroup takes 128 entries of the vocabulary, a wave 32 of them against 32 RB tokens, and
 // NS slots of 64 features are on their way (of w alone, 16 KB each; two-slot tiles of 256 entries kept half of the compute units
-// waiting, 16 tokens x 4096 against 32768: 85 -> 66 us).  Six slots where the workgroups have a compute unit each, three where two share
+// waiting, 16 tokens x 4096 against 32768: 85 -> 66 us).  Six slots (64 tokens) where the workgroups have a compute unit each, three where two share
 // one.  Behind the last features the copies go on with these again, so that every step waits for the same number.
 template <int MODE, int RB, int NS>
 __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
@@ -963,8 +963,10 @@ template <int MODE, int RB> hipError_t launch_tiles(const XentArgs& a, long grid
   xent_bf16_kernel<MODE, RB><<<(unsigned)(grid < stay ? grid : stay), 64 * NW, SMEM_B, s>>>(a);
   return hipGetLastError();
 }
-// (GRAD: 64 tokens whatever their number: the contraction of dw runs over g's rows 64 at a time)
-constexpr int FEW = 64;
+// Up to 128 tokens where their workgroups have a compute unit each (128 x 4096 against 32768: statistics 96 -> 74 us, gradient 83 -> 62; where they take
+// turns, 100 x 1024 against 131072, 67 -> 75 and 57 -> 74), up to 64 always.  (GRAD: 64 or 128 tokens whatever their number: the contraction of
+// dw runs over g's rows 64 at a time.)
+bool few_takes(long n, long cols, int n_cu) { return n <= 64 || (n <= 128 && (cols + 127) / 128 <= n_cu); }
 template <int MODE, int RB, int NS> hipError_t launch_few(const XentArgs& a, long wgs, hipStream_t s) {
   constexpr int bytes = NS * (128 + 32 * RB) * RK_ROWB;
   static SmemOnce once;
@@ -998,10 +1000,11 @@ template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long co
 template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t s) {
   const long cols = a.v1 - a.v0;
   if (is_f32) return f32_product<MODE>(a, a.n, cols, f32_edge(a.n, cols, a.n_cu), s);
-  if (a.n <= FEW) {
+  if (few_takes(a.n, cols, a.n_cu)) {
     const long wgs = up(cols, 128);
     if constexpr (MODE == STATS)
       if (a.n <= 32) return wgs <= a.n_cu ? launch_few<MODE, 1, 6>(a, wgs, s) : launch_few<MODE, 1, 3>(a, wgs, s);
+    if (a.n > 64) return launch_few<MODE, 4, 4>(a, wgs, s);
     return wgs <= a.n_cu ? launch_few<MODE, 2, 6>(a, wgs, s) : launch_few<MODE, 2, 3>(a, wgs, s);
   }
   return product<MODE>(a, a.n, cols, a.E / BK, s);
@@ -1032,7 +1035,7 @@ hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
   const hipError_t e = logits<STATS>(a, is_f32, s);
   if (e != hipSuccess) return e;
   const long wgs = up(a.n, 8);
-  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : a.n <= FEW ? (int)up(a.V, 128) : (int)up(a.V, T));
+  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : few_takes(a.n, a.V, a.n_cu) ? (int)up(a.V, 128) : (int)up(a.V, T));
   return hipGetLastError();
 }
 
