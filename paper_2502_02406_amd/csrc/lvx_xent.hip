@@ -645,8 +645,12 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
     bo[j] = (unsigned)a.tok[min(r, M - 1)] * xrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(r));
   }
   const char* const wg = (const char*)a.w + (a.v0 + c0) * wrow_b;
+  // (every workgroup begins at another feature: at the same one, the lines that all of them ask for lie 2 E bytes apart, in few of the memory's
+  // channels; 16 x 4096 against 32768 69 -> 53 us, against 131072 217 -> 186, 5.8 TB/s)
+  const int turn = (int)(blockIdx.x * 7u % (unsigned)nk);
   const auto issue = [&](int kt, int slot) __attribute__((always_inline)) {
-    const long k_b = (long)min(kt, nk - 1) * RK_ROWB;
+    const int k = min(kt, nk - 1) + turn;
+    const long k_b = (long)(k < nk ? k : k - nk) * RK_ROWB;
     const unsigned st = smem_u + (unsigned)(slot * S_B);
 #pragma unroll
     for (int j = 0; j < 4; ++j) dma16u(wg + k_b, ao[j], st + (unsigned)((32 * wave + 8 * j) * RK_ROWB));
