@@ -222,7 +222,7 @@ struct XentArgs {
   float* zlab;          // forward, [n]: the label's logit
   float2* row;          // backward, [n]: lse log2 e, and d_loss (NaN where the label is not in the vocabulary)
   void* g;              // backward, [Mp][g_pitch] of x's type: the logits' gradient of a piece of the vocabulary
-  long g_pitch, piece;  // columns of a piece; a row of g has as many, rounded up to 256
+  long g_pitch, piece;  // columns of a piece (a multiple of 256), and from a row of g to the next
   float* dx_part;       // backward, [slots] tiles of sums of dx
   int slots;
   // set by the launches

@@ -111,7 +111,7 @@ def test_small_workspace_and_parts_left_out(dtype):
     up = lambda v: (v + 255) // 256 * 256
     edge = 64 if dtype == "f32" else 256
     tiles = -(-n // edge) * -(-E // edge)
-    least = 256 + 2 * up(4 * n) + up(8 * n) + max(tiles, min(64 * tiles, 2 * torch.cuda.get_device_properties(0).multi_processor_count)) * edge * edge * 4 + 256 * Mp * el
+    least = 256 + 2 * up(4 * n) + up(8 * n) + max(tiles, min(64 * tiles, 2 * torch.cuda.get_device_properties(0).multi_processor_count)) * edge * edge * 4 + 320 * Mp * el
     check(run(*args, ws_bytes=least), ref, tol, "pieces of 256")
     with pytest.raises(B.LvxError):
         run(*args, ws_bytes=least - 256)

@@ -59,7 +59,7 @@ def test_workspace(lib):  # noqa: F811
         edge = 256 if dt == B.LVX_BF16 else 64 if -(-n // 128) * -(-E // 128) < 512 else 128
         rows = 128 if dt == B.LVX_BF16 and n <= 128 else edge
         tiles = -(-n // rows) * -(-E // edge)
-        need = 256 + 2 * up(4 * n) + up(8 * n) + max(tiles, min(64 * tiles, 512)) * rows * edge * 4 + 256 * Mp * el   # lists, sums of dx, 256 columns
+        need = 256 + 2 * up(4 * n) + up(8 * n) + max(tiles, min(64 * tiles, 512)) * rows * edge * 4 + 320 * Mp * el   # lists, sums of dx, 256 columns and 64 between
         assert bwd(lib, p, dtype=dt, n=need - 1) == -6
         return need
     for dt in (B.LVX_BF16, B.LVX_F32):
