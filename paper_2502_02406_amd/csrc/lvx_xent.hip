@@ -23,6 +23,7 @@
 #include "lvx_mfma.h"
 #include "lvx_kv_ring.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace lvx {
@@ -66,8 +67,8 @@ inline long strip_grid(long tiles) { return (tiles + 7) / 8 * 8; }
 // workgroups take the next ones of it in turn.  The grid (a multiple of 8) may be made for more entries, or for fewer.
 struct Turns { long entry, end, step; };
 __device__ __forceinline__ Turns turns_of(long total) {
-  const long x = blockIdx.x % 8;
-  return {total * x / 8 + blockIdx.x / 8, total * (x + 1) / 8, (long)(gridDim.x / 8)};
+  const long x = blockIdx.x % 8, wg = (long)blockIdx.y * gridDim.x + blockIdx.x;
+  return {total * x / 8 + wg / 8, total * (x + 1) / 8, (long)(gridDim.x / 8) * gridDim.y};
 }
 // The tile of an entry, and (DX) the part of its contraction.
 template <int MODE> __device__ __forceinline__ void tile_of(long entry, int n_rt, int n_ct, int* rt, int* ct, int* part) {
@@ -802,9 +803,9 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   const int n_rt = MODE == DW ? (cols + FT - 1) / FT : (M + FT - 1) / FT;
   const int n_ct = LOGITS ? (cols + FT - 1) / FT : (E + FT - 1) / FT;
   const int parts = MODE == DX ? a.head->parts : 1;
-  int rt, ct, part;
-  const Turns turn = turns_of((long)n_rt * n_ct * parts);
+  const Turns turn = turns_of((long)n_rt * n_ct * parts);      // (one tile a workgroup: a loop over them costs dw a fifth, in registers)
   if (turn.entry >= turn.end) return;
+  int rt, ct, part;
   tile_of<MODE>(turn.entry, n_rt, n_ct, &rt, &ct, &part);
   const int r0 = rt * FT, c0 = ct * FT;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
@@ -936,21 +937,21 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
 __global__ void __launch_bounds__(256) xent_dx_f32_kernel(XentArgs a, unsigned rows) {
   const int M = a.head->count, E = a.E;
   if (blockIdx.x < rows) {
-    const int r = blockIdx.x;
-    if (r >= M) return;
     const int t = a.tile, n_ct = (E + t - 1) / t, parts = a.head->parts;
     const long step = (long)((M + t - 1) / t) * n_ct * (t * t);
-    for (int e = threadIdx.x; e < E; e += 256) {
-      const float* const from = a.dx_part + ((long)(r / t) * n_ct + e / t) * (t * t) + (r % t) * t + e % t;
-      float s = 0.f;
-      for (int p0 = 0; p0 < parts; p0 += 8) {
-        float v[8];
+    for (int r = blockIdx.x; r < M; r += rows) {
+      for (int e = threadIdx.x; e < E; e += 256) {
+        const float* const from = a.dx_part + ((long)(r / t) * n_ct + e / t) * (t * t) + (r % t) * t + e % t;
+        float s = 0.f;
+        for (int p0 = 0; p0 < parts; p0 += 8) {
+          float v[8];
 #pragma unroll
-        for (int p = 0; p < 8; ++p) v[p] = from[min(p0 + p, parts - 1) * step];
+          for (int p = 0; p < 8; ++p) v[p] = from[min(p0 + p, parts - 1) * step];
 #pragma unroll
-        for (int p = 0; p < 8; ++p) s += p0 + p < parts ? v[p] : 0.f;
+          for (int p = 0; p < 8; ++p) s += p0 + p < parts ? v[p] : 0.f;
+        }
+        ((float*)a.dx)[a.tok[r] * a.ldx + e] = s * a.head->scale;
       }
-      ((float*)a.dx)[a.tok[r] * a.ldx + e] = s * a.head->scale;
     }
     return;
   }
@@ -995,8 +996,10 @@ template <int MODE> hipError_t product(const XentArgs& a, long rows, long cols, 
 // float32: the edge of the tiles of a product.  64 where 128 makes less than two for every compute unit: 300 tokens x 512 features against 5003,
 // the four products 246 -> 112 us
 int f32_edge(long rows, long cols, int n_cu) { return up(rows, 128) * up(cols, 128) < 2L * n_cu ? 64 : 128; }
+constexpr long MOST_WGS = 1 << 14;     // along one side of a launch, whose threads may not pass 2^32
 template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long cols, int edge, hipStream_t s) {
-  const unsigned grid = (unsigned)strip_grid(MODE == DX ? a.slots : up(rows, edge) * up(cols, edge));
+  const long wgs = strip_grid(MODE == DX ? (long)a.slots : up(rows, edge) * up(cols, edge));
+  const dim3 grid((unsigned)std::min(wgs, MOST_WGS), (unsigned)up(wgs, MOST_WGS));
   if (edge == 64) xent_f32_kernel<MODE, 64><<<grid, 256, 0, s>>>(a);
   else xent_f32_kernel<MODE, 128><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
@@ -1064,7 +1067,8 @@ hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
   if (e != hipSuccess || !a.dx) return e;
   const long zero = up(a.n, 4) < 1024 ? up(a.n, 4) : 1024;
   if (is_f32) {
-    xent_dx_f32_kernel<<<(unsigned)(a.n + zero), 256, 0, s>>>(a, (unsigned)a.n);
+    const unsigned rows = (unsigned)std::min(a.n, MOST_WGS);
+    xent_dx_f32_kernel<<<rows + (unsigned)zero, 256, 0, s>>>(a, rows);
   } else {
     const unsigned tiles = (unsigned)(up(a.n, 32) * up(a.E, 32));
     xent_dx_bf16_kernel<<<tiles + (unsigned)zero, 256, 0, s>>>(a, tiles);

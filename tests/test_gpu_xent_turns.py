@@ -1,0 +1,48 @@
+"""The cross entropy where workgroups take several tiles one after the other, in each of its products, against float64.  Inputs, tolerances and
+their derivation as in test_gpu_xent.py; the long float32 case takes its reference on the GPU, in float64 as well."""
+import pytest
+import torch
+
+from paper_2502_02406_amd import binding as B
+from test_gpu_xent import check, inputs, reference, run
+
+pytestmark = pytest.mark.gpu
+
+
+# more than 256 tiles of 256 x 256 or 128 x 256 on a chip of 256 compute units: of logits and of dw; of dx; of both with few features
+@pytest.mark.parametrize("n,E,V", [(1030, 1280, 16500), (6300, 3840, 300), (2100, 64, 9001)])
+def test_bf16_tiles_in_turn(n, E, V):
+    print(f"[xent] bf16 {n}x{E} V={V}", flush=True)
+    args = inputs(n, E, V, "bf16", n + V)
+    got = run(*args)
+    ref, tol = reference(*args, "bf16")
+    check(got, ref, tol, f"{n}x{E}x{V}")
+    assert all(torch.equal(a, b) for a, b in zip(got, run(*args))), "not repeatable"
+
+
+def test_f32_tiles_in_turn():
+    """More tiles and rows than a launch has workgroups.  A logit: 8 products; errors as in test_gpu_xent.py with E = 8 and the largest values of
+    the case in place of every token's."""
+    n, E, V = 70000, 8, 4100
+    x, w, labels, d = inputs(n, E, V, "f32", 5)
+    loss, lse, dx, dw = run(x, w, labels, d)
+    on = labels >= 0
+    u = 2.0 ** -24
+    w64, dw64, tol_w = w.double(), torch.zeros(V, E, dtype=torch.float64, device="cuda"), torch.zeros(V, E, dtype=torch.float64, device="cuda")
+    assert not loss[~on].any() and not lse[~on].any() and not dx[~on].any()
+    for part in on.nonzero()[:, 0].split(10000):
+        x64, d64, lab = x[part].double(), d[part].double(), labels[part, None]
+        z = x64 @ w64.T
+        ref = torch.logsumexp(z, 1)
+        zl = z.gather(1, lab)[:, 0]
+        p = torch.exp(z - ref[:, None])
+        g = p.scatter_add(1, lab, torch.full_like(zl, -1.0)[:, None]) * d64[:, None]
+        ez = (E / 2 + 16) * u * (x64.abs() @ w64.abs().T)
+        e_lse = ez.max(1).values + (V / 4096 + 200 + 4 * (ref.abs() + z.abs().max(1).values)) * u
+        assert ((lse[part] - ref).abs() <= 1.02 * e_lse).all()
+        assert ((loss[part] - (ref - zl)).abs() <= 1.02 * (e_lse + ez.gather(1, lab)[:, 0] + 2 * u * (ref.abs() + zl.abs()))).all()
+        eg = p * d64.abs()[:, None] * (ez + e_lse[:, None] + (8 + 4 * (ref.abs()[:, None] + z.abs())) * u) + 2 * u * g.abs()
+        assert ((dx[part] - g @ w64).abs() <= 1.02 * (eg @ w64.abs() + (V / 2 + 64) * u * (g.abs() @ w64.abs()))).all()
+        dw64 += g.T @ x64
+        tol_w += eg.T @ x64.abs() + (n / 2 + 64) * u * (g.abs().T @ x64.abs())
+    assert ((dw - dw64).abs() <= 1.02 * tol_w).all()
