@@ -1016,21 +1016,26 @@ template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t
   }
   return product<MODE>(a, a.n, cols, a.E / BK, s);
 }
-// dx: columns and rows of a tile
-int dx_edge(long n, int E, int n_cu, int is_f32) { return is_f32 ? f32_edge(n, E, n_cu) : T; }
-int dx_rows(long n, int E, int n_cu, int is_f32) { return is_f32 ? f32_edge(n, E, n_cu) : n <= 128 ? 128 : T; }
+// dx: columns and rows of a tile.  float32: 128 where the parts make one for every compute unit (3000 tokens x 512 features against 40000 1610 -> 1210
+// us, 1000 x 512 against 10000 148 -> 118, 2000 x 200 against 3000 53 -> 43; where they do not, 100 x 256 against 30000 32 -> 47, 300 x 1024 against
+// 1000 13.6 -> 26).
+int dx_f32_edge(long n, int E, long V, int n_cu) {
+  return up(n, 128) * up(E, 128) * std::max(1L, std::min((long)MOST_PARTS, V / 256)) < n_cu ? 64 : 128;
+}
+int dx_edge(long n, int E, long V, int n_cu, int is_f32) { return is_f32 ? dx_f32_edge(n, E, V, n_cu) : T; }
+int dx_rows(long n, int E, long V, int n_cu, int is_f32) { return is_f32 ? dx_f32_edge(n, E, V, n_cu) : n <= 128 ? 128 : T; }
 }  // namespace
 
 bool xent_bf16_supported(int E) { return E % BK == 0; }
 int xent_stat_parts(long V, int is_f32) { return (int)(2 * up(V, is_f32 ? 64 : T)); }
 // Bytes of the tiles of dx's sums, and how many these are: one for every tile at least, two for every compute unit where 64 parts of a tile
-// make so many; no more with fewer tokens or features.
-long xent_dx_slots(long n, int E, int n_cu, int is_f32) {
-  const long tiles = up(n, dx_rows(n, E, n_cu, is_f32)) * up(E, dx_edge(n, E, n_cu, is_f32)), some = MOST_PARTS * tiles < 2L * n_cu ? MOST_PARTS * tiles : 2L * n_cu;
+// make so many; no more with fewer tokens or features or a smaller vocabulary.
+long xent_dx_slots(long n, int E, long V, int n_cu, int is_f32) {
+  const long tiles = up(n, dx_rows(n, E, V, n_cu, is_f32)) * up(E, dx_edge(n, E, V, n_cu, is_f32)), some = MOST_PARTS * tiles < 2L * n_cu ? MOST_PARTS * tiles : 2L * n_cu;
   return tiles > some ? tiles : some;
 }
-size_t xent_dx_bytes(long n, int E, int n_cu, int is_f32) {
-  return sizeof(float) * dx_rows(n, E, n_cu, is_f32) * dx_edge(n, E, n_cu, is_f32) * xent_dx_slots(n, E, n_cu, is_f32);
+size_t xent_dx_bytes(long n, int E, long V, int n_cu, int is_f32) {
+  return sizeof(float) * dx_rows(n, E, V, n_cu, is_f32) * dx_edge(n, E, V, n_cu, is_f32) * xent_dx_slots(n, E, V, n_cu, is_f32);
 }
 
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
@@ -1047,8 +1052,8 @@ hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
 }
 
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
-  a.tile = dx_edge(a.n, a.E, a.n_cu, is_f32);
-  a.tile_rows = dx_rows(a.n, a.E, a.n_cu, is_f32);
+  a.tile = dx_edge(a.n, a.E, a.V, a.n_cu, is_f32);
+  a.tile_rows = dx_rows(a.n, a.E, a.V, a.n_cu, is_f32);
   xent_list_kernel<<<1, 1024, 0, s>>>(a);
   a.first = 1;
   hipError_t e = hipGetLastError();

@@ -23,14 +23,14 @@ struct Plan { size_t tok, lab, zlab, part, fwd, dx, g, row; int64_t Mp, slots; }
 Plan plan_of(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
   const int f32 = dtype == LVX_F32;
   Plan p;
-  p.slots = xent_dx_slots(n, E, device_cu_count(), f32);
+  p.slots = xent_dx_slots(n, E, V, device_cu_count(), f32);
   p.Mp = (n + 255) / 256 * 256;
   p.tok = ALIGN;
   p.lab = p.tok + align_up(n * 4);
   p.zlab = p.lab + align_up(n * 4);
   p.part = p.dx = p.zlab + align_up(n * 8);              // (zlab: the forward pass's label logits or the backward pass's rows)
   p.fwd = p.part + (size_t)xent_stat_parts(V, f32) * p.Mp * sizeof(float2);
-  p.g = p.dx + align_up(xent_dx_bytes(n, E, device_cu_count(), f32));
+  p.g = p.dx + align_up(xent_dx_bytes(n, E, V, device_cu_count(), f32));
   p.row = (size_t)p.Mp * (f32 ? 4 : 2);                // bytes of a column of the logits' gradient
   return p;
 }
