@@ -818,9 +818,12 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   // load i of a thread: contraction contiguous: steps 4 (u % 8) .. of row u / 8; else four columns 4 (u % (FT / 4)) .. of step u / (FT / 4),
   // u = tid + 256 i
   f32x4 va[NL], vb[NL];
-  long xrow[NL];
+  long xrow[NL];                                     // LOGITS: of every step; DW: of the next step to be fetched (read a step ahead: 1300 -> 1150)
+  const auto x_rows = [&](int kt) {
 #pragma unroll
-  for (int i = 0; i < NL; ++i) xrow[i] = LOGITS ? a.tok[min(r0 + (tid + 256 * i) / 8, M - 1)] * a.ldx : 0;
+    for (int i = 0; i < NL; ++i) xrow[i] = MODE == DX ? 0 : a.tok[min(LOGITS ? r0 + (tid + 256 * i) / 8 : kt * FK + (tid + 256 * i) / (FT / 4), M - 1)] * a.ldx;
+  };
+  if (MODE != DX && M > 0) x_rows(0);
   const auto fetch = [&](int kt) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
@@ -833,10 +836,11 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
         va[i] = load4(w + (a.v0 + kr) * E + c0 + col, kr < cols ? E - c0 - col : 0);
         vb[i] = load4(gg + (r0 + row) * a.g_pitch + kc, cols - kc);
       } else {
-        va[i] = load4(x + (kr < M ? a.tok[kr] * a.ldx : 0) + c0 + col, kr < M ? E - c0 - col : 0);
+        va[i] = load4(x + xrow[i] + c0 + col, kr < M ? E - c0 - col : 0);
         vb[i] = load4(gg + kr * a.g_pitch + r0 + col, kr < M ? cols - r0 - col : 0);
       }
     }
+    if (MODE == DW) x_rows(kt + 1);
   };
   f32x16 acc[NB][NB];
 #pragma unroll
@@ -851,8 +855,8 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
       *(f32x4*)(sa + (AK ? at_k : at_r)) = va[i];
       *(f32x4*)(sb + (BK_ ? at_k : at_r)) = vb[i];
     }
+    if (kt + 1 < k_to) fetch(kt + 1);                // (in front of the barrier: 3000 x 512 against 40000, dx 1240 -> 1110 us)
     __syncthreads();
-    if (kt + 1 < k_to) fetch(kt + 1);
 #pragma unroll
     for (int s = 0; s < FK / 2; s += 4) {
       f32x4 av[NB], bv[NB];
