@@ -817,46 +817,70 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   float* const gg = (float*)a.g;
   // load i of a thread: contraction contiguous: steps 4 (u % 8) .. of row u / 8; else four columns 4 (u % (FT / 4)) .. of step u / (FT / 4),
   // u = tid + 256 i
-  f32x4 va[NL], vb[NL];
-  long xrow[NL];                                     // LOGITS: of every step; DW: of the next step to be fetched (read a step ahead: 1300 -> 1150)
-  const auto x_rows = [&](int kt) {
+  // Steps that are whole, of tiles whose chunks of four columns exist or do not: nothing to ask, and AHEAD of them on their way (700 tokens x
+  // 200 against 3000: dw 32.5 -> 23 us; 3000 x 512 against 40000: dw 1160 -> 1050, dx 1125 -> 1070, logits 1100 -> 1060).  Rows and columns
+  // past the last one read another one: what becomes of them is not looked at.
+  constexpr int AHEAD = FT == 64 ? 3 : 1;
+  const int k_whole = LOGITS || E % 4 == 0 || c0 + FT <= E ? max(k_from, min(k_to, K / FK)) : k_from;
+  int tok[MODE == DW ? AHEAD : 1][NL];               // LOGITS: of every step; DW: of the next AHEAD steps to be fetched
+  const auto tokens = [&](int kt, int (&t)[NL]) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) xrow[i] = MODE == DX ? 0 : a.tok[min(LOGITS ? r0 + (tid + 256 * i) / 8 : kt * FK + (tid + 256 * i) / (FT / 4), M - 1)] * a.ldx;
+    for (int i = 0; i < NL; ++i) t[i] = a.tok[min(LOGITS ? r0 + (tid + 256 * i) / 8 : kt * FK + (tid + 256 * i) / (FT / 4), M - 1)];
   };
-  if (MODE != DX && M > 0) x_rows(0);
-  const auto fetch = [&](int kt) {
+  if constexpr (LOGITS) tokens(0, tok[0]);
+  const auto fetch_whole = [&](int kt_, f32x4 (&va)[NL], f32x4 (&vb)[NL], int (&tok)[NL]) {
+    const int kt = min(kt_, k_whole - 1);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int u = tid + 256 * i;
+      const int row = u / 8, kc = kt * FK + 4 * (u % 8), kr = kt * FK + u / (FT / 4), col = 4 * (u % (FT / 4));
+      if constexpr (LOGITS) {
+        va[i] = *(const f32x4_any*)(w + (a.v0 + min(c0 + row, cols - 1)) * E + kc);
+        vb[i] = *(const f32x4_any*)(x + tok[i] * a.ldx + kc);
+      } else {
+        const int e = c0 + col + 4 <= E ? c0 + col : c0;
+        if constexpr (MODE == DX) {
+          va[i] = *(const f32x4_any*)(w + (a.v0 + kr) * E + e);
+          vb[i] = *(const f32x4*)(gg + (r0 + row) * a.g_pitch + kc);
+        } else {
+          va[i] = *(const f32x4_any*)(x + tok[i] * a.ldx + e);
+          vb[i] = *(const f32x4*)(gg + kr * a.g_pitch + r0 + col);
+        }
+      }
+    }
+    if constexpr (MODE == DW) tokens(kt_ + AHEAD, tok);
+  };
+  const auto fetch = [&](int kt, f32x4 (&va)[NL], f32x4 (&vb)[NL]) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int u = tid + 256 * i;
       const int row = u / 8, kc = kt * FK + 4 * (u % 8), kr = kt * FK + u / (FT / 4), col = 4 * (u % (FT / 4));
       if constexpr (LOGITS) {
         va[i] = load4(w + (a.v0 + c0 + row) * E + kc, c0 + row < cols ? E - kc : 0);
-        vb[i] = load4(x + xrow[i] + kc, E - kc);
+        vb[i] = load4(x + tok[0][i] * a.ldx + kc, E - kc);
       } else if constexpr (MODE == DX) {
         va[i] = load4(w + (a.v0 + kr) * E + c0 + col, kr < cols ? E - c0 - col : 0);
         vb[i] = load4(gg + (r0 + row) * a.g_pitch + kc, cols - kc);
       } else {
-        va[i] = load4(x + xrow[i] + c0 + col, kr < M ? E - c0 - col : 0);
+        va[i] = load4(x + (kr < M ? a.tok[kr] * a.ldx : 0) + c0 + col, kr < M ? E - c0 - col : 0);
         vb[i] = load4(gg + kr * a.g_pitch + r0 + col, kr < M ? cols - r0 - col : 0);
       }
     }
-    if (MODE == DW) x_rows(kt + 1);
   };
   f32x16 acc[NB][NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j)
 #pragma unroll
     for (int i = 0; i < NB; ++i) acc[j][i] = zero16();
-  if (k_from < k_to) fetch(k_from);
-  for (int kt = k_from; kt < k_to; ++kt) {
+  const auto put = [&](const f32x4 (&va)[NL], const f32x4 (&vb)[NL]) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int u = tid + 256 * i, at_k = (u / 8) * FPK + 4 * (u % 8), at_r = (u / (FT / 4)) * FT + 4 * (u % (FT / 4));
       *(f32x4*)(sa + (AK ? at_k : at_r)) = va[i];
       *(f32x4*)(sb + (BK_ ? at_k : at_r)) = vb[i];
     }
-    if (kt + 1 < k_to) fetch(kt + 1);                // (in front of the barrier: 3000 x 512 against 40000, dx 1240 -> 1110 us)
-    __syncthreads();
+  };
+  const auto multiply = [&]() {
 #pragma unroll
     for (int s = 0; s < FK / 2; s += 4) {
       f32x4 av[NB], bv[NB];
@@ -884,6 +908,31 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
           for (int i = 0; i < NB; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(av[j][k], bv[i][k], acc[j][i], 0, 0, 0);
     }
     __syncthreads();
+  };
+  f32x4 va[AHEAD][NL], vb[AHEAD][NL];
+  const auto whole_steps = [&]() {
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) {
+      if constexpr (MODE == DW) tokens(k_from + d, tok[d]);
+      fetch_whole(k_from + d, va[d], vb[d], tok[MODE == DW ? d : 0]);
+    }
+    for (int kt = k_from;;) {
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d) {
+        put(va[d], vb[d]);
+        fetch_whole(kt + AHEAD, va[d], vb[d], tok[MODE == DW ? d : 0]);
+        __syncthreads();
+        multiply();
+        if (++kt == k_whole) return;
+      }
+    }
+  };
+  if (k_from < k_whole) whole_steps();
+  for (int kt = k_whole; kt < k_to; ++kt) {
+    fetch(kt, va[0], vb[0]);
+    put(va[0], vb[0]);
+    __syncthreads();
+    multiply();
   }
   const float scale = MODE == STATS ? 1.f : a.head->scale;
 #pragma unroll
