@@ -173,3 +173,31 @@ def test_step_replays_from_a_graph():
             assert torch.equal(t, want[n]), f"replay {i}: {n}"
         again = s.run()                                          # eager work between the replays
         assert all(torch.equal(again[n], want[n]) for n in want)
+
+
+@pytest.mark.parametrize("kind,packed", [("layer", True), ("rms", False), (None, True)])
+def test_two_batches_are_two_layers(kind, packed):
+    """float32, the bound of test_step_against_autograd on either side: each batch's results are a layer's of its own, and the weights' gradients
+    add up."""
+    from paper_2502_02406_amd.blockloop import Norm, RecomputeLayer
+    Sq, Skv, E, Hq, Hkv, D = 40, 130, 96, 3, 1, 64
+    g = torch.Generator().manual_seed(21)
+    rnd = lambda *s, std=1.0: (torch.randn(s, generator=g) * std).cuda()
+    x, y, wq, wkv, d_o = rnd(2, Sq, E), rnd(2, Skv, E), rnd(Hq * D, E, std=E ** -0.5), rnd(2 * Hkv * D, E, std=E ** -0.5), rnd(2, Hq, Sq, D)
+    norms = [Norm(1.0 + rnd(E, std=0.2), rnd(E, std=0.2) if kind == "layer" else None) for _ in range(2)] if kind else []
+
+    def run(b, e):
+        layer = RecomputeLayer(e - b, Sq, Skv, E, Hq, Hkv, D, torch.float32, norm=kind, packed=packed)
+        xb, yb = x[b:e].contiguous(), y[b:e].contiguous()
+        o, lse = layer.forward(xb, yb, wq, wkv, *norms)
+        keep = (None, None) if packed else (xb, yb)
+        return [o.clone(), lse.clone()] + [t if t is None else t.clone() for t in layer.backward(*keep, wq, wkv, o, lse, d_o[b:e].contiguous(), *norms)]
+
+    both, one, two = run(0, 2), run(0, 1), run(1, 2)
+    torch.cuda.synchronize()
+    for i, (t, a, b) in enumerate(zip(both, one, two)):
+        if t is None:
+            assert a is None and b is None
+            continue
+        r = (torch.cat([a, b]) if i < 4 else a + b).double()
+        assert t.shape == r.shape and torch.linalg.norm(t.double() - r) <= 2e-4 * torch.linalg.norm(r), i
