@@ -93,8 +93,10 @@ __device__ inline int dx_parts(int tiles, int pairs, int n_cu, int slots) {
 
 // ---- the tokens that have a label, in order: tok[i], its label (-1: not in the vocabulary) and (backward) its lse log2 e and d_loss (NaN for
 // such a label), and how many they are ----
+// 8192 tokens at a time, thread t those with number t modulo 1024, so that a wave's loads and stores are whole lines; every wave sums up the
+// 128 counts of 64 tokens for itself.
 __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
-  __shared__ int sums[2][16];
+  __shared__ int counts[2][128];
   __shared__ float tops[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int total = 0, turn = 0;
@@ -102,45 +104,44 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
   for (long base = 0; base < a.n; base += 8192) {
     long lab[8];
     float d[8], lse[8];
-    int mine = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const long i = base + 8 * tid + k;
+      const long i = base + 1024 * k + tid;
       lab[k] = i < a.n ? a.labels[i] : -1;
       d[k] = a.d_loss && i < a.n ? a.d_loss[i] : 0.f;
       lse[k] = a.d_loss && i < a.n ? a.lse[i] : 0.f;
     }
+    turn ^= 1;                                       // (who writes a place again has crossed the barrier between)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) mine += lab[k] >= 0 ? 1 : 0;
-    int upto = mine;
+    for (int k = 0; k < 8; ++k) {
+      const int c = __popcll(__ballot(lab[k] >= 0));
+      if (lane == 0) counts[turn][16 * k + wave] = c;
+    }
+    __syncthreads();
+    const int c0 = counts[turn][2 * lane], c1 = counts[turn][2 * lane + 1];
+    int upto = c0 + c1;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
       const int y = __shfl_up(upto, o);
       upto += lane >= o ? y : 0;
     }
-    turn ^= 1;                                       // (who writes a place again has crossed the barrier between)
-    if (lane == 63) sums[turn][wave] = upto;
-    __syncthreads();
-    int at = total + upto - mine;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      at += w < wave ? sums[turn][w] : 0;
-      total += sums[turn][w];
-    }
+    const int before = upto - c1 - (wave % 2 == 0 ? c0 : 0);      // of number 2 lane + wave % 2
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const long i = base + 8 * tid + k;
+      const long i = base + 1024 * k + tid;
+      const unsigned long long on = __ballot(lab[k] >= 0);
+      const int at = total + __shfl(before, 8 * k + wave / 2) + __popcll(on & ((1ull << lane) - 1));
       if (lab[k] >= 0) {
         a.tok[at] = (int)i;
         a.lab[at] = lab[k] < a.V ? (int)lab[k] : -1;
         if (a.d_loss) a.row[at] = make_float2(lse[k] * LOG2E, lab[k] < a.V ? d[k] : __builtin_nanf(""));
-        ++at;
         if (fabsf(d[k]) > top && fabsf(d[k]) < __builtin_inff()) top = fabsf(d[k]);
       } else if (a.loss && i < a.n) {
         a.loss[i] = 0.f;
         a.lse_out[i] = 0.f;
       }
     }
+    total += __shfl(upto, 63);
   }
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
