@@ -202,7 +202,7 @@ hipError_t launch_unpack(const NormArgs& a, int is_f32, hipStream_t s);     // t
 // Cross entropy against a vocabulary (lvx_xent.hip).
 struct XentHead {       // what the first launch of a call finds out
   int count;            // tokens that have a label
-  int parts;            // workgroups that share a tile of dx
+  int parts, dw_parts;  // workgroups that share a tile of dx, of dw
   float scale;          // the largest |d_loss|: the logits' gradient is kept divided by it
 };
 struct XentArgs {
@@ -224,16 +224,19 @@ struct XentArgs {
   void* g;              // backward, [Mp][g_pitch] of x's type: the logits' gradient of a piece of the vocabulary
   long g_pitch, piece;  // columns of a piece (a multiple of 256), and from a row of g to the next
   float* dx_part;       // backward, [slots] tiles of sums of dx
-  int slots;
+  float* dw_part;       // backward, [dw_slots] tiles of sums of dw (0: it is not summed in parts)
+  int slots, dw_slots;
   // set by the launches
   long v0, v1;          // the piece at hand
   int first;            // whether it is the first one
-  int tile, tile_rows;  // columns and rows of a tile of dx
+  int tile, tile_rows, dw_tiles;        // columns and rows of a tile of dx; tiles of dw in parts
 };
 bool xent_bf16_supported(int E);
 int xent_stat_parts(long V, int is_f32);
 long xent_dx_slots(long n, int E, long V, int n_cu, int is_f32);
 size_t xent_dx_bytes(long n, int E, long V, int n_cu, int is_f32);
+long xent_dw_slots(long n, int E, long cols, int n_cu, int is_f32);
+size_t xent_dw_bytes(long n, int E, long cols, int n_cu, int is_f32);
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s);
 

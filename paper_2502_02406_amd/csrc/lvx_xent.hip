@@ -40,7 +40,7 @@ constexpr int CB = 16 / NW, WC = 32 * CB;              // a wave's column blocks
 constexpr int OUT_B = 32 * WC * 2;     // epilogue: 32 rows of a wave on their way out
 constexpr int SMEM_B = RING_B + NW * OUT_B;
 static_assert(SMEM_B <= 160 * 1024 && NW / 2 * T * 8 <= NW * OUT_B, "the layout fits a compute unit, and a tile's statistics the way out");
-enum { STATS = 0, GRAD = 1, DX = 2, DW = 3 };
+enum { STATS = 0, GRAD = 1, DX = 2, DW = 3, DW_PARTS = 4 };
 
 __device__ __forceinline__ int perm_of(int r) { return (r & 7) ^ ((r >> 3) & 1); }
 template <int J> __device__ __forceinline__ unsigned row_lane(unsigned x) {       // lane J of every 16
@@ -70,11 +70,11 @@ __device__ __forceinline__ Turns turns_of(long total) {
   const long x = blockIdx.x % 8, wg = (long)blockIdx.y * gridDim.x + blockIdx.x;
   return {total * x / 8 + wg / 8, total * (x + 1) / 8, (long)(gridDim.x / 8) * gridDim.y};
 }
-// The tile of an entry, and (DX) the part of its contraction.
+// The tile of an entry, and (DX, DW_PARTS) the part of its contraction.
 template <int MODE> __device__ __forceinline__ void tile_of(long entry, int n_rt, int n_ct, int* rt, int* ct, int* part) {
   const long tiles = (long)n_rt * n_ct;
-  *part = MODE == DX ? (int)(entry / tiles) : 0;
-  if (MODE == DX) entry -= *part * tiles;
+  *part = MODE == DX || MODE == DW_PARTS ? (int)(entry / tiles) : 0;
+  if (MODE == DX || MODE == DW_PARTS) entry -= *part * tiles;
   if (MODE == STATS || MODE == GRAD) strip_tile(entry, n_ct, n_rt, ct, rt);
   else strip_tile(entry, n_rt, n_ct, rt, ct);
 }
@@ -148,11 +148,13 @@ __global__ void __launch_bounds__(1024) xent_list_kernel(XentArgs a) {
   if (lane == 0) tops[wave] = top;
   __syncthreads();
   const int parts = dx_parts((total + a.tile_rows - 1) / a.tile_rows * ((a.E + a.tile - 1) / a.tile), (int)(a.piece / BK), a.n_cu, a.slots);
+  const int dw_parts = a.dw_slots > 0 ? dx_parts(a.dw_tiles, (total + BK - 1) / BK, a.n_cu, a.dw_slots) : 1;
   if (tid != 0) return;
   for (int w = 0; w < 16; ++w) top = fmaxf(top, tops[w]);
   a.head->count = total;
   a.head->scale = top > 0.f ? top : 1.f;
   a.head->parts = parts;
+  a.head->dw_parts = dw_parts;
 }
 
 // ---- a wave's columns of a logits tile.  z(v, j): the logit in column 32 j + 8 (v / 4) + 4 g + v % 4 of the wave's, JB blocks of 32 ----
@@ -244,6 +246,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(XentArgs a, int n_parts)
 // MODE DX: rows = listed tokens, columns = features, contraction over the piece's vocabulary; g like x before, w as [64][256 features]
 //   with transposing reads.
 // MODE DW: rows = vocabulary of the piece, columns = features, contraction over the listed tokens: both as [64 tokens][256].
+// MODE DW_PARTS: the same where the tiles are few and the tokens many, the contraction cut like DX's.
 // Rows of x go by the list; rows behind the last token read the last one again (their g is 0), rows of w behind the vocabulary its last
 // (their columns of g are 0).
 //
@@ -254,7 +257,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(XentArgs a, int n_parts)
 template <int MODE, int RB>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4, NW / 4)))
 xent_bf16_kernel(XentArgs a) {
-  constexpr bool LOGITS = MODE == STATS || MODE == GRAD;
+  constexpr bool LOGITS = MODE == STATS || MODE == GRAD, OF_W = MODE == DW || MODE == DW_PARTS, SUMS = MODE == DX || MODE == DW_PARTS;
   static_assert(RB == 4 || RB == 2, "tile heights");
   constexpr int TR = 64 * RB;                        // rows of a workgroup's tile
   constexpr int NA = 32 / NW, NB = 8 * RB / NW;      // copies per wave and tile pair: A side (columns), B side (rows)
@@ -262,9 +265,9 @@ xent_bf16_kernel(XentArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int M = a.head->count, E = a.E;
   const int cols = (int)(a.v1 - a.v0);               // of the piece
-  const int n_rt = ((MODE == DW ? cols : M) + TR - 1) / TR;
+  const int n_rt = ((OF_W ? cols : M) + TR - 1) / TR;
   const int n_ct = LOGITS ? (cols + T - 1) / T : (E + T - 1) / T;
-  const int parts = MODE == DX ? a.head->parts : 1;
+  const int parts = MODE == DX ? a.head->parts : MODE == DW_PARTS ? a.head->dw_parts : 1;
   const int nk_all = LOGITS ? E / BK : MODE == DX ? (cols + BK - 1) / BK : (M + BK - 1) / BK;
   struct Tile { int rt, ct, part, r0, c0, k0, nk; }; // (r0: of the list / of the piece, c0: of the piece / of the features)
   const auto tile_at = [&](long entry) __attribute__((always_inline)) -> Tile {
@@ -272,8 +275,8 @@ xent_bf16_kernel(XentArgs a) {
     tile_of<MODE>(entry, n_rt, n_ct, &t.rt, &t.ct, &t.part);
     t.r0 = t.rt * TR;
     t.c0 = t.ct * T;
-    t.k0 = MODE == DX ? (int)((long)t.part * nk_all / parts) : 0;
-    t.nk = MODE == DX ? (int)((long)(t.part + 1) * nk_all / parts) - t.k0 : nk_all;
+    t.k0 = SUMS ? (int)((long)t.part * nk_all / parts) : 0;
+    t.nk = SUMS ? (int)((long)(t.part + 1) * nk_all / parts) - t.k0 : nk_all;
     return t;
   };
   Turns turn = turns_of((long)n_rt * n_ct * parts);
@@ -292,13 +295,13 @@ xent_bf16_kernel(XentArgs a) {
   // (DW's tile of g: [64][TR], an instruction moves BR rows, lane l position l % (64 / BR) of row l / (64 / BR))
   constexpr int BR = 512 / TR, B_ROWB = TR * 2;
   const int lh = lane >> 5, pos = lane & 31, l8 = lane >> 3;
-  unsigned bo[MODE == DW ? 1 : NB], ao[LOGITS ? NA : 1], kr_a[2], kr_b[2];
+  unsigned bo[OF_W ? 1 : NB], ao[LOGITS ? NA : 1], kr_a[2], kr_b[2];
   if constexpr (MODE == DX) {
 #pragma unroll
     for (int j = 0; j < NB; ++j)
       bo[j] = (unsigned)((8 * NB * wave + 8 * j + l8) * g_row_b) + 16u * (unsigned)((lane & 7) ^ perm_of(8 * j + l8));
   }
-  if constexpr (MODE == DW) {
+  if constexpr (OF_W) {
     const int row = lane / (64 / BR);
 #pragma unroll
     for (int par = 0; par < 2; ++par)
@@ -308,9 +311,10 @@ xent_bf16_kernel(XentArgs a) {
   // DW: the rows of x that a wave copies of a pair, lane l row 2 NA wave + 2 (l % 8) + l / 32; those of the first two pairs are every tile's
   const auto x_rows = [&](int kt) __attribute__((always_inline)) -> int { return a.tok[min(kt * BK + 2 * NA * wave + 2 * (lane & 7) + lh, M - 1)]; };
   unsigned xr = 0u, xr01[2] = {0u, 0u};              // their byte offsets
-  if (MODE == DW && M > 0) {
-    xr01[0] = (unsigned)x_rows(0) * xrow_b;
-    xr01[1] = (unsigned)x_rows(1) * xrow_b;
+  if (OF_W && M > 0) {                               // (DW_PARTS: a workgroup has one tile)
+    const int k0 = MODE == DW_PARTS ? tile_at(turn.entry).k0 : 0;
+    xr01[0] = (unsigned)x_rows(k0) * xrow_b;
+    xr01[1] = (unsigned)x_rows(k0 + 1) * xrow_b;
   }
   // LOGITS: the tokens of a tile that a wave copies
   int tok[NB];
@@ -340,7 +344,7 @@ xent_bf16_kernel(XentArgs a) {
         kr_a[par] = t.c0 + 8 * c >= E ? 0u : 16u * (unsigned)c;
       }
       ap = MODE == DX ? (const char*)a.w + ((a.v0 + t.k0 * BK) * E + t.c0) * 2 : (const char*)a.x + 2L * t.c0;
-      bp = MODE == DX ? (const char*)a.g + t.r0 * g_row_b + (long)t.k0 * RK_ROWB : (const char*)a.g + 2L * t.r0;
+      bp = MODE == DX ? (const char*)a.g + t.r0 * g_row_b + (long)t.k0 * RK_ROWB : (const char*)a.g + 2L * t.r0 + (long)t.k0 * BK * g_row_b;
       w_left = a.V - 1 - a.v0 - (long)t.k0 * BK;
     }
   };
@@ -372,9 +376,9 @@ xent_bf16_kernel(XentArgs a) {
       }
     } else {                                         // B side
       const int j = p - NA;
-      if constexpr (MODE != DW) dma16u(bp, bo[j], st + (unsigned)(TILE_B + (8 * NB * wave + 8 * j) * RK_ROWB));
+      if constexpr (!OF_W) dma16u(bp, bo[j], st + (unsigned)(TILE_B + (8 * NB * wave + 8 * j) * RK_ROWB));
       else dma16u(bp, kr_b[j & 1] + (unsigned)(BR * j) * (unsigned)g_row_b, st + (unsigned)(TILE_B + BR * (NB * wave + j) * B_ROWB));
-      if (j == NB - 1) bp += MODE == DW ? 64 * g_row_b : RK_ROWB;
+      if (j == NB - 1) bp += OF_W ? 64 * g_row_b : RK_ROWB;
     }
   };
   const auto start = [&](const Tile& t) __attribute__((always_inline)) {      // a tile's first two pairs
@@ -382,7 +386,7 @@ xent_bf16_kernel(XentArgs a) {
 #pragma unroll
     for (int q = 0; q < NSLOT; ++q)
       if (q < t.nk) {
-        if (MODE == DW) xr = xr01[q];
+        if (OF_W) xr = xr01[q];
 #pragma unroll
         for (int p = 0; p < NPART; ++p) issue_part(q, p);
       }
@@ -410,7 +414,7 @@ xent_bf16_kernel(XentArgs a) {
     else return tr_op(st + ka[j] + 16 * q * KR_ROWB, std::integral_constant<int, KR_ROWB>{});
   };
   auto b_op = [&](const char* st, int q, int i) __attribute__((always_inline)) -> bf16x8 {
-    if constexpr (MODE != DW) return *(const bf16x8*)(st + TILE_B + (wm * 32 * RB + 32 * i) * RK_ROWB + rd[q]);
+    if constexpr (!OF_W) return *(const bf16x8*)(st + TILE_B + (wm * 32 * RB + 32 * i) * RK_ROWB + rd[q]);
     else return tr_op(st + kb[i] + 16 * q * B_ROWB, std::integral_constant<int, B_ROWB>{});
   };
 
@@ -478,14 +482,14 @@ xent_bf16_kernel(XentArgs a) {
           if ((STEADY || send2) && u % EB == EB - 1) issue_part(P + 1, NA + u / EB);
         });
         int next_rows = 0;
-        if constexpr (MODE == DW) next_rows = x_rows(P + 2);        // (has come when the wait below is over)
+        if constexpr (OF_W) next_rows = x_rows(cur.k0 + P + 2);        // (has come when the wait below is over)
         mma16(bb, ab, [&](int u) __attribute__((always_inline)) { fetch(st, 2, u, ba, aa); });
         mma16(ba, aa, [&](int u) __attribute__((always_inline)) { fetch(st, 3, u, bb, ab); });
         if (STEADY || more) {
           __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) and lgkmcnt(0)
           wg_barrier();
         }
-        if constexpr (MODE == DW) xr = (unsigned)next_rows * xrow_b;
+        if constexpr (OF_W) xr = (unsigned)next_rows * xrow_b;
         mma16(bb, ab, [&](int u) __attribute__((always_inline)) {
           if (STEADY || more) fetch(sn, 0, u, ba, aa);
           if ((STEADY || send1) && u % EA == EA - 1) issue_part(P + 2, u / EA);
@@ -535,15 +539,16 @@ xent_bf16_kernel(XentArgs a) {
         for (int w = 0; w < NW / 2; ++w) join_stats(&m, &s, sums[w * TR + tid].x, sums[w * TR + tid].y);
         a.part[(long)cur.ct * a.Mp + cur.r0 + tid] = make_float2(m, s);
       }
-    } else if constexpr (MODE == DX) {
-      // in the order of the registers, 16 bytes a lane (xent_dx_kernel reads them so), on top of what the pieces before left
-      float* const to = a.dx_part + (((long)cur.part * n_rt + cur.rt) * n_ct + cur.ct) * (TR * T) + wave * (TR * T / NW) + lane * 4;
+    } else if constexpr (SUMS) {
+      // in the order of the registers, 16 bytes a lane (xent_sum_bf16_kernel reads them so), on top of what the pieces before left (DX)
+      const bool first = MODE == DW_PARTS || a.first;
+      float* const to = (MODE == DX ? a.dx_part : a.dw_part) + (((long)cur.part * n_rt + cur.rt) * n_ct + cur.ct) * (TR * T) + wave * (TR * T / NW) + lane * 4;
 #pragma unroll
       for (int j = 0; j < CB; ++j)
 #pragma unroll
         for (int i0 = 0; i0 < RB; i0 += 2) {             // (eight old values on their way: more would not fit the registers)
           f32x4 old[2][4];
-          if (!a.first) {
+          if (!first) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -555,7 +560,7 @@ xent_bf16_kernel(XentArgs a) {
             for (int q = 0; q < 4; ++q) {
               const f32x16& s = acc[j][i0 + i];
               f32x4 v = {s[4 * q], s[4 * q + 1], s[4 * q + 2], s[4 * q + 3]};
-              if (!a.first) v += old[i][q];
+              if (!first) v += old[i][q];
               *(f32x4*)(to + ((j * RB + i0 + i) * 4 + q) * 256) = v;
             }
         }
@@ -747,18 +752,18 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
   }
 }
 
-// dx of the listed tokens: the parts' sums, 32 tokens x 32 features a workgroup; 0 for the others
-__global__ void __launch_bounds__(256) xent_dx_bf16_kernel(XentArgs a, unsigned tiles) {
-  const int M = a.head->count, E = a.E, tid = threadIdx.x, n_ec = (E + 31) / 32;
+// Sums of parts, 32 rows x 32 features a workgroup.  DX: of the listed tokens; 0 for the others.  DW_PARTS: of the piece's vocabulary.
+template <int MODE> __global__ void __launch_bounds__(256) xent_sum_bf16_kernel(XentArgs a, unsigned tiles) {
+  const int M = MODE == DX ? a.head->count : (int)(a.v1 - a.v0), E = a.E, tid = threadIdx.x, n_ec = (E + 31) / 32;
   if (blockIdx.x < tiles) {
     const int r = (int)(blockIdx.x / n_ec) * 32 + tid % 32, c = (int)(blockIdx.x % n_ec) * 32 + 4 * (tid / 32);
     if (r >= M || c >= E) return;
-    const int tr = a.tile_rows, n_ct = (E + T - 1) / T, rl = r % tr, cl = c % T;
+    const int tr = MODE == DX ? a.tile_rows : 128, n_ct = (E + T - 1) / T, rl = r % tr, cl = c % T;
     const long tile = (long)(r / tr) * n_ct + c / T, step = (long)((M + tr - 1) / tr) * n_ct * tr * T;
     const int wave = rl / (tr / 2) * (NW / 2) + cl / WC, i = rl % (tr / 2) / 32, j = cl % WC / 32, q = cl % 32 / 8;
-    const float* from = a.dx_part + tile * (tr * T) + wave * (tr * T / NW) + ((j * (tr / 64) + i) * 4 + q) * 256 + (rl % 32 + 32 * (cl / 4 % 2)) * 4;
+    const float* from = (MODE == DX ? a.dx_part : a.dw_part) + tile * (tr * T) + wave * (tr * T / NW) + ((j * (tr / 64) + i) * 4 + q) * 256 + (rl % 32 + 32 * (cl / 4 % 2)) * 4;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    const int parts = a.head->parts;
+    const int parts = MODE == DX ? a.head->parts : a.head->dw_parts;
     for (int p0 = 0; p0 < parts; p0 += 8) {              // (eight on their way at once)
       f32x4 v[8];
 #pragma unroll
@@ -768,7 +773,8 @@ __global__ void __launch_bounds__(256) xent_dx_bf16_kernel(XentArgs a, unsigned 
         if (p0 + p < parts) s += v[p];
     }
     s *= a.head->scale;
-    *(u32x2*)((uint16_t*)a.dx + a.tok[r] * a.ldx + c) = u32x2{pack2_bf16(s[0], s[1]), pack2_bf16(s[2], s[3])};
+    uint16_t* const to = MODE == DX ? (uint16_t*)a.dx + a.tok[r] * a.ldx : (uint16_t*)a.dw + (a.v0 + r) * E;
+    *(u32x2*)(to + c) = u32x2{pack2_bf16(s[0], s[1]), pack2_bf16(s[2], s[3])};
     return;
   }
   for (long i = (long)(blockIdx.x - tiles) * 4 + (tid >> 6); i < a.n; i += (long)(gridDim.x - tiles) * 4)
@@ -796,14 +802,14 @@ __device__ __forceinline__ f32x4 load4(const float* p, int there) {      // four
 }
 template <int MODE, int FT>
 __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
-  constexpr bool LOGITS = MODE == STATS || MODE == GRAD;
-  constexpr bool AK = LOGITS, BK_ = MODE != DW;      // whether the operand has the contraction contiguous
+  constexpr bool LOGITS = MODE == STATS || MODE == GRAD, OF_W = MODE == DW || MODE == DW_PARTS, SUMS = MODE == DX || MODE == DW_PARTS;
+  constexpr bool AK = LOGITS, BK_ = !OF_W;      // whether the operand has the contraction contiguous
   constexpr int NB = FT / 64, NL = FT * FK / 1024;   // 32-blocks of a wave per side; 16-byte loads of a thread per side
   __shared__ __attribute__((aligned(16))) float sa[FT * FPK], sb[FT * FPK];
   const int M = a.head->count, E = a.E, cols = (int)(a.v1 - a.v0);
-  const int n_rt = MODE == DW ? (cols + FT - 1) / FT : (M + FT - 1) / FT;
+  const int n_rt = OF_W ? (cols + FT - 1) / FT : (M + FT - 1) / FT;
   const int n_ct = LOGITS ? (cols + FT - 1) / FT : (E + FT - 1) / FT;
-  const int parts = MODE == DX ? a.head->parts : 1;
+  const int parts = MODE == DX ? a.head->parts : MODE == DW_PARTS ? a.head->dw_parts : 1;
   const Turns turn = turns_of((long)n_rt * n_ct * parts);      // (one tile a workgroup: a loop over them costs dw a fifth, in registers)
   if (turn.entry >= turn.end) return;
   int rt, ct, part;
@@ -812,8 +818,8 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
   const int K = LOGITS ? E : MODE == DX ? cols : M;
   const int nk_all = (K + FK - 1) / FK;
-  const int k_from = MODE == DX ? (int)((long)part * nk_all / parts) : 0;
-  const int k_to = MODE == DX ? (int)((long)(part + 1) * nk_all / parts) : nk_all;
+  const int k_from = SUMS ? (int)((long)part * nk_all / parts) : 0;
+  const int k_to = SUMS ? (int)((long)(part + 1) * nk_all / parts) : nk_all;
   const float *const x = (const float*)a.x, *const w = (const float*)a.w;
   float* const gg = (float*)a.g;
   // load i of a thread: contraction contiguous: steps 4 (u % 8) .. of row u / 8; else four columns 4 (u % (FT / 4)) .. of step u / (FT / 4),
@@ -823,7 +829,7 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   // past the last one read another one: what becomes of them is not looked at.
   constexpr int AHEAD = FT == 64 ? 3 : 1;
   const int k_whole = LOGITS || E % 4 == 0 || c0 + FT <= E ? max(k_from, min(k_to, K / FK)) : k_from;
-  int tok[MODE == DW ? AHEAD : 1][NL];               // LOGITS: of every step; DW: of the next AHEAD steps to be fetched
+  int tok[OF_W ? AHEAD : 1][NL];               // LOGITS: of every step; DW: of the next AHEAD steps to be fetched
   const auto tokens = [&](int kt, int (&t)[NL]) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) t[i] = a.tok[min(LOGITS ? r0 + (tid + 256 * i) / 8 : kt * FK + (tid + 256 * i) / (FT / 4), M - 1)];
@@ -849,7 +855,7 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
         }
       }
     }
-    if constexpr (MODE == DW) tokens(kt_ + AHEAD, tok);
+    if constexpr (OF_W) tokens(kt_ + AHEAD, tok);
   };
   const auto fetch = [&](int kt, f32x4 (&va)[NL], f32x4 (&vb)[NL]) {
 #pragma unroll
@@ -914,14 +920,14 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
   const auto whole_steps = [&]() {
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d) {
-      if constexpr (MODE == DW) tokens(k_from + d, tok[d]);
-      fetch_whole(k_from + d, va[d], vb[d], tok[MODE == DW ? d : 0]);
+      if constexpr (OF_W) tokens(k_from + d, tok[d]);
+      fetch_whole(k_from + d, va[d], vb[d], tok[OF_W ? d : 0]);
     }
     for (int kt = k_from;;) {
 #pragma unroll
       for (int d = 0; d < AHEAD; ++d) {
         put(va[d], vb[d]);
-        fetch_whole(kt + AHEAD, va[d], vb[d], tok[MODE == DW ? d : 0]);
+        fetch_whole(kt + AHEAD, va[d], vb[d], tok[OF_W ? d : 0]);
         __syncthreads();
         multiply();
         if (++kt == k_whole) return;
@@ -972,9 +978,9 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
               y[k] = at + k < cols && d != 0.f ? p * d : 0.f;
             }
             *(f32x4*)(gg + r * a.g_pitch + at) = y;            // (a row of g has room for whole tiles)
-          } else if constexpr (MODE == DX) {
-            float* const to = a.dx_part + (((long)part * n_rt + rt) * n_ct + ct) * (FT * FT) + (r - r0) * FT + (at - c0);
-            if (!a.first) y += *(const f32x4*)to;
+          } else if constexpr (SUMS) {
+            float* const to = (MODE == DX ? a.dx_part : a.dw_part) + (((long)part * n_rt + rt) * n_ct + ct) * (FT * FT) + (r - r0) * FT + (at - c0);
+            if (MODE == DX && !a.first) y += *(const f32x4*)to;
             *(f32x4*)to = y;
           } else if (r < cols) {
             float* const to = (float*)a.dw + (a.v0 + r) * E + at;
@@ -988,14 +994,14 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
     }
   }
 }
-__global__ void __launch_bounds__(256) xent_dx_f32_kernel(XentArgs a, unsigned rows) {
-  const int M = a.head->count, E = a.E;
+template <int MODE> __global__ void __launch_bounds__(256) xent_sum_f32_kernel(XentArgs a, unsigned rows) {
+  const int M = MODE == DX ? a.head->count : (int)(a.v1 - a.v0), E = a.E;
   if (blockIdx.x < rows) {
-    const int t = a.tile, n_ct = (E + t - 1) / t, parts = a.head->parts;
+    const int t = MODE == DX ? a.tile : 64, n_ct = (E + t - 1) / t, parts = MODE == DX ? a.head->parts : a.head->dw_parts;
     const long step = (long)((M + t - 1) / t) * n_ct * (t * t);
     for (int r = blockIdx.x; r < M; r += rows) {
       for (int e = threadIdx.x; e < E; e += 256) {
-        const float* const from = a.dx_part + ((long)(r / t) * n_ct + e / t) * (t * t) + (r % t) * t + e % t;
+        const float* const from = (MODE == DX ? a.dx_part : a.dw_part) + ((long)(r / t) * n_ct + e / t) * (t * t) + (r % t) * t + e % t;
         float s = 0.f;
         for (int p0 = 0; p0 < parts; p0 += 8) {
           float v[8];
@@ -1004,7 +1010,7 @@ __global__ void __launch_bounds__(256) xent_dx_f32_kernel(XentArgs a, unsigned r
 #pragma unroll
           for (int p = 0; p < 8; ++p) s += p0 + p < parts ? v[p] : 0.f;
         }
-        ((float*)a.dx)[a.tok[r] * a.ldx + e] = s * a.head->scale;
+        (MODE == DX ? (float*)a.dx + a.tok[r] * a.ldx : (float*)a.dw + (a.v0 + r) * E)[e] = s * a.head->scale;
       }
     }
     return;
@@ -1052,7 +1058,7 @@ template <int MODE> hipError_t product(const XentArgs& a, long rows, long cols, 
 int f32_edge(long rows, long cols, int n_cu) { return up(rows, 128) * up(cols, 128) < 2L * n_cu ? 64 : 128; }
 constexpr long MOST_WGS = 1 << 14;     // along one side of a launch, whose threads may not pass 2^32
 template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long cols, int edge, hipStream_t s) {
-  const long wgs = strip_grid(MODE == DX ? (long)a.slots : up(rows, edge) * up(cols, edge));
+  const long wgs = strip_grid(MODE == DX ? (long)a.slots : MODE == DW_PARTS ? (long)a.dw_slots : up(rows, edge) * up(cols, edge));
   const dim3 grid((unsigned)std::min(wgs, MOST_WGS), (unsigned)up(wgs, MOST_WGS));
   if (edge == 64) xent_f32_kernel<MODE, 64><<<grid, 256, 0, s>>>(a);
   else xent_f32_kernel<MODE, 128><<<grid, 256, 0, s>>>(a);
@@ -1078,7 +1084,35 @@ int dx_f32_edge(long n, int E, long V, int n_cu) {
 }
 int dx_edge(long n, int E, long V, int n_cu, int is_f32) { return is_f32 ? dx_f32_edge(n, E, V, n_cu) : T; }
 int dx_rows(long n, int E, long V, int n_cu, int is_f32) { return is_f32 ? dx_f32_edge(n, E, V, n_cu) : n <= 128 ? 128 : T; }
+// dw in parts: its tiles
+int dw_rows(int is_f32) { return is_f32 ? 64 : 128; }
+int dw_edge(int is_f32) { return is_f32 ? 64 : T; }
+long dw_tiles(long cols, int E, int is_f32) { return up(cols, dw_rows(is_f32)) * up(E, dw_edge(is_f32)); }
+hipError_t dw_in_parts(const XentArgs& a, int is_f32, hipStream_t s) {
+  const long cols = a.v1 - a.v0;
+  const hipError_t e = is_f32 ? f32_product<DW_PARTS>(a, cols, a.E, 64, s) : launch_tiles<DW_PARTS, 2>(a, strip_grid(a.dw_slots), s);
+  if (e != hipSuccess) return e;
+  if (is_f32) {
+    xent_sum_f32_kernel<DW_PARTS><<<(unsigned)cols, 256, 0, s>>>(a, (unsigned)cols);
+  } else {
+    const unsigned tiles = (unsigned)(up(cols, 32) * up(a.E, 32));
+    xent_sum_bf16_kernel<DW_PARTS><<<tiles, 256, 0, s>>>(a, tiles);
+  }
+  return hipGetLastError();
+}
 }  // namespace
+
+// Tiles of sums of dw that a piece of `cols` columns takes; at most one for a compute unit, so that a workgroup has one.  0 where the tiles of the
+// product are as good: a tile pair's time (64 tokens) is 0.85 us, float32 1.6, and writing the parts, reading them and the launch cost 12.
+// dw of 16384 tokens x 128 against 1000 191 -> 25 us, 5000 x 512 against 1500 68 -> 25, 2048 x 512 against 4000 30 -> 27, float32 4000 x 256 against
+// 1000 101 -> 37; where the rule keeps one part, 1024 x 1024 against 2000 17 -> 23.
+long xent_dw_slots(long n, int E, long cols, int n_cu, int is_f32) {
+  const long tiles = dw_tiles(cols, E, is_f32), pairs = up(n, BK), parts = std::min({(long)MOST_PARTS, pairs / 4, n_cu / 8 * 8 / tiles});
+  return parts < 2 || (is_f32 ? 1.6 : 0.85) * (pairs - pairs / parts) < 12.0 ? 0 : parts * tiles;
+}
+size_t xent_dw_bytes(long n, int E, long cols, int n_cu, int is_f32) {
+  return sizeof(float) * dw_rows(is_f32) * dw_edge(is_f32) * xent_dw_slots(n, E, cols, n_cu, is_f32);
+}
 
 bool xent_bf16_supported(int E) { return E % BK == 0; }
 int xent_stat_parts(long V, int is_f32) { return (int)(2 * up(V, is_f32 ? 64 : T)); }
@@ -1106,6 +1140,7 @@ hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
 }
 
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
+  a.dw_tiles = (int)dw_tiles(std::min(a.piece, a.V), a.E, is_f32);
   a.tile = dx_edge(a.n, a.E, a.V, a.n_cu, is_f32);
   a.tile_rows = dx_rows(a.n, a.E, a.V, a.n_cu, is_f32);
   xent_list_kernel<<<1, 1024, 0, s>>>(a);
@@ -1115,7 +1150,8 @@ hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
     a.v1 = a.v0 + a.piece < a.V ? a.v0 + a.piece : a.V;
     const long cols = a.v1 - a.v0;
     e = logits<GRAD>(a, is_f32, s);
-    if (e == hipSuccess && a.dw)
+    if (e == hipSuccess && a.dw && a.dw_slots > 0) e = dw_in_parts(a, is_f32, s);
+    else if (e == hipSuccess && a.dw)
       e = is_f32 ? f32_product<DW>(a, cols, a.E, f32_edge(cols, a.E, a.n_cu), s) : product<DW>(a, cols, a.E, up(a.n, BK), s);
     if (e == hipSuccess && a.dx) {
       e = is_f32 ? f32_product<DX>(a, a.n, a.E, a.tile, s)
@@ -1127,10 +1163,10 @@ hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
   const long zero = up(a.n, 4) < 1024 ? up(a.n, 4) : 1024;
   if (is_f32) {
     const unsigned rows = (unsigned)std::min(a.n, MOST_WGS);
-    xent_dx_f32_kernel<<<rows + (unsigned)zero, 256, 0, s>>>(a, rows);
+    xent_sum_f32_kernel<DX><<<rows + (unsigned)zero, 256, 0, s>>>(a, rows);
   } else {
     const unsigned tiles = (unsigned)(up(a.n, 32) * up(a.E, 32));
-    xent_dx_bf16_kernel<<<tiles + (unsigned)zero, 256, 0, s>>>(a, tiles);
+    xent_sum_bf16_kernel<DX><<<tiles + (unsigned)zero, 256, 0, s>>>(a, tiles);
   }
   return hipGetLastError();
 }

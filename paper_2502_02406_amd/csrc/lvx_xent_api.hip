@@ -18,7 +18,8 @@ lvx_status check_sizes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
   return LVX_OK;
 }
 
-// The workspace: the list of tokens; then (forward) what the tiles leave, or (backward) dx's sums and the gradient of a piece of the logits.
+// The workspace: the list of tokens; then (forward) what the tiles leave, or (backward) dx's sums, the gradient of a piece of the logits
+// and dw's sums.
 struct Plan { size_t tok, lab, zlab, part, fwd, dx, g, row; int64_t Mp, slots; };
 Plan plan_of(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
   const int f32 = dtype == LVX_F32;
@@ -79,7 +80,8 @@ extern "C" {
 size_t lvx_xent_workspace_bytes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
   if (check_sizes(n, E, V, dtype) != LVX_OK) return 0;
   const Plan p = plan_of(n, E, V, dtype);
-  const size_t bwd = p.g + (size_t)(piece_of(p, V) + PAD) * p.row;
+  const int64_t piece = piece_of(p, V);
+  const size_t bwd = align_up(p.g + (size_t)(piece + PAD) * p.row) + xent_dw_bytes(n, E, piece < V ? piece : V, device_cu_count(), dtype == LVX_F32);
   return align_up(p.fwd > bwd ? p.fwd : bwd);
 }
 
@@ -113,6 +115,13 @@ lvx_status lvx_xent_bwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const
   a.piece = piece;
   a.g_pitch = piece + PAD;
   a.lse = lse; a.d_loss = d_loss; a.dx = dx; a.dw = dw;
+  // parts of dw, if there is room for them behind it
+  const int64_t cols = piece < p->V ? piece : p->V;
+  const size_t end = align_up(plan.g + (size_t)a.g_pitch * plan.row);
+  if (end + xent_dw_bytes(p->n, p->E, cols, a.n_cu, dtype == LVX_F32) <= workspace_bytes) {
+    a.dw_slots = (int)xent_dw_slots(p->n, p->E, cols, a.n_cu, dtype == LVX_F32);
+    a.dw_part = (float*)((char*)workspace + end);
+  }
   return launch_xent_bwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
 }
 

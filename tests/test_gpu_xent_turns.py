@@ -46,3 +46,35 @@ def test_f32_tiles_in_turn():
         dw64 += g.T @ x64
         tol_w += eg.T @ x64.abs() + (n / 2 + 64) * u * (g.abs().T @ x64.abs())
     assert ((dw - dw64).abs() <= 1.02 * tol_w).all()
+
+
+# few tiles of dw and many tokens: its contraction is cut into parts
+@pytest.mark.parametrize("dtype,n,E,V,ignored", [("bf16", 5000, 64, 300, 0.3), ("bf16", 3000, 320, 1000, 0.0), ("bf16", 1280, 64, 1, 0.5), ("bf16", 2000, 64, 129, 0.999),
+                                                 ("f32", 3000, 40, 200, 0.3), ("f32", 1030, 67, 130, 0.0), ("f32", 1500, 3, 1, 0.9)])
+def test_dw_in_parts(dtype, n, E, V, ignored):
+    print(f"[xent] {dtype} {n}x{E} V={V}", flush=True)
+    args = inputs(n, E, V, dtype, n + V, ignored=ignored)
+    got = run(*args)
+    ref, tol = reference(*args, dtype)
+    check(got, ref, tol, f"{dtype} {n}x{E}x{V}")
+    assert all(torch.equal(a, b) for a, b in zip(got, run(*args))), "not repeatable"
+    assert torch.equal(run(*args, dx=False)[3], got[3])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_dw_in_parts_piece_by_piece(dtype):
+    """Room for pieces of 256 entries and, with one byte too few for them and with enough, for the parts of dw."""
+    n, E, V = 3000, 64, 700
+    args = inputs(n, E, V, dtype, 8)
+    ref, tol = reference(*args, dtype)
+    f32 = dtype == "f32"
+    up = lambda v: (v + 255) // 256 * 256
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    edge = 64 if f32 and -(-n // 128) * -(-E // 128) * max(1, min(64, V // 256)) < cus else 128 if f32 else 256
+    tiles = -(-n // edge) * -(-E // edge)
+    least = 256 + 2 * up(4 * n) + up(8 * n) + max(tiles, min(64 * tiles, 2 * cus)) * edge * edge * 4 + 320 * up(n) * (4 if f32 else 2)
+    dw_tiles = 4 if f32 else 2
+    room = min(64, (-(-n // 64)) // 4, cus // 8 * 8 // dw_tiles) * dw_tiles * (64 * 64 if f32 else 128 * 256) * 4
+    assert room < 256 * up(n) * (4 if f32 else 2) or least + room <= B.lvx_xent_workspace_bytes(n, E, V, B.dtype_code(args[0].dtype))
+    for ws in (least, least + room - 1, least + room):
+        check(run(*args, ws_bytes=ws), ref, tol, f"{ws - least} bytes for parts")
