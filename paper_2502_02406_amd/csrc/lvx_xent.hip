@@ -623,7 +623,7 @@ xent_bf16_kernel(XentArgs a) {
   }
 }
 
-// Logits of few tokens (few_takes): bound by reading w.  A workgroup takes 128 entries of the vocabulary, a wave 32 of them against 32 RB tokens, and
+// Logits of few tokens (few_rows): bound by reading w.  A workgroup takes 128 entries of the vocabulary, a wave 32 of them against 32 RB tokens, and
 // NS slots of 64 features are on their way (of w alone, 16 KB each; two-slot tiles of 256 entries kept half of the compute units
 // waiting, 16 tokens x 4096 against 32768: 85 -> 66 us).  Six slots (64 tokens) where the workgroups have a compute unit each, three where two share
 // one.  Behind the last features the copies go on with these again, so that every step waits for the same number.
@@ -634,8 +634,10 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
   static_assert(4 * W_B <= NS * S_B, "they fit the slots");
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int M = a.head->count, E = a.E, cols = (int)(a.v1 - a.v0), nk = E / BK;
-  if (M == 0) return;
-  const int c0 = blockIdx.x * CT;
+  const int n_rt = (M + 32 * RB - 1) / (32 * RB), n_ct = (cols + CT - 1) / CT;
+  const Turns turn = turns_of((long)n_rt * n_ct);
+  if (turn.entry >= turn.end) return;
+  const int ct = (int)(turn.entry / n_rt), c0 = ct * CT, r0 = (int)(turn.entry % n_rt) * 32 * RB;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned xrow_b = (unsigned)(a.ldx * 2), wrow_b = (unsigned)(E * 2);
@@ -649,14 +651,14 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
 #pragma unroll
   for (int j = 0; j < RB; ++j) {
     const int r = 8 * RB * wave + 8 * j + (lane >> 3);
-    bo[j] = (unsigned)a.tok[min(r, M - 1)] * xrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(r));
+    bo[j] = (unsigned)a.tok[min(r0 + r, M - 1)] * xrow_b + 16u * (unsigned)((lane & 7) ^ perm_of(r));
   }
   const char* const wg = (const char*)a.w + (a.v0 + c0) * wrow_b;
   // (every workgroup begins at another feature: at the same one, the lines that all of them ask for lie 2 E bytes apart, in few of the memory's
   // channels; 16 x 4096 against 32768 69 -> 53 us, against 131072 217 -> 186, 5.8 TB/s)
-  const int turn = (int)(blockIdx.x * 7u % (unsigned)nk);
+  const int from = (int)(ct * 7u % (unsigned)nk);
   const auto issue = [&](int kt, int slot) __attribute__((always_inline)) {
-    const int k = min(kt, nk - 1) + turn;
+    const int k = min(kt, nk - 1) + from;
     const long k_b = (long)(k < nk ? k : k - nk) * RK_ROWB;
     const unsigned st = smem_u + (unsigned)(slot * S_B);
 #pragma unroll
@@ -705,16 +707,16 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       float m2, s;
       tile_stats<1>(g, left, z, &m2, &s);
       if (g == 0) sums[wave * 32 * RB + r] = make_float2(m2, s);
-      const int c = r < M ? a.lab[r] - c0 - cw : -1;
+      const int c = r0 + r < M ? a.lab[r0 + r] - c0 - cw : -1;
       const float y = tile_pick<1>(g, c, z);
-      if (c >= 0 && c < 32 && ((c >> 2) & 1) == g) a.zlab[r] = y;
+      if (c >= 0 && c < 32 && ((c >> 2) & 1) == g) a.zlab[r0 + r] = y;
     }
     __syncthreads();
-    if (tid < 32 * RB && tid < M) {
+    if (tid < 32 * RB && r0 + tid < M) {
       float m = -__builtin_inff(), s = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) join_stats(&m, &s, sums[w * 32 * RB + tid].x, sums[w * 32 * RB + tid].y);
-      a.part[(long)blockIdx.x * a.Mp + tid] = make_float2(m, s);
+      a.part[(long)ct * a.Mp + r0 + tid] = make_float2(m, s);
     }
   } else {
     const float scale = a.head->scale;
@@ -724,10 +726,10 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       const int r = 32 * i + l31;
       float lse2 = 0.f, d = 0.f;
       int c = -1;
-      if (r < M) {
-        lse2 = a.row[r].x;
-        d = a.row[r].y / scale;
-        c = a.lab[r] - (int)a.v0 - c0 - cw;
+      if (r0 + r < M) {
+        lse2 = a.row[r0 + r].x;
+        d = a.row[r0 + r].y / scale;
+        c = a.lab[r0 + r] - (int)a.v0 - c0 - cw;
       }
       const int end = d != 0.f ? left - 4 * g : 0, hot = c - 4 * g;
 #pragma unroll
@@ -747,7 +749,7 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
     for (int it = 0; it < 2 * RB; ++it) {
       const int r = 16 * it + (lane >> 2), ch = lane & 3;
       const u32x4 y = *(const u32x4*)(tb + r * W_PITCH + 16 * ch);
-      *(u32x4*)((char*)a.g + (long)r * a.g_pitch * 2 + 2L * (c0 + cw + 8 * ch)) = y;
+      *(u32x4*)((char*)a.g + (long)(r0 + r) * a.g_pitch * 2 + 2L * (c0 + cw + 8 * ch)) = y;
     }
   }
 }
@@ -1028,16 +1030,12 @@ template <int MODE, int RB> hipError_t launch_tiles(const XentArgs& a, long grid
   xent_bf16_kernel<MODE, RB><<<(unsigned)(grid < stay ? grid : stay), 64 * NW, SMEM_B, s>>>(a);
   return hipGetLastError();
 }
-// Up to 128 tokens where their workgroups have a compute unit each (128 x 4096 against 32768: statistics 96 -> 74 us, gradient 83 -> 62; where they take
-// turns, 100 x 1024 against 131072, 67 -> 75 and 57 -> 74), up to 64 always.  (GRAD: 64 or 128 tokens whatever their number: the contraction of
-// dw runs over g's rows 64 at a time.)
-bool few_takes(long n, long cols, int n_cu) { return n <= 64 || (n <= 128 && (cols + 127) / 128 <= n_cu); }
 template <int MODE, int RB, int NS> hipError_t launch_few(const XentArgs& a, long wgs, hipStream_t s) {
   constexpr int bytes = NS * (128 + 32 * RB) * RK_ROWB;
   static SmemOnce once;
   const hipError_t e = ensure_dynamic_lds((const void*)xent_few_bf16_kernel<MODE, RB, NS>, bytes, &once);
   if (e != hipSuccess) return e;
-  xent_few_bf16_kernel<MODE, RB, NS><<<(unsigned)wgs, 256, bytes, s>>>(a);
+  xent_few_bf16_kernel<MODE, RB, NS><<<(unsigned)strip_grid(wgs), 256, bytes, s>>>(a);
   return hipGetLastError();
 }
 long up(long n, long by) { return (n + by - 1) / by; }
@@ -1048,6 +1046,17 @@ long up(long n, long by) { return (n + by - 1) / by; }
 bool low_tiles(long rows, long cols, long pairs, int n_cu) {
   const long ct = up(cols, T);
   return rows <= 128 || up(up(rows, 128) * ct, n_cu) * (0.85 * pairs + 3.5) < up(up(rows, T) * ct, n_cu) * (1.55 * pairs + 6.0);
+}
+// Rows of the tiles of logits of xent_few_bf16_kernel; 0: xent_bf16_kernel.  Up to 64 tokens there is one row of tiles.  With more, tiles of 64 x
+// 128 where all of them have a place at once: statistics of 664 tokens x 2496 features against 2171 34 -> 20 us, 130 x 3392 against 13376 74 -> 51,
+// 922 x 1280 against 3838 22 -> 17.5, 100 x 512 against 4000 10 -> 7.5; where they take turns, 300 x 256 against 20000 9.6 -> 11.5, 1024 x 512
+// against 8192 13 -> 17.5.  Up to 128 tokens of many features the copies are what counts, and every entry of the vocabulary is copied once: 128 x
+// 4096 against 32768 91 (xent_bf16_kernel), 68 (64 rows), 54 (128 rows); 100 x 1024 against 30000 20, 16, 17, against 10000 17, 11, 16.
+// (GRAD: 64 or 128 tokens whatever their number: the contraction of dw runs over g's rows 64 at a time.)
+int few_rows(long n, long cols, long pairs, int n_cu) {
+  const long ct = up(cols, 128);
+  if (n > 64 && n <= 128 && ct <= n_cu && pairs >= 32) return 128;
+  return n <= 64 || up(n, 64) * ct <= 2L * n_cu ? 64 : 0;
 }
 template <int MODE> hipError_t product(const XentArgs& a, long rows, long cols, long pairs, hipStream_t s) {
   if (low_tiles(rows, cols, pairs, a.n_cu)) return launch_tiles<MODE, 2>(a, strip_grid(up(rows, 128) * up(cols, T)), s);
@@ -1067,11 +1076,12 @@ template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long co
 template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t s) {
   const long cols = a.v1 - a.v0;
   if (is_f32) return f32_product<MODE>(a, a.n, cols, f32_edge(a.n, cols, a.n_cu), s);
-  if (few_takes(a.n, cols, a.n_cu)) {
-    const long wgs = up(cols, 128);
+  const int rows = few_rows(a.n, cols, a.E / BK, a.n_cu);
+  const long wgs = rows > 0 ? up(cols, 128) * up(a.n, rows) : 0;
+  if (rows == 128) return launch_few<MODE, 4, 4>(a, wgs, s);
+  if (rows > 0) {
     if constexpr (MODE == STATS)
       if (a.n <= 32) return wgs <= a.n_cu ? launch_few<MODE, 1, 6>(a, wgs, s) : launch_few<MODE, 1, 3>(a, wgs, s);
-    if (a.n > 64) return launch_few<MODE, 4, 4>(a, wgs, s);
     return wgs <= a.n_cu ? launch_few<MODE, 2, 6>(a, wgs, s) : launch_few<MODE, 2, 3>(a, wgs, s);
   }
   return product<MODE>(a, a.n, cols, a.E / BK, s);
@@ -1135,7 +1145,7 @@ hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
   const hipError_t e = logits<STATS>(a, is_f32, s);
   if (e != hipSuccess) return e;
   const long wgs = up(a.n, 8);
-  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : few_takes(a.n, a.V, a.n_cu) ? (int)up(a.V, 128) : (int)up(a.V, T));
+  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : few_rows(a.n, a.V, a.E / BK, a.n_cu) > 0 ? (int)up(a.V, 128) : (int)up(a.V, T));
   return hipGetLastError();
 }
 
