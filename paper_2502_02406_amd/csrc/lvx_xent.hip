@@ -996,30 +996,119 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
     }
   }
 }
+// Logits of few tokens (f32_few): 32 x 32 tiles, the features dealt out to the four waves, 32 at a time, which bring their operands straight
+// into registers: a lane has 64 bytes of a row of w and of x.
+template <int MODE> __global__ void __launch_bounds__(256) xent_few_f32_kernel(XentArgs a) {
+  __shared__ __attribute__((aligned(16))) float sums[3][4][256];
+  const int M = a.head->count, E = a.E, cols = (int)(a.v1 - a.v0), n_rt = (M + 31) / 32, n_ct = (cols + 31) / 32;
+  const Turns turn = turns_of((long)n_rt * n_ct);
+  if (turn.entry >= turn.end) return;
+  const int ct = (int)(turn.entry / n_rt), c0 = ct * 32, r0 = (int)(turn.entry % n_rt) * 32;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const float* const w = (const float*)a.w + (a.v0 + min(c0 + l31, cols - 1)) * E + 16 * g;
+  const float* const x = (const float*)a.x + a.tok[min(r0 + l31, M - 1)] * a.ldx + 16 * g;
+  f32x16 acc = zero16();
+  const auto multiply = [&](const f32x4 (&av)[4], const f32x4 (&bv)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(av[j][k], bv[j][k], acc, 0, 0, 0);
+  };
+  const int whole = E / 32;                          // step s: features 32 s ..; the wave's are wave, wave + 4, ..
+  f32x4 av[2][4], bv[2][4];
+  const auto fetch = [&](int s, int d) {
+    const int at = 32 * min(s, whole - 1);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      av[d][j] = *(const f32x4_any*)(w + at + 4 * j);
+      bv[d][j] = *(const f32x4_any*)(x + at + 4 * j);
+    }
+  };
+  if (wave < whole) {
+    fetch(wave, 0);
+    for (int s = wave; s < whole; s += 8) {
+      fetch(s + 4, 1);
+      multiply(av[0], bv[0]);
+      if (s + 4 >= whole) break;
+      fetch(s + 8, 0);
+      multiply(av[1], bv[1]);
+    }
+  }
+  if (E % 32 != 0 && wave == whole % 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int left = E - 32 * whole - 16 * g - 4 * j;
+      av[0][j] = load4(w + 32 * whole + 4 * j, left);
+      bv[0][j] = load4(x + 32 * whole + 4 * j, left);
+    }
+    multiply(av[0], bv[0]);
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *(f32x4*)(&sums[wave - 1][q][4 * lane]) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    f32x4 s = *(const f32x4*)(&sums[0][q][4 * lane]);
+#pragma unroll
+    for (int o = 1; o < 3; ++o) s += *(const f32x4*)(&sums[o][q][4 * lane]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[4 * q + k] += s[k];
+  }
+  const int r = r0 + l31;
+  if constexpr (MODE == STATS) {
+    const auto z = [&](int v, int) -> float { return acc[v]; };
+    float m2, s;
+    tile_stats<1>(g, cols - c0, z, &m2, &s);
+    if (g == 0 && r < M) a.part[(long)ct * a.Mp + r] = make_float2(m2, s);
+    const int c = r < M ? a.lab[r] - c0 : -1;
+    if (__any(c >= 0 && c < 32)) {
+      const float y = tile_pick<1>(g, c, z);
+      if (c >= 0 && c < 32 && ((c >> 2) & 1) == g) a.zlab[r] = y;
+    }
+  } else {
+    if (r >= M) return;
+    const float lse2 = a.row[r].x, d = a.row[r].y / a.head->scale;
+    const int c = a.lab[r] - (int)a.v0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = c0 + 8 * q + 4 * g;
+      f32x4 y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float p = exp2_fast(fmaf(acc[4 * q + k], LOG2E, -lse2)) - (at + k == c ? 1.f : 0.f);
+        y[k] = at + k < cols && d != 0.f ? p * d : 0.f;
+      }
+      *(f32x4*)((float*)a.g + r * a.g_pitch + at) = y;
+    }
+  }
+}
+// The same in float32: a row and 256 features (blockIdx.y) a workgroup.
 template <int MODE> __global__ void __launch_bounds__(256) xent_sum_f32_kernel(XentArgs a, unsigned rows) {
-  const int M = MODE == DX ? a.head->count : (int)(a.v1 - a.v0), E = a.E;
+  const int M = MODE == DX ? a.head->count : (int)(a.v1 - a.v0), E = a.E, e = (int)blockIdx.y * 256 + threadIdx.x;
+  if (e >= E) return;
   if (blockIdx.x < rows) {
     const int t = MODE == DX ? a.tile : 64, n_ct = (E + t - 1) / t, parts = MODE == DX ? a.head->parts : a.head->dw_parts;
     const long step = (long)((M + t - 1) / t) * n_ct * (t * t);
     for (int r = blockIdx.x; r < M; r += rows) {
-      for (int e = threadIdx.x; e < E; e += 256) {
-        const float* const from = (MODE == DX ? a.dx_part : a.dw_part) + ((long)(r / t) * n_ct + e / t) * (t * t) + (r % t) * t + e % t;
-        float s = 0.f;
-        for (int p0 = 0; p0 < parts; p0 += 8) {
-          float v[8];
+      const float* const from = (MODE == DX ? a.dx_part : a.dw_part) + ((long)(r / t) * n_ct + e / t) * (t * t) + (r % t) * t + e % t;
+      float s = 0.f;
+      for (int p0 = 0; p0 < parts; p0 += 8) {
+        float v[8];
 #pragma unroll
-          for (int p = 0; p < 8; ++p) v[p] = from[min(p0 + p, parts - 1) * step];
+        for (int p = 0; p < 8; ++p) v[p] = from[min(p0 + p, parts - 1) * step];
 #pragma unroll
-          for (int p = 0; p < 8; ++p) s += p0 + p < parts ? v[p] : 0.f;
-        }
-        (MODE == DX ? (float*)a.dx + a.tok[r] * a.ldx : (float*)a.dw + (a.v0 + r) * E)[e] = s * a.head->scale;
+        for (int p = 0; p < 8; ++p) s += p0 + p < parts ? v[p] : 0.f;
       }
+      (MODE == DX ? (float*)a.dx + a.tok[r] * a.ldx : (float*)a.dw + (a.v0 + r) * E)[e] = s * a.head->scale;
     }
     return;
   }
   for (long i = blockIdx.x - rows; i < a.n; i += gridDim.x - rows)
-    if (a.labels[i] < 0)
-      for (int e = threadIdx.x; e < E; e += 256) ((float*)a.dx)[i * a.ldx + e] = 0.f;
+    if (a.labels[i] < 0) ((float*)a.dx)[i * a.ldx + e] = 0.f;
 }
 
 template <int MODE, int RB> hipError_t launch_tiles(const XentArgs& a, long grid, hipStream_t s) {
@@ -1065,6 +1154,9 @@ template <int MODE> hipError_t product(const XentArgs& a, long rows, long cols, 
 // float32: the edge of the tiles of a product.  64 where 128 makes less than two for every compute unit: 300 tokens x 512 features against 5003,
 // the four products 246 -> 112 us
 int f32_edge(long rows, long cols, int n_cu) { return up(rows, 128) * up(cols, 128) < 2L * n_cu ? 64 : 128; }
+// float32: logits by xent_few_f32_kernel.  20 tokens x 512 against 131072 161 -> 99 us, 23 x 1664 against 5347 38 -> 20, 4 x 2048 against 1967 44 -> 20;
+// with more tokens rows are brought too often, 300 x 512 against 5003 25 -> 34, 64 x 256 against 65536 42 -> 41
+bool f32_few(long n) { return n <= 32; }
 constexpr long MOST_WGS = 1 << 14;     // along one side of a launch, whose threads may not pass 2^32
 template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long cols, int edge, hipStream_t s) {
   const long wgs = strip_grid(MODE == DX ? (long)a.slots : MODE == DW_PARTS ? (long)a.dw_slots : up(rows, edge) * up(cols, edge));
@@ -1075,6 +1167,10 @@ template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long co
 }
 template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t s) {
   const long cols = a.v1 - a.v0;
+  if (is_f32 && f32_few(a.n)) {
+    xent_few_f32_kernel<MODE><<<(unsigned)strip_grid(up(a.n, 32) * up(cols, 32)), 256, 0, s>>>(a);
+    return hipGetLastError();
+  }
   if (is_f32) return f32_product<MODE>(a, a.n, cols, f32_edge(a.n, cols, a.n_cu), s);
   const int rows = few_rows(a.n, cols, a.E / BK, a.n_cu);
   const long wgs = rows > 0 ? up(cols, 128) * up(a.n, rows) : 0;
@@ -1088,9 +1184,9 @@ template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t
 }
 // dx: columns and rows of a tile.  float32: 128 where the parts make one for every compute unit (3000 tokens x 512 features against 40000 1610 -> 1210
 // us, 1000 x 512 against 10000 148 -> 118, 2000 x 200 against 3000 53 -> 43; where they do not, 100 x 256 against 30000 32 -> 47, 300 x 1024 against
-// 1000 13.6 -> 26).
+// 1000 13.6 -> 26) and there is more than half a tile of tokens (20 x 512 against 131072 181 -> 110 with 64, 2 x 640 against 32768 57 -> 35).
 int dx_f32_edge(long n, int E, long V, int n_cu) {
-  return up(n, 128) * up(E, 128) * std::max(1L, std::min((long)MOST_PARTS, V / 256)) < n_cu ? 64 : 128;
+  return n <= 64 || up(n, 128) * up(E, 128) * std::max(1L, std::min((long)MOST_PARTS, V / 256)) < n_cu ? 64 : 128;
 }
 int dx_edge(long n, int E, long V, int n_cu, int is_f32) { return is_f32 ? dx_f32_edge(n, E, V, n_cu) : T; }
 int dx_rows(long n, int E, long V, int n_cu, int is_f32) { return is_f32 ? dx_f32_edge(n, E, V, n_cu) : n <= 128 ? 128 : T; }
@@ -1103,7 +1199,7 @@ hipError_t dw_in_parts(const XentArgs& a, int is_f32, hipStream_t s) {
   const hipError_t e = is_f32 ? f32_product<DW_PARTS>(a, cols, a.E, 64, s) : launch_tiles<DW_PARTS, 2>(a, strip_grid(a.dw_slots), s);
   if (e != hipSuccess) return e;
   if (is_f32) {
-    xent_sum_f32_kernel<DW_PARTS><<<(unsigned)cols, 256, 0, s>>>(a, (unsigned)cols);
+    xent_sum_f32_kernel<DW_PARTS><<<dim3((unsigned)cols, (unsigned)up(a.E, 256)), 256, 0, s>>>(a, (unsigned)cols);
   } else {
     const unsigned tiles = (unsigned)(up(cols, 32) * up(a.E, 32));
     xent_sum_bf16_kernel<DW_PARTS><<<tiles, 256, 0, s>>>(a, tiles);
@@ -1145,7 +1241,7 @@ hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
   const hipError_t e = logits<STATS>(a, is_f32, s);
   if (e != hipSuccess) return e;
   const long wgs = up(a.n, 8);
-  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : few_rows(a.n, a.V, a.E / BK, a.n_cu) > 0 ? (int)up(a.V, 128) : (int)up(a.V, T));
+  xent_join_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), 256, 0, s>>>(a, is_f32 ? (int)(f32_few(a.n) ? up(a.V, 32) : 2 * up(a.V, f32_edge(a.n, a.V, a.n_cu))) : few_rows(a.n, a.V, a.E / BK, a.n_cu) > 0 ? (int)up(a.V, 128) : (int)up(a.V, T));
   return hipGetLastError();
 }
 
@@ -1173,7 +1269,7 @@ hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
   const long zero = up(a.n, 4) < 1024 ? up(a.n, 4) : 1024;
   if (is_f32) {
     const unsigned rows = (unsigned)std::min(a.n, MOST_WGS);
-    xent_sum_f32_kernel<DX><<<rows + (unsigned)zero, 256, 0, s>>>(a, rows);
+    xent_sum_f32_kernel<DX><<<dim3(rows + (unsigned)zero, (unsigned)up(a.E, 256)), 256, 0, s>>>(a, rows);
   } else {
     const unsigned tiles = (unsigned)(up(a.n, 32) * up(a.E, 32));
     xent_sum_bf16_kernel<DX><<<tiles + (unsigned)zero, 256, 0, s>>>(a, tiles);

@@ -56,7 +56,7 @@ def test_workspace(lib):  # noqa: F811
         p = prob(n=n, E=E, V=V, x_ss=E)
         el, Mp = (4 if dt == B.LVX_F32 else 2), (n + 255) // 256 * 256
         up = lambda x: (x + 255) // 256 * 256
-        edge = 256 if dt == B.LVX_BF16 else 64 if -(-n // 128) * -(-E // 128) * max(1, min(64, V // 256)) < 256 else 128
+        edge = 256 if dt == B.LVX_BF16 else 64 if n <= 64 or -(-n // 128) * -(-E // 128) * max(1, min(64, V // 256)) < 256 else 128
         rows = 128 if dt == B.LVX_BF16 and n <= 128 else edge
         tiles = -(-n // rows) * -(-E // edge)
         need = 256 + 2 * up(4 * n) + up(8 * n) + max(tiles, min(64 * tiles, 512)) * rows * edge * 4 + 320 * Mp * el   # lists, sums of dx, 256 columns and 64 between
