@@ -8,15 +8,20 @@
  * and, in the backward pass, recomputes the attention probabilities from the
  * saved statistic L instead of storing them (Section 3.2)       lvx_xattn_bwd,
  * after recomputing Q, K and V from the token features          lvx_xattn_project.
+ * Around the layer stand the norms of its token features          lvx_norm_fwd,
+ * the 8-bit form in which they are kept                           lvx_pack,
+ * and the loss at the end of a training step                      lvx_xent_fwd.
  *
  * General rules for every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The library
  *     never allocates, frees or synchronises; all work is enqueued on the HIP
  *     stream the caller passes (a hipStream_t cast to void*, NULL = default).
  *   - Scratch memory is a caller-provided workspace whose size comes from
- *     lvx_xattn_workspace_bytes; it must be 256-byte aligned.
- *   - lvx_problem / lvx_mask structs and the pointer arrays of lvx_xattn_merge
- *     live in HOST memory and are read before the call returns.
+ *     lvx_xattn_workspace_bytes (lvx_norm_workspace_bytes, lvx_xent_workspace_bytes);
+ *     it must be 256-byte aligned, and what it holds is a call's own: two calls that may
+ *     run at the same time (two streams, two captured graphs) need one each.
+ *   - The structs of arguments (lvx_problem, lvx_mask, lvx_norm, ..) and the pointer
+ *     arrays of lvx_xattn_merge live in HOST memory and are read before the call returns.
  *   - Errors are returned as negative lvx_status values; argument errors are
  *     detected on the host before anything is launched.  No exceptions, no aborts.
  *   - The library keeps no state between calls that a result depends on (it only
@@ -322,7 +327,8 @@ lvx_status lvx_norm_bwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const
  * aligned pointers and x_ss % 8 == 0; n and V are arbitrary.  LVX_F32 takes any E and alignment.  n * x_ss may not pass 2^31
  * (LVX_ERR_STRIDE): larger batches go in several calls.
  * workspace   of lvx_xent_workspace_bytes(n, E, V, dtype) (0: invalid sizes), for either pass; it also serves fewer tokens, fewer
- *         features and smaller vocabularies.  lvx_xent_bwd takes less, down to pieces of 256 entries of the vocabulary, and is slower. */
+ *         features and smaller vocabularies.  lvx_xent_bwd takes less, down to pieces of 256 entries of the vocabulary, and is slower;
+ *         its sums are then cut, and rounded, in other places. */
 typedef struct {
   int64_t n, V;             /* tokens, entries of the vocabulary */
   int32_t E;                /* features */

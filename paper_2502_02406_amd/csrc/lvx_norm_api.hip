@@ -72,6 +72,7 @@ lvx_status lvx_norm_fwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const
   if (!aligned_for(x, dtype) || !aligned_for(y, dtype) || !aligned_for(gamma, dtype) || !aligned_for(beta, dtype) ||
       (uintptr_t)stats % 4 != 0)
     return LVX_ERR_STRIDE;
+  if (x == y && p->x_ss != p->y_ss && p->n > 1) return LVX_ERR_STRIDE;
   a.x = x; a.gamma = gamma; a.beta = beta; a.y = y; a.stats = stats;
   if (packed) { a.q = packed->q; a.b = packed->e; }
   return launch_norm_fwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
@@ -94,6 +95,7 @@ lvx_status lvx_norm_bwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const
   if (!aligned_for(x, dtype) || !aligned_for(dy, dtype) || !aligned_for(dx, dtype) || !aligned_for(gamma, dtype) ||
       (uintptr_t)stats % 4 != 0 || (uintptr_t)dgamma % 4 != 0 || (uintptr_t)dbeta % 4 != 0)
     return LVX_ERR_STRIDE;
+  if (dx == dy && p->x_ss != p->y_ss && p->n > 1) return LVX_ERR_STRIDE;
   a.x = x; a.gamma = gamma; a.stats_in = stats; a.dy = dy; a.dx = dx; a.dgamma = dgamma; a.dbeta = dbeta;
   if (packed) { a.q = packed->q; a.b = packed->e; }
   if (dgamma || dbeta) {

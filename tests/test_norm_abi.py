@@ -38,6 +38,7 @@ def test_norm_fwd_refusals(lib):  # noqa: F811
     assert fwd(lib, norm(), x=FAKE + 1) == -4 and fwd(lib, norm(), y=FAKE + 1) == -4 and fwd(lib, norm(), beta=FAKE + 1) == -4
     assert fwd(lib, norm(), dtype=B.LVX_F32, x=FAKE + 2) == -4
     assert fwd(lib, norm(), stats=FAKE + 2) == -4
+    assert fwd(lib, norm(x_ss=264)) == -4                        # y is x, with other strides
 
 
 def test_norm_bwd_refusals(lib):  # noqa: F811
@@ -51,6 +52,7 @@ def test_norm_bwd_refusals(lib):  # noqa: F811
     assert bwd(lib, norm(), ws=None) == -6 and bwd(lib, norm(), ws=FAKE + 16) == -6
     assert bwd(lib, norm(), n=B.lvx_norm_workspace_bytes(100, 256) - 1) == -6
     assert bwd(lib, norm(), dx=FAKE + 1) == -4 and bwd(lib, norm(), dgamma=FAKE + 2) == -4 and bwd(lib, norm(), dbeta=FAKE + 2) == -4
+    assert bwd(lib, norm(x_ss=264)) == -4 and bwd(lib, norm(y_ss=264)) == -4       # dx is dy, with other strides
     assert bwd(lib, norm(x_ss=8)) == -4 and bwd(lib, norm(n=-1)) == -2 and bwd(lib, norm(), dtype=2) == -3
 
 
