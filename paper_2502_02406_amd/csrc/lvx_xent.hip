@@ -1129,12 +1129,13 @@ template <int MODE, int RB, int NS> hipError_t launch_few(const XentArgs& a, lon
 }
 long up(long n, long by) { return (n + by - 1) / by; }
 // Whether tiles of 128 rows are the better ones for a product of `rows` x `cols` with `pairs` tile pairs: by the rounds of workgroups, a
-// tile's pairs at 1.55 us (128 rows: 0.85) and what a tile costs beside them, 6 us (3.5).  Statistics and gradient of 300 tokens x 256 against
-// 50000 26.8 -> 20.8 and 31.5 -> 24.7, x 1024 66 -> 61 and 62 -> 54; dw of 2000 x 512 against 8000 43 -> 31; where the rule keeps 256
-// rows, 2048 x 1024 against 8192 34.5 -> 39.4 and 37 -> 40, 1000 x 512 against 30000 40 -> 44, 44 -> 46 and (dw) 34 -> 38.
+// tile's pairs at 1.55 us (128 rows: 0.85, where they take turns 1.05) and what a tile costs beside them, 6 us (3.5).  Statistics and gradient of 300
+// tokens x 256 against 50000 26.8 -> 20.8 and 31.5 -> 24.7, x 1024 66 -> 61 and 62 -> 54, 384 x 1024 against 20000 29 -> 23 and 32 -> 22; dw of
+// 1261 x 192 against 10305 30 -> 20; where the rule keeps 256 rows, statistics and gradient of 512 x 3840 against 32818 186 -> 216 and 175 -> 194,
+// 1000 x 1024 against 30000 60 -> 71 and 66 -> 73; dw of 2206 x 1024 against 50021 298 -> 329, 4000 x 256 against 40000 133 -> 165.
 bool low_tiles(long rows, long cols, long pairs, int n_cu) {
-  const long ct = up(cols, T);
-  return rows <= 128 || up(up(rows, 128) * ct, n_cu) * (0.85 * pairs + 3.5) < up(up(rows, T) * ct, n_cu) * (1.55 * pairs + 6.0);
+  const long low = up(rows, 128) * up(cols, T), high = up(rows, T) * up(cols, T);
+  return rows <= 128 || up(low, n_cu) * ((low <= n_cu ? 0.85 : 1.05) * pairs + 3.5) < up(high, n_cu) * (1.55 * pairs + 6.0);
 }
 // Rows of the tiles of logits of xent_few_bf16_kernel; 0: xent_bf16_kernel.  Up to 64 tokens there is one row of tiles.  With more, tiles of 64 x
 // 128 where all of them have a place at once: statistics of 664 tokens x 2496 features against 2171 34 -> 20 us, 130 x 3392 against 13376 74 -> 51,
