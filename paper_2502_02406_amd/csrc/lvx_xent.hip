@@ -1159,9 +1159,10 @@ int f32_edge(long rows, long cols, int n_cu) { return up(rows, 128) * up(cols, 1
 // with more tokens rows are brought too often, 300 x 512 against 5003 25 -> 34, 64 x 256 against 65536 42 -> 41
 bool f32_few(long n) { return n <= 32; }
 constexpr long MOST_WGS = 1 << 14;     // along one side of a launch, whose threads may not pass 2^32
+dim3 grid_of(long wgs) { return dim3((unsigned)std::min(wgs, MOST_WGS), (unsigned)up(wgs, MOST_WGS)); }
 template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long cols, int edge, hipStream_t s) {
   const long wgs = strip_grid(MODE == DX ? (long)a.slots : MODE == DW_PARTS ? (long)a.dw_slots : up(rows, edge) * up(cols, edge));
-  const dim3 grid((unsigned)std::min(wgs, MOST_WGS), (unsigned)up(wgs, MOST_WGS));
+  const dim3 grid = grid_of(wgs);
   if (edge == 64) xent_f32_kernel<MODE, 64><<<grid, 256, 0, s>>>(a);
   else xent_f32_kernel<MODE, 128><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
@@ -1169,7 +1170,7 @@ template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long co
 template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t s) {
   const long cols = a.v1 - a.v0;
   if (is_f32 && f32_few(a.n)) {
-    xent_few_f32_kernel<MODE><<<(unsigned)strip_grid(up(a.n, 32) * up(cols, 32)), 256, 0, s>>>(a);
+    xent_few_f32_kernel<MODE><<<grid_of(strip_grid(up(a.n, 32) * up(cols, 32))), 256, 0, s>>>(a);
     return hipGetLastError();
   }
   if (is_f32) return f32_product<MODE>(a, a.n, cols, f32_edge(a.n, cols, a.n_cu), s);

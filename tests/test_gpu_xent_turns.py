@@ -78,3 +78,32 @@ def test_dw_in_parts_piece_by_piece(dtype):
     assert room < 256 * up(n) * (4 if f32 else 2) or least + room <= B.lvx_xent_workspace_bytes(n, E, V, B.dtype_code(args[0].dtype))
     for ws in (least, least + room - 1, least + room):
         check(run(*args, ws_bytes=ws), ref, tol, f"{ws - least} bytes for parts")
+
+
+@pytest.mark.parametrize("dtype,n,E,V", [("bf16", 2000, 64, 129), ("f32", 1500, 40, 200), ("f32", 20, 40, 200), ("bf16", 200, 128, 300)])
+def test_no_labels(dtype, n, E, V):
+    """Nothing to do, in each form of the products: zeros."""
+    x, w, labels, d = inputs(n, E, V, dtype, 3)
+    loss, lse, dx, dw = run(x, w, torch.full_like(labels, -1), d)
+    assert not loss.any() and not lse.any() and not dx.any() and not dw.any()
+
+
+def test_f32_few_tokens_of_a_long_vocabulary():
+    """More workgroups than one side of a launch takes.  The loss of 2 tokens of 2 features; errors as in test_gpu_xent.py."""
+    n, E, V = 2, 2, 32 * 16384 + 77
+    x, w, labels, d = inputs(n, E, V, "f32", 6, ignored=0.0)
+    labels[1] = V - 1
+    loss, lse, dx, dw = run(x, w, labels, d)
+    z = x.double() @ w.double().T
+    ref = torch.logsumexp(z, 1)
+    u = 2.0 ** -24
+    ez = 17 * u * (x.double().abs() @ w.double().abs().T)
+    e_lse = ez.max(1).values + (V / 4096 + 200 + 4 * (ref.abs() + z.abs().max(1).values)) * u
+    zl = z.gather(1, labels[:, None])[:, 0]
+    assert ((lse - ref).abs() <= 1.02 * e_lse).all()
+    assert ((loss - (ref - zl)).abs() <= 1.02 * (e_lse + ez.gather(1, labels[:, None])[:, 0] + 2 * u * (ref.abs() + zl.abs()))).all()
+    p = torch.exp(z - ref[:, None])
+    g = p.scatter_add(1, labels[:, None], torch.full_like(zl, -1.0)[:, None]) * d.double()[:, None]
+    eg = p * d.double().abs()[:, None] * (ez + e_lse[:, None] + (8 + 4 * (ref.abs()[:, None] + z.abs())) * u) + 2 * u * g.abs()
+    assert ((dx - g @ w.double()).abs() <= 1.02 * (eg @ w.double().abs() + (V / 2 + 64) * u * (g.abs() @ w.double().abs()))).all()
+    assert ((dw - g.T @ x.double()).abs() <= 1.02 * (eg.T @ x.double().abs() + 65 * u * (g.abs().T @ x.double().abs()))).all()
