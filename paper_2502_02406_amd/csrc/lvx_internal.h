@@ -229,6 +229,7 @@ struct XentArgs {
   // set by the launches
   long v0, v1;          // the piece at hand
   int first;            // whether it is the first one
+  int own;              // so few tokens that every wave lists them for itself
   int tile, tile_rows, dw_tiles;        // columns and rows of a tile of dx; tiles of dw in parts
 };
 bool xent_bf16_supported(int E);

@@ -41,7 +41,7 @@ def test_tile_loop_moves_no_accumulator(mode, row_blocks):
         assert "scratch_" not in loop, "register spill inside the loop"
 
 
-@pytest.mark.parametrize("name", ["xent_few_bf16_kernelILi0ELi1ELi6E", "xent_few_bf16_kernelILi0ELi2ELi3E", "xent_few_bf16_kernelILi1ELi2ELi6E",
-                                  "xent_few_bf16_kernelILi1ELi4ELi4E", "xent_f32_kernelILi0ELi128E", "xent_f32_kernelILi2ELi64E"])
+@pytest.mark.parametrize("name", ["xent_few_bf16_kernelILi0ELi1ELi6ELb1E", "xent_few_bf16_kernelILi0ELi2ELi3ELb0E", "xent_few_bf16_kernelILi1ELi2ELi6ELb1E",
+                                  "xent_few_bf16_kernelILi1ELi4ELi4ELb0E", "xent_f32_kernelILi0ELi128E", "xent_f32_kernelILi2ELi64E"])
 def test_no_spills(name):
     assert kernel(name)[1] == 0

@@ -107,3 +107,21 @@ def test_f32_few_tokens_of_a_long_vocabulary():
     eg = p * d.double().abs()[:, None] * (ez + e_lse[:, None] + (8 + 4 * (ref.abs()[:, None] + z.abs())) * u) + 2 * u * g.abs()
     assert ((dx - g @ w.double()).abs() <= 1.02 * (eg @ w.double().abs() + (V / 2 + 64) * u * (g.abs() @ w.double().abs()))).all()
     assert ((dw - g.T @ x.double()).abs() <= 1.02 * (eg.T @ x.double().abs() + 65 * u * (g.abs().T @ x.double().abs()))).all()
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 20), ("bf16", 64), ("f32", 32)])
+def test_labels_outside_among_few_tokens(dtype, n):
+    x, w, labels, d = inputs(n, 64, 300, dtype, 19, ignored=0.0)
+    ref, tol = reference(x, w, labels, d, dtype)
+    far = labels.clone()
+    far[3], far[5], far[7], far[n - 1] = 300, 1 << 40, -(1 << 40), -1
+    loss, lse, dx, dw = run(x, w, far, d)
+    bad, off = torch.zeros(n, dtype=torch.bool), torch.zeros(n, dtype=torch.bool)
+    bad[[3, 5]] = True
+    off[[7, n - 1]] = True
+    assert loss.cpu().isnan().equal(bad) and lse.cpu().isnan().equal(bad) and dw.isnan().all()
+    assert dx.cpu()[bad].isnan().all() and not loss.cpu()[off].any() and not lse.cpu()[off].any() and not dx.cpu()[off].any()
+    good = ~(bad | off)
+    for name, t in (("loss", loss), ("lse", lse), ("dx", dx)):
+        err = (t.double().cpu()[good] - torch.from_numpy(ref[name])[good]).abs()
+        assert (err <= 1.02 * torch.from_numpy(tol[name])[good] + 1e-30).all(), name
