@@ -809,16 +809,110 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
   }
 }
 
+// dx of up to 64 tokens, bound by reading w as well: 128 features and a part of the vocabulary a workgroup, a wave 32 of them against 32 RB tokens,
+// NS slots of 64 entries (16 KB of w) on their way.  The parts' sums go out as rows of floats, [part][64][E rounded up to 128].  2 tokens x 640
+// against 2560 7.8 -> 4.5 us, 1 x 1664 against 16384 17 -> 11, 64 x 256 against 65536 20 -> 12.5, 16 x 3520 against 131072 230 -> 200 (4.6 TB/s, while
+// dw of the launch before is still on its way to memory; 16 x 4096 against 32768 85 in either form).
+template <int RB, int NS>
+__global__ void __launch_bounds__(256) xent_few_dx_bf16_kernel(XentArgs a) {
+  constexpr int CT = 128, PITCH = CT * 2, A_B = BK * PITCH, B_B = 32 * RB * RK_ROWB, S_B = A_B + B_B, NP = 4 + RB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int M = a.head->count, E = a.E, cols = (int)(a.v1 - a.v0), n_ct = (E + CT - 1) / CT, nk_all = (cols + BK - 1) / BK, parts = a.head->parts;
+  const Turns turn = turns_of((long)n_ct * parts);
+  if (turn.entry >= turn.end || M == 0) return;
+  const int ct = (int)(turn.entry % n_ct), part = (int)(turn.entry / n_ct), e0 = ct * CT;
+  const int k0 = (int)((long)part * nk_all / parts), nk = (int)((long)(part + 1) * nk_all / parts) - k0;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l31 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned wrow_b = (unsigned)(E * 2), g_row_b = (unsigned)(a.g_pitch * 2);
+  const unsigned smem_u = lds_base(smem);
+  // copies of w: 4 rows x 256 bytes an instruction, lane l position l % 16 of row l / 16, which holds the chunk (l % 16) ^ 4 (row % 4); features past
+  // the last one: the tile's first chunk again
+  const int chunk = (lane & 15) ^ (4 * (lane >> 4));
+  const unsigned a_chunk = e0 + 8 * chunk >= E ? 0u : 16u * (unsigned)chunk;
+  unsigned bo[RB];
+#pragma unroll
+  for (int j = 0; j < RB; ++j) {
+    const int r = 8 * RB * wave + 8 * j + (lane >> 3);
+    bo[j] = (unsigned)r * g_row_b + 16u * (unsigned)((lane & 7) ^ perm_of(r));
+  }
+  const auto issue = [&](int kt, int slot) __attribute__((always_inline)) {
+    const int k = k0 + min(kt, nk - 1);              // (behind the last pair that one again, so that every step waits for the same number)
+    const unsigned st = smem_u + (unsigned)(slot * S_B);
+    const int last = (int)min(63L, a.V - 1 - a.v0 - (long)k * BK);
+    const char* const ap = (const char*)a.w + ((a.v0 + (long)k * BK) * E + e0) * 2;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      dma16u(ap, (unsigned)min(16 * wave + 4 * j + (lane >> 4), last) * wrow_b + a_chunk, st + (unsigned)((16 * wave + 4 * j) * PITCH));
+#pragma unroll
+    for (int j = 0; j < RB; ++j) dma16u((const char*)a.g + (long)k * RK_ROWB, bo[j], st + (unsigned)(A_B + (8 * RB * wave + 8 * j) * RK_ROWB));
+  };
+  f32x16 acc[RB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i) acc[i] = zero16();
+  const int j16 = lane & 15, jr = j16 >> 2, ka = (8 * g + jr) * PITCH + 32 * ((lane >> 4) & 1) + 8 * (j16 & 3) + 64 * (wave ^ jr);
+  if (nk > 0) {                                      // (a short last piece leaves parts without a pair)
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) issue(s, s);
+  }
+  int slot = 0, free = NS - 1;
+  for (int kt = 0; kt < nk; ++kt) {                  // (as in xent_few_bf16_kernel)
+    wait_vmcnt<NP * (NS - 2)>();
+    __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    wg_barrier();
+    asm volatile("" ::: "memory");
+    issue(kt + NS - 1, free);
+    const char* const st = smem + slot * S_B;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const char* const p = st + ka + 16 * q * PITCH;
+      const s16x4 lo = lds_read_tr(p), hi = lds_read_tr(p + 4 * PITCH);
+      typedef __attribute__((ext_vector_type(8))) short s16x8;
+      const bf16x8 av = __builtin_bit_cast(bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+      const int rd = l31 * RK_ROWB + 16 * ((2 * q + g) ^ perm_of(l31));
+#pragma unroll
+      for (int i = 0; i < RB; ++i) acc[i] = mfma32(av, *(const bf16x8*)(st + A_B + 32 * i * RK_ROWB + rd), acc[i]);
+    }
+    asm volatile("" ::: "memory");
+    free = slot;
+    slot = slot + 1 == NS ? 0 : slot + 1;
+  }
+  wait_vmcnt<0>();
+  asm volatile("" ::: "memory");
+  const long pitch = (long)n_ct * CT;
+#pragma unroll
+  for (int i = 0; i < RB; ++i) {
+    const int r = 32 * i + l31;
+    if (r < M) {
+      float* const to = a.dx_part + ((long)part * 64 + r) * pitch + e0 + 32 * wave + 4 * g;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 y = {acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
+        if (!a.first) y += *(const f32x4*)(to + 8 * q);
+        *(f32x4*)(to + 8 * q) = y;
+      }
+    }
+  }
+}
+
 // Sums of parts, 32 rows x 32 features a workgroup.  DX: of the listed tokens; 0 for the others.  DW_PARTS: of the piece's vocabulary.
 template <int MODE> __global__ void __launch_bounds__(256) xent_sum_bf16_kernel(XentArgs a, unsigned tiles) {
   const int M = MODE == DX ? a.head->count : (int)(a.v1 - a.v0), E = a.E, tid = threadIdx.x, n_ec = (E + 31) / 32;
   if (blockIdx.x < tiles) {
-    const int r = (int)(blockIdx.x / n_ec) * 32 + tid % 32, c = (int)(blockIdx.x % n_ec) * 32 + 4 * (tid / 32);
+    const bool rows = MODE == DX && a.own;             // (what xent_few_dx_bf16_kernel left)
+    const int r = (int)(blockIdx.x / n_ec) * 32 + (rows ? tid / 8 : tid % 32), c = (int)(blockIdx.x % n_ec) * 32 + 4 * (rows ? tid % 8 : tid / 32);
     if (r >= M || c >= E) return;
     const int tr = MODE == DX ? a.tile_rows : 128, n_ct = (E + T - 1) / T, rl = r % tr, cl = c % T;
-    const long tile = (long)(r / tr) * n_ct + c / T, step = (long)((M + tr - 1) / tr) * n_ct * tr * T;
+    const long tile = (long)(r / tr) * n_ct + c / T;
+    long step = (long)((M + tr - 1) / tr) * n_ct * tr * T;
     const int wave = rl / (tr / 2) * (NW / 2) + cl / WC, i = rl % (tr / 2) / 32, j = cl % WC / 32, q = cl % 32 / 8;
     const float* from = (MODE == DX ? a.dx_part : a.dw_part) + tile * (tr * T) + wave * (tr * T / NW) + ((j * (tr / 64) + i) * 4 + q) * 256 + (rl % 32 + 32 * (cl / 4 % 2)) * 4;
+    if (rows) {
+      const long pitch = (E + 127) / 128 * 128L;
+      from = a.dx_part + r * pitch + c;
+      step = 64 * pitch;
+    }
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     const int parts = MODE == DX ? a.head->parts : a.head->dw_parts;
     for (int p0 = 0; p0 < parts; p0 += 8) {              // (eight on their way at once)
@@ -1184,6 +1278,14 @@ template <int MODE, int RB, int NS, bool OWN> hipError_t launch_few(const XentAr
   xent_few_bf16_kernel<MODE, RB, NS, OWN><<<(unsigned)strip_grid(wgs), 256, bytes, s>>>(a);
   return hipGetLastError();
 }
+template <int RB, int NS> hipError_t launch_few_dx(const XentArgs& a, hipStream_t s) {
+  constexpr int bytes = NS * (BK * 256 + 32 * RB * RK_ROWB);
+  static SmemOnce once;
+  const hipError_t e = ensure_dynamic_lds((const void*)xent_few_dx_bf16_kernel<RB, NS>, bytes, &once);
+  if (e != hipSuccess) return e;
+  xent_few_dx_bf16_kernel<RB, NS><<<(unsigned)strip_grid(a.slots), 256, bytes, s>>>(a);
+  return hipGetLastError();
+}
 long up(long n, long by) { return (n + by - 1) / by; }
 // Whether tiles of 128 rows are the better ones for a product of `rows` x `cols` with `pairs` tile pairs: by the rounds of workgroups, a
 // tile's pairs at 1.55 us (128 rows: 0.85, where they take turns 1.05) and what a tile costs beside them, 6 us (3.5).  Statistics and gradient of 300
@@ -1311,6 +1413,11 @@ hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
   a.dw_tiles = (int)dw_tiles(std::min(a.piece, a.V), a.E, is_f32);
   a.tile = dx_edge(a.n, a.E, a.V, a.n_cu, is_f32);
   a.tile_rows = dx_rows(a.n, a.E, a.V, a.n_cu, is_f32);
+  if (a.own && !is_f32) {                            // (tiles of a quarter of the size that there is room for)
+    a.tile = 128;
+    a.tile_rows = 64;
+    a.slots = (int)std::max(up(a.E, 128), std::min(MOST_PARTS * up(a.E, 128), 2L * a.n_cu));
+  }
   if (!a.own) xent_list_kernel<<<1, 1024, 0, s>>>(a);
   a.first = 1;
   hipError_t e = hipGetLastError();
@@ -1323,6 +1430,7 @@ hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) {
       e = is_f32 ? f32_product<DW>(a, cols, a.E, f32_edge(cols, a.E, a.n_cu), s) : product<DW>(a, cols, a.E, up(a.n, BK), s);
     if (e == hipSuccess && a.dx) {
       e = is_f32 ? f32_product<DX>(a, a.n, a.E, a.tile, s)
+          : a.own ? a.n <= 32 ? launch_few_dx<1, 6>(a, s) : launch_few_dx<2, 6>(a, s)
                  : a.tile_rows == 128 ? launch_tiles<DX, 2>(a, strip_grid(a.slots), s) : launch_tiles<DX, 4>(a, strip_grid(a.slots), s);
       a.first = 0;
     }

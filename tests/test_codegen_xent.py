@@ -42,6 +42,6 @@ def test_tile_loop_moves_no_accumulator(mode, row_blocks):
 
 
 @pytest.mark.parametrize("name", ["xent_few_bf16_kernelILi0ELi1ELi6ELb1E", "xent_few_bf16_kernelILi0ELi2ELi3ELb0E", "xent_few_bf16_kernelILi1ELi2ELi6ELb1E",
-                                  "xent_few_bf16_kernelILi1ELi4ELi4ELb0E", "xent_f32_kernelILi0ELi128E", "xent_f32_kernelILi2ELi64E"])
+                                  "xent_few_bf16_kernelILi1ELi4ELi4ELb0E", "xent_few_dx_bf16_kernelILi2ELi6E", "xent_few_f32_kernelILi1E", "xent_f32_kernelILi0ELi128E", "xent_f32_kernelILi2ELi64E"])
 def test_no_spills(name):
     assert kernel(name)[1] == 0

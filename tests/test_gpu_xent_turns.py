@@ -125,3 +125,20 @@ def test_labels_outside_among_few_tokens(dtype, n):
     for name, t in (("loss", loss), ("lse", lse), ("dx", dx)):
         err = (t.double().cpu()[good] - torch.from_numpy(ref[name])[good]).abs()
         assert (err <= 1.02 * torch.from_numpy(tol[name])[good] + 1e-30).all(), name
+
+
+@pytest.mark.parametrize("dtype,n,E", [("bf16", 20, 64), ("bf16", 50, 192), ("bf16", 64, 1024), ("f32", 20, 40), ("bf16", 150, 64)])
+def test_few_tokens_piece_by_piece(dtype, n, E):
+    """Pieces of 2048 entries, of which the last has one: parts of dx without anything to add."""
+    V = 4097
+    args = inputs(n, E, V, dtype, 23, pad=8)
+    ref, tol = reference(*args, dtype)
+    check(run(*args), ref, tol, "whole")
+    f32 = dtype == "f32"
+    up = lambda v: (v + 255) // 256 * 256
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    edge = 64 if f32 else 256
+    rows = 64 if f32 else 128 if n <= 128 else 256
+    tiles = -(-n // rows) * -(-E // edge)
+    ws = 256 + 2 * up(4 * n) + up(8 * n) + max(tiles, min(64 * tiles, 2 * cus)) * rows * edge * 4 + (2048 + 64) * up(n) * (4 if f32 else 2)
+    check(run(*args, ws_bytes=ws), ref, tol, "pieces of 2048")
