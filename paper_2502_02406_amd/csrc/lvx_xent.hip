@@ -1322,8 +1322,8 @@ dim3 grid_of(long wgs) { return dim3((unsigned)std::min(wgs, MOST_WGS), (unsigne
 template <int MODE> hipError_t f32_product(const XentArgs& a, long rows, long cols, int edge, hipStream_t s) {
   const long wgs = strip_grid(MODE == DX ? (long)a.slots : MODE == DW_PARTS ? (long)a.dw_slots : up(rows, edge) * up(cols, edge));
   const dim3 grid = grid_of(wgs);
-  if (edge == 64) xent_f32_kernel<MODE, 64><<<grid, 256, 0, s>>>(a);
-  else xent_f32_kernel<MODE, 128><<<grid, 256, 0, s>>>(a);
+  if (edge == 64 || MODE == DW_PARTS) xent_f32_kernel<MODE, 64><<<grid, 256, 0, s>>>(a);
+  else if constexpr (MODE != DW_PARTS) xent_f32_kernel<MODE, 128><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int MODE> hipError_t logits(const XentArgs& a, int is_f32, hipStream_t s) {

@@ -142,3 +142,17 @@ def test_few_tokens_piece_by_piece(dtype, n, E):
     tiles = -(-n // rows) * -(-E // edge)
     ws = 256 + 2 * up(4 * n) + up(8 * n) + max(tiles, min(64 * tiles, 2 * cus)) * rows * edge * 4 + (2048 + 64) * up(n) * (4 if f32 else 2)
     check(run(*args, ws_bytes=ws), ref, tol, "pieces of 2048")
+
+
+@pytest.mark.parametrize("n,E,V", [(70, 36, 300), (10, 33, 500), (1400, 64, 100)])
+def test_f32_at_any_address(n, E, V):
+    args = inputs(n, E, V, "f32", 41)
+    ref, tol = reference(*args, "f32")
+    off = lambda t: torch.cat([t.new_zeros(1), t.reshape(-1)])[1:].view(t.shape)          # 4 bytes behind an allocation's start
+    x, w, labels, d = (off(t.contiguous()) for t in args)
+    assert x.data_ptr() % 16 == 4 and w.data_ptr() % 16 == 4
+    loss, lse, dx, dw = (off(torch.full(s, 5.0, device="cuda")) for s in ((n,), (n,), (n, E), (V, E)))
+    ws = torch.empty(B.lvx_xent_workspace_bytes(n, E, V, B.LVX_F32), dtype=torch.uint8, device="cuda")
+    B.lvx_xent_fwd(x, w, labels, loss, lse, ws)
+    B.lvx_xent_bwd(x, w, labels, lse, d, dx, dw, ws)
+    check((loss, lse, dx, dw), ref, tol, f"{n}x{E}x{V}")
