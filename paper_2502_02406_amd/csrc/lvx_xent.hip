@@ -1299,12 +1299,13 @@ bool low_tiles(long rows, long cols, long pairs, int n_cu) {
 // Rows of the tiles of logits of xent_few_bf16_kernel; 0: xent_bf16_kernel.  Up to 64 tokens there is one row of tiles.  With more, tiles of 64 x
 // 128 where all of them have a place at once: statistics of 664 tokens x 2496 features against 2171 34 -> 20 us, 130 x 3392 against 13376 74 -> 51,
 // 922 x 1280 against 3838 22 -> 17.5, 100 x 512 against 4000 10 -> 7.5; where they take turns, 300 x 256 against 20000 9.6 -> 11.5, 1024 x 512
-// against 8192 13 -> 17.5.  Up to 128 tokens of many features the copies are what counts, and every entry of the vocabulary is copied once: 128 x
-// 4096 against 32768 91 (xent_bf16_kernel), 68 (64 rows), 54 (128 rows); 100 x 1024 against 30000 20, 16, 17, against 10000 17, 11, 16.
+// against 8192 13 -> 17.5.  Up to 128 tokens of many features against a long vocabulary the copies are what counts, and every entry is copied
+// once: 128 x 4096 against 32768 91 (xent_bf16_kernel), 68 (64 rows), 54 (128 rows); 100 x 1024 against 30000 20, 16, 17, against 10000 17, 11,
+// 16; 95 x 2432 against 4096 19 (64 rows), 29 (128).
 // (GRAD: 64 or 128 tokens whatever their number: the contraction of dw runs over g's rows 64 at a time.)
 int few_rows(long n, long cols, long pairs, int n_cu) {
   const long ct = up(cols, 128);
-  if (n > 64 && n <= 128 && ct <= n_cu && pairs >= 32) return 128;
+  if (n > 64 && n <= 128 && ct <= n_cu && 2 * ct > n_cu && pairs >= 32) return 128;
   return n <= 64 || up(n, 64) * ct <= 2L * n_cu ? 64 : 0;
 }
 template <int MODE> hipError_t product(const XentArgs& a, long rows, long cols, long pairs, hipStream_t s) {

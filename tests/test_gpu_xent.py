@@ -85,7 +85,7 @@ def check(got, ref, tol, tag):
 
 
 BF16 = [(1, 64, 1, 0), (1, 64, 2, 0), (3, 64, 100, 8), (64, 128, 256, 0), (65, 64, 257, 0), (128, 192, 1000, 64), (129, 64, 511, 0), (200, 320, 777, 8),
-        (300, 512, 3001, 0), (257, 1024, 300, 0), (16, 256, 9000, 0), (33, 640, 1111, 0), (64, 128, 40000, 8), (128, 192, 700, 0), (100, 640, 1111, 8), (100, 2048, 900, 0), (300, 256, 20001, 0), (2, 64, 33000, 0), (700, 256, 20001, 0), (1300, 64, 129, 0)]
+        (300, 512, 3001, 0), (257, 1024, 300, 0), (16, 256, 9000, 0), (33, 640, 1111, 0), (64, 128, 40000, 8), (128, 192, 700, 0), (100, 640, 1111, 8), (100, 2048, 900, 0), (70, 2048, 16500, 0), (300, 256, 20001, 0), (2, 64, 33000, 0), (700, 256, 20001, 0), (1300, 64, 129, 0)]
 F32 = [(1, 1, 1, 0), (5, 33, 7, 3), (130, 100, 129, 0), (64, 64, 500, 0), (200, 257, 333, 1), (300, 40, 9000, 0), (1, 512, 3000, 0), (31, 130, 1000, 0), (33, 96, 700, 0), (64, 2048, 300, 0), (20, 29, 3001, 3)]
 
 
