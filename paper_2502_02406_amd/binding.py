@@ -351,8 +351,9 @@ def lvx_xattn_dq_finalize(p: lvx_problem, dq_accum, dq) -> None:
 def _token_strides(x):
     """(batch stride, token stride) of x [B, S, E]; with one batch the batch stride means nothing (a
     window of a longer token sequence reports the whole sequence's), so it is set to what the
-    entry points ask for: batches that follow each other."""
-    return (x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.stride(1)), x.stride(1)
+    entry points ask for: batches that follow each other.  Nor does the stride of a single token."""
+    ss = x.stride(1) if x.shape[0] * x.shape[1] > 1 else x.shape[2]
+    return (x.stride(0) if x.shape[0] > 1 else x.shape[1] * ss), ss
 
 
 def lvx_xattn_project(x, w, outs) -> None:
@@ -376,7 +377,7 @@ def lvx_xattn_project(x, w, outs) -> None:
 def lvx_xattn_project_bwd(x, w, d_outs, dx=None, dw=None) -> None:
     """d_outs: one or two tensors [B, H, S, D] (contiguous, dtype of x), the gradients of the heads
     that lvx_xattn_project made from x [B, S, E] and w [len(d_outs) * H * D, E].  dx (x's shape,
-    strides and dtype) is overwritten with the gradient of x; dw (w's shape, float32) has the
+    strides (but a single batch's) and dtype) is overwritten with the gradient of x; dw (w's shape, float32) has the
     gradient of w added to it."""
     if not x.is_cuda:
         raise RuntimeError("lvx_xattn_project_bwd needs device tensors")
@@ -390,7 +391,8 @@ def lvx_xattn_project_bwd(x, w, d_outs, dx=None, dw=None) -> None:
     assert tuple(w.shape) == (len(d_outs) * p.H * p.D, p.E)
     p.x_sb, p.x_ss = _token_strides(x)
     if dx is not None:
-        assert dx.shape == x.shape and dx.stride() == x.stride() and dx.dtype == x.dtype and dx.is_cuda
+        assert dx.shape == x.shape and dx.stride(2) == 1 and _token_strides(dx) == (p.x_sb, p.x_ss)
+        assert dx.dtype == x.dtype and dx.is_cuda
     if dw is not None:
         assert dw.shape == w.shape and dw.is_contiguous() and dw.dtype == torch.float32 and dw.is_cuda
     arr = (C.c_void_p * len(d_outs))(*[g.data_ptr() for g in d_outs])

@@ -221,6 +221,11 @@ class _Features:
         """The same features once more, bit for bit (t is not read where they are packed)."""
         return self.forward(t if self.packed is None else None, first, shape, weights)
 
+    def check_rows(self, t, name):
+        """The backward pass writes gradients whose rows follow each other, with the strides of the tokens that it reads."""
+        if self.packed is None and t is not None and not t.is_contiguous():
+            raise ValueError(f"backward: {name} has to be contiguous (a window of a wider tensor: packed layers do not read it again)")
+
     def start_backward(self):
         if self.norm is not None:
             self.dparam.zero_()
@@ -247,7 +252,8 @@ class RecomputeLayer:
 
     x [B, Sq, E] text tokens, y [B, Skv, E] visual tokens (B > 1: n_blocks must be 1, the
     projection entry points want the batches of a call to follow each other), wq [Hq D, E],
-    wkv [2 Hkv D, E] (W_K^T on top of W_V^T).  Only sequences C-ABI calls.
+    wkv [2 Hkv D, E] (W_K^T on top of W_V^T).  The forward pass reads x and y as windows of wider tensors too; the backward
+    pass asks for contiguous ones, where it reads them again (not where the layer keeps them packed).  Only sequences C-ABI calls.
 
     norm = "layer" or "rms": the projections read the norm of x and of y; forward and backward take the two norms'
     weights, and backward returns their gradients behind the others.
@@ -306,6 +312,8 @@ class RecomputeLayer:
         """(dx, dy in the input dtype, dW_Q, dW_KV float32) from x, y (None where the layer keeps them packed), (O, L) and dO alone;
         with norms followed by the gradients (float32, or None) of norm_x's gamma and beta and of norm_y's."""
         lp = self.loop
+        self.fx.check_rows(x, "x")
+        self.fy.check_rows(y, "y")
         feat_x = self.fx.again(x, 0, self.dx.shape, norm_x)
         B.lvx_xattn_project(feat_x, wq, [self.q])                  # Q again
         self.dwq.zero_()
@@ -319,8 +327,7 @@ class RecomputeLayer:
             B.lvx_xattn_bwd_visit(p, self.q, self.k, self.v, o, lse, d_o, None, lp.dq_accum, self.dk, self.dv, lp.ws, n == 0,
                                   last if n == self.n_blocks - 1 else None)
             dyb = self.dy[:, n * self.blk:(n + 1) * self.blk]
-            # (a single batch's stride means nothing, but has to be the same in a block's features and in its gradient)
-            B.lvx_xattn_project_bwd(feat, wkv, [self.dk, self.dv], dx=dyb.as_strided(feat.shape, feat.stride()), dw=self.dwkv)
+            B.lvx_xattn_project_bwd(feat, wkv, [self.dk, self.dv], dx=dyb, dw=self.dwkv)
             self.fy.backward(yb, n * self.blk, norm_y, dyb)
         B.lvx_xattn_project_bwd(feat_x, wq, [lp.dq], dx=self.dx, dw=self.dwq)
         self.fx.backward(x, 0, norm_x, self.dx)
