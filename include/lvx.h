@@ -343,7 +343,8 @@ lvx_status lvx_xent_fwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const
  * lse     what lvx_xent_fwd left for the same x, w and labels.
  * d_loss  device, [n] float32: the gradient of every token's loss (1 / number of labels for their mean); not read where the label
  *         is negative.
- * dx      `dtype`, x's strides, OVERWRITTEN (0 for tokens without a label); may not be x; NULL = not wanted.
+ * dx and dw may not lie in x or w, nor in each other (LVX_ERR_STRIDE; windows beside each other of one wider tensor do not).
+ * dx      `dtype`, x's strides, OVERWRITTEN (0 for tokens without a label); NULL = not wanted.
  * dw      `dtype`, [V, E], contiguous, OVERWRITTEN: unlike lvx_xattn_project_bwd's, every row of w is in one call only, and g is
  *         rounded to `dtype` before it is multiplied, which float32 sums would not undo; NULL = not wanted.  At least one must be given.
  * Sums are float32, in a fixed order: results repeat bit for bit. */

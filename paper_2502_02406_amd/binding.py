@@ -582,8 +582,8 @@ def lvx_xent_fwd(x, w, labels, loss, lse, workspace) -> None:
 
 
 def lvx_xent_bwd(x, w, labels, lse, d_loss, dx=None, dw=None, workspace=None) -> None:
-    """dx (x's shape, strides and type) and dw (w's) are overwritten with the gradients; either may be None.  lse: what lvx_xent_fwd left;
-    d_loss: the gradient of every token's loss."""
+    """dx (x's shape, strides and type) and dw (w's) are overwritten with the gradients; either may be None, and neither may lie in x or w.  lse:
+    what lvx_xent_fwd left; d_loss: the gradient of every token's loss."""
     where = "lvx_xent_bwd"
     if workspace is None or (dx is None and dw is None):
         raise ValueError(f"{where}: no workspace, or nothing asked for")

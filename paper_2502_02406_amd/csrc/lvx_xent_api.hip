@@ -11,6 +11,19 @@ constexpr size_t ALIGN = 256;
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 bool aligned(const void* p, size_t by) { return (uintptr_t)p % by == 0; }
 
+// Whether the `len_b` bytes at b meet one of n rows of `len_a` bytes, `pitch` apart, at a: row k does where `behind` < k pitch < `before`
+bool meet(int64_t a, int64_t n, int64_t pitch, int64_t len_a, int64_t b, int64_t len_b) {
+  const int64_t behind = b - a - len_a, before = b + len_b - a, k = behind < 0 ? 0 : behind / pitch + 1;
+  return k < n && k * pitch < before;
+}
+// Whether dx or dw lies in x or w, or one in the other (windows of one wider tensor beside each other do not)
+bool gradients_in_operands(const lvx_xent* p, int64_t el, const void* x, const void* w, const void* dx, const void* dw) {
+  const int64_t pitch = p->x_ss * el, row = p->E * el, vocab = p->V * row, xa = (int64_t)x, wa = (int64_t)w, dxa = (int64_t)dx, dwa = (int64_t)dw;
+  return (dx && (meet(xa - (p->n - 1) * pitch, 2 * p->n - 1, pitch, row, dxa, row) || meet(dxa, p->n, pitch, row, wa, vocab))) ||
+         (dw && (meet(wa, 1, vocab, vocab, dwa, vocab) || meet(xa, p->n, pitch, row, dwa, vocab))) ||
+         (dx && dw && meet(dxa, p->n, pitch, row, dwa, vocab));
+}
+
 lvx_status check_sizes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
   if (dtype != LVX_F32 && dtype != LVX_BF16) return LVX_ERR_DTYPE;
   if (n < 1 || E < 1 || V < 1 || n > (1 << 30) || V > (1 << 30) || E > (1 << 20)) return LVX_ERR_SHAPE;
@@ -112,6 +125,7 @@ lvx_status lvx_xent_bwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const
   const int64_t room = workspace_bytes > plan.g ? ((int64_t)((workspace_bytes - plan.g) / plan.row) - PAD) / 256 * 256 : 0;
   if (piece > room) piece = room;
   if (piece < 256) return LVX_ERR_WORKSPACE;
+  if (gradients_in_operands(p, dtype == LVX_F32 ? 4 : 2, x, w, dx, dw)) return LVX_ERR_STRIDE;
   a.piece = piece;
   a.g_pitch = piece + PAD;
   a.lse = lse; a.d_loss = d_loss; a.dx = dx; a.dw = dw;
