@@ -327,8 +327,8 @@ lvx_status lvx_norm_bwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const
  * aligned pointers and x_ss % 8 == 0; n and V are arbitrary.  LVX_F32 takes any E and alignment.  n * x_ss may not pass 2^31
  * (LVX_ERR_STRIDE): larger batches go in several calls.
  * workspace   of lvx_xent_workspace_bytes(n, E, V, dtype) (0: invalid sizes), for either pass; it also serves fewer tokens, fewer
- *         features and smaller vocabularies.  lvx_xent_bwd takes less, down to pieces of 256 entries of the vocabulary, and is slower;
- *         its sums are then cut, and rounded, in other places. */
+ *         features and smaller vocabularies, with the results of their own (more of any takes no fewer bytes).  Given less than its
+ *         own, down to pieces of 256 entries of the vocabulary, lvx_xent_bwd is slower, and its sums are cut, and rounded, in other places. */
 typedef struct {
   int64_t n, V;             /* tokens, entries of the vocabulary */
   int32_t E;                /* features */

@@ -238,6 +238,7 @@ long xent_dx_slots(long n, int E, long V, int n_cu, int is_f32);
 size_t xent_dx_bytes(long n, int E, long V, int n_cu, int is_f32);
 long xent_dw_slots(long n, int E, long cols, int n_cu, int is_f32);
 size_t xent_dw_bytes(long n, int E, long cols, int n_cu, int is_f32);
+size_t xent_dw_room(long n, int E, long V, int n_cu, int is_f32);
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s);
 

@@ -1357,6 +1357,10 @@ int dx_rows(long n, int E, long V, int n_cu, int is_f32) { return is_f32 ? dx_f3
 int dw_rows(int is_f32) { return is_f32 ? 64 : 128; }
 int dw_edge(int is_f32) { return is_f32 ? 64 : T; }
 long dw_tiles(long cols, int E, int is_f32) { return up(cols, dw_rows(is_f32)) * up(E, dw_edge(is_f32)); }
+// Whether the contraction of dw is better cut into parts: a tile pair's time (64 tokens) is 0.85 us, float32 1.6, and writing the parts, reading
+// them and the launch cost 12.  dw of 16384 tokens x 128 against 1000 191 -> 25 us, 5000 x 512 against 1500 68 -> 25, 2048 x 512 against 4000
+// 30 -> 27, float32 4000 x 256 against 1000 101 -> 37; where the rule keeps one part, 1024 x 1024 against 2000 17 -> 23.
+bool dw_parts_pay(long pairs, long parts, int is_f32) { return (is_f32 ? 1.6 : 0.85) * (pairs - pairs / parts) >= 12.0; }
 hipError_t dw_in_parts(const XentArgs& a, int is_f32, hipStream_t s) {
   const long cols = a.v1 - a.v0;
   const hipError_t e = is_f32 ? f32_product<DW_PARTS>(a, cols, a.E, 64, s) : launch_tiles<DW_PARTS, 2>(a, strip_grid(a.dw_slots), s);
@@ -1371,16 +1375,20 @@ hipError_t dw_in_parts(const XentArgs& a, int is_f32, hipStream_t s) {
 }
 }  // namespace
 
-// Tiles of sums of dw that a piece of `cols` columns takes; at most one for a compute unit, so that a workgroup has one.  0 where the tiles of the
-// product are as good: a tile pair's time (64 tokens) is 0.85 us, float32 1.6, and writing the parts, reading them and the launch cost 12.
-// dw of 16384 tokens x 128 against 1000 191 -> 25 us, 5000 x 512 against 1500 68 -> 25, 2048 x 512 against 4000 30 -> 27, float32 4000 x 256 against
-// 1000 101 -> 37; where the rule keeps one part, 1024 x 1024 against 2000 17 -> 23.
+// Tiles of sums of dw that a piece of `cols` columns takes; at most one for a compute unit, so that a workgroup has one.  0: it is not cut.
 long xent_dw_slots(long n, int E, long cols, int n_cu, int is_f32) {
   const long tiles = dw_tiles(cols, E, is_f32), pairs = up(n, BK), parts = std::min({(long)MOST_PARTS, pairs / 4, n_cu / 8 * 8 / tiles});
-  return parts < 2 || (is_f32 ? 1.6 : 0.85) * (pairs - pairs / parts) < 12.0 ? 0 : parts * tiles;
+  return parts < 2 || !dw_parts_pay(pairs, parts, is_f32) ? 0 : parts * tiles;
 }
 size_t xent_dw_bytes(long n, int E, long cols, int n_cu, int is_f32) {
   return sizeof(float) * dw_rows(is_f32) * dw_edge(is_f32) * xent_dw_slots(n, E, cols, n_cu, is_f32);
+}
+// Room for them, and for those of every problem with fewer tokens, features or entries, which may have parts where this one has none: no more tiles
+// than compute units, nor than this one's tiles in the most parts that its tokens allow.
+size_t xent_dw_room(long n, int E, long V, int n_cu, int is_f32) {
+  const long pairs = up(n, BK), parts = std::min((long)MOST_PARTS, pairs / 4);
+  if (parts < 2 || !dw_parts_pay(pairs, parts, is_f32)) return 0;
+  return sizeof(float) * dw_rows(is_f32) * dw_edge(is_f32) * std::min((long)(n_cu / 8 * 8), parts * dw_tiles(V, E, is_f32));
 }
 
 bool xent_bf16_supported(int E) { return E % BK == 0; }

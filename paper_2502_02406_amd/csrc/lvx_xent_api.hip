@@ -55,12 +55,23 @@ constexpr int64_t PAD = 64;
 // piece.  Pieces that the last-level cache (256 MB) holds gain nothing, and more of them have more last rounds of workgroups: passes with 128 MB,
 // 512 MB and 1 GiB, us: 5514 x 1024, V = 50021, 2200 labelled 1087, 943, 941; 16000 x 1024, V = 32000 4274, 3658, 3646; 4096 x 4096,
 // V = 131072 13050, 13130, 12860.
+constexpr size_t PIECE_BYTES = (size_t)1 << 30;
+constexpr int64_t LEAST_PIECE = 8192, MOST_PIECE = 1 << 18;
 int64_t piece_of(const Plan& p, int64_t V) {
-  int64_t piece = (int64_t)(((size_t)1 << 30) / p.row) / 256 * 256;
-  if (piece < 8192) piece = 8192;
-  if (piece > (1 << 18)) piece = 1 << 18;
+  int64_t piece = (int64_t)(PIECE_BYTES / p.row) / 256 * 256;
+  if (piece < LEAST_PIECE) piece = LEAST_PIECE;
+  if (piece > MOST_PIECE) piece = MOST_PIECE;
   const int64_t pieces = (V + piece - 1) / piece;      // (even ones)
   return ((V + pieces - 1) / pieces + 255) / 256 * 256;
+}
+// Room for a piece, and for a piece of every problem with fewer tokens or entries: even pieces get shorter where one more begins, and those of
+// fewer tokens longer, so theirs may be the larger ones.
+size_t piece_room(const Plan& p, int64_t V) {
+  size_t room = p.row * LEAST_PIECE;
+  if (room < PIECE_BYTES) room = PIECE_BYTES;
+  if (room > p.row * MOST_PIECE) room = p.row * MOST_PIECE;
+  const size_t all = p.row * ((V + 255) / 256 * 256);
+  return (room < all ? room : all) + p.row * PAD;
 }
 
 lvx_status xent_args(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, void* workspace,
@@ -93,8 +104,7 @@ extern "C" {
 size_t lvx_xent_workspace_bytes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
   if (check_sizes(n, E, V, dtype) != LVX_OK) return 0;
   const Plan p = plan_of(n, E, V, dtype);
-  const int64_t piece = piece_of(p, V);
-  const size_t bwd = align_up(p.g + (size_t)(piece + PAD) * p.row) + xent_dw_bytes(n, E, piece < V ? piece : V, device_cu_count(), dtype == LVX_F32);
+  const size_t bwd = align_up(p.g + piece_room(p, V)) + xent_dw_room(n, E, V, device_cu_count(), dtype == LVX_F32);
   return align_up(p.fwd > bwd ? p.fwd : bwd);
 }
 
