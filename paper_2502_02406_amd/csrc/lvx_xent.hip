@@ -15,10 +15,11 @@
 // No atomics: results repeat bit for bit.
 //
 // bf16 tiles of 256 x 256 and tile pairs of 64 contraction steps in two slots of 64 KB, as in the projections (lvx_project.hip,
-// lvx_project_bwd.hip), but of 8 waves, two on a SIMD, each 128 x 64 as 4 x 2 blocks in the accumulation registers: the tile loop is
-// no faster than that of 4 waves with 128 x 128 each (it reads a third more from LDS, and both run at what the chip's power allows), but
-// what stands before and behind it is: a tile with one pair 13.7 -> 10.6 us (statistics), 19.5 -> 16.9 (gradient), 300 tokens x 1024 x 50000,
-// 16 pairs, dw 64 -> 57.
+// lvx_project_bwd.hip), but of 8 waves, two on a SIMD, each 128 x 64 as 4 x 2 blocks in the accumulation registers.  Against 4 waves with
+// 128 x 128 each (which read a third less from LDS) this pays where tiles have few pairs, by what stands before and behind their loop, and
+// costs where they have many.  A tile with one pair 13.7 -> 10.6 us (statistics), 19.5 -> 16.9 (gradient), 300 tokens x 1024 x 50000, 16 pairs, dw
+// 64 -> 57; loss and gradients, in one session: 2206 x 1024 against 50021 (16 pairs) 959 (4 waves), 948 (8), 973 (8 that stay for their tiles,
+// as here), 2048 x 4096 against 32768 (64 pairs) 1783, 1802, 1833, 4096 x 4096 against 131072 13200, 13550, 13770.
 #include "lvx_internal.h"
 #include "lvx_mfma.h"
 #include "lvx_kv_ring.h"

@@ -53,8 +53,8 @@ Plan plan_of(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
 constexpr int64_t PAD = 64;
 // Columns of a piece of the vocabulary: a GiB of the logits' gradient, 8192 at least, since the sums of dx go through memory once a
 // piece.  Pieces that the last-level cache (256 MB) holds gain nothing, and more of them have more last rounds of workgroups: passes with 128 MB,
-// 512 MB and 1 GiB, us: 5514 x 1024, V = 50021, 2200 labelled 1087, 943, 941; 16000 x 1024, V = 32000 4274, 3658, 3646; 4096 x 4096,
-// V = 131072 13050, 13130, 12860.
+// 512 MB and 1 GiB, us, in one session: 5514 x 1024, V = 50021, 2200 labelled 1088, 999, 966; 16000 x 1024, V = 32000 4710, 4180, 3750;
+// 4096 x 4096, V = 131072 13880, 13840, 13790.
 constexpr size_t PIECE_BYTES = (size_t)1 << 30;
 constexpr int64_t LEAST_PIECE = 8192, MOST_PIECE = 1 << 18;
 int64_t piece_of(const Plan& p, int64_t V) {
