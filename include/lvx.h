@@ -10,7 +10,9 @@
  * after recomputing Q, K and V from the token features          lvx_xattn_project.
  * Around the layer stand the norms of its token features          lvx_norm_fwd,
  * the 8-bit form in which they are kept                           lvx_pack,
- * and the loss at the end of a training step                      lvx_xent_fwd.
+ * and the loss at the end of a training step                      lvx_xent_fwd,
+ * whose logits exist in tiles only; the backward pass keeps their gradient, up to 1 GiB
+ * of it at a time, in the workspace.
  *
  * General rules for every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The library
@@ -315,7 +317,8 @@ lvx_status lvx_norm_bwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const
                         const float* stats, const void* dy, void* dx, float* dgamma, float* dbeta, void* workspace,
                         size_t workspace_bytes, void* hip_stream);
 
-/* Softmax cross entropy of n tokens against a vocabulary of V entries, whose logits z = x w^T are never kept:
+/* Softmax cross entropy of n tokens against a vocabulary of V entries, whose logits z = x w^T are never kept (they are made twice, and their
+ * gradient lies in the workspace piece by piece of the vocabulary):
  *     lse[i] = ln sum_v exp z[i, v],   loss[i] = lse[i] - z[i, labels[i]].
  * x       device, n rows of E features of `dtype`, x_ss elements apart.
  * w       device, [V, E] of `dtype`, contiguous: one row of weights per entry, the layout of lvx_xattn_project's w.
@@ -327,8 +330,10 @@ lvx_status lvx_norm_bwd(const lvx_norm* p, lvx_dtype dtype, const void* x, const
  * aligned pointers and x_ss % 8 == 0; n and V are arbitrary.  LVX_F32 takes any E and alignment.  n * x_ss may not pass 2^31
  * (LVX_ERR_STRIDE): larger batches go in several calls.
  * workspace   of lvx_xent_workspace_bytes(n, E, V, dtype) (0: invalid sizes), for either pass; it also serves fewer tokens, fewer
- *         features and smaller vocabularies, with the results of their own (more of any takes no fewer bytes).  Given less than its
- *         own, down to pieces of 256 entries of the vocabulary, lvx_xent_bwd is slower, and its sums are cut, and rounded, in other places. */
+ *         features and smaller vocabularies, with the results of their own (more of any takes no fewer bytes).  Most of it is the
+ *         logits' gradient of a piece of the vocabulary: all n x V of it up to 1 GiB, or 8192 entries where these are more.  Given
+ *         less than its own, down to pieces of 256 entries of the vocabulary, lvx_xent_bwd is slower, and its sums are cut, and
+ *         rounded, in other places. */
 typedef struct {
   int64_t n, V;             /* tokens, entries of the vocabulary */
   int32_t E;                /* features */

@@ -259,7 +259,11 @@ class RecomputeLayer:
     weights, and backward returns their gradients behind the others.
     packed: the layer keeps x and y in 8 bits (33 / 64 of their bf16 size) and the caller need not: the forward pass works from
     the values that these stand for, so what the backward pass makes again from them, x and y None, is the forward
-    pass's bit for bit.  The gradients are those with respect to these values."""
+    pass's bit for bit.  The gradients are those with respect to these values.
+
+    With norm or packed the object also owns room for the features of x and of one block of y that the projections read (with n_blocks = 1: of
+    all of y), in either case dx and dy.  What packing saves is the caller's copy of x and y, where nobody else needs it: one such object a layer
+    keeps 33 / 64 of a copy each, and layers that read the same y may share the caller's one copy instead."""
 
     def __init__(self, Bsz, Sq, Skv, E, Hq, Hkv, D, dtype: torch.dtype, n_blocks: int = 1,
                  softmax_scale: float = 0.0, device: str = "cuda", norm: Optional[str] = None, packed: bool = False,
