@@ -356,6 +356,81 @@ lvx_status lvx_xent_fwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const
 lvx_status lvx_xent_bwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, const float* lse,
                         const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- at either end of a step: token features from a table, and losses of whole sequences ---- */
+
+/* Embedding lookup of n tokens in a table of V rows of E features:
+ *     y[i, f] = scale * table[ids[i], f].
+ * table  device, [V, E] of `dtype`, contiguous: the layout of lvx_xent_fwd's w, which it may be.
+ * ids    device, [n] int64.  A negative id (padding): y's row is 0, and the token takes no part in the gradient.  V or more: y's row is
+ *        NaN, and the gradient goes without the token.
+ * y      device, `dtype`, rows y_ss elements apart, overwritten (one rounding).
+ * Any alignment that the types have, any width, any stride of at least E.  y may not lie in the table (LVX_ERR_STRIDE).  No workspace. */
+typedef struct {
+  int64_t n, V;             /* tokens, rows of the table; up to 2^28 */
+  int32_t E;                /* features */
+  float scale;
+  int64_t y_ss;             /* elements from one row of y (and d_y) to the next */
+} lvx_embed;
+lvx_status lvx_embed_fwd(const lvx_embed* p, lvx_dtype dtype, const void* table, const int64_t* ids, void* y, void* hip_stream);
+
+/* Its gradient with respect to the table,
+ *     d_table[v, f] = scale * sum over the tokens i with ids[i] = v of d_y[i, f].
+ * d_y      like y; what belongs to tokens without a row (NaN included) is not read.  May not lie in d_table.
+ * d_table  device, [V, E] of `dtype`, contiguous.  accumulate == 0: OVERWRITTEN, rows without tokens with 0.  Otherwise ADDED TO, with one
+ *          rounding of the sum to `dtype`, and rows without tokens are left alone: what lvx_xent_bwd wrote as dw of the same weights.
+ * Sums are float32, in a fixed order (the tokens' order, in pieces): results repeat bit for bit.
+ * workspace  of lvx_embed_workspace_bytes(n, E, V) (0: invalid sizes); it also serves fewer tokens, features and rows. */
+size_t lvx_embed_workspace_bytes(int64_t n, int32_t E, int64_t V);
+lvx_status lvx_embed_bwd(const lvx_embed* p, lvx_dtype dtype, const void* d_y, const int64_t* ids, void* d_table, int accumulate,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Losses of sequences from their tokens' negative log likelihoods nll = lse - z[label], what lvx_xent_fwd leaves as loss, and d_nll, what
+ * lvx_xent_bwd takes as d_loss.
+ * nll, ref, old  device, [n] float32: under the policy that is trained, under the reference, and under the one that gave the answers.
+ * labels   device, [n] int64.  A negative label: the token takes no part, what the other tensors hold there (NaN included) reaches nothing, and
+ *          d_nll is 0 there.
+ * first    device, int64: sequence s has the tokens first[s] .. first[s + 1] - 1; rising, within 0 .. n (values outside are taken
+ *          as the nearer end, and a sequence that ends before it begins as empty; results of others are then undefined, but nothing outside
+ *          the tensors is read or written).  Tokens of no sequence: d_nll is left as it is.
+ * d_loss, d_nll  device, [S] and [n] float32, overwritten; both NULL: only the loss is wanted.  d_nll may be nll.
+ * Sums and what hangs on them are float64, in a fixed order; results are rounded once, gradients of a mean twice.
+ * workspace  of lvx_preference_workspace_bytes(n, S), lvx_policy_workspace_bytes(n, S) (0: invalid sizes), which also serve less.
+ *
+ * Preference loss of S pairs: sequences 0 .. S - 1 are the chosen ones, S .. 2 S - 1 the rejected ones, first has 2 S + 1 entries.  With
+ * m = sum over a sequence's labelled tokens of (ref - nll), of the chosen one less that of the rejected one, and h = beta m:
+ *     LVX_PREF_LOGISTIC  loss = (1 - smoothing) ln(1 + exp(-h)) + smoothing ln(1 + exp(h))
+ *     LVX_PREF_HINGE     loss = max(0, 1 - h)
+ *     LVX_PREF_SQUARE    loss = (m - 1 / (2 beta))^2
+ * ref may be NULL (0).  loss, margin: device, [S] float32, overwritten (margin: m; may be NULL). */
+typedef enum { LVX_PREF_LOGISTIC = 0, LVX_PREF_HINGE = 1, LVX_PREF_SQUARE = 2 } lvx_pref_form;
+typedef struct {
+  int64_t n, S;             /* tokens (up to 2^30), pairs (up to 2^21) */
+  int32_t form;             /* lvx_pref_form */
+  double beta;              /* > 0 */
+  double smoothing;         /* 0 .. 1, of LVX_PREF_LOGISTIC; otherwise 0 */
+} lvx_pref;
+size_t lvx_preference_workspace_bytes(int64_t n, int64_t S);
+lvx_status lvx_preference(const lvx_pref* p, const float* nll, const float* ref, const int64_t* labels, const int64_t* first, float* loss,
+                          float* margin, const float* d_loss, float* d_nll, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Clipped policy loss of S sequences (first has S + 1 entries), with r = exp(old - nll), d = nll - ref and the advantage A of the sequence or token:
+ *     l = -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A) + beta (exp(d) - 1 - d),
+ * summed over a sequence's labelled tokens or (mean) their mean; 0 of none.  The gradient of a clipped token's first part is 0.
+ * ref      NULL where beta is 0.
+ * adv      device, float32: [S], or (per_token) [n].
+ * loss     device, [S] float32, overwritten.
+ * stats    device, [S, 3] float32, overwritten, or NULL: the number of labelled tokens, the share of them whose ratio is clipped, and their mean of
+ *          exp(d) - 1 - d (0 where beta is 0). */
+typedef struct {
+  int64_t n, S;             /* tokens (up to 2^30), sequences (up to 2^21) */
+  int32_t mean, per_token;
+  double clip_low, clip_high, beta;       /* each >= 0 */
+} lvx_clip;
+size_t lvx_policy_workspace_bytes(int64_t n, int64_t S);
+lvx_status lvx_policy(const lvx_clip* p, const float* nll, const float* old, const float* ref, const float* adv, const int64_t* labels,
+                      const int64_t* first, float* loss, float* stats, const float* d_loss, float* d_nll, void* workspace,
+                      size_t workspace_bytes, void* hip_stream);
+
 /* Human-readable name of a status code (static storage). */
 const char* lvx_strerror(lvx_status s);
 

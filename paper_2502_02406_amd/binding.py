@@ -28,7 +28,9 @@ LVX_STATIC_SCRATCH_BYTES = 64 << 20
 EXPORTS = ("lvx_xattn_workspace_bytes", "lvx_xattn_fwd", "lvx_xattn_fwd_static", "lvx_xattn_fwd_merge", "lvx_xattn_fwd_merge_last", "lvx_xattn_merge", "lvx_xattn_bwd",
            "lvx_xattn_bwd_stages", "lvx_xattn_bwd_visit", "lvx_xattn_bwd_error_word", "lvx_xattn_dq_finalize", "lvx_xattn_project", "lvx_xattn_project_bwd",
            "lvx_pack", "lvx_unpack", "lvx_norm_fwd", "lvx_norm_workspace_bytes", "lvx_norm_bwd",
-           "lvx_xent_workspace_bytes", "lvx_xent_fwd", "lvx_xent_bwd", "lvx_strerror")
+           "lvx_xent_workspace_bytes", "lvx_xent_fwd", "lvx_xent_bwd",
+           "lvx_embed_fwd", "lvx_embed_workspace_bytes", "lvx_embed_bwd",
+           "lvx_preference_workspace_bytes", "lvx_preference", "lvx_policy_workspace_bytes", "lvx_policy", "lvx_strerror")
 
 
 class LvxError(RuntimeError):
@@ -63,6 +65,19 @@ class lvx_norm(C.Structure):
 
 class lvx_xent(C.Structure):
     _fields_ = [("n", C.c_int64), ("V", C.c_int64), ("E", C.c_int32), ("x_ss", C.c_int64)]
+
+
+class lvx_embed(C.Structure):
+    _fields_ = [("n", C.c_int64), ("V", C.c_int64), ("E", C.c_int32), ("scale", C.c_float), ("y_ss", C.c_int64)]
+
+
+class lvx_pref(C.Structure):
+    _fields_ = [("n", C.c_int64), ("S", C.c_int64), ("form", C.c_int32), ("beta", C.c_double), ("smoothing", C.c_double)]
+
+
+class lvx_clip(C.Structure):
+    _fields_ = [("n", C.c_int64), ("S", C.c_int64), ("mean", C.c_int32), ("per_token", C.c_int32), ("clip_low", C.c_double),
+                ("clip_high", C.c_double), ("beta", C.c_double)]
 
 
 class lvx_packed(C.Structure):
@@ -134,6 +149,14 @@ def load() -> C.CDLL:
         lib.lvx_xent_fwd.restype = lib.lvx_xent_bwd.restype = C.c_int
         lib.lvx_xent_fwd.argtypes = [C.POINTER(lvx_xent), C.c_int] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
         lib.lvx_xent_bwd.argtypes = [C.POINTER(lvx_xent), C.c_int] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
+        lib.lvx_embed_workspace_bytes.restype = lib.lvx_preference_workspace_bytes.restype = lib.lvx_policy_workspace_bytes.restype = C.c_size_t
+        lib.lvx_embed_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int64]
+        lib.lvx_preference_workspace_bytes.argtypes = lib.lvx_policy_workspace_bytes.argtypes = [C.c_int64, C.c_int64]
+        lib.lvx_embed_fwd.restype = lib.lvx_embed_bwd.restype = lib.lvx_preference.restype = lib.lvx_policy.restype = C.c_int
+        lib.lvx_embed_fwd.argtypes = [C.POINTER(lvx_embed), C.c_int] + [C.c_void_p] * 4
+        lib.lvx_embed_bwd.argtypes = [C.POINTER(lvx_embed), C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.lvx_preference.argtypes = [C.POINTER(lvx_pref)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
+        lib.lvx_policy.argtypes = [C.POINTER(lvx_clip)] + [C.c_void_p] * 11 + [C.c_size_t, C.c_void_p]
         lib.lvx_strerror.restype = C.c_char_p
         lib.lvx_strerror.argtypes = [C.c_int]
         _lib = lib
@@ -596,3 +619,115 @@ def lvx_xent_bwd(x, w, labels, lse, d_loss, dx=None, dw=None, workspace=None) ->
     _check(load().lvx_xent_bwd(C.byref(p), dtype_code(x.dtype), x.data_ptr(), w.data_ptr(), labels.data_ptr(), lse.data_ptr(), d_loss.data_ptr(),
                                dx.data_ptr() if dx is not None else None, dw.data_ptr() if dw is not None else None,
                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), s), where)
+
+
+# ---- at either end of a step: token features from a table, losses of whole sequences ----
+
+def lvx_embed_workspace_bytes(n: int, E: int, V: int) -> int:
+    return int(load().lvx_embed_workspace_bytes(n, E, V))
+
+
+def _embed_struct(where, table, ids, y, scale):
+    n, E, y_ss = _token_rows(y, "y")
+    if table.dim() != 2 or table.shape[1] != E or table.dtype != y.dtype or not table.is_contiguous():
+        raise ValueError(f"{where}: the table has to be [V, {E}] of the rows' type, contiguous")
+    if ids.numel() != n or ids.dtype != torch.int64 or not ids.is_contiguous():
+        raise ValueError(f"{where}: ids have to be int64 [{n}], contiguous")
+    return lvx_embed(n, table.shape[0], E, scale, y_ss)
+
+
+def lvx_embed_fwd(table, ids, y, scale: float = 1.0) -> None:
+    """y ([n, E] or [B, S, E]) is overwritten with scale times the rows ids (int64) of table [V, E]; 0 for a negative id."""
+    s = _on_device("lvx_embed_fwd", table, ids, y)
+    p = _embed_struct("lvx_embed_fwd", table, ids, y, scale)
+    _check(load().lvx_embed_fwd(C.byref(p), dtype_code(y.dtype), table.data_ptr(), ids.data_ptr(), y.data_ptr(), s), "lvx_embed_fwd")
+
+
+def lvx_embed_bwd(d_y, ids, d_table, workspace, scale: float = 1.0, accumulate: bool = False) -> None:
+    """d_table [V, E] is overwritten with the gradient of the table, from d_y ([n, E] or [B, S, E]), or has it added (accumulate)."""
+    w = "lvx_embed_bwd"
+    s = _on_device(w, d_y, ids, d_table, workspace)
+    p = _embed_struct(w, d_table, ids, d_y, scale)
+    if not workspace.is_contiguous():
+        raise ValueError(f"{w}: the workspace has to be contiguous")
+    _check(load().lvx_embed_bwd(C.byref(p), dtype_code(d_y.dtype), d_y.data_ptr(), ids.data_ptr(), d_table.data_ptr(), int(accumulate),
+                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), s), w)
+
+
+LVX_PREF_FORMS = {"logistic": 0, "hinge": 1, "square": 2}
+
+
+def lvx_preference_workspace_bytes(n: int, S: int) -> int:
+    return int(load().lvx_preference_workspace_bytes(n, S))
+
+
+def lvx_policy_workspace_bytes(n: int, S: int) -> int:
+    return int(load().lvx_policy_workspace_bytes(n, S))
+
+
+def _floats(where, name, t, *numbers):
+    """t (float32, contiguous) has one of these numbers of elements."""
+    if t is not None and (t.numel() not in numbers or t.dtype != torch.float32 or not t.is_contiguous()):
+        raise ValueError(f"{where}: {name} has to be float32, contiguous, of {' or '.join(map(str, numbers))} elements")
+
+
+def _sequences(where, tokens, labels, first, d_loss, d_nll, workspace):
+    """(tokens, sequences); tokens: the float32 tensors of one value a token, by name."""
+    n = labels.numel()
+    if labels.dtype != torch.int64 or not labels.is_contiguous():
+        raise ValueError(f"{where}: labels have to be int64, contiguous")
+    if first.dim() != 1 or first.dtype != torch.int64 or not first.is_contiguous():
+        raise ValueError(f"{where}: first has to be int64, one dimension, contiguous")
+    if (d_loss is None) != (d_nll is None):
+        raise ValueError(f"{where}: d_loss and d_nll, both or neither")
+    for name, t in tokens:
+        _floats(where, name, t, n)
+    _floats(where, "d_nll", d_nll, n)
+    if not workspace.is_contiguous():
+        raise ValueError(f"{where}: the workspace has to be contiguous")
+    return n, first.numel() - 1
+
+
+def lvx_preference(nll, ref, labels, first, loss, margin=None, d_loss=None, d_nll=None, workspace=None, form: str = "logistic",
+                   beta: float = 0.1, smoothing: float = 0.0) -> None:
+    """loss and margin (float32 [S]; margin may be None) are overwritten with the preference losses of S pairs of sequences, d_nll (float32 [n])
+    with the gradient of sum(loss * d_loss).  Sequence s has the tokens first[s] .. first[s + 1] - 1 (int64 [2 S + 1]); the first S are the
+    chosen ones.  nll and ref (None: 0): the tokens' negative log likelihoods; tokens with a negative label take no part."""
+    w = "lvx_preference"
+    if workspace is None:
+        raise ValueError(f"{w}: no workspace")
+    s = _on_device(w, nll, ref, labels, first, loss, margin, d_loss, d_nll, workspace)
+    n, count = _sequences(w, (("nll", nll), ("ref", ref)), labels, first, d_loss, d_nll, workspace)
+    if count < 2 or count % 2 != 0:
+        raise ValueError(f"{w}: first has to have 2 S + 1 entries")
+    for name, t in (("loss", loss), ("margin", margin), ("d_loss", d_loss)):
+        _floats(w, name, t, count // 2)
+    if form not in LVX_PREF_FORMS:
+        raise ValueError(f"{w}: form is one of {', '.join(LVX_PREF_FORMS)}")
+    p = lvx_pref(n, count // 2, LVX_PREF_FORMS[form], beta, smoothing)
+    at = lambda t: t.data_ptr() if t is not None else None
+    _check(load().lvx_preference(C.byref(p), at(nll), at(ref), at(labels), at(first), at(loss), at(margin), at(d_loss), at(d_nll), at(workspace),
+                                 workspace.numel() * workspace.element_size(), s), w)
+
+
+def lvx_policy(nll, old, ref, adv, labels, first, loss, stats=None, d_loss=None, d_nll=None, workspace=None, clip=(0.2, 0.2), beta: float = 0.0,
+               mean: bool = True) -> None:
+    """loss (float32 [S]) and stats (float32 [S, 3], or None: labelled tokens, share of clipped ones, mean divergence) are overwritten with the
+    clipped policy losses of S sequences (first: int64 [S + 1]), d_nll (float32 [n]) with the gradient of sum(loss * d_loss).  adv: an advantage a
+    sequence [S] or (any other number of elements) a token [n].  clip: a ratio's room below and above 1; beta: weight of the divergence from ref
+    (which may be None without it); mean: over a sequence's labelled tokens, otherwise their sum."""
+    w = "lvx_policy"
+    if workspace is None:
+        raise ValueError(f"{w}: no workspace")
+    s = _on_device(w, nll, old, ref, adv, labels, first, loss, stats, d_loss, d_nll, workspace)
+    n, count = _sequences(w, (("nll", nll), ("old", old), ("ref", ref)), labels, first, d_loss, d_nll, workspace)
+    if count < 1:
+        raise ValueError(f"{w}: first has to have S + 1 entries")
+    for name, t, numbers in (("loss", loss, (count,)), ("stats", stats, (3 * count,)), ("d_loss", d_loss, (count,)), ("adv", adv, (count, n))):
+        _floats(w, name, t, *numbers)
+    if ref is None and beta != 0.0:
+        raise ValueError(f"{w}: a divergence needs ref")
+    p = lvx_clip(n, count, int(mean), int(adv.numel() != count), clip[0], clip[1], beta)
+    at = lambda t: t.data_ptr() if t is not None else None
+    _check(load().lvx_policy(C.byref(p), at(nll), at(old), at(ref), at(adv), at(labels), at(first), at(loss), at(stats), at(d_loss), at(d_nll),
+                             at(workspace), workspace.numel() * workspace.element_size(), s), w)

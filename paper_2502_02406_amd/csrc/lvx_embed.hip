@@ -1,0 +1,541 @@
+// Rows of a table for token ids, scaled, and the table's gradient:
+//
+//   y_i = scale table[id_i],   d_table[v] = (what is there) + scale sum over i with id_i = v of d_y_i
+//
+// Both are bound by memory.  Forward: a team of threads for a row, 8 elements each.  Backward: the tokens are sorted by id, equal ids in the
+// order of the tokens (a stable sort by digits), and sums run over chunks of the sorted tokens: an id that a chunk has for itself is
+// finished there, one that goes on in the next chunk leaves a float32 sum a chunk, which a last launch adds up in the order of the
+// chunks.  However often an id occurs, its rows are shared by as many workgroups as there are chunks.  No float atomics: results repeat bit for bit.
+#include "lvx_internal.h"
+#include "lvx_mfma.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace lvx {
+
+namespace {
+
+constexpr int V8 = 8;                  // elements a thread takes of a row
+typedef u32x4 __attribute__((aligned(2))) u32x4_any2;
+typedef u32x4 __attribute__((aligned(4))) u32x4_any4;
+constexpr int chunks8(int E) { return (E + V8 - 1) / V8; }
+// Threads of a team (a power of two, 256 at most): as many as a row has pieces of 8 elements.
+int team_log(int E) {
+  int l = 0;
+  while (l < 8 && (1 << l) < chunks8(E)) ++l;
+  return l;
+}
+
+// 8 elements of a row from element e on, as they lie in memory, of which `there` exist (0 for the others)
+template <typename T> struct Piece;
+template <> struct Piece<__bf16> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const __bf16* p, int there) {
+    w = u32x4{0u, 0u, 0u, 0u};
+    if (there >= V8) {
+      w = *(const u32x4_any2*)p;
+    } else {
+#pragma unroll
+      for (int k = 0; k < V8 - 1; ++k)
+        if (k < there) w[k / 2] |= (unsigned)((const uint16_t*)p)[k] << (16 * (k % 2));
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
+  static __device__ __forceinline__ void store(__bf16* p, int there, const float (&v)[V8]) {
+    if (there >= V8) {
+      *(u32x4_any2*)p = u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+    } else {
+#pragma unroll
+      for (int k = 0; k < V8 - 1; ++k)
+        if (k < there) p[k] = (__bf16)v[k];
+    }
+  }
+};
+template <> struct Piece<float> {
+  u32x4 w[2];
+  __device__ __forceinline__ void load(const float* p, int there) {
+    w[0] = w[1] = u32x4{0u, 0u, 0u, 0u};
+    if (there >= V8) {
+      w[0] = ((const u32x4_any4*)p)[0];
+      w[1] = ((const u32x4_any4*)p)[1];
+    } else {
+#pragma unroll
+      for (int k = 0; k < V8 - 1; ++k)
+        if (k < there) w[k / 4][k % 4] = ((const uint32_t*)p)[k];
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i / 4][i % 4]); }
+  static __device__ __forceinline__ void store(float* p, int there, const float (&v)[V8]) {
+    if (there >= V8) {
+      ((u32x4_any4*)p)[0] = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+      ((u32x4_any4*)p)[1] = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
+    } else {
+#pragma unroll
+      for (int k = 0; k < V8 - 1; ++k)
+        if (k < there) p[k] = v[k];
+    }
+  }
+};
+
+// ---- forward: ROWS rows of a team on their way at once ----
+constexpr int ROWS = 4;
+template <typename T> __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a, int tl) {
+  const int E = a.E, e = (((int)blockIdx.y << tl) + (threadIdx.x & ((1 << tl) - 1))) * V8, there = E - e;
+  if (there <= 0) return;
+  const long teams = 256 >> tl;
+  for (long i0 = (long)blockIdx.x * (teams * ROWS) + (threadIdx.x >> tl); i0 < a.n; i0 += (long)gridDim.x * (teams * ROWS)) {
+    long id[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) id[k] = a.ids[min(i0 + k * teams, a.n - 1)];
+    Piece<T> x[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) x[k].load((const T*)a.table + min(max(id[k], 0L), a.V - 1) * E + e, there);
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const long i = i0 + k * teams;
+      if (i >= a.n) break;
+      float v[V8];
+#pragma unroll
+      for (int j = 0; j < V8; ++j) v[j] = id[k] < 0 ? 0.f : id[k] < a.V ? x[k][j] * a.scale : __builtin_nanf("");
+      Piece<T>::store((T*)a.y + i * a.y_ss + e, there, v);
+    }
+  }
+}
+
+// ---- backward: the sort ----
+
+constexpr int SORT_WG = 1024, SORT_WAVES = SORT_WG / 64;
+struct Sort { int bits, passes; };                   // bits of a digit, digits of an id
+inline Sort sort_of(long V) {
+  int bits = 1;
+  while (bits < 62 && (1L << bits) < V) ++bits;
+  const int passes = (bits + EMBED_DIGIT_BITS - 1) / EMBED_DIGIT_BITS;
+  return {(bits + passes - 1) / passes, passes};
+}
+
+// The rank of every token among those of its wave with the same digit, in order: ROUNDS x 64 tokens a wave, `dig` < 0: none.  cnt[digit]: the
+// wave's counts, which start at 0.
+template <int ROUNDS> __device__ __forceinline__ void rank_in_wave(const int (&dig)[ROUNDS], int (&rank)[ROUNDS], int* cnt, int bits) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    unsigned long long same = __ballot(dig[r] >= 0);
+    for (int b = 0; b < bits; ++b) {
+      const bool one = (dig[r] >> b) & 1;
+      const unsigned long long ones = __ballot(one);
+      same &= one ? ones : ~ones;
+    }
+    const int below = __popcll(same & ((1ull << lane) - 1));
+    int at = 0;
+    if (dig[r] >= 0 && below == 0) at = atomicAdd(&cnt[dig[r]], __popcll(same));
+    rank[r] = __shfl(at, dig[r] >= 0 ? __ffsll(same) - 1 : lane) + below;
+  }
+}
+// Exclusive sums of x over the workgroup's threads; *total: of all.  `at`: SORT_WAVES numbers of LDS.
+__device__ __forceinline__ int exclusive_sum(int x, int* at, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int upto = x;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int y = __shfl_up(upto, o);
+    upto += lane >= o ? y : 0;
+  }
+  if (lane == 63) at[wave] = upto;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int w = 0; w < SORT_WAVES; ++w) {
+    const int y = at[w];
+    before += w < wave ? y : 0;
+    all += y;
+  }
+  __syncthreads();
+  *total = all;
+  return before + upto - x;
+}
+// LDS of the sort: counts [waves][digits], where every digit starts [digits], exclusive_sum's [waves]
+inline int sort_lds(int bits) { return (int)sizeof(int) * ((SORT_WAVES + 1) * (1 << bits) + SORT_WAVES); }
+// Turns the waves' counts of a digit (thread t: digit t) into where the wave's first one stands among all of the workgroup's; returns how many there are.
+__device__ __forceinline__ int counts_to_starts(int* cnt, int digits) {
+  int run = 0;
+  if ((int)threadIdx.x < digits)
+    for (int w = 0; w < SORT_WAVES; ++w) {
+      const int c = cnt[w * digits + threadIdx.x];
+      cnt[w * digits + threadIdx.x] = run;
+      run += c;
+    }
+  return run;
+}
+__device__ __forceinline__ void clear_counts(int* cnt, int digits) {
+  for (int i = threadIdx.x; i < SORT_WAVES * digits; i += SORT_WG) cnt[i] = 0;
+}
+// The table's rows set to 0, in whole (of `elements`): workgroup `wg` of `wgs`.
+template <typename T> __device__ __forceinline__ void clear_table(T* p, long elements, long wg, long wgs) {
+  // (up to the first 16-byte boundary, and behind the last one, by single elements)
+  const long head = min(elements, (long)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T))), vecs = (elements - head) * (long)sizeof(T) / 16;
+  u32x4* const v = (u32x4*)(p + head);
+  for (long i = wg * SORT_WG + threadIdx.x; i < vecs; i += wgs * SORT_WG) v[i] = u32x4{0u, 0u, 0u, 0u};
+  const long tail = head + vecs * (16 / (long)sizeof(T));
+  if (wg == 0) {
+    if ((long)threadIdx.x < head) p[threadIdx.x] = (T)0.f;
+    if (tail + threadIdx.x < elements) p[tail + threadIdx.x] = (T)0.f;
+  }
+}
+
+// All digits by one workgroup, for up to ONE_WG tokens; the other workgroups clear the table meanwhile (rows that tokens have are written again
+// behind it).
+constexpr int ONE_ROUNDS = 8, ONE_WG = SORT_WG * ONE_ROUNDS;
+inline int one_lds(int bits, long n) { return sort_lds(bits) + 2 * (int)sizeof(int) * (int)((n + SORT_WG - 1) / SORT_WG * SORT_WG); }
+template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_kernel(EmbedArgs a, int bits, int passes) {
+  if (blockIdx.x > 0) {
+    clear_table((T*)a.d_table, a.V * a.E, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
+  extern __shared__ __attribute__((aligned(16))) int sort_mem[];
+  const int digits = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int* const cnt = sort_mem;
+  int* const start = cnt + SORT_WAVES * digits;
+  int* const sums = start + digits;
+  int* const skey = sums + SORT_WAVES;
+  const int per_wave = (int)((a.n + SORT_WG - 1) / SORT_WG) * 64, rounds = per_wave / 64;
+  int* const stok = skey + SORT_WAVES * per_wave;
+  int key[ONE_ROUNDS], tok[ONE_ROUNDS], dig[ONE_ROUNDS], rank[ONE_ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ONE_ROUNDS; ++r) {
+    const long i = wave * per_wave + 64 * r + lane;
+    const long id = r < rounds && i < a.n ? a.ids[i] : -1;
+    key[r] = id < a.V ? (int)id : -1;
+    if (id < 0) key[r] = -1;
+    tok[r] = (int)i;
+  }
+  int m = 0;
+  for (int p = 0; p < passes; ++p) {
+    clear_counts(cnt, digits);
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ONE_ROUNDS; ++r) dig[r] = key[r] < 0 ? -1 : (key[r] >> (p * bits)) & (digits - 1);
+    rank_in_wave<ONE_ROUNDS>(dig, rank, cnt + wave * digits, bits);
+    __syncthreads();
+    const int count = counts_to_starts(cnt, digits);
+    const int at = exclusive_sum(count, sums, &m);
+    if (tid < digits) start[tid] = at;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ONE_ROUNDS; ++r)
+      if (dig[r] >= 0) {
+        const int to = start[dig[r]] + cnt[wave * digits + dig[r]] + rank[r];
+        skey[to] = key[r];
+        stok[to] = tok[r];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ONE_ROUNDS; ++r) {
+      const int i = wave * per_wave + 64 * r + lane;
+      const bool on = r < rounds && i < m;
+      key[r] = on ? skey[i] : -1;
+      tok[r] = on ? stok[i] : 0;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < ONE_ROUNDS; ++r) {
+    const int i = wave * per_wave + 64 * r + lane;
+    if (key[r] >= 0) {
+      a.key[0][i] = key[r];
+      a.tok[0][i] = tok[r];
+    }
+  }
+  if (tid == 0) {
+    a.head->count = m;
+    a.head->n_long = 0;
+  }
+}
+
+// More tokens: a pass is two launches of up to EMBED_BLOCKS workgroups, each with a run of the tokens; the first counts the digits of every run, the
+// second moves the tokens.  Pass 0 reads the ids and leaves tokens out that have no row.
+constexpr int RUN_ROUNDS = 4, RUN_STEP = SORT_WG * RUN_ROUNDS;
+inline long run_of(long n) { return std::max((long)RUN_STEP, (n + EMBED_BLOCKS * SORT_WG - 1) / (EMBED_BLOCKS * SORT_WG) * SORT_WG); }
+__device__ __forceinline__ int sort_key(const EmbedArgs& a, int p, int from, long i, long n) {
+  if (i >= n) return -1;
+  if (p > 0) return a.key[from][i];
+  const long id = a.ids[i];
+  return id >= 0 && id < a.V ? (int)id : -1;
+}
+// (`from`: which of the two lists a pass reads)
+__global__ void __launch_bounds__(SORT_WG) embed_count_kernel(EmbedArgs a, int bits, int p, int from, long run) {
+  extern __shared__ __attribute__((aligned(16))) int sort_mem[];
+  const int digits = 1 << bits, tid = threadIdx.x;
+  for (int i = tid; i < digits; i += SORT_WG) sort_mem[i] = 0;
+  __syncthreads();
+  const long n = p > 0 ? a.head->count : a.n, end = min(n, (blockIdx.x + 1) * run);
+  for (long i = blockIdx.x * run + tid; i < end; i += SORT_WG) {
+    const int key = sort_key(a, p, from, i, n);
+    if (key >= 0) atomicAdd(&sort_mem[(key >> (p * bits)) & (digits - 1)], 1);
+  }
+  __syncthreads();
+  for (int i = tid; i < digits; i += SORT_WG) a.hist[(long)blockIdx.x * digits + i] = sort_mem[i];
+}
+__global__ void __launch_bounds__(SORT_WG) embed_move_kernel(EmbedArgs a, int bits, int p, int from, int to, long run, int last) {
+  extern __shared__ __attribute__((aligned(16))) int sort_mem[];
+  const int digits = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int* const cnt = sort_mem;
+  int* const start = cnt + SORT_WAVES * digits;
+  int* const sums = start + digits;
+  const long n = p > 0 ? a.head->count : a.n, begin = blockIdx.x * run, end = min(n, begin + run);
+  // where this run's tokens of every digit go: behind all smaller digits, and behind the runs before
+  int all = 0, before = 0;
+  if (tid < digits) {
+    for (int b0 = 0; b0 < (int)gridDim.x; b0 += 8) {
+      int c[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) c[k] = a.hist[(long)min(b0 + k, (int)gridDim.x - 1) * digits + tid];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int b = b0 + k;
+        all += b < (int)gridDim.x ? c[k] : 0;
+        before += b < (int)blockIdx.x ? c[k] : 0;
+      }
+    }
+  }
+  int m;
+  const int at = exclusive_sum(all, sums, &m);
+  if (tid < digits) start[tid] = at + before;
+  if (blockIdx.x == 0) {
+    if (last) {
+      if (tid < digits) a.top[tid] = at;
+      if (tid == 0) a.top[digits] = m;
+    }
+    if (tid == 0) {
+      if (p == 0) a.head->count = m;                 // (pass 0 does not read it)
+      a.head->n_long = 0;
+    }
+  }
+  for (long base = begin; base < end; base += RUN_STEP) {
+    int key[RUN_ROUNDS], tok[RUN_ROUNDS], dig[RUN_ROUNDS], rank[RUN_ROUNDS];
+    __syncthreads();
+    clear_counts(cnt, digits);
+#pragma unroll
+    for (int r = 0; r < RUN_ROUNDS; ++r) {
+      const long i = base + (wave * RUN_ROUNDS + r) * 64 + lane;
+      key[r] = sort_key(a, p, from, i, end);
+      tok[r] = p == 0 ? (int)i : key[r] >= 0 ? a.tok[from][i] : 0;
+      dig[r] = key[r] < 0 ? -1 : (key[r] >> (p * bits)) & (digits - 1);
+    }
+    __syncthreads();
+    rank_in_wave<RUN_ROUNDS>(dig, rank, cnt + wave * digits, bits);
+    __syncthreads();
+    const int count = counts_to_starts(cnt, digits);
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RUN_ROUNDS; ++r)
+      if (dig[r] >= 0) {
+        const int at = start[dig[r]] + cnt[wave * digits + dig[r]] + rank[r];
+        a.key[to][at] = key[r];
+        a.tok[to][at] = tok[r];
+      }
+    __syncthreads();
+    if (tid < digits) start[tid] += count;
+  }
+}
+
+// ---- backward: the sums ----
+
+template <typename T> __device__ __forceinline__ void finish_row(const EmbedArgs& a, int id, int e, int there, const float (&s)[V8]) {
+  T* const to = (T*)a.d_table + (long)id * a.E + e;
+  float v[V8];
+  if (a.accumulate) {
+    Piece<T> old;
+    old.load(to, there);
+#pragma unroll
+    for (int j = 0; j < V8; ++j) v[j] = fmaf(s[j], a.scale, old[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V8; ++j) v[j] = s[j] * a.scale;
+  }
+  Piece<T>::store(to, there, v);
+}
+
+// Rows that no token has are set to 0: workgroup `wg` takes 2^sub of the ids that share their last digit, finds which of them tokens have (their
+// sorted tokens are from top[digit] on) and clears the others.
+constexpr int ROWS_LOG = 6;
+template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs& a, long wg, int low) {
+  __shared__ unsigned has[1 << (ROWS_LOG - 5)];
+  const int sub = min(low, ROWS_LOG), tid = threadIdx.x;
+  const long v0 = wg << sub, v1 = min(a.V, v0 + (1L << sub));
+  if (tid < (1 << (ROWS_LOG - 5))) has[tid] = 0u;
+  __syncthreads();
+  const int digit = (int)(v0 >> low);
+  for (int i = a.top[digit] + tid; i < a.top[digit + 1]; i += 256) {
+    const int r = a.key[0][i] - (int)v0;
+    if (r >= 0 && r < (1 << sub)) atomicOr(&has[r / 32], 1u << (r % 32));
+  }
+  __syncthreads();
+  const int per = chunks8(a.E), rows = (int)(v1 - v0);
+  const float zero[V8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < rows; ++r) {
+    if ((has[r / 32] >> (r % 32)) & 1u) continue;
+    T* const to = (T*)a.d_table + (v0 + r) * a.E;
+    for (int c = tid; c < per; c += 256) Piece<T>::store(to + c * V8, a.E - c * V8, zero);
+  }
+}
+
+// Sums over a chunk of the sorted tokens, by a team; workgroups from `sums` on clear rows (low: bits of an id below its last digit)
+template <typename T> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, int tl, unsigned sums_x, int n_eb, int low) {
+  if (blockIdx.x >= sums_x) {
+    clear_rows<T>(a, blockIdx.x - sums_x, low);
+    return;
+  }
+  const int E = a.E, lane = threadIdx.x & ((1 << tl) - 1), eb = (int)(blockIdx.x % n_eb), e = ((eb << tl) + lane) * V8, there = E - e;
+  const long c = (long)(blockIdx.x / n_eb) * (256 >> tl) + (threadIdx.x >> tl), p0 = c * a.chunk;
+  const int m = a.head->count;
+  if (p0 >= m || there <= 0) return;
+  const int first = (int)p0, end = (int)min((long)m, p0 + a.chunk);
+  const int *const key = a.key[0], *const tok = a.tok[0];
+  const int prev = first > 0 ? key[first - 1] : -1, next = end < m ? key[end] : -1;
+  int cur = key[first];
+  bool before = prev == cur;
+  float s[V8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const auto flush = [&](bool after) {
+    if (!before && !after) {
+      finish_row<T>(a, cur, e, there, s);
+    } else {
+      Piece<float>::store(a.part + (2 * c + (before ? 0 : 1)) * E + e, there, s);
+    }
+  };
+  constexpr int U = 8;                               // rows on their way at once
+  for (int p = first; p < end; p += U) {
+    int id[U];
+    Piece<T> x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      id[k] = key[min(p + k, end - 1)];
+      x[k].load((const T*)a.d_y + tok[min(p + k, end - 1)] * a.y_ss + e, there);
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (p + k < end) {
+        if (id[k] != cur) {
+          flush(false);
+#pragma unroll
+          for (int j = 0; j < V8; ++j) s[j] = 0.f;
+          cur = id[k];
+          before = false;
+        }
+#pragma unroll
+        for (int j = 0; j < V8; ++j) s[j] += x[k][j];
+      }
+  }
+  const bool after = next == cur;
+  flush(after);
+  if (after && !before && e == 0) a.long_list[atomicAdd(&a.head->n_long, 1)] = (int)c;      // (their order changes no result)
+}
+
+// Ids that go over several chunks: 256 features a workgroup, its four waves with a run of the chunks each.
+template <typename T> __global__ void __launch_bounds__(256) embed_join_kernel(EmbedArgs a, int n_eb) {
+  __shared__ float sums[4][256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.E, m = a.head->count;
+  const long items = (long)a.head->n_long * n_eb;
+  for (long it = blockIdx.x; it < items; it += gridDim.x) {
+    const int c0 = a.long_list[it / n_eb], e0 = (int)(it % n_eb) * 256, e = e0 + 4 * lane;
+    const int id = a.key[0][(long)(c0 + 1) * a.chunk];
+    // behind the id's last token
+    int lo = (c0 + 1) * a.chunk, hi = m;             // key[lo] is the id; key[hi] is not (or is not there)
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (a.key[0][mid] == id) lo = mid;
+      else hi = mid;
+    }
+    const int c1 = lo / a.chunk, parts = c1 - c0 + 1;            // chunks c0 .. c1
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    const int q1 = (int)((long)(wave + 1) * parts / 4);
+    for (int q = (int)((long)wave * parts / 4); q < q1; q += 8) {
+      float v[8][4];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int c = c0 + min(q + k, q1 - 1);
+        const float* const from = a.part + (2L * c + (c == c0 ? 1 : 0)) * E + e;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[k][j] = e + j < E ? from[j] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (q + k < q1) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[j] += v[k][j];
+        }
+    }
+    __syncthreads();                                 // (the sums of the id before have been read)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[wave][4 * lane + j] = s[j];
+    __syncthreads();
+    if (e0 + tid < E) {
+      const float all = (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]);
+      T* const to = (T*)a.d_table + (long)id * E + e0 + tid;
+      *to = (T)(a.accumulate ? fmaf(all, a.scale, (float)*to) : all * a.scale);
+    }
+  }
+}
+
+long up(long n, long by) { return (n + by - 1) / by; }
+
+template <typename T> hipError_t embed_fwd(const EmbedArgs& a, hipStream_t s) {
+  const int tl = team_log(a.E);
+  embed_fwd_kernel<T><<<dim3((unsigned)std::min(up(a.n, (256 >> tl) * ROWS), 1L << 18), (unsigned)up(a.E, V8 << tl)), 256, 0, s>>>(a, tl);
+  return hipGetLastError();
+}
+
+template <typename T> hipError_t embed_bwd(const EmbedArgs& a, hipStream_t s) {
+  const Sort sort = sort_of(a.V);
+  const bool one = a.n <= ONE_WG;
+  hipError_t e;
+  if (one) {
+    static SmemOnce once;
+    e = ensure_dynamic_lds((const void*)embed_sort_one_kernel<T>, one_lds(EMBED_DIGIT_BITS, ONE_WG), &once);
+    if (e != hipSuccess) return e;
+    const long clear = a.accumulate ? 0 : std::min(4L * a.n_cu, up(a.V * a.E, SORT_WG * 16));
+    embed_sort_one_kernel<T><<<(unsigned)(1 + clear), SORT_WG, one_lds(sort.bits, a.n), s>>>(a, sort.bits, sort.passes);
+  } else {
+    static SmemOnce once;
+    e = ensure_dynamic_lds((const void*)embed_move_kernel, sort_lds(EMBED_DIGIT_BITS), &once);
+    if (e != hipSuccess) return e;
+    const long run = run_of(a.n);
+    const unsigned blocks = (unsigned)up(a.n, run);
+    for (int p = 0; p < sort.passes; ++p) {
+      const int to = (sort.passes - 1 - p) % 2, from = 1 - to;
+      embed_count_kernel<<<blocks, SORT_WG, (1 << sort.bits) * sizeof(int), s>>>(a, sort.bits, p, from, run);
+      embed_move_kernel<<<blocks, SORT_WG, sort_lds(sort.bits), s>>>(a, sort.bits, p, from, to, run, p == sort.passes - 1);
+    }
+  }
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int tl = team_log(a.E), n_eb = (int)up(a.E, V8 << tl), low = sort.bits * (sort.passes - 1);
+  const long n_chunks = up(a.n, a.chunk), wgs = up(n_chunks, 256 >> tl) * n_eb;
+  const long clear = one || a.accumulate ? 0 : up(a.V, 1L << std::min(low, ROWS_LOG));
+  embed_sum_kernel<T><<<(unsigned)(wgs + clear), 256, 0, s>>>(a, tl, (unsigned)wgs, n_eb, low);
+  if (n_chunks > 1) {
+    const int eb = (int)up(a.E, 256);
+    embed_join_kernel<T><<<(unsigned)std::min((n_chunks - 1) * eb, 4L * a.n_cu), 256, 0, s>>>(a, eb);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Sorted tokens of a chunk: 8 to 64, so that there are threads for about 2^17 pieces of 8 features.
+int embed_chunk(long n, int E) {
+  int c = 8;
+  while (c < 64 && n * chunks8(E) / c > (1L << 17)) c *= 2;
+  return c;
+}
+// Chunks are the shorter the less there is: of n E / 8 = P pieces or fewer, no more than min(P / 8, max(2^17, P / 64)) chunk pieces and a row of them.
+size_t embed_part_room(long n, int E) {
+  const long P = n * chunks8(E);
+  return 2 * sizeof(float) * (size_t)V8 * (std::min(P / 8, std::max(1L << 17, P / 64)) + chunks8(E) + 1);
+}
+
+hipError_t launch_embed_fwd(const EmbedArgs& a, int is_f32, hipStream_t s) { return is_f32 ? embed_fwd<float>(a, s) : embed_fwd<__bf16>(a, s); }
+hipError_t launch_embed_bwd(EmbedArgs a, int is_f32, hipStream_t s) {
+  a.chunk = embed_chunk(a.n, a.E);
+  return is_f32 ? embed_bwd<float>(a, s) : embed_bwd<__bf16>(a, s);
+}
+
+}  // namespace lvx

@@ -242,6 +242,60 @@ size_t xent_dw_room(long n, int E, long V, int n_cu, int is_f32);
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s);
 
+// Rows of an embedding table (lvx_embed.hip)
+struct EmbedHead {
+  int count;            // tokens that have a row of the table
+  int n_long;           // entries of long_list
+  int pad[62];
+};
+struct EmbedArgs {
+  const void* table;    // [V, E] (forward)
+  const int64_t* ids;   // [n]
+  void* y;              // [n, E], row stride y_ss elements (forward)
+  const void* d_y;      // like y (backward)
+  void* d_table;        // [V, E] (backward)
+  long n, V, y_ss;
+  int E, n_cu, accumulate;
+  float scale;
+  // workspace
+  EmbedHead* head;
+  int *key[2], *tok[2]; // [n]: ids and numbers of the tokens, from one pass of the sort to the next; the last one leaves key[0], tok[0]
+  int* hist;            // [EMBED_BLOCKS][EMBED_DIGITS]
+  int* top;             // [EMBED_DIGITS + 1]: where the ids with every value of the last digit start
+  int* long_list;       // chunks whose last id goes on in the next one
+  float* part;          // [chunks][2][E]
+  int chunk;            // sorted tokens of a chunk
+};
+constexpr int EMBED_BLOCKS = 256, EMBED_DIGIT_BITS = 10, EMBED_DIGITS = 1 << EMBED_DIGIT_BITS;
+int embed_chunk(long n, int E);
+size_t embed_part_room(long n, int E);      // bytes of `part` for n tokens of E features or fewer
+hipError_t launch_embed_fwd(const EmbedArgs& a, int is_f32, hipStream_t s);
+hipError_t launch_embed_bwd(EmbedArgs a, int is_f32, hipStream_t s);
+
+// Losses of sequences of tokens from the tokens' negative log likelihoods (lvx_sequence_loss.hip)
+struct SequenceArgs {
+  const float *nll, *ref, *old, *adv;          // [n]; adv [n] or [count]
+  const int64_t *labels, *first;        // [n], [count + 1]
+  float *loss, *margin, *stats;         // [S]; [S]; [S, 3]
+  const float* d_loss;  // [S]
+  float* d_nll;         // [n], or null
+  long n, count;        // tokens, sequences
+  int form, mean, per_token;
+  double beta, smoothing;               // preferences; beta: also the weight of the divergence
+  double low, high, ln_low, ln_high;    // a ratio's bounds, and their logarithms
+  void *head, *block;   // workspace: sums of every sequence's first piece, and of every block of tokens that goes on in one
+};
+constexpr int SEQUENCE_BLOCK = 2048;    // tokens of a block
+size_t sequence_part_bytes();           // of one of these sums
+hipError_t launch_preference(const SequenceArgs& a, hipStream_t s);
+hipError_t launch_policy(const SequenceArgs& a, hipStream_t s);
+
+// Whether the `len_b` bytes at b meet one of n rows of `len_a` bytes, `pitch` apart, at a: row k does where `behind` < k pitch < `before`
+inline bool rows_meet(int64_t a, int64_t n, int64_t pitch, int64_t len_a, int64_t b, int64_t len_b) {
+  const int64_t behind = b - a - len_a, before = b + len_b - a, k = behind < 0 ? 0 : behind / pitch + 1;
+  return k < n && k * pitch < before;
+}
+
 int device_cu_count();   // of the first device asked for (256 where there is none)
 
 // Bytes of workspace that lvx_xattn_fwd needs for exactly this call (with this mask or without

@@ -11,17 +11,12 @@ constexpr size_t ALIGN = 256;
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 bool aligned(const void* p, size_t by) { return (uintptr_t)p % by == 0; }
 
-// Whether the `len_b` bytes at b meet one of n rows of `len_a` bytes, `pitch` apart, at a: row k does where `behind` < k pitch < `before`
-bool meet(int64_t a, int64_t n, int64_t pitch, int64_t len_a, int64_t b, int64_t len_b) {
-  const int64_t behind = b - a - len_a, before = b + len_b - a, k = behind < 0 ? 0 : behind / pitch + 1;
-  return k < n && k * pitch < before;
-}
 // Whether dx or dw lies in x or w, or one in the other (windows of one wider tensor beside each other do not)
 bool gradients_in_operands(const lvx_xent* p, int64_t el, const void* x, const void* w, const void* dx, const void* dw) {
   const int64_t pitch = p->x_ss * el, row = p->E * el, vocab = p->V * row, xa = (int64_t)x, wa = (int64_t)w, dxa = (int64_t)dx, dwa = (int64_t)dw;
-  return (dx && (meet(xa - (p->n - 1) * pitch, 2 * p->n - 1, pitch, row, dxa, row) || meet(dxa, p->n, pitch, row, wa, vocab))) ||
-         (dw && (meet(wa, 1, vocab, vocab, dwa, vocab) || meet(xa, p->n, pitch, row, dwa, vocab))) ||
-         (dx && dw && meet(dxa, p->n, pitch, row, dwa, vocab));
+  return (dx && (rows_meet(xa - (p->n - 1) * pitch, 2 * p->n - 1, pitch, row, dxa, row) || rows_meet(dxa, p->n, pitch, row, wa, vocab))) ||
+         (dw && (rows_meet(wa, 1, vocab, vocab, dwa, vocab) || rows_meet(xa, p->n, pitch, row, dwa, vocab))) ||
+         (dx && dw && rows_meet(dxa, p->n, pitch, row, dwa, vocab));
 }
 
 lvx_status check_sizes(int64_t n, int32_t E, int64_t V, lvx_dtype dtype) {
