@@ -11,15 +11,17 @@
  * Around the layer stand the norms of its token features          lvx_norm_fwd,
  * the 8-bit form in which they are kept                           lvx_pack,
  * and the loss at the end of a training step                      lvx_xent_fwd,
+ * or a teacher's in its place                                     lvx_distil_fwd,
  * whose logits exist in tiles only; the backward pass keeps their gradient, up to 1 GiB
- * of it at a time, in the workspace.
+ * of it at a time, in the workspace.  At its beginning stand token features from a table   lvx_embed_fwd,
+ * behind the tokens' losses those of whole sequences              lvx_preference, lvx_policy.
  *
  * General rules for every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The library
  *     never allocates, frees or synchronises; all work is enqueued on the HIP
  *     stream the caller passes (a hipStream_t cast to void*, NULL = default).
  *   - Scratch memory is a caller-provided workspace whose size comes from
- *     lvx_xattn_workspace_bytes (lvx_norm_workspace_bytes, lvx_xent_workspace_bytes);
+ *     lvx_xattn_workspace_bytes (lvx_norm_workspace_bytes, lvx_xent_workspace_bytes, ..);
  *     it must be 256-byte aligned, and what it holds is a call's own: two calls that may
  *     run at the same time (two streams, two captured graphs) need one each.
  *   - The structs of arguments (lvx_problem, lvx_mask, lvx_norm, ..) and the pointer
@@ -355,6 +357,38 @@ lvx_status lvx_xent_fwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const
  * Sums are float32, in a fixed order: results repeat bit for bit. */
 lvx_status lvx_xent_bwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, const float* lse,
                         const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Distillation: the divergence of n tokens' softmax over a vocabulary of V entries from a teacher's, of which K logits a token are known, both at a
+ * temperature T; the logits z = x w^T are never kept, as in lvx_xent_fwd.  Over the entries k of token i, with v = ids[i, k]:
+ *     q[k] = exp(t[i, k] / T) / sum_j exp(t[i, j] / T),   lse[i] = ln sum_v exp(z[i, v] / T),   ln_p[i, k] = z[i, v] / T - lse[i],
+ *     loss[i] = sum_k q[k] (ln q[k] - ln_p[i, k]).
+ * x, w     as for lvx_xent_fwd, with its rules for types, widths, strides and alignment.
+ * ids      device, [n, K] int64, in any order.  A negative id: the entry is not there (its logit may hold anything, its ln_p is 0).  A token of which no
+ *          entry is there, or only entries with a logit of -infinity, takes no part (loss, lse and ln_p 0, no gradient; its features may hold anything,
+ *          NaN included).  V or more: loss and lse are NaN, and the gradients that the token is in.  An id that comes more than once
+ *          counts once for each time.
+ * teacher  device, [n, K] of `teacher_dtype`: the teacher's logits t; -infinity counts as q = 0.  A NaN or +infinity makes the loss NaN.
+ * loss, lse   device, [n] float32, overwritten.     ln_p   device, [n, K] float32, overwritten.
+ * K is 1 to 1024 (more: LVX_ERR_UNSUPPORTED).  T > 0.  The loss has no factor T^2: put it into d_loss where it is wanted.
+ * workspace   of lvx_distil_workspace_bytes(n, E, V, K, dtype) (0: invalid sizes), for either pass; it also serves fewer of each, as
+ *          lvx_xent_workspace_bytes' does, and a smaller one as it says there. */
+typedef struct {
+  int64_t n, V;             /* tokens, entries of the vocabulary */
+  int32_t E, K;             /* features, known entries of a token */
+  int64_t x_ss;             /* elements from one row of x (and dx) to the next */
+  float temperature;
+} lvx_distil;
+size_t lvx_distil_workspace_bytes(int64_t n, int32_t E, int64_t V, int32_t K, lvx_dtype dtype);
+lvx_status lvx_distil_fwd(const lvx_distil* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* ids, const void* teacher,
+                          lvx_dtype teacher_dtype, float* loss, float* lse, float* ln_p, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients, as lvx_xent_bwd's:
+ *     g[i, v] = (exp(z[i, v] / T - lse[i]) - sum over k with ids[i, k] = v of q[k]) d_loss[i] / T,   dx[i] = sum_v g[i, v] w[v],   dw[v] = sum_i g[i, v] x[i].
+ * lse, ln_p   what lvx_distil_fwd left for the same x, w, ids, teacher and T.
+ * d_loss, dx, dw   as for lvx_xent_bwd: the same types and refusals, OVERWRITTEN, either of dx and dw may be NULL.  No gradient goes to the teacher. */
+lvx_status lvx_distil_bwd(const lvx_distil* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* ids, const void* teacher,
+                          lvx_dtype teacher_dtype, const float* lse, const float* ln_p, const float* d_loss, void* dx, void* dw, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
 
 /* ---- at either end of a step: token features from a table, and losses of whole sequences ---- */
 

@@ -28,7 +28,7 @@ LVX_STATIC_SCRATCH_BYTES = 64 << 20
 EXPORTS = ("lvx_xattn_workspace_bytes", "lvx_xattn_fwd", "lvx_xattn_fwd_static", "lvx_xattn_fwd_merge", "lvx_xattn_fwd_merge_last", "lvx_xattn_merge", "lvx_xattn_bwd",
            "lvx_xattn_bwd_stages", "lvx_xattn_bwd_visit", "lvx_xattn_bwd_error_word", "lvx_xattn_dq_finalize", "lvx_xattn_project", "lvx_xattn_project_bwd",
            "lvx_pack", "lvx_unpack", "lvx_norm_fwd", "lvx_norm_workspace_bytes", "lvx_norm_bwd",
-           "lvx_xent_workspace_bytes", "lvx_xent_fwd", "lvx_xent_bwd",
+           "lvx_xent_workspace_bytes", "lvx_xent_fwd", "lvx_xent_bwd", "lvx_distil_workspace_bytes", "lvx_distil_fwd", "lvx_distil_bwd",
            "lvx_embed_fwd", "lvx_embed_workspace_bytes", "lvx_embed_bwd",
            "lvx_preference_workspace_bytes", "lvx_preference", "lvx_policy_workspace_bytes", "lvx_policy", "lvx_strerror")
 
@@ -65,6 +65,10 @@ class lvx_norm(C.Structure):
 
 class lvx_xent(C.Structure):
     _fields_ = [("n", C.c_int64), ("V", C.c_int64), ("E", C.c_int32), ("x_ss", C.c_int64)]
+
+
+class lvx_distil(C.Structure):
+    _fields_ = [("n", C.c_int64), ("V", C.c_int64), ("E", C.c_int32), ("K", C.c_int32), ("x_ss", C.c_int64), ("temperature", C.c_float)]
 
 
 class lvx_embed(C.Structure):
@@ -149,6 +153,11 @@ def load() -> C.CDLL:
         lib.lvx_xent_fwd.restype = lib.lvx_xent_bwd.restype = C.c_int
         lib.lvx_xent_fwd.argtypes = [C.POINTER(lvx_xent), C.c_int] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
         lib.lvx_xent_bwd.argtypes = [C.POINTER(lvx_xent), C.c_int] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
+        lib.lvx_distil_workspace_bytes.restype = C.c_size_t
+        lib.lvx_distil_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.c_int]
+        lib.lvx_distil_fwd.restype = lib.lvx_distil_bwd.restype = C.c_int
+        lib.lvx_distil_fwd.argtypes = [C.POINTER(lvx_distil), C.c_int] + [C.c_void_p] * 4 + [C.c_int] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+        lib.lvx_distil_bwd.argtypes = [C.POINTER(lvx_distil), C.c_int] + [C.c_void_p] * 4 + [C.c_int] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
         lib.lvx_embed_workspace_bytes.restype = lib.lvx_preference_workspace_bytes.restype = lib.lvx_policy_workspace_bytes.restype = C.c_size_t
         lib.lvx_embed_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int64]
         lib.lvx_preference_workspace_bytes.argtypes = lib.lvx_policy_workspace_bytes.argtypes = [C.c_int64, C.c_int64]
@@ -619,6 +628,59 @@ def lvx_xent_bwd(x, w, labels, lse, d_loss, dx=None, dw=None, workspace=None) ->
     _check(load().lvx_xent_bwd(C.byref(p), dtype_code(x.dtype), x.data_ptr(), w.data_ptr(), labels.data_ptr(), lse.data_ptr(), d_loss.data_ptr(),
                                dx.data_ptr() if dx is not None else None, dw.data_ptr() if dw is not None else None,
                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), s), where)
+
+
+def lvx_distil_workspace_bytes(n: int, E: int, V: int, K: int, dtype: int) -> int:
+    return int(load().lvx_distil_workspace_bytes(n, E, V, K, dtype))
+
+
+def _distil_struct(where, x, w, ids, teacher, ln_p, per_token, workspace, temperature):
+    """Sizes of a distillation call; per_token: the float32 [n] tensors of it."""
+    n, E, x_ss = _token_rows(x, "x")
+    if w.dim() != 2 or w.shape[1] != E or w.dtype != x.dtype or not w.is_contiguous():
+        raise ValueError(f"{where}: w has to be [V, {E}] of x's type, contiguous")
+    K = ids.shape[-1] if ids.dim() > 1 else 0
+    if K < 1 or ids.numel() != n * K or ids.dtype != torch.int64 or not ids.is_contiguous():
+        raise ValueError(f"{where}: ids have to be int64 [{n}, K], contiguous")
+    if teacher.shape != ids.shape or not teacher.is_contiguous():
+        raise ValueError(f"{where}: the teacher's logits have to be like ids, contiguous")
+    if ln_p.numel() != n * K or ln_p.dtype != torch.float32 or not ln_p.is_contiguous():
+        raise ValueError(f"{where}: ln_p has to be float32 [{n}, {K}], contiguous")
+    for t in per_token:
+        if t.numel() != n or t.dtype != torch.float32 or not t.is_contiguous():
+            raise ValueError(f"{where}: loss, lse and d_loss have to be float32 [{n}], contiguous")
+    if not workspace.is_contiguous():
+        raise ValueError(f"{where}: the workspace has to be contiguous")
+    return lvx_distil(n, w.shape[0], E, K, x_ss, temperature)
+
+
+def lvx_distil_fwd(x, w, ids, teacher, loss, lse, ln_p, workspace, temperature: float = 1.0) -> None:
+    """loss, lse (float32, one value for every token) and ln_p (float32 [n, K]) are overwritten with the divergence of softmax(x w^T / temperature) from
+    the softmax of the teacher's logits (float32 or bfloat16 [n, K]) of the entries ids (int64 [n, K]) of the vocabulary w [V, E].  Negative ids are
+    entries that are not there; a token without any takes no part."""
+    where = "lvx_distil_fwd"
+    s = _on_device(where, x, w, ids, teacher, loss, lse, ln_p, workspace)
+    p = _distil_struct(where, x, w, ids, teacher, ln_p, (loss, lse), workspace, temperature)
+    _check(load().lvx_distil_fwd(C.byref(p), dtype_code(x.dtype), x.data_ptr(), w.data_ptr(), ids.data_ptr(), teacher.data_ptr(),
+                                 dtype_code(teacher.dtype), loss.data_ptr(), lse.data_ptr(), ln_p.data_ptr(), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), s), where)
+
+
+def lvx_distil_bwd(x, w, ids, teacher, lse, ln_p, d_loss, dx=None, dw=None, workspace=None, temperature: float = 1.0) -> None:
+    """dx (x's shape, strides and type) and dw (w's) are overwritten with the gradients; either may be None, and neither may lie in x or w.  lse and ln_p:
+    what lvx_distil_fwd left; d_loss: the gradient of every token's loss."""
+    where = "lvx_distil_bwd"
+    if workspace is None or (dx is None and dw is None):
+        raise ValueError(f"{where}: no workspace, or nothing asked for")
+    s = _on_device(where, x, w, ids, teacher, lse, ln_p, d_loss, dx, dw, workspace)
+    p = _distil_struct(where, x, w, ids, teacher, ln_p, (lse, d_loss), workspace, temperature)
+    if dx is not None and (dx.shape != x.shape or dx.dtype != x.dtype or _token_rows(dx, "dx")[2] != p.x_ss):
+        raise ValueError(f"{where}: dx has to have x's shape, strides and type")
+    if dw is not None and (dw.shape != w.shape or dw.dtype != w.dtype or not dw.is_contiguous()):
+        raise ValueError(f"{where}: dw has to be [{p.V}, {p.E}] of w's type, contiguous")
+    at = lambda t: t.data_ptr() if t is not None else None
+    _check(load().lvx_distil_bwd(C.byref(p), dtype_code(x.dtype), at(x), at(w), at(ids), at(teacher), dtype_code(teacher.dtype), at(lse), at(ln_p),
+                                 at(d_loss), at(dx), at(dw), at(workspace), workspace.numel() * workspace.element_size(), s), where)
 
 
 # ---- at either end of a step: token features from a table, losses of whole sequences ----

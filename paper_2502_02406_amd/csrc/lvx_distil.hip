@@ -1,0 +1,208 @@
+// Distillation from a teacher's top logits: the divergence of softmax(x w^T / T) from the softmax of K known logits a token, without keeping
+// z = x w^T (the products and their tiles: lvx_xent_kernels.h).
+//
+//   loss_i = sum_k q_k (ln q_k - z_ik / T + lse_i),   lse_i = ln sum_v exp(z_iv / T)
+//   g_iv = (exp(z_iv / T - lse_i) - sum over k with id_ik = v of q_k) d_loss_i / T,   dx = g w,   dw = g^T x
+//
+// What differs from the cross entropy is that a token has K logits to be handed out instead of one.  The first launch sorts every token's ids
+// and counts those below every multiple of 64, so that a tile's epilogue finds the ones among its columns with one lookup a row, and
+// leaves their logits in their order.  The gradient's tiles write exp(z / T - lse) d_loss / T everywhere; at the teacher's entries another launch
+// puts exp(ln p) - q in its place, from the ln p of the forward pass, with one rounding like everywhere else: n K values beside the n V.
+#include "lvx_xent_kernels.h"
+
+namespace lvx {
+
+namespace {
+
+// entry k of token i: whether it is there, and its logit by the temperature
+struct Entry { bool there; long id; float t; };
+__device__ __forceinline__ Entry entry_of(const XentArgs& a, long i, int k) {
+  Entry e;
+  e.id = a.ids[i * a.K + k];
+  e.there = e.id >= 0;
+  const float t = a.teacher_bf16 ? __uint_as_float((unsigned)((const uint16_t*)a.teacher)[i * a.K + k] << 16) : ((const float*)a.teacher)[i * a.K + k];
+  e.t = t / a.temperature;
+  return e;
+}
+__device__ __forceinline__ float ln_q_of(const Entry& e, float2 stat) { return (e.t - stat.x) - stat.y; }
+
+// A wave a token: whether it takes part (a.labels: 0, -1 if not, V if an id is outside), the sum of its exponentials, and (SORT) its ids in order.
+template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kernel(XentArgs a) {
+  extern __shared__ __attribute__((aligned(16))) int prepare_mem[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K;
+  int* const keys = prepare_mem + wave * 2 * K;
+  int* const sorted = keys + K;
+  for (long base = blockIdx.x * 4L; base < a.n; base += gridDim.x * 4L) {
+    const long i = min(base + wave, a.n - 1);        // (the last token again: the same results)
+    float top = -__builtin_inff();
+    bool any = false, far = false;
+    for (int k = lane; k < K; k += 64) {
+      const Entry e = entry_of(a, i, k);
+      any |= e.there && !(e.t == -__builtin_inff());
+      far |= e.there && e.id >= a.V;
+      if (e.there) top = fmaxf(top, e.t);            // (a NaN is dropped here and comes back in the sum)
+      if (SORT) keys[k] = e.there && e.id < a.V ? (int)e.id : 0x7fffffff;
+    }
+    any = __any(any);
+    far = __any(far);
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+    float sum = 0.f;
+    for (int k = lane; k < K; k += 64) {
+      const Entry e = entry_of(a, i, k);
+      sum += e.there ? expf(e.t - top) : 0.f;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
+    if (lane == 0) {
+      ((int64_t*)a.labels)[i] = !any ? -1 : far ? a.V : 0;
+      a.q_stat[i] = make_float2(top, logf(sum));
+    }
+    if constexpr (SORT) {
+      __syncthreads();
+      for (int k = lane; k < K; k += 64) {
+        const int mine = keys[k];
+        int r = 0;
+        for (int j = 0; j < K; ++j) r += keys[j] < mine || (keys[j] == mine && j < k);
+        sorted[r] = mine;
+        a.sorted[i * K + r] = mine;
+        a.rank[i * K + k] = (uint16_t)r;
+        if (!any) a.ln_p[i * K + k] = 0.f;
+      }
+      __syncthreads();
+      for (int b = lane; b <= a.blocks; b += 64) {
+        int lo = 0, hi = K;                          // the first that is not below 64 b
+        while (lo < hi) {
+          const int mid = (lo + hi) / 2;
+          if (sorted[mid] < 64 * b) lo = mid + 1;
+          else hi = mid;
+        }
+        a.starts[i * (a.blocks + 1) + b] = (uint16_t)lo;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// lse, loss and ln p of the listed tokens from what the tiles left: 8 tokens a workgroup, 32 threads each
+__global__ void __launch_bounds__(256) distil_join_kernel(XentArgs a, int n_parts) {
+  __shared__ float sm[8][33], ss[8][33], lses[8];
+  const int row_l = threadIdx.x % 8, lane = threadIdx.x / 8;
+  const Own own = a.own ? own_list(a) : Own{};
+  const int count = a.own ? own.count : a.head->count;
+  if (a.own && blockIdx.x == 0 && (int)threadIdx.x >= count && threadIdx.x < a.n) {        // (the tokens that are not listed)
+    a.loss[own.tok] = 0.f;
+    a.lse_out[own.tok] = 0.f;
+  }
+  for (int r0 = blockIdx.x * 8; r0 < count; r0 += gridDim.x * 8) {
+    const int r = min(r0 + row_l, count - 1);
+    float m = -__builtin_inff(), s = 0.f;
+    for (int p0 = lane; p0 < n_parts; p0 += 32 * 8) {
+      float2 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = a.part[(long)min(p0 + 32 * i, n_parts - 1) * a.Mp + r];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (p0 + 32 * i < n_parts) join_stats(&m, &s, v[i].x, v[i].y);
+    }
+    sm[row_l][lane] = m;
+    ss[row_l][lane] = s;
+    __syncthreads();
+    if (threadIdx.x < 8) {
+      m = -__builtin_inff();
+      s = 0.f;
+      for (int i = 0; i < 32; ++i) join_stats(&m, &s, sm[threadIdx.x][i], ss[threadIdx.x][i]);
+      lses[threadIdx.x] = (m + __builtin_amdgcn_logf(s)) * LN2;
+    }
+    __syncthreads();
+    const int mine = threadIdx.x / 32, r1 = r0 + mine;
+    const int listed = min(r1, count - 1), tok = a.own ? __shfl(own.tok, listed) : a.tok[listed];
+    if (r1 < count) {
+      const float lse = a.labels[tok] < a.V ? lses[mine] : __builtin_nanf("");
+      const float2 stat = a.q_stat[tok];
+      float loss = 0.f;
+      for (int k = threadIdx.x % 32; k < a.K; k += 32) {
+        const Entry e = entry_of(a, tok, k);
+        const float z = e.there && e.id < a.V ? a.z_entry[(long)tok * a.K + a.rank[(long)tok * a.K + k]] : __builtin_nanf("");
+        const float ln_p = z * a.inv_t - lse, ln_q = ln_q_of(e, stat), q = expf(ln_q);
+        a.ln_p[(long)tok * a.K + k] = e.there ? ln_p : 0.f;
+        loss += !e.there || q == 0.f ? 0.f : q * (ln_q - ln_p);
+      }
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) loss += __shfl_xor(loss, o);
+      if (threadIdx.x % 32 == 0) {
+        a.loss[tok] = loss + 0.f * lse;              // (NaN where an id is outside, also if no entry counts)
+        a.lse_out[tok] = lse;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// g at the teacher's entries of a piece of the vocabulary: a wave a token
+template <typename G> __global__ void __launch_bounds__(256) distil_entries_kernel(XentArgs a) {
+  extern __shared__ __attribute__((aligned(16))) int entries_mem[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K, count = a.head->count;
+  int* const ids = entries_mem + wave * 2 * K;
+  float* const qs = (float*)(ids + K);
+  const float scale = a.head->scale;
+  for (int base = blockIdx.x * 4; base < count; base += gridDim.x * 4) {
+    const int r = min(base + wave, count - 1);
+    const long tok = a.tok[r];
+    const float2 stat = a.q_stat[tok];
+    const float d = (a.labels[tok] < a.V ? a.d_loss[tok] * a.inv_t : __builtin_nanf("")) / scale;
+    __syncthreads();
+    for (int k = lane; k < K; k += 64) {
+      const Entry e = entry_of(a, tok, k);
+      ids[k] = e.there && e.id < a.V ? (int)e.id : -1;
+      qs[k] = expf(ln_q_of(e, stat));
+    }
+    __syncthreads();
+    for (int k = lane; k < K; k += 64) {
+      const int id = ids[k];
+      if (id < a.v0 || id >= a.v1) continue;
+      float q = 0.f;                                 // (every entry of an id writes the same)
+      for (int j = 0; j < K; ++j) q += ids[j] == id ? qs[j] : 0.f;
+      const float p = exp2_fast(a.ln_p[tok * K + k] * LOG2E);
+      ((G*)a.g)[r * a.g_pitch + (id - a.v0)] = (G)(d != 0.f ? (p - q) * d : 0.f);
+    }
+  }
+}
+
+hipError_t prepare(const XentArgs& a, bool sort, hipStream_t s) {
+  const unsigned wgs = (unsigned)std::min(up(a.n, 4), 1L << 16);
+  if (sort) distil_prepare_kernel<true><<<wgs, 256, 4 * 2 * a.K * sizeof(int), s>>>(a);
+  else distil_prepare_kernel<false><<<wgs, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+hipError_t gradient(const XentArgs& a, int is_f32, hipStream_t s) {
+  const hipError_t e = logits<GRAD, TEACHER>(a, is_f32, s);
+  if (e != hipSuccess) return e;
+  const unsigned wgs = (unsigned)std::min(up(a.n, 4), 1L << 16);
+  if (is_f32) distil_entries_kernel<float><<<wgs, 256, 4 * 2 * a.K * sizeof(int), s>>>(a);
+  else distil_entries_kernel<__bf16><<<wgs, 256, 4 * 2 * a.K * sizeof(int), s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_distil_fwd(XentArgs a, int is_f32, hipStream_t s) {
+  hipError_t e = prepare(a, true, s);
+  if (e != hipSuccess) return e;
+  xent_fwd_sizes(&a, is_f32);
+  if (!a.own) {
+    e = launch_xent_list(a, s);
+    if (e != hipSuccess) return e;
+  }
+  e = logits<STATS, TEACHER>(a, is_f32, s);
+  if (e != hipSuccess) return e;
+  distil_join_kernel<<<(unsigned)std::min(up(a.n, 8), 4096L), 256, 0, s>>>(a, stat_parts_of(a, is_f32));
+  return hipGetLastError();
+}
+
+hipError_t launch_distil_bwd(XentArgs a, int is_f32, hipStream_t s) {
+  const hipError_t e = prepare(a, false, s);
+  return e != hipSuccess ? e : launch_xent_products(a, is_f32, s, gradient);
+}
+
+}  // namespace lvx

@@ -231,6 +231,19 @@ struct XentArgs {
   int first;            // whether it is the first one
   int own;              // so few tokens that every wave lists them for itself
   int tile, tile_rows, dw_tiles;        // columns and rows of a tile of dx; tiles of dw in parts
+  // a teacher's logits instead of labels (lvx_distil.hip; labels is then made by its first launch)
+  float inv_t, z2;      // 1 / temperature (1 without a teacher), log2 e / temperature
+  float temperature;
+  int K, blocks;        // entries of a token; pieces of 64 entries of the vocabulary
+  const int64_t* ids;   // [n, K]
+  const void* teacher;  // [n, K] float32, or (teacher_bf16) bf16
+  int teacher_bf16;
+  float* ln_p;          // [n, K] (forward: written)
+  float2* q_stat;       // [n]: the largest of the teacher's logits / temperature, and the logarithm of their sum of exponentials against it
+  int* sorted;          // forward, [n, K]: the ids in order, those that are none behind them
+  uint16_t* rank;       // [n, K]: where an entry stands among them
+  uint16_t* starts;     // [n, blocks + 1]: how many of them are below 64 b
+  float* z_entry;       // [n, K]: their logits, in their order
 };
 bool xent_bf16_supported(int E);
 int xent_stat_parts(long V, int is_f32);
@@ -241,6 +254,11 @@ size_t xent_dw_bytes(long n, int E, long cols, int n_cu, int is_f32);
 size_t xent_dw_room(long n, int E, long V, int n_cu, int is_f32);
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s);
+hipError_t launch_xent_list(const XentArgs& a, hipStream_t s);
+hipError_t launch_xent_products(XentArgs a, int is_f32, hipStream_t s, hipError_t (*gradient)(const XentArgs&, int, hipStream_t));
+constexpr int DISTIL_MOST_ENTRIES = 1024;
+hipError_t launch_distil_fwd(XentArgs a, int is_f32, hipStream_t s);
+hipError_t launch_distil_bwd(XentArgs a, int is_f32, hipStream_t s);
 
 // Rows of an embedding table (lvx_embed.hip)
 struct EmbedHead {

@@ -1,4 +1,4 @@
-// C ABI of the cross entropy against a vocabulary (see include/lvx.h): argument validation on the host, workspace carving, and
+// C ABI of the losses against a vocabulary, cross entropy and distillation (see include/lvx.h): argument validation on the host, workspace carving, and
 // launches on the caller's stream.
 #include "../../include/lvx.h"
 #include "lvx_internal.h"
@@ -89,7 +89,77 @@ lvx_status xent_args(const lvx_xent* p, lvx_dtype dtype, const void* x, const vo
   a->part = (float2*)at(plan->part); a->dx_part = (float*)at(plan->dx); a->g = at(plan->g);
   a->Mp = plan->Mp;
   a->slots = (int)plan->slots;
+  a->inv_t = 1.f;
   return LVX_OK;
+}
+// ... and of the backward pass
+lvx_status xent_bwd_args(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, const float* lse,
+                         const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes, XentArgs* a) {
+  Plan plan;
+  if (!lse || !d_loss || (!dx && !dw)) return LVX_ERR_NULL;
+  const lvx_status st = xent_args(p, dtype, x, w, labels, workspace, a, &plan);
+  if (st != LVX_OK) return st;
+  const size_t out = dtype == LVX_F32 ? 4 : 16;
+  if (!aligned(lse, 4) || !aligned(d_loss, 4) || !aligned(dx, out) || !aligned(dw, out) || dx == x) return LVX_ERR_STRIDE;
+  // the piece that there is room for
+  int64_t piece = piece_of(plan, p->V);
+  const int64_t room = workspace_bytes > plan.g ? ((int64_t)((workspace_bytes - plan.g) / plan.row) - PAD) / 256 * 256 : 0;
+  if (piece > room) piece = room;
+  if (piece < 256) return LVX_ERR_WORKSPACE;
+  if (gradients_in_operands(p, dtype == LVX_F32 ? 4 : 2, x, w, dx, dw)) return LVX_ERR_STRIDE;
+  a->piece = piece;
+  a->g_pitch = piece + PAD;
+  a->lse = lse; a->d_loss = d_loss; a->dx = dx; a->dw = dw;
+  // parts of dw, if there is room for them behind it
+  const int64_t cols = piece < p->V ? piece : p->V;
+  const size_t end = align_up(plan.g + (size_t)a->g_pitch * plan.row);
+  if (end + xent_dw_bytes(p->n, p->E, cols, a->n_cu, dtype == LVX_F32) <= workspace_bytes) {
+    a->dw_slots = (int)xent_dw_slots(p->n, p->E, cols, a->n_cu, dtype == LVX_F32);
+    a->dw_part = (float*)((char*)workspace + end);
+  }
+  return LVX_OK;
+}
+
+// Distillation: in front of the workspace of the cross entropy, what the tokens' entries need (backward: the first two of it)
+struct EntryPlan { size_t q_stat, sorted, rank, starts, z, fwd, bwd; };
+EntryPlan entries_of(int64_t n, int64_t V, int32_t K) {
+  EntryPlan e;
+  size_t at = align_up(n * 8);                       // (labels)
+  e.q_stat = at; at += align_up(n * 8);
+  e.bwd = at;
+  e.sorted = at; at += align_up((size_t)n * K * 4);
+  e.rank = at; at += align_up((size_t)n * K * 2);
+  e.starts = at; at += align_up((size_t)n * ((V + 63) / 64 + 1) * 2);
+  e.z = at; at += align_up((size_t)n * K * 4);
+  e.fwd = at;
+  return e;
+}
+bool entries_ok(int32_t K) { return K >= 1 && K <= DISTIL_MOST_ENTRIES; }
+// what a call names beside the product's operands
+lvx_status distil_check(const lvx_distil* p, lvx_dtype dtype, const int64_t* ids, const void* teacher, lvx_dtype teacher_dtype, const void* loss,
+                        const void* lse, const void* ln_p, const void* workspace) {
+  if (!p || !ids || !teacher || !loss || !lse || !ln_p) return LVX_ERR_NULL;
+  const lvx_status st = check_sizes(p->n, p->E, p->V, dtype);
+  if (st != LVX_OK) return st;
+  if (teacher_dtype != LVX_F32 && teacher_dtype != LVX_BF16) return LVX_ERR_DTYPE;
+  if (p->K < 1) return LVX_ERR_SHAPE;
+  if (!entries_ok(p->K)) return LVX_ERR_UNSUPPORTED;
+  if (!(p->temperature > 0.f) || !(1.f / p->temperature > 0.f) || !(1.f / p->temperature < __builtin_inff())) return LVX_ERR_SHAPE;
+  if (!aligned(ids, 8) || !aligned(teacher, teacher_dtype == LVX_F32 ? 4 : 2) || !aligned(loss, 4) || !aligned(lse, 4) || !aligned(ln_p, 4))
+    return LVX_ERR_STRIDE;
+  return workspace && aligned(workspace, ALIGN) ? LVX_OK : LVX_ERR_WORKSPACE;
+}
+void distil_args(const lvx_distil* p, const int64_t* ids, const void* teacher, lvx_dtype teacher_dtype, float* ln_p, void* workspace, XentArgs* a) {
+  const EntryPlan e = entries_of(p->n, p->V, p->K);
+  const auto at = [&](size_t o) -> char* { return (char*)workspace + o; };
+  a->temperature = p->temperature;
+  a->inv_t = 1.f / p->temperature;
+  a->z2 = (float)(1.4426950408889634 / p->temperature);
+  a->K = p->K;
+  a->blocks = (int)((p->V + 63) / 64);
+  a->ids = ids; a->teacher = teacher; a->teacher_bf16 = teacher_dtype == LVX_BF16; a->ln_p = ln_p;
+  a->q_stat = (float2*)at(e.q_stat); a->sorted = (int*)at(e.sorted); a->rank = (uint16_t*)at(e.rank); a->starts = (uint16_t*)at(e.starts);
+  a->z_entry = (float*)at(e.z);
 }
 
 }  // namespace
@@ -119,29 +189,47 @@ lvx_status lvx_xent_fwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const
 lvx_status lvx_xent_bwd(const lvx_xent* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* labels, const float* lse,
                         const float* d_loss, void* dx, void* dw, void* workspace, size_t workspace_bytes, void* hip_stream) {
   XentArgs a;
-  Plan plan;
-  if (!lse || !d_loss || (!dx && !dw)) return LVX_ERR_NULL;
-  const lvx_status st = xent_args(p, dtype, x, w, labels, workspace, &a, &plan);
+  const lvx_status st = xent_bwd_args(p, dtype, x, w, labels, lse, d_loss, dx, dw, workspace, workspace_bytes, &a);
   if (st != LVX_OK) return st;
-  const size_t out = dtype == LVX_F32 ? 4 : 16;
-  if (!aligned(lse, 4) || !aligned(d_loss, 4) || !aligned(dx, out) || !aligned(dw, out) || dx == x) return LVX_ERR_STRIDE;
-  // the piece that there is room for
-  int64_t piece = piece_of(plan, p->V);
-  const int64_t room = workspace_bytes > plan.g ? ((int64_t)((workspace_bytes - plan.g) / plan.row) - PAD) / 256 * 256 : 0;
-  if (piece > room) piece = room;
-  if (piece < 256) return LVX_ERR_WORKSPACE;
-  if (gradients_in_operands(p, dtype == LVX_F32 ? 4 : 2, x, w, dx, dw)) return LVX_ERR_STRIDE;
-  a.piece = piece;
-  a.g_pitch = piece + PAD;
-  a.lse = lse; a.d_loss = d_loss; a.dx = dx; a.dw = dw;
-  // parts of dw, if there is room for them behind it
-  const int64_t cols = piece < p->V ? piece : p->V;
-  const size_t end = align_up(plan.g + (size_t)a.g_pitch * plan.row);
-  if (end + xent_dw_bytes(p->n, p->E, cols, a.n_cu, dtype == LVX_F32) <= workspace_bytes) {
-    a.dw_slots = (int)xent_dw_slots(p->n, p->E, cols, a.n_cu, dtype == LVX_F32);
-    a.dw_part = (float*)((char*)workspace + end);
-  }
   return launch_xent_bwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
+}
+
+size_t lvx_distil_workspace_bytes(int64_t n, int32_t E, int64_t V, int32_t K, lvx_dtype dtype) {
+  if (check_sizes(n, E, V, dtype) != LVX_OK || !entries_ok(K)) return 0;
+  const EntryPlan e = entries_of(n, V, K);
+  const size_t fwd = e.fwd + align_up(plan_of(n, E, V, dtype).fwd), bwd = e.bwd + lvx_xent_workspace_bytes(n, E, V, dtype);
+  return fwd > bwd ? fwd : bwd;
+}
+
+lvx_status lvx_distil_fwd(const lvx_distil* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* ids, const void* teacher,
+                          lvx_dtype teacher_dtype, float* loss, float* lse, float* ln_p, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  lvx_status st = distil_check(p, dtype, ids, teacher, teacher_dtype, loss, lse, ln_p, workspace);
+  if (st != LVX_OK) return st;
+  const size_t own = entries_of(p->n, p->V, p->K).fwd;
+  const lvx_xent product = {p->n, p->V, p->E, p->x_ss};
+  XentArgs a;
+  Plan plan;
+  st = xent_args(&product, dtype, x, w, (const int64_t*)workspace, (char*)workspace + own, &a, &plan);
+  if (st != LVX_OK) return st;
+  if (workspace_bytes < own || workspace_bytes - own < plan.fwd) return LVX_ERR_WORKSPACE;
+  distil_args(p, ids, teacher, teacher_dtype, ln_p, workspace, &a);
+  a.loss = loss; a.lse_out = lse;
+  return launch_distil_fwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
+}
+
+lvx_status lvx_distil_bwd(const lvx_distil* p, lvx_dtype dtype, const void* x, const void* w, const int64_t* ids, const void* teacher,
+                          lvx_dtype teacher_dtype, const float* lse, const float* ln_p, const float* d_loss, void* dx, void* dw, void* workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+  lvx_status st = distil_check(p, dtype, ids, teacher, teacher_dtype, d_loss, lse, ln_p, workspace);
+  if (st != LVX_OK) return st;
+  const size_t own = entries_of(p->n, p->V, p->K).bwd;
+  if (workspace_bytes < own) return LVX_ERR_WORKSPACE;
+  const lvx_xent product = {p->n, p->V, p->E, p->x_ss};
+  XentArgs a;
+  st = xent_bwd_args(&product, dtype, x, w, (const int64_t*)workspace, lse, d_loss, dx, dw, (char*)workspace + own, workspace_bytes - own, &a);
+  if (st != LVX_OK) return st;
+  distil_args(p, ids, teacher, teacher_dtype, (float*)ln_p, workspace, &a);      // (read only)
+  return launch_distil_bwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
 }
 
 }  // extern "C"
