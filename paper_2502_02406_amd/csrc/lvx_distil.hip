@@ -26,12 +26,38 @@ __device__ __forceinline__ Entry entry_of(const XentArgs& a, long i, int k) {
 }
 __device__ __forceinline__ float ln_q_of(const Entry& e, float2 stat) { return (e.t - stat.x) - stat.y; }
 
+// Entries of token `tok` in the order of their ids, as row `row` of what the tiles look them up in, by a wave.  keys, sorted: K numbers of LDS each, keys
+// filled in by the wave.  All waves of the workgroup take part.
+__device__ __forceinline__ void sort_entries(const XentArgs& a, long row, const int* keys, int* sorted) {
+  const int lane = threadIdx.x & 63, K = a.K;
+  __syncthreads();
+  for (int k = lane; k < K; k += 64) {
+    const int mine = keys[k];
+    int r = 0;
+    for (int j = 0; j < K; ++j) r += keys[j] < mine || (keys[j] == mine && j < k);
+    sorted[r] = mine;
+    a.sorted[row * K + r] = mine;
+    a.rank[row * K + k] = (uint16_t)r;
+  }
+  __syncthreads();
+  for (int b = lane; b <= a.blocks; b += 64) {
+    int lo = 0, hi = K;                              // the first that is not below 64 b
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (sorted[mid] < 64 * b) lo = mid + 1;
+      else hi = mid;
+    }
+    a.starts[row * (a.blocks + 1) + b] = (uint16_t)lo;
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ int key_of(const XentArgs& a, long id) { return id >= 0 && id < a.V ? (int)id : 0x7fffffff; }
+
 // A wave a token: whether it takes part (a.labels: 0, -1 if not, V if an id is outside), the sum of its exponentials, and (SORT) its ids in order.
-template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kernel(XentArgs a) {
+template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kernel(XentArgs a, bool forward) {
   extern __shared__ __attribute__((aligned(16))) int prepare_mem[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K;
   int* const keys = prepare_mem + wave * 2 * K;
-  int* const sorted = keys + K;
   for (long base = blockIdx.x * 4L; base < a.n; base += gridDim.x * 4L) {
     const long i = min(base + wave, a.n - 1);        // (the last token again: the same results)
     float top = -__builtin_inff();
@@ -41,7 +67,7 @@ template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kerne
       any |= e.there && !(e.t == -__builtin_inff());
       far |= e.there && e.id >= a.V;
       if (e.there) top = fmaxf(top, e.t);            // (a NaN is dropped here and comes back in the sum)
-      if (SORT) keys[k] = e.there && e.id < a.V ? (int)e.id : 0x7fffffff;
+      if (SORT) keys[k] = key_of(a, e.id);
     }
     any = __any(any);
     far = __any(far);
@@ -51,6 +77,7 @@ template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kerne
     for (int k = lane; k < K; k += 64) {
       const Entry e = entry_of(a, i, k);
       sum += e.there ? expf(e.t - top) : 0.f;
+      if (forward && !any) a.ln_p[i * K + k] = 0.f;
     }
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
@@ -58,29 +85,19 @@ template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kerne
       ((int64_t*)a.labels)[i] = !any ? -1 : far ? a.V : 0;
       a.q_stat[i] = make_float2(top, logf(sum));
     }
-    if constexpr (SORT) {
-      __syncthreads();
-      for (int k = lane; k < K; k += 64) {
-        const int mine = keys[k];
-        int r = 0;
-        for (int j = 0; j < K; ++j) r += keys[j] < mine || (keys[j] == mine && j < k);
-        sorted[r] = mine;
-        a.sorted[i * K + r] = mine;
-        a.rank[i * K + k] = (uint16_t)r;
-        if (!any) a.ln_p[i * K + k] = 0.f;
-      }
-      __syncthreads();
-      for (int b = lane; b <= a.blocks; b += 64) {
-        int lo = 0, hi = K;                          // the first that is not below 64 b
-        while (lo < hi) {
-          const int mid = (lo + hi) / 2;
-          if (sorted[mid] < 64 * b) lo = mid + 1;
-          else hi = mid;
-        }
-        a.starts[i * (a.blocks + 1) + b] = (uint16_t)lo;
-      }
-      __syncthreads();
-    }
+    if constexpr (SORT) sort_entries(a, i, keys, keys + K);
+  }
+}
+// The listed tokens' ids in order
+__global__ void __launch_bounds__(256) distil_sort_kernel(XentArgs a) {
+  extern __shared__ __attribute__((aligned(16))) int prepare_mem[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K, count = a.head->count;
+  int* const keys = prepare_mem + wave * 2 * K;
+  for (int base = blockIdx.x * 4; base < count; base += gridDim.x * 4) {
+    const int r = min(base + wave, count - 1);
+    const long tok = a.tok[r];
+    for (int k = lane; k < K; k += 64) keys[k] = key_of(a, a.ids[tok * K + k]);
+    sort_entries(a, r, keys, keys + K);
   }
 }
 
@@ -120,10 +137,11 @@ __global__ void __launch_bounds__(256) distil_join_kernel(XentArgs a, int n_part
     if (r1 < count) {
       const float lse = a.labels[tok] < a.V ? lses[mine] : __builtin_nanf("");
       const float2 stat = a.q_stat[tok];
+      const long row = a.own ? tok : r1;             // among the entries
       float loss = 0.f;
       for (int k = threadIdx.x % 32; k < a.K; k += 32) {
         const Entry e = entry_of(a, tok, k);
-        const float z = e.there && e.id < a.V ? a.z_entry[(long)tok * a.K + a.rank[(long)tok * a.K + k]] : __builtin_nanf("");
+        const float z = e.there && e.id < a.V ? a.z_entry[row * a.K + a.rank[row * a.K + k]] : __builtin_nanf("");
         const float ln_p = z * a.inv_t - lse, ln_q = ln_q_of(e, stat), q = expf(ln_q);
         a.ln_p[(long)tok * a.K + k] = e.there ? ln_p : 0.f;
         loss += !e.there || q == 0.f ? 0.f : q * (ln_q - ln_p);
@@ -169,39 +187,38 @@ template <typename G> __global__ void __launch_bounds__(256) distil_entries_kern
   }
 }
 
-hipError_t prepare(const XentArgs& a, bool sort, hipStream_t s) {
-  const unsigned wgs = (unsigned)std::min(up(a.n, 4), 1L << 16);
-  if (sort) distil_prepare_kernel<true><<<wgs, 256, 4 * 2 * a.K * sizeof(int), s>>>(a);
-  else distil_prepare_kernel<false><<<wgs, 256, 0, s>>>(a);
-  return hipGetLastError();
-}
+unsigned waves_for(long n) { return (unsigned)std::min(up(n, 4), 1L << 16); }
+int entries_lds(const XentArgs& a) { return 4 * 2 * a.K * (int)sizeof(int); }
 hipError_t gradient(const XentArgs& a, int is_f32, hipStream_t s) {
   const hipError_t e = logits<GRAD, TEACHER>(a, is_f32, s);
   if (e != hipSuccess) return e;
-  const unsigned wgs = (unsigned)std::min(up(a.n, 4), 1L << 16);
-  if (is_f32) distil_entries_kernel<float><<<wgs, 256, 4 * 2 * a.K * sizeof(int), s>>>(a);
-  else distil_entries_kernel<__bf16><<<wgs, 256, 4 * 2 * a.K * sizeof(int), s>>>(a);
+  if (is_f32) distil_entries_kernel<float><<<waves_for(a.n), 256, entries_lds(a), s>>>(a);
+  else distil_entries_kernel<__bf16><<<waves_for(a.n), 256, entries_lds(a), s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_distil_fwd(XentArgs a, int is_f32, hipStream_t s) {
-  hipError_t e = prepare(a, true, s);
-  if (e != hipSuccess) return e;
   xent_fwd_sizes(&a, is_f32);
-  if (!a.own) {
-    e = launch_xent_list(a, s);
+  if (a.own) {
+    distil_prepare_kernel<true><<<waves_for(a.n), 256, entries_lds(a), s>>>(a, true);
+  } else {
+    distil_prepare_kernel<false><<<waves_for(a.n), 256, 0, s>>>(a, true);
+    const hipError_t e = launch_xent_list(a, s);
     if (e != hipSuccess) return e;
+    distil_sort_kernel<<<waves_for(a.n), 256, entries_lds(a), s>>>(a);
   }
-  e = logits<STATS, TEACHER>(a, is_f32, s);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess) e = logits<STATS, TEACHER>(a, is_f32, s);
   if (e != hipSuccess) return e;
   distil_join_kernel<<<(unsigned)std::min(up(a.n, 8), 4096L), 256, 0, s>>>(a, stat_parts_of(a, is_f32));
   return hipGetLastError();
 }
 
 hipError_t launch_distil_bwd(XentArgs a, int is_f32, hipStream_t s) {
-  const hipError_t e = prepare(a, false, s);
+  distil_prepare_kernel<false><<<waves_for(a.n), 256, 0, s>>>(a, false);
+  const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : launch_xent_products(a, is_f32, s, gradient);
 }
 

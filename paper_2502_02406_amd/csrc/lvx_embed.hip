@@ -114,12 +114,13 @@ inline Sort sort_of(long V) {
   return {(bits + passes - 1) / passes, passes};
 }
 
-// The rank of every token among those of its wave with the same digit, in order: ROUNDS x 64 tokens a wave, `dig` < 0: none.  cnt[digit]: the
+// The rank of every token among those of its wave with the same digit, in order: `rounds` x 64 tokens a wave, `dig` < 0: none.  cnt[digit]: the
 // wave's counts, which start at 0.
-template <int ROUNDS> __device__ __forceinline__ void rank_in_wave(const int (&dig)[ROUNDS], int (&rank)[ROUNDS], int* cnt, int bits) {
+template <int ROUNDS> __device__ __forceinline__ void rank_in_wave(const int (&dig)[ROUNDS], int (&rank)[ROUNDS], int rounds, int* cnt, int bits) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
+    if (r >= rounds) break;                          // (uniform)
     unsigned long long same = __ballot(dig[r] >= 0);
     for (int b = 0; b < bits; ++b) {
       const bool one = (dig[r] >> b) & 1;
@@ -214,7 +215,7 @@ template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < ONE_ROUNDS; ++r) dig[r] = key[r] < 0 ? -1 : (key[r] >> (p * bits)) & (digits - 1);
-    rank_in_wave<ONE_ROUNDS>(dig, rank, cnt + wave * digits, bits);
+    rank_in_wave<ONE_ROUNDS>(dig, rank, rounds, cnt + wave * digits, bits);
     __syncthreads();
     const int count = counts_to_starts(cnt, digits);
     const int at = exclusive_sum(count, sums, &m);
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(SORT_WG) embed_move_kernel(EmbedArgs a, int bi
       dig[r] = key[r] < 0 ? -1 : (key[r] >> (p * bits)) & (digits - 1);
     }
     __syncthreads();
-    rank_in_wave<RUN_ROUNDS>(dig, rank, cnt + wave * digits, bits);
+    rank_in_wave<RUN_ROUNDS>(dig, rank, RUN_ROUNDS, cnt + wave * digits, bits);
     __syncthreads();
     const int count = counts_to_starts(cnt, digits);
     __syncthreads();
@@ -437,14 +438,14 @@ template <typename T> __global__ void __launch_bounds__(256) embed_join_kernel(E
   for (long it = blockIdx.x; it < items; it += gridDim.x) {
     const int c0 = a.long_list[it / n_eb], e0 = (int)(it % n_eb) * 256, e = e0 + 4 * lane;
     const int id = a.key[0][(long)(c0 + 1) * a.chunk];
-    // behind the id's last token
-    int lo = (c0 + 1) * a.chunk, hi = m;             // key[lo] is the id; key[hi] is not (or is not there)
-    while (hi - lo > 1) {
-      const int mid = lo + (hi - lo) / 2;
-      if (a.key[0][mid] == id) lo = mid;
-      else hi = mid;
+    // the chunks that begin with the id follow each other: c0 + 1 ..
+    int parts = 1;
+    for (;;) {
+      const long at = (long)(c0 + parts + lane) * a.chunk;
+      const unsigned long long more = __ballot(at < m && a.key[0][min(at, (long)m - 1)] == id);
+      parts += more == ~0ull ? 64 : __ffsll(~more) - 1;
+      if (more != ~0ull) break;
     }
-    const int c1 = lo / a.chunk, parts = c1 - c0 + 1;            // chunks c0 .. c1
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     const int q1 = (int)((long)(wave + 1) * parts / 4);
     for (int q = (int)((long)wave * parts / 4); q < q1; q += 8) {

@@ -157,21 +157,21 @@ template <int JB, class Z> __device__ __forceinline__ float tile_pick(int g, int
   return y;
 }
 
-// A token's sorted entries of the teacher that lie in the 64 columns of the vocabulary around `col`
-struct Entries { int at, end; };
-__device__ __forceinline__ Entries entries_of(const XentArgs& a, int tok, int col) {
-  const uint16_t* const p = a.starts + (long)tok * (a.blocks + 1) + col / 64;
-  return {p[0], p[1]};
+// The sorted entries of row `row` (a listed token, or where every wave lists for itself a token) that lie in the 64 columns of the vocabulary around
+// `col`: the first one's number, and above it the one's behind the last.
+typedef unsigned __attribute__((aligned(2))) unsigned_any2;
+__device__ __forceinline__ unsigned entries_of(const XentArgs& a, long row, int col) {
+  return *(const unsigned_any2*)(a.starts + row * (a.blocks + 1) + min(col / 64, a.blocks - 1));
 }
-// Leaves the logits of those among the wave's 32 JB columns, of which `cw` is the first; z as above.  id: that of the first entry.
-__device__ __forceinline__ int entry_id(const XentArgs& a, int tok, const Entries& e) { return e.at < e.end ? a.sorted[(long)tok * a.K + e.at] : -1; }
-template <int JB, class Z> __device__ __forceinline__ void pick_entries(const XentArgs& a, int tok, Entries e, int id, int cw, int g, Z&& z) {
-  while (__any(e.at < e.end)) {
-    const int c = e.at < e.end ? id - cw : -1;
+__device__ __forceinline__ int entry_id(const XentArgs& a, long row, unsigned e) { return (e & 0xffffu) < e >> 16 ? a.sorted[row * a.K + (e & 0xffffu)] : -1; }
+// Leaves the logits of those among the wave's 32 JB columns, of which `cw` is the first; z as above, id: that of the first entry.
+template <int JB, class Z> __device__ __forceinline__ void pick_entries(const XentArgs& a, long row, unsigned e, int id, int cw, int g, Z&& z) {
+  while (__any((e & 0xffffu) < e >> 16)) {
+    const int c = (e & 0xffffu) < e >> 16 ? id - cw : -1;
     const float y = tile_pick<JB>(g, c, z);
-    if (c >= 0 && c < 32 * JB && ((c >> 2) & 1) == g) a.z_entry[(long)tok * a.K + e.at] = y;
-    ++e.at;
-    id = entry_id(a, tok, e);
+    if (c >= 0 && c < 32 * JB && ((c >> 2) & 1) == g) a.z_entry[row * a.K + (e & 0xffffu)] = y;
+    ++e;
+    id = entry_id(a, row, e);
   }
 }
 
@@ -386,7 +386,7 @@ xent_bf16_kernel(XentArgs a) {
     for (int j = 0; j < CB; ++j)
 #pragma unroll
       for (int i = 0; i < RB; ++i) { acc[j][i] = zero16(); asm volatile("" : "+a"(acc[j][i])); }
-    // what the epilogue needs of the rows, and the next tile's (lab: TEACHER: the rows' tokens)
+    // what the epilogue needs of the rows, and the next tile's (lab: TEACHER: the rows' entries)
     int lab[LOGITS ? RB : 1];
     float2 row[MODE == GRAD ? RB : 1];
     const auto load_rows = [&]() __attribute__((always_inline)) {
@@ -394,7 +394,8 @@ xent_bf16_kernel(XentArgs a) {
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
           const int r = min(cur.r0 + wm * 32 * RB + 32 * i + l31, M - 1);
-          if (LOSS == LABEL || MODE == STATS) lab[i] = LOSS == TEACHER ? a.tok[r] : a.lab[r];
+          if (LOSS == LABEL) lab[i] = a.lab[r];
+          else if (MODE == STATS) lab[i] = (int)entries_of(a, opaque(r), cur.c0 + wn * WC);
           if constexpr (MODE == GRAD) row[i] = a.row[r];
         }
       }
@@ -457,13 +458,13 @@ xent_bf16_kernel(XentArgs a) {
     if constexpr (MODE == STATS) {
       const int cw = cur.c0 + wn * WC, left = (int)min((long)WC, a.V - cw);      // columns of this wave
       float2* const sums = (float2*)(smem + RING_B);  // [NW / 2][TR]
-      Entries en[LOSS == TEACHER ? RB : 1];
+      int id[LOSS == TEACHER ? RB : 1];                // (on their way while the statistics are made)
       if constexpr (LOSS == TEACHER) {
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
-          const bool on = cur.r0 + wm * 32 * RB + 32 * i + l31 < M && left > 0;
-          const Entries e = entries_of(a, lab[i], left > 0 ? cw : 0);
-          en[i] = {e.at, on ? e.end : e.at};
+          const int r = opaque(cur.r0 + wm * 32 * RB + 32 * i + l31);
+          if (r >= M || left <= 0) lab[i] = 0;
+          id[i] = entry_id(a, r, (unsigned)lab[i]);
         }
       }
 #pragma unroll
@@ -481,13 +482,15 @@ xent_bf16_kernel(XentArgs a) {
           }
         }
       }
-      if constexpr (LOSS == TEACHER) {                  // (the first ids of all rows on their way at once)
-        int id[RB];
-#pragma unroll
-        for (int i = 0; i < RB; ++i) id[i] = entry_id(a, lab[i], en[i]);
+      if constexpr (LOSS == TEACHER) {
 #pragma unroll
         for (int i = 0; i < RB; ++i)
-          pick_entries<CB>(a, lab[i], en[i], id[i], cw, g, [&](int v, int j) __attribute__((always_inline)) -> float { return acc[j][i][v]; });
+          pick_entries<CB>(a, opaque(cur.r0 + wm * 32 * RB + 32 * i + l31), (unsigned)lab[i], id[i], cw, g,
+                           [&](int v, int j) __attribute__((always_inline)) -> float {      // (read where it stands: all of them, ahead of the loop, spill)
+                             float y;
+                             asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(acc[j][i][v]));
+                             return y;
+                           });
       }
       __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0)
       asm volatile("" ::: "memory");
@@ -635,16 +638,15 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
 #pragma unroll
   for (int i = 0; i < RB; ++i) acc[i] = zero16();
   constexpr bool PICK = MODE == STATS && LOSS == TEACHER;
-  int token[PICK ? RB : 1];                          // the rows' tokens and their entries (loaded in front of the copies, which then need not be waited for)
-  Entries en[PICK ? RB : 1];
+  int row_e[PICK ? RB : 1];                          // the rows' places among the entries, and those (loaded in front of the copies, which then need not be waited for)
+  unsigned en[PICK ? RB : 1];
   if constexpr (PICK) {
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
       const int r = 32 * i + l31;
-      token[i] = OWN ? __shfl(own.tok, min(r, M - 1)) : a.tok[min(r0 + r, M - 1)];
-      const bool on = r0 + r < M && c0 + 32 * wave < cols;
-      const Entries e = entries_of(a, token[i], c0 + 32 * wave < cols ? c0 + 32 * wave : 0);
-      en[i] = {e.at, on ? e.end : e.at};
+      row_e[i] = OWN ? __shfl(own.tok, min(r, M - 1)) : min(r0 + r, M - 1);
+      en[i] = entries_of(a, row_e[i], c0 + 32 * wave);
+      if (r0 + r >= M || c0 + 32 * wave >= cols) en[i] = 0u;
     }
   }
 #pragma unroll
@@ -681,7 +683,7 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
     int id[PICK ? RB : 1];
     if constexpr (PICK) {
 #pragma unroll
-      for (int i = 0; i < RB; ++i) id[i] = entry_id(a, token[i], en[i]);
+      for (int i = 0; i < RB; ++i) id[i] = entry_id(a, row_e[i], en[i]);
     }
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
@@ -691,7 +693,7 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       tile_stats<1>(g, left, log2_unit<LOSS>(a), z, &m2, &s);
       if (g == 0) sums[wave * 32 * RB + r] = make_float2(m2, s);
       if constexpr (LOSS == TEACHER) {
-        pick_entries<1>(a, token[i], en[i], id[i], c0 + cw, g, z);
+        pick_entries<1>(a, row_e[i], en[i], id[i], c0 + cw, g, z);
       } else {
         const int label = OWN ? __shfl(own.lab, r) : r0 + r < M ? a.lab[r0 + r] : -1;
         const int c = r0 + r < M ? label - c0 - cw : -1;
@@ -1007,10 +1009,9 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
       tile_stats<NB>(g, left, log2_unit<LOSS>(a), z, &m2, &s);
       if (g == 0 && r < M) a.part[(2L * ct + wn) * a.Mp + r] = make_float2(m2, s);
       if constexpr (LOSS == TEACHER) {
-        const int token = a.tok[min(r, M - 1)];
-        Entries e = entries_of(a, token, left > 0 ? cw : 0);
-        if (r >= M || left <= 0) e.end = e.at;
-        pick_entries<NB>(a, token, e, entry_id(a, token, e), cw, g, z);
+        const int row = min(r, M - 1);
+        const unsigned e = r < M && left > 0 ? entries_of(a, row, cw) : 0u;
+        pick_entries<NB>(a, row, e, entry_id(a, row, e), cw, g, z);
       } else {
         const int c = r < M ? a.lab[r] - cw : -1;
         if (__any(c >= 0 && c < FT / 2)) {
@@ -1129,8 +1130,7 @@ template <int MODE, int LOSS> __global__ void __launch_bounds__(256) xent_few_f3
     if (g == 0 && r < M) a.part[(long)ct * a.Mp + r] = make_float2(m2, s);
     if constexpr (LOSS == TEACHER) {
       const int token = __shfl(own.tok, min(r, M - 1));
-      Entries e = entries_of(a, token, c0);
-      if (r >= M) e.end = e.at;
+      const unsigned e = r < M ? entries_of(a, token, c0) : 0u;
       pick_entries<1>(a, token, e, entry_id(a, token, e), c0, g, z);
     } else {
       const int c = r < M ? label - c0 : -1;
