@@ -164,12 +164,22 @@ __device__ __forceinline__ unsigned entries_of(const XentArgs& a, long row, int 
   return *(const unsigned_any2*)(a.starts + row * (a.blocks + 1) + min(col / 64, a.blocks - 1));
 }
 __device__ __forceinline__ int entry_id(const XentArgs& a, long row, unsigned e) { return (e & 0xffffu) < e >> 16 ? a.sorted[row * a.K + (e & 0xffffu)] : -1; }
-// Leaves the logits of those among the wave's 32 JB columns, of which `cw` is the first; z as above, id: that of the first entry.
+// Leaves the logits of those among the wave's 32 JB columns, of which `cw` is the first; z as above, id: that of the first entry.  An entry's logit is
+// chosen by the bits of its column.
 template <int JB, class Z> __device__ __forceinline__ void pick_entries(const XentArgs& a, long row, unsigned e, int id, int cw, int g, Z&& z) {
+  const auto choose = [](int bit, float one, float zero) __attribute__((always_inline)) -> float { return bit ? one : zero; };
   while (__any((e & 0xffffu) < e >> 16)) {
     const int c = (e & 0xffffu) < e >> 16 ? id - cw : -1;
-    const float y = tile_pick<JB>(g, c, z);
-    if (c >= 0 && c < 32 * JB && ((c >> 2) & 1) == g) a.z_entry[row * a.K + (e & 0xffffu)] = y;
+    float y[JB];
+#pragma unroll
+    for (int j = 0; j < JB; ++j) {
+      float t[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        t[q] = choose(c & 2, choose(c & 1, z(4 * q + 3, j), z(4 * q + 2, j)), choose(c & 1, z(4 * q + 1, j), z(4 * q, j)));
+      y[j] = choose(c & 16, choose(c & 8, t[3], t[2]), choose(c & 8, t[1], t[0]));
+    }
+    if (c >= 0 && c < 32 * JB && ((c >> 2) & 1) == g) a.z_entry[row * a.K + (e & 0xffffu)] = JB == 2 ? choose(c & 32, y[JB - 1], y[0]) : y[0];
     ++e;
     id = entry_id(a, row, e);
   }
@@ -389,6 +399,7 @@ xent_bf16_kernel(XentArgs a) {
     // what the epilogue needs of the rows, and the next tile's (lab: TEACHER: the rows' entries)
     int lab[LOGITS ? RB : 1];
     float2 row[MODE == GRAD ? RB : 1];
+    constexpr bool PICK = MODE == STATS && LOSS == TEACHER;
     const auto load_rows = [&]() __attribute__((always_inline)) {
       if constexpr (LOGITS) {
 #pragma unroll
@@ -454,19 +465,21 @@ xent_bf16_kernel(XentArgs a) {
     for (int j = 0; j < CB; ++j)
 #pragma unroll
       for (int i = 0; i < RB; i += 2) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[j][i]), "+a"(acc[j][i + 1]));
+    int id[PICK ? RB : 1];
+    if constexpr (PICK) {                              // the rows' first entries (waited for here: behind the copies they would wait for these)
+      const int left = (int)min((long)WC, a.V - cur.c0 - wn * WC);
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        const int r = opaque(cur.r0 + wm * 32 * RB + 32 * i + l31);
+        if (r >= M || left <= 0) lab[i] = 0;
+        id[i] = entry_id(a, r, (unsigned)lab[i]);
+      }
+      __builtin_amdgcn_s_waitcnt(0x0070);
+    }
     if (MODE != DX && again) start(nxt);
     if constexpr (MODE == STATS) {
       const int cw = cur.c0 + wn * WC, left = (int)min((long)WC, a.V - cw);      // columns of this wave
       float2* const sums = (float2*)(smem + RING_B);  // [NW / 2][TR]
-      int id[LOSS == TEACHER ? RB : 1];                // (on their way while the statistics are made)
-      if constexpr (LOSS == TEACHER) {
-#pragma unroll
-        for (int i = 0; i < RB; ++i) {
-          const int r = opaque(cur.r0 + wm * 32 * RB + 32 * i + l31);
-          if (r >= M || left <= 0) lab[i] = 0;
-          id[i] = entry_id(a, r, (unsigned)lab[i]);
-        }
-      }
 #pragma unroll
       for (int i = 0; i < RB; ++i) {
         const int rl = wm * 32 * RB + 32 * i + l31, r = cur.r0 + rl;
@@ -482,7 +495,7 @@ xent_bf16_kernel(XentArgs a) {
           }
         }
       }
-      if constexpr (LOSS == TEACHER) {
+      if constexpr (PICK) {
 #pragma unroll
         for (int i = 0; i < RB; ++i)
           pick_entries<CB>(a, opaque(cur.r0 + wm * 32 * RB + 32 * i + l31), (unsigned)lab[i], id[i], cw, g,
