@@ -154,8 +154,9 @@ __device__ __forceinline__ int exclusive_sum(int x, int* at, int* total) {
   *total = all;
   return before + upto - x;
 }
-// LDS of the sort: counts [waves][digits], where every digit starts [digits], exclusive_sum's [waves]
-inline int sort_lds(int bits) { return (int)sizeof(int) * ((SORT_WAVES + 1) * (1 << bits) + SORT_WAVES); }
+// LDS of the sort: counts [waves][digits] (or two numbers a thread), where every digit starts [digits], exclusive_sum's [waves]
+__host__ __device__ constexpr int sort_counts(int digits) { return SORT_WAVES * digits > 2 * SORT_WG ? SORT_WAVES * digits : 2 * SORT_WG; }
+inline int sort_lds(int bits) { return (int)sizeof(int) * (sort_counts(1 << bits) + (1 << bits) + SORT_WAVES); }
 // Turns the waves' counts of a digit (thread t: digit t) into where the wave's first one stands among all of the workgroup's; returns how many there are.
 __device__ __forceinline__ int counts_to_starts(int* cnt, int digits) {
   int run = 0;
@@ -170,7 +171,9 @@ __device__ __forceinline__ int counts_to_starts(int* cnt, int digits) {
 __device__ __forceinline__ void clear_counts(int* cnt, int digits) {
   for (int i = threadIdx.x; i < SORT_WAVES * digits; i += SORT_WG) cnt[i] = 0;
 }
-// The table's rows set to 0, in whole (of `elements`): workgroup `wg` of `wgs`.
+// Elements of the table's gradient that a launch of the sort sets to 0 beside its own work, by `wgs` further workgroups: the sort keeps few compute units busy, and
+// rows that no token has, most of a large table's, have to be written anyway.  (Those that tokens have are written again behind it.)
+struct Clear { long from, count; unsigned wgs; };
 template <typename T> __device__ __forceinline__ void clear_table(T* p, long elements, long wg, long wgs) {
   // (up to the first 16-byte boundary, and behind the last one, by single elements)
   const long head = min(elements, (long)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T))), vecs = (elements - head) * (long)sizeof(T) / 16;
@@ -183,19 +186,18 @@ template <typename T> __device__ __forceinline__ void clear_table(T* p, long ele
   }
 }
 
-// All digits by one workgroup, for up to ONE_WG tokens; the other workgroups clear the table meanwhile (rows that tokens have are written again
-// behind it).
+// All digits by one workgroup, for up to ONE_WG tokens.
 constexpr int ONE_ROUNDS = 8, ONE_WG = SORT_WG * ONE_ROUNDS;
 inline int one_lds(int bits, long n) { return sort_lds(bits) + 2 * (int)sizeof(int) * (int)((n + SORT_WG - 1) / SORT_WG * SORT_WG); }
-template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_kernel(EmbedArgs a, int bits, int passes) {
+template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_kernel(EmbedArgs a, int bits, int passes, Clear clear) {
   if (blockIdx.x > 0) {
-    clear_table((T*)a.d_table, a.V * a.E, blockIdx.x - 1, gridDim.x - 1);
+    clear_table((T*)a.d_table + clear.from, clear.count, blockIdx.x - 1, clear.wgs);
     return;
   }
   extern __shared__ __attribute__((aligned(16))) int sort_mem[];
   const int digits = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int* const cnt = sort_mem;
-  int* const start = cnt + SORT_WAVES * digits;
+  int* const start = cnt + sort_counts(digits);
   int* const sums = start + digits;
   int* const skey = sums + SORT_WAVES;
   const int per_wave = (int)((a.n + SORT_WG - 1) / SORT_WG) * 64, rounds = per_wave / 64;
@@ -219,7 +221,10 @@ template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_
     __syncthreads();
     const int count = counts_to_starts(cnt, digits);
     const int at = exclusive_sum(count, sums, &m);
-    if (tid < digits) start[tid] = at;
+    if (tid < digits) {
+      start[tid] = at;
+      if (p == passes - 1) a.top[tid] = at;
+    }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < ONE_ROUNDS; ++r)
@@ -246,14 +251,15 @@ template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_
     }
   }
   if (tid == 0) {
+    a.top[digits] = m;
     a.head->count = m;
-    a.head->n_long = 0;
+    a.head->n_many = a.head->n_few = 0;
   }
 }
 
 // More tokens: a pass is two launches of up to EMBED_BLOCKS workgroups, each with a run of the tokens; the first counts the digits of every run, the
 // second moves the tokens.  Pass 0 reads the ids and leaves tokens out that have no row.
-constexpr int RUN_ROUNDS = 4, RUN_STEP = SORT_WG * RUN_ROUNDS;
+constexpr int RUN_ROUNDS = 2, RUN_STEP = SORT_WG * RUN_ROUNDS;
 inline long run_of(long n) { return std::max((long)RUN_STEP, (n + EMBED_BLOCKS * SORT_WG - 1) / (EMBED_BLOCKS * SORT_WG) * SORT_WG); }
 __device__ __forceinline__ int sort_key(const EmbedArgs& a, int p, int from, long i, long n) {
   if (i >= n) return -1;
@@ -275,28 +281,40 @@ __global__ void __launch_bounds__(SORT_WG) embed_count_kernel(EmbedArgs a, int b
   __syncthreads();
   for (int i = tid; i < digits; i += SORT_WG) a.hist[(long)blockIdx.x * digits + i] = sort_mem[i];
 }
-__global__ void __launch_bounds__(SORT_WG) embed_move_kernel(EmbedArgs a, int bits, int p, int from, int to, long run, int last) {
+template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_move_kernel(EmbedArgs a, int bits, int p, int from, int to, long run, int blocks, int last, Clear clear) {
+  if ((int)blockIdx.x >= blocks) {
+    clear_table((T*)a.d_table + clear.from, clear.count, blockIdx.x - blocks, clear.wgs);
+    return;
+  }
   extern __shared__ __attribute__((aligned(16))) int sort_mem[];
   const int digits = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int* const cnt = sort_mem;
-  int* const start = cnt + SORT_WAVES * digits;
+  int* const start = cnt + sort_counts(digits);
   int* const sums = start + digits;
   const long n = p > 0 ? a.head->count : a.n, begin = blockIdx.x * run, end = min(n, begin + run);
-  // where this run's tokens of every digit go: behind all smaller digits, and behind the runs before
+  // where this run's tokens of every digit go: behind all smaller digits, and behind the runs before.  Several threads add up a digit's counts.
+  const int per = SORT_WG / digits, digit = tid & (digits - 1), part = tid / digits;
   int all = 0, before = 0;
-  if (tid < digits) {
-    for (int b0 = 0; b0 < (int)gridDim.x; b0 += 8) {
-      int c[8];
+  for (int b0 = part; b0 < blocks; b0 += 8 * per) {
+    int c[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) c[k] = a.hist[(long)min(b0 + k, (int)gridDim.x - 1) * digits + tid];
+    for (int k = 0; k < 8; ++k) c[k] = a.hist[(long)min(b0 + k * per, blocks - 1) * digits + digit];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int b = b0 + k;
-        all += b < (int)gridDim.x ? c[k] : 0;
-        before += b < (int)blockIdx.x ? c[k] : 0;
-      }
+    for (int k = 0; k < 8; ++k) {
+      const int b = b0 + k * per;
+      all += b < blocks ? c[k] : 0;
+      before += b < min(blocks, (int)blockIdx.x) ? c[k] : 0;
     }
   }
+  cnt[2 * tid] = all;
+  cnt[2 * tid + 1] = before;
+  __syncthreads();
+  all = before = 0;
+  if (tid < digits)
+    for (int k = 0; k < per; ++k) {
+      all += cnt[2 * (tid + k * digits)];
+      before += cnt[2 * (tid + k * digits) + 1];
+    }
   int m;
   const int at = exclusive_sum(all, sums, &m);
   if (tid < digits) start[tid] = at + before;
@@ -307,7 +325,7 @@ __global__ void __launch_bounds__(SORT_WG) embed_move_kernel(EmbedArgs a, int bi
     }
     if (tid == 0) {
       if (p == 0) a.head->count = m;                 // (pass 0 does not read it)
-      a.head->n_long = 0;
+      a.head->n_many = a.head->n_few = 0;
     }
   }
   for (long base = begin; base < end; base += RUN_STEP) {
@@ -340,12 +358,12 @@ __global__ void __launch_bounds__(SORT_WG) embed_move_kernel(EmbedArgs a, int bi
 
 // ---- backward: the sums ----
 
-template <typename T> __device__ __forceinline__ void finish_row(const EmbedArgs& a, int id, int e, int there, const float (&s)[V8]) {
+constexpr int MANY_PARTS = 32;
+
+template <typename T, bool ADD> __device__ __forceinline__ void finish_row(const EmbedArgs& a, int id, int e, int there, const float (&s)[V8], const Piece<T>& old) {
   T* const to = (T*)a.d_table + (long)id * a.E + e;
   float v[V8];
-  if (a.accumulate) {
-    Piece<T> old;
-    old.load(to, there);
+  if constexpr (ADD) {
 #pragma unroll
     for (int j = 0; j < V8; ++j) v[j] = fmaf(s[j], a.scale, old[j]);
   } else {
@@ -379,11 +397,14 @@ template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs
   }
 }
 
-// Sums over a chunk of the sorted tokens, by a team; workgroups from `sums` on clear rows (low: bits of an id below its last digit)
-template <typename T> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, int tl, unsigned sums_x, int n_eb, int low) {
-  if (blockIdx.x >= sums_x) {
-    clear_rows<T>(a, blockIdx.x - sums_x, low);
-    return;
+// Sums over a chunk of the sorted tokens, by a team (ADD: to what is there); workgroups from `sums_x` on clear rows, the first of them piece `early` of the table
+// (low: bits of an id below its last digit)
+template <typename T, bool ADD> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, int tl, unsigned sums_x, int n_eb, long early, int low) {
+  if constexpr (!ADD) {
+    if (blockIdx.x >= sums_x) {
+      clear_rows<T>(a, early + (blockIdx.x - sums_x), low);
+      return;
+    }
   }
   const int E = a.E, lane = threadIdx.x & ((1 << tl) - 1), eb = (int)(blockIdx.x % n_eb), e = ((eb << tl) + lane) * V8, there = E - e;
   const long c = (long)(blockIdx.x / n_eb) * (256 >> tl) + (threadIdx.x >> tl), p0 = c * a.chunk;
@@ -392,91 +413,110 @@ template <typename T> __global__ void __launch_bounds__(256) embed_sum_kernel(Em
   const int first = (int)p0, end = (int)min((long)m, p0 + a.chunk);
   const int *const key = a.key[0], *const tok = a.tok[0];
   const int prev = first > 0 ? key[first - 1] : -1, next = end < m ? key[end] : -1;
-  int cur = key[first];
-  bool before = prev == cur;
+  bool before = prev == key[first];
   float s[V8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const auto flush = [&](bool after) {
-    if (!before && !after) {
-      finish_row<T>(a, cur, e, there, s);
-    } else {
-      Piece<float>::store(a.part + (2 * c + (before ? 0 : 1)) * E + e, there, s);
-    }
-  };
-  constexpr int U = 8;                               // rows on their way at once
+  constexpr int U = ADD ? 4 : 8;                     // rows on their way at once
   for (int p = first; p < end; p += U) {
     int id[U];
-    Piece<T> x[U];
+    Piece<T> x[U], old[ADD ? U : 1];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       id[k] = key[min(p + k, end - 1)];
       x[k].load((const T*)a.d_y + tok[min(p + k, end - 1)] * a.y_ss + e, there);
     }
+    if constexpr (ADD) {                             // (of an id that is finished here: nobody else writes its row)
+#pragma unroll
+      for (int k = 0; k < U; ++k) old[k].load((const T*)a.d_table + (long)id[k] * E + e, there);
+    }
 #pragma unroll
     for (int k = 0; k < U; ++k)
       if (p + k < end) {
-        if (id[k] != cur) {
-          flush(false);
-#pragma unroll
-          for (int j = 0; j < V8; ++j) s[j] = 0.f;
-          cur = id[k];
-          before = false;
-        }
 #pragma unroll
         for (int j = 0; j < V8; ++j) s[j] += x[k][j];
+        // the last of its id in this chunk?
+        const int q = p + k + 1, following = q < end ? (k + 1 < U ? id[min(k + 1, U - 1)] : key[q]) : -1;
+        if (following != id[k]) {
+          const bool after = q == end && next == id[k];
+          if (!before && !after) {
+            finish_row<T, ADD>(a, id[k], e, there, s, old[ADD ? k : 0]);
+          } else {
+            Piece<float>::store(a.part + (2 * c + (before ? 0 : 1)) * E + e, there, s);
+            if (after && !before && e == 0) {        // (the lists' order changes no result)
+              const long far = (c + MANY_PARTS) * a.chunk;
+              if (far < m && key[far] == id[k]) a.long_list[atomicAdd(&a.head->n_many, 1)] = make_int2((int)c, id[k]);
+              else a.long_list[a.list_end - 1 - atomicAdd(&a.head->n_few, 1)] = make_int2((int)c, id[k]);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < V8; ++j) s[j] = 0.f;
+          before = false;
+        }
       }
   }
-  const bool after = next == cur;
-  flush(after);
-  if (after && !before && e == 0) a.long_list[atomicAdd(&a.head->n_long, 1)] = (int)c;      // (their order changes no result)
 }
 
-// Ids that go over several chunks: 256 features a workgroup, its four waves with a run of the chunks each.
-template <typename T> __global__ void __launch_bounds__(256) embed_join_kernel(EmbedArgs a, int n_eb) {
+// Ids that go over several chunks.  Of more than MANY_PARTS: 256 features a workgroup, its four waves with a run of the chunks each; of fewer, most of them:
+// 256 features a wave.
+template <typename T> __global__ void __launch_bounds__(256) embed_join_kernel(EmbedArgs a) {
   __shared__ float sums[4][256];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.E, m = a.head->count;
-  const long items = (long)a.head->n_long * n_eb;
+  const long n_many = (long)a.head->n_many * ((E + 255) / 256), items = n_many + (long)a.head->n_few * ((E + 1023) / 1024);
   for (long it = blockIdx.x; it < items; it += gridDim.x) {
-    const int c0 = a.long_list[it / n_eb], e0 = (int)(it % n_eb) * 256, e = e0 + 4 * lane;
-    const int id = a.key[0][(long)(c0 + 1) * a.chunk];
+    const bool many = it < n_many;                   // (uniform)
+    const int of = many ? (E + 255) / 256 : (E + 1023) / 1024;
+    const long at = many ? it : it - n_many;
+    const int2 run = many ? a.long_list[at / of] : a.long_list[a.list_end - 1 - at / of];
+    const int c0 = run.x, id = run.y, e0 = many ? (int)(at % of) * 256 : (int)(at % of) * 1024 + 256 * wave, e = e0 + 4 * lane;
     // the chunks that begin with the id follow each other: c0 + 1 ..
     int parts = 1;
     for (;;) {
-      const long at = (long)(c0 + parts + lane) * a.chunk;
-      const unsigned long long more = __ballot(at < m && a.key[0][min(at, (long)m - 1)] == id);
+      const long first = (long)(c0 + parts + lane) * a.chunk;
+      const unsigned long long more = __ballot(first < m && a.key[0][min(first, (long)m - 1)] == id);
       parts += more == ~0ull ? 64 : __ffsll(~more) - 1;
       if (more != ~0ull) break;
     }
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    const int q1 = (int)((long)(wave + 1) * parts / 4);
-    for (int q = (int)((long)wave * parts / 4); q < q1; q += 8) {
-      float v[8][4];
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    const int q0 = many ? (int)((long)wave * parts / 4) : 0, q1 = many ? (int)((long)(wave + 1) * parts / 4) : parts;
+    const auto sum = [&](auto whole) {
+      for (int q = q0; q < q1; q += 8) {
+        f32x4 v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int c = c0 + min(q + k, q1 - 1);
-        const float* const from = a.part + (2L * c + (c == c0 ? 1 : 0)) * E + e;
+        for (int k = 0; k < 8; ++k) {
+          const int c = c0 + min(q + k, q1 - 1);
+          const float* const from = a.part + (2L * c + (c == c0 ? 1 : 0)) * E + e;
+          if constexpr (decltype(whole)::value) {
+            v[k] = __builtin_bit_cast(f32x4, *(const u32x4_any4*)from);
+          } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[k][j] = e + j < E ? from[j] : 0.f;
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (q + k < q1) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) s[j] += v[k][j];
+            for (int j = 0; j < 4; ++j) v[k][j] = e + j < E ? from[j] : 0.f;
+          }
         }
-    }
-    __syncthreads();                                 // (the sums of the id before have been read)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sums[wave][4 * lane + j] = s[j];
-    __syncthreads();
-    if (e0 + tid < E) {
-      const float all = (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]);
-      T* const to = (T*)a.d_table + (long)id * E + e0 + tid;
-      *to = (T)(a.accumulate ? fmaf(all, a.scale, (float)*to) : all * a.scale);
+        for (int k = 0; k < 8; ++k)
+          if (q + k < q1) s += v[k];
+      }
+    };
+    if (e0 + 256 <= E) sum(std::true_type{});
+    else sum(std::false_type{});
+    if (many) {
+      __syncthreads();                               // (the sums of the id before have been read)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sums[wave][4 * lane + j] = s[j];
+      __syncthreads();
+      s = (*(const f32x4*)&sums[0][4 * lane] + *(const f32x4*)&sums[1][4 * lane]) + (*(const f32x4*)&sums[2][4 * lane] + *(const f32x4*)&sums[3][4 * lane]);
+      if (wave > 0) continue;
     }
+    T* const to = (T*)a.d_table + (long)id * E + e;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (e + j < E) to[j] = (T)(a.accumulate ? fmaf(s[j], a.scale, (float)to[j]) : s[j] * a.scale);
   }
 }
 
 long up(long n, long by) { return (n + by - 1) / by; }
+
+// Bytes of the table that a launch of the sort clears: about what goes to memory in its time.
+constexpr long CLEAR_ONE = 16 << 20, CLEAR_ROUND = 8 << 20, CLEAR_MOVE = 48 << 20;
 
 template <typename T> hipError_t embed_fwd(const EmbedArgs& a, hipStream_t s) {
   const int tl = team_log(a.E);
@@ -484,59 +524,71 @@ template <typename T> hipError_t embed_fwd(const EmbedArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T> hipError_t embed_bwd(const EmbedArgs& a, hipStream_t s) {
+// Workgroups that clear `bytes` of the table, of those that are left from row `*row` on, in whole pieces of `piece` rows
+template <typename T> Clear clear_some(const EmbedArgs& a, long bytes, long piece, long* row) {
+  const long rows = std::min(a.V - *row, up(bytes, (long)sizeof(T) * a.E * piece) * piece);
+  const Clear c = {*row * a.E, rows * a.E, (unsigned)std::min(4L * a.n_cu, up(rows * a.E, SORT_WG * 16))};
+  *row += rows;
+  return c;
+}
+template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStream_t s) {
   const Sort sort = sort_of(a.V);
-  const bool one = a.n <= ONE_WG;
+  const int low = sort.bits * (sort.passes - 1);
+  const long piece = 1L << std::min(low, ROWS_LOG);
+  long row = ADD ? a.V : 0;                          // the rows before are cleared already
   hipError_t e;
-  if (one) {
+  if (a.n <= ONE_WG) {
     static SmemOnce once;
     e = ensure_dynamic_lds((const void*)embed_sort_one_kernel<T>, one_lds(EMBED_DIGIT_BITS, ONE_WG), &once);
     if (e != hipSuccess) return e;
-    const long clear = a.accumulate ? 0 : std::min(4L * a.n_cu, up(a.V * a.E, SORT_WG * 16));
-    embed_sort_one_kernel<T><<<(unsigned)(1 + clear), SORT_WG, one_lds(sort.bits, a.n), s>>>(a, sort.bits, sort.passes);
+    const Clear clear = clear_some<T>(a, CLEAR_ONE + CLEAR_ROUND * up(a.n, SORT_WG), piece, &row);
+    embed_sort_one_kernel<T><<<1 + clear.wgs, SORT_WG, one_lds(sort.bits, a.n), s>>>(a, sort.bits, sort.passes, clear);
   } else {
     static SmemOnce once;
-    e = ensure_dynamic_lds((const void*)embed_move_kernel, sort_lds(EMBED_DIGIT_BITS), &once);
+    e = ensure_dynamic_lds((const void*)embed_move_kernel<T>, sort_lds(EMBED_DIGIT_BITS), &once);
     if (e != hipSuccess) return e;
     const long run = run_of(a.n);
     const unsigned blocks = (unsigned)up(a.n, run);
     for (int p = 0; p < sort.passes; ++p) {
       const int to = (sort.passes - 1 - p) % 2, from = 1 - to;
       embed_count_kernel<<<blocks, SORT_WG, (1 << sort.bits) * sizeof(int), s>>>(a, sort.bits, p, from, run);
-      embed_move_kernel<<<blocks, SORT_WG, sort_lds(sort.bits), s>>>(a, sort.bits, p, from, to, run, p == sort.passes - 1);
+      const Clear clear = clear_some<T>(a, CLEAR_MOVE, piece, &row);
+      embed_move_kernel<T><<<blocks + clear.wgs, SORT_WG, sort_lds(sort.bits), s>>>(a, sort.bits, p, from, to, run, (int)blocks, p == sort.passes - 1, clear);
     }
   }
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int tl = team_log(a.E), n_eb = (int)up(a.E, V8 << tl), low = sort.bits * (sort.passes - 1);
+  const int tl = team_log(a.E), n_eb = (int)up(a.E, V8 << tl);
   const long n_chunks = up(a.n, a.chunk), wgs = up(n_chunks, 256 >> tl) * n_eb;
-  const long clear = one || a.accumulate ? 0 : up(a.V, 1L << std::min(low, ROWS_LOG));
-  embed_sum_kernel<T><<<(unsigned)(wgs + clear), 256, 0, s>>>(a, tl, (unsigned)wgs, n_eb, low);
+  embed_sum_kernel<T, ADD><<<(unsigned)(wgs + up(a.V - row, piece)), 256, 0, s>>>(a, tl, (unsigned)wgs, n_eb, row / piece, low);
   if (n_chunks > 1) {
-    const int eb = (int)up(a.E, 256);
-    embed_join_kernel<T><<<(unsigned)std::min((n_chunks - 1) * eb, 4L * a.n_cu), 256, 0, s>>>(a, eb);
+    embed_join_kernel<T><<<(unsigned)std::min((n_chunks - 1) * up(a.E, 256), 8L * a.n_cu), 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-// Sorted tokens of a chunk: 8 to 64, so that there are threads for about 2^17 pieces of 8 features.
+// Sorted tokens of a chunk: 4 to 64, so that there are threads for about 2^18 pieces of 8 features.
+constexpr int LEAST_CHUNK = 4;
 int embed_chunk(long n, int E) {
-  int c = 8;
-  while (c < 64 && n * chunks8(E) / c > (1L << 17)) c *= 2;
+  int c = LEAST_CHUNK;
+  while (c < 64 && n * chunks8(E) / c > (1L << 18)) c *= 2;
   return c;
 }
-// Chunks are the shorter the less there is: of n E / 8 = P pieces or fewer, no more than min(P / 8, max(2^17, P / 64)) chunk pieces and a row of them.
+long embed_chunks_room(long n) { return n / LEAST_CHUNK + 1; }
+// Chunks are the shorter the less there is: of n E / 8 = P pieces or fewer, no more than min(P / 4, max(2^18, P / 64)) chunk pieces and a row of them.
 size_t embed_part_room(long n, int E) {
   const long P = n * chunks8(E);
-  return 2 * sizeof(float) * (size_t)V8 * (std::min(P / 8, std::max(1L << 17, P / 64)) + chunks8(E) + 1);
+  return 2 * sizeof(float) * (size_t)V8 * (std::min(P / LEAST_CHUNK, std::max(1L << 18, P / 64)) + chunks8(E) + 1);
 }
 
 hipError_t launch_embed_fwd(const EmbedArgs& a, int is_f32, hipStream_t s) { return is_f32 ? embed_fwd<float>(a, s) : embed_fwd<__bf16>(a, s); }
 hipError_t launch_embed_bwd(EmbedArgs a, int is_f32, hipStream_t s) {
   a.chunk = embed_chunk(a.n, a.E);
-  return is_f32 ? embed_bwd<float>(a, s) : embed_bwd<__bf16>(a, s);
+  a.list_end = embed_chunks_room(a.n);
+  if (a.accumulate) return is_f32 ? embed_bwd<float, true>(a, s) : embed_bwd<__bf16, true>(a, s);
+  return is_f32 ? embed_bwd<float, false>(a, s) : embed_bwd<__bf16, false>(a, s);
 }
 
 }  // namespace lvx

@@ -36,7 +36,7 @@ Plan plan_of(int64_t n, int32_t E) {
   for (size_t& l : p.list) { l = at; at += align_up(n * sizeof(int)); }
   p.hist = at; at += (size_t)EMBED_BLOCKS * EMBED_DIGITS * sizeof(int);
   p.top = at; at += align_up((EMBED_DIGITS + 1) * sizeof(int));
-  p.long_list = at; at += align_up((n / 8 + 1) * sizeof(int));
+  p.long_list = at; at += align_up(embed_chunks_room(n) * sizeof(int2));
   p.part = at; at += align_up(embed_part_room(n, E));
   p.all = at;
   return p;
@@ -70,7 +70,7 @@ lvx_status lvx_embed_bwd(const lvx_embed* p, lvx_dtype dtype, const void* d_y, c
     a.key[i] = (int*)at(plan.list[i]);
     a.tok[i] = (int*)at(plan.list[2 + i]);
   }
-  a.hist = (int*)at(plan.hist); a.top = (int*)at(plan.top); a.long_list = (int*)at(plan.long_list); a.part = (float*)at(plan.part);
+  a.hist = (int*)at(plan.hist); a.top = (int*)at(plan.top); a.long_list = (int2*)at(plan.long_list); a.part = (float*)at(plan.part);
   return launch_embed_bwd(a, dtype == LVX_F32, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
 }
 
