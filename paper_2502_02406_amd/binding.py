@@ -506,7 +506,21 @@ def _of(t, dtype, *shape) -> bool:
     return t.shape == shape and t.dtype == dtype and t.is_contiguous()
 
 
-_norms = {}
+def _at(t):
+    return t.data_ptr() if t is not None else None
+
+
+_structs = {}
+
+
+def _struct(cls, *key):
+    """The struct of these sizes (made once for a set of them: 1 us a call)."""
+    p = _structs.get((cls, key))
+    if p is None:
+        if len(_structs) >= 256:
+            _structs.clear()
+        p = _structs[cls, key] = cls(*key)
+    return p
 
 
 def _norm_struct(where, like_x, like_y, gamma, stats, rms, eps):
@@ -521,13 +535,7 @@ def _norm_struct(where, like_x, like_y, gamma, stats, rms, eps):
         raise ValueError(f"{where}: gamma has to be [{E}] of y's type")
     if stats.numel() != 2 * n or stats.dtype != torch.float32 or not stats.is_contiguous():
         raise ValueError(f"{where}: stats has to be float32 [{n}, 2]")
-    key = (n, E, 1 if rms else 0, x_ss, y_ss, eps)
-    p = _norms.get(key)                              # (made once for a set of sizes: 1 us a call)
-    if p is None:
-        if len(_norms) >= 256:
-            _norms.clear()
-        p = _norms[key] = lvx_norm(*key)
-    return p
+    return _struct(lvx_norm, n, E, 1 if rms else 0, x_ss, y_ss, eps)
 
 
 def lvx_norm_fwd(x, gamma, beta, y, stats, rms: bool = False, eps: float = 1e-5, packed: Optional[Packed] = None) -> None:
@@ -651,7 +659,7 @@ def _distil_struct(where, x, w, ids, teacher, ln_p, per_token, workspace, temper
             raise ValueError(f"{where}: loss, lse and d_loss have to be float32 [{n}], contiguous")
     if not workspace.is_contiguous():
         raise ValueError(f"{where}: the workspace has to be contiguous")
-    return lvx_distil(n, w.shape[0], E, K, x_ss, temperature)
+    return _struct(lvx_distil, n, w.shape[0], E, K, x_ss, temperature)
 
 
 def lvx_distil_fwd(x, w, ids, teacher, loss, lse, ln_p, workspace, temperature: float = 1.0) -> None:
@@ -678,9 +686,9 @@ def lvx_distil_bwd(x, w, ids, teacher, lse, ln_p, d_loss, dx=None, dw=None, work
         raise ValueError(f"{where}: dx has to have x's shape, strides and type")
     if dw is not None and (dw.shape != w.shape or dw.dtype != w.dtype or not dw.is_contiguous()):
         raise ValueError(f"{where}: dw has to be [{p.V}, {p.E}] of w's type, contiguous")
-    at = lambda t: t.data_ptr() if t is not None else None
-    _check(load().lvx_distil_bwd(C.byref(p), dtype_code(x.dtype), at(x), at(w), at(ids), at(teacher), dtype_code(teacher.dtype), at(lse), at(ln_p),
-                                 at(d_loss), at(dx), at(dw), at(workspace), workspace.numel() * workspace.element_size(), s), where)
+    _check(load().lvx_distil_bwd(C.byref(p), dtype_code(x.dtype), x.data_ptr(), w.data_ptr(), ids.data_ptr(), teacher.data_ptr(), dtype_code(teacher.dtype),
+                                 lse.data_ptr(), ln_p.data_ptr(), d_loss.data_ptr(), _at(dx), _at(dw), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), s), where)
 
 
 # ---- at either end of a step: token features from a table, losses of whole sequences ----
@@ -695,7 +703,7 @@ def _embed_struct(where, table, ids, y, scale):
         raise ValueError(f"{where}: the table has to be [V, {E}] of the rows' type, contiguous")
     if ids.numel() != n or ids.dtype != torch.int64 or not ids.is_contiguous():
         raise ValueError(f"{where}: ids have to be int64 [{n}], contiguous")
-    return lvx_embed(n, table.shape[0], E, scale, y_ss)
+    return _struct(lvx_embed, n, table.shape[0], E, scale, y_ss)
 
 
 def lvx_embed_fwd(table, ids, y, scale: float = 1.0) -> None:
@@ -727,27 +735,31 @@ def lvx_policy_workspace_bytes(n: int, S: int) -> int:
     return int(load().lvx_policy_workspace_bytes(n, S))
 
 
-def _floats(where, name, t, *numbers):
-    """t (float32, contiguous) has one of these numbers of elements."""
-    if t is not None and (t.numel() not in numbers or t.dtype != torch.float32 or not t.is_contiguous()):
-        raise ValueError(f"{where}: {name} has to be float32, contiguous, of {' or '.join(map(str, numbers))} elements")
+def _are_floats(n, *ts) -> bool:
+    for t in ts:
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
+            return False
+    return True
 
 
-def _sequences(where, tokens, labels, first, d_loss, d_nll, workspace):
-    """(tokens, sequences); tokens: the float32 tensors of one value a token, by name."""
-    n = labels.numel()
-    if labels.dtype != torch.int64 or not labels.is_contiguous():
+def _sequences(where, tokens, per_sequence, labels, first, d_loss, d_nll, workspace, pairs):
+    """(tokens, sequences or pairs); tokens, per_sequence: the float32 tensors of one value each."""
+    n, count = labels.numel(), first.numel() - 1
+    if labels.dtype is not torch.int64 or not labels.is_contiguous():
         raise ValueError(f"{where}: labels have to be int64, contiguous")
-    if first.dim() != 1 or first.dtype != torch.int64 or not first.is_contiguous():
-        raise ValueError(f"{where}: first has to be int64, one dimension, contiguous")
+    if first.dim() != 1 or first.dtype is not torch.int64 or not first.is_contiguous() or count < (2 if pairs else 1) or (pairs and count % 2 != 0):
+        raise ValueError(f"{where}: first has to be int64 [{'2 S' if pairs else 'S'} + 1], contiguous")
+    if pairs:
+        count //= 2
     if (d_loss is None) != (d_nll is None):
         raise ValueError(f"{where}: d_loss and d_nll, both or neither")
-    for name, t in tokens:
-        _floats(where, name, t, n)
-    _floats(where, "d_nll", d_nll, n)
+    if not _are_floats(n, d_nll, *tokens):
+        raise ValueError(f"{where}: what belongs to the tokens has to be float32 [{n}], contiguous")
+    if not _are_floats(count, d_loss, *per_sequence):
+        raise ValueError(f"{where}: what belongs to the {'pairs' if pairs else 'sequences'} has to be float32 [{count}], contiguous")
     if not workspace.is_contiguous():
         raise ValueError(f"{where}: the workspace has to be contiguous")
-    return n, first.numel() - 1
+    return n, count
 
 
 def lvx_preference(nll, ref, labels, first, loss, margin=None, d_loss=None, d_nll=None, workspace=None, form: str = "logistic",
@@ -759,17 +771,12 @@ def lvx_preference(nll, ref, labels, first, loss, margin=None, d_loss=None, d_nl
     if workspace is None:
         raise ValueError(f"{w}: no workspace")
     s = _on_device(w, nll, ref, labels, first, loss, margin, d_loss, d_nll, workspace)
-    n, count = _sequences(w, (("nll", nll), ("ref", ref)), labels, first, d_loss, d_nll, workspace)
-    if count < 2 or count % 2 != 0:
-        raise ValueError(f"{w}: first has to have 2 S + 1 entries")
-    for name, t in (("loss", loss), ("margin", margin), ("d_loss", d_loss)):
-        _floats(w, name, t, count // 2)
+    n, S = _sequences(w, (nll, ref), (loss, margin), labels, first, d_loss, d_nll, workspace, True)
     if form not in LVX_PREF_FORMS:
         raise ValueError(f"{w}: form is one of {', '.join(LVX_PREF_FORMS)}")
-    p = lvx_pref(n, count // 2, LVX_PREF_FORMS[form], beta, smoothing)
-    at = lambda t: t.data_ptr() if t is not None else None
-    _check(load().lvx_preference(C.byref(p), at(nll), at(ref), at(labels), at(first), at(loss), at(margin), at(d_loss), at(d_nll), at(workspace),
-                                 workspace.numel() * workspace.element_size(), s), w)
+    p = _struct(lvx_pref, n, S, LVX_PREF_FORMS[form], beta, smoothing)
+    _check(load().lvx_preference(C.byref(p), nll.data_ptr(), _at(ref), labels.data_ptr(), first.data_ptr(), loss.data_ptr(), _at(margin), _at(d_loss),
+                                 _at(d_nll), workspace.data_ptr(), workspace.numel() * workspace.element_size(), s), w)
 
 
 def lvx_policy(nll, old, ref, adv, labels, first, loss, stats=None, d_loss=None, d_nll=None, workspace=None, clip=(0.2, 0.2), beta: float = 0.0,
@@ -782,14 +789,12 @@ def lvx_policy(nll, old, ref, adv, labels, first, loss, stats=None, d_loss=None,
     if workspace is None:
         raise ValueError(f"{w}: no workspace")
     s = _on_device(w, nll, old, ref, adv, labels, first, loss, stats, d_loss, d_nll, workspace)
-    n, count = _sequences(w, (("nll", nll), ("old", old), ("ref", ref)), labels, first, d_loss, d_nll, workspace)
-    if count < 1:
-        raise ValueError(f"{w}: first has to have S + 1 entries")
-    for name, t, numbers in (("loss", loss, (count,)), ("stats", stats, (3 * count,)), ("d_loss", d_loss, (count,)), ("adv", adv, (count, n))):
-        _floats(w, name, t, *numbers)
+    n, S = _sequences(w, (nll, old, ref), (loss,), labels, first, d_loss, d_nll, workspace, False)
+    per_token = adv.numel() != S
+    if not _are_floats(n if per_token else S, adv) or not _are_floats(3 * S, stats):
+        raise ValueError(f"{w}: adv has to be float32 [{S}] or [{n}], stats [{S}, 3], contiguous")
     if ref is None and beta != 0.0:
         raise ValueError(f"{w}: a divergence needs ref")
-    p = lvx_clip(n, count, int(mean), int(adv.numel() != count), clip[0], clip[1], beta)
-    at = lambda t: t.data_ptr() if t is not None else None
-    _check(load().lvx_policy(C.byref(p), at(nll), at(old), at(ref), at(adv), at(labels), at(first), at(loss), at(stats), at(d_loss), at(d_nll),
-                             at(workspace), workspace.numel() * workspace.element_size(), s), w)
+    p = _struct(lvx_clip, n, S, 1 if mean else 0, 1 if per_token else 0, clip[0], clip[1], beta)
+    _check(load().lvx_policy(C.byref(p), nll.data_ptr(), old.data_ptr(), _at(ref), adv.data_ptr(), labels.data_ptr(), first.data_ptr(), loss.data_ptr(),
+                             _at(stats), _at(d_loss), _at(d_nll), workspace.data_ptr(), workspace.numel() * workspace.element_size(), s), w)

@@ -305,7 +305,7 @@ struct SequenceArgs {
   double low, high, ln_low, ln_high;    // a ratio's bounds, and their logarithms
   void *head, *block;   // workspace: sums of every sequence's first piece, and of every block of tokens that goes on in one
 };
-constexpr int SEQUENCE_BLOCK = 2048;    // tokens of a block
+constexpr int SEQUENCE_BLOCK = 1024;    // tokens of a block
 size_t sequence_part_bytes();           // of one of these sums
 hipError_t launch_preference(const SequenceArgs& a, hipStream_t s);
 hipError_t launch_policy(const SequenceArgs& a, hipStream_t s);

@@ -21,27 +21,23 @@ namespace lvx {
 
 namespace {
 
+__device__ __forceinline__ double other(double x, int o) { return __shfl_xor(x, o); }
+__device__ __forceinline__ int other(int x, int o) { return __shfl_xor(x, o); }
 struct PrefPart {
   double s;
-  __device__ void add(const PrefPart& o) { s += o.s; }
+  __device__ __forceinline__ void add(const PrefPart& o) { s += o.s; }
+  __device__ __forceinline__ PrefPart from_lane(int o) const { return {other(s, o)}; }
 };
 struct PolicyPart {
   double loss, kl;
   int count, clipped;
-  __device__ void add(const PolicyPart& o) { loss += o.loss; kl += o.kl; count += o.count; clipped += o.clipped; }
+  __device__ __forceinline__ void add(const PolicyPart& o) { loss += o.loss; kl += o.kl; count += o.count; clipped += o.clipped; }
+  __device__ __forceinline__ PolicyPart from_lane(int o) const { return {other(loss, o), other(kl, o), other(count, o), other(clipped, o)}; }
 };
-template <class P> __device__ __forceinline__ P from_lane(const P& x, int o) {
-  P y;
-  const int* const a = (const int*)&x;
-  int* const b = (int*)&y;
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof(P) / 4); ++i) b[i] = __shfl_xor(a[i], o);
-  return y;
-}
 // Sums over the workgroup, the same in every thread (`at`: a place a wave in LDS)
 template <class P> __device__ __forceinline__ P wg_sum(P x, P* at) {
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) x.add(from_lane(x, o));
+  for (int o = 1; o < 64; o *= 2) x.add(x.from_lane(o));
   const int waves = blockDim.x >> 6;
   if (waves == 1) return x;
   __syncthreads();
@@ -59,32 +55,96 @@ __device__ __forceinline__ Span span_of(const SequenceArgs& a, long s) {
   return {b, max(b, e)};
 }
 
-// ---- a token ----
-__device__ __forceinline__ void token_pref(const SequenceArgs& a, long i, PrefPart* p) {
-  const bool on = a.labels[i] >= 0;
-  const float nll = a.nll[i], ref = a.ref ? a.ref[i] : 0.f;
-  p->s += on ? (double)ref - (double)nll : 0.0;
+// exp(x) in 64 bits, off by some 1e-14 of itself: 2^k by the exponent, the rest, up to ln 2 / 2, by its series (the last term left out is 6e-15).
+__device__ __forceinline__ double exp_of(double x) {
+  x = x < -800.0 ? -800.0 : x > 800.0 ? 800.0 : x;  // (a NaN stays one)
+  const double k = rint(x * 1.4426950408889634);
+  double r = fma(k, -0.693147180369123816490, x);    // (ln 2 in two parts, of which the first has zeros at its end)
+  r = fma(k, -1.90821492927058770002e-10, r);
+  double p = 1.0 / 39916800.0;
+  const double c[11] = {1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+  for (int i = 0; i < 11; ++i) p = fma(p, r, c[i]);
+  return ldexp(p, (int)k);
 }
-// adv: the sequence's advantage.  Returns the gradient of the token's loss (0 without a label).
-__device__ __forceinline__ double token_policy(const SequenceArgs& a, long i, float adv, PolicyPart* p) {
-  const bool on = a.labels[i] >= 0;
-  const double nll = a.nll[i], old = a.old[i], ref = a.beta != 0.0 ? a.ref[i] : 0.f, A = a.per_token ? a.adv[i] : adv;
-  if (!on) return 0.0;
+// exp(x) - 1 - x, to the last digits for small x too: x^2 times a series up to 1/2 (the last term left out is 2e-17 of the sum)
+__device__ __forceinline__ double exp_less_line(double x) {
+  double p = 1.0 / 6227020800.0;
+  const double c[11] = {1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5};
+#pragma unroll
+  for (int i = 0; i < 11; ++i) p = fma(p, x, c[i]);
+  return fabs(x) <= 0.5 ? p * x * x : exp_of(x) - 1.0 - x;
+}
+
+// ---- tokens: U of a thread on their way at once, `wg` apart (behind the last one that one again) ----
+constexpr int U = 4;
+struct Batch { long label[U]; float nll[U], ref[U], old[U], adv[U]; };
+template <bool POLICY> __device__ __forceinline__ void load(const SequenceArgs& a, long t, long end, long wg, Batch* b) {
+#pragma unroll
+  for (int k = 0; k < U; ++k) {
+    const long i = min(t + k * wg, end - 1);
+    b->label[k] = a.labels[i];
+    b->nll[k] = a.nll[i];
+    b->ref[k] = (POLICY ? a.beta != 0.0 : a.ref != nullptr) ? a.ref[i] : 0.f;
+    if (POLICY) {
+      b->old[k] = a.old[i];
+      b->adv[k] = a.per_token ? a.adv[i] : 0.f;
+    }
+  }
+}
+__device__ __forceinline__ void sum_pref(const Batch& b, long t, long end, long wg, PrefPart* p) {
+#pragma unroll
+  for (int k = 0; k < U; ++k) p->s += t + k * wg < end && b.label[k] >= 0 ? (double)b.ref[k] - (double)b.nll[k] : 0.0;
+}
+// d_nll = d where there is a label
+__device__ __forceinline__ void put_pref(const SequenceArgs& a, const long (&label)[U], long t, long end, long wg, float d) {
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+    if (t + k * wg < end) a.d_nll[t + k * wg] = label[k] >= 0 ? d : 0.f;
+}
+__device__ __forceinline__ void load_labels(const SequenceArgs& a, long t, long end, long wg, long (&label)[U]) {
+#pragma unroll
+  for (int k = 0; k < U; ++k) label[k] = a.labels[min(t + k * wg, end - 1)];
+}
+// One token's share of the loss; returns the gradient.  A: its advantage.
+__device__ __forceinline__ double token_policy(const SequenceArgs& a, double nll, double old, double ref, double A, PolicyPart* p) {
   const double gone = old - nll;
-  const double ratio = exp(gone);
+  const double ratio = exp_of(gone);
   // (by logarithms, of which the difference is exact)
   const bool over = A > 0.0 ? gone > a.ln_high : A < 0.0 && gone < a.ln_low;
-  double loss = over ? -(A > 0.0 ? a.high : a.low) * A : -ratio * A, slope = over ? 0.0 : ratio * A;
+  const double high = a.high, low = a.low;
+  double loss = over ? -(A > 0.0 ? high : low) * A : -ratio * A, slope = over ? 0.0 : ratio * A;
   if (a.beta != 0.0) {
-    const double d = nll - ref, up = expm1(d);
-    loss += a.beta * (up - d);
-    slope += a.beta * up;
-    p->kl += up - d;
+    const double d = nll - ref, more = exp_less_line(d);
+    loss += a.beta * more;
+    slope += a.beta * (more + d);
+    p->kl += more;
   }
   p->loss += loss;
   p->count += 1;
   p->clipped += over;
   return slope;
+}
+// adv: the sequence's advantage, d: what the gradients are multiplied by
+__device__ __forceinline__ void do_policy(const SequenceArgs& a, Batch& b, long t, long end, long wg, float adv, float d, PolicyPart* p) {
+  if (!a.per_token) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) b.adv[k] = adv;
+  }
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+    if (t + k * wg < end) {
+      const double slope = b.label[k] >= 0 ? token_policy(a, b.nll[k], b.old[k], b.ref[k], b.adv[k], p) : 0.0;
+      if (a.d_nll) a.d_nll[t + k * wg] = b.label[k] >= 0 ? (float)(slope * (double)d) : 0.f;
+    }
+}
+__device__ __forceinline__ void scale_policy(const SequenceArgs& a, long t, long end, long wg, float by) {
+  float x[U];
+#pragma unroll
+  for (int k = 0; k < U; ++k) x[k] = a.d_nll[min(t + k * wg, end - 1)];
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+    if (t + k * wg < end) a.d_nll[t + k * wg] = x[k] * by;
 }
 
 // ---- a pair ----
@@ -112,18 +172,30 @@ __device__ __forceinline__ void put_stats(const SequenceArgs& a, long s, const P
 }
 
 // ---- few tokens: a pair or a sequence a workgroup ----
+__device__ __forceinline__ PrefPart sum_span(const SequenceArgs& a, const Span& s) {
+  PrefPart p{};
+  for (long t = s.begin + threadIdx.x; t < s.end; t += U * blockDim.x) {
+    Batch b;
+    load<false>(a, t, s.end, blockDim.x, &b);
+    sum_pref(b, t, s.end, blockDim.x, &p);
+  }
+  return p;
+}
+__device__ __forceinline__ void put_span(const SequenceArgs& a, const Span& s, float d) {
+  for (long t = s.begin + threadIdx.x; t < s.end; t += U * blockDim.x) {
+    long label[U];
+    load_labels(a, t, s.end, blockDim.x, label);
+    put_pref(a, label, t, s.end, blockDim.x, d);
+  }
+}
 __global__ void __launch_bounds__(1024) preference_one_kernel(SequenceArgs a) {
   __shared__ PrefPart at[16];
-  const long pairs = a.count / 2, wg = blockDim.x;
+  const long pairs = a.count / 2;
   for (long i = blockIdx.x; i < pairs; i += gridDim.x) {
     const Span c = span_of(a, i), r = span_of(a, pairs + i);
-    PrefPart pc{}, pr{};
-#pragma unroll 4
-    for (long t = c.begin + threadIdx.x; t < c.end; t += wg) token_pref(a, t, &pc);
-#pragma unroll 4
-    for (long t = r.begin + threadIdx.x; t < r.end; t += wg) token_pref(a, t, &pr);
-    pc.s -= pr.s;
-    const double margin = wg_sum(pc, at).s;
+    PrefPart p = sum_span(a, c);
+    p.s -= sum_span(a, r).s;
+    const double margin = wg_sum(p, at).s;
     double slope;
     const double loss = pair_loss(a, margin, &slope);
     if (threadIdx.x == 0) {
@@ -132,10 +204,8 @@ __global__ void __launch_bounds__(1024) preference_one_kernel(SequenceArgs a) {
     }
     if (!a.d_nll) continue;
     const float d = (float)(slope * (double)a.d_loss[i]);
-#pragma unroll 4
-    for (long t = c.begin + threadIdx.x; t < c.end; t += wg) a.d_nll[t] = a.labels[t] >= 0 ? -d : 0.f;
-#pragma unroll 4
-    for (long t = r.begin + threadIdx.x; t < r.end; t += wg) a.d_nll[t] = a.labels[t] >= 0 ? d : 0.f;
+    put_span(a, c, -d);
+    put_span(a, r, d);
   }
 }
 __global__ void __launch_bounds__(1024) policy_one_kernel(SequenceArgs a) {
@@ -145,15 +215,15 @@ __global__ void __launch_bounds__(1024) policy_one_kernel(SequenceArgs a) {
     const Span c = span_of(a, i);
     const float adv = a.per_token ? 0.f : a.adv[i], d = a.d_nll ? a.d_loss[i] : 0.f;
     PolicyPart p{};
-    for (long t = c.begin + threadIdx.x; t < c.end; t += wg) {
-      const double slope = token_policy(a, t, adv, &p);
-      if (a.d_nll) a.d_nll[t] = (float)(a.labels[t] >= 0 ? slope * (double)d : 0.0);
+    for (long t = c.begin + threadIdx.x; t < c.end; t += U * wg) {
+      Batch b;
+      load<true>(a, t, c.end, wg, &b);
+      do_policy(a, b, t, c.end, wg, adv, d, &p);
     }
     p = wg_sum(p, at);
     if (threadIdx.x == 0) put_stats(a, i, p);
     if (!a.d_nll || !a.mean || p.count == 0) continue;
-    const float per = (float)(1.0 / p.count);
-    for (long t = c.begin + threadIdx.x; t < c.end; t += wg) a.d_nll[t] *= per;      // (what this thread has written)
+    for (long t = c.begin + threadIdx.x; t < c.end; t += U * wg) scale_policy(a, t, c.end, wg, (float)(1.0 / p.count));      // (what this thread has written)
   }
 }
 
@@ -162,14 +232,15 @@ __global__ void __launch_bounds__(1024) policy_one_kernel(SequenceArgs a) {
 // Workgroups 0 .. count - 1: a sequence up to the first multiple of SEQUENCE_BLOCK behind its start; the others: from a multiple on, where it is inside
 // a sequence.  (seq < 0: nothing)
 struct Job { long seq, begin, end; };
+__device__ __forceinline__ bool is_block(const SequenceArgs& a) { return blockIdx.x >= a.count; }
+__device__ __forceinline__ long block_begin(const SequenceArgs& a) { return (blockIdx.x - a.count) * SEQUENCE_BLOCK; }
 __device__ __forceinline__ Job job_of(const SequenceArgs& a, int* lds) {
   constexpr long P = SEQUENCE_BLOCK;
-  const long b = blockIdx.x;
-  if (b < a.count) {
-    const Span s = span_of(a, b);
-    return {b, s.begin, min(s.end, (s.begin / P + 1) * P)};
+  if (!is_block(a)) {
+    const Span s = span_of(a, blockIdx.x);
+    return {blockIdx.x, s.begin, min(s.end, (s.begin / P + 1) * P)};
   }
-  const long x = (b - a.count) * P;
+  const long x = block_begin(a);
   long lo = 0, hi = a.count + 1;                     // first[lo] <= x < first[hi] (or the ends)
   while (hi - lo > 1) {
     const long step = (hi - lo + 255) / 256, at = lo + (long)threadIdx.x * step;
@@ -196,27 +267,34 @@ template <class P> __device__ __forceinline__ P share_of(const SequenceArgs& a, 
 }
 template <class P> __device__ __forceinline__ void leave(const SequenceArgs& a, const P& p) {
   if (threadIdx.x != 0) return;
-  if (blockIdx.x < a.count) ((P*)a.head)[blockIdx.x] = p;
+  if (!is_block(a)) ((P*)a.head)[blockIdx.x] = p;
   else ((P*)a.block)[blockIdx.x - a.count] = p;
 }
+static_assert(SEQUENCE_BLOCK == 256 * U, "a piece is one batch of a workgroup");
 
 __global__ void __launch_bounds__(256) preference_sum_kernel(SequenceArgs a) {
   __shared__ PrefPart at[4];
   __shared__ int found[4];
+  Batch b;
+  if (is_block(a)) load<false>(a, block_begin(a) + threadIdx.x, a.n, 256, &b);       // (ahead of the search for its sequence)
   const Job j = job_of(a, found);
   if (j.seq < 0) return;
+  const long t = j.begin + threadIdx.x;
+  if (!is_block(a) && j.begin < j.end) load<false>(a, t, j.end, 256, &b);
   PrefPart p{};
-#pragma unroll 8
-  for (long t = j.begin + threadIdx.x; t < j.end; t += 256) token_pref(a, t, &p);
+  sum_pref(b, t, j.end, 256, &p);
   leave(a, wg_sum(p, at));
 }
 __global__ void __launch_bounds__(256) preference_grad_kernel(SequenceArgs a) {
   __shared__ PrefPart at[4];
   __shared__ int found[4];
+  long label[U];
+  if (is_block(a)) load_labels(a, block_begin(a) + threadIdx.x, a.n, 256, label);
   const Job j = job_of(a, found);
   if (j.seq < 0) return;
+  const long t = j.begin + threadIdx.x;
+  if (!is_block(a) && j.begin < j.end) load_labels(a, t, j.end, 256, label);
   const long pairs = a.count / 2, i = j.seq < pairs ? j.seq : j.seq - pairs;
-  if (i >= pairs) return;
   PrefPart pc = share_of<PrefPart>(a, span_of(a, i), i);
   pc.s -= share_of<PrefPart>(a, span_of(a, pairs + i), pairs + i).s;
   const double margin = wg_sum(pc, at).s;
@@ -227,22 +305,21 @@ __global__ void __launch_bounds__(256) preference_grad_kernel(SequenceArgs a) {
     if (a.margin) a.margin[i] = (float)margin;
   }
   if (!a.d_nll) return;
-  float d = (float)(slope * (double)a.d_loss[i]);
-  if (j.seq < pairs) d = -d;
-#pragma unroll 8
-  for (long t = j.begin + threadIdx.x; t < j.end; t += 256) a.d_nll[t] = a.labels[t] >= 0 ? d : 0.f;
+  const float d = (float)(slope * (double)a.d_loss[i]);
+  put_pref(a, label, t, j.end, 256, j.seq < pairs ? -d : d);
 }
 __global__ void __launch_bounds__(256) policy_sum_kernel(SequenceArgs a) {
   __shared__ PolicyPart at[4];
   __shared__ int found[4];
+  Batch b;
+  if (is_block(a)) load<true>(a, block_begin(a) + threadIdx.x, a.n, 256, &b);
   const Job j = job_of(a, found);
   if (j.seq < 0) return;
+  const long t = j.begin + threadIdx.x;
+  if (!is_block(a) && j.begin < j.end) load<true>(a, t, j.end, 256, &b);
   const float adv = a.per_token ? 0.f : a.adv[j.seq], d = a.d_nll ? a.d_loss[j.seq] : 0.f;
   PolicyPart p{};
-  for (long t = j.begin + threadIdx.x; t < j.end; t += 256) {
-    const double slope = token_policy(a, t, adv, &p);
-    if (a.d_nll) a.d_nll[t] = (float)(a.labels[t] >= 0 ? slope * (double)d : 0.0);
-  }
+  do_policy(a, b, t, j.end, 256, adv, d, &p);
   leave(a, wg_sum(p, at));
 }
 // The sequences' losses, and (mean) the gradients divided by the tokens' number
@@ -252,11 +329,9 @@ __global__ void __launch_bounds__(256) policy_finish_kernel(SequenceArgs a) {
   const Job j = job_of(a, found);
   if (j.seq < 0) return;
   const PolicyPart p = wg_sum(share_of<PolicyPart>(a, span_of(a, j.seq), j.seq), at);
-  if (blockIdx.x < a.count && threadIdx.x == 0) put_stats(a, j.seq, p);
-  if (!a.d_nll || !a.mean || p.count == 0) return;
-  const float per = (float)(1.0 / p.count);
-#pragma unroll 8
-  for (long t = j.begin + threadIdx.x; t < j.end; t += 256) a.d_nll[t] *= per;
+  if (!is_block(a) && threadIdx.x == 0) put_stats(a, j.seq, p);
+  if (!a.d_nll || !a.mean || p.count == 0 || j.begin == j.end) return;
+  scale_policy(a, j.begin + threadIdx.x, j.end, 256, (float)(1.0 / p.count));
 }
 
 constexpr long ONE_TOKENS = 32768;

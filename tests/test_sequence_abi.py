@@ -67,10 +67,11 @@ def test_binding_checks():
     n, S = 10, 2
     f, i = torch.zeros(n), torch.zeros(n, dtype=torch.int64)
     first, one, ws = torch.arange(2 * S + 1), torch.zeros(S), torch.zeros(64)
-    good = dict(where="t", tokens=(("nll", f),), labels=i, first=first, d_loss=one, d_nll=f, workspace=ws)
-    assert B._sequences(**good) == (n, 2 * S)
-    for bad in (dict(labels=i.int()), dict(labels=i[::2]), dict(first=first.int()), dict(first=first.view(1, -1)), dict(d_loss=None),
-                dict(tokens=(("nll", f[:3]),)), dict(tokens=(("nll", f.double()),)), dict(d_nll=f[:4]), dict(workspace=torch.zeros(4, 4).t())):
+    good = dict(where="t", tokens=(f, None), per_sequence=(one,), labels=i, first=first, d_loss=one, d_nll=f, workspace=ws, pairs=True)
+    assert B._sequences(**good) == (n, S)
+    for bad in (dict(labels=i.int()), dict(labels=i[::2]), dict(first=first.int()), dict(first=first.view(1, -1)), dict(first=first[:4]), dict(first=first[:1]),
+                dict(d_loss=None), dict(tokens=(f[:3],)), dict(tokens=(f.double(),)), dict(per_sequence=(f,)), dict(d_nll=f[:4]),
+                dict(workspace=torch.zeros(4, 4).t())):
         with pytest.raises(ValueError):
             B._sequences(**{**good, **bad})
     with pytest.raises(ValueError):
