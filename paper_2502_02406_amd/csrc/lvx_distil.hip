@@ -26,40 +26,62 @@ __device__ __forceinline__ Entry entry_of(const XentArgs& a, long i, int k) {
 }
 __device__ __forceinline__ float ln_q_of(const Entry& e, float2 stat) { return (e.t - stat.x) - stat.y; }
 
-// Entries of token `tok` in the order of their ids, as row `row` of what the tiles look them up in, by a wave.  keys, sorted: K numbers of LDS each, keys
-// filled in by the wave.  All waves of the workgroup take part.
+// K entries in LDS, rounded up to four
+constexpr int NO_KEY = 0x7fffffff;
+__host__ __device__ constexpr int entries_up(int K) { return (K + 3) / 4 * 4; }
+// A token's entries in the order of their ids, as row `row` of what the tiles look them up in, by a workgroup.  keys: filled in by it, NO_KEY behind the last one.
 __device__ __forceinline__ void sort_entries(const XentArgs& a, long row, const int* keys, int* sorted) {
-  const int lane = threadIdx.x & 63, K = a.K;
+  const int tid = threadIdx.x, K = a.K, K4 = entries_up(K);
   __syncthreads();
-  for (int k = lane; k < K; k += 64) {
+  for (int k = tid; k < K4; k += 256) {
     const int mine = keys[k];
     int r = 0;
-    for (int j = 0; j < K; ++j) r += keys[j] < mine || (keys[j] == mine && j < k);
-    sorted[r] = mine;
-    a.sorted[row * K + r] = mine;
-    a.rank[row * K + k] = (uint16_t)r;
+#pragma unroll 4
+    for (int j = 0; j < K4; j += 4) {
+      const int4 y = *(const int4*)(keys + j);
+      r += y.x < mine || (y.x == mine && j < k);
+      r += y.y < mine || (y.y == mine && j + 1 < k);
+      r += y.z < mine || (y.z == mine && j + 2 < k);
+      r += y.w < mine || (y.w == mine && j + 3 < k);
+    }
+    sorted[r] = mine;                                // (those behind K stay there)
+    if (k < K) {
+      a.sorted[row * K + r] = mine;
+      a.rank[row * K + k] = (uint16_t)r;
+    }
   }
   __syncthreads();
-  for (int b = lane; b <= a.blocks; b += 64) {
-    int lo = 0, hi = K;                              // the first that is not below 64 b
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (sorted[mid] < 64 * b) lo = mid + 1;
-      else hi = mid;
-    }
-    a.starts[row * (a.blocks + 1) + b] = (uint16_t)lo;
-  }
+  // how many are below 64 b, two b of a thread at a time: steps of powers of two
+  int most = 1;
+  while (2 * most <= K) most *= 2;
+  uint16_t* const starts = a.starts + row * (a.blocks + 1);
+  const auto below = [&](auto many, int b0) {
+    int at[decltype(many)::value] = {};
+    for (int step = most; step > 0; step /= 2)
+#pragma unroll
+      for (int i = 0; i < decltype(many)::value; ++i) {
+        const int to = at[i] + step;
+        if (to <= K && sorted[min(to, K) - 1] < 64 * (b0 + 256 * i)) at[i] = to;
+      }
+#pragma unroll
+    for (int i = 0; i < decltype(many)::value; ++i)
+      if (b0 + 256 * i <= a.blocks) starts[b0 + 256 * i] = (uint16_t)at[i];
+  };
+  for (int b0 = tid; b0 < a.blocks; b0 += 2 * 256) below(std::integral_constant<int, 2>{}, b0);
+  if (tid == 255) below(std::integral_constant<int, 1>{}, a.blocks);
   __syncthreads();
 }
-__device__ __forceinline__ int key_of(const XentArgs& a, long id) { return id >= 0 && id < a.V ? (int)id : 0x7fffffff; }
+__device__ __forceinline__ int key_of(const XentArgs& a, long id) { return id >= 0 && id < a.V ? (int)id : NO_KEY; }
 
-// A wave a token: whether it takes part (a.labels: 0, -1 if not, V if an id is outside), the sum of its exponentials, and (SORT) its ids in order.
+// A wave a token: whether it takes part (a.labels: 0, -1 if not, V if an id is outside), and the sum of its exponentials.  SORT: and its ids in order, by a workgroup
+// a token, whose waves do the rest four times.
 template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kernel(XentArgs a, bool forward) {
   extern __shared__ __attribute__((aligned(16))) int prepare_mem[];
+  constexpr int TOKENS = SORT ? 1 : 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K;
-  int* const keys = prepare_mem + wave * 2 * K;
-  for (long base = blockIdx.x * 4L; base < a.n; base += gridDim.x * 4L) {
-    const long i = min(base + wave, a.n - 1);        // (the last token again: the same results)
+  int* const keys = prepare_mem;
+  for (long base = blockIdx.x * (long)TOKENS; base < a.n; base += gridDim.x * (long)TOKENS) {
+    const long i = SORT ? base : min(base + wave, a.n - 1);      // (the last token again: the same results)
     float top = -__builtin_inff();
     bool any = false, far = false;
     for (int k = lane; k < K; k += 64) {
@@ -67,7 +89,7 @@ template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kerne
       any |= e.there && !(e.t == -__builtin_inff());
       far |= e.there && e.id >= a.V;
       if (e.there) top = fmaxf(top, e.t);            // (a NaN is dropped here and comes back in the sum)
-      if (SORT) keys[k] = key_of(a, e.id);
+      if (SORT && wave == 0) keys[k] = key_of(a, e.id);
     }
     any = __any(any);
     far = __any(far);
@@ -85,19 +107,21 @@ template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kerne
       ((int64_t*)a.labels)[i] = !any ? -1 : far ? a.V : 0;
       a.q_stat[i] = make_float2(top, logf(sum));
     }
-    if constexpr (SORT) sort_entries(a, i, keys, keys + K);
+    if constexpr (SORT) {
+      if (wave == 0 && lane < 3 && K + lane < entries_up(K)) keys[K + lane] = NO_KEY;
+      sort_entries(a, i, keys, keys + entries_up(K));
+    }
   }
 }
 // The listed tokens' ids in order
 __global__ void __launch_bounds__(256) distil_sort_kernel(XentArgs a) {
   extern __shared__ __attribute__((aligned(16))) int prepare_mem[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K, count = a.head->count;
-  int* const keys = prepare_mem + wave * 2 * K;
-  for (int base = blockIdx.x * 4; base < count; base += gridDim.x * 4) {
-    const int r = min(base + wave, count - 1);
+  const int K = a.K, count = a.head->count;
+  int* const keys = prepare_mem;
+  for (int r = blockIdx.x; r < count; r += gridDim.x) {
     const long tok = a.tok[r];
-    for (int k = lane; k < K; k += 64) keys[k] = key_of(a, a.ids[tok * K + k]);
-    sort_entries(a, r, keys, keys + K);
+    for (int k = threadIdx.x; k < entries_up(K); k += 256) keys[k] = k < K ? key_of(a, a.ids[tok * K + k]) : NO_KEY;
+    sort_entries(a, r, keys, keys + entries_up(K));
   }
 }
 
@@ -161,8 +185,7 @@ __global__ void __launch_bounds__(256) distil_join_kernel(XentArgs a, int n_part
 template <typename G> __global__ void __launch_bounds__(256) distil_entries_kernel(XentArgs a) {
   extern __shared__ __attribute__((aligned(16))) int entries_mem[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K, count = a.head->count;
-  int* const ids = entries_mem + wave * 2 * K;
-  float* const qs = (float*)(ids + K);
+  int2* const known = (int2*)entries_mem + wave * entries_up(K);      // id and q
   const float scale = a.head->scale;
   for (int base = blockIdx.x * 4; base < count; base += gridDim.x * 4) {
     const int r = min(base + wave, count - 1);
@@ -170,30 +193,38 @@ template <typename G> __global__ void __launch_bounds__(256) distil_entries_kern
     const float2 stat = a.q_stat[tok];
     const float d = (a.labels[tok] < a.V ? a.d_loss[tok] * a.inv_t : __builtin_nanf("")) / scale;
     __syncthreads();
-    for (int k = lane; k < K; k += 64) {
-      const Entry e = entry_of(a, tok, k);
-      ids[k] = e.there && e.id < a.V ? (int)e.id : -1;
-      qs[k] = expf(ln_q_of(e, stat));
+    for (int k = lane; k < entries_up(K); k += 64) {
+      int2 y = {-1, 0};
+      if (k < K) {
+        const Entry e = entry_of(a, tok, k);
+        y = {e.there && e.id < a.V ? (int)e.id : -1, __float_as_int(expf(ln_q_of(e, stat)))};
+      }
+      known[k] = y;
     }
     __syncthreads();
     for (int k = lane; k < K; k += 64) {
-      const int id = ids[k];
-      if (id < a.v0 || id >= a.v1) continue;
-      float q = 0.f;                                 // (every entry of an id writes the same)
-      for (int j = 0; j < K; ++j) q += ids[j] == id ? qs[j] : 0.f;
+      const int id = known[k].x;
       const float p = exp2_fast(a.ln_p[tok * K + k] * LOG2E);
-      ((G*)a.g)[r * a.g_pitch + (id - a.v0)] = (G)(d != 0.f ? (p - q) * d : 0.f);
+      float q = 0.f;                                 // (every entry of an id writes the same)
+#pragma unroll 4
+      for (int j = 0; j < entries_up(K); j += 2) {
+        const int4 y = *(const int4*)(known + j);
+        q += y.x == id ? __int_as_float(y.y) : 0.f;
+        q += y.z == id ? __int_as_float(y.w) : 0.f;
+      }
+      if (id >= a.v0 && id < a.v1) ((G*)a.g)[r * a.g_pitch + (id - a.v0)] = (G)(d != 0.f ? (p - q) * d : 0.f);
     }
   }
 }
 
 unsigned waves_for(long n) { return (unsigned)std::min(up(n, 4), 1L << 16); }
-int entries_lds(const XentArgs& a) { return 4 * 2 * a.K * (int)sizeof(int); }
+unsigned groups_for(long n) { return (unsigned)std::min(n, 1L << 16); }
+int entries_lds(const XentArgs& a, int tokens) { return tokens * 2 * entries_up(a.K) * (int)sizeof(int); }
 hipError_t gradient(const XentArgs& a, int is_f32, hipStream_t s) {
   const hipError_t e = logits<GRAD, TEACHER>(a, is_f32, s);
   if (e != hipSuccess) return e;
-  if (is_f32) distil_entries_kernel<float><<<waves_for(a.n), 256, entries_lds(a), s>>>(a);
-  else distil_entries_kernel<__bf16><<<waves_for(a.n), 256, entries_lds(a), s>>>(a);
+  if (is_f32) distil_entries_kernel<float><<<waves_for(a.n), 256, entries_lds(a, 4), s>>>(a);
+  else distil_entries_kernel<__bf16><<<waves_for(a.n), 256, entries_lds(a, 4), s>>>(a);
   return hipGetLastError();
 }
 
@@ -202,12 +233,12 @@ hipError_t gradient(const XentArgs& a, int is_f32, hipStream_t s) {
 hipError_t launch_distil_fwd(XentArgs a, int is_f32, hipStream_t s) {
   xent_fwd_sizes(&a, is_f32);
   if (a.own) {
-    distil_prepare_kernel<true><<<waves_for(a.n), 256, entries_lds(a), s>>>(a, true);
+    distil_prepare_kernel<true><<<groups_for(a.n), 256, entries_lds(a, 1), s>>>(a, true);
   } else {
     distil_prepare_kernel<false><<<waves_for(a.n), 256, 0, s>>>(a, true);
     const hipError_t e = launch_xent_list(a, s);
     if (e != hipSuccess) return e;
-    distil_sort_kernel<<<waves_for(a.n), 256, entries_lds(a), s>>>(a);
+    distil_sort_kernel<<<groups_for(a.n), 256, entries_lds(a, 1), s>>>(a);
   }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) e = logits<STATS, TEACHER>(a, is_f32, s);
