@@ -338,20 +338,49 @@ class RecomputeLayer:
         return (self.dx, self.dy, self.dwq, self.dwkv) + self.fx.gradients(norm_x) + self.fy.gradients(norm_y)
 
 
-class LossHead:
-    """The end of a training step on one GPU: the norm of the last hidden features (norm = "layer" or "rms", or None), their product
-    with a vocabulary's weights, and the cross entropy of every token, without the logits.  Between the passes it keeps the norm's
-    statistics and lse, and (packed) the features in 8 bits, so that the caller need not keep them; the rest is made again.
+class TokenTable:
+    """The beginning of a training step on one GPU: the features of n tokens, rows of a table [V, E] times a scale (0 where the id is negative), and
+    the table's gradient.  A table that is also the vocabulary's weights of a LossHead or DistilHead ("tied") has two gradients: given as d_table, what
+    that head's backward returned as dw has this one added to it.  ids int64, n of them.  Only sequences C-ABI calls."""
 
-    h [n, E] or [B, S, E], contiguous, w [V, E], labels int64 (negative: the token takes no part).  Only sequences C-ABI calls."""
-
-    def __init__(self, n, E, V, dtype: torch.dtype, norm: Optional[str] = None, packed: bool = False, eps: float = 1e-5,
-                 device: str = "cuda"):
+    def __init__(self, n, E, V, dtype: torch.dtype, scale: float = 1.0, device: str = "cuda"):
         if not torch.cuda.is_available():
-            raise RuntimeError("LossHead needs a GPU: there is no CPU fallback")
-        nbytes = B.lvx_xent_workspace_bytes(n, E, V, B.dtype_code(dtype))
+            raise RuntimeError("TokenTable needs a GPU: there is no CPU fallback")
+        nbytes = B.lvx_embed_workspace_bytes(n, E, V)
         if nbytes == 0:
-            raise B.LvxError(-2, "lvx_xent_workspace_bytes")
+            raise B.LvxError(-2, "lvx_embed_workspace_bytes")
+        self.scale, self.V = scale, V
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.x = torch.empty((n, E), dtype=dtype, device=device)
+        self.d_table = None
+
+    def _check(self, table, ids):
+        if table.shape != (self.V, self.x.shape[1]) or ids.numel() != self.x.shape[0]:
+            raise ValueError("the table and the ids have to be as large as this object was made for")
+
+    def forward(self, table, ids) -> torch.Tensor:
+        """The tokens' features ([n, E], a buffer of this object)."""
+        self._check(table, ids)
+        B.lvx_embed_fwd(table, ids, self.x, self.scale)
+        return self.x
+
+    def backward(self, d_x, ids, d_table: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The table's gradient (a buffer of this object), or d_table with it added; d_x [n, E] or [B, S, E], also windows of wider tensors."""
+        add = d_table is not None
+        if not add and self.d_table is None:
+            self.d_table = torch.empty((self.V, self.x.shape[1]), dtype=self.x.dtype, device=self.x.device)
+        d_table = d_table if add else self.d_table
+        self._check(d_table, ids)
+        B.lvx_embed_bwd(d_x, ids, d_table, self.ws, self.scale, accumulate=add)
+        return d_table
+
+
+class _Head:
+    """Norm, vocabulary and the buffers of a loss against it, of n tokens (`nbytes`: its workspace)."""
+
+    def __init__(self, n, E, V, dtype, norm, packed, eps, device, nbytes, where):
+        if nbytes == 0:
+            raise B.LvxError(-2, where)
         self.f = _Features(n, E, n, dtype, norm, packed, eps, device)
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.loss = torch.empty(n, dtype=torch.float32, device=device)
@@ -366,6 +395,31 @@ class LossHead:
             raise ValueError("h has to be contiguous, of as many tokens and features as this object was made for")
         return h.view(self.dh.shape)
 
+    def _again(self, h, norm):
+        """(h, the features of the forward pass once more), and the norm's gradients at 0."""
+        h = self._tokens(h)
+        feat = self.f.again(h, 0, self.dh.shape, norm)
+        self.f.start_backward()
+        return h, feat
+
+    def _gradients(self, h, norm):
+        self.f.backward(h, 0, norm, self.dh)
+        return (self.dh, self.dw) + self.f.gradients(norm)
+
+
+class LossHead(_Head):
+    """The end of a training step on one GPU: the norm of the last hidden features (norm = "layer" or "rms", or None), their product
+    with a vocabulary's weights, and the cross entropy of every token, without the logits.  Between the passes it keeps the norm's
+    statistics and lse, and (packed) the features in 8 bits, so that the caller need not keep them; the rest is made again.
+
+    h [n, E] or [B, S, E], contiguous, w [V, E], labels int64 (negative: the token takes no part).  Only sequences C-ABI calls."""
+
+    def __init__(self, n, E, V, dtype: torch.dtype, norm: Optional[str] = None, packed: bool = False, eps: float = 1e-5,
+                 device: str = "cuda"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("LossHead needs a GPU: there is no CPU fallback")
+        super().__init__(n, E, V, dtype, norm, packed, eps, device, B.lvx_xent_workspace_bytes(n, E, V, B.dtype_code(dtype)), "lvx_xent_workspace_bytes")
+
     def forward(self, h, w, labels, norm: Optional[Norm] = None) -> torch.Tensor:
         """The tokens' losses (float32 [n], a buffer of this object; 0 without a label)."""
         feat = self.f.forward(self._tokens(h), 0, self.dh.shape, norm)
@@ -375,9 +429,64 @@ class LossHead:
     def backward(self, h, w, labels, d_loss, norm: Optional[Norm] = None):
         """(dh [n, E], dw in the input dtype) of sum(loss * d_loss), d_loss float32 [n]; h None where it is kept packed.  With a norm
         followed by the gradients (float32, or None) of its gamma and beta."""
-        h = self._tokens(h)
-        feat = self.f.again(h, 0, self.dh.shape, norm)
-        self.f.start_backward()
+        h, feat = self._again(h, norm)
         B.lvx_xent_bwd(feat, w, labels, self.lse, d_loss, self.dh, self.dw, self.ws)
-        self.f.backward(h, 0, norm, self.dh)
-        return (self.dh, self.dw) + self.f.gradients(norm)
+        return self._gradients(h, norm)
+
+
+class DistilHead(_Head):
+    """LossHead with a teacher in place of labels: the divergence of every token's softmax from the softmax of K known logits of a teacher, both at a
+    temperature.  ids [n, K] int64 (a negative one: the entry is not there; a token without any takes no part), teacher [n, K] float32 or bfloat16."""
+
+    def __init__(self, n, E, V, K, dtype: torch.dtype, temperature: float = 1.0, norm: Optional[str] = None, packed: bool = False, eps: float = 1e-5,
+                 device: str = "cuda"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("DistilHead needs a GPU: there is no CPU fallback")
+        super().__init__(n, E, V, dtype, norm, packed, eps, device, B.lvx_distil_workspace_bytes(n, E, V, K, B.dtype_code(dtype)),
+                         "lvx_distil_workspace_bytes")
+        self.temperature = temperature
+        self.ln_p = torch.empty((n, K), dtype=torch.float32, device=device)
+
+    def forward(self, h, w, ids, teacher, norm: Optional[Norm] = None) -> torch.Tensor:
+        """The tokens' losses (float32 [n], a buffer of this object; 0 without an entry).  ln_p: the logarithms of the entries' probabilities."""
+        feat = self.f.forward(self._tokens(h), 0, self.dh.shape, norm)
+        B.lvx_distil_fwd(feat, w, ids, teacher, self.loss, self.lse, self.ln_p, self.ws, self.temperature)
+        return self.loss
+
+    def backward(self, h, w, ids, teacher, d_loss, norm: Optional[Norm] = None):
+        """As LossHead.backward."""
+        h, feat = self._again(h, norm)
+        B.lvx_distil_bwd(feat, w, ids, teacher, self.lse, self.ln_p, d_loss, self.dh, self.dw, self.ws, self.temperature)
+        return self._gradients(h, norm)
+
+
+class SequenceLoss:
+    """Losses of whole sequences of tokens, between LossHead.forward (whose tokens' losses are their negative log likelihoods nll) and LossHead.backward (whose
+    d_loss is the d_nll returned here).  n tokens; S pairs or sequences, which are the tokens first[s] .. first[s + 1] - 1 (int64); labels: the head's, tokens
+    with a negative one take no part, d_nll is 0 there and where no sequence is.  d_loss float32 [S], or None: the mean over the S.  Returns buffers of
+    this object.  Only sequences C-ABI calls."""
+
+    def __init__(self, n, S, device: str = "cuda"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("SequenceLoss needs a GPU: there is no CPU fallback")
+        nbytes = max(B.lvx_preference_workspace_bytes(n, S), B.lvx_policy_workspace_bytes(n, S))
+        if nbytes == 0:
+            raise B.LvxError(-2, "lvx_preference_workspace_bytes")
+        f32 = dict(dtype=torch.float32, device=device)
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.loss, self.margin, self.stats = torch.empty(S, **f32), torch.empty(S, **f32), torch.empty((S, 3), **f32)
+        self.d_nll, self.mean = torch.empty(n, **f32), torch.full((S,), 1.0 / S, **f32)
+
+    def preference(self, nll, ref, labels, first, d_loss=None, form: str = "logistic", beta: float = 0.1, smoothing: float = 0.0):
+        """(loss [S], margin [S], d_nll [n]) of S pairs: sequences 0 .. S - 1 are the chosen ones, the next S the rejected ones; ref: the tokens' nll under
+        the reference (None: 0)."""
+        self.d_nll.zero_()
+        B.lvx_preference(nll, ref, labels, first, self.loss, self.margin, self.mean if d_loss is None else d_loss, self.d_nll, self.ws, form, beta, smoothing)
+        return self.loss, self.margin, self.d_nll
+
+    def policy(self, nll, old, ref, adv, labels, first, d_loss=None, clip=(0.2, 0.2), beta: float = 0.0, mean: bool = True):
+        """(loss [S], stats [S, 3], d_nll [n]) of S sequences: old: the tokens' nll when they were sampled, ref: under the reference (None without
+        beta), adv [S] or [n]; stats: labelled tokens, share of clipped ones, mean divergence."""
+        self.d_nll.zero_()
+        B.lvx_policy(nll, old, ref, adv, labels, first, self.loss, self.stats, self.mean if d_loss is None else d_loss, self.d_nll, self.ws, clip, beta, mean)
+        return self.loss, self.stats, self.d_nll
