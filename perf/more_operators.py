@@ -333,10 +333,10 @@ def _own(s):
         B.lvx_embed_fwd(s["table"], s["ids"], b["y"], scale=SCALE)
         if not c["train"]:
             return b["y"]
-        if c["tied"]:
-            b["d_table"].copy_(s["dw"])
-        B.lvx_embed_bwd(s["d_y"], s["ids"], b["d_table"], b["ws"], scale=SCALE, accumulate=c["tied"])
-        return b["y"], b["d_table"]
+        # (what the plain form adds to: a float32 gradient itself, a copy of a bf16 one)
+        d_table = s["dw"] if c["tied"] and c["dtype"] == "f32" else b["d_table"].copy_(s["dw"]) if c["tied"] else b["d_table"]
+        B.lvx_embed_bwd(s["d_y"], s["ids"], d_table, b["ws"], scale=SCALE, accumulate=c["tied"])
+        return b["y"], d_table
     if c["kind"] == "distil":
         T = c["temperature"]
         B.lvx_distil_fwd(s["x"], s["w"], s["ids"], s["teacher"], b["loss"], b["lse"], b["top"], b["ws"], temperature=T)
