@@ -113,12 +113,14 @@ template <typename T, bool PAST> __global__ void __launch_bounds__(256) embed_fw
 // ---- backward: the sort ----
 
 constexpr int SORT_WG = 1024, SORT_WAVES = SORT_WG / 64;
-struct Sort { int bits, passes; };                   // bits of a digit, digits of an id
-inline Sort sort_of(long V) {
+// Bits of a digit, digits of an id; log2 of the workgroups that share a sort by one launch, by the highest bits of an id, and the bits below these, which the digits are of.
+struct Sort { int bits, passes, split, of; };
+inline Sort sort_of(long V, int split) {
   int bits = 1;
   while (bits < 62 && (1L << bits) < V) ++bits;
-  const int passes = (bits + EMBED_DIGIT_BITS - 1) / EMBED_DIGIT_BITS;
-  return {(bits + passes - 1) / passes, passes};
+  split = std::min(split, bits - 1);
+  const int of = bits - split, passes = (of + EMBED_DIGIT_BITS - 1) / EMBED_DIGIT_BITS;
+  return {(of + passes - 1) / passes, passes, split, of};
 }
 
 // The rank of every token among those of its wave with the same digit, in order: `rounds` x 64 tokens a wave, `dig` < 0: none.  cnt[digit]: the
@@ -167,12 +169,16 @@ inline int sort_lds(int bits) { return (int)sizeof(int) * (sort_counts(1 << bits
 // Turns the waves' counts of a digit (thread t: digit t) into where the wave's first one stands among all of the workgroup's; returns how many there are.
 __device__ __forceinline__ int counts_to_starts(int* cnt, int digits) {
   int run = 0;
-  if ((int)threadIdx.x < digits)
+  if ((int)threadIdx.x < digits) {
+    int c[SORT_WAVES];
+#pragma unroll
+    for (int w = 0; w < SORT_WAVES; ++w) c[w] = cnt[w * digits + threadIdx.x];
+#pragma unroll
     for (int w = 0; w < SORT_WAVES; ++w) {
-      const int c = cnt[w * digits + threadIdx.x];
       cnt[w * digits + threadIdx.x] = run;
-      run += c;
+      run += c[w];
     }
+  }
   return run;
 }
 __device__ __forceinline__ void clear_counts(int* cnt, int digits) {
@@ -193,33 +199,127 @@ template <typename T> __device__ __forceinline__ void clear_table(T* p, long ele
   }
 }
 
-// All digits by one workgroup, for up to ONE_WG tokens.
-constexpr int ONE_ROUNDS = 8, ONE_WG = SORT_WG * ONE_ROUNDS;
+// Up to FEW tokens: every id is compared with all others.  (8 ids 9.6 -> 2.8 us, 64 9.8 -> 3.9, 120 9.9 -> 5.1; 250 of them, in the same way, 13.)
+constexpr int FEW = 128;
+__device__ __forceinline__ void sort_few(const EmbedArgs& a, const Sort& sort, int* keys) {
+  const int tid = threadIdx.x, n = (int)a.n, none = 0x7ffffffe;
+  int* const sorted = keys + FEW;
+  __shared__ int count[2];
+  static_assert(FEW == 128, "two waves");
+  const long id = tid < n ? a.ids[tid] : -1;
+  const int mine = id >= 0 && id < a.V ? (int)id : none;
+  if (tid < FEW) keys[tid] = mine;
+  const int on = __popcll(__ballot(mine != none));
+  if (tid == 0) count[0] = on;
+  if (tid == 64) count[1] = on;
+  __syncthreads();
+  if (tid < FEW) {
+    int r = 0;
+    const auto before = [&](int y, int j) { return y < mine + (j < tid ? 1 : 0) ? 1 : 0; };      // (equal ids: in the tokens' order)
+    for (int j = 0; j < n; j += 16) {
+      int4 y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = *(const int4*)(keys + j + 4 * k);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) r += before(y[k].x, j + 4 * k) + before(y[k].y, j + 4 * k + 1) + before(y[k].z, j + 4 * k + 2) + before(y[k].w, j + 4 * k + 3);
+    }
+    if (tid < n) sorted[r] = mine;
+    if (mine != none) {
+      a.key[0][r] = mine;
+      a.tok[0][r] = tid;
+    }
+  }
+  __syncthreads();
+  const int low = sort.bits * (sort.passes - 1), tops = 1 << (sort.of - low), m = count[0] + count[1];
+  for (int d = tid; d <= tops; d += SORT_WG) {
+    int lo = 0, hi = m;                              // the first whose last digit is d or more
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if ((sorted[mid] >> low) < d) lo = mid + 1;
+      else hi = mid;
+    }
+    a.top[d] = lo;
+  }
+  if (tid == 0) {
+    a.head->count = m;
+    a.head->n_many = a.head->n_few = 0;
+  }
+}
+
+// Up to ONE_WG tokens: all digits in one launch, by one workgroup, or by 2^split of them, each of which takes the ids with its value of the highest bits
+// and counts those with lower ones (all ids of a batch in one of these: as slow as one workgroup).
+constexpr int ONE_ROUNDS = 8, ONE_WG = SORT_WG * ONE_ROUNDS, ONE_SPLIT = 3;
 inline int one_lds(int bits, long n) { return sort_lds(bits) + 2 * (int)sizeof(int) * (int)((n + SORT_WG - 1) / SORT_WG * SORT_WG); }
-template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_kernel(EmbedArgs a, int bits, int passes, Clear clear) {
-  if (blockIdx.x > 0) {
-    clear_table((T*)a.d_table + clear.from, clear.count, blockIdx.x - 1, clear.wgs);
+template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_kernel(EmbedArgs a, Sort sort, Clear clear) {
+  const int groups = 1 << sort.split, mine = blockIdx.x;
+  if (mine >= groups) {
+    clear_table((T*)a.d_table + clear.from, clear.count, mine - groups, clear.wgs);
     return;
   }
   extern __shared__ __attribute__((aligned(16))) int sort_mem[];
-  const int digits = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (a.n <= FEW) {
+    sort_few(a, sort, sort_mem);
+    return;
+  }
+  const int bits = sort.bits, digits = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int* const cnt = sort_mem;
   int* const start = cnt + sort_counts(digits);
   int* const sums = start + digits;
   int* const skey = sums + SORT_WAVES;
-  const int per_wave = (int)((a.n + SORT_WG - 1) / SORT_WG) * 64, rounds = per_wave / 64;
+  int per_wave = (int)((a.n + SORT_WG - 1) / SORT_WG) * 64, rounds = per_wave / 64;
   int* const stok = skey + SORT_WAVES * per_wave;
   int key[ONE_ROUNDS], tok[ONE_ROUNDS], dig[ONE_ROUNDS], rank[ONE_ROUNDS];
+  // the ids, in order
+  long id[ONE_ROUNDS];
 #pragma unroll
   for (int r = 0; r < ONE_ROUNDS; ++r) {
     const long i = wave * per_wave + 64 * r + lane;
-    const long id = r < rounds && i < a.n ? a.ids[i] : -1;
-    key[r] = id < a.V ? (int)id : -1;
-    if (id < 0) key[r] = -1;
-    tok[r] = (int)i;
+    id[r] = r < rounds && i < a.n ? a.ids[i] : -1;
   }
-  int m = 0;
-  for (int p = 0; p < passes; ++p) {
+  int own = 0, lower = 0;                            // of the wave
+#pragma unroll
+  for (int r = 0; r < ONE_ROUNDS; ++r) {
+    const int group = id[r] >= 0 && id[r] < a.V ? (int)(id[r] >> sort.of) : -1;
+    key[r] = group == mine ? (int)id[r] & ((1 << sort.of) - 1) : -1;
+    const unsigned long long on = __ballot(group == mine);
+    rank[r] = own + __popcll(on & ((1ull << lane) - 1));
+    own += __popcll(on);
+    lower += __popcll(__ballot(group >= 0 && group < mine));
+  }
+  if (lane == 0) {
+    cnt[wave] = own;
+    cnt[SORT_WAVES + wave] = lower;
+  }
+  __syncthreads();
+  int before = 0, m = 0, base = 0;                   // own ones of the waves before, of all; ids of the groups before
+#pragma unroll
+  for (int w = 0; w < SORT_WAVES; ++w) {
+    const int c = cnt[w];
+    before += w < wave ? c : 0;
+    m += c;
+    base += cnt[SORT_WAVES + w];
+  }
+#pragma unroll
+  for (int r = 0; r < ONE_ROUNDS; ++r)
+    if (key[r] >= 0) {
+      skey[before + rank[r]] = key[r];
+      stok[before + rank[r]] = wave * per_wave + 64 * r + lane;
+    }
+  rounds = (m + SORT_WG - 1) / SORT_WG;              // (of the group's own)
+  per_wave = 64 * rounds;
+  const auto take = [&]() {
+#pragma unroll
+    for (int r = 0; r < ONE_ROUNDS; ++r) {
+      const int i = wave * per_wave + 64 * r + lane;
+      const bool on = r < rounds && i < m;
+      key[r] = on ? skey[i] : -1;
+      tok[r] = on ? stok[i] : 0;
+    }
+  };
+  __syncthreads();
+  take();
+  const int low = bits * (sort.passes - 1), tops = 1 << (sort.of - low);      // (values of the last digit)
+  for (int p = 0; p < sort.passes; ++p) {
     clear_counts(cnt, digits);
     __syncthreads();
 #pragma unroll
@@ -227,11 +327,10 @@ template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_
     rank_in_wave<ONE_ROUNDS>(dig, rank, rounds, cnt + wave * digits, bits);
     __syncthreads();
     const int count = counts_to_starts(cnt, digits);
-    const int at = exclusive_sum(count, sums, &m);
-    if (tid < digits) {
-      start[tid] = at;
-      if (p == passes - 1) a.top[tid] = at;
-    }
+    int all;
+    const int at = exclusive_sum(count, sums, &all);
+    if (tid < digits) start[tid] = at;
+    if (p == sort.passes - 1 && tid < tops) a.top[mine * tops + tid] = base + at;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < ONE_ROUNDS; ++r)
@@ -241,25 +340,19 @@ template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_
         stok[to] = tok[r];
       }
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < ONE_ROUNDS; ++r) {
-      const int i = wave * per_wave + 64 * r + lane;
-      const bool on = r < rounds && i < m;
-      key[r] = on ? skey[i] : -1;
-      tok[r] = on ? stok[i] : 0;
-    }
+    take();
   }
 #pragma unroll
   for (int r = 0; r < ONE_ROUNDS; ++r) {
     const int i = wave * per_wave + 64 * r + lane;
     if (key[r] >= 0) {
-      a.key[0][i] = key[r];
-      a.tok[0][i] = tok[r];
+      a.key[0][base + i] = key[r] + (mine << sort.of);
+      a.tok[0][base + i] = tok[r];
     }
   }
-  if (tid == 0) {
-    a.top[digits] = m;
-    a.head->count = m;
+  if (tid == 0 && mine == groups - 1) {
+    a.top[groups * tops] = base + m;
+    a.head->count = base + m;
     a.head->n_many = a.head->n_few = 0;
   }
 }
@@ -526,7 +619,7 @@ template <typename T> __global__ void __launch_bounds__(256) embed_join_kernel(E
 long up(long n, long by) { return (n + by - 1) / by; }
 
 // Bytes of the table that a launch of the sort clears: about what goes to memory in its time.
-constexpr long CLEAR_ONE = 16 << 20, CLEAR_ROUND = 8 << 20, CLEAR_MOVE = 48 << 20;
+constexpr long CLEAR_ONE = 20 << 20, CLEAR_ROUND = 4 << 20, CLEAR_MOVE = 48 << 20;
 
 template <typename T> hipError_t embed_fwd(const EmbedArgs& a, hipStream_t s) {
   const int tl = team_log(a.E);
@@ -544,7 +637,7 @@ template <typename T> Clear clear_some(const EmbedArgs& a, long bytes, long piec
   return c;
 }
 template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStream_t s) {
-  const Sort sort = sort_of(a.V);
+  const Sort sort = sort_of(a.V, a.n > SORT_WG && a.n <= ONE_WG ? ONE_SPLIT : 0);
   const int low = sort.bits * (sort.passes - 1);
   const long piece = 1L << std::min(low, ROWS_LOG);
   long row = ADD ? a.V : 0;                          // the rows before are cleared already
@@ -554,7 +647,7 @@ template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStre
     e = ensure_dynamic_lds((const void*)embed_sort_one_kernel<T>, one_lds(EMBED_DIGIT_BITS, ONE_WG), &once);
     if (e != hipSuccess) return e;
     const Clear clear = clear_some<T>(a, CLEAR_ONE + CLEAR_ROUND * up(a.n, SORT_WG), piece, &row);
-    embed_sort_one_kernel<T><<<1 + clear.wgs, SORT_WG, one_lds(sort.bits, a.n), s>>>(a, sort.bits, sort.passes, clear);
+    embed_sort_one_kernel<T><<<(1 << sort.split) + clear.wgs, SORT_WG, one_lds(sort.bits, a.n), s>>>(a, sort, clear);
   } else {
     static SmemOnce once;
     e = ensure_dynamic_lds((const void*)embed_move_kernel<T>, sort_lds(EMBED_DIGIT_BITS), &once);
@@ -585,6 +678,7 @@ template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStre
 // Sorted tokens of a chunk: 4 to 64, so that there are threads for about 2^18 pieces of 8 features.
 constexpr int LEAST_CHUNK = 4;
 int embed_chunk(long n, int E) {
+  if (n <= 16) return 16;                            // (then nothing is left to join)
   int c = LEAST_CHUNK;
   while (c < 64 && n * chunks8(E) / c > (1L << 18)) c *= 2;
   return c;

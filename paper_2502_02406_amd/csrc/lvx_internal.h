@@ -279,13 +279,13 @@ struct EmbedArgs {
   EmbedHead* head;
   int *key[2], *tok[2]; // [n]: ids and numbers of the tokens, from one pass of the sort to the next; the last one leaves key[0], tok[0]
   int* hist;            // [EMBED_BLOCKS][EMBED_DIGITS]
-  int* top;             // [EMBED_DIGITS + 1]: where the ids with every value of the last digit start
+  int* top;             // [EMBED_TOPS + 1]: where the ids with every value of the last digit (and of what stands above it) start
   int2* long_list;      // [list_end]: chunks whose last id goes on in the next one, and that id; of ids of many chunks first
   long list_end;
   float* part;          // [chunks][2][E]
   int chunk;            // sorted tokens of a chunk
 };
-constexpr int EMBED_BLOCKS = 256, EMBED_DIGIT_BITS = 10, EMBED_DIGITS = 1 << EMBED_DIGIT_BITS;
+constexpr int EMBED_BLOCKS = 256, EMBED_DIGIT_BITS = 10, EMBED_DIGITS = 1 << EMBED_DIGIT_BITS, EMBED_TOPS = 8 * EMBED_DIGITS;
 int embed_chunk(long n, int E);
 long embed_chunks_room(long n);             // the most chunks of n tokens
 size_t embed_part_room(long n, int E);      // bytes of `part` for n tokens of E features or fewer

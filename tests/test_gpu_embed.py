@@ -73,7 +73,8 @@ def check(table, ids, dy, scale, y, dt, old=None):
 
 
 SIZES = [(1, 1, 1), (1, 4096, 100), (3, 7, 5), (64, 64, 1000), (65, 129, 1), (700, 1001, 300), (2000, 512, 33000), (8192, 64, 1025), (8193, 40, 50021),
-         (20000, 8, 131072), (10000, 2056, 7), (9000, 16, (1 << 20) + 5), (12289, 520, 1024), (40000, 24, 300)]
+         (20000, 8, 131072), (10000, 2056, 7), (9000, 16, (1 << 20) + 5), (12289, 520, 1024), (40000, 24, 300), (5000, 40, 9), (1025, 16, 2), (7000, 24, 200000), (1024, 8, 5000), (16, 256, 3), (17, 40, 2), (256, 16, 900), (257, 16, 900),
+         (3000, 8, (1 << 21) + 3)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -90,7 +91,7 @@ def test_lookup_and_gradient(dtype, n, E, V):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n", [300, 8192, 30000])
+@pytest.mark.parametrize("n", [9, 200, 300, 3000, 8192, 30000])
 @pytest.mark.parametrize("which", ["none", "same", "two", "outside", "last"])
 def test_few_ids(dtype, n, which):
     """All tokens padding, one id for all, two that alternate, ids outside the table, the table's last row among others."""
