@@ -27,7 +27,7 @@ __device__ __forceinline__ Entry entry_of(const XentArgs& a, long i, int k) {
 __device__ __forceinline__ float ln_q_of(const Entry& e, float2 stat) { return (e.t - stat.x) - stat.y; }
 
 // K entries in LDS, rounded up to four
-constexpr int NO_KEY = 0x7fffffff;
+constexpr int NO_KEY = 0x7ffffffe;
 __host__ __device__ constexpr int entries_up(int K) { return (K + 3) / 4 * 4; }
 // A token's entries in the order of their ids, as row `row` of what the tiles look them up in, by a workgroup.  keys: filled in by it, NO_KEY behind the last one.
 __device__ __forceinline__ void sort_entries(const XentArgs& a, long row, const int* keys, int* sorted) {
@@ -39,10 +39,8 @@ __device__ __forceinline__ void sort_entries(const XentArgs& a, long row, const 
 #pragma unroll 4
     for (int j = 0; j < K4; j += 4) {
       const int4 y = *(const int4*)(keys + j);
-      r += y.x < mine || (y.x == mine && j < k);
-      r += y.y < mine || (y.y == mine && j + 1 < k);
-      r += y.z < mine || (y.z == mine && j + 2 < k);
-      r += y.w < mine || (y.w == mine && j + 3 < k);
+      const auto before = [&](int y, int j) { return y < mine + (j < k ? 1 : 0) ? 1 : 0; };      // (equal ids: in the order of the entries)
+      r += before(y.x, j) + before(y.y, j + 1) + before(y.z, j + 2) + before(y.w, j + 3);
     }
     sorted[r] = mine;                                // (those behind K stay there)
     if (k < K) {

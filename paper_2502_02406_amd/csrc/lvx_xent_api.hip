@@ -127,7 +127,7 @@ EntryPlan entries_of(int64_t n, int64_t V, int32_t K) {
   size_t at = align_up(n * 8);                       // (labels)
   e.q_stat = at; at += align_up(n * 8);
   e.bwd = at;
-  e.sorted = at; at += align_up((size_t)n * K * 4);
+  e.sorted = at; at += align_up((size_t)n * K * 4 + 16);      // (they are read four at a time)
   e.rank = at; at += align_up((size_t)n * K * 2);
   e.starts = at; at += align_up((size_t)n * ((V + 63) / 64 + 1) * 2);
   e.z = at; at += align_up((size_t)n * K * 4);

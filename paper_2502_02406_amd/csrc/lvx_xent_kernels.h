@@ -21,7 +21,7 @@ constexpr int NW = 8;                  // waves of a workgroup
 constexpr int CB = 16 / NW, WC = 32 * CB;              // a wave's column blocks, and its columns
 constexpr int OUT_B = 32 * WC * 2;     // epilogue: 32 rows of a wave on their way out
 constexpr int SMEM_B = RING_B + NW * OUT_B;
-static_assert(SMEM_B <= 160 * 1024 && NW / 2 * T * 8 <= NW * OUT_B, "the layout fits a compute unit, and a tile's statistics the way out");
+static_assert(SMEM_B <= 160 * 1024 && NW / 2 * T * 8 + NW * 2048 <= NW * OUT_B, "the layout fits a compute unit, and a tile's statistics and patches the way out");
 enum { STATS = 0, GRAD = 1, DX = 2, DW = 3, DW_PARTS = 4 };
 // What a token's logits are measured against: its label, or a teacher's logits of some entries of the vocabulary (then z is divided by a
 // temperature, and the epilogues of the logits hand out those of the entries; g of these is put right by another launch, behind the epilogues).
@@ -164,24 +164,55 @@ __device__ __forceinline__ unsigned entries_of(const XentArgs& a, long row, int 
   return *(const unsigned_any2*)(a.starts + row * (a.blocks + 1) + min(col / 64, a.blocks - 1));
 }
 __device__ __forceinline__ int entry_id(const XentArgs& a, long row, unsigned e) { return (e & 0xffffu) < e >> 16 ? a.sorted[row * a.K + (e & 0xffffu)] : -1; }
-// Leaves the logits of those among the wave's 32 JB columns, of which `cw` is the first; z as above, id: that of the first entry.  An entry's logit is
-// chosen by the bits of its column.
-template <int JB, class Z> __device__ __forceinline__ void pick_entries(const XentArgs& a, long row, unsigned e, int id, int cw, int g, Z&& z) {
-  const auto choose = [](int bit, float one, float zero) __attribute__((always_inline)) -> float { return bit ? one : zero; };
-  while (__any((e & 0xffffu) < e >> 16)) {
-    const int c = (e & 0xffffu) < e >> 16 ? id - cw : -1;
-    float y[JB];
+// Leaves the logits of those among the wave's 32 JB columns, of which `cw` is the first; z as above, id: that of the first entry, which is chosen by the bits of
+// its column.  The others, where a row has more in these columns, through `patch`, 2 KB of LDS of the wave's own: 32 rows x 16 columns at a time, where both halves of the
+// wave then look up four entries of a row each (2000 tokens x 256 against 1000, 128 entries: one after the other, by their bits, 40 us, 17 so).
+constexpr int PATCH = 32 * 16;
+template <int JB, class Z> __device__ __forceinline__ void pick_entries(const XentArgs& a, long row, unsigned e, int id, int cw, int g, float* patch, Z&& z) {
+  int at = (int)(e & 0xffffu);
+  const int end = (int)(e >> 16);
+  {
+    const auto choose = [](int bit, float one, float zero) __attribute__((always_inline)) -> float { return bit ? one : zero; };      // (of values, not of places)
+    const int c = at < end ? id - cw : -1;
+    if (__any(c >= 0 && c < 32 * JB)) {
+      float y[JB];
 #pragma unroll
-    for (int j = 0; j < JB; ++j) {
-      float t[4];
+      for (int j = 0; j < JB; ++j) {
+        float t[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        t[q] = choose(c & 2, choose(c & 1, z(4 * q + 3, j), z(4 * q + 2, j)), choose(c & 1, z(4 * q + 1, j), z(4 * q, j)));
-      y[j] = choose(c & 16, choose(c & 8, t[3], t[2]), choose(c & 8, t[1], t[0]));
+        for (int q = 0; q < 4; ++q)
+          t[q] = choose(c & 2, choose(c & 1, z(4 * q + 3, j), z(4 * q + 2, j)), choose(c & 1, z(4 * q + 1, j), z(4 * q, j)));
+        y[j] = choose(c & 16, choose(c & 8, t[3], t[2]), choose(c & 8, t[1], t[0]));
+      }
+      if (c >= 0 && c < 32 * JB && ((c >> 2) & 1) == g) a.z_entry[row * a.K + at] = JB == 2 ? choose(c & 32, y[JB - 1], y[0]) : y[0];
     }
-    if (c >= 0 && c < 32 * JB && ((c >> 2) & 1) == g) a.z_entry[row * a.K + (e & 0xffffu)] = JB == 2 ? choose(c & 32, y[JB - 1], y[0]) : y[0];
-    ++e;
-    id = entry_id(a, row, e);
+  }
+  const int l31 = threadIdx.x & 31;
+  for (++at; __any(at < end); at += 8) {
+    typedef __attribute__((ext_vector_type(4))) int i32x4;
+    typedef i32x4 __attribute__((aligned(4))) i32x4_any;
+    const int mine = at + 4 * g;
+    i32x4 ids = {0, 0, 0, 0};
+    if (mine < end) ids = *(const i32x4_any*)(a.sorted + row * a.K + mine);      // (there is room behind the last one)
+    int c[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c[k] = mine + k < end ? ids[k] - cw : -1;
+#pragma unroll
+    for (int j = 0; j < JB; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const auto here = [&](int k) __attribute__((always_inline)) -> bool { return (unsigned)(c[k] - (32 * j + 16 * h)) < 16u; };
+        if (!__any(here(0) || here(1) || here(2) || here(3))) continue;
+        // (the patch is this wave's own: its reads are ordered after its writes, and the next writes after them)
+        asm volatile("" ::: "memory");
+        *(f32x4*)(patch + 16 * l31 + 4 * g) = f32x4{z(8 * h, j), z(8 * h + 1, j), z(8 * h + 2, j), z(8 * h + 3, j)};
+        *(f32x4*)(patch + 16 * l31 + 8 + 4 * g) = f32x4{z(8 * h + 4, j), z(8 * h + 5, j), z(8 * h + 6, j), z(8 * h + 7, j)};
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (here(k)) a.z_entry[row * a.K + mine + k] = patch[16 * l31 + c[k] - (32 * j + 16 * h)];
+        asm volatile("" ::: "memory");
+      }
   }
 }
 
@@ -498,7 +529,7 @@ xent_bf16_kernel(XentArgs a) {
       if constexpr (PICK) {
 #pragma unroll
         for (int i = 0; i < RB; ++i)
-          pick_entries<CB>(a, opaque(cur.r0 + wm * 32 * RB + 32 * i + l31), (unsigned)lab[i], id[i], cw, g,
+          pick_entries<CB>(a, opaque(cur.r0 + wm * 32 * RB + 32 * i + l31), (unsigned)lab[i], id[i], cw, g, (float*)(smem + RING_B + NW / 2 * TR * 8) + wave * PATCH,
                            [&](int v, int j) __attribute__((always_inline)) -> float {      // (read where it stands: all of them, ahead of the loop, spill)
                              float y;
                              asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(acc[j][i][v]));
@@ -706,7 +737,7 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       tile_stats<1>(g, left, log2_unit<LOSS>(a), z, &m2, &s);
       if (g == 0) sums[wave * 32 * RB + r] = make_float2(m2, s);
       if constexpr (LOSS == TEACHER) {
-        pick_entries<1>(a, row_e[i], en[i], id[i], c0 + cw, g, z);
+        pick_entries<1>(a, row_e[i], en[i], id[i], c0 + cw, g, (float*)(smem + 4 * 32 * RB * 8) + wave * PATCH, z);
       } else {
         const int label = OWN ? __shfl(own.lab, r) : r0 + r < M ? a.lab[r0 + r] : -1;
         const int c = r0 + r < M ? label - c0 - cw : -1;
@@ -1024,7 +1055,7 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
       if constexpr (LOSS == TEACHER) {
         const int row = min(r, M - 1);
         const unsigned e = r < M && left > 0 ? entries_of(a, row, cw) : 0u;
-        pick_entries<NB>(a, row, e, entry_id(a, row, e), cw, g, z);
+        pick_entries<NB>(a, row, e, entry_id(a, row, e), cw, g, sa + wave * PATCH, z);
       } else {
         const int c = r < M ? a.lab[r] - cw : -1;
         if (__any(c >= 0 && c < FT / 2)) {
@@ -1144,7 +1175,7 @@ template <int MODE, int LOSS> __global__ void __launch_bounds__(256) xent_few_f3
     if constexpr (LOSS == TEACHER) {
       const int token = __shfl(own.tok, min(r, M - 1));
       const unsigned e = r < M ? entries_of(a, token, c0) : 0u;
-      pick_entries<1>(a, token, e, entry_id(a, token, e), c0, g, z);
+      pick_entries<1>(a, token, e, entry_id(a, token, e), c0, g, &sums[0][0][0], z);
     } else {
       const int c = r < M ? label - c0 : -1;
       if (__any(c >= 0 && c < 32)) {
