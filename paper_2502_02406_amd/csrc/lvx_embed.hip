@@ -558,61 +558,87 @@ template <typename T, bool ADD> __global__ void __launch_bounds__(256) embed_sum
   }
 }
 
-// Ids that go over several chunks.  Of more than MANY_PARTS: 256 features a workgroup, its four waves with a run of the chunks each; of fewer, most of them:
-// 256 features a wave.
-template <typename T> __global__ void __launch_bounds__(256) embed_join_kernel(EmbedArgs a) {
-  __shared__ float sums[4][256];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.E, m = a.head->count;
-  const long n_many = (long)a.head->n_many * ((E + 255) / 256), items = n_many + (long)a.head->n_few * ((E + 1023) / 1024);
-  for (long it = blockIdx.x; it < items; it += gridDim.x) {
-    const bool many = it < n_many;                   // (uniform)
-    const int of = many ? (E + 255) / 256 : (E + 1023) / 1024;
-    const long at = many ? it : it - n_many;
-    const int2 run = many ? a.long_list[at / of] : a.long_list[a.list_end - 1 - at / of];
-    const int c0 = run.x, id = run.y, e0 = many ? (int)(at % of) * 256 : (int)(at % of) * 1024 + 256 * wave, e = e0 + 4 * lane;
-    // the chunks that begin with the id follow each other: c0 + 1 ..
-    int parts = 1;
-    for (;;) {
-      const long first = (long)(c0 + parts + lane) * a.chunk;
-      const unsigned long long more = __ballot(first < m && a.key[0][min(first, (long)m - 1)] == id);
-      parts += more == ~0ull ? 64 : __ffsll(~more) - 1;
-      if (more != ~0ull) break;
-    }
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    const int q0 = many ? (int)((long)wave * parts / 4) : 0, q1 = many ? (int)((long)(wave + 1) * parts / 4) : parts;
-    const auto sum = [&](auto whole) {
-      for (int q = q0; q < q1; q += 8) {
-        f32x4 v[8];
+// Ids that go over several chunks.
+// The chunks that begin with the id follow each other from c0 + 1 on; returns the last of them, by a wave: 64 of them, or 64 that are even over what is left, at once.
+__device__ __forceinline__ int last_chunk(const EmbedArgs& a, int c0, int id, int m) {
+  const int lane = threadIdx.x & 63;
+  long c1 = c0, behind = (m + a.chunk - 1) / a.chunk, stride = 1;
+  do {
+    const long c = c1 + (lane + 1) * stride;
+    const unsigned long long more = __ballot(c < behind && a.key[0][min(c, behind - 1) * a.chunk] == id);
+    const int found = more == ~0ull ? 64 : __ffsll(~more) - 1;
+    c1 += found * stride;
+    if (found < 64) behind = min(behind, c1 + stride);
+    stride = (behind - c1 + 63) / 64;
+  } while (behind - c1 > 1);
+  return (int)c1;
+}
+// Sums q0 .. q1 - 1 of an id's (the first is the end of chunk c0, the others the beginnings of the chunks behind), four features from e on
+__device__ __forceinline__ f32x4 add_parts(const EmbedArgs& a, int c0, int q0, int q1, int e) {
+  const int E = a.E;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  const auto run = [&](auto whole) {
+    for (int q = q0; q < q1; q += 8) {
+      f32x4 v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int c = c0 + min(q + k, q1 - 1);
-          const float* const from = a.part + (2L * c + (c == c0 ? 1 : 0)) * E + e;
-          if constexpr (decltype(whole)::value) {
-            v[k] = __builtin_bit_cast(f32x4, *(const u32x4_any4*)from);
-          } else {
+      for (int k = 0; k < 8; ++k) {
+        const int c = min(q + k, q1 - 1);
+        const float* const from = a.part + (2L * (c0 + c) + (c == 0 ? 1 : 0)) * E + e;
+        if constexpr (decltype(whole)::value) {
+          v[k] = __builtin_bit_cast(f32x4, *(const u32x4_any4*)from);
+        } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[k][j] = e + j < E ? from[j] : 0.f;
-          }
+          for (int j = 0; j < 4; ++j) v[k][j] = e + j < E ? from[j] : 0.f;
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (q + k < q1) s += v[k];
       }
-    };
-    if (e0 + 256 <= E) sum(std::true_type{});
-    else sum(std::false_type{});
-    if (many) {
-      __syncthreads();                               // (the sums of the id before have been read)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sums[wave][4 * lane + j] = s[j];
-      __syncthreads();
-      s = (*(const f32x4*)&sums[0][4 * lane] + *(const f32x4*)&sums[1][4 * lane]) + (*(const f32x4*)&sums[2][4 * lane] + *(const f32x4*)&sums[3][4 * lane]);
-      if (wave > 0) continue;
+      for (int k = 0; k < 8; ++k)
+        if (q + k < q1) s += v[k];
     }
-    T* const to = (T*)a.d_table + (long)id * E + e;
+  };
+  if (e + 4 <= E) run(std::true_type{});
+  else run(std::false_type{});
+  return s;
+}
+template <typename T> __device__ __forceinline__ void put_joined(const EmbedArgs& a, int id, int e, const f32x4& s) {
+  T* const to = (T*)a.d_table + (long)id * a.E + e;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (e + j < E) to[j] = (T)(a.accumulate ? fmaf(s[j], a.scale, (float)to[j]) : s[j] * a.scale);
+  for (int j = 0; j < 4; ++j)
+    if (e + j < a.E) to[j] = (T)(a.accumulate ? fmaf(s[j], a.scale, (float)to[j]) : s[j] * a.scale);
+}
+// An id of more than MANY_PARTS chunks: 256 features a workgroup, whose waves, and in them groups of 2^cl lanes, where a row has no more, take a run of the
+// chunks each (the first wgs_many workgroups).  The others, most of them: 256 features a wave.  (131072 tokens x 64, two in three the same id: 928 us with four waves and whole rows, 112 so; x 1024 145 and 124)
+constexpr int JOIN_WG = 512, JOIN_WAVES = JOIN_WG / 64;
+template <typename T> __global__ void __launch_bounds__(JOIN_WG) embed_join_kernel(EmbedArgs a, int cl, int wgs_many) {
+  __shared__ __attribute__((aligned(16))) float sums[JOIN_WAVES][256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = a.head->count, blocks = (a.E + 255) / 256;
+  const int units = JOIN_WAVES << (6 - cl), unit = (wave << (6 - cl)) + (lane >> cl), l = lane & ((1 << cl) - 1);
+  if ((int)blockIdx.x >= wgs_many) {
+    const long n_few = (long)a.head->n_few * blocks, step = (long)(gridDim.x - wgs_many) * JOIN_WAVES;
+    for (long it = (long)(blockIdx.x - wgs_many) * JOIN_WAVES + wave; it < n_few; it += step) {
+      const int2 run = a.long_list[a.list_end - 1 - it / blocks];
+      const int e = (int)(it % blocks) * 256 + 4 * lane, last = last_chunk(a, run.x, run.y, m);
+      if (e < a.E) put_joined<T>(a, run.y, e, add_parts(a, run.x, 0, last - run.x + 1, e));
+    }
+    return;
+  }
+  const long n_many = (long)a.head->n_many * blocks;
+  for (long it = blockIdx.x; it < n_many; it += wgs_many) {
+    const int2 run = a.long_list[it / blocks];
+    const int e = (int)(it % blocks) * 256 + 4 * l, parts = last_chunk(a, run.x, run.y, m) - run.x + 1;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (e < a.E) s = add_parts(a, run.x, (int)((long)unit * parts / units), (int)((long)(unit + 1) * parts / units), e);
+    for (int o = 1 << cl; o < 64; o *= 2)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] += __shfl_xor(s[j], o);
+    __syncthreads();                                 // (the sums of the id before have been read)
+    if (lane < (1 << cl)) *(f32x4*)&sums[wave][4 * l] = s;
+    __syncthreads();
+    if (wave == 0 && lane < (1 << cl) && e < a.E) {
+      s = *(const f32x4*)&sums[0][4 * l];
+      for (int w = 1; w < JOIN_WAVES; ++w) s += *(const f32x4*)&sums[w][4 * l];
+      put_joined<T>(a, run.y, e, s);
+    }
   }
 }
 
@@ -668,7 +694,11 @@ template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStre
   const bool past = whole_lines(a.d_table, (long)sizeof(T) * a.E, (long)sizeof(T) * a.E);
   embed_sum_kernel<T, ADD><<<(unsigned)(wgs + up(a.V - row, piece)), 256, 0, s>>>(a, tl, (unsigned)wgs, n_eb, row / piece, low, past);
   if (n_chunks > 1) {
-    embed_join_kernel<T><<<(unsigned)std::min((n_chunks - 1) * up(a.E, 256), 8L * a.n_cu), 256, 0, s>>>(a);
+    int cl = 0;                                      // lanes for four features each of a row, or of 256 features
+    while (cl < 6 && (4 << cl) < a.E) ++cl;
+    const long blocks = up(a.E, 256), many = n_chunks > MANY_PARTS ? std::min(n_chunks / MANY_PARTS * blocks, (long)a.n_cu) : 0;
+    const long few = std::min(up((n_chunks - 1) * blocks, JOIN_WAVES), 3L * a.n_cu);
+    embed_join_kernel<T><<<(unsigned)(many + few), JOIN_WG, 0, s>>>(a, cl, (int)many);
   }
   return hipGetLastError();
 }

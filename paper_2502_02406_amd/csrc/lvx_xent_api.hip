@@ -134,6 +134,7 @@ EntryPlan entries_of(int64_t n, int64_t V, int32_t K) {
   e.fwd = at;
   return e;
 }
+float log2_over(float temperature) { return (float)(1.4426950408889634 / temperature); }      // log2 e / temperature
 bool entries_ok(int32_t K) { return K >= 1 && K <= DISTIL_MOST_ENTRIES; }
 // what a call names beside the product's operands
 lvx_status distil_check(const lvx_distil* p, lvx_dtype dtype, const int64_t* ids, const void* teacher, lvx_dtype teacher_dtype, const void* loss,
@@ -144,7 +145,7 @@ lvx_status distil_check(const lvx_distil* p, lvx_dtype dtype, const int64_t* ids
   if (teacher_dtype != LVX_F32 && teacher_dtype != LVX_BF16) return LVX_ERR_DTYPE;
   if (p->K < 1) return LVX_ERR_SHAPE;
   if (!entries_ok(p->K)) return LVX_ERR_UNSUPPORTED;
-  if (!(p->temperature > 0.f) || !(1.f / p->temperature > 0.f) || !(1.f / p->temperature < __builtin_inff())) return LVX_ERR_SHAPE;
+  if (!(p->temperature > 0.f) || !(1.f / p->temperature > 0.f) || !(log2_over(p->temperature) < __builtin_inff())) return LVX_ERR_SHAPE;
   if (!aligned(ids, 8) || !aligned(teacher, teacher_dtype == LVX_F32 ? 4 : 2) || !aligned(loss, 4) || !aligned(lse, 4) || !aligned(ln_p, 4))
     return LVX_ERR_STRIDE;
   return workspace && aligned(workspace, ALIGN) ? LVX_OK : LVX_ERR_WORKSPACE;
@@ -154,7 +155,7 @@ void distil_args(const lvx_distil* p, const int64_t* ids, const void* teacher, l
   const auto at = [&](size_t o) -> char* { return (char*)workspace + o; };
   a->temperature = p->temperature;
   a->inv_t = 1.f / p->temperature;
-  a->z2 = (float)(1.4426950408889634 / p->temperature);
+  a->z2 = log2_over(p->temperature);
   a->K = p->K;
   a->blocks = (int)((p->V + 63) / 64);
   a->ids = ids; a->teacher = teacher; a->teacher_bf16 = teacher_dtype == LVX_BF16; a->ln_p = ln_p;

@@ -31,7 +31,7 @@ def test_shared_refusals(lib, call):  # noqa: F811
         assert call(lib, prob(), **{name: None}) == -1, name
     assert call(lib, prob(n=0)) == -2 and call(lib, prob(V=0)) == -2 and call(lib, prob(E=0)) == -2 and call(lib, prob(K=0)) == -2
     assert call(lib, prob(K=1025)) == -7 and call(lib, prob(E=200)) == -7
-    for T in (0.0, -1.0, float("nan"), float("inf"), 1e-45):
+    for T in (0.0, -1.0, float("nan"), float("inf"), 1e-45, 4e-39):
         assert call(lib, prob(temperature=T)) == -2, T
     assert call(lib, prob(), dtype=4) == -3 and call(lib, prob(), td=2) == -3
     assert call(lib, prob(x_ss=255)) == -4 and call(lib, prob(x_ss=260)) == -4 and call(lib, prob(n=1 << 20, x_ss=4096)) == -4

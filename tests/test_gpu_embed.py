@@ -179,3 +179,18 @@ def test_refused_overlap():
         B.lvx_embed_fwd(t, ids, t[8:16])
     with pytest.raises(B.LvxError):
         B.lvx_embed_bwd(t[:8], ids, t, ws)
+
+
+@pytest.mark.parametrize("n,E,V,share", [(131072, 64, 5000, 1.0), (70000, 24, 900, 0.7), (20000, 40, 50, 0.5), (9000, 520, 9000, 0.9), (3000, 8, 7, 0.95)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_id_that_most_tokens_have(dtype, n, E, V, share):
+    """Its sums go over whole groups of chunks, which begin and end anywhere; other ids stand in front of it and behind."""
+    g = torch.Generator().manual_seed(n)
+    for hot in (0, V // 2, V - 1):
+        ids = torch.where(torch.rand(n, generator=g) < share, hot, torch.randint(V, (n,), generator=g))
+        args = inputs(n, E, V, dtype, 5, ids=ids)
+        y, dt = run(*args, 0.5)
+        check(*args, 0.5, y, dt)
+        old = torch.ones((V, E), dtype=DT[dtype], device="cuda")
+        y, dt = run(*args, 0.5, old=old)
+        check(*args, 0.5, y, dt, old)
