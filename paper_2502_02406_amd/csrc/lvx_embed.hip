@@ -246,98 +246,47 @@ __device__ __forceinline__ void sort_few(const EmbedArgs& a, const Sort& sort, i
   }
 }
 
-// Up to ONE_WG tokens: all digits in one launch, by one workgroup, or by 2^split of them, each of which takes the ids with its value of the highest bits
-// and counts those with lower ones (all ids of a batch in one of these: as slow as one workgroup).
-constexpr int ONE_ROUNDS = 8, ONE_WG = SORT_WG * ONE_ROUNDS, ONE_SPLIT = 3;
-inline int one_lds(int bits, long n) { return sort_lds(bits) + 2 * (int)sizeof(int) * (int)((n + SORT_WG - 1) / SORT_WG * SORT_WG); }
-template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_kernel(EmbedArgs a, Sort sort, Clear clear) {
-  const int groups = 1 << sort.split, mine = blockIdx.x;
-  if (mine >= groups) {
-    clear_table((T*)a.d_table + clear.from, clear.count, mine - groups, clear.wgs);
-    return;
-  }
-  extern __shared__ __attribute__((aligned(16))) int sort_mem[];
-  if (a.n <= FEW) {
-    sort_few(a, sort, sort_mem);
-    return;
-  }
+// Up to ONE_MOST tokens: all digits in one launch, by one workgroup, or by 2^split of them, each of which takes the ids with its value of the highest bits
+// and counts those with lower ones.  LDS holds ONE_WG tokens of a workgroup; one that has more of them (most ids alike) sorts in the two lists in memory.
+constexpr int ONE_ROUNDS = 8, ONE_WG = SORT_WG * ONE_ROUNDS, ONE_MOST = 32 * SORT_WG;
+inline int one_room(long n) { return (int)std::min((long)ONE_WG, (n + SORT_WG - 1) / SORT_WG * SORT_WG); }
+inline int one_lds(int bits, long n) { return sort_lds(bits) + 2 * (int)sizeof(int) * one_room(n); }
+struct SortMem { int *cnt, *start, *sums, *skey, *stok; };
+// The m tokens of group `mine`, in order in skey and stok (ids without the bits of the group), to places `base` and behind
+__device__ __forceinline__ void sort_own(const EmbedArgs& a, const Sort& sort, const SortMem& s, int mine, int m, int base) {
   const int bits = sort.bits, digits = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int* const cnt = sort_mem;
-  int* const start = cnt + sort_counts(digits);
-  int* const sums = start + digits;
-  int* const skey = sums + SORT_WAVES;
-  int per_wave = (int)((a.n + SORT_WG - 1) / SORT_WG) * 64, rounds = per_wave / 64;
-  int* const stok = skey + SORT_WAVES * per_wave;
+  const int rounds = (m + SORT_WG - 1) / SORT_WG, per_wave = 64 * rounds;
   int key[ONE_ROUNDS], tok[ONE_ROUNDS], dig[ONE_ROUNDS], rank[ONE_ROUNDS];
-  // the ids, in order
-  long id[ONE_ROUNDS];
-#pragma unroll
-  for (int r = 0; r < ONE_ROUNDS; ++r) {
-    const long i = wave * per_wave + 64 * r + lane;
-    id[r] = r < rounds && i < a.n ? a.ids[i] : -1;
-  }
-  int own = 0, lower = 0;                            // of the wave
-#pragma unroll
-  for (int r = 0; r < ONE_ROUNDS; ++r) {
-    const int group = id[r] >= 0 && id[r] < a.V ? (int)(id[r] >> sort.of) : -1;
-    key[r] = group == mine ? (int)id[r] & ((1 << sort.of) - 1) : -1;
-    const unsigned long long on = __ballot(group == mine);
-    rank[r] = own + __popcll(on & ((1ull << lane) - 1));
-    own += __popcll(on);
-    lower += __popcll(__ballot(group >= 0 && group < mine));
-  }
-  if (lane == 0) {
-    cnt[wave] = own;
-    cnt[SORT_WAVES + wave] = lower;
-  }
-  __syncthreads();
-  int before = 0, m = 0, base = 0;                   // own ones of the waves before, of all; ids of the groups before
-#pragma unroll
-  for (int w = 0; w < SORT_WAVES; ++w) {
-    const int c = cnt[w];
-    before += w < wave ? c : 0;
-    m += c;
-    base += cnt[SORT_WAVES + w];
-  }
-#pragma unroll
-  for (int r = 0; r < ONE_ROUNDS; ++r)
-    if (key[r] >= 0) {
-      skey[before + rank[r]] = key[r];
-      stok[before + rank[r]] = wave * per_wave + 64 * r + lane;
-    }
-  rounds = (m + SORT_WG - 1) / SORT_WG;              // (of the group's own)
-  per_wave = 64 * rounds;
   const auto take = [&]() {
 #pragma unroll
     for (int r = 0; r < ONE_ROUNDS; ++r) {
       const int i = wave * per_wave + 64 * r + lane;
       const bool on = r < rounds && i < m;
-      key[r] = on ? skey[i] : -1;
-      tok[r] = on ? stok[i] : 0;
+      key[r] = on ? s.skey[i] : -1;
+      tok[r] = on ? s.stok[i] : 0;
     }
   };
-  __syncthreads();
   take();
   const int low = bits * (sort.passes - 1), tops = 1 << (sort.of - low);      // (values of the last digit)
   for (int p = 0; p < sort.passes; ++p) {
-    clear_counts(cnt, digits);
+    clear_counts(s.cnt, digits);
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < ONE_ROUNDS; ++r) dig[r] = key[r] < 0 ? -1 : (key[r] >> (p * bits)) & (digits - 1);
-    rank_in_wave<ONE_ROUNDS>(dig, rank, rounds, cnt + wave * digits, bits);
+    rank_in_wave<ONE_ROUNDS>(dig, rank, rounds, s.cnt + wave * digits, bits);
     __syncthreads();
-    const int count = counts_to_starts(cnt, digits);
+    const int count = counts_to_starts(s.cnt, digits);
     int all;
-    const int at = exclusive_sum(count, sums, &all);
-    if (tid < digits) start[tid] = at;
+    const int at = exclusive_sum(count, s.sums, &all);
+    if (tid < digits) s.start[tid] = at;
     if (p == sort.passes - 1 && tid < tops) a.top[mine * tops + tid] = base + at;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < ONE_ROUNDS; ++r)
       if (dig[r] >= 0) {
-        const int to = start[dig[r]] + cnt[wave * digits + dig[r]] + rank[r];
-        skey[to] = key[r];
-        stok[to] = tok[r];
+        const int to = s.start[dig[r]] + s.cnt[wave * digits + dig[r]] + rank[r];
+        s.skey[to] = key[r];
+        s.stok[to] = tok[r];
       }
     __syncthreads();
     take();
@@ -350,8 +299,128 @@ template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_
       a.tok[0][base + i] = tok[r];
     }
   }
+}
+// Which list pass p writes; it reads the other one.
+__device__ __forceinline__ int list_of(const Sort& sort, int p) { return (sort.passes - 1 - p) & 1; }
+// The same of any number of tokens, which stand from `base` on in the list that pass 0 reads
+__device__ __forceinline__ void sort_own_in_memory(const EmbedArgs& a, const Sort& sort, const SortMem& s, int mine, int m, int base) {
+  constexpr int R = 4;
+  const int bits = sort.bits, digits = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int low = bits * (sort.passes - 1), tops = 1 << (sort.of - low);
+  for (int p = 0; p < sort.passes; ++p) {
+    const int to = list_of(sort, p), from = 1 - to;
+    const bool last = p == sort.passes - 1;
+    __syncthreads();
+    if (tid < digits) s.start[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < m; i += SORT_WG) atomicAdd(&s.start[(a.key[from][base + i] >> (p * bits)) & (digits - 1)], 1);
+    __syncthreads();
+    const int count = tid < digits ? s.start[tid] : 0;
+    int all;
+    const int at = exclusive_sum(count, s.sums, &all);
+    if (tid < digits) s.start[tid] = at;
+    if (last && tid < tops) a.top[mine * tops + tid] = base + at;
+    for (int b = 0; b < m; b += SORT_WG * R) {
+      int key[R], tok[R], dig[R], rank[R];
+      __syncthreads();
+      clear_counts(s.cnt, digits);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int i = b + (wave * R + r) * 64 + lane;
+        key[r] = i < m ? a.key[from][base + i] : -1;
+        tok[r] = i < m ? a.tok[from][base + i] : 0;
+        dig[r] = key[r] < 0 ? -1 : (key[r] >> (p * bits)) & (digits - 1);
+      }
+      __syncthreads();
+      rank_in_wave<R>(dig, rank, R, s.cnt + wave * digits, bits);
+      __syncthreads();
+      const int in_step = counts_to_starts(s.cnt, digits);
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (dig[r] >= 0) {
+          const int i = base + s.start[dig[r]] + s.cnt[wave * digits + dig[r]] + rank[r];
+          a.key[to][i] = last ? key[r] + (mine << sort.of) : key[r];
+          a.tok[to][i] = tok[r];
+        }
+      __syncthreads();
+      if (tid < digits) s.start[tid] += in_step;
+    }
+    __threadfence_block();                           // (the next pass reads what other waves of this workgroup have written)
+  }
+}
+template <typename T, int ROUNDS> __global__ void __launch_bounds__(SORT_WG) embed_sort_one_kernel(EmbedArgs a, Sort sort, Clear clear, int room) {
+  const int groups = 1 << sort.split, mine = blockIdx.x;
+  if (mine >= groups) {
+    clear_table((T*)a.d_table + clear.from, clear.count, mine - groups, clear.wgs);
+    return;
+  }
+  extern __shared__ __attribute__((aligned(16))) int sort_mem[];
+  if (ROUNDS == ONE_ROUNDS && a.n <= FEW) {
+    sort_few(a, sort, sort_mem);
+    return;
+  }
+  const int digits = 1 << sort.bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  SortMem s;
+  s.cnt = sort_mem;
+  s.start = s.cnt + sort_counts(digits);
+  s.sums = s.start + digits;
+  s.skey = s.sums + SORT_WAVES;
+  s.stok = s.skey + room;
+  const int per_wave = (int)((a.n + SORT_WG - 1) / SORT_WG) * 64, rounds = per_wave / 64;
+  // the ids, in order
+  int id[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int i = wave * per_wave + 64 * r + lane;
+    const long x = r < rounds && i < a.n ? a.ids[i] : -1;
+    id[r] = x >= 0 && x < a.V ? (int)x : -1;
+  }
+  int own = 0, lower = 0;                            // of the wave
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int group = id[r] >> sort.of;              // (-1: none)
+    own += __popcll(__ballot(group == mine));
+    lower += __popcll(__ballot(group >= 0 && group < mine));
+  }
+  if (lane == 0) {
+    s.cnt[wave] = own;
+    s.cnt[SORT_WAVES + wave] = lower;
+  }
+  __syncthreads();
+  int before = 0, m = 0, base = 0;                   // own ones of the waves before, of all; ids of the groups before
+#pragma unroll
+  for (int w = 0; w < SORT_WAVES; ++w) {
+    const int c = s.cnt[w];
+    before += w < wave ? c : 0;
+    m += c;
+    base += s.cnt[SORT_WAVES + w];
+  }
+  const bool fits = m <= room;
+  int* const far_key = a.key[1 - list_of(sort, 0)] + base;
+  int* const far_tok = a.tok[1 - list_of(sort, 0)] + base;
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const bool mine_too = id[r] >> sort.of == mine;
+    const unsigned long long on = __ballot(mine_too);
+    if (mine_too) {
+      const int to = before + __popcll(on & ((1ull << lane) - 1)), key = id[r] & ((1 << sort.of) - 1), tok = wave * per_wave + 64 * r + lane;
+      if (fits) {
+        s.skey[to] = key;
+        s.stok[to] = tok;
+      } else {
+        far_key[to] = key;
+        far_tok[to] = tok;
+      }
+    }
+    before += __popcll(on);
+  }
+  if (!fits) __threadfence_block();
+  __syncthreads();
+  if (ROUNDS == ONE_ROUNDS || fits) sort_own(a, sort, s, mine, m, base);
+  else sort_own_in_memory(a, sort, s, mine, m, base);
   if (tid == 0 && mine == groups - 1) {
-    a.top[groups * tops] = base + m;
+    a.top[groups << (sort.of - sort.bits * (sort.passes - 1))] = base + m;
     a.head->count = base + m;
     a.head->n_many = a.head->n_few = 0;
   }
@@ -645,7 +714,7 @@ template <typename T> __global__ void __launch_bounds__(JOIN_WG) embed_join_kern
 long up(long n, long by) { return (n + by - 1) / by; }
 
 // Bytes of the table that a launch of the sort clears: about what goes to memory in its time.
-constexpr long CLEAR_ONE = 20 << 20, CLEAR_ROUND = 4 << 20, CLEAR_MOVE = 48 << 20;
+constexpr long CLEAR_ONE = 20 << 20, CLEAR_ROUND = 3 << 20, CLEAR_MORE = 1 << 20, CLEAR_MOVE = 48 << 20;
 
 template <typename T> hipError_t embed_fwd(const EmbedArgs& a, hipStream_t s) {
   const int tl = team_log(a.E);
@@ -662,18 +731,26 @@ template <typename T> Clear clear_some(const EmbedArgs& a, long bytes, long piec
   *row += rows;
   return c;
 }
+template <typename T, int ROUNDS> hipError_t sort_one(const EmbedArgs& a, const Sort& sort, const Clear& clear, hipStream_t s) {
+  static SmemOnce once;
+  const hipError_t e = ensure_dynamic_lds((const void*)embed_sort_one_kernel<T, ROUNDS>, one_lds(EMBED_DIGIT_BITS, ONE_WG), &once);
+  if (e != hipSuccess) return e;
+  embed_sort_one_kernel<T, ROUNDS><<<(1 << sort.split) + clear.wgs, SORT_WG, one_lds(sort.bits, a.n), s>>>(a, sort, clear, one_room(a.n));
+  return hipGetLastError();
+}
+// log2 of the workgroups that share a sort (5514 ids: one 17 us, eight 11.5; 20000: 32 workgroups 17.6, the passes over two launches each 26; 65536: 38 and 36)
+int split_of(long n) { return n <= SORT_WG || n > ONE_MOST ? 0 : n <= ONE_WG ? 3 : 5; }
 template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStream_t s) {
-  const Sort sort = sort_of(a.V, a.n > SORT_WG && a.n <= ONE_WG ? ONE_SPLIT : 0);
+  const Sort sort = sort_of(a.V, split_of(a.n));
   const int low = sort.bits * (sort.passes - 1);
   const long piece = 1L << std::min(low, ROWS_LOG);
   long row = ADD ? a.V : 0;                          // the rows before are cleared already
   hipError_t e;
-  if (a.n <= ONE_WG) {
-    static SmemOnce once;
-    e = ensure_dynamic_lds((const void*)embed_sort_one_kernel<T>, one_lds(EMBED_DIGIT_BITS, ONE_WG), &once);
+  if (a.n <= ONE_MOST) {
+    const long rounds = up(a.n, SORT_WG);
+    const Clear clear = clear_some<T>(a, CLEAR_ONE + CLEAR_ROUND * std::min(rounds, 8L) + CLEAR_MORE * rounds, piece, &row);
+    e = a.n <= ONE_WG ? sort_one<T, ONE_ROUNDS>(a, sort, clear, s) : sort_one<T, ONE_MOST / SORT_WG>(a, sort, clear, s);
     if (e != hipSuccess) return e;
-    const Clear clear = clear_some<T>(a, CLEAR_ONE + CLEAR_ROUND * up(a.n, SORT_WG), piece, &row);
-    embed_sort_one_kernel<T><<<(1 << sort.split) + clear.wgs, SORT_WG, one_lds(sort.bits, a.n), s>>>(a, sort, clear);
   } else {
     static SmemOnce once;
     e = ensure_dynamic_lds((const void*)embed_move_kernel<T>, sort_lds(EMBED_DIGIT_BITS), &once);

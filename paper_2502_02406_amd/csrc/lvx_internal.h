@@ -285,7 +285,7 @@ struct EmbedArgs {
   float* part;          // [chunks][2][E]
   int chunk;            // sorted tokens of a chunk
 };
-constexpr int EMBED_BLOCKS = 256, EMBED_DIGIT_BITS = 10, EMBED_DIGITS = 1 << EMBED_DIGIT_BITS, EMBED_TOPS = 8 * EMBED_DIGITS;
+constexpr int EMBED_BLOCKS = 256, EMBED_DIGIT_BITS = 10, EMBED_DIGITS = 1 << EMBED_DIGIT_BITS, EMBED_TOPS = 32 * EMBED_DIGITS;
 int embed_chunk(long n, int E);
 long embed_chunks_room(long n);             // the most chunks of n tokens
 size_t embed_part_room(long n, int E);      // bytes of `part` for n tokens of E features or fewer

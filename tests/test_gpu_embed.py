@@ -74,7 +74,7 @@ def check(table, ids, dy, scale, y, dt, old=None):
 
 SIZES = [(1, 1, 1), (1, 4096, 100), (3, 7, 5), (64, 64, 1000), (65, 129, 1), (700, 1001, 300), (2000, 512, 33000), (8192, 64, 1025), (8193, 40, 50021),
          (20000, 8, 131072), (10000, 2056, 7), (9000, 16, (1 << 20) + 5), (12289, 520, 1024), (40000, 24, 300), (5000, 40, 9), (1025, 16, 2), (7000, 24, 200000), (1024, 8, 5000), (16, 256, 3), (17, 40, 2), (256, 16, 900), (257, 16, 900),
-         (3000, 8, (1 << 21) + 3)]
+         (3000, 8, (1 << 21) + 3), (32768, 16, 4000), (32769, 16, 4000), (30000, 8, 2), (15000, 8, (1 << 20) + 7)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
