@@ -543,13 +543,20 @@ template <typename T, bool ADD> __device__ __forceinline__ void finish_row(const
 }
 
 // Rows that no token has are set to 0: workgroup `wg` takes 2^sub of the ids that share their last digit, finds which of them tokens have (their
-// sorted tokens are from top[digit] on) and clears the others.
-constexpr int ROWS_LOG = 6;
-template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs& a, long wg, int low, bool past) {
-  __shared__ unsigned has[1 << (ROWS_LOG - 5)];
-  const int sub = min(low, ROWS_LOG), tid = threadIdx.x;
+// sorted tokens are from top[digit] on) and clears the others.  About 16 KB of rows: many even workgroups (forward and backward of 65536 x
+// 4096, table 131072, with 512 KB 500 us, 64 KB 490, 32 KB 480, 16 KB 473, 8 KB 486; of 2048 x 4096, table 32768, 72, 69, 68, 67, 64.  Sums among them instead of in
+// front of them: 580 and 65).
+constexpr int MOST_ROWS_LOG = 6;
+inline int clear_rows_log(long row_bytes, int low) {
+  int l = 0;
+  while (l < std::min(low, MOST_ROWS_LOG) && (row_bytes << l) < (16 << 10)) ++l;
+  return l;
+}
+template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs& a, long wg, int low, int sub, bool past) {
+  __shared__ unsigned has[1 << (MOST_ROWS_LOG - 5)];
+  const int tid = threadIdx.x;
   const long v0 = wg << sub, v1 = min(a.V, v0 + (1L << sub));
-  if (tid < (1 << (ROWS_LOG - 5))) has[tid] = 0u;
+  if (tid < (1 << (MOST_ROWS_LOG - 5))) has[tid] = 0u;
   __syncthreads();
   const int digit = (int)(v0 >> low);
   for (int i = a.top[digit] + tid; i < a.top[digit + 1]; i += 256) {
@@ -570,11 +577,11 @@ template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs
 }
 
 // Sums over a chunk of the sorted tokens, by a team (ADD: to what is there); workgroups from `sums_x` on clear rows, the first of them piece `early` of the table
-// (low: bits of an id below its last digit)
-template <typename T, bool ADD> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, int tl, unsigned sums_x, int n_eb, long early, int low, bool past) {
+// (2^sub rows; low: bits of an id below its last digit)
+template <typename T, bool ADD> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, int tl, unsigned sums_x, int n_eb, long early, int low, int sub, bool past) {
   if constexpr (!ADD) {
     if (blockIdx.x >= sums_x) {
-      clear_rows<T>(a, early + (blockIdx.x - sums_x), low, past);
+      clear_rows<T>(a, early + (blockIdx.x - sums_x), low, sub, past);
       return;
     }
   }
@@ -743,7 +750,8 @@ int split_of(long n) { return n <= SORT_WG || n > ONE_MOST ? 0 : n <= ONE_WG ? 3
 template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStream_t s) {
   const Sort sort = sort_of(a.V, split_of(a.n));
   const int low = sort.bits * (sort.passes - 1);
-  const long piece = 1L << std::min(low, ROWS_LOG);
+  const int sub = clear_rows_log((long)sizeof(T) * a.E, low);
+  const long piece = 1L << sub;
   long row = ADD ? a.V : 0;                          // the rows before are cleared already
   hipError_t e;
   if (a.n <= ONE_MOST) {
@@ -769,7 +777,7 @@ template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStre
   const int tl = team_log(a.E), n_eb = (int)up(a.E, V8 << tl);
   const long n_chunks = up(a.n, a.chunk), wgs = up(n_chunks, 256 >> tl) * n_eb;
   const bool past = whole_lines(a.d_table, (long)sizeof(T) * a.E, (long)sizeof(T) * a.E);
-  embed_sum_kernel<T, ADD><<<(unsigned)(wgs + up(a.V - row, piece)), 256, 0, s>>>(a, tl, (unsigned)wgs, n_eb, row / piece, low, past);
+  embed_sum_kernel<T, ADD><<<(unsigned)(wgs + up(a.V - row, piece)), 256, 0, s>>>(a, tl, (unsigned)wgs, n_eb, row / piece, low, sub, past);
   if (n_chunks > 1) {
     int cl = 0;                                      // lanes for four features each of a row, or of 256 features
     while (cl < 6 && (4 << cl) < a.E) ++cl;
