@@ -4,9 +4,9 @@
 //   loss_i = sum_k q_k (ln q_k - z_ik / T + lse_i),   lse_i = ln sum_v exp(z_iv / T)
 //   g_iv = (exp(z_iv / T - lse_i) - sum over k with id_ik = v of q_k) d_loss_i / T,   dx = g w,   dw = g^T x
 //
-// What differs from the cross entropy is that a token has K logits to be handed out instead of one.  The first launch sorts every token's ids
+// What differs from the cross entropy is that a token has K logits to be handed out instead of one.  A launch sorts every listed token's ids
 // and counts those below every multiple of 64, so that a tile's epilogue finds the ones among its columns with one lookup a row, and
-// leaves their logits in their order.  The gradient's tiles write exp(z / T - lse) d_loss / T everywhere; at the teacher's entries another launch
+// leaves their logits in their order (few tokens' few entries: direct_of).  The gradient's tiles write exp(z / T - lse) d_loss / T everywhere; at the teacher's entries another launch
 // puts exp(ln p) - q in its place, from the ln p of the forward pass, with one rounding like everywhere else: n K values beside the n V.
 #include "lvx_xent_kernels.h"
 
@@ -14,16 +14,7 @@ namespace lvx {
 
 namespace {
 
-// entry k of token i: whether it is there, and its logit by the temperature
-struct Entry { bool there; long id; float t; };
-__device__ __forceinline__ Entry entry_of(const XentArgs& a, long i, int k) {
-  Entry e;
-  e.id = a.ids[i * a.K + k];
-  e.there = e.id >= 0;
-  const float t = a.teacher_bf16 ? __uint_as_float((unsigned)((const uint16_t*)a.teacher)[i * a.K + k] << 16) : ((const float*)a.teacher)[i * a.K + k];
-  e.t = t / a.temperature;
-  return e;
-}
+// stat: of a token's entries, the largest logit by the temperature and the logarithm of the sum of exponentials against it
 __device__ __forceinline__ float ln_q_of(const Entry& e, float2 stat) { return (e.t - stat.x) - stat.y; }
 
 // K entries in LDS, rounded up to four
@@ -102,7 +93,7 @@ template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kerne
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
     if (lane == 0) {
-      ((int64_t*)a.labels)[i] = !any ? -1 : far ? a.V : 0;
+      ((int64_t*)a.labels)[i] = label_of(any, far, a.V);
       a.q_stat[i] = make_float2(top, logf(sum));
     }
     if constexpr (SORT) {
@@ -110,6 +101,96 @@ template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kerne
       sort_entries(a, i, keys, keys + entries_up(K));
     }
   }
+}
+// stat by lanes that share its entries: `lane` of W of them
+template <int W> __device__ __forceinline__ float2 stat_of(const XentArgs& a, long tok, int lane) {
+  float top = -__builtin_inff(), sum = 0.f;
+  for (int k = lane; k < a.K; k += W) {
+    const Entry e = entry_of(a, tok, k);
+    if (e.there) top = fmaxf(top, e.t);
+  }
+#pragma unroll
+  for (int o = 1; o < W; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+  for (int k = lane; k < a.K; k += W) {
+    const Entry e = entry_of(a, tok, k);
+    sum += e.there ? expf(e.t - top) : 0.f;
+  }
+#pragma unroll
+  for (int o = 1; o < W; o *= 2) sum += __shfl_xor(sum, o);
+  return make_float2(top, logf(sum));
+}
+// The first two launches of a pass in one, for up to LISTED tokens of few entries: a thread a token, then the list of those that take part
+// (xent_list_kernel).  It saves a launch, twice with gradients, but one workgroup's loads have no others beside them (with gradients of n x 512 against 2048,
+// two launches and one: 128 with 4 entries 61.6 -> 57.0 us, with 16 63.4 -> 63.9; 512 with 8 74.9 -> 73.9; 768 with 8 79.0 -> 80.1; 1024 with 6 83.3 -> 81.0,
+// with 8 83.4 -> 86.7).
+constexpr int LISTED = 1024, LISTED_ENTRIES = 8, LISTED_IN_ALL = 6144;
+__global__ void __launch_bounds__(LISTED) distil_list_kernel(XentArgs a, bool forward) {
+  __shared__ int counts[16];
+  __shared__ float tops[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = a.K;
+  const long i = min((long)tid, a.n - 1);
+  const bool there = tid < a.n;
+  float top = -__builtin_inff(), sum = 0.f;
+  bool any = false, far = false;
+  for (int k0 = 0; k0 < K; k0 += 8) {
+    Entry e[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      e[k] = entry_of(a, i, min(k0 + k, K - 1));
+      e[k].there &= k0 + k < K;
+    }
+    // (the sum goes along with the largest so far; one that is still -infinity has none)
+    float most = top;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      any |= e[k].there && !(e[k].t == -__builtin_inff());
+      far |= e[k].there && e[k].id >= a.V;
+      if (e[k].there) most = fmaxf(most, e[k].t);
+    }
+    sum = top == most || top == -__builtin_inff() ? sum : sum * expf(top - most);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += e[k].there && (most != -__builtin_inff() || e[k].t != most) ? expf(e[k].t - most) : 0.f;
+    top = most;
+  }
+  const long label = there ? label_of(any, far, a.V) : -1;
+  const float d = a.d_loss && label >= 0 ? a.d_loss[i] * a.inv_t : 0.f, lse = a.d_loss && label >= 0 ? a.lse[i] : 0.f;
+  if (there) {
+    ((int64_t*)a.labels)[i] = label;
+    a.q_stat[i] = make_float2(top, logf(sum));
+  }
+  const unsigned long long on = __ballot(label >= 0);
+  float largest = fabsf(d) < __builtin_inff() ? fabsf(d) : 0.f;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) largest = fmaxf(largest, __shfl_xor(largest, o));
+  if (lane == 0) {
+    counts[wave] = __popcll(on);
+    tops[wave] = largest;
+  }
+  __syncthreads();
+  int at = __popcll(on & ((1ull << lane) - 1)), total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    const int c = counts[w];
+    at += w < wave ? c : 0;
+    total += c;
+    largest = fmaxf(largest, tops[w]);
+  }
+  if (label >= 0) {
+    a.tok[at] = (int)i;
+    a.lab[at] = label < a.V ? (int)label : -1;
+    if (a.d_loss) a.row[at] = make_float2(lse * LOG2E, label < a.V ? d : __builtin_nanf(""));
+  } else if (forward && there) {
+    a.loss[i] = 0.f;
+    a.lse_out[i] = 0.f;
+    for (int k = 0; k < K; ++k) a.ln_p[i * K + k] = 0.f;
+  }
+  const int parts = dx_parts((total + a.tile_rows - 1) / a.tile_rows * ((a.E + a.tile - 1) / a.tile), (int)(a.piece / BK), a.n_cu, a.slots);
+  const int dw_parts = a.dw_slots > 0 ? dx_parts(a.dw_tiles, (total + BK - 1) / BK, a.n_cu, a.dw_slots) : 1;
+  if (tid != 0) return;
+  a.head->count = total;
+  a.head->scale = largest > 0.f ? largest : 1.f;
+  a.head->parts = parts;
+  a.head->dw_parts = dw_parts;
 }
 // The listed tokens' ids in order
 __global__ void __launch_bounds__(256) distil_sort_kernel(XentArgs a) {
@@ -127,11 +208,13 @@ __global__ void __launch_bounds__(256) distil_sort_kernel(XentArgs a) {
 __global__ void __launch_bounds__(256) distil_join_kernel(XentArgs a, int n_parts) {
   __shared__ float sm[8][33], ss[8][33], lses[8];
   const int row_l = threadIdx.x % 8, lane = threadIdx.x / 8;
-  const Own own = a.own ? own_list(a) : Own{};
+  const Own own = a.own ? own_list<TEACHER>(a) : Own{};
   const int count = a.own ? own.count : a.head->count;
   if (a.own && blockIdx.x == 0 && (int)threadIdx.x >= count && threadIdx.x < a.n) {        // (the tokens that are not listed)
     a.loss[own.tok] = 0.f;
     a.lse_out[own.tok] = 0.f;
+    if (a.direct)
+      for (int k = 0; k < a.K; ++k) a.ln_p[(long)own.tok * a.K + k] = 0.f;
   }
   for (int r0 = blockIdx.x * 8; r0 < count; r0 += gridDim.x * 8) {
     const int r = min(r0 + row_l, count - 1);
@@ -156,14 +239,15 @@ __global__ void __launch_bounds__(256) distil_join_kernel(XentArgs a, int n_part
     __syncthreads();
     const int mine = threadIdx.x / 32, r1 = r0 + mine;
     const int listed = min(r1, count - 1), tok = a.own ? __shfl(own.tok, listed) : a.tok[listed];
+    const int lab = a.own ? __shfl(own.lab, listed) : a.lab[listed];
     if (r1 < count) {
-      const float lse = a.labels[tok] < a.V ? lses[mine] : __builtin_nanf("");
-      const float2 stat = a.q_stat[tok];
+      const float lse = lab >= 0 ? lses[mine] : __builtin_nanf("");
+      const float2 stat = a.direct ? stat_of<32>(a, tok, threadIdx.x % 32) : a.q_stat[tok];
       const long row = a.own ? tok : r1;             // among the entries
       float loss = 0.f;
       for (int k = threadIdx.x % 32; k < a.K; k += 32) {
         const Entry e = entry_of(a, tok, k);
-        const float z = e.there && e.id < a.V ? a.z_entry[row * a.K + a.rank[row * a.K + k]] : __builtin_nanf("");
+        const float z = e.there && e.id < a.V ? a.z_entry[row * a.K + (a.direct ? k : a.rank[row * a.K + k])] : __builtin_nanf("");
         const float ln_p = z * a.inv_t - lse, ln_q = ln_q_of(e, stat), q = expf(ln_q);
         a.ln_p[(long)tok * a.K + k] = e.there ? ln_p : 0.f;
         loss += !e.there || q == 0.f ? 0.f : q * (ln_q - ln_p);
@@ -188,7 +272,7 @@ template <typename G> __global__ void __launch_bounds__(256) distil_entries_kern
   for (int base = blockIdx.x * 4; base < count; base += gridDim.x * 4) {
     const int r = min(base + wave, count - 1);
     const long tok = a.tok[r];
-    const float2 stat = a.q_stat[tok];
+    const float2 stat = a.direct ? stat_of<64>(a, tok, lane) : a.q_stat[tok];
     const float d = (a.labels[tok] < a.V ? a.d_loss[tok] * a.inv_t : __builtin_nanf("")) / scale;
     __syncthreads();
     for (int k = lane; k < entries_up(K); k += 64) {
@@ -228,13 +312,29 @@ hipError_t gradient(const XentArgs& a, int is_f32, hipStream_t s) {
 
 }  // namespace
 
+// Whether few tokens' entries are looked at where they stand, without a launch that prepares them, by every wave and every tile: with gradients of 10 x 256
+// against 1024 41.7 us prepared, 36.5 so with one entry a token, 42.7 and 38.9 with 8, 43.1 and 42.9 with 16, 44.2 and 50.7 with 32; the loss of 64 x 1024
+// against 32768 with 8 26.0 and 25.1, with 16 26.2 and 31.0.
+constexpr int DIRECT_ENTRIES = 8;
+static bool direct_of(const XentArgs& a, int is_f32) { return own_of(a.n, is_f32) && a.K <= DIRECT_ENTRIES; }
+// The list of a pass with more tokens than that, and what belongs to each
+template <bool FORWARD> static hipError_t list(const XentArgs& a, hipStream_t s) {
+  if (a.n <= LISTED && a.K <= LISTED_ENTRIES && a.n * a.K <= LISTED_IN_ALL) {
+    distil_list_kernel<<<1, LISTED, 0, s>>>(a, FORWARD);
+    return hipGetLastError();
+  }
+  distil_prepare_kernel<false><<<waves_for(a.n), 256, 0, s>>>(a, FORWARD);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_xent_list(a, s);
+}
+
 hipError_t launch_distil_fwd(XentArgs a, int is_f32, hipStream_t s) {
   xent_fwd_sizes(&a, is_f32);
-  if (a.own) {
+  a.direct = direct_of(a, is_f32);
+  if (a.own && !a.direct) {
     distil_prepare_kernel<true><<<groups_for(a.n), 256, entries_lds(a, 1), s>>>(a, true);
-  } else {
-    distil_prepare_kernel<false><<<waves_for(a.n), 256, 0, s>>>(a, true);
-    const hipError_t e = launch_xent_list(a, s);
+  } else if (!a.own) {
+    const hipError_t e = list<true>(a, s);
     if (e != hipSuccess) return e;
     distil_sort_kernel<<<groups_for(a.n), 256, entries_lds(a, 1), s>>>(a);
   }
@@ -246,9 +346,13 @@ hipError_t launch_distil_fwd(XentArgs a, int is_f32, hipStream_t s) {
 }
 
 hipError_t launch_distil_bwd(XentArgs a, int is_f32, hipStream_t s) {
-  distil_prepare_kernel<false><<<waves_for(a.n), 256, 0, s>>>(a, false);
-  const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_xent_products(a, is_f32, s, gradient);
+  a.direct = direct_of(a, is_f32);
+  if (own_of(a.n, is_f32) && !a.direct) {
+    distil_prepare_kernel<false><<<waves_for(a.n), 256, 0, s>>>(a, false);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return launch_xent_products(a, is_f32, s, list<false>, gradient);
 }
 
 }  // namespace lvx

@@ -235,6 +235,7 @@ struct XentArgs {
   float inv_t, z2;      // 1 / temperature (1 without a teacher), log2 e / temperature
   float temperature;
   int K, blocks;        // entries of a token; pieces of 64 entries of the vocabulary
+  int direct;           // few tokens (own) of few entries, which are looked at where they stand
   const int64_t* ids;   // [n, K]
   const void* teacher;  // [n, K] float32, or (teacher_bf16) bf16
   int teacher_bf16;
@@ -255,7 +256,7 @@ size_t xent_dw_room(long n, int E, long V, int n_cu, int is_f32);
 hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_xent_list(const XentArgs& a, hipStream_t s);
-hipError_t launch_xent_products(XentArgs a, int is_f32, hipStream_t s, hipError_t (*gradient)(const XentArgs&, int, hipStream_t));
+hipError_t launch_xent_products(XentArgs a, int is_f32, hipStream_t s, hipError_t (*list)(const XentArgs&, hipStream_t), hipError_t (*gradient)(const XentArgs&, int, hipStream_t));
 constexpr int DISTIL_MOST_ENTRIES = 1024;
 hipError_t launch_distil_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_distil_bwd(XentArgs a, int is_f32, hipStream_t s);

@@ -265,11 +265,12 @@ hipError_t launch_xent_fwd(XentArgs a, int is_f32, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) { return launch_xent_products(a, is_f32, s, logits<GRAD, LABEL>); }
+hipError_t launch_xent_bwd(XentArgs a, int is_f32, hipStream_t s) { return launch_xent_products(a, is_f32, s, launch_xent_list, logits<GRAD, LABEL>); }
 
-// gradient: leaves that of a piece's logits
-hipError_t launch_xent_products(XentArgs a, int is_f32, hipStream_t s, hipError_t (*gradient)(const XentArgs&, int, hipStream_t)) {
-  a.own = is_f32 ? f32_few(a.n) : a.n <= 64;
+// list: what xent_list_kernel leaves; gradient: leaves that of a piece's logits
+hipError_t launch_xent_products(XentArgs a, int is_f32, hipStream_t s, hipError_t (*list)(const XentArgs&, hipStream_t),
+                                hipError_t (*gradient)(const XentArgs&, int, hipStream_t)) {
+  a.own = own_of(a.n, is_f32);
   a.dw_tiles = (int)dw_tiles(std::min(a.piece, a.V), a.E, is_f32);
   a.tile = dx_edge(a.n, a.E, a.V, a.n_cu, is_f32);
   a.tile_rows = dx_rows(a.n, a.E, a.V, a.n_cu, is_f32);
@@ -278,9 +279,8 @@ hipError_t launch_xent_products(XentArgs a, int is_f32, hipStream_t s, hipError_
     a.tile_rows = 64;
     a.slots = (int)std::max(up(a.E, 128), std::min(MOST_PARTS * up(a.E, 128), 2L * a.n_cu));
   }
-  if (!a.own) xent_list_kernel<<<1, 1024, 0, s>>>(a);
+  hipError_t e = a.own ? hipSuccess : list(a, s);
   a.first = 1;
-  hipError_t e = hipGetLastError();
   for (a.v0 = 0; a.v0 < a.V && e == hipSuccess; a.v0 = a.v1) {
     a.v1 = a.v0 + a.piece < a.V ? a.v0 + a.piece : a.V;
     const long cols = a.v1 - a.v0;

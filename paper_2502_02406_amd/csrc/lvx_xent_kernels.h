@@ -79,13 +79,42 @@ __device__ inline int dx_parts(int tiles, int pairs, int n_cu, int slots) {
 // The same of up to 64 tokens, by every wave for itself (a.own: there is no list launch, whose 5 us a call of few tokens waits for; loss of 16 x
 // 4096 against 32768 56.6 -> 53.1 us, of 2 x 640 against 2560 15.4 -> 12.3, with gradients of 58 x 384 against 5568 47 -> 39): lane i has listed
 // token i (i < count) and what belongs to it.
-struct Own { int count, tok, lab; float2 row; float scale; };
-__device__ __forceinline__ Own own_list(const XentArgs& a) {
+struct Own { int count, tok, lab; float2 row; float scale; long label; };      // (label: of token `lane`)
+// Entry k of a teacher's of token i: whether it is there, and its logit by the temperature
+struct Entry { bool there; long id; float t; };
+__device__ __forceinline__ Entry entry_of(const XentArgs& a, long i, int k) {
+  Entry e;
+  e.id = a.ids[i * a.K + k];
+  e.there = e.id >= 0;
+  const float t = a.teacher_bf16 ? __uint_as_float((unsigned)((const uint16_t*)a.teacher)[i * a.K + k] << 16) : ((const float*)a.teacher)[i * a.K + k];
+  e.t = t / a.temperature;
+  return e;
+}
+// Whether a token with these entries takes part: 0, -1 if not, V if an id is outside
+__device__ __forceinline__ long label_of(bool any, bool far, long V) { return !any ? -1 : far ? V : 0; }
+template <int LOSS = LABEL> __device__ __forceinline__ Own own_list(const XentArgs& a) {
   const int lane = threadIdx.x & 63, n = (int)a.n;
-  const long label = lane < n ? a.labels[lane] : -1;
+  long label = -1;
+  if (LOSS == TEACHER && a.direct) {
+    bool any = false, far = false;
+    for (int k0 = 0; k0 < a.K; k0 += 4) {
+      Entry e[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k] = entry_of(a, min(lane, n - 1), min(k0 + k, a.K - 1));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        any |= e[k].there && !(e[k].t == -__builtin_inff());
+        far |= e[k].there && e[k].id >= a.V;
+      }
+    }
+    if (lane < n) label = label_of(any, far, a.V);
+  } else if (lane < n) {
+    label = a.labels[lane];
+  }
   const float d = a.d_loss && label >= 0 ? a.d_loss[lane] * a.inv_t : 0.f, lse = a.d_loss && label >= 0 ? a.lse[lane] : 0.f;
   const unsigned long long on = __ballot(label >= 0), below = (1ull << lane) - 1;
   Own o;
+  o.label = label;
   o.count = __popcll(on);
   // (the others behind them: every lane is written)
   const int to = 4 * (label >= 0 ? __popcll(on & below) : o.count + __popcll(~on & below));
@@ -100,8 +129,9 @@ __device__ __forceinline__ Own own_list(const XentArgs& a) {
   return o;
 }
 // ... for the launches behind: a wave of one workgroup
-__device__ inline void own_publish(const XentArgs& a, const Own& o) {
+template <int LOSS> __device__ inline void own_publish(const XentArgs& a, const Own& o) {
   const int lane = threadIdx.x & 63;
+  if (LOSS == TEACHER && a.direct && lane < a.n) ((int64_t*)a.labels)[lane] = o.label;
   const int parts = dx_parts((o.count + a.tile_rows - 1) / a.tile_rows * ((a.E + a.tile - 1) / a.tile), (int)(a.piece / BK), a.n_cu, a.slots);
   if (lane < o.count) a.tok[lane] = o.tok;
   if (lane == 0) {
@@ -164,6 +194,35 @@ __device__ __forceinline__ unsigned entries_of(const XentArgs& a, long row, int 
   return *(const unsigned_any2*)(a.starts + row * (a.blocks + 1) + min(col / 64, a.blocks - 1));
 }
 __device__ __forceinline__ int entry_id(const XentArgs& a, long row, unsigned e) { return (e & 0xffffu) < e >> 16 ? a.sorted[row * a.K + (e & 0xffffu)] : -1; }
+// The logit of column c of the wave's (0 .. 32 JB - 1), chosen by its bits: right in the half of the wave that has the column
+template <int JB, class Z> __device__ __forceinline__ float by_bits(int c, Z&& z) {
+  const auto choose = [](int bit, float one, float zero) __attribute__((always_inline)) -> float { return bit ? one : zero; };      // (of values, not of places)
+  float y[JB];
+#pragma unroll
+  for (int j = 0; j < JB; ++j) {
+    float t[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) t[q] = choose(c & 2, choose(c & 1, z(4 * q + 3, j), z(4 * q + 2, j)), choose(c & 1, z(4 * q + 1, j), z(4 * q, j)));
+    y[j] = choose(c & 16, choose(c & 8, t[3], t[2]), choose(c & 8, t[1], t[0]));
+  }
+  return JB == 2 ? choose(c & 32, y[JB - 1], y[0]) : y[0];
+}
+// Of few entries of few tokens (a.direct) all are looked at where they stand: token `row` (`on`: there is one).
+template <int JB, class Z> __device__ __forceinline__ void pick_direct(const XentArgs& a, long row, bool on, int cw, int g, Z&& z) {
+  for (int k0 = 0; k0 < a.K; k0 += 4) {
+    long id[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) id[k] = a.ids[row * a.K + min(k0 + k, a.K - 1)];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const long at = id[k] - cw;
+      const int c = on && k0 + k < a.K && at >= 0 && at < 32 * JB ? (int)at : -1;
+      if (!__any(c >= 0)) continue;
+      const float y = by_bits<JB>(c, z);
+      if (c >= 0 && ((c >> 2) & 1) == g) a.z_entry[row * a.K + k0 + k] = y;
+    }
+  }
+}
 // Leaves the logits of those among the wave's 32 JB columns, of which `cw` is the first; z as above, id: that of the first entry, which is chosen by the bits of
 // its column.  The others, where a row has more in these columns, through `patch`, 2 KB of LDS of the wave's own: 32 rows x 16 columns at a time, where both halves of the
 // wave then look up four entries of a row each (2000 tokens x 256 against 1000, 128 entries: one after the other, by their bits, 40 us, 17 so).
@@ -172,19 +231,10 @@ template <int JB, class Z> __device__ __forceinline__ void pick_entries(const Xe
   int at = (int)(e & 0xffffu);
   const int end = (int)(e >> 16);
   {
-    const auto choose = [](int bit, float one, float zero) __attribute__((always_inline)) -> float { return bit ? one : zero; };      // (of values, not of places)
     const int c = at < end ? id - cw : -1;
     if (__any(c >= 0 && c < 32 * JB)) {
-      float y[JB];
-#pragma unroll
-      for (int j = 0; j < JB; ++j) {
-        float t[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          t[q] = choose(c & 2, choose(c & 1, z(4 * q + 3, j), z(4 * q + 2, j)), choose(c & 1, z(4 * q + 1, j), z(4 * q, j)));
-        y[j] = choose(c & 16, choose(c & 8, t[3], t[2]), choose(c & 8, t[1], t[0]));
-      }
-      if (c >= 0 && c < 32 * JB && ((c >> 2) & 1) == g) a.z_entry[row * a.K + at] = JB == 2 ? choose(c & 32, y[JB - 1], y[0]) : y[0];
+      const float y = by_bits<JB>(c, z);
+      if (c >= 0 && c < 32 * JB && ((c >> 2) & 1) == g) a.z_entry[row * a.K + at] = y;
     }
   }
   const int l31 = threadIdx.x & 31;
@@ -642,8 +692,8 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   Own own;
   if constexpr (OWN) {
-    own = own_list(a);
-    if (MODE == GRAD && blockIdx.x == 0 && threadIdx.x < 64) own_publish(a, own);
+    own = own_list<LOSS>(a);
+    if (MODE == GRAD && blockIdx.x == 0 && threadIdx.x < 64) own_publish<LOSS>(a, own);
   }
   const int M = OWN ? own.count : a.head->count, E = a.E, cols = (int)(a.v1 - a.v0), nk = E / BK;
   const int n_rt = (M + 32 * RB - 1) / (32 * RB), n_ct = (cols + CT - 1) / CT;
@@ -689,8 +739,8 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
     for (int i = 0; i < RB; ++i) {
       const int r = 32 * i + l31;
       row_e[i] = OWN ? __shfl(own.tok, min(r, M - 1)) : min(r0 + r, M - 1);
-      en[i] = entries_of(a, row_e[i], c0 + 32 * wave);
-      if (r0 + r >= M || c0 + 32 * wave >= cols) en[i] = 0u;
+      en[i] = 0u;
+      if (!(OWN && a.direct) && r0 + r < M && c0 + 32 * wave < cols) en[i] = entries_of(a, row_e[i], c0 + 32 * wave);
     }
   }
 #pragma unroll
@@ -737,7 +787,8 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       tile_stats<1>(g, left, log2_unit<LOSS>(a), z, &m2, &s);
       if (g == 0) sums[wave * 32 * RB + r] = make_float2(m2, s);
       if constexpr (LOSS == TEACHER) {
-        pick_entries<1>(a, row_e[i], en[i], id[i], c0 + cw, g, (float*)(smem + 4 * 32 * RB * 8) + wave * PATCH, z);
+        if (OWN && a.direct) pick_direct<1>(a, row_e[i], r < M, c0 + cw, g, z);
+        else pick_entries<1>(a, row_e[i], en[i], id[i], c0 + cw, g, (float*)(smem + 4 * 32 * RB * 8) + wave * PATCH, z);
       } else {
         const int label = OWN ? __shfl(own.lab, r) : r0 + r < M ? a.lab[r0 + r] : -1;
         const int c = r0 + r < M ? label - c0 - cw : -1;
@@ -1106,8 +1157,8 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
 // into registers: a lane has 64 bytes of a row of w and of x.
 template <int MODE, int LOSS> __global__ void __launch_bounds__(256) xent_few_f32_kernel(XentArgs a) {
   __shared__ __attribute__((aligned(16))) float sums[3][4][256];
-  const Own own = own_list(a);
-  if (MODE == GRAD && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64) own_publish(a, own);
+  const Own own = own_list<LOSS>(a);
+  if (MODE == GRAD && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64) own_publish<LOSS>(a, own);
   const int M = own.count, E = a.E, cols = (int)(a.v1 - a.v0);
   const Turns turn = turns_of((cols + 31) / 32);
   if (turn.entry >= turn.end || M == 0) return;
@@ -1174,8 +1225,12 @@ template <int MODE, int LOSS> __global__ void __launch_bounds__(256) xent_few_f3
     if (g == 0 && r < M) a.part[(long)ct * a.Mp + r] = make_float2(m2, s);
     if constexpr (LOSS == TEACHER) {
       const int token = __shfl(own.tok, min(r, M - 1));
-      const unsigned e = r < M ? entries_of(a, token, c0) : 0u;
-      pick_entries<1>(a, token, e, entry_id(a, token, e), c0, g, &sums[0][0][0], z);
+      if (a.direct) {
+        pick_direct<1>(a, token, r < M, c0, g, z);
+      } else {
+        const unsigned e = r < M ? entries_of(a, token, c0) : 0u;
+        pick_entries<1>(a, token, e, entry_id(a, token, e), c0, g, &sums[0][0][0], z);
+      }
     } else {
       const int c = r < M ? label - c0 : -1;
       if (__any(c >= 0 && c < 32)) {
@@ -1288,11 +1343,13 @@ inline int stat_parts_of(const XentArgs& a, int is_f32) {
   if (is_f32) return (int)(f32_few(a.n) ? up(a.V, 32) : 2 * up(a.V, f32_edge(a.n, a.V, a.n_cu)));
   return (int)(few_rows(a.n, a.V, a.E / BK, a.n_cu) > 0 ? up(a.V, 128) : up(a.V, T));
 }
+// So few tokens that every wave lists them for itself
+inline bool own_of(long n, int is_f32) { return is_f32 ? f32_few(n) : n <= 64; }
 // What the launches of a forward pass have in common: the whole vocabulary at once
 inline void xent_fwd_sizes(XentArgs* a, int is_f32) {
   a->tile = a->tile_rows = T;
   a->piece = a->V;
-  a->own = is_f32 ? f32_few(a->n) : a->n <= 64;
+  a->own = own_of(a->n, is_f32);
   a->v0 = 0;
   a->v1 = a->V;
 }

@@ -151,6 +151,26 @@ def test_ids_that_come_more_than_once(dtype, n):
     check(run(*args, 1.0), ref, tol, "twice")
 
 
+@pytest.mark.parametrize("dtype,n,K", [("bf16", 64, 8), ("bf16", 64, 9), ("bf16", 65, 8), ("bf16", 33, 1), ("bf16", 768, 8), ("bf16", 769, 8), ("bf16", 1024, 6), ("bf16", 1025, 2),
+                                       ("f32", 32, 8), ("f32", 33, 8), ("f32", 32, 9), ("f32", 1024, 5)])
+def test_few_entries(dtype, n, K):
+    """Where the ways of few entries begin and end, with ids that come more than once, and with half of the tokens or none taking part."""
+    args = inputs(n, 64, 333, K, dtype, n + K, twice=True)
+    ref, tol, on = reference(*args, 0.5, dtype)
+    got = run(*args, 0.5)
+    check(got, ref, tol, "few")
+    assert all(torch.equal(a, b) for a, b in zip(got, run(*args, 0.5)))
+    x, w, ids, t, d = args
+    t = t.clone()
+    t[: n // 2] = -float("inf")
+    ref, tol, on = reference(x, w, ids, t, d, 0.5, dtype)
+    got = run(x, w, ids, t, d, 0.5)
+    check(got, ref, tol, "behind others")
+    assert not any(v[: n // 2].any() for v in got[:4])
+    t[:] = -float("inf")
+    assert not any(v.any() for v in run(x, w, ids, t, d, 0.5))
+
+
 @pytest.mark.parametrize("dtype,n", [("bf16", 70), ("bf16", 300), ("f32", 30), ("f32", 100)])
 def test_a_whole_teacher(dtype, n):
     """All entries of the vocabulary are known, in any order: the divergence of two whole softmaxes."""
