@@ -433,7 +433,7 @@ lvx_status lvx_embed_bwd(const lvx_embed* p, lvx_dtype dtype, const void* d_y, c
  * Preference loss of S pairs: sequences 0 .. S - 1 are the chosen ones, S .. 2 S - 1 the rejected ones, first has 2 S + 1 entries.  With
  * m = sum over a sequence's labelled tokens of (ref - nll), of the chosen one less that of the rejected one, and h = beta m:
  *     LVX_PREF_LOGISTIC  loss = (1 - smoothing) ln(1 + exp(-h)) + smoothing ln(1 + exp(h))
- *     LVX_PREF_HINGE     loss = max(0, 1 - h)
+ *     LVX_PREF_HINGE     loss = max(0, 1 - h), its gradient 0 at h = 1
  *     LVX_PREF_SQUARE    loss = (m - 1 / (2 beta))^2
  * ref may be NULL (0).  loss, margin: device, [S] float32, overwritten (margin: m; may be NULL). */
 typedef enum { LVX_PREF_LOGISTIC = 0, LVX_PREF_HINGE = 1, LVX_PREF_SQUARE = 2 } lvx_pref_form;
@@ -449,7 +449,8 @@ lvx_status lvx_preference(const lvx_pref* p, const float* nll, const float* ref,
 
 /* Clipped policy loss of S sequences (first has S + 1 entries), with r = exp(old - nll), d = nll - ref and the advantage A of the sequence or token:
  *     l = -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A) + beta (exp(d) - 1 - d),
- * summed over a sequence's labelled tokens or (mean) their mean; 0 of none.  The gradient of a clipped token's first part is 0.
+ * summed over a sequence's labelled tokens or (mean) their mean; 0 of none.  The gradient of a clipped token's first part is 0; a ratio
+ * on the bound is not clipped.
  * ref      NULL where beta is 0.
  * adv      device, float32: [S], or (per_token) [n].
  * loss     device, [S] float32, overwritten.

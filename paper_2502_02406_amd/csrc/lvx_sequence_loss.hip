@@ -152,7 +152,7 @@ __device__ __forceinline__ double pair_loss(const SequenceArgs& a, double margin
   const double h = a.beta * margin;
   if (a.form == LVX_PREF_LOGISTIC) {
     const double e = exp(-fabs(h)), soft = log1p(e), q = a.smoothing;
-    *slope = a.beta * ((h >= 0.0 ? 1.0 : e) / (1.0 + e) - (1.0 - q));
+    *slope = a.beta * (q * ((h >= 0.0 ? 1.0 : e) / (1.0 + e)) - (1.0 - q) * ((h < 0.0 ? 1.0 : e) / (1.0 + e)));      // (s(h) - (1 - q) would lose what is left of a sure pair's)
     return (1.0 - q) * (soft + (h < 0.0 ? -h : 0.0)) + q * (soft + (h > 0.0 ? h : 0.0));
   }
   if (a.form == LVX_PREF_HINGE) {

@@ -161,6 +161,25 @@ def test_policy(n, S, kind, mean, per_token, beta):
     assert all(torch.equal(a, b) for a, b in zip(got, run_policy(s, S, d, **kw))), "not repeatable"
 
 
+@pytest.mark.parametrize("n", [80, 33000])
+def test_gradient_of_sure_pairs(n):
+    """One labelled token a sequence, margins from -80 to 80 without a rounding: the gradient of a pair that is nearly certain is exp(-h), with one rounding
+    to float32 (2^-24) and a few of float64."""
+    S = 40
+    h = torch.linspace(-80, 80, S).round()
+    z = lambda: torch.zeros(n, device="cuda")
+    s = {"nll": z(), "ref": z(), "labels": torch.full((n,), -1, device="cuda"), "first": torch.arange(2 * S + 1, device="cuda") * (n // (2 * S))}
+    at = s["first"][:S]
+    s["labels"][at], s["labels"][s["first"][S:-1]] = 1, 1
+    s["ref"][at] = h.cuda()
+    loss, margin, grad = run_pref(s, S, torch.ones(S, device="cuda"), form="logistic", beta=1.0)
+    want = np.exp(-np.logaddexp(0.0, h.double().numpy()))
+    assert torch.equal(margin.cpu(), h)
+    for rows, sign in ((at, 1.0), (s["first"][S:-1], -1.0)):
+        assert (np.abs(grad[rows].double().cpu().numpy() - sign * want) <= want * (2.0 ** -24 + 2.0 ** -48)).all()
+    assert (np.abs(loss.double().cpu().numpy() - np.logaddexp(0.0, -h.double().numpy())) <= np.logaddexp(0.0, -h.double().numpy()) * (2.0 ** -24 + 2.0 ** -48)).all()
+
+
 @pytest.mark.parametrize("n", [3000, 50000])
 def test_in_place_loss_alone_and_no_reference(n):
     S = 6
