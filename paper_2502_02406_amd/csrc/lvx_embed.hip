@@ -552,7 +552,7 @@ inline int clear_rows_log(long row_bytes, int low) {
   while (l < std::min(low, MOST_ROWS_LOG) && (row_bytes << l) < (16 << 10)) ++l;
   return l;
 }
-template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs& a, long wg, int low, int sub, bool past) {
+template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs& a, int tl, long wg, int low, int sub, bool past) {
   __shared__ unsigned has[1 << (MOST_ROWS_LOG - 5)];
   const int tid = threadIdx.x;
   const long v0 = wg << sub, v1 = min(a.V, v0 + (1L << sub));
@@ -566,10 +566,10 @@ template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs
   __syncthreads();
   const int per = chunks8(a.E), rows = (int)(v1 - v0);
   const float zero[V8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int r = 0; r < rows; ++r) {
+  for (int r = tid >> tl; r < rows; r += 256 >> tl) {      // (a team a row, as in the sums; by whole workgroups 2000 tokens x 64, table 1000000, took 112 us, 37 so; x 256, 131072 34 and 28)
     if ((has[r / 32] >> (r % 32)) & 1u) continue;
     T* const to = (T*)a.d_table + (v0 + r) * a.E;
-    for (int c = tid; c < per; c += 256) {
+    for (int c = tid & ((1 << tl) - 1); c < per; c += 1 << tl) {
       if (past) Piece<T>::template store<true>(to + c * V8, a.E - c * V8, zero);
       else Piece<T>::store(to + c * V8, a.E - c * V8, zero);
     }
@@ -581,7 +581,7 @@ template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs
 template <typename T, bool ADD> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, int tl, unsigned sums_x, int n_eb, long early, int low, int sub, bool past) {
   if constexpr (!ADD) {
     if (blockIdx.x >= sums_x) {
-      clear_rows<T>(a, early + (blockIdx.x - sums_x), low, sub, past);
+      clear_rows<T>(a, tl, early + (blockIdx.x - sums_x), low, sub, past);
       return;
     }
   }
