@@ -199,6 +199,10 @@ template <typename T> __device__ __forceinline__ void clear_table(T* p, long ele
   }
 }
 
+// For the lists that the sums leave, by a workgroup
+__device__ __forceinline__ void lists_empty(const EmbedArgs& a) {
+  if (threadIdx.x <= EMBED_LISTS) a.head->run[threadIdx.x].count = 0;
+}
 // Up to FEW tokens: every id is compared with all others.  (8 ids 9.6 -> 2.8 us, 64 9.8 -> 3.9, 120 9.9 -> 5.1; 250 of them, in the same way, 13.)
 constexpr int FEW = 128;
 __device__ __forceinline__ void sort_few(const EmbedArgs& a, const Sort& sort, int* keys) {
@@ -240,10 +244,8 @@ __device__ __forceinline__ void sort_few(const EmbedArgs& a, const Sort& sort, i
     }
     a.top[d] = lo;
   }
-  if (tid == 0) {
-    a.head->count = m;
-    a.head->n_many = a.head->n_few = 0;
-  }
+  if (tid == 0) a.head->tokens.count = m;
+  lists_empty(a);
 }
 
 // Up to ONE_MOST tokens: all digits in one launch, by one workgroup, or by 2^split of them, each of which takes the ids with its value of the highest bits
@@ -419,10 +421,10 @@ template <typename T, int ROUNDS> __global__ void __launch_bounds__(SORT_WG) emb
   __syncthreads();
   if (ROUNDS == ONE_ROUNDS || fits) sort_own(a, sort, s, mine, m, base);
   else sort_own_in_memory(a, sort, s, mine, m, base);
+  if (mine == groups - 1) lists_empty(a);
   if (tid == 0 && mine == groups - 1) {
     a.top[groups << (sort.of - sort.bits * (sort.passes - 1))] = base + m;
-    a.head->count = base + m;
-    a.head->n_many = a.head->n_few = 0;
+    a.head->tokens.count = base + m;
   }
 }
 
@@ -442,7 +444,7 @@ __global__ void __launch_bounds__(SORT_WG) embed_count_kernel(EmbedArgs a, int b
   const int digits = 1 << bits, tid = threadIdx.x;
   for (int i = tid; i < digits; i += SORT_WG) sort_mem[i] = 0;
   __syncthreads();
-  const long n = p > 0 ? a.head->count : a.n, end = min(n, (blockIdx.x + 1) * run);
+  const long n = p > 0 ? a.head->tokens.count : a.n, end = min(n, (blockIdx.x + 1) * run);
   for (long i = blockIdx.x * run + tid; i < end; i += SORT_WG) {
     const int key = sort_key(a, p, from, i, n);
     if (key >= 0) atomicAdd(&sort_mem[(key >> (p * bits)) & (digits - 1)], 1);
@@ -460,7 +462,7 @@ template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_move_kern
   int* const cnt = sort_mem;
   int* const start = cnt + sort_counts(digits);
   int* const sums = start + digits;
-  const long n = p > 0 ? a.head->count : a.n, begin = blockIdx.x * run, end = min(n, begin + run);
+  const long n = p > 0 ? a.head->tokens.count : a.n, begin = blockIdx.x * run, end = min(n, begin + run);
   // where this run's tokens of every digit go: behind all smaller digits, and behind the runs before.  Several threads add up a digit's counts.
   const int per = SORT_WG / digits, digit = tid & (digits - 1), part = tid / digits;
   int all = 0, before = 0;
@@ -492,10 +494,8 @@ template <typename T> __global__ void __launch_bounds__(SORT_WG) embed_move_kern
       if (tid < digits) a.top[tid] = at;
       if (tid == 0) a.top[digits] = m;
     }
-    if (tid == 0) {
-      if (p == 0) a.head->count = m;                 // (pass 0 does not read it)
-      a.head->n_many = a.head->n_few = 0;
-    }
+    if (tid == 0 && p == 0) a.head->tokens.count = m;       // (pass 0 does not read it)
+    lists_empty(a);
   }
   for (long base = begin; base < end; base += RUN_STEP) {
     int key[RUN_ROUNDS], tok[RUN_ROUNDS], dig[RUN_ROUNDS], rank[RUN_ROUNDS];
@@ -576,6 +576,8 @@ template <typename T> __device__ __forceinline__ void clear_rows(const EmbedArgs
   }
 }
 
+// Chunks whose last id goes on are listed for the join, in EMBED_LISTS lists: additions to one counter take turns (12945 tokens x 256, added to a table of 3723,
+// with one list 12.3 us, 6.0 so).
 // Sums over a chunk of the sorted tokens, by a team (ADD: to what is there); workgroups from `sums_x` on clear rows, the first of them piece `early` of the table
 // (2^sub rows; low: bits of an id below its last digit)
 template <typename T, bool ADD> __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, int tl, unsigned sums_x, int n_eb, long early, int low, int sub, bool past) {
@@ -587,7 +589,7 @@ template <typename T, bool ADD> __global__ void __launch_bounds__(256) embed_sum
   }
   const int E = a.E, lane = threadIdx.x & ((1 << tl) - 1), eb = (int)(blockIdx.x % n_eb), e = ((eb << tl) + lane) * V8, there = E - e;
   const long c = (long)(blockIdx.x / n_eb) * (256 >> tl) + (threadIdx.x >> tl), p0 = c * a.chunk;
-  const int m = a.head->count;
+  const int m = a.head->tokens.count;
   if (p0 >= m || there <= 0) return;
   const int first = (int)p0, end = (int)min((long)m, p0 + a.chunk);
   const int *const key = a.key[0], *const tok = a.tok[0];
@@ -622,8 +624,8 @@ template <typename T, bool ADD> __global__ void __launch_bounds__(256) embed_sum
             Piece<float>::store(a.part + (2 * c + (before ? 0 : 1)) * E + e, there, s);
             if (after && !before && e == 0) {        // (the lists' order changes no result)
               const long far = (c + MANY_PARTS) * a.chunk;
-              if (far < m && key[far] == id[k]) a.long_list[atomicAdd(&a.head->n_many, 1)] = make_int2((int)c, id[k]);
-              else a.long_list[a.list_end - 1 - atomicAdd(&a.head->n_few, 1)] = make_int2((int)c, id[k]);
+              const int to = far < m && key[far] == id[k] ? EMBED_LISTS : (int)(c % EMBED_LISTS);
+              a.long_list[to * a.list_room + atomicAdd(&a.head->run[to].count, 1)] = make_int2((int)c, id[k]);
             }
           }
 #pragma unroll
@@ -676,32 +678,47 @@ __device__ __forceinline__ f32x4 add_parts(const EmbedArgs& a, int c0, int q0, i
   else run(std::false_type{});
   return s;
 }
-template <typename T> __device__ __forceinline__ void put_joined(const EmbedArgs& a, int id, int e, const f32x4& s) {
+// What is there of a row, where it is added to (ahead of the sums), and the row
+template <typename T> __device__ __forceinline__ f32x4 joined_to(const EmbedArgs& a, int id, int e) {
+  f32x4 old = {0.f, 0.f, 0.f, 0.f};
+  if (a.accumulate) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) old[j] = (float)((const T*)a.d_table)[(long)id * a.E + min(e + j, a.E - 1)];
+  }
+  return old;
+}
+template <typename T> __device__ __forceinline__ void put_joined(const EmbedArgs& a, int id, int e, const f32x4& s, const f32x4& old) {
   T* const to = (T*)a.d_table + (long)id * a.E + e;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (e + j < a.E) to[j] = (T)(a.accumulate ? fmaf(s[j], a.scale, (float)to[j]) : s[j] * a.scale);
+    if (e + j < a.E) to[j] = (T)(a.accumulate ? fmaf(s[j], a.scale, old[j]) : s[j] * a.scale);
 }
 // An id of more than MANY_PARTS chunks: 256 features a workgroup, whose waves, and in them groups of 2^cl lanes, where a row has no more, take a run of the
 // chunks each (the first wgs_many workgroups).  The others, most of them: 256 features a wave.  (131072 tokens x 64, two in three the same id: 928 us with four waves and whole rows, 112 so; x 1024 145 and 124)
 constexpr int JOIN_WG = 512, JOIN_WAVES = JOIN_WG / 64;
 template <typename T> __global__ void __launch_bounds__(JOIN_WG) embed_join_kernel(EmbedArgs a, int cl, int wgs_many) {
   __shared__ __attribute__((aligned(16))) float sums[JOIN_WAVES][256];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = a.head->count, blocks = (a.E + 255) / 256;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = a.head->tokens.count, blocks = (a.E + 255) / 256;
   const int units = JOIN_WAVES << (6 - cl), unit = (wave << (6 - cl)) + (lane >> cl), l = lane & ((1 << cl) - 1);
   if ((int)blockIdx.x >= wgs_many) {
-    const long n_few = (long)a.head->n_few * blocks, step = (long)(gridDim.x - wgs_many) * JOIN_WAVES;
-    for (long it = (long)(blockIdx.x - wgs_many) * JOIN_WAVES + wave; it < n_few; it += step) {
-      const int2 run = a.long_list[a.list_end - 1 - it / blocks];
+    const int w = ((int)blockIdx.x - wgs_many) * JOIN_WAVES + wave, step = ((int)gridDim.x - wgs_many) * JOIN_WAVES / EMBED_LISTS, list = w % EMBED_LISTS;
+    const long n_few = (long)a.head->run[list].count * blocks;
+    for (long it = w / EMBED_LISTS; it < n_few; it += step) {
+      const int2 run = a.long_list[list * a.list_room + it / blocks];
       const int e = (int)(it % blocks) * 256 + 4 * lane, last = last_chunk(a, run.x, run.y, m);
-      if (e < a.E) put_joined<T>(a, run.y, e, add_parts(a, run.x, 0, last - run.x + 1, e));
+      if (e < a.E) {
+        const f32x4 old = joined_to<T>(a, run.y, e);
+        put_joined<T>(a, run.y, e, add_parts(a, run.x, 0, last - run.x + 1, e), old);
+      }
     }
     return;
   }
-  const long n_many = (long)a.head->n_many * blocks;
+  const long n_many = (long)a.head->run[EMBED_LISTS].count * blocks;
   for (long it = blockIdx.x; it < n_many; it += wgs_many) {
-    const int2 run = a.long_list[it / blocks];
+    const int2 run = a.long_list[EMBED_LISTS * a.list_room + it / blocks];
     const int e = (int)(it % blocks) * 256 + 4 * l, parts = last_chunk(a, run.x, run.y, m) - run.x + 1;
+    const bool mine = wave == 0 && lane < (1 << cl) && e < a.E;
+    const f32x4 old = mine ? joined_to<T>(a, run.y, e) : f32x4{0.f, 0.f, 0.f, 0.f};
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (e < a.E) s = add_parts(a, run.x, (int)((long)unit * parts / units), (int)((long)(unit + 1) * parts / units), e);
     for (int o = 1 << cl; o < 64; o *= 2)
@@ -710,10 +727,10 @@ template <typename T> __global__ void __launch_bounds__(JOIN_WG) embed_join_kern
     __syncthreads();                                 // (the sums of the id before have been read)
     if (lane < (1 << cl)) *(f32x4*)&sums[wave][4 * l] = s;
     __syncthreads();
-    if (wave == 0 && lane < (1 << cl) && e < a.E) {
+    if (mine) {
       s = *(const f32x4*)&sums[0][4 * l];
       for (int w = 1; w < JOIN_WAVES; ++w) s += *(const f32x4*)&sums[w][4 * l];
-      put_joined<T>(a, run.y, e, s);
+      put_joined<T>(a, run.y, e, s, old);
     }
   }
 }
@@ -782,7 +799,7 @@ template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStre
     int cl = 0;                                      // lanes for four features each of a row, or of 256 features
     while (cl < 6 && (4 << cl) < a.E) ++cl;
     const long blocks = up(a.E, 256), many = n_chunks > MANY_PARTS ? std::min(n_chunks / MANY_PARTS * blocks, (long)a.n_cu) : 0;
-    const long few = std::min(up((n_chunks - 1) * blocks, JOIN_WAVES), 3L * a.n_cu);
+    const long few = up(std::min((n_chunks - 1) * blocks, 3L * a.n_cu * JOIN_WAVES), EMBED_LISTS) * (EMBED_LISTS / JOIN_WAVES);
     embed_join_kernel<T><<<(unsigned)(many + few), JOIN_WG, 0, s>>>(a, cl, (int)many);
   }
   return hipGetLastError();
@@ -798,7 +815,7 @@ int embed_chunk(long n, int E) {
   while (c < 64 && n * chunks8(E) / c > (1L << 18)) c *= 2;
   return c;
 }
-long embed_chunks_room(long n) { return n / LEAST_CHUNK + 1; }
+long embed_list_room(long n) { return n / LEAST_CHUNK / EMBED_LISTS + 1; }
 // Chunks are the shorter the less there is: of n E / 8 = P pieces or fewer, no more than min(P / 4, max(2^18, P / 64)) chunk pieces and a row of them.
 size_t embed_part_room(long n, int E) {
   const long P = n * chunks8(E);
@@ -808,7 +825,7 @@ size_t embed_part_room(long n, int E) {
 hipError_t launch_embed_fwd(const EmbedArgs& a, int is_f32, hipStream_t s) { return is_f32 ? embed_fwd<float>(a, s) : embed_fwd<__bf16>(a, s); }
 hipError_t launch_embed_bwd(EmbedArgs a, int is_f32, hipStream_t s) {
   a.chunk = embed_chunk(a.n, a.E);
-  a.list_end = embed_chunks_room(a.n);
+  a.list_room = embed_list_room(a.n);
   if (a.accumulate) return is_f32 ? embed_bwd<float, true>(a, s) : embed_bwd<__bf16, true>(a, s);
   return is_f32 ? embed_bwd<float, false>(a, s) : embed_bwd<__bf16, false>(a, s);
 }

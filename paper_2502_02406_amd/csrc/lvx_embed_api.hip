@@ -36,7 +36,7 @@ Plan plan_of(int64_t n, int32_t E) {
   for (size_t& l : p.list) { l = at; at += align_up(n * sizeof(int)); }
   p.hist = at; at += (size_t)EMBED_BLOCKS * EMBED_DIGITS * sizeof(int);
   p.top = at; at += align_up((EMBED_TOPS + 1) * sizeof(int));
-  p.long_list = at; at += align_up(embed_chunks_room(n) * sizeof(int2));
+  p.long_list = at; at += align_up((EMBED_LISTS + 1) * embed_list_room(n) * sizeof(int2));
   p.part = at; at += align_up(embed_part_room(n, E));
   p.all = at;
   return p;

@@ -262,10 +262,11 @@ hipError_t launch_distil_fwd(XentArgs a, int is_f32, hipStream_t s);
 hipError_t launch_distil_bwd(XentArgs a, int is_f32, hipStream_t s);
 
 // Rows of an embedding table (lvx_embed.hip)
+constexpr int EMBED_LISTS = 32;
+struct alignas(256) EmbedCount { int count; };        // (apart from each other: what is added to at once)
 struct EmbedHead {
-  int count;            // tokens that have a row of the table
-  int n_many, n_few;    // entries of long_list, from its beginning and from its end on
-  int pad[61];
+  EmbedCount tokens;    // that have a row of the table
+  EmbedCount run[EMBED_LISTS + 1];                    // entries of the lists
 };
 struct EmbedArgs {
   const void* table;    // [V, E] (forward)
@@ -281,14 +282,14 @@ struct EmbedArgs {
   int *key[2], *tok[2]; // [n]: ids and numbers of the tokens, from one pass of the sort to the next; the last one leaves key[0], tok[0]
   int* hist;            // [EMBED_BLOCKS][EMBED_DIGITS]
   int* top;             // [EMBED_TOPS + 1]: where the ids with every value of the last digit (and of what stands above it) start
-  int2* long_list;      // [list_end]: chunks whose last id goes on in the next one, and that id; of ids of many chunks first
-  long list_end;
+  int2* long_list;      // [EMBED_LISTS + 1][list_room]: chunks whose last id goes on in the next one, and that id; those of ids of many chunks in the last list
+  long list_room;
   float* part;          // [chunks][2][E]
   int chunk;            // sorted tokens of a chunk
 };
 constexpr int EMBED_BLOCKS = 256, EMBED_DIGIT_BITS = 10, EMBED_DIGITS = 1 << EMBED_DIGIT_BITS, EMBED_TOPS = 32 * EMBED_DIGITS;
 int embed_chunk(long n, int E);
-long embed_chunks_room(long n);             // the most chunks of n tokens
+long embed_list_room(long n);               // the most chunks of a list, of n tokens
 size_t embed_part_room(long n, int E);      // bytes of `part` for n tokens of E features or fewer
 hipError_t launch_embed_fwd(const EmbedArgs& a, int is_f32, hipStream_t s);
 hipError_t launch_embed_bwd(EmbedArgs a, int is_f32, hipStream_t s);

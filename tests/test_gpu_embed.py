@@ -181,6 +181,26 @@ def test_refused_overlap():
         B.lvx_embed_bwd(t[:8], ids, t, ws)
 
 
+@pytest.mark.parametrize("times,E", [(1, 8), (1, 300), (7, 24), (18, 8), (40, 16)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ids_of_so_many_chunks(dtype, times, E):
+    """Sorted tokens are summed four at a time here: ids of as many tokens as end before, at and behind the edges of 1 to 65 such chunks and of 32 of them, in
+    several orders."""
+    g = torch.Generator().manual_seed(times + E)
+    counts = [4 * k + d for k in (1, 2, 31, 32, 33, 63, 64, 65) for d in (-1, 0, 1)] + [1, 2, 3, 4, 128, 128, 256]
+    counts = torch.tensor(counts)
+    per_id = torch.cat([counts[torch.randperm(len(counts), generator=g)] for _ in range(times)])
+    V = len(per_id)
+    ids = torch.repeat_interleave(torch.arange(V), per_id)
+    ids = ids[torch.randperm(len(ids), generator=g)]
+    table, ids, dy = inputs(len(ids), E, V, dtype, times, ids=ids)
+    old = torch.randn((V, E), generator=g).to(DT[dtype]).cuda()
+    for there in (None, old):
+        y, dt = run(table, ids, dy, 0.5, old=there)
+        check(table, ids, dy, 0.5, y, dt, there)
+        assert torch.equal(dt, run(table, ids, dy, 0.5, old=there)[1])
+
+
 @pytest.mark.parametrize("n,E,V,share", [(131072, 64, 5000, 1.0), (70000, 24, 900, 0.7), (20000, 40, 50, 0.5), (9000, 520, 9000, 0.9), (3000, 8, 7, 0.95)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_an_id_that_most_tokens_have(dtype, n, E, V, share):
