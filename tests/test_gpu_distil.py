@@ -206,6 +206,22 @@ def test_small_workspace_and_parts_left_out(dtype):
     check((loss, lse, ln_p, dx, dw), ref, tol, "a larger problem's workspace")
 
 
+@pytest.mark.parametrize("dtype,n,K", [("bf16", 40, 4), ("bf16", 40, 20), ("f32", 20, 4), ("bf16", 200, 5)])
+def test_few_entries_in_pieces_of_the_vocabulary(dtype, n, K):
+    """The least workspace that the backward pass takes (found by what it refuses, before any launch): the entries are handed to several pieces."""
+    args = inputs(n, 128, 1500, K, dtype, 12, twice=True)
+    ref, tol, _ = reference(*args, 1.5, dtype)
+    low, high = 0, B.lvx_distil_workspace_bytes(n, 128, 1500, K, B.dtype_code(DT[dtype])) // 256
+    while high - low > 1:
+        mid = (low + high) // 2
+        try:
+            run(*args, 1.5, ws_bytes=mid * 256)
+            high = mid
+        except B.LvxError:
+            low = mid
+    check(run(*args, 1.5, ws_bytes=high * 256), ref, tol, f"{high * 256} bytes")
+
+
 @pytest.mark.parametrize("dtype,n", [("bf16", 70), ("bf16", 30), ("f32", 70), ("f32", 20)])
 def test_nothing_to_learn_and_ids_outside(dtype, n):
     x, w, ids, t, d = inputs(n, 64, 300, 4, dtype, 9, ignored=0.0)
