@@ -214,3 +214,29 @@ def test_an_id_that_most_tokens_have(dtype, n, E, V, share):
         old = torch.ones((V, E), dtype=DT[dtype], device="cuda")
         y, dt = run(*args, 0.5, old=old)
         check(*args, 0.5, y, dt, old)
+
+
+def test_offsets_that_pass_32_bits():
+    """A table of more than 2^32 elements and rows of y so far apart that theirs pass 2^32 too: the last rows, ids that few and that many tokens have."""
+    V, E, n = 530000, 8192, 1200
+    far = (1 << 32) // 1000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ids = torch.randint(V - 300, V, (n,), generator=g, device="cuda")
+    ids[::3] = V - 1
+    ids[1::7] = 5
+    table = torch.empty((V, E), dtype=torch.bfloat16, device="cuda")
+    for rows in (table[:10], table[V - 300:]):
+        rows.normal_(generator=g)
+    y = torch.empty((n, far), dtype=torch.bfloat16, device="cuda")
+    B.lvx_embed_fwd(table, ids, y[:, :E], 0.25)
+    assert torch.equal(y[:, :E], table[ids] * 0.25)               # (a power of two)
+    grad = torch.full_like(table, 3.0)
+    ws = torch.empty(B.lvx_embed_workspace_bytes(n, E, V), dtype=torch.uint8, device="cuda")
+    B.lvx_embed_bwd(y[:, :E], ids, grad, ws, 1.0)
+    want = torch.zeros((V, 4), dtype=torch.float64, device="cuda").index_add_(0, ids, y[:, E - 4:E].double())
+    size = torch.zeros((V, 4), dtype=torch.float64, device="cuda").index_add_(0, ids, y[:, E - 4:E].double().abs())
+    tol = (n * U * size) * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs()
+    assert ((grad[:, E - 4:].double() - want).abs() <= tol).all()
+    some = torch.zeros(V, dtype=torch.bool, device="cuda")
+    some[ids] = True
+    assert not any(grad[r:r + 50000][~some[r:r + 50000]].any() for r in range(0, V, 50000))
