@@ -6,7 +6,7 @@
 //
 // What differs from the cross entropy is that a token has K logits to be handed out instead of one.  A launch sorts every listed token's ids
 // and counts those below every multiple of 64, so that a tile's epilogue finds the ones among its columns with one lookup a row, and
-// leaves their logits in their order (few tokens' few entries: direct_of).  The gradient's tiles write exp(z / T - lse) d_loss / T everywhere; at the teacher's entries another launch
+// leaves their logits in their order (few tokens' few entries stay where they are: direct_of).  The gradient's tiles write exp(z / T - lse) d_loss / T everywhere; at the teacher's entries another launch
 // puts exp(ln p) - q in its place, from the ln p of the forward pass, with one rounding like everywhere else: n K values beside the n V.
 // (To bf16, which the matrix cores take: dx and dw of 2048 x 4096 against 32768 with 64 entries are off by 0.0023 of their size, by 0.0017 from their own rounding.)
 #include "lvx_xent_kernels.h"
@@ -14,9 +14,6 @@
 namespace lvx {
 
 namespace {
-
-// stat: of a token's entries, the largest logit by the temperature and the logarithm of the sum of exponentials against it
-__device__ __forceinline__ float ln_q_of(const Entry& e, float2 stat) { return (e.t - stat.x) - stat.y; }
 
 // K entries in LDS, rounded up to four
 constexpr int NO_KEY = 0x7ffffffe;
@@ -273,7 +270,7 @@ template <typename G> __global__ void __launch_bounds__(256) distil_entries_kern
   for (int base = blockIdx.x * 4; base < count; base += gridDim.x * 4) {
     const int r = min(base + wave, count - 1);
     const long tok = a.tok[r];
-    const float2 stat = a.direct ? stat_of<64>(a, tok, lane) : a.q_stat[tok];
+    const float2 stat = a.q_stat[tok];
     const float d = (a.labels[tok] < a.V ? a.d_loss[tok] * a.inv_t : __builtin_nanf("")) / scale;
     __syncthreads();
     for (int k = lane; k < entries_up(K); k += 64) {
@@ -305,7 +302,7 @@ unsigned groups_for(long n) { return (unsigned)std::min(n, 1L << 16); }
 int entries_lds(const XentArgs& a, int tokens) { return tokens * 2 * entries_up(a.K) * (int)sizeof(int); }
 hipError_t gradient(const XentArgs& a, int is_f32, hipStream_t s) {
   const hipError_t e = logits<GRAD, TEACHER>(a, is_f32, s);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.direct) return e;
   if (is_f32) distil_entries_kernel<float><<<waves_for(a.n), 256, entries_lds(a, 4), s>>>(a);
   else distil_entries_kernel<__bf16><<<waves_for(a.n), 256, entries_lds(a, 4), s>>>(a);
   return hipGetLastError();
@@ -313,11 +310,7 @@ hipError_t gradient(const XentArgs& a, int is_f32, hipStream_t s) {
 
 }  // namespace
 
-// Whether few tokens' entries are looked at where they stand, without a launch that prepares them, by every wave and every tile: with gradients of 10 x 256
-// against 1024 41.7 us prepared, 36.5 so with one entry a token, 42.7 and 38.9 with 8, 43.1 and 42.9 with 16, 44.2 and 50.7 with 32; the loss of 64 x 1024
-// against 32768 with 8 26.0 and 25.1, with 16 26.2 and 31.0.
-constexpr int DIRECT_ENTRIES = 8;
-static bool direct_of(const XentArgs& a, int is_f32) { return own_of(a.n, is_f32) && a.K <= DIRECT_ENTRIES; }
+static bool direct_of(const XentArgs& a, int is_f32) { return own_of(a.n, is_f32) && a.K <= DIRECT_ENTRIES && a.K * a.V <= DIRECT_IN_ALL; }
 // The list of a pass with more tokens than that, and what belongs to each
 template <bool FORWARD> static hipError_t list(const XentArgs& a, hipStream_t s) {
   if (a.n <= LISTED && a.K <= LISTED_ENTRIES && a.n * a.K <= LISTED_IN_ALL) {

@@ -90,6 +90,14 @@ __device__ __forceinline__ Entry entry_of(const XentArgs& a, long i, int k) {
   e.t = t / a.temperature;
   return e;
 }
+// stat: of a token's entries, the largest logit by the temperature and the logarithm of the sum of exponentials against it
+__device__ __forceinline__ float ln_q_of(const Entry& e, float2 stat) { return (e.t - stat.x) - stat.y; }
+// Whether few tokens' entries (a.own) are looked at where they stand, by every wave and every tile, without launches that prepare them and, for the gradient,
+// write them: with both passes of 10 x 256 against 1024 prepared 41.7 us, 33.8 so with one entry a token, 42.7 and 36.4 with 8; of 64 x 64 against 32768 with 8 51.1 and
+// 48.8, 65536 with 4 58.7 and 52.2, with 8 59.2 and 59.8, 100000 with one 76.8 and 72.2, with 8 78.7 and 88.0, 300000 with one 165.4 and 165.2; of 32 x 64 float32 against
+// 65536 with 4 92.7 and 86.2, with 8 93.1 and 97.9; the loss alone of 64 x 1024 against 32768 with 8 26.0 and 25.1, with 16 26.2 and 31.0.
+constexpr int DIRECT_ENTRIES = 8;
+constexpr long DIRECT_IN_ALL = 1 << 18;              // entries of a token x the vocabulary's
 // Whether a token with these entries takes part: 0, -1 if not, V if an id is outside
 __device__ __forceinline__ long label_of(bool any, bool far, long V) { return !any ? -1 : far ? V : 0; }
 template <int LOSS = LABEL> __device__ __forceinline__ Own own_list(const XentArgs& a) {
@@ -221,6 +229,33 @@ template <int JB, class Z> __device__ __forceinline__ void pick_direct(const Xen
       const float y = by_bits<JB>(c, z);
       if (c >= 0 && ((c >> 2) & 1) == g) a.z_entry[row * a.K + k0 + k] = y;
     }
+  }
+}
+// ... and of the gradient: takes q off p at the entries of token `row` among 32 columns from `cw` on, where p[v] is that of column 8 (v / 4) + 4 g + v % 4.
+// (In a launch of its own, as in the other cases, both passes of 10 x 256 against 1024 with one entry a token take 36.5 us, 33.8 so.)
+__device__ __forceinline__ void subtract_direct(const XentArgs& a, long row, bool on, long cw, int g, float (&p)[16]) {
+  Entry e[DIRECT_ENTRIES];
+  bool any = false;
+#pragma unroll
+  for (int k = 0; k < DIRECT_ENTRIES; ++k) {
+    e[k] = entry_of(a, row, min(k, a.K - 1));
+    e[k].there &= on && k < a.K;
+    any |= e[k].there && e[k].id >= cw && e[k].id < cw + 32;
+  }
+  if (!__any(any)) return;
+  float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < DIRECT_ENTRIES; ++k) top = e[k].there ? fmaxf(top, e[k].t) : top;
+#pragma unroll
+  for (int k = 0; k < DIRECT_ENTRIES; ++k) sum += e[k].there ? expf(e[k].t - top) : 0.f;
+  const float2 stat = make_float2(top, logf(sum));
+#pragma unroll
+  for (int k = 0; k < DIRECT_ENTRIES; ++k) {
+    const int hot = e[k].there && e[k].id >= cw && e[k].id < cw + 32 ? (int)(e[k].id - cw) - 4 * g : -64;
+    if (!__any(hot >= -4)) continue;
+    const float q = expf(ln_q_of(e[k], stat));
+#pragma unroll
+    for (int v = 0; v < 16; ++v) p[v] -= 8 * (v / 4) + v % 4 == hot ? q : 0.f;
   }
 }
 // Leaves the logits of those among the wave's 32 JB columns, of which `cw` is the first; z as above, id: that of the first entry, which is chosen by the bits of
@@ -825,13 +860,19 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
         if (LOSS == LABEL) c = a.lab[r0 + r] - (int)a.v0 - c0 - cw;
       }
       const int end = d != 0.f ? left - 4 * g : 0, hot = c - 4 * g;
+      float p[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) p[v] = exp2_fast(fmaf(acc[i][v], log2_unit<LOSS>(a), -lse2));
+      if constexpr (OWN && LOSS == TEACHER) {
+        if (a.direct) subtract_direct(a, __shfl(own.tok, min(r, M - 1)), r < M, a.v0 + c0 + cw, g, p);
+      }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float y[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int at = 8 * q + k;
-          y[k] = exp2_fast(fmaf(acc[i][4 * q + k], log2_unit<LOSS>(a), -lse2));
+          y[k] = p[4 * q + k];
           if (LOSS == LABEL) y[k] -= at == hot ? 1.f : 0.f;
           y[k] = at < end ? y[k] * d : 0.f;
         }
@@ -1241,6 +1282,12 @@ template <int MODE, int LOSS> __global__ void __launch_bounds__(256) xent_few_f3
   } else {
     const float lse2 = __shfl(own.row.x, r), d = __shfl(own.row.y, r) / own.scale;
     const int c = LOSS == LABEL ? label - (int)a.v0 : -1;
+    float p[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) p[v] = exp2_fast(fmaf(acc[v], log2_unit<LOSS>(a), -lse2));
+    if constexpr (LOSS == TEACHER) {
+      if (a.direct) subtract_direct(a, __shfl(own.tok, min(r, M - 1)), r < M, a.v0 + c0, g, p);
+    }
     if (r >= M) return;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -1248,8 +1295,8 @@ template <int MODE, int LOSS> __global__ void __launch_bounds__(256) xent_few_f3
       f32x4 y;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float p = exp2_fast(fmaf(acc[4 * q + k], log2_unit<LOSS>(a), -lse2)) - (LOSS == LABEL && at + k == c ? 1.f : 0.f);
-        y[k] = at + k < cols && d != 0.f ? p * d : 0.f;
+        const float of_it = p[4 * q + k] - (LOSS == LABEL && at + k == c ? 1.f : 0.f);
+        y[k] = at + k < cols && d != 0.f ? of_it * d : 0.f;
       }
       *(f32x4*)((float*)a.g + r * a.g_pitch + at) = y;
     }

@@ -206,6 +206,14 @@ def test_small_workspace_and_parts_left_out(dtype):
     check((loss, lse, ln_p, dx, dw), ref, tol, "a larger problem's workspace")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,K", [(32768, 8), (32769, 8), (131072, 2), (131073, 2)])
+def test_few_entries_of_a_long_vocabulary(dtype, V, K):
+    args = inputs(20, 64, V, K, dtype, 3)
+    ref, tol, _ = reference(*args, 1.0, dtype)
+    check(run(*args, 1.0), ref, tol, "long")
+
+
 @pytest.mark.parametrize("dtype,n,K", [("bf16", 40, 4), ("bf16", 40, 20), ("f32", 20, 4), ("bf16", 200, 5)])
 def test_few_entries_in_pieces_of_the_vocabulary(dtype, n, K):
     """The least workspace that the backward pass takes (found by what it refuses, before any launch): the entries are handed to several pieces."""
