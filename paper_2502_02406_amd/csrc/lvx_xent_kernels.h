@@ -231,9 +231,9 @@ template <int JB, class Z> __device__ __forceinline__ void pick_direct(const Xen
     }
   }
 }
-// ... and of the gradient: takes q off p at the entries of token `row` among 32 columns from `cw` on, where p[v] is that of column 8 (v / 4) + 4 g + v % 4.
+// ... and of the gradient: takes q off p at the entries of token `row` among 32 columns from `cw` on (KNOWN: its statistics are), where p[v] is that of column 8 (v / 4) + 4 g + v % 4.
 // (In a launch of its own, as in the other cases, both passes of 10 x 256 against 1024 with one entry a token take 36.5 us, 33.8 so.)
-__device__ __forceinline__ void subtract_direct(const XentArgs& a, long row, bool on, long cw, int g, float (&p)[16]) {
+template <bool KNOWN> __device__ __forceinline__ void subtract_direct(const XentArgs& a, long row, bool on, long cw, int g, float (&p)[16]) {
   Entry e[DIRECT_ENTRIES];
   bool any = false;
 #pragma unroll
@@ -243,12 +243,17 @@ __device__ __forceinline__ void subtract_direct(const XentArgs& a, long row, boo
     any |= e[k].there && e[k].id >= cw && e[k].id < cw + 32;
   }
   if (!__any(any)) return;
-  float top = -__builtin_inff(), sum = 0.f;
+  float2 stat;
+  if constexpr (KNOWN) {
+    stat = a.q_stat[row];
+  } else {
+    float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-  for (int k = 0; k < DIRECT_ENTRIES; ++k) top = e[k].there ? fmaxf(top, e[k].t) : top;
+    for (int k = 0; k < DIRECT_ENTRIES; ++k) top = e[k].there ? fmaxf(top, e[k].t) : top;
 #pragma unroll
-  for (int k = 0; k < DIRECT_ENTRIES; ++k) sum += e[k].there ? expf(e[k].t - top) : 0.f;
-  const float2 stat = make_float2(top, logf(sum));
+    for (int k = 0; k < DIRECT_ENTRIES; ++k) sum += e[k].there ? expf(e[k].t - top) : 0.f;
+    stat = make_float2(top, logf(sum));
+  }
 #pragma unroll
   for (int k = 0; k < DIRECT_ENTRIES; ++k) {
     const int hot = e[k].there && e[k].id >= cw && e[k].id < cw + 32 ? (int)(e[k].id - cw) - 4 * g : -64;
@@ -775,7 +780,7 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       const int r = 32 * i + l31;
       row_e[i] = OWN ? __shfl(own.tok, min(r, M - 1)) : min(r0 + r, M - 1);
       en[i] = 0u;
-      if (!(OWN && a.direct) && r0 + r < M && c0 + 32 * wave < cols) en[i] = entries_of(a, row_e[i], c0 + 32 * wave);
+      if (!a.direct && r0 + r < M && c0 + 32 * wave < cols) en[i] = entries_of(a, row_e[i], c0 + 32 * wave);
     }
   }
 #pragma unroll
@@ -822,7 +827,7 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       tile_stats<1>(g, left, log2_unit<LOSS>(a), z, &m2, &s);
       if (g == 0) sums[wave * 32 * RB + r] = make_float2(m2, s);
       if constexpr (LOSS == TEACHER) {
-        if (OWN && a.direct) pick_direct<1>(a, row_e[i], r < M, c0 + cw, g, z);
+        if (a.direct) pick_direct<1>(a, OWN ? row_e[i] : a.tok[row_e[i]], r0 + r < M, c0 + cw, g, z);
         else pick_entries<1>(a, row_e[i], en[i], id[i], c0 + cw, g, (float*)(smem + 4 * 32 * RB * 8) + wave * PATCH, z);
       } else {
         const int label = OWN ? __shfl(own.lab, r) : r0 + r < M ? a.lab[r0 + r] : -1;
@@ -863,8 +868,8 @@ __global__ void __launch_bounds__(256) xent_few_bf16_kernel(XentArgs a) {
       float p[16];
 #pragma unroll
       for (int v = 0; v < 16; ++v) p[v] = exp2_fast(fmaf(acc[i][v], log2_unit<LOSS>(a), -lse2));
-      if constexpr (OWN && LOSS == TEACHER) {
-        if (a.direct) subtract_direct(a, __shfl(own.tok, min(r, M - 1)), r < M, a.v0 + c0 + cw, g, p);
+      if constexpr (LOSS == TEACHER) {
+        if (a.direct) subtract_direct<!OWN>(a, OWN ? __shfl(own.tok, min(r, M - 1)) : a.tok[min(r0 + r, M - 1)], r0 + r < M, a.v0 + c0 + cw, g, p);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -1146,8 +1151,12 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
       if (g == 0 && r < M) a.part[(2L * ct + wn) * a.Mp + r] = make_float2(m2, s);
       if constexpr (LOSS == TEACHER) {
         const int row = min(r, M - 1);
-        const unsigned e = r < M && left > 0 ? entries_of(a, row, cw) : 0u;
-        pick_entries<NB>(a, row, e, entry_id(a, row, e), cw, g, sa + wave * PATCH, z);
+        if (a.direct) {
+          pick_direct<NB>(a, a.tok[row], r < M, cw, g, z);
+        } else {
+          const unsigned e = r < M && left > 0 ? entries_of(a, row, cw) : 0u;
+          pick_entries<NB>(a, row, e, entry_id(a, row, e), cw, g, sa + wave * PATCH, z);
+        }
       } else {
         const int c = r < M ? a.lab[r] - cw : -1;
         if (__any(c >= 0 && c < FT / 2)) {
@@ -1166,7 +1175,15 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
         }
       }
 #pragma unroll
-      for (int j = 0; j < NB; ++j)
+      for (int j = 0; j < NB; ++j) {
+        float p[MODE == GRAD ? 16 : 1];
+        if constexpr (MODE == GRAD) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) p[v] = exp2_fast(fmaf(acc[j][i][v], log2_unit<LOSS>(a), -lse2));
+          if constexpr (LOSS == TEACHER) {
+            if (a.direct) subtract_direct<true>(a, a.tok[min(r, M - 1)], r < M, a.v0 + cw + 32 * j, g, p);
+          }
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int at = cw + 32 * j + 8 * q + 4 * g;          // four columns from here
@@ -1174,8 +1191,8 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
           if constexpr (MODE == GRAD) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float p = exp2_fast(fmaf(y[k], log2_unit<LOSS>(a), -lse2)) - (LOSS == LABEL && at + k == c ? 1.f : 0.f);
-              y[k] = at + k < cols && d != 0.f ? p * d : 0.f;
+              const float of_it = p[4 * q + k] - (LOSS == LABEL && at + k == c ? 1.f : 0.f);
+              y[k] = at + k < cols && d != 0.f ? of_it * d : 0.f;
             }
             *(f32x4*)(gg + r * a.g_pitch + at) = y;            // (a row of g has room for whole tiles)
           } else if constexpr (SUMS) {
@@ -1191,6 +1208,7 @@ __global__ void __launch_bounds__(256) xent_f32_kernel(XentArgs a) {
                 if (at + k < E) to[k] = y[k];
           }
         }
+      }
     }
   }
 }
@@ -1286,7 +1304,7 @@ template <int MODE, int LOSS> __global__ void __launch_bounds__(256) xent_few_f3
 #pragma unroll
     for (int v = 0; v < 16; ++v) p[v] = exp2_fast(fmaf(acc[v], log2_unit<LOSS>(a), -lse2));
     if constexpr (LOSS == TEACHER) {
-      if (a.direct) subtract_direct(a, __shfl(own.tok, min(r, M - 1)), r < M, a.v0 + c0, g, p);
+      if (a.direct) subtract_direct<false>(a, __shfl(own.tok, min(r, M - 1)), r < M, a.v0 + c0, g, p);
     }
     if (r >= M) return;
 #pragma unroll
