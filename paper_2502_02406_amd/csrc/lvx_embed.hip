@@ -27,8 +27,9 @@ int team_log(int E) {
   return l;
 }
 
-// 16 bytes to memory, PAST the caches where nothing reads them soon and whole lines are written (y and cleared rows of 2048 x 4096 bf16, table 32768: 78 -> 70 us
-// forward and backward, of 65536 x 4096, table 131072: 522 -> 499; rows of 1001 floats 12.4 -> 13.1 us: not these)
+// 16 bytes to memory, PAST the caches where nothing reads them soon: y, and cleared rows that are whole lines (both of 2048 x 4096 bf16, table 32768: 78 -> 70 us
+// forward and backward, of 65536 x 4096, table 131072: 522 -> 499).  Of rows that begin anywhere, y: 65536 x 4090, table 50021, forward 203 -> 143 us, with the backward
+// pass 458 -> 410, 200000 x 333 59 -> 41, 5514 x 1001 floats 9.3 -> 10.0, with the backward pass 74.7 -> 73.8; but clears of them, the last of these: 74 -> 96.
 template <bool PAST> __device__ __forceinline__ void put16(void* p, u32x4 v) {
   if constexpr (PAST) __builtin_nontemporal_store(v, (u32x4_any2*)p);
   else *(u32x4_any2*)p = v;
@@ -105,7 +106,7 @@ template <> struct Piece<float> {
 
 // ---- forward: ROWS rows of a team on their way at once ----
 constexpr int ROWS = 4;
-template <typename T, bool PAST> __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a, int tl) {
+template <typename T> __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a, int tl) {
   const int E = a.E, e = (((int)blockIdx.y << tl) + (threadIdx.x & ((1 << tl) - 1))) * V8, there = E - e;
   if (there <= 0) return;
   const long teams = 256 >> tl;
@@ -125,7 +126,7 @@ template <typename T, bool PAST> __global__ void __launch_bounds__(256) embed_fw
       float v[V8];
 #pragma unroll
       for (int j = 0; j < V8; ++j) v[j] = id[k] < 0 ? 0.f : id[k] < a.V ? x[k][j] * a.scale : __builtin_nanf("");
-      Piece<T>::template store<PAST>((T*)a.y + i * a.y_ss + e, there, v);
+      Piece<T>::template store<true>((T*)a.y + i * a.y_ss + e, there, v);
     }
   }
 }
@@ -767,8 +768,7 @@ constexpr long CLEAR_ONE = 20 << 20, CLEAR_ROUND = 3 << 20, CLEAR_MORE = 1 << 20
 template <typename T> hipError_t embed_fwd(const EmbedArgs& a, hipStream_t s) {
   const int tl = team_log(a.E);
   const dim3 grid((unsigned)std::min(up(a.n, (256 >> tl) * ROWS), 1L << 18), (unsigned)up(a.E, V8 << tl));
-  if (whole_lines(a.y, (long)sizeof(T) * a.E, (long)sizeof(T) * a.y_ss)) embed_fwd_kernel<T, true><<<grid, 256, 0, s>>>(a, tl);
-  else embed_fwd_kernel<T, false><<<grid, 256, 0, s>>>(a, tl);
+  embed_fwd_kernel<T><<<grid, 256, 0, s>>>(a, tl);
   return hipGetLastError();
 }
 
