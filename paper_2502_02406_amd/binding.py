@@ -779,20 +779,31 @@ def lvx_preference(nll, ref, labels, first, loss, margin=None, d_loss=None, d_nl
                                  _at(d_nll), workspace.data_ptr(), workspace.numel() * workspace.element_size(), s), w)
 
 
+def _advantage_a_token(where, adv, n, S, per_token: Optional[bool]) -> bool:
+    """Whether adv holds an advantage a token [n] instead of one a sequence [S]: said by per_token, or (None) by its size, where that says it."""
+    if per_token is None:
+        if n == S > 1 and adv.numel() == n:
+            raise ValueError(f"{where}: {n} tokens and as many sequences: per_token has to say which of them adv belongs to")
+        per_token = adv.numel() != S
+    if not _are_floats(n if per_token else S, adv):
+        raise ValueError(f"{where}: adv has to be float32 [{n if per_token else S}] (an advantage a {'token' if per_token else 'sequence'}), contiguous")
+    return per_token
+
+
 def lvx_policy(nll, old, ref, adv, labels, first, loss, stats=None, d_loss=None, d_nll=None, workspace=None, clip=(0.2, 0.2), beta: float = 0.0,
-               mean: bool = True) -> None:
+               mean: bool = True, per_token: Optional[bool] = None) -> None:
     """loss (float32 [S]) and stats (float32 [S, 3], or None: labelled tokens, share of clipped ones, mean divergence) are overwritten with the
     clipped policy losses of S sequences (first: int64 [S + 1]), d_nll (float32 [n]) with the gradient of sum(loss * d_loss).  adv: an advantage a
-    sequence [S] or (any other number of elements) a token [n].  clip: a ratio's room below and above 1; beta: weight of the divergence from ref
-    (which may be None without it); mean: over a sequence's labelled tokens, otherwise their sum."""
+    sequence [S] or (per_token) a token [n]; per_token = None: by its size, refused where the two are alike.  clip: a ratio's room below and above 1;
+    beta: weight of the divergence from ref (which may be None without it); mean: over a sequence's labelled tokens, otherwise their sum."""
     w = "lvx_policy"
     if workspace is None:
         raise ValueError(f"{w}: no workspace")
     s = _on_device(w, nll, old, ref, adv, labels, first, loss, stats, d_loss, d_nll, workspace)
     n, S = _sequences(w, (nll, old, ref), (loss,), labels, first, d_loss, d_nll, workspace, False)
-    per_token = adv.numel() != S
-    if not _are_floats(n if per_token else S, adv) or not _are_floats(3 * S, stats):
-        raise ValueError(f"{w}: adv has to be float32 [{S}] or [{n}], stats [{S}, 3], contiguous")
+    per_token = _advantage_a_token(w, adv, n, S, per_token)
+    if not _are_floats(3 * S, stats):
+        raise ValueError(f"{w}: stats has to be float32 [{S}, 3], contiguous")
     if ref is None and beta != 0.0:
         raise ValueError(f"{w}: a divergence needs ref")
     p = _struct(lvx_clip, n, S, 1 if mean else 0, 1 if per_token else 0, clip[0], clip[1], beta)

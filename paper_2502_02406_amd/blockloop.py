@@ -484,9 +484,11 @@ class SequenceLoss:
         B.lvx_preference(nll, ref, labels, first, self.loss, self.margin, self.mean if d_loss is None else d_loss, self.d_nll, self.ws, form, beta, smoothing)
         return self.loss, self.margin, self.d_nll
 
-    def policy(self, nll, old, ref, adv, labels, first, d_loss=None, clip=(0.2, 0.2), beta: float = 0.0, mean: bool = True):
+    def policy(self, nll, old, ref, adv, labels, first, d_loss=None, clip=(0.2, 0.2), beta: float = 0.0, mean: bool = True,
+               per_token: Optional[bool] = None):
         """(loss [S], stats [S, 3], d_nll [n]) of S sequences: old: the tokens' nll when they were sampled, ref: under the reference (None without
-        beta), adv [S] or [n]; stats: labelled tokens, share of clipped ones, mean divergence."""
+        beta), adv [S] or (per_token) [n]; per_token = None: by adv's size, refused where n = S; stats: labelled tokens, share of clipped ones, mean divergence."""
         self.d_nll.zero_()
-        B.lvx_policy(nll, old, ref, adv, labels, first, self.loss, self.stats, self.mean if d_loss is None else d_loss, self.d_nll, self.ws, clip, beta, mean)
+        B.lvx_policy(nll, old, ref, adv, labels, first, self.loss, self.stats, self.mean if d_loss is None else d_loss, self.d_nll, self.ws, clip, beta, mean,
+                     per_token)
         return self.loss, self.stats, self.d_nll

@@ -1,0 +1,46 @@
+"""Losses of sequences where two readings of a call, infinities or roundings meet: against the definitions in float64."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_02406_amd import binding as B
+from test_gpu_sequence_loss import D, U, compare, host, inputs, policy_reference, run_policy, run_pref
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+@pytest.mark.parametrize("n,first", [(3, [0, 2, 2, 3]), (3, [0, 0, 1, 3]), (5000, None), (40000, None)])
+@pytest.mark.parametrize("per_token", [True, False])
+@pytest.mark.parametrize("mean", [True, False])
+def test_as_many_sequences_as_tokens(n, first, per_token, mean):
+    """An advantage a token and one a sequence are as many: which of them they are is said."""
+    s = inputs(n, n, 11, "any", masked=0.0, adv=n)
+    for name in ("nll", "ref", "old", "adv"):
+        s[name].nan_to_num_(0.5)
+    if first is not None:
+        s["first"] = torch.tensor(first, device="cuda")
+        s["labels"].fill_(3)
+    d = torch.randn(n, generator=torch.Generator().manual_seed(n)).cuda()
+    h, hd = host(s), d.double().cpu().numpy()
+    if per_token:
+        h["adv"] = np.append(h["adv"], 0.0)          # (one more, by which policy_reference knows them)
+    want, tol = policy_reference(h, n, n, hd, 0.2, 0.2, 0.1, mean)
+    compare(run_policy(s, n, d, beta=0.1, mean=mean, per_token=per_token), want, tol, "as many")
+    with pytest.raises(ValueError):
+        run_policy(s, n, d, beta=0.1, mean=mean)
+
+
+def test_advantages_through_the_sequence_loss():
+    from paper_2502_02406_amd.blockloop import SequenceLoss
+    s = inputs(3, 3, 5, "even", masked=0.0)
+    s.update(first=torch.tensor([0, 2, 2, 3], device="cuda"), labels=torch.ones(3, dtype=torch.int64, device="cuda"), adv=torch.tensor([1.0, -2.0, 3.0], device="cuda"))
+    for name in ("nll", "ref", "old"):
+        s[name] = torch.ones(3, device="cuda")       # (ratios of 1: a token's loss is its advantage with the other sign)
+    seq = SequenceLoss(3, 3)
+    call = lambda **kw: seq.policy(s["nll"], s["old"], None, s["adv"], s["labels"], s["first"], mean=False, **kw)[0].tolist()
+    assert call(per_token=True) == [1.0, 0.0, -3.0] and call(per_token=False) == [-2.0, 0.0, -3.0]
+    with pytest.raises(ValueError):
+        call()
