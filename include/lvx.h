@@ -432,7 +432,7 @@ lvx_status lvx_embed_bwd(const lvx_embed* p, lvx_dtype dtype, const void* d_y, c
  *
  * Preference loss of S pairs: sequences 0 .. S - 1 are the chosen ones, S .. 2 S - 1 the rejected ones, first has 2 S + 1 entries.  With
  * m = sum over a sequence's labelled tokens of (ref - nll), of the chosen one less that of the rejected one, and h = beta m:
- *     LVX_PREF_LOGISTIC  loss = (1 - smoothing) ln(1 + exp(-h)) + smoothing ln(1 + exp(h))
+ *     LVX_PREF_LOGISTIC  loss = (1 - smoothing) ln(1 + exp(-h)) + smoothing ln(1 + exp(h)); a part of weight 0 is 0, for an infinite h too
  *     LVX_PREF_HINGE     loss = max(0, 1 - h), its gradient 0 at h = 1
  *     LVX_PREF_SQUARE    loss = (m - 1 / (2 beta))^2
  * ref may be NULL (0).  loss, margin: device, [S] float32, overwritten (margin: m; may be NULL). */

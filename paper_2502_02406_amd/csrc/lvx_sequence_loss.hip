@@ -153,7 +153,9 @@ __device__ __forceinline__ double pair_loss(const SequenceArgs& a, double margin
   if (a.form == LVX_PREF_LOGISTIC) {
     const double e = exp(-fabs(h)), soft = log1p(e), q = a.smoothing;
     *slope = a.beta * (q * ((h >= 0.0 ? 1.0 : e) / (1.0 + e)) - (1.0 - q) * ((h < 0.0 ? 1.0 : e) / (1.0 + e)));      // (s(h) - (1 - q) would lose what is left of a sure pair's)
-    return (1.0 - q) * (soft + (h < 0.0 ? -h : 0.0)) + q * (soft + (h > 0.0 ? h : 0.0));
+    // (a part of no weight is left out: of an infinite margin it would be 0 times infinity)
+    const double won = soft + (h < 0.0 ? -h : 0.0), lost = soft + (h > 0.0 ? h : 0.0);
+    return (q < 1.0 ? (1.0 - q) * won : 0.0) + (q > 0.0 ? q * lost : 0.0);
   }
   if (a.form == LVX_PREF_HINGE) {
     *slope = h >= 1.0 ? 0.0 : h < 1.0 ? -a.beta : h;             // (a NaN stays one)

@@ -44,3 +44,31 @@ def test_advantages_through_the_sequence_loss():
     assert call(per_token=True) == [1.0, 0.0, -3.0] and call(per_token=False) == [-2.0, 0.0, -3.0]
     with pytest.raises(ValueError):
         call()
+
+
+def pairs_of_one(n, S, nll):
+    """S pairs of one labelled token a sequence, among n tokens: (inputs, the chosen ones' places, the rejected ones')."""
+    z = lambda: torch.zeros(n, device="cuda")
+    s = {"nll": z(), "ref": z(), "labels": torch.full((n,), -1, device="cuda"), "first": torch.arange(2 * S + 1, device="cuda") * (n // (2 * S))}
+    c, r = s["first"][:S], s["first"][S:-1]
+    s["labels"][c] = s["labels"][r] = 1
+    s["nll"][c], s["nll"][r] = nll[0].cuda(), nll[1].cuda()
+    return s, c, r
+
+
+@pytest.mark.parametrize("n", [80, 40000])
+@pytest.mark.parametrize("form,smooth", [("logistic", 0.0), ("logistic", 0.25), ("logistic", 1.0), ("hinge", 0.0)])
+def test_an_answer_without_likelihood(n, form, smooth):
+    """A margin of +infinity (the rejected one's nll is), or -infinity: a part of the loss that counts for nothing adds nothing, whatever it would be, and the slope is
+    that of the loss far out.  All values are exact in float32."""
+    beta = 0.5
+    s, c, r = pairs_of_one(n, 3, torch.tensor([[1.0, INF, 2.0], [INF, 1.0, 2.0]]))
+    loss, margin, grad = run_pref(s, 3, torch.tensor([1.0, 1.0, 0.0], device="cuda"), form=form, beta=beta, smoothing=smooth)
+    assert margin.tolist() == [INF, -INF, 0.0]
+    if form == "hinge":
+        want, slope = [0.0, INF], [0.0, -beta]
+    else:
+        want = [INF if smooth > 0 else 0.0, INF if smooth < 1 else 0.0]
+        slope = [beta * smooth, -beta * (1 - smooth)]
+    assert loss.tolist()[:2] == want
+    assert grad[c].tolist()[:2] == [-x for x in slope] and grad[r].tolist()[:2] == slope
