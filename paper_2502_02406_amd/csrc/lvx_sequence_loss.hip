@@ -67,13 +67,17 @@ __device__ __forceinline__ double exp_of(double x) {
   for (int i = 0; i < 11; ++i) p = fma(p, r, c[i]);
   return ldexp(p, (int)k);
 }
-// exp(x) - 1 - x, to the last digits for small x too: x^2 times a series up to 1/2 (the last term left out is 2e-17 of the sum)
-__device__ __forceinline__ double exp_less_line(double x) {
+// exp(x) - 1 - x, to the last digits for small x too: x^2 times a series up to 1/2 (the last term left out is 2e-17 of the sum).  *less_one: exp(x) - 1, which far out
+// is more than the sum of that and x says: -1 for -infinity.
+__device__ __forceinline__ double exp_less_line(double x, double* less_one) {
   double p = 1.0 / 6227020800.0;
   const double c[11] = {1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5};
 #pragma unroll
   for (int i = 0; i < 11; ++i) p = fma(p, x, c[i]);
-  return fabs(x) <= 0.5 ? p * x * x : exp_of(x) - 1.0 - x;
+  const double near = p * x * x, far = exp_of(x) - 1.0;
+  const bool small = fabs(x) <= 0.5;
+  *less_one = small ? near + x : far;
+  return small ? near : far - x;
 }
 
 // ---- tokens: U of a thread on their way at once, `wg` apart (behind the last one that one again) ----
@@ -115,9 +119,11 @@ __device__ __forceinline__ double token_policy(const SequenceArgs& a, double nll
   const double high = a.high, low = a.low;
   double loss = over ? -(A > 0.0 ? high : low) * A : -ratio * A, slope = over ? 0.0 : ratio * A;
   if (a.beta != 0.0) {
-    const double d = nll - ref, more = exp_less_line(d);
+    const double d = nll - ref;
+    double less_one;
+    const double more = exp_less_line(d, &less_one);
     loss += a.beta * more;
-    slope += a.beta * (more + d);
+    slope += a.beta * less_one;
     p->kl += more;
   }
   p->loss += loss;

@@ -72,3 +72,18 @@ def test_an_answer_without_likelihood(n, form, smooth):
         slope = [beta * smooth, -beta * (1 - smooth)]
     assert loss.tolist()[:2] == want
     assert grad[c].tolist()[:2] == [-x for x in slope] and grad[r].tolist()[:2] == slope
+
+
+@pytest.mark.parametrize("n", [40, 40000])
+@pytest.mark.parametrize("mean", [True, False])
+def test_a_token_that_the_reference_rules_out(n, mean):
+    """ref = +infinity: the divergence is infinite, its slope exp(-infinity) - 1 = -1, and no other token's gradient is touched.  Also far out, where d is finite."""
+    beta, S = 0.25, 2
+    z = lambda x: torch.full((n,), x, device="cuda")
+    s = {"nll": z(1.0), "old": z(1.0), "ref": z(1.0), "labels": z(1.0).long(), "adv": torch.zeros(S, device="cuda"), "first": torch.tensor([0, 8, 16], device="cuda")}
+    s["ref"][3], s["ref"][11] = INF, 1e30
+    loss, stats, grad = run_policy(s, S, torch.full((S,), 8.0 if mean else 1.0, device="cuda"), beta=beta, mean=mean)
+    want = torch.zeros(16)
+    want[3] = want[11] = -beta
+    assert loss[0].item() == INF and stats[0, 2].item() == INF and loss[1].item() == pytest.approx(0.25e30 / (8 if mean else 1), rel=2 * U)
+    assert torch.equal(grad[:16].cpu(), want) and (grad[16:] == 7.0).all()
