@@ -144,13 +144,13 @@ __device__ __forceinline__ void do_policy(const SequenceArgs& a, Batch& b, long 
       if (a.d_nll) a.d_nll[t + k * wg] = b.label[k] >= 0 ? (float)(slope * (double)d) : 0.f;
     }
 }
-__device__ __forceinline__ void scale_policy(const SequenceArgs& a, long t, long end, long wg, float by) {
+__device__ __forceinline__ void scale_policy(const SequenceArgs& a, long t, long end, long wg, double by) {
   float x[U];
 #pragma unroll
   for (int k = 0; k < U; ++k) x[k] = a.d_nll[min(t + k * wg, end - 1)];
 #pragma unroll
   for (int k = 0; k < U; ++k)
-    if (t + k * wg < end) a.d_nll[t + k * wg] = x[k] * by;
+    if (t + k * wg < end) a.d_nll[t + k * wg] = (float)((double)x[k] * by);
 }
 
 // ---- a pair ----
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(1024) policy_one_kernel(SequenceArgs a) {
     p = wg_sum(p, at);
     if (threadIdx.x == 0) put_stats(a, i, p);
     if (!a.d_nll || !a.mean || p.count == 0) continue;
-    for (long t = c.begin + threadIdx.x; t < c.end; t += U * wg) scale_policy(a, t, c.end, wg, (float)(1.0 / p.count));      // (what this thread has written)
+    for (long t = c.begin + threadIdx.x; t < c.end; t += U * wg) scale_policy(a, t, c.end, wg, 1.0 / p.count);      // (what this thread has written)
   }
 }
 
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(256) policy_finish_kernel(SequenceArgs a) {
   const PolicyPart p = wg_sum(share_of<PolicyPart>(a, span_of(a, j.seq), j.seq), at);
   if (!is_block(a) && threadIdx.x == 0) put_stats(a, j.seq, p);
   if (!a.d_nll || !a.mean || p.count == 0 || j.begin == j.end) return;
-  scale_policy(a, j.begin + threadIdx.x, j.end, 256, (float)(1.0 / p.count));
+  scale_policy(a, j.begin + threadIdx.x, j.end, 256, 1.0 / p.count);
 }
 
 constexpr long ONE_TOKENS = 32768;

@@ -87,3 +87,22 @@ def test_a_token_that_the_reference_rules_out(n, mean):
     want[3] = want[11] = -beta
     assert loss[0].item() == INF and stats[0, 2].item() == INF and loss[1].item() == pytest.approx(0.25e30 / (8 if mean else 1), rel=2 * U)
     assert torch.equal(grad[:16].cpu(), want) and (grad[16:] == 7.0).all()
+
+
+@pytest.mark.parametrize("count", [7, 120, 1000])
+@pytest.mark.parametrize("S", [25, 300])
+def test_a_means_gradient_is_rounded_twice(S, count):
+    """Once as the token's and once by the number of tokens, 2^-24 each; the rest is float64, as in policy_reference.  (300 sequences of 120 tokens and more: two launches.)"""
+    n = S * count
+    print(f"[mean] {S} sequences of {count} tokens", flush=True)
+    s = inputs(n, S, count, "even", masked=0.0)
+    for name in ("nll", "ref", "old"):
+        s[name].nan_to_num_(0.5)
+    s["labels"].fill_(3)
+    d = torch.randn(S, generator=torch.Generator().manual_seed(S)).cuda()
+    got = run_policy(s, S, d, beta=0.2)
+    h = host(s)
+    want, (tl, ts, _) = policy_reference(h, n, S, d.double().cpu().numpy(), 0.2, 0.2, 0.2, True)
+    size = np.exp(h["old"] - h["nll"]) * np.abs(np.repeat(h["adv"], count)) + 0.2 * np.exp(np.abs(h["nll"] - h["ref"]))
+    of_it = np.repeat(np.abs(d.double().cpu().numpy()), count) / count
+    compare(got, want, (tl, ts, (2 * U * np.abs(want[2]) + D * size * of_it + 2.0 ** -148) / 1.01), "mean")      # (compare allows a hundredth more)
