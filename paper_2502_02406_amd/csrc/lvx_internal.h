@@ -306,11 +306,12 @@ struct SequenceArgs {
   double beta, smoothing;               // preferences; beta: also the weight of the divergence
   double low, high, ln_low, ln_high;    // a ratio's bounds, and their logarithms
   void *head, *block;   // workspace: sums of every sequence's first piece, and of every block of tokens that goes on in one
+  int totals;           // whether a launch has made whole sequences' sums of head
 };
 constexpr int SEQUENCE_BLOCK = 1024;    // tokens of a block
 size_t sequence_part_bytes();           // of one of these sums
-hipError_t launch_preference(const SequenceArgs& a, hipStream_t s);
-hipError_t launch_policy(const SequenceArgs& a, hipStream_t s);
+hipError_t launch_preference(SequenceArgs a, hipStream_t s);
+hipError_t launch_policy(SequenceArgs a, hipStream_t s);
 
 // Whether the `len_b` bytes at b meet one of n rows of `len_a` bytes, `pitch` apart, at a: row k does where `behind` < k pitch < `before`
 inline bool rows_meet(int64_t a, int64_t n, int64_t pitch, int64_t len_a, int64_t b, int64_t len_b) {

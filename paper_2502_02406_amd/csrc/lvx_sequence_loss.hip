@@ -11,7 +11,8 @@
 // A token is some 20 bytes and, in 64 bits (sums over long sequences of which differences are taken, values next to a bound; the float64 units are as fast
 // as the float32 ones here), some hundred instructions: bound by memory, and by launches where there are few.  Few tokens (ONE_TOKENS): a workgroup a pair or
 // sequence, in one launch.  More: cut at the multiples of SEQUENCE_BLOCK, a workgroup a piece; the first launch leaves the pieces' sums, the
-// second adds up those of its sequence, in order, and does what hangs on them.  No atomics: results repeat bit for bit.
+// second adds up those of its sequence, in order, and does what hangs on them; of very many tokens a launch between the two makes the
+// sequences' sums.  No atomics: results repeat bit for bit.
 #include "lvx_internal.h"
 
 #include <algorithm>
@@ -270,8 +271,20 @@ __device__ __forceinline__ Job job_of(const SequenceArgs& a, int* lds) {
 template <class P> __device__ __forceinline__ P share_of(const SequenceArgs& a, const Span& s, long seq) {
   P p{};
   if (threadIdx.x == 0) p.add(((const P*)a.head)[seq]);
-  for (long j = s.begin / SEQUENCE_BLOCK + 1 + threadIdx.x; j * SEQUENCE_BLOCK < s.end; j += 256) p.add(((const P*)a.block)[j]);
+  if (a.totals) return p;
+  for (long j = s.begin / SEQUENCE_BLOCK + 1 + threadIdx.x; j * SEQUENCE_BLOCK < s.end; j += blockDim.x) p.add(((const P*)a.block)[j]);
   return p;
+}
+// Whole sequences' sums in place of their first pieces' (`total`): otherwise every piece's workgroup adds up all pieces of its sequence again, which goes with the
+// square of its length
+template <class P> __global__ void __launch_bounds__(1024) sequence_total_kernel(SequenceArgs a) {
+  __shared__ P at[16];
+  for (long i = blockIdx.x; i < a.count; i += gridDim.x) {
+    const Span s = span_of(a, i);
+    if ((s.begin / SEQUENCE_BLOCK + 1) * SEQUENCE_BLOCK >= s.end) continue;      // (uniform)
+    const P p = wg_sum(share_of<P>(a, s, i), at);
+    if (threadIdx.x == 0) ((P*)a.head)[i] = p;
+  }
 }
 template <class P> __device__ __forceinline__ void leave(const SequenceArgs& a, const P& p) {
   if (threadIdx.x != 0) return;
@@ -342,15 +355,25 @@ __global__ void __launch_bounds__(256) policy_finish_kernel(SequenceArgs a) {
   scale_policy(a, j.begin + threadIdx.x, j.end, 256, 1.0 / p.count);
 }
 
-constexpr long ONE_TOKENS = 32768;
+constexpr long ONE_TOKENS = 32768, LONG_TOKENS = 1L << 24;
 // Threads for a sequence (or pair) of `per` tokens on average
 unsigned threads_for(long per) { return per >= 2048 ? 1024 : per >= 64 ? 256 : 64; }
+// The launch between those of more tokens, where sequences may be long; a piece or more a sequence on average, or so many tokens that one long sequence among
+// short ones would cost more than the launch.  us without and with it, preferences / policies, of 2^24 tokens: two sequences 193 / 220 and 87 / 123, 4096 116 / 146 and
+// 113 / 155, 4096 of which one has half of the tokens 136 / 188 and 115 / 147, 65536 of these (then it is left out) 354 / 396 and 364 / 460; of 2^26: two 2118 / 2345 and
+// 337 / 447, 65536 644 / 668 and 658 / 689, one of them with half 1156 / 1680 and 742 / 869; of 2^27: two 7760 / 8660 and 650 / 870.  (2^22: two 39 / 48 and 34 / 47, 256 36 / 44 and 37 / 47.)
+template <class P> void total(SequenceArgs* a, hipStream_t s) {
+  if (a->n < LONG_TOKENS || (a->n < 4 * LONG_TOKENS && a->n / a->count < SEQUENCE_BLOCK)) return;
+  const unsigned wg = a->n / a->count >= 256 * SEQUENCE_BLOCK ? 1024 : 256;
+  sequence_total_kernel<P><<<(unsigned)std::min(a->count, 1L << 16), wg, 0, s>>>(*a);
+  a->totals = 1;
+}
 
 }  // namespace
 
 size_t sequence_part_bytes() { return sizeof(PolicyPart); }
 
-hipError_t launch_preference(const SequenceArgs& a, hipStream_t s) {
+hipError_t launch_preference(SequenceArgs a, hipStream_t s) {
   const long pairs = a.count / 2;
   if (a.n <= ONE_TOKENS) {
     preference_one_kernel<<<(unsigned)std::min(pairs, 1L << 20), threads_for(a.n / pairs), 0, s>>>(a);
@@ -358,17 +381,19 @@ hipError_t launch_preference(const SequenceArgs& a, hipStream_t s) {
   }
   const unsigned all = (unsigned)(a.count + (a.n + SEQUENCE_BLOCK - 1) / SEQUENCE_BLOCK);
   preference_sum_kernel<<<all, 256, 0, s>>>(a);
+  total<PrefPart>(&a, s);
   preference_grad_kernel<<<a.d_nll ? all : (unsigned)pairs, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_policy(const SequenceArgs& a, hipStream_t s) {
+hipError_t launch_policy(SequenceArgs a, hipStream_t s) {
   if (a.n <= ONE_TOKENS) {
     policy_one_kernel<<<(unsigned)std::min(a.count, 1L << 20), threads_for(a.n / a.count), 0, s>>>(a);
     return hipGetLastError();
   }
   const unsigned all = (unsigned)(a.count + (a.n + SEQUENCE_BLOCK - 1) / SEQUENCE_BLOCK);
   policy_sum_kernel<<<all, 256, 0, s>>>(a);
+  total<PolicyPart>(&a, s);
   policy_finish_kernel<<<a.d_nll && a.mean ? all : (unsigned)a.count, 256, 0, s>>>(a);
   return hipGetLastError();
 }

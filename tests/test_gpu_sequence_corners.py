@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2502_02406_amd import binding as B
-from test_gpu_sequence_loss import D, U, compare, host, inputs, policy_reference, run_policy, run_pref
+from test_gpu_sequence_loss import D, U, compare, host, inputs, policy_reference, pref_reference, run_policy, run_pref
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -106,3 +106,54 @@ def test_a_means_gradient_is_rounded_twice(S, count):
     size = np.exp(h["old"] - h["nll"]) * np.abs(np.repeat(h["adv"], count)) + 0.2 * np.exp(np.abs(h["nll"] - h["ref"]))
     of_it = np.repeat(np.abs(d.double().cpu().numpy()), count) / count
     compare(got, want, (tl, ts, (2 * U * np.abs(want[2]) + D * size * of_it + 2.0 ** -148) / 1.01), "mean")      # (compare allows a hundredth more)
+
+
+def many_tokens(n):
+    g = torch.Generator(device="cuda").manual_seed(n)
+    s = {"nll": torch.rand(n, generator=g, device="cuda"), "labels": torch.randint(-2, 9, (n,), generator=g, device="cuda")}
+    s["ref"] = s["nll"] + 0.01 * torch.randn(n, generator=g, device="cuda")
+    s["old"] = s["nll"] + 0.2 * torch.randn(n, generator=g, device="cuda")
+    return s
+
+
+@pytest.mark.parametrize("op", ["preference", "policy"])
+def test_time_goes_with_the_tokens_not_with_their_square(op):
+    """2^27 tokens in two sequences, and in 16384 of them: the same bytes and arithmetic, so no more than four times the time."""
+    n, times = 1 << 27, {}
+    s = many_tokens(n)
+    d_nll = torch.empty(n, device="cuda")
+    for count in (2, 16384):
+        first = torch.arange(count + 1, device="cuda") * (n // count)
+        S = count // 2 if op == "preference" else count
+        loss, one = torch.empty(S, device="cuda"), torch.ones(S, device="cuda")
+        ws = torch.empty(max(B.lvx_preference_workspace_bytes(n, S), B.lvx_policy_workspace_bytes(n, S)), dtype=torch.uint8, device="cuda")
+        took = []
+        for _ in range(4):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            if op == "preference":
+                B.lvx_preference(s["nll"], s["ref"], s["labels"], first, loss, None, one, d_nll, ws)
+            else:
+                B.lvx_policy(s["nll"], s["old"], s["ref"], one, s["labels"], first, loss, None, one, d_nll, ws, beta=0.1)
+            b.record()
+            torch.cuda.synchronize()
+            took.append(a.elapsed_time(b))
+        times[count] = min(took[1:])
+    print(f"[long] {op}: ms {times}", flush=True)
+    assert times[2] <= 4 * times[16384], times
+
+
+@pytest.mark.parametrize("n,S,kind", [((1 << 24) - 1, 2, "any"), (1 << 24, 1, "even"), ((1 << 24) + 777, 3, "gaps"), ((1 << 24) + 1025, 3000, "any")])
+def test_sums_of_long_sequences(n, S, kind):
+    print(f"[long] {n} tokens, {S}, {kind}", flush=True)
+    d = torch.randn(S, generator=torch.Generator().manual_seed(S)).cuda()
+    hd = d.double().cpu().numpy()
+    s = inputs(n, 2 * S, n + S, kind)
+    got = run_pref(s, S, d, beta=0.01)
+    compare(got, *pref_reference(host(s), n, S, hd, "logistic", 0.01, 0.0), "preference")
+    assert all(torch.equal(a, b) for a, b in zip(got, run_pref(s, S, d, beta=0.01))), "not repeatable"
+    s = inputs(n, S, n + S, kind)
+    for mean in (True, False):
+        got = run_policy(s, S, d, beta=0.1, mean=mean)
+        compare(got, *policy_reference(host(s), n, S, hd, 0.2, 0.2, 0.1, mean), "policy")
+        assert all(torch.equal(a, b) for a, b in zip(got, run_policy(s, S, d, beta=0.1, mean=mean))), "not repeatable"
