@@ -56,20 +56,21 @@ __device__ __forceinline__ Span span_of(const SequenceArgs& a, long s) {
   return {b, max(b, e)};
 }
 
-// exp(x) in 64 bits, off by some 1e-14 of itself: 2^k by the exponent, the rest, up to ln 2 / 2, by its series (the last term left out is 6e-15).
+// exp(x) in 64 bits, off by some 1e-14 of itself: 2^k by the exponent, the rest, up to ln 2 / 2, by its series (the first term left out is 6e-15).  The rest is x - k ln 2
+// after Cody and Waite: ln 2 as its first 32 bits, whose product with k is exact, and what is left of it.
 __device__ __forceinline__ double exp_of(double x) {
   x = x < -800.0 ? -800.0 : x > 800.0 ? 800.0 : x;  // (a NaN stays one)
   const double k = rint(x * 1.4426950408889634);
-  double r = fma(k, -0.693147180369123816490, x);    // (ln 2 in two parts, of which the first has zeros at its end)
-  r = fma(k, -1.90821492927058770002e-10, r);
+  double r = fma(k, -0x1.62e42feep-1, x);
+  r = fma(k, -0x1.a39ef35793c76p-33, r);
   double p = 1.0 / 39916800.0;
   const double c[11] = {1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
 #pragma unroll
   for (int i = 0; i < 11; ++i) p = fma(p, r, c[i]);
   return ldexp(p, (int)k);
 }
-// exp(x) - 1 - x, to the last digits for small x too: x^2 times a series up to 1/2 (the last term left out is 2e-17 of the sum).  *less_one: exp(x) - 1, which far out
-// is more than the sum of that and x says: -1 for -infinity.
+// exp(x) - 1 - x, which keeps its digits for small x too: x^2 times a series up to 1/2 (the first term left out is 7e-15 of it).  *less_one: exp(x) - 1, which far
+// out is not the sum of that and x: -1 for -infinity.
 __device__ __forceinline__ double exp_less_line(double x, double* less_one) {
   double p = 1.0 / 6227020800.0;
   const double c[11] = {1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5};
@@ -355,8 +356,12 @@ __global__ void __launch_bounds__(256) policy_finish_kernel(SequenceArgs a) {
   scale_policy(a, j.begin + threadIdx.x, j.end, 256, 1.0 / p.count);
 }
 
+// Up to ONE_TOKENS one launch.  us in one launch and in two, preferences / policies: 32768 tokens in 16 sequences alike 7.9 / 7.7 and 7.5 / 9.1, in 512 4.9 / 4.7 and 7.6 / 7.6,
+// in 2 17 / 22 and 7.8 / 9.1; 65536 in 16 8.3 / 9.4 and 7.7 / 9.4, in 512 5.1 / 5.0 and 7.7 / 7.7, in 2 29 / 40 and 7.9 / 9.2.  One launch has no bound where
+// lengths differ: 32768 tokens in 2048 sequences, of which one has half, 64 / 138 and 15 / 17; 524288 in 512, of which one has half, 104 / 748 and 11 / 13, alike 8.4 / 6.9 and 8.2 / 9.9.
 constexpr long ONE_TOKENS = 32768, LONG_TOKENS = 1L << 24;
-// Threads for a sequence (or pair) of `per` tokens on average
+// Threads for a sequence (or pair) of `per` tokens on average.  us with 64, 256 and 1024, policies of 32768 tokens: per = 16 5.1, 8.9, 36; 64 4.2, 4.7, 10; 256 5.0, 4.8, 5.9; 1024
+// 11, 5.8, 7.1; 2048 20, 8.1, 7.7; 8192 70, 22, 14.
 unsigned threads_for(long per) { return per >= 2048 ? 1024 : per >= 64 ? 256 : 64; }
 // The launch between those of more tokens, where sequences may be long; a piece or more a sequence on average, or so many tokens that one long sequence among
 // short ones would cost more than the launch.  us without and with it, preferences / policies, of 2^24 tokens: two sequences 193 / 220 and 87 / 123, 4096 116 / 146 and
