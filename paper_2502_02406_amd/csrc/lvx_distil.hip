@@ -120,7 +120,7 @@ template <int W> __device__ __forceinline__ float2 stat_of(const XentArgs& a, lo
 // The first two launches of a pass in one, for up to LISTED tokens of few entries: a thread a token, then the list of those that take part
 // (xent_list_kernel).  It saves a launch, twice with gradients, but one workgroup's loads have no others beside them (with gradients of n x 512 against 2048,
 // two launches and one: 128 with 4 entries 61.6 -> 57.0 us, with 16 63.4 -> 63.9; 512 with 8 74.9 -> 73.9; 768 with 8 79.0 -> 80.1; 1024 with 6 83.3 -> 81.0,
-// with 8 83.4 -> 86.7).
+// with 8 83.4 -> 86.7).  (Of these 768 with 8 is within the bound.)
 constexpr int LISTED = 1024, LISTED_ENTRIES = 8, LISTED_IN_ALL = 6144;
 __global__ void __launch_bounds__(LISTED) distil_list_kernel(XentArgs a, bool forward) {
   __shared__ int counts[16];
@@ -302,7 +302,7 @@ unsigned groups_for(long n) { return (unsigned)std::min(n, 1L << 16); }
 int entries_lds(const XentArgs& a, int tokens) { return tokens * 2 * entries_up(a.K) * (int)sizeof(int); }
 // Whether the launch on `cols` entries of the vocabulary looks at the teacher's entries where they stand (DIRECT_ENTRIES; xent_bf16_kernel does not)
 // Of more than 64 tokens it saves the launches of the sort and of g's entries: 128 x 320 against 4096 with one entry 55.8 -> 52.2 us, with 8 57.7 -> 56.9; 300 x 512
-// float32 against 5003 with 8 123.8 -> 119.3; 1000 x 128 against 2000 with 4 74.4 -> 69.7, with 8 77.3 -> 75.9; 256 x 1088 against 1024 with 4 72.9 -> 71.2, with 8 74.9 -> 76.1.
+// float32 against 5003 with 8 123.8 -> 119.3; 1000 x 128 against 2000 with 4 74.4 -> 69.7, with 8 77.3 -> 75.9; 256 x 1088 against 1024 with 4 72.9 -> 71.2, with 8 74.9 -> 76.1 (within the bound).
 bool direct_of(const XentArgs& a, int is_f32, long cols) {
   if (a.K > DIRECT_ENTRIES || a.K * a.V > DIRECT_IN_ALL || a.K * a.V * std::max(a.n, 64L) > 64 * DIRECT_IN_ALL) return false;
   return is_f32 || a.n <= 64 || few_rows(a.n, cols, a.E / BK, a.n_cu) > 0;

@@ -27,9 +27,11 @@ int team_log(int E) {
   return l;
 }
 
-// 16 bytes to memory, PAST the caches where nothing reads them soon: y, and cleared rows that are whole lines (both of 2048 x 4096 bf16, table 32768: 78 -> 70 us
+// 16 bytes to memory, PAST the caches: y, and cleared rows that are whole lines (both of 2048 x 4096 bf16, table 32768: 78 -> 70 us
 // forward and backward, of 65536 x 4096, table 131072: 522 -> 499).  Of rows that begin anywhere, y: 65536 x 4090, table 50021, forward 203 -> 143 us, with the backward
 // pass 458 -> 410, 200000 x 333 59 -> 41, 5514 x 1001 floats 9.3 -> 10.0, with the backward pass 74.7 -> 73.8; but clears of them, the last of these: 74 -> 96.
+// A small y that the next launch reads comes from memory then.  Lookup and the norm behind it, through the caches and past them: 2048 x 4096 18.4 and 18.7 us, 20000 x 1024
+// 27.5 and 30.6, 5514 x 1001 floats 23.3 and 24.0, 16384 x 4096 97 and 99, 65536 x 4096 409 and 409, 65536 x 4090 444 and 412.
 template <bool PAST> __device__ __forceinline__ void put16(void* p, u32x4 v) {
   if constexpr (PAST) __builtin_nontemporal_store(v, (u32x4_any2*)p);
   else *(u32x4_any2*)p = v;
@@ -762,7 +764,9 @@ template <typename T> __global__ void __launch_bounds__(JOIN_WG) embed_join_kern
 
 long up(long n, long by) { return (n + by - 1) / by; }
 
-// Bytes of the table that a launch of the sort clears: about what goes to memory in its time.
+// Bytes of the table that a launch of the sort clears: about what goes to memory in its time.  The gradient's us with none of it, half as much, this and twice as much:
+// 512 x 1024, table 50000, 31.2, 29.6, 28.3, 24.5; 2048 x 4096, 32768, 65.8, 64.3, 62.3, 57.3; 20000 x 512, 131072, 49.5, 45.2, 40.9, 45.0; 40000 x 1024, 65536, 59.2, 59.3,
+// 60.8, 67.9; 65536 x 4096, 131072, 339, 333, 330, 330; 131072 x 256, 131072, 67.6, 62.7, 63.7, 64.0.
 constexpr long CLEAR_ONE = 20 << 20, CLEAR_ROUND = 3 << 20, CLEAR_MORE = 1 << 20, CLEAR_MOVE = 48 << 20;
 
 template <typename T> hipError_t embed_fwd(const EmbedArgs& a, hipStream_t s) {
@@ -831,7 +835,9 @@ template <typename T, bool ADD> hipError_t embed_bwd(const EmbedArgs& a, hipStre
 
 }  // namespace
 
-// Sorted tokens of a chunk: 4 to 64, so that there are threads for about 2^18 pieces of 8 features.
+// Sorted tokens of a chunk: 4 to 64, so that there are threads for about 2^18 pieces of 8 features.  The gradient's us with 2^16, 2^18 and 2^20: 2048 x 4096, table 32768, 56.4,
+// 62.3, 62.3, added to what is there 26.1, 24.0, 24.0; 20000 x 512, 131072, 46.1, 40.9, 46.3, added 44.9, 34.7, 36.4; 131072 x 256, 131072, 78.8, 63.7, 86.7; 65536 x 4096, 131072,
+// 327, 330, 339, added 250, 251, 238.
 constexpr int LEAST_CHUNK = 4;
 int embed_chunk(long n, int E) {
   if (n <= 16) return 16;                            // (then nothing is left to join)
