@@ -85,7 +85,7 @@ template <bool SORT> __global__ void __launch_bounds__(256) distil_prepare_kerne
     float sum = 0.f;
     for (int k = lane; k < K; k += 64) {
       const Entry e = entry_of(a, i, k);
-      sum += e.there ? expf(e.t - top) : 0.f;
+      sum += e.there ? expf(apart(a, e.t, top)) : 0.f;
       if (forward && !any) a.ln_p[i * K + k] = 0.f;
     }
 #pragma unroll
@@ -111,7 +111,7 @@ template <int W> __device__ __forceinline__ float2 stat_of(const XentArgs& a, lo
   for (int o = 1; o < W; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
   for (int k = lane; k < a.K; k += W) {
     const Entry e = entry_of(a, tok, k);
-    sum += e.there ? expf(e.t - top) : 0.f;
+    sum += e.there ? expf(apart(a, e.t, top)) : 0.f;
   }
 #pragma unroll
   for (int o = 1; o < W; o *= 2) sum += __shfl_xor(sum, o);
@@ -145,9 +145,9 @@ __global__ void __launch_bounds__(LISTED) distil_list_kernel(XentArgs a, bool fo
       far |= e[k].there && e[k].id >= a.V;
       if (e[k].there) most = fmaxf(most, e[k].t);
     }
-    sum = top == most || top == -__builtin_inff() ? sum : sum * expf(top - most);
+    sum = top == most || top == -__builtin_inff() ? sum : sum * expf(apart(a, top, most));
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum += e[k].there && (most != -__builtin_inff() || e[k].t != most) ? expf(e[k].t - most) : 0.f;
+    for (int k = 0; k < 8; ++k) sum += e[k].there && (most != -__builtin_inff() || e[k].t != most) ? expf(apart(a, e[k].t, most)) : 0.f;
     top = most;
   }
   const long label = there ? label_of(any, far, a.V) : -1;
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(256) distil_join_kernel(XentArgs a, int n_part
       for (int k = threadIdx.x % 32; k < a.K; k += 32) {
         const Entry e = entry_of(a, tok, k);
         const float z = e.there && e.id < a.V ? a.z_entry[row * a.K + (a.direct ? k : a.rank[row * a.K + k])] : __builtin_nanf("");
-        const float ln_p = z * a.inv_t - lse, ln_q = ln_q_of(e, stat), q = expf(ln_q);
+        const float ln_p = z * a.inv_t - lse, ln_q = ln_q_of(a, e, stat), q = expf(ln_q);
         a.ln_p[(long)tok * a.K + k] = e.there ? ln_p : 0.f;
         loss += !e.there || q == 0.f ? 0.f : q * (ln_q - ln_p);
       }
@@ -277,7 +277,7 @@ template <typename G> __global__ void __launch_bounds__(256) distil_entries_kern
       int2 y = {-1, 0};
       if (k < K) {
         const Entry e = entry_of(a, tok, k);
-        y = {e.there && e.id < a.V ? (int)e.id : -1, __float_as_int(expf(ln_q_of(e, stat)))};
+        y = {e.there && e.id < a.V ? (int)e.id : -1, __float_as_int(expf(ln_q_of(a, e, stat)))};
       }
       known[k] = y;
     }

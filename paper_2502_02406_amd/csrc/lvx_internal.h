@@ -240,7 +240,7 @@ struct XentArgs {
   const void* teacher;  // [n, K] float32, or (teacher_bf16) bf16
   int teacher_bf16;
   float* ln_p;          // [n, K] (forward: written)
-  float2* q_stat;       // [n]: the largest of the teacher's logits / temperature, and the logarithm of their sum of exponentials against it
+  float2* q_stat;       // [n]: the largest of the teacher's logits, and the logarithm of the sum of exponentials of their distances from it / temperature
   int* sorted;          // forward, [n, K]: the ids in order, those that are none behind them
   uint16_t* rank;       // [n, K]: where an entry stands among them
   uint16_t* starts;     // [n, blocks + 1]: how many of them are below 64 b

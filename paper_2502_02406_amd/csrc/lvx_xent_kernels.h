@@ -80,18 +80,19 @@ __device__ inline int dx_parts(int tiles, int pairs, int n_cu, int slots) {
 // 4096 against 32768 56.6 -> 53.1 us, of 2 x 640 against 2560 15.4 -> 12.3, with gradients of 58 x 384 against 5568 47 -> 39): lane i has listed
 // token i (i < count) and what belongs to it.
 struct Own { int count, tok, lab; float2 row; float scale; long label; };      // (label: of token `lane`)
-// Entry k of a teacher's of token i: whether it is there, and its logit by the temperature
+// Entry k of a teacher's of token i: whether it is there, and its logit
 struct Entry { bool there; long id; float t; };
 __device__ __forceinline__ Entry entry_of(const XentArgs& a, long i, int k) {
   Entry e;
   e.id = a.ids[i * a.K + k];
   e.there = e.id >= 0;
-  const float t = a.teacher_bf16 ? __uint_as_float((unsigned)((const uint16_t*)a.teacher)[i * a.K + k] << 16) : ((const float*)a.teacher)[i * a.K + k];
-  e.t = t / a.temperature;
+  e.t = a.teacher_bf16 ? __uint_as_float((unsigned)((const uint16_t*)a.teacher)[i * a.K + k] << 16) : ((const float*)a.teacher)[i * a.K + k];
   return e;
 }
-// stat: of a token's entries, the largest logit by the temperature and the logarithm of the sum of exponentials against it
-__device__ __forceinline__ float ln_q_of(const Entry& e, float2 stat) { return (e.t - stat.x) - stat.y; }
+// A logit's distance from another one by the temperature (of the difference: the type's lowest value, a mask's, by one below 1 would be -infinity)
+__device__ __forceinline__ float apart(const XentArgs& a, float t, float from) { return (t - from) / a.temperature; }
+// stat: of a token's entries, the largest logit and the logarithm of the sum of exponentials against it
+__device__ __forceinline__ float ln_q_of(const XentArgs& a, const Entry& e, float2 stat) { return apart(a, e.t, stat.x) - stat.y; }
 // Whether few tokens' entries (a.own) are looked at where they stand, by every wave and every tile, without launches that prepare them and, for the gradient,
 // write them: with both passes of 10 x 256 against 1024 prepared 41.7 us, 33.8 so with one entry a token, 42.7 and 36.4 with 8; of 64 x 64 against 32768 with 8 51.1 and
 // 48.8, 65536 with 4 58.7 and 52.2, with 8 59.2 and 59.8, 100000 with one 76.8 and 72.2, with 8 78.7 and 88.0, 300000 with one 165.4 and 165.2; of 32 x 64 float32 against
@@ -251,14 +252,14 @@ template <bool KNOWN> __device__ __forceinline__ void subtract_direct(const Xent
 #pragma unroll
     for (int k = 0; k < DIRECT_ENTRIES; ++k) top = e[k].there ? fmaxf(top, e[k].t) : top;
 #pragma unroll
-    for (int k = 0; k < DIRECT_ENTRIES; ++k) sum += e[k].there ? expf(e[k].t - top) : 0.f;
+    for (int k = 0; k < DIRECT_ENTRIES; ++k) sum += e[k].there ? expf(apart(a, e[k].t, top)) : 0.f;
     stat = make_float2(top, logf(sum));
   }
 #pragma unroll
   for (int k = 0; k < DIRECT_ENTRIES; ++k) {
     const int hot = e[k].there && e[k].id >= cw && e[k].id < cw + 32 ? (int)(e[k].id - cw) - 4 * g : -64;
     if (!__any(hot >= -4)) continue;
-    const float q = expf(ln_q_of(e[k], stat));
+    const float q = expf(ln_q_of(a, e[k], stat));
 #pragma unroll
     for (int v = 0; v < 16; ++v) p[v] -= 8 * (v / 4) + v % 4 == hot ? q : 0.f;
   }
