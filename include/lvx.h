@@ -435,7 +435,7 @@ lvx_status lvx_embed_bwd(const lvx_embed* p, lvx_dtype dtype, const void* d_y, c
  *     LVX_PREF_LOGISTIC  loss = (1 - smoothing) ln(1 + exp(-h)) + smoothing ln(1 + exp(h)); a part of weight 0 is 0, for an infinite h too
  *     LVX_PREF_HINGE     loss = max(0, 1 - h), its gradient 0 at h = 1
  *     LVX_PREF_SQUARE    loss = (m - 1 / (2 beta))^2
- * ref may be NULL (0).  loss, margin: device, [S] float32, overwritten (margin: m; may be NULL). */
+ * ref may be NULL (0).  loss, margin: device, [S] float32, overwritten (margin: m; may be NULL); not where d_loss lies (LVX_ERR_STRIDE). */
 typedef enum { LVX_PREF_LOGISTIC = 0, LVX_PREF_HINGE = 1, LVX_PREF_SQUARE = 2 } lvx_pref_form;
 typedef struct {
   int64_t n, S;             /* tokens (up to 2^30), pairs (up to 2^21) */

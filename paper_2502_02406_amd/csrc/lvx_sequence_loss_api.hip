@@ -47,6 +47,9 @@ lvx_status lvx_preference(const lvx_pref* p, const float* nll, const float* ref,
   const lvx_status st = sequence_args(p->n, 2 * p->S, nll, ref, labels, first, loss, d_loss, d_nll, workspace, workspace_bytes, &a);
   if (st != LVX_OK) return st;
   if (!aligned(margin, 4)) return LVX_ERR_STRIDE;
+  // (a pair's d_loss is read by several workgroups, one of which writes its loss and margin)
+  const int64_t len = p->S * 4, d = (int64_t)d_loss;
+  if (d_loss && (rows_meet(d, 1, len, len, (int64_t)loss, len) || (margin && rows_meet(d, 1, len, len, (int64_t)margin, len)))) return LVX_ERR_STRIDE;
   a.margin = margin;
   a.form = p->form; a.beta = p->beta; a.smoothing = p->smoothing;
   return launch_preference(a, (hipStream_t)hip_stream) == hipSuccess ? LVX_OK : LVX_ERR_HIP;
